@@ -282,6 +282,111 @@ int oapl_entropy(const oapl_problem* problem /*host*/, float* token_entropy, flo
 int oapl_batch_stats(const oapl_problem* problem /*host*/, const float* vhat, float* stats, void* ws,
                      size_t ws_bytes, int flags, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * The inference policy's side of the ratio in Eq. 3.  An engine that samples with lagged weights
+ * produces logits, often through an 8-bit LM head; the calls below take ln pi_vllm(y_t|.) from such
+ * logits (logp_inf of oapl_problem), give their gradient for objectives that are stated on logits,
+ * and form the 8-bit products themselves.  They need no workspace and are one launch each.
+ *
+ * device_status: device int32 or NULL.  The caller clears it (0); a call only ever changes it from
+ * OAPL_OK to the error it met.
+ * ------------------------------------------------------------------------------------------ */
+
+/* element types */
+#define OAPL_TYPE_BF16 0
+#define OAPL_TYPE_F16 1
+#define OAPL_TYPE_F32 2
+#define OAPL_TYPE_E4M3 3 /* 8-bit floating point, 3 bits of mantissa, largest value 448 */
+#define OAPL_TYPE_E5M2 4 /* 2 bits of mantissa, largest value 57344 */
+
+/* N rows of V logits; a row's distribution is softmax(scale * logits). */
+typedef struct {
+  const void* logits;     /* [N, V], rows ld elements apart; only the natural alignment of the type */
+  int64_t N;              /* rows                                                                   */
+  int64_t ld;             /* >= V, elements                                                         */
+  int32_t V;              /* vocabulary size, >= 1                                                  */
+  int32_t type;           /* OAPL_TYPE_BF16, _F16 or _F32                                           */
+  const int32_t* targets; /* [N] or NULL; in [0,V) where mask==1                                    */
+  const uint8_t* mask;    /* [N] or NULL (all rows live); rows with mask==0 are not read            */
+  float scale;            /* > 0: 1 / sampling temperature                                          */
+} oapl_logits;
+
+/*
+ * With p = softmax(scale * z) of a row z:
+ *   token_logp    [N] f32 or NULL: ln p[target]                (needs targets)
+ *   token_entropy [N] f32 or NULL: - sum_v p_v ln p_v
+ *   token_lse     [N] f32 or NULL: ln sum_v exp(scale * z_v)
+ *   top_id  [N,K] int32 or NULL, top_logp [N,K] f32 or NULL: the K largest logits (0 <= K <= 32; at
+ *                 least one of the two for K > 0), largest first, equal ones by the lower index,
+ *                 and their ln p.
+ * Rows with mask==0: 0 in every f32 output, -1 in top_id.  A logit of -inf has probability 0 and is no
+ * alternative; where fewer than K are left, top_id is -1 and top_logp -inf.  A row without a finite
+ * logit: token_logp and token_lse -inf, token_entropy 0.  A row with a NaN or +inf logit: NaN in every
+ * f32 output, status OAPL_ERR_NONFINITE_INPUT.  A target outside [0,V) on a live row: token_logp NaN,
+ * status OAPL_ERR_BAD_TARGET.  Results do not depend on the order of execution.
+ */
+int oapl_logits_logprobs(const oapl_logits* logits /*host*/, float* token_logp, float* token_entropy,
+                         float* token_lse, int32_t K, float* top_logp, int32_t* top_id,
+                         int32_t* device_status, void* stream);
+
+/*
+ * Gradient of sum_n ( g_logp token_logp + g_entropy token_entropy + sum_k g_top ln p[top_id] ):
+ *   dlogits_v = scale ( -p_v (G + g_entropy (ln p_v + entropy)) + g_logp [v == target]
+ *                       + sum_k g_top_k [v == top_id_k] ),     G = g_logp + sum_k g_top_k.
+ *   token_lse [N], token_entropy [N] (needed with g_entropy): as the forward left them.
+ *   g_logp [N] or NULL (needs targets); g_entropy [N] or NULL; g_top [N,K] or NULL with top_id [N,K]
+ *   (K = 0 without): any K token ids, not only the forward's; an id may occur twice.  Ids and targets
+ *   outside [0,V) count for nothing (their share of G included).
+ *   dlogits [N,V], the logits' type, rows ld_d elements apart; rows with mask==0 are written as 0.
+ *   It may be the logits' own memory (then ld_d == ld), but must not overlap them otherwise.
+ * ln p_v is scale * z_v - token_lse in fp32, so a common offset c of a row's logits costs about |c| 2^-24 of
+ * a probability.  token_lse below -1e30 (no logit but -inf, or a type's lowest value used as a mask) counts
+ * as p = 0 throughout: only the point terms are left.
+ */
+int oapl_logits_logprobs_bwd(const oapl_logits* logits /*host*/, const float* token_lse,
+                             const float* token_entropy, const float* g_logp, const float* g_entropy,
+                             int32_t K, const float* g_top, const int32_t* top_id, void* dlogits,
+                             int64_t ld_d, void* stream);
+
+/* A matrix of 8-bit floating point: element (i, j) stands for
+ * data[i * ld + j] * scale[(i / block_rows) * scale_row_stride + (j / 128) * scale_col_stride]. */
+typedef struct {
+  void* data;               /* 16-byte aligned                              */
+  float* scale;
+  int64_t rows;
+  int64_t cols;             /* the axis that a product contracts            */
+  int64_t ld;               /* >= cols, multiple of 16                      */
+  int64_t scale_row_stride; /* elements, >= 0; any layout.  Scales of one   */
+  int64_t scale_col_stride; /* column block next to one another load best   */
+  int32_t type;             /* OAPL_TYPE_E4M3 or OAPL_TYPE_E5M2             */
+  int32_t block_rows;       /* 1: a scale per row and 128 columns; 128: per 128 x 128 block */
+} oapl_scaled;
+
+/*
+ * Quantise x [rows, cols] (bf16, f16 or f32; rows ld_x elements apart) into `out`:
+ *   amax = max(largest |x| of the block, 2^-100), scale = amax / top (top: the type's largest value),
+ *   values = x * top / amax, correctly rounded to fp32 and then to the 8-bit type (nearest even).
+ * OAPL_QUANT_POW2: scale = 2^ceil(log2(amax / top)) instead.  OAPL_QUANT_TRANSPOSE: out is x turned,
+ * [cols, rows], with blocks of the turned matrix.  Only rows x cols values are written, never the padding
+ * behind a row.  A NaN makes its block's scale and values NaN, an infinity the scale infinite.
+ */
+#define OAPL_QUANT_TRANSPOSE 1
+#define OAPL_QUANT_POW2 2
+int oapl_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ld_x,
+                  const oapl_scaled* out /*host*/, int flags, void* stream);
+
+/*
+ * C [A.rows, B.rows] = A . B^T, or C += A . B^T when accumulate != 0.  A.cols == B.cols; the types and
+ * block_rows of A and B may differ.  C: bf16, f16 or f32 (c_type), rows ldc elements apart, natural
+ * alignment.  Products of a block of 128 are summed by the tensor cores in fp32, scaled blocks in fp32;
+ * one rounding to c_type at the end (accumulate: of the sum with the old C).  Bitwise reproducible.
+ *   logits = H . W^T:  A = H, B = W (128 x 128 blocks);
+ *   dH = g . W:        A = g, B = W quantised with OAPL_QUANT_TRANSPOSE;
+ *   dW = g^T . H:      A = g, B = H, both with OAPL_QUANT_TRANSPOSE (block_rows 1), accumulate.
+ */
+int oapl_scaled_matmul(const oapl_scaled* A /*host*/, const oapl_scaled* B /*host*/, void* C, int32_t c_type,
+                       int64_t ldc, int accumulate, int32_t* device_status, void* stream);
+
 /* Synchronises `stream` and returns the status word the device recorded in `ws`
  * since the last forward call (OAPL_OK if none). */
 int oapl_get_last_status(void* ws, void* stream);

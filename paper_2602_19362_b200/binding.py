@@ -25,7 +25,8 @@ EXPORTS = ["oapl_workspace_bytes", "oapl_token_logprobs", "oapl_value_estimate",
            "oapl_status_string", "oapl_debug_gemm", "oapl_profile_enable", "oapl_profile_read",
            "oapl_token_logprobs_static", "oapl_loss_fwd_bwd", "oapl_profile_read_clocks", "oapl_entropy", "oapl_group_advantage",
            "oapl_grpo_loss_fwd_bwd", "oapl_adamw_workspace_bytes", "oapl_adamw_step", "oapl_loss_fwd_bwd_ex",
-           "oapl_get_range_count", "oapl_profile_applies", "oapl_range_slots", "oapl_batch_stats"]
+           "oapl_get_range_count", "oapl_profile_applies", "oapl_range_slots", "oapl_batch_stats",
+           "oapl_logits_logprobs", "oapl_logits_logprobs_bwd", "oapl_quantize", "oapl_scaled_matmul"]
 
 
 class OaplProblem(ctypes.Structure):
@@ -40,6 +41,18 @@ class OaplProblem(ctypes.Structure):
 class OaplCallOptions(ctypes.Structure):
     _fields_ = [("live_rows_bound", ctypes.c_int64), ("max_seq_rows_bound", ctypes.c_int32),
                 ("dW_ready_event", ctypes.c_void_p)]
+
+
+class OaplLogits(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("N", ctypes.c_int64), ("ld", ctypes.c_int64), ("V", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("targets", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("scale", ctypes.c_float)]
+
+
+class OaplScaled(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("scale_row_stride", ctypes.c_int64),
+                ("scale_col_stride", ctypes.c_int64), ("type", ctypes.c_int32), ("block_rows", ctypes.c_int32)]
 
 
 class OaplError(RuntimeError):
@@ -106,6 +119,15 @@ def lib() -> ctypes.CDLL:
         L.oapl_adamw_step.argtypes = [vp, vp, vp, vp, vp, i64, i64, f32, f32, f32, f32, f32, f32, vp, vp, vp, sz, vp]
         L.oapl_entropy.restype = i32
         L.oapl_entropy.argtypes = [pp, vp, vp, vp, vp, sz, i32, vp]
+        pl, ps = ctypes.POINTER(OaplLogits), ctypes.POINTER(OaplScaled)
+        L.oapl_logits_logprobs.restype = i32
+        L.oapl_logits_logprobs.argtypes = [pl, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp]
+        L.oapl_logits_logprobs_bwd.restype = i32
+        L.oapl_logits_logprobs_bwd.argtypes = [pl, vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, i64, vp]
+        L.oapl_quantize.restype = i32
+        L.oapl_quantize.argtypes = [vp, ctypes.c_int32, i64, i64, i64, ps, i32, vp]
+        L.oapl_scaled_matmul.restype = i32
+        L.oapl_scaled_matmul.argtypes = [ps, ps, vp, ctypes.c_int32, i64, i32, vp, vp]
         L.oapl_profile_enable.restype = i32
         L.oapl_profile_enable.argtypes = [i32]
         L.oapl_profile_read.restype = i32
@@ -338,3 +360,138 @@ def oapl_loss_fwd_bwd(problem, loss, seq_logp, vhat, delta, token_logp, dH, dW, 
                                  ws.numel(), flags, _stream())
     if rc != OAPL_OK:
         raise OaplError(rc, "oapl_loss_fwd_bwd")
+
+
+# ---- logits in memory, and 8-bit matrices with a scale per block -----------------------------------
+
+OAPL_QUANT_TRANSPOSE, OAPL_QUANT_POW2 = 1, 2
+FLOAT_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+SCALED_TYPES = {torch.float8_e4m3fn: 3, torch.float8_e5m2: 4}
+MAX_TOP = 32
+
+
+def _rows(t, types, name):
+    """Check a [rows, cols] CUDA tensor with contiguous rows; its leading dimension."""
+    if t.dtype not in types or t.dim() != 2 or not t.is_cuda:
+        raise TypeError(f"{name}: expected a 2-D CUDA tensor of one of {[str(x) for x in types]}")
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise TypeError(f"{name}: elements of a row must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vec(t, dtype, shape, device, name):
+    """Address of a contiguous tensor of that type, shape and device; None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise TypeError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the logits' device")
+    return t.data_ptr()
+
+
+def _stream_of(device):
+    """The current stream of `device`, which has to be the current device."""
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def make_logits(logits, targets=None, mask=None, scale: float = 1.0) -> OaplLogits:
+    """Fill oapl_logits.  logits: [N, V] bf16, fp16 or fp32, rows any stride apart; targets: int32 [N];
+    mask: uint8 [N].  The struct keeps the tensors alive."""
+    ld = _rows(logits, FLOAT_TYPES, "logits")
+    N, V = logits.shape
+    dev = logits.get_device()
+    L = OaplLogits(logits.data_ptr(), N, ld, V, FLOAT_TYPES[logits.dtype], _vec(targets, torch.int32, (N,), dev, "targets"),
+                   _vec(mask, torch.uint8, (N,), dev, "mask"), scale)
+    L.tensors = (logits, targets, mask)
+    return L
+
+
+def oapl_logits_logprobs(L, token_logp=None, token_entropy=None, token_lse=None, top_logp=None, top_id=None,
+                         device_status=None):
+    """Log-probability of the targets, entropy, log-sum-exp [N] and the top K alternatives [N, K]; each
+    output may be None.  device_status: int32 [1], zero before the call."""
+    dev, N = L.tensors[0].get_device(), L.N
+    first = top_id if top_id is not None else top_logp
+    K = 0 if first is None else first.shape[-1]
+    f32 = torch.float32
+    rc = lib().oapl_logits_logprobs(
+        L, _vec(token_logp, f32, (N,), dev, "token_logp"), _vec(token_entropy, f32, (N,), dev, "token_entropy"),
+        _vec(token_lse, f32, (N,), dev, "token_lse"), K, _vec(top_logp, f32, (N, K), dev, "top_logp"),
+        _vec(top_id, torch.int32, (N, K), dev, "top_id"), _vec(device_status, torch.int32, (1,), dev, "device_status"),
+        _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_logits_logprobs")
+
+
+def oapl_logits_logprobs_bwd(L, token_lse, token_entropy, g_logp, g_entropy, g_top, top_id, dlogits):
+    """Gradient of the logits from the gradients of token_logp, token_entropy (each [N] or None) and of the
+    log-probabilities of the ids top_id ([N, K] or None).  dlogits may be the logits themselves."""
+    logits = L.tensors[0]
+    dev, N = logits.get_device(), L.N
+    K = 0 if g_top is None else g_top.shape[-1]
+    f32 = torch.float32
+    ld_d = _rows(dlogits, (logits.dtype,), "dlogits")
+    if dlogits.shape != logits.shape or dlogits.get_device() != dev:
+        raise TypeError("dlogits: expected the logits' shape and device")
+    rc = lib().oapl_logits_logprobs_bwd(
+        L, _vec(token_lse, f32, (N,), dev, "token_lse"), _vec(token_entropy, f32, (N,), dev, "token_entropy"),
+        _vec(g_logp, f32, (N,), dev, "g_logp"), _vec(g_entropy, f32, (N,), dev, "g_entropy"), K,
+        _vec(g_top, f32, (N, K), dev, "g_top"), _vec(top_id, torch.int32, (N, K), dev, "top_id") if K else None,
+        dlogits.data_ptr(), ld_d, _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_logits_logprobs_bwd")
+
+
+def make_scaled(data, scale, block_rows: int) -> OaplScaled:
+    """Fill oapl_scaled.  data: [rows, cols] float8_e4m3fn or float8_e5m2, rows a multiple of 16 bytes apart;
+    scale: fp32 [ceil(rows / block_rows), ceil(cols / 128)] of any strides; block_rows 1 or 128.  The struct
+    keeps the tensors alive."""
+    ld = _rows(data, SCALED_TYPES, "data")
+    rows, cols = data.shape
+    if data.shape[0] == 1:
+        ld = -(-ld // 16) * 16      # one row: no second one to find
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows: 1 or 128")
+    if (scale.dtype != torch.float32 or scale.get_device() != data.get_device()
+            or scale.shape != (-(-rows // block_rows), -(-cols // 128))):
+        raise TypeError("scale: expected fp32 [ceil(rows / block_rows), ceil(cols / 128)] on the data's device")
+    m = OaplScaled(data.data_ptr(), scale.data_ptr(), rows, cols, ld, scale.stride(0), scale.stride(1),
+                   SCALED_TYPES[data.dtype], block_rows)
+    m.tensors = (data, scale)
+    return m
+
+
+def alloc_scaled(rows: int, cols: int, block_rows: int, dtype=torch.float8_e4m3fn, device="cuda") -> OaplScaled:
+    """An oapl_scaled with uninitialised memory laid out for the product: padded rows, and the scales of a
+    block of 128 columns next to one another.  Its tensors are `.tensors` = (data, scale)."""
+    data = torch.empty(rows, -(-cols // 16) * 16, dtype=dtype, device=device)[:, :cols]
+    scale = torch.empty(-(-cols // 128), -(-rows // block_rows), dtype=torch.float32, device=device).t()
+    return make_scaled(data, scale, block_rows)
+
+
+def oapl_quantize(x, out: OaplScaled, transpose: bool = False, pow2: bool = False):
+    """Quantise x [rows, cols] (bf16, fp16, fp32) into `out`, turned when transpose is set."""
+    ld = _rows(x, FLOAT_TYPES, "x")
+    dev = x.get_device()
+    if out.tensors[0].get_device() != dev:
+        raise TypeError("out: expected x's device")
+    rc = lib().oapl_quantize(x.data_ptr(), FLOAT_TYPES[x.dtype], x.shape[0], x.shape[1], ld, out,
+                             (OAPL_QUANT_TRANSPOSE if transpose else 0) | (OAPL_QUANT_POW2 if pow2 else 0),
+                             _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_quantize")
+
+
+def oapl_scaled_matmul(A: OaplScaled, B: OaplScaled, C, accumulate: bool = False, device_status=None):
+    """C [A.rows, B.rows] (bf16, fp16, fp32) = A . B^T, or C += A . B^T."""
+    ldc = _rows(C, FLOAT_TYPES, "C")
+    dev = C.get_device()
+    if C.shape != (A.rows, B.rows):
+        raise TypeError(f"C: expected shape {(A.rows, B.rows)}")
+    if A.tensors[0].get_device() != dev or B.tensors[0].get_device() != dev:
+        raise TypeError("A, B: expected C's device")
+    rc = lib().oapl_scaled_matmul(A, B, C.data_ptr(), FLOAT_TYPES[C.dtype], ldc, int(accumulate),
+                                  _vec(device_status, torch.int32, (1,), dev, "device_status"), _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_scaled_matmul")

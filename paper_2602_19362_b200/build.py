@@ -9,6 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liboapl.so")
 SOURCES = ["oapl_api.cu"]
 DEPS = ["oapl_api.cu", "gemm_sm100.cuh", "small_kernels.cuh", "sm100_ptx.cuh", "sweep_schedule.cuh", "adamw.cuh",
+        "logits_ops.cuh", "quantize.cuh", "scaled_matmul.cuh",
         os.path.join("..", "..", "include", "oapl.h")]
 
 

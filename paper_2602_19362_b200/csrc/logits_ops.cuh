@@ -1,0 +1,713 @@
+// Log-probabilities of given tokens, entropy and top alternatives from logits in memory, and the
+// gradient of all of them with respect to the logits.
+//
+// Forward, one pass over a row (z: the row's logits, a: the caller's factor):
+//     x_v = a (z_v - m),  S = sum_v e^x_v,  T = sum_v e^x_v x_v      (m: a reference near the maximum)
+//     lse = a m + ln S,   ln p_t = a z_t - lse,   entropy = ln S - T / S.
+// The entropy is formed from sums relative to m, so a peaked row does not lose it in the difference of
+// two large numbers.  Sums are fp32: a thread adds a few hundred terms, the rest are trees.
+//
+// What bounds it: HBM.  A 16-bit logit has a budget of about eleven lane instructions per SM cycle, the
+// pass takes about six, one of them the exponential (16 per cycle and SM), so the reference m is moved
+// only when a group's maximum exceeds it by 2^8 (no rescaling in the steady state), and the additions and
+// products run two at a time (f32x2).  The top alternatives cost the pass nothing but the group maxima
+// it needs anyway: see top-K below.
+//
+// A row goes to a cluster of 1, 2, 4 or 8 CTAs (few rows: the row is split and joined through
+// distributed shared memory, so a call is always a single launch without a workspace).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "sm100_ptx.cuh"
+
+namespace oapl {
+
+constexpr int kLgThreads = 256;
+constexpr int kLgWarps = kLgThreads / 32;
+constexpr int kLgUnroll = 4;       // 16-byte loads in flight per thread
+constexpr int kLgMaxGroups = 32;   // groups of a thread whose maxima are kept for the top alternatives
+constexpr int kLgMaxTop = 32;
+constexpr int kLgMaxCluster = 8;
+constexpr int kErrBadTarget = -5;  // OAPL_ERR_BAD_TARGET
+constexpr int kErrNonfinite = -7;  // OAPL_ERR_NONFINITE_INPUT
+
+struct LogitsParams {
+  const void* z;
+  int64_t ld;  // elements
+  int32_t V;
+  int32_t N;
+  const int32_t* targets;
+  const uint8_t* mask;
+  float scale;
+  // forward
+  float* token_logp;
+  float* token_entropy;
+  float* token_lse;
+  float* top_logp;
+  int32_t* top_id;
+  int32_t K;
+  int32_t slots;  // rows of group maxima in shared memory: the most groups any CTA forms, and one
+  int32_t* status;
+  // backward
+  const float* lse;
+  const float* entropy;
+  const float* g_logp;
+  const float* g_entropy;
+  const float* g_top;
+  const int32_t* ids;
+  void* dz;
+  int64_t ld_d;
+};
+
+// ------------------------------------------------------------------------------------ small pieces
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint4 ldg_stream(const uint4* p) {
+  uint4 v;
+  asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+      : "l"(p));
+  return v;
+}
+
+// Element type: kN elements per 16 bytes, widening to fp32 (exact), the packed -inf word.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<__nv_bfloat16> {
+  static constexpr int kN = 8;
+  static constexpr uint32_t kNegInf = 0xFF80FF80u;
+  static __device__ __forceinline__ void widen(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ float one(const void* p, int64_t i) {
+    return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
+  }
+  static __device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float pmax_final(uint32_t a) {
+    return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint4 narrow(const float (&f)[8]) {
+    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                      pack_bf16x2(f[6], f[7]));
+  }
+  static __device__ __forceinline__ void put(void* p, int64_t i, float x) {
+    reinterpret_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
+  }
+};
+template <>
+struct Elem<__half> {
+  static constexpr int kN = 8;
+  static constexpr uint32_t kNegInf = 0xFC00FC00u;
+  static __device__ __forceinline__ void widen(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[2 * i] = t.x;
+      f[2 * i + 1] = t.y;
+    }
+  }
+  static __device__ __forceinline__ float one(const void* p, int64_t i) {
+    return __half2float(reinterpret_cast<const __half*>(p)[i]);
+  }
+  static __device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float pmax_final(uint32_t a) {
+    const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&a));
+    return fmaxf(t.x, t.y);
+  }
+  static __device__ __forceinline__ uint32_t pk(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint4 narrow(const float (&f)[8]) {
+    return make_uint4(pk(f[0], f[1]), pk(f[2], f[3]), pk(f[4], f[5]), pk(f[6], f[7]));
+  }
+  static __device__ __forceinline__ void put(void* p, int64_t i, float x) {
+    reinterpret_cast<__half*>(p)[i] = __float2half_rn(x);
+  }
+};
+template <>
+struct Elem<float> {
+  static constexpr int kN = 4;
+  static constexpr uint32_t kNegInf = 0xFF800000u;
+  static __device__ __forceinline__ void widen(const uint4& v, float (&f)[4]) {
+    f[0] = __uint_as_float(v.x);
+    f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z);
+    f[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ float one(const void* p, int64_t i) {
+    return reinterpret_cast<const float*>(p)[i];
+  }
+  static __device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }
+  static __device__ __forceinline__ float pmax_final(uint32_t a) { return __uint_as_float(a); }
+  static __device__ __forceinline__ uint4 narrow(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+  static __device__ __forceinline__ void put(void* p, int64_t i, float x) { reinterpret_cast<float*>(p)[i] = x; }
+};
+
+// Running sums of one thread: x relative to m, in units of log2.
+struct RowSums {
+  float m;       // reference (a logit); -inf: nothing seen yet
+  uint64_t s, t; // two lanes each: sum e^x and sum e^x x
+};
+
+// x below this has e^x = 0 in fp32; also keeps 0 * x finite for logits of -inf.  NaN passes.
+constexpr float kLgFloor = -200.f;
+constexpr float kLgMove = 8.f;  // the reference follows when a maximum exceeds it by 2^8
+
+__device__ __forceinline__ void row_move(RowSums& r, float to, float c) {
+  // e^(x + d) = e^x 2^d, and x e^x becomes (x + d) e^x 2^d
+  if (r.m == -INFINITY) {
+    r.m = to;
+    return;
+  }
+  const float d = max_nan((r.m - to) * c, kLgFloor);
+  const float f = ex2_approx(d);
+  float s0, s1, t0, t1;
+  unpack2(r.s, s0, s1);
+  unpack2(r.t, t0, t1);
+  r.t = pack2(f * fmaf(d, s0, t0), f * fmaf(d, s1, t1));
+  r.s = pack2(f * s0, f * s1);
+  r.m = to;
+}
+
+template <int KN>
+__device__ __forceinline__ void row_add(RowSums& r, const float (&f)[KN], float negm, float c) {
+  const uint64_t nm = pack2(negm, negm), cc = pack2(c, c);
+#pragma unroll
+  for (int i = 0; i < KN; i += 2) {
+    const uint64_t x2 = mul2(add2(pack2(f[i], f[i + 1]), nm), cc);
+    float x0, x1;
+    unpack2(x2, x0, x1);
+    x0 = max_nan(x0, kLgFloor);
+    x1 = max_nan(x1, kLgFloor);
+    const uint64_t e2 = pack2(ex2_approx(x0), ex2_approx(x1));
+    r.s = add2(r.s, e2);
+    r.t = fma2(e2, pack2(x0, x1), r.t);
+  }
+}
+
+struct RowTotal {
+  float m, s, t;
+};
+__device__ __forceinline__ RowTotal row_join(const RowTotal& a, const RowTotal& b, float c) {
+  RowTotal o;
+  o.m = fmaxf(a.m, b.m);
+  if (o.m == -INFINITY) {
+    o.s = a.s + b.s;  // zeros, or a NaN that has to stay
+    o.t = 0.f;
+    return o;
+  }
+  const float da = max_nan((a.m - o.m) * c, kLgFloor), db = max_nan((b.m - o.m) * c, kLgFloor);
+  const float fa = ex2_approx(da), fb = ex2_approx(db);
+  o.s = fa * a.s + fb * b.s;
+  o.t = fa * fmaf(da, a.s, a.t) + fb * fmaf(db, b.s, b.t);
+  return o;
+}
+
+// Order of the alternatives: larger logit first, then the lower index.  0 = no entry.
+__device__ __forceinline__ uint64_t top_key(float v, uint32_t idx) {
+  const uint32_t u = __float_as_uint(v + 0.f);  // -0 counts as +0
+  const uint32_t o = u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
+  return (uint64_t(o) << 32) | (0xFFFFFFFFu - idx);
+}
+__device__ __forceinline__ float top_value(uint64_t key) {
+  const uint32_t o = uint32_t(key >> 32);
+  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+}
+
+// A warp's best entries, lane i the i-th best: insert `key` (uniform over the warp).
+__device__ __forceinline__ void top_insert(uint64_t& mine, uint64_t key, int lane) {
+  const uint32_t better = __ballot_sync(0xffffffffu, mine > key);
+  const int pos = __popc(better);  // the list is sorted, so `better` is a prefix
+  const uint64_t up = __shfl_up_sync(0xffffffffu, mine, 1);
+  if (lane == pos) mine = key;
+  if (lane > pos) mine = up;
+}
+
+// out[rank] = the K best of entries[0..M); keys are distinct apart from empty ones.  All threads.
+__device__ __forceinline__ void top_rank(const uint64_t* entries, int M, int K, uint64_t* out) {
+  for (int i = threadIdx.x; i < M; i += kLgThreads) {
+    const uint64_t k = entries[i];
+    if (k == 0) continue;
+    int r = 0;
+    for (int j = 0; j < M; ++j) r += entries[j] > k;
+    if (r < K) out[r] = k;
+  }
+}
+
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void st_cluster_u64(uint32_t addr, uint64_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+
+// ------------------------------------------------------------------------------------ forward
+// Top K: a thread's logits form up to 32 groups, whose maxima the pass writes to shared memory (a
+// store per 32 logits).  With j = ceil(K / 8), every one of the eight warps holds j threads whose
+// maximum is at least its own j-th largest thread maximum; the smallest of these over the warps, thr,
+// therefore has at least K logits at or above it.  Only groups whose maximum reaches thr can hold an
+// alternative: a few dozen of a few thousand.  They are read once more (a warp takes 32 at a time, one
+// per lane), and their entries at or above thr go through a list kept sorted over the warp's lanes.
+// The lists are joined by counting ranks.  Order and ties are decided by distinct keys, so the result
+// does not depend on the order of work.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsParams p) {
+  using E = Elem<T>;
+  constexpr int kN = E::kN;
+  extern __shared__ float gmax[];  // TOP: [groups + 1][kLgThreads], then the warps' queues
+  __shared__ RowTotal sh_tot[kLgWarps];
+  __shared__ RowTotal sh_cl[kLgMaxCluster];
+  __shared__ uint64_t sh_list[kLgWarps * kLgMaxTop];
+  __shared__ uint64_t sh_cl_list[kLgMaxCluster * kLgMaxTop];
+  __shared__ uint64_t sh_best[kLgMaxTop];
+  __shared__ uint32_t sh_thr[kLgWarps];
+  __shared__ int sh_count;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint32_t nc, rank;
+  asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(nc));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int64_t row = blockIdx.x / nc;
+  const int K = p.K;
+
+  if (p.mask && p.mask[row] == 0) {
+    if (rank == 0) {
+      if (tid == 0) {
+        if (p.token_logp) p.token_logp[row] = 0.f;
+        if (p.token_entropy) p.token_entropy[row] = 0.f;
+        if (p.token_lse) p.token_lse[row] = 0.f;
+      }
+      if (TOP && tid < K) {
+        if (p.top_logp) p.top_logp[row * K + tid] = 0.f;
+        if (p.top_id) p.top_id[row * K + tid] = -1;
+      }
+    }
+    return;  // every CTA of the cluster alike
+  }
+  // The other CTAs' shared memory may be written once they run: this barrier's first half here, its
+  // second before the join.
+  if (nc > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+
+  const float c = p.scale * 1.4426950408889634f;
+  const T* zrow = reinterpret_cast<const T*>(p.z) + row * p.ld;
+  float z_target = 0.f;
+  int target = -1;
+  bool bad_target = false;
+  if (rank == 0 && tid == 0 && p.token_logp) {
+    target = p.targets[row];
+    bad_target = target < 0 || target >= p.V;
+    if (!bad_target) z_target = E::one(zrow, target);
+  }
+
+  // the row as nh single elements, nv 16-byte vectors, and the rest
+  const int V = p.V;
+  int nh = int(((16u - (uint32_t(reinterpret_cast<uintptr_t>(zrow)) & 15u)) & 15u) / sizeof(T));
+  if (nh > V) nh = V;
+  const int nv = (V - nh) / kN;
+  const int nsingle = V - nv * kN;  // head and tail elements: the last CTA takes them
+  const uint4* zv = reinterpret_cast<const uint4*>(zrow + nh);
+  const int v0 = int(int64_t(nv) * rank / nc), v1 = int(int64_t(nv) * (rank + 1) / nc);
+  const int nb = (v1 - v0 + kLgThreads * kLgUnroll - 1) / (kLgThreads * kLgUnroll);
+  const int per = (nb + kLgMaxGroups - 1) / kLgMaxGroups;  // batches per group
+
+  RowSums r;
+  r.m = -INFINITY;
+  r.s = r.t = pack2(0.f, 0.f);
+  float tmax = -INFINITY, gm = -INFINITY;
+  int g = 0, in_group = 0;
+
+  uint4 cur[kLgUnroll], nxt[kLgUnroll];
+  auto load = [&](int b, uint4 (&v)[kLgUnroll]) {
+#pragma unroll
+    for (int u = 0; u < kLgUnroll; ++u) {
+      const int i = v0 + (b * kLgUnroll + u) * kLgThreads + tid;
+      v[u] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
+      if (i < v1) v[u] = ldg_stream(zv + i);
+    }
+  };
+  if (nb > 0) load(0, cur);
+  for (int b = 0; b < nb; ++b) {
+    if (b + 1 < nb) load(b + 1, nxt);
+    uint32_t pm = E::kNegInf;
+#pragma unroll
+    for (int u = 0; u < kLgUnroll; ++u)
+      pm = E::pmax(pm, E::pmax(E::pmax(cur[u].x, cur[u].y), E::pmax(cur[u].z, cur[u].w)));
+    const float bm = E::pmax_final(pm);
+    if (TOP) {
+      gm = fmaxf(gm, bm);
+      if (++in_group == per) {
+        gmax[g * kLgThreads + tid] = gm;
+        tmax = fmaxf(tmax, gm);
+        gm = -INFINITY;
+        in_group = 0;
+        ++g;
+      }
+    }
+    if ((bm - r.m) * c > kLgMove || r.m == -INFINITY) row_move(r, bm, c);
+    const float negm = r.m == -INFINITY ? 0.f : -r.m;
+#pragma unroll
+    for (int u = 0; u < kLgUnroll; ++u) {
+      float f[kN];
+      E::widen(cur[u], f);
+      row_add<kN>(r, f, negm, c);
+    }
+#pragma unroll
+    for (int u = 0; u < kLgUnroll; ++u) cur[u] = nxt[u];
+  }
+  if (TOP && in_group) {
+    gmax[g * kLgThreads + tid] = gm;
+    tmax = fmaxf(tmax, gm);
+    ++g;
+  }
+  float zs = -INFINITY;  // this thread's single element
+  int single = -1;
+  if (rank == nc - 1 && tid < nsingle) {
+    single = tid < nh ? tid : nv * kN + tid;
+    zs = E::one(zrow, single);
+    if ((zs - r.m) * c > kLgMove || r.m == -INFINITY) row_move(r, zs, c);
+    const float f[2] = {zs, -INFINITY};
+    row_add<2>(r, f, r.m == -INFINITY ? 0.f : -r.m, c);
+  }
+
+  // ---- join the sums: lanes, warps
+  RowTotal tot;
+  {
+    float s0, s1, t0, t1;
+    unpack2(r.s, s0, s1);
+    unpack2(r.t, t0, t1);
+    tot.m = r.m;
+    tot.s = s0 + s1;
+    tot.t = t0 + t1;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    RowTotal other;
+    other.m = __shfl_xor_sync(0xffffffffu, tot.m, o);
+    other.s = __shfl_xor_sync(0xffffffffu, tot.s, o);
+    other.t = __shfl_xor_sync(0xffffffffu, tot.t, o);
+    // both partners form the same sum in the same order
+    tot = (lane & o) ? row_join(other, tot, c) : row_join(tot, other, c);
+  }
+  if (lane == 0) sh_tot[warp] = tot;
+
+  // ---- top alternatives of this CTA's part
+  if (TOP) {
+    gmax[g * kLgThreads + tid] = zs;
+    float left = fmaxf(tmax, zs);
+    const int j = (K + kLgWarps - 1) / kLgWarps;
+    uint32_t jth = 0;
+    for (int q = 0; q < j; ++q) {
+      const uint32_t o = uint32_t(top_key(left, 0) >> 32);
+      jth = __reduce_max_sync(0xffffffffu, o);
+      const uint32_t who = __ballot_sync(0xffffffffu, o == jth);
+      if (lane == __ffs(who) - 1) left = -INFINITY;
+    }
+    if (lane == 0) sh_thr[warp] = jth;
+    if (tid == 0) sh_count = 0;
+    if (tid < kLgMaxTop) sh_best[tid] = 0;
+    __syncthreads();
+    uint32_t thr = sh_thr[0];
+#pragma unroll
+    for (int w = 1; w < kLgWarps; ++w) thr = min(thr, sh_thr[w]);
+    const uint32_t none = uint32_t(top_key(-INFINITY, 0) >> 32);  // -inf is no alternative
+    uint16_t* queue = reinterpret_cast<uint16_t*>(gmax + p.slots * kLgThreads) + warp * p.slots * 32;
+    int nq = 0;
+    for (int q = 0; q <= g; ++q) {
+      const uint32_t o = uint32_t(top_key(gmax[q * kLgThreads + tid], 0) >> 32);
+      const bool in = o >= thr && o > none;
+      const uint32_t b = __ballot_sync(0xffffffffu, in);
+      if (in) queue[nq + __popc(b & ((1u << lane) - 1u))] = uint16_t(q * 32 + lane);
+      nq += __popc(b);
+    }
+    __syncwarp();
+    uint64_t mine = 0;  // lane i: the warp's i-th best entry so far
+    for (int q0 = 0; q0 < nq; q0 += 32) {
+      uint64_t kth = __shfl_sync(0xffffffffu, mine, K - 1);
+      const int item = q0 + lane < nq ? queue[q0 + lane] : -1;
+      const int ig = item >> 5, it = (item & 31) + warp * 32;
+      bool act = item >= 0;
+      const bool is_single = act && ig == g;
+      const int first = act && !is_single ? v0 + ig * per * kLgUnroll * kLgThreads + it : 0;
+      // nothing in the group can enter when its maximum at its lowest index would not
+      if (act && !is_single)
+        act = top_key(gmax[ig * kLgThreads + it], uint32_t(nh + first * kN)) > kth;
+      if (!__any_sync(0xffffffffu, act)) continue;
+      // the single elements: one entry per thread
+      {
+        const int tsingle = it < nh ? it : nv * kN + it;
+        const float v = is_single ? gmax[g * kLgThreads + it] : -INFINITY;
+        const uint64_t key = top_key(v, uint32_t(tsingle));
+        uint32_t b = __ballot_sync(0xffffffffu, is_single && uint32_t(key >> 32) >= thr && v > -INFINITY && key > kth);
+        while (b) {
+          const int src = __ffs(b) - 1;
+          b &= b - 1;
+          top_insert(mine, __shfl_sync(0xffffffffu, key, src), lane);
+        }
+        kth = __shfl_sync(0xffffffffu, mine, K - 1);
+      }
+      act = act && !is_single;
+      for (int u = 0; u < per * kLgUnroll; u += kLgUnroll) {
+        uint4 v[kLgUnroll];
+#pragma unroll
+        for (int w = 0; w < kLgUnroll; ++w) {
+          const int i = first + (u + w) * kLgThreads;
+          v[w] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
+          if (act && i < v1) v[w] = ldg_stream(zv + i);
+        }
+#pragma unroll
+        for (int w = 0; w < kLgUnroll; ++w) {
+          const float vm = E::pmax_final(E::pmax(E::pmax(v[w].x, v[w].y), E::pmax(v[w].z, v[w].w)));
+          const uint32_t om = uint32_t(top_key(vm, 0) >> 32);
+          if (!__any_sync(0xffffffffu, om >= thr && om > none)) continue;
+          float f[kN];
+          E::widen(v[w], f);
+          const uint32_t i0 = uint32_t(nh + (first + (u + w) * kLgThreads) * kN);
+#pragma unroll
+          for (int e = 0; e < kN; ++e) {
+            const uint64_t key = top_key(f[e], i0 + e);
+            uint32_t b = __ballot_sync(0xffffffffu, uint32_t(key >> 32) >= thr && f[e] > -INFINITY && key > kth);
+            if (b) {
+              do {
+                const int src = __ffs(b) - 1;
+                b &= b - 1;
+                top_insert(mine, __shfl_sync(0xffffffffu, key, src), lane);
+              } while (b);
+              kth = __shfl_sync(0xffffffffu, mine, K - 1);
+            }
+          }
+        }
+      }
+    }
+    // the warps' lists one behind the other; their order does not matter
+    const int have = __popc(__ballot_sync(0xffffffffu, lane < K && mine != 0));
+    int to = 0;
+    if (lane == 0 && have) to = atomicAdd(&sh_count, have);
+    to = __shfl_sync(0xffffffffu, to, 0);
+    if (lane < have) sh_list[to + lane] = mine;
+  }
+  __syncthreads();
+  if (TOP) {
+    top_rank(sh_list, sh_count, K, sh_best);
+    __syncthreads();
+  }
+  tot = sh_tot[0];
+#pragma unroll
+  for (int w = 1; w < kLgWarps; ++w) tot = row_join(tot, sh_tot[w], c);
+
+  // ---- join the CTAs of the row in CTA 0
+  if (nc > 1) {
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (tid == 0) {
+      const uint32_t to = mapa_shared(smem_u32(&sh_cl[rank]), 0);
+      st_cluster_u32(to, __float_as_uint(tot.m));
+      st_cluster_u32(to + 4, __float_as_uint(tot.s));
+      st_cluster_u32(to + 8, __float_as_uint(tot.t));
+    }
+    if (TOP && tid < K) st_cluster_u64(mapa_shared(smem_u32(&sh_cl_list[rank * K + tid]), 0), sh_best[tid]);
+    cluster_sync_all();
+    if (rank != 0) return;
+    tot = sh_cl[0];
+    for (uint32_t q = 1; q < nc; ++q) tot = row_join(tot, sh_cl[q], c);
+    if (TOP) {
+      if (tid < kLgMaxTop) sh_best[tid] = 0;
+      __syncthreads();
+      top_rank(sh_cl_list, int(nc) * K, K, sh_best);
+      __syncthreads();
+    }
+  }
+
+  // ---- results
+  // no finite logit: every probability is 0, lse = -inf, nothing to choose from
+  const bool empty = tot.m == -INFINITY && tot.s == 0.f;
+  const bool broken = !empty && !(tot.m > -INFINITY && tot.m < INFINITY && tot.s > 0.f && tot.s < INFINITY);
+  const float nan = __int_as_float(0x7FC00000);
+  const float ln_s = logf(tot.s);
+  const float lse = broken ? nan : (empty ? -INFINITY : fmaf(p.scale, tot.m, ln_s));
+  if (tid == 0) {
+    if (p.token_lse) p.token_lse[row] = lse;
+    if (p.token_entropy)
+      p.token_entropy[row] = broken ? nan : (empty ? 0.f : fmaxf(0.f, ln_s - 0.6931471805599453f * (tot.t / tot.s)));
+    if (p.token_logp) {
+      // relative to the reference, so that a large common offset does not cost digits
+      const float lp = bad_target || broken ? nan : (empty ? -INFINITY : p.scale * (z_target - tot.m) - ln_s);
+      p.token_logp[row] = lp;
+    }
+    if (p.status && (bad_target || broken)) atomicCAS(p.status, 0, bad_target ? kErrBadTarget : kErrNonfinite);
+  }
+  if (TOP && tid < K) {
+    const uint64_t key = sh_best[tid];
+    if (p.top_id) p.top_id[row * K + tid] = key ? int32_t(0xFFFFFFFFu - uint32_t(key)) : -1;
+    if (p.top_logp)
+      p.top_logp[row * K + tid] = broken ? nan : (key ? p.scale * (top_value(key) - tot.m) - ln_s : -INFINITY);
+  }
+}
+
+// ------------------------------------------------------------------------------------ backward
+// dz_v = a ( -p_v (G + g_H (ln p_v + H)) + g_lp [v = t] + sum_k g_k [v = id_k] ),  G = g_lp + sum_k g_k,
+// p_v = e^(a z_v - lse).  One read and one write per logit, HBM-bound; dz may be the logits themselves.
+// A CTA takes kLgSpan logits of a row; the few entries with a point term are written again after the
+// CTA's stores, from logits read before them.
+constexpr int kLgSpanVecs = kLgThreads * kLgUnroll;
+
+struct RowGrad {
+  float scale, lse, G, ge, H;
+};
+__device__ __forceinline__ float grad_smooth(float z, const RowGrad& r) {
+  const float lp = fmaf(z, r.scale, -r.lse);
+  const float pr = ex2_approx(lp * 1.4426950408889634f);
+  // p = 0: nothing flows, whatever ln p is (0 * inf must not turn into NaN)
+  const float w = fmaf(r.ge, lp + r.H, r.G);
+  const float v = -r.scale * (pr * w);
+  return pr == 0.f ? 0.f : v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLgThreads, 4) logits_bwd_kernel(const LogitsParams p, int spans) {
+  using E = Elem<T>;
+  constexpr int kN = E::kN;
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x / spans;
+  const int span = blockIdx.x % spans;
+  const int V = p.V, K = p.K;
+  const T* zrow = reinterpret_cast<const T*>(p.z) + row * p.ld;
+  T* drow = reinterpret_cast<T*>(p.dz) + row * p.ld_d;
+
+  const uint32_t az = uint32_t(reinterpret_cast<uintptr_t>(zrow)) & 15u;
+  const uint32_t ad = uint32_t(reinterpret_cast<uintptr_t>(drow)) & 15u;
+  int nh = int(((16u - ad) & 15u) / sizeof(T));
+  if (nh > V) nh = V;
+  const int nv = (V - nh) / kN;
+  const int nsingle = V - nv * kN;
+  const bool together = az == ad;  // loads and stores share the vector boundaries
+  const bool live = !p.mask || p.mask[row] != 0;
+  const int w0 = span * kLgSpanVecs;
+  const int w1 = min(nv, w0 + kLgSpanVecs);
+
+  if (!live) {
+    for (int i = w0 + tid; i < w1; i += kLgThreads)
+      *reinterpret_cast<uint4*>(drow + nh + int64_t(i) * kN) = make_uint4(0, 0, 0, 0);
+    if (span == 0 && tid < nsingle) E::put(drow, tid < nh ? tid : nv * kN + tid, 0.f);
+    return;
+  }
+
+  RowGrad r;
+  r.scale = p.scale;
+  r.lse = p.lse[row];
+  r.ge = p.g_entropy ? p.g_entropy[row] : 0.f;
+  r.H = p.g_entropy ? p.entropy[row] : 0.f;
+  const int target = p.g_logp ? p.targets[row] : -1;
+  r.G = target >= 0 && target < V ? p.g_logp[row] : 0.f;  // indexes outside [0, V) count for nothing
+  // a row without a finite logit, or with nothing but a type's lowest value as a mask: every p is 0
+  if (r.lse < -1e30f) r.lse = INFINITY;
+  if (p.g_top)
+    for (int k = 0; k < K; ++k) {
+      const int id = p.ids[row * K + k];
+      r.G += id >= 0 && id < V ? p.g_top[row * K + k] : 0.f;
+    }
+
+  // the entries with a point term: thread 0 the target, thread 1 + k alternative k
+  int at = -1;
+  float point = 0.f, z_at = 0.f;
+  if (tid == 0) at = target;
+  if (tid >= 1 && tid <= K && p.g_top) at = p.ids[row * K + tid - 1];
+  if (at >= V) at = -1;
+  if (at >= 0) {
+    // owned by the CTA that stores it
+    const int vec = (at - nh) / kN;
+    const bool is_single = at < nh || at >= nh + nv * kN;
+    if (is_single ? span != 0 : (vec < w0 || vec >= w1)) at = -1;
+  }
+  if (at >= 0) {
+    z_at = E::one(zrow, at);
+    // every term at this entry, so that equal indexes write the same value
+    if (target == at) point += p.g_logp[row];
+    if (p.g_top)
+      for (int k = 0; k < K; ++k)
+        if (p.ids[row * K + k] == at) point += p.g_top[row * K + k];
+  }
+  const bool any_point = __syncthreads_or(at >= 0);
+
+  uint4 v[kLgUnroll];
+  if (together) {
+#pragma unroll
+    for (int u = 0; u < kLgUnroll; ++u) {
+      const int i = w0 + u * kLgThreads + tid;
+      if (i < w1) v[u] = *(reinterpret_cast<const uint4*>(zrow + nh) + i);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kLgUnroll; ++u) {
+    const int i = w0 + u * kLgThreads + tid;
+    if (i < w1) {
+      float f[kN];
+      if (together) {
+        E::widen(v[u], f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) f[e] = E::one(zrow, nh + int64_t(i) * kN + e);
+      }
+#pragma unroll
+      for (int e = 0; e < kN; ++e) f[e] = grad_smooth(f[e], r);
+      *reinterpret_cast<uint4*>(drow + nh + int64_t(i) * kN) = E::narrow(f);
+    }
+  }
+  if (span == 0 && tid < nsingle) {
+    const int i = tid < nh ? tid : nv * kN + tid;
+    E::put(drow, i, grad_smooth(E::one(zrow, i), r));
+  }
+  if (any_point) {
+    __syncthreads();
+    if (at >= 0) E::put(drow, at, fmaf(r.scale, point, grad_smooth(z_at, r)));
+  }
+}
+
+}  // namespace oapl

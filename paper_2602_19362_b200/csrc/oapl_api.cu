@@ -14,6 +14,9 @@
 #include "../../include/oapl.h"
 #include "adamw.cuh"
 #include "gemm_sm100.cuh"
+#include "logits_ops.cuh"
+#include "quantize.cuh"
+#include "scaled_matmul.cuh"
 #include "small_kernels.cuh"
 
 namespace oapl {
@@ -191,6 +194,20 @@ static bool make_map_f32(CUtensorMap* m, const void* base, uint64_t rows, uint64
   const cuuint32_t box[2] = {32, 128};
   const cuuint32_t estr[2] = {1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Matrix of 8-bit values [rows, cols], leading dimension ld bytes, seen through 128 x 128 boxes (128-byte
+// rows, 128-byte swizzle): an operand half of the block-scaled product.  What lies outside reads as 0.
+static bool make_map_u8(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t ld) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {ld};
+  const cuuint32_t box[2] = {128, 128};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -606,6 +623,141 @@ static int staged_fwd_bwd(const oapl_problem* p, const Objective& ob, float* los
     loss_kernel<<<1, 256, 0, st>>>(p->reward, p->group_id, ob.vhat, seq_D, p->S, p->P, p->beta_loss,
                                    p->loss_scale, coef, ob.delta, loss, state);
   }
+  CKL();
+  return OAPL_OK;
+}
+
+// ---------------------------------------------------------------------------------------
+// Logits in memory: log-probabilities, entropy, top alternatives, and their gradient.
+static int logits_type_size(int32_t type) {
+  return type == OAPL_TYPE_BF16 || type == OAPL_TYPE_F16 ? 2 : (type == OAPL_TYPE_F32 ? 4 : 0);
+}
+
+static int check_logits(const oapl_logits* L) {
+  if (!L || !L->logits || L->N <= 0 || L->V <= 0 || L->ld < L->V) return OAPL_ERR_INVALID_ARG;
+  const int es = logits_type_size(L->type);
+  if (!es) return OAPL_ERR_INVALID_ARG;
+  if (!(L->scale > 0.f) || !std::isfinite(L->scale)) return OAPL_ERR_INVALID_ARG;
+  if ((uintptr_t)L->logits % es) return OAPL_ERR_MISALIGNED;
+  if (L->N > (int64_t)2000000000 || (int64_t)L->V > (int64_t)2000000000) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  return OAPL_OK;
+}
+
+static LogitsParams logits_params(const oapl_logits* L) {
+  LogitsParams lp;
+  memset(&lp, 0, sizeof(lp));
+  lp.z = L->logits;
+  lp.ld = L->ld;
+  lp.V = L->V;
+  lp.N = (int32_t)L->N;
+  lp.targets = L->targets;
+  lp.mask = L->mask;
+  lp.scale = L->scale;
+  return lp;
+}
+
+template <typename T, bool TOP>
+static int launch_logits_fwd(LogitsParams lp, cudaStream_t st) {
+  const int n_sm = sm_count();
+  int dev = -1;
+  if (n_sm <= 0 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return OAPL_ERR_CUDA;
+  // CTAs of a row: split it while the split rows still fit the SMs twice and every thread keeps a load
+  const int nv = lp.V / Elem<T>::kN;
+  int nc = 1;
+  while (nc < kLgMaxCluster && (int64_t)lp.N * nc * 2 <= 2 * n_sm && nv / (nc * 2) >= kLgThreads) nc *= 2;
+  if ((int64_t)lp.N * nc > (int64_t)2147483647) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  size_t smem = 0;
+  if (TOP) {
+    const int span = kLgThreads * kLgUnroll;
+    const int nb = (nv / nc + 1 + span - 1) / span;  // the largest part of a row has one vector more
+    const int per = (nb + kLgMaxGroups - 1) / kLgMaxGroups;
+    lp.slots = (nb + per - 1) / per + 1;
+    smem = (size_t)lp.slots * (kLgThreads * 4 + kLgWarps * 32 * 2);
+  }
+  auto kern = logits_fwd_kernel<T, TOP>;
+  static bool attr_set[kMaxDevices] = {false};
+  if (TOP && !attr_set[dev]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (kLgMaxGroups + 1) * (kLgThreads * 4 + kLgWarps * 32 * 2)) != cudaSuccess)
+      return OAPL_ERR_CUDA;
+    attr_set[dev] = true;
+  }
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)(lp.N * (int64_t)nc));
+  cfg.blockDim = dim3(kLgThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = (unsigned)nc;
+  at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kern, lp) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return OAPL_ERR_CUDA;
+  }
+  OAPL_LAUNCHED();
+  return OAPL_OK;
+}
+
+template <typename T>
+static int launch_logits_bwd(const LogitsParams& lp, cudaStream_t st) {
+  const int64_t spans = ((int64_t)lp.V / Elem<T>::kN + kLgSpanVecs) / kLgSpanVecs;
+  if (spans * lp.N > (int64_t)2147483647) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  logits_bwd_kernel<T><<<(unsigned)(spans * lp.N), kLgThreads, 0, st>>>(lp, (int)spans);
+  CKL();
+  return OAPL_OK;
+}
+
+// ---------------------------------------------------------------------------------------
+// 8-bit floating point with a scale per block of 128: quantisation and product.
+static int check_scaled(const oapl_scaled* m) {
+  if (!m || !m->data || !m->scale || m->rows <= 0 || m->cols <= 0 || m->ld < m->cols) return OAPL_ERR_INVALID_ARG;
+  if (m->type != OAPL_TYPE_E4M3 && m->type != OAPL_TYPE_E5M2) return OAPL_ERR_INVALID_ARG;
+  if (m->block_rows != 1 && m->block_rows != 128) return OAPL_ERR_INVALID_ARG;
+  if (m->scale_row_stride < 0 || m->scale_col_stride < 0) return OAPL_ERR_INVALID_ARG;
+  if (((uintptr_t)m->data | (uintptr_t)m->ld) & 15) return OAPL_ERR_MISALIGNED;
+  if ((uintptr_t)m->scale & 3) return OAPL_ERR_MISALIGNED;
+  if (m->rows > (int64_t)2000000000 || m->cols > (int64_t)2000000000) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  return OAPL_OK;
+}
+
+template <typename T>
+static int launch_quantize(const QuantParams& qp, bool e5, bool block, bool turn, cudaStream_t st) {
+  const int64_t grid = (((int64_t)qp.R + 127) / 128) * (((int64_t)qp.C + 127) / 128);
+  if (grid > (int64_t)2147483647) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  const int pick = (e5 ? 4 : 0) | (block ? 2 : 0) | (turn ? 1 : 0);
+  void (*kern)(QuantParams) = nullptr;
+  switch (pick) {
+    case 0: kern = quantize_kernel<T, 0, false, false>; break;
+    case 1: kern = quantize_kernel<T, 0, false, true>; break;
+    case 2: kern = quantize_kernel<T, 0, true, false>; break;
+    case 3: kern = quantize_kernel<T, 0, true, true>; break;
+    case 4: kern = quantize_kernel<T, 1, false, false>; break;
+    case 5: kern = quantize_kernel<T, 1, false, true>; break;
+    case 6: kern = quantize_kernel<T, 1, true, false>; break;
+    default: kern = quantize_kernel<T, 1, true, true>; break;
+  }
+  kern<<<(unsigned)grid, kQtThreads, 0, st>>>(qp);
+  CKL();
+  return OAPL_OK;
+}
+
+template <int OUT, bool PERCOL>
+static int launch_scaled_matmul(const CUtensorMap& a, const CUtensorMap& b, const ScaledParams& sp, int grid,
+                                cudaStream_t st) {
+  static bool attr_set[kMaxDevices] = {false};
+  auto kern = scaled_matmul_kernel<OUT, PERCOL>;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return OAPL_ERR_CUDA;
+  if (!attr_set[dev]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmSmemBytes) != cudaSuccess)
+      return OAPL_ERR_CUDA;
+    attr_set[dev] = true;
+  }
+  kern<<<grid, kSmThreads, kSmSmemBytes, st>>>(a, b, sp);
   CKL();
   return OAPL_OK;
 }
@@ -1154,6 +1306,139 @@ int oapl_token_logprobs_static(const oapl_problem* p, float* token_logp, float* 
     CK(cudaMemcpyAsync(device_status, &reinterpret_cast<DevState*>(base + c.state)->status, sizeof(int),
                        cudaMemcpyDeviceToDevice, st));
   return OAPL_OK;
+}
+
+int oapl_logits_logprobs(const oapl_logits* L, float* token_logp, float* token_entropy, float* token_lse, int32_t K,
+                         float* top_logp, int32_t* top_id, int32_t* device_status, void* stream) {
+  const int rc = check_logits(L);
+  if (rc != OAPL_OK) return rc;
+  if (K < 0 || K > kLgMaxTop) return OAPL_ERR_INVALID_ARG;
+  if (token_logp && !L->targets) return OAPL_ERR_INVALID_ARG;
+  if ((K > 0) != (top_logp || top_id)) return OAPL_ERR_INVALID_ARG;
+  if (!token_logp && !token_entropy && !token_lse && K == 0) return OAPL_ERR_INVALID_ARG;
+  LogitsParams lp = logits_params(L);
+  lp.token_logp = token_logp;
+  lp.token_entropy = token_entropy;
+  lp.token_lse = token_lse;
+  lp.K = K;
+  lp.top_logp = top_logp;
+  lp.top_id = top_id;
+  lp.status = device_status;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (L->type == OAPL_TYPE_BF16)
+    return K ? launch_logits_fwd<__nv_bfloat16, true>(lp, st) : launch_logits_fwd<__nv_bfloat16, false>(lp, st);
+  if (L->type == OAPL_TYPE_F16)
+    return K ? launch_logits_fwd<__half, true>(lp, st) : launch_logits_fwd<__half, false>(lp, st);
+  return K ? launch_logits_fwd<float, true>(lp, st) : launch_logits_fwd<float, false>(lp, st);
+}
+
+int oapl_logits_logprobs_bwd(const oapl_logits* L, const float* token_lse, const float* token_entropy,
+                             const float* g_logp, const float* g_entropy, int32_t K, const float* g_top,
+                             const int32_t* top_id, void* dlogits, int64_t ld_d, void* stream) {
+  const int rc = check_logits(L);
+  if (rc != OAPL_OK) return rc;
+  if (!token_lse || !dlogits || ld_d < L->V || K < 0 || K > kLgMaxTop) return OAPL_ERR_INVALID_ARG;
+  if (!g_logp && !g_entropy && !g_top) return OAPL_ERR_INVALID_ARG;
+  if (g_logp && !L->targets) return OAPL_ERR_INVALID_ARG;
+  if (g_entropy && !token_entropy) return OAPL_ERR_INVALID_ARG;
+  if ((g_top != nullptr) != (K > 0) || (g_top && !top_id)) return OAPL_ERR_INVALID_ARG;
+  if (dlogits == L->logits && ld_d != L->ld) return OAPL_ERR_INVALID_ARG;  // in place means the same rows
+  if ((uintptr_t)dlogits % logits_type_size(L->type)) return OAPL_ERR_MISALIGNED;
+  LogitsParams lp = logits_params(L);
+  lp.K = K;
+  lp.lse = token_lse;
+  lp.entropy = token_entropy;
+  lp.g_logp = g_logp;
+  lp.g_entropy = g_entropy;
+  lp.g_top = g_top;
+  lp.ids = top_id;
+  lp.dz = dlogits;
+  lp.ld_d = ld_d;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (L->type == OAPL_TYPE_BF16) return launch_logits_bwd<__nv_bfloat16>(lp, st);
+  if (L->type == OAPL_TYPE_F16) return launch_logits_bwd<__half>(lp, st);
+  return launch_logits_bwd<float>(lp, st);
+}
+
+int oapl_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ld_x, const oapl_scaled* out,
+                  int flags, void* stream) {
+  const int rc = check_scaled(out);
+  if (rc != OAPL_OK) return rc;
+  const int es = logits_type_size(x_type);
+  if (!x || !es || rows <= 0 || cols <= 0 || ld_x < cols) return OAPL_ERR_INVALID_ARG;
+  if (flags & ~(OAPL_QUANT_TRANSPOSE | OAPL_QUANT_POW2)) return OAPL_ERR_INVALID_ARG;
+  const bool turn = (flags & OAPL_QUANT_TRANSPOSE) != 0;
+  if (out->rows != (turn ? cols : rows) || out->cols != (turn ? rows : cols)) return OAPL_ERR_INVALID_ARG;
+  if ((uintptr_t)x % es) return OAPL_ERR_MISALIGNED;
+  QuantParams qp;
+  memset(&qp, 0, sizeof(qp));
+  qp.x = x;
+  qp.ldx = ld_x;
+  qp.R = (int32_t)rows;
+  qp.C = (int32_t)cols;
+  qp.q = static_cast<uint8_t*>(out->data);
+  qp.ldq = out->ld;
+  qp.scale = out->scale;
+  qp.srow = out->scale_row_stride;
+  qp.scol = out->scale_col_stride;
+  qp.pow2 = (flags & OAPL_QUANT_POW2) != 0;
+  qp.vec = (((uintptr_t)x | (uintptr_t)(ld_x * es)) & 15) == 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool e5 = out->type == OAPL_TYPE_E5M2, block = out->block_rows == 128;
+  if (x_type == OAPL_TYPE_BF16) return launch_quantize<__nv_bfloat16>(qp, e5, block, turn, st);
+  if (x_type == OAPL_TYPE_F16) return launch_quantize<__half>(qp, e5, block, turn, st);
+  return launch_quantize<float>(qp, e5, block, turn, st);
+}
+
+int oapl_scaled_matmul(const oapl_scaled* A, const oapl_scaled* B, void* C, int32_t c_type, int64_t ldc,
+                       int accumulate, int32_t* device_status, void* stream) {
+  int rc = check_scaled(A);
+  if (rc == OAPL_OK) rc = check_scaled(B);
+  if (rc != OAPL_OK) return rc;
+  const int es = logits_type_size(c_type);
+  if (!C || !es || A->cols != B->cols || ldc < B->rows) return OAPL_ERR_INVALID_ARG;
+  if ((uintptr_t)C % es) return OAPL_ERR_MISALIGNED;
+  const int n_sm = sm_count();
+  if (n_sm < 2) return OAPL_ERR_CUDA;
+  CUtensorMap ta, tb;
+  if (!make_map_u8(&ta, A->data, (uint64_t)A->rows, (uint64_t)A->cols, (uint64_t)A->ld) ||
+      !make_map_u8(&tb, B->data, (uint64_t)B->rows, (uint64_t)B->cols, (uint64_t)B->ld))
+    return OAPL_ERR_CUDA;
+  ScaledParams sp;
+  memset(&sp, 0, sizeof(sp));
+  sp.sa = A->scale;
+  sp.sb = B->scale;
+  sp.sa_row = A->scale_row_stride;
+  sp.sa_col = A->scale_col_stride;
+  sp.sb_row = B->scale_row_stride;
+  sp.sb_col = B->scale_col_stride;
+  sp.ga = A->block_rows;
+  sp.gb = B->block_rows;
+  sp.M = (int32_t)A->rows;
+  sp.N = (int32_t)B->rows;
+  sp.K = (int32_t)A->cols;
+  sp.C = C;
+  sp.ldc = ldc;
+  sp.accumulate = accumulate != 0;
+  sp.wide = (((uintptr_t)C | (uintptr_t)(ldc * es)) & 31) == 0;
+  sp.e5_a = A->type == OAPL_TYPE_E5M2;
+  sp.e5_b = B->type == OAPL_TYPE_E5M2;
+  sp.mt = (sp.M + kSmTile - 1) / kSmTile;
+  sp.nt = (sp.N + kSmTile - 1) / kSmTile;
+  sp.group = sp.mt < 16 ? sp.mt : 16;
+  sp.err = device_status;
+  const int64_t tiles = (int64_t)sp.mt * sp.nt;
+  const int grid = 2 * (int)(tiles < n_sm / 2 ? tiles : n_sm / 2);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool percol = sp.gb == 1;
+  if (c_type == OAPL_TYPE_BF16)
+    return percol ? launch_scaled_matmul<OUT_BF16, true>(ta, tb, sp, grid, st)
+                  : launch_scaled_matmul<OUT_BF16, false>(ta, tb, sp, grid, st);
+  if (c_type == OAPL_TYPE_F16)
+    return percol ? launch_scaled_matmul<OUT_F16, true>(ta, tb, sp, grid, st)
+                  : launch_scaled_matmul<OUT_F16, false>(ta, tb, sp, grid, st);
+  return percol ? launch_scaled_matmul<OUT_F32, true>(ta, tb, sp, grid, st)
+                : launch_scaled_matmul<OUT_F32, false>(ta, tb, sp, grid, st);
 }
 
 }  // extern "C"
