@@ -308,7 +308,7 @@ typedef struct {
   int32_t type;           /* OAPL_TYPE_BF16, _F16 or _F32                                           */
   const int32_t* targets; /* [N] or NULL; in [0,V) where mask==1                                    */
   const uint8_t* mask;    /* [N] or NULL (all rows live); rows with mask==0 are not read            */
-  float scale;            /* > 0: 1 / sampling temperature                                          */
+  float scale;            /* in (0, 1e6]: 1 / sampling temperature                                  */
 } oapl_logits;
 
 /*

@@ -2,9 +2,9 @@
 // gradient of all of them with respect to the logits.
 //
 // Forward, one pass over a row (z: the row's logits, a: the caller's factor):
-//     x_v = a (z_v - m),  S = sum_v e^x_v,  T = sum_v e^x_v x_v      (m: a reference near the maximum)
-//     lse = a m + ln S,   ln p_t = a z_t - lse,   entropy = ln S - T / S.
-// The entropy is formed from sums relative to m, so a peaked row does not lose it in the difference of
+//     x_v = a log2(e) z_v - R,  S = sum_v 2^x_v,  T = sum_v 2^x_v x_v      (R: a reference near the maximum)
+//     lse = R ln 2 + ln S,   ln p_t = x_t ln 2 - ln S,   entropy = ln S - ln 2 T / S.
+// The entropy is formed from sums relative to R, so a peaked row does not lose it in the difference of
 // two large numbers.  Sums are fp32: a thread adds a few hundred terms, the rest are trees.
 //
 // What bounds it: HBM.  A 16-bit logit has a budget of about eleven lane instructions per SM cycle, the
@@ -27,7 +27,7 @@ namespace oapl {
 
 constexpr int kLgThreads = 256;
 constexpr int kLgWarps = kLgThreads / 32;
-constexpr int kLgUnroll = 4;       // 16-byte loads in flight per thread
+constexpr int kLgUnroll = 4;       // 16-byte vectors that a thread loads together (a batch)
 constexpr int kLgMaxGroups = 32;   // groups of a thread whose maxima are kept for the top alternatives
 constexpr int kLgMaxTop = 32;
 constexpr int kLgMaxCluster = 8;
@@ -43,13 +43,16 @@ struct LogitsParams {
   const uint8_t* mask;
   float scale;
   // forward
+  float clamp;         // see logits_fwd_kernel
+  uint32_t clamp_pk;   // packed in the logits' type
   float* token_logp;
   float* token_entropy;
   float* token_lse;
   float* top_logp;
   int32_t* top_id;
   int32_t K;
-  int32_t slots;  // rows of group maxima in shared memory: the most groups any CTA forms, and one
+  int32_t per;    // batches of a group whose maxima are kept
+  int32_t slots;  // the most groups that a warp forms
   int32_t* status;
   // backward
   const float* lse;
@@ -122,6 +125,11 @@ struct Elem<__nv_bfloat16> {
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
   }
+  static __device__ __forceinline__ uint32_t pclamp(uint32_t a, uint32_t low) {  // a NaN stays
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(low));
+    return r;
+  }
   static __device__ __forceinline__ float pmax_final(uint32_t a) {
     return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
   }
@@ -152,6 +160,11 @@ struct Elem<__half> {
   static __device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ uint32_t pclamp(uint32_t a, uint32_t low) {
+    uint32_t r;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(low));
     return r;
   }
   static __device__ __forceinline__ float pmax_final(uint32_t a) {
@@ -185,6 +198,9 @@ struct Elem<float> {
   static __device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
     return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
   }
+  static __device__ __forceinline__ uint32_t pclamp(uint32_t a, uint32_t low) {
+    return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(low)));
+  }
   static __device__ __forceinline__ float pmax_final(uint32_t a) { return __uint_as_float(a); }
   static __device__ __forceinline__ uint4 narrow(const float (&f)[4]) {
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
@@ -192,60 +208,50 @@ struct Elem<float> {
   static __device__ __forceinline__ void put(void* p, int64_t i, float x) { reinterpret_cast<float*>(p)[i] = x; }
 };
 
-// Running sums of one thread: x relative to m, in units of log2.
+// Running sums of one thread.  x = c z - R, c = a log2(e): the reference R is a number of its own in units
+// of log2, not a rounded product that stands for a logit, so one multiply-add gives x with one rounding.
 struct RowSums {
-  float m;       // reference (a logit); -inf: nothing seen yet
-  uint64_t s, t; // two lanes each: sum e^x and sum e^x x
+  float R;
+  uint64_t s, t;  // two lanes each: sum 2^x and sum 2^x x
+};
+struct RowTotal {
+  float R, s, t, m;  // m: the largest logit, clamped
 };
 
-// x below this has e^x = 0 in fp32; also keeps 0 * x finite for logits of -inf.  NaN passes.
-constexpr float kLgFloor = -200.f;
-constexpr float kLgMove = 8.f;  // the reference follows when a maximum exceeds it by 2^8
+constexpr float kLgFloor = -200.f;  // 2^x is 0 in fp32 below this
+constexpr float kLgMove = 8.f;      // the reference follows when a maximum exceeds it by 2^8
 
-__device__ __forceinline__ void row_move(RowSums& r, float to, float c) {
-  // e^(x + d) = e^x 2^d, and x e^x becomes (x + d) e^x 2^d
-  if (r.m == -INFINITY) {
-    r.m = to;
-    return;
-  }
-  const float d = max_nan((r.m - to) * c, kLgFloor);
+__device__ __forceinline__ void row_move(RowSums& r, float to) {
+  // x + d in place of x: 2^x turns into 2^x 2^d, and 2^x x into (x + d) 2^x 2^d
+  const float d = fmaxf(r.R - to, kLgFloor);
   const float f = ex2_approx(d);
   float s0, s1, t0, t1;
   unpack2(r.s, s0, s1);
   unpack2(r.t, t0, t1);
   r.t = pack2(f * fmaf(d, s0, t0), f * fmaf(d, s1, t1));
   r.s = pack2(f * s0, f * s1);
-  r.m = to;
+  r.R = to;
 }
 
 template <int KN>
-__device__ __forceinline__ void row_add(RowSums& r, const float (&f)[KN], float negm, float c) {
-  const uint64_t nm = pack2(negm, negm), cc = pack2(c, c);
+__device__ __forceinline__ void row_add(RowSums& r, const float (&f)[KN], float c) {
+  const uint64_t nr = pack2(-r.R, -r.R), cc = pack2(c, c);
 #pragma unroll
   for (int i = 0; i < KN; i += 2) {
-    const uint64_t x2 = mul2(add2(pack2(f[i], f[i + 1]), nm), cc);
+    const uint64_t x2 = fma2(pack2(f[i], f[i + 1]), cc, nr);
     float x0, x1;
     unpack2(x2, x0, x1);
-    x0 = max_nan(x0, kLgFloor);
-    x1 = max_nan(x1, kLgFloor);
     const uint64_t e2 = pack2(ex2_approx(x0), ex2_approx(x1));
     r.s = add2(r.s, e2);
-    r.t = fma2(e2, pack2(x0, x1), r.t);
+    r.t = fma2(e2, x2, r.t);
   }
 }
 
-struct RowTotal {
-  float m, s, t;
-};
-__device__ __forceinline__ RowTotal row_join(const RowTotal& a, const RowTotal& b, float c) {
+__device__ __forceinline__ RowTotal row_join(const RowTotal& a, const RowTotal& b) {
   RowTotal o;
+  o.R = fmaxf(a.R, b.R);
   o.m = fmaxf(a.m, b.m);
-  if (o.m == -INFINITY) {
-    o.s = a.s + b.s;  // zeros, or a NaN that has to stay
-    o.t = 0.f;
-    return o;
-  }
-  const float da = max_nan((a.m - o.m) * c, kLgFloor), db = max_nan((b.m - o.m) * c, kLgFloor);
+  const float da = fmaxf(a.R - o.R, kLgFloor), db = fmaxf(b.R - o.R, kLgFloor);
   const float fa = ex2_approx(da), fb = ex2_approx(db);
   o.s = fa * a.s + fb * b.s;
   o.t = fa * fmaf(da, a.s, a.t) + fb * fmaf(db, b.s, b.t);
@@ -291,19 +297,97 @@ __device__ __forceinline__ void st_cluster_u64(uint32_t addr, uint64_t v) {
 }
 
 // ------------------------------------------------------------------------------------ forward
-// Top K: a thread's logits form up to 32 groups, whose maxima the pass writes to shared memory (a
-// store per 32 logits).  With j = ceil(K / 8), every one of the eight warps holds j threads whose
-// maximum is at least its own j-th largest thread maximum; the smallest of these over the warps, thr,
-// therefore has at least K logits at or above it.  Only groups whose maximum reaches thr can hold an
-// alternative: a few dozen of a few thousand.  They are read once more (a warp takes 32 at a time, one
-// per lane), and their entries at or above thr go through a list kept sorted over the warp's lanes.
-// The lists are joined by counting ranks.  Order and ties are decided by distinct keys, so the result
-// does not depend on the order of work.
+// The pass clamps logits where c z = -2^27 (a packed maximum), so that -inf and large negative masks give
+// 2^x = 0 and a finite x: below 2^27 in magnitude, x is off from c z - R by at most 8.  (fp16 ends at
+// -65504: there only -inf is clamped.)  That is exact for every row whose largest logit m lies 1000 / c
+// above the clamp, with |c m| < 2^26.  The others are done again by row_slow, which is only careful: rows
+// that hold nothing but masked logits, an infinity, or a huge common offset.
+//
+// Top K: a thread's logits form up to 32 groups, whose maxima the pass writes to shared memory (16 bits:
+// the upper half of the ordered value, a lower bound).  Each of the w warps with data has j = ceil(K / w)
+// threads whose maximum is at least the warp's own j-th largest thread maximum; the smallest of these over
+// the warps, thr, therefore has at least K logits at or above it.  Only groups whose maximum reaches thr
+// can hold an alternative: a few dozen of a few thousand.  They are read once more (a warp takes 32 at a
+// time, one per lane), and their entries at or above thr go through a list kept sorted over the warp's
+// lanes.  The lists are joined by counting ranks.  Order and ties are decided by distinct keys, so the
+// result does not depend on the order of work.
+constexpr int kLgQueue = 64;  // groups a warp has waiting
+constexpr float kLgPlainX = 67108864.f;    // 2^26
+
+// Where a row's part lies: nh single elements, vectors [v0, v1) of this CTA behind them.
+struct RowPart {
+  const uint4* zv;
+  int nh, nv, v0, v1;
+};
+template <typename T>
+__device__ __forceinline__ RowPart row_part(const LogitsParams& p, int64_t row, int rank, int nc) {
+  constexpr int kN = Elem<T>::kN;
+  const T* zrow = reinterpret_cast<const T*>(p.z) + row * p.ld;
+  RowPart q;
+  q.nh = int(((16u - (uint32_t(reinterpret_cast<uintptr_t>(zrow)) & 15u)) & 15u) / sizeof(T));
+  if (q.nh > p.V) q.nh = p.V;
+  q.nv = (p.V - q.nh) / kN;
+  q.zv = reinterpret_cast<const uint4*>(zrow + q.nh);
+  q.v0 = int(int64_t(q.nv) * rank / nc);
+  q.v1 = int(int64_t(q.nv) * (rank + 1) / nc);
+  return q;
+}
+
+// A whole row by one CTA, any logits: the exact maximum m first, then x = c (z - m).  All threads get
+// {m, sum 2^x, sum 2^x x}; sh: kLgWarps entries.
+template <typename T>
+__device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* sh) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  float m = -INFINITY;
+  bool nan = false;
+  for (int i = tid; i < V; i += kLgThreads) {
+    const float v = Elem<T>::one(z, i);
+    nan |= v != v;
+    m = fmaxf(m, v);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  __syncthreads();
+  if (lane == 0) sh[warp].m = m;
+  nan = __syncthreads_or(nan);
+  for (int w = 0; w < kLgWarps; ++w) m = fmaxf(m, sh[w].m);
+  RowTotal r;
+  r.R = 0.f;
+  r.m = m;
+  r.s = r.t = 0.f;
+  if (!nan && m > -INFINITY) {
+    for (int i = tid; i < V; i += kLgThreads) {
+      const float x = max_nan((Elem<T>::one(z, i) - m) * c, kLgFloor);
+      const float e = ex2_approx(x);
+      r.s += e;
+      r.t = fmaf(e, x, r.t);
+    }
+  } else if (nan) {
+    r.s = __int_as_float(0x7FC00000);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float s = __shfl_xor_sync(0xffffffffu, r.s, o), t = __shfl_xor_sync(0xffffffffu, r.t, o);
+    r.s = (lane & o) ? s + r.s : r.s + s;
+    r.t = (lane & o) ? t + r.t : r.t + t;
+  }
+  __syncthreads();
+  if (lane == 0) sh[warp] = r;
+  __syncthreads();
+  r = sh[0];
+  for (int w = 1; w < kLgWarps; ++w) {
+    r.s += sh[w].s;
+    r.t += sh[w].t;
+  }
+  __syncthreads();
+  return r;
+}
+
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsParams p) {
   using E = Elem<T>;
   constexpr int kN = E::kN;
-  extern __shared__ float gmax[];  // TOP: [groups + 1][kLgThreads], then the warps' queues
+  extern __shared__ __align__(16) uint16_t gmax[];  // TOP: [slots][kLgThreads] group maxima, the warps' queues
   __shared__ RowTotal sh_tot[kLgWarps];
   __shared__ RowTotal sh_cl[kLgMaxCluster];
   __shared__ uint64_t sh_list[kLgWarps * kLgMaxTop];
@@ -316,9 +400,9 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   uint32_t nc, rank;
   asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(nc));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int K = p.K, V = p.V;
+  const float c = p.scale * 1.4426950408889634f;
   const int64_t row = blockIdx.x / nc;
-  const int K = p.K;
-
   if (p.mask && p.mask[row] == 0) {
     if (rank == 0) {
       if (tid == 0) {
@@ -331,91 +415,85 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
         if (p.top_id) p.top_id[row * K + tid] = -1;
       }
     }
-    return;  // every CTA of the cluster alike
+    return;  // every CTA of a cluster alike
   }
   // The other CTAs' shared memory may be written once they run: this barrier's first half here, its
   // second before the join.
   if (nc > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 
-  const float c = p.scale * 1.4426950408889634f;
   const T* zrow = reinterpret_cast<const T*>(p.z) + row * p.ld;
   float z_target = 0.f;
-  int target = -1;
   bool bad_target = false;
   if (rank == 0 && tid == 0 && p.token_logp) {
-    target = p.targets[row];
-    bad_target = target < 0 || target >= p.V;
+    const int target = p.targets[row];
+    bad_target = target < 0 || target >= V;
     if (!bad_target) z_target = E::one(zrow, target);
   }
-
-  // the row as nh single elements, nv 16-byte vectors, and the rest
-  const int V = p.V;
-  int nh = int(((16u - (uint32_t(reinterpret_cast<uintptr_t>(zrow)) & 15u)) & 15u) / sizeof(T));
-  if (nh > V) nh = V;
-  const int nv = (V - nh) / kN;
-  const int nsingle = V - nv * kN;  // head and tail elements: the last CTA takes them
-  const uint4* zv = reinterpret_cast<const uint4*>(zrow + nh);
-  const int v0 = int(int64_t(nv) * rank / nc), v1 = int(int64_t(nv) * (rank + 1) / nc);
-  const int nb = (v1 - v0 + kLgThreads * kLgUnroll - 1) / (kLgThreads * kLgUnroll);
-  const int per = (nb + kLgMaxGroups - 1) / kLgMaxGroups;  // batches per group
+  const RowPart q = row_part<T>(p, row, rank, nc);
+  const int nsingle = V - q.nv * kN;  // head and tail elements: the last CTA takes them
+  const int nb = (q.v1 - q.v0 + kLgThreads * kLgUnroll - 1) / (kLgThreads * kLgUnroll);
+  const int per = p.per;
+  float zs = -INFINITY;
+  if (rank == nc - 1 && tid < nsingle) zs = E::one(zrow, tid < q.nh ? tid : q.nv * kN + tid);
 
   RowSums r;
-  r.m = -INFINITY;
+  r.R = fmaf(p.clamp, c, 1000.f);  // a clamped logit counts for nothing
   r.s = r.t = pack2(0.f, 0.f);
-  float tmax = -INFINITY, gm = -INFINITY;
+  float tmax = p.clamp, gm = p.clamp;
   int g = 0, in_group = 0;
-
   uint4 cur[kLgUnroll], nxt[kLgUnroll];
   auto load = [&](int b, uint4 (&v)[kLgUnroll]) {
 #pragma unroll
     for (int u = 0; u < kLgUnroll; ++u) {
-      const int i = v0 + (b * kLgUnroll + u) * kLgThreads + tid;
+      const int i = q.v0 + (b * kLgUnroll + u) * kLgThreads + tid;
       v[u] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
-      if (i < v1) v[u] = ldg_stream(zv + i);
+      if (i < q.v1) v[u] = ldg_stream(q.zv + i);
     }
   };
   if (nb > 0) load(0, cur);
   for (int b = 0; b < nb; ++b) {
     if (b + 1 < nb) load(b + 1, nxt);
-    uint32_t pm = E::kNegInf;
+    uint32_t pm = 0;
 #pragma unroll
-    for (int u = 0; u < kLgUnroll; ++u)
-      pm = E::pmax(pm, E::pmax(E::pmax(cur[u].x, cur[u].y), E::pmax(cur[u].z, cur[u].w)));
+    for (int u = 0; u < kLgUnroll; ++u) {
+      uint4& v = cur[u];
+      v = make_uint4(E::pclamp(v.x, p.clamp_pk), E::pclamp(v.y, p.clamp_pk), E::pclamp(v.z, p.clamp_pk),
+                     E::pclamp(v.w, p.clamp_pk));
+      const uint32_t a = E::pmax(E::pmax(v.x, v.y), E::pmax(v.z, v.w));
+      pm = u ? E::pmax(pm, a) : a;
+    }
     const float bm = E::pmax_final(pm);
+    tmax = fmaxf(tmax, bm);
     if (TOP) {
       gm = fmaxf(gm, bm);
       if (++in_group == per) {
-        gmax[g * kLgThreads + tid] = gm;
-        tmax = fmaxf(tmax, gm);
-        gm = -INFINITY;
+        gmax[g * kLgThreads + tid] = uint16_t(top_key(gm, 0) >> 48);
+        gm = p.clamp;
         in_group = 0;
         ++g;
       }
     }
-    if ((bm - r.m) * c > kLgMove || r.m == -INFINITY) row_move(r, bm, c);
-    const float negm = r.m == -INFINITY ? 0.f : -r.m;
+    if (fmaf(bm, c, -r.R) > kLgMove) row_move(r, bm * c);
 #pragma unroll
     for (int u = 0; u < kLgUnroll; ++u) {
       float f[kN];
       E::widen(cur[u], f);
-      row_add<kN>(r, f, negm, c);
+      row_add<kN>(r, f, c);
     }
 #pragma unroll
     for (int u = 0; u < kLgUnroll; ++u) cur[u] = nxt[u];
   }
   if (TOP && in_group) {
-    gmax[g * kLgThreads + tid] = gm;
-    tmax = fmaxf(tmax, gm);
+    gmax[g * kLgThreads + tid] = uint16_t(top_key(gm, 0) >> 48);
     ++g;
   }
-  float zs = -INFINITY;  // this thread's single element
-  int single = -1;
+  float wmax = tmax;
   if (rank == nc - 1 && tid < nsingle) {
-    single = tid < nh ? tid : nv * kN + tid;
-    zs = E::one(zrow, single);
-    if ((zs - r.m) * c > kLgMove || r.m == -INFINITY) row_move(r, zs, c);
-    const float f[2] = {zs, -INFINITY};
-    row_add<2>(r, f, r.m == -INFINITY ? 0.f : -r.m, c);
+    const float z = max_nan(zs, p.clamp);
+    if (fmaf(z, c, -r.R) > kLgMove) row_move(r, z * c);
+    const float f[2] = {z, p.clamp};
+    row_add<2>(r, f, c);
+    wmax = fmaxf(wmax, z);
   }
 
   // ---- join the sums: lanes, warps
@@ -424,108 +502,109 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     float s0, s1, t0, t1;
     unpack2(r.s, s0, s1);
     unpack2(r.t, t0, t1);
-    tot.m = r.m;
+    tot.R = r.R;
     tot.s = s0 + s1;
     tot.t = t0 + t1;
+    tot.m = wmax;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     RowTotal other;
-    other.m = __shfl_xor_sync(0xffffffffu, tot.m, o);
+    other.R = __shfl_xor_sync(0xffffffffu, tot.R, o);
     other.s = __shfl_xor_sync(0xffffffffu, tot.s, o);
     other.t = __shfl_xor_sync(0xffffffffu, tot.t, o);
+    other.m = __shfl_xor_sync(0xffffffffu, tot.m, o);
     // both partners form the same sum in the same order
-    tot = (lane & o) ? row_join(other, tot, c) : row_join(tot, other, c);
+    tot = (lane & o) ? row_join(other, tot) : row_join(tot, other);
   }
   if (lane == 0) sh_tot[warp] = tot;
 
   // ---- top alternatives of this CTA's part
   if (TOP) {
-    gmax[g * kLgThreads + tid] = zs;
-    float left = fmaxf(tmax, zs);
-    const int j = (K + kLgWarps - 1) / kLgWarps;
+    const uint32_t none = uint32_t(top_key(-INFINITY, 0) >> 32);  // -inf is no alternative
+    const int with = min((q.v1 - q.v0 + 31) / 32, kLgWarps);      // warps with data
+    float left = tmax;
     uint32_t jth = 0;
-    for (int q = 0; q < j; ++q) {
-      const uint32_t o = uint32_t(top_key(left, 0) >> 32);
-      jth = __reduce_max_sync(0xffffffffu, o);
-      const uint32_t who = __ballot_sync(0xffffffffu, o == jth);
-      if (lane == __ffs(who) - 1) left = -INFINITY;
+    if (warp < with) {
+      for (int n = (K + with - 1) / with; n > 0; --n) {
+        const uint32_t o = uint32_t(top_key(left, 0) >> 32);
+        jth = __reduce_max_sync(0xffffffffu, o);
+        const uint32_t who = __ballot_sync(0xffffffffu, o == jth);
+        if (lane == __ffs(who) - 1) left = -INFINITY;
+      }
     }
     if (lane == 0) sh_thr[warp] = jth;
     if (tid == 0) sh_count = 0;
     if (tid < kLgMaxTop) sh_best[tid] = 0;
     __syncthreads();
-    uint32_t thr = sh_thr[0];
-#pragma unroll
-    for (int w = 1; w < kLgWarps; ++w) thr = min(thr, sh_thr[w]);
-    const uint32_t none = uint32_t(top_key(-INFINITY, 0) >> 32);  // -inf is no alternative
-    uint16_t* queue = reinterpret_cast<uint16_t*>(gmax + p.slots * kLgThreads) + warp * p.slots * 32;
-    int nq = 0;
-    for (int q = 0; q <= g; ++q) {
-      const uint32_t o = uint32_t(top_key(gmax[q * kLgThreads + tid], 0) >> 32);
-      const bool in = o >= thr && o > none;
-      const uint32_t b = __ballot_sync(0xffffffffu, in);
-      if (in) queue[nq + __popc(b & ((1u << lane) - 1u))] = uint16_t(q * 32 + lane);
-      nq += __popc(b);
-    }
-    __syncwarp();
+    uint32_t thr = with ? 0xFFFFFFFFu : 0u;
+    for (int w = 0; w < with; ++w) thr = min(thr, sh_thr[w]);
+    // at the clamp the maxima say nothing: everything above -inf is to be looked at
+    if (thr <= uint32_t(top_key(p.clamp, 0) >> 32)) thr = none + 1;
+    const uint32_t thr16 = thr > none + 1 ? thr >> 16 : 0;
+
     uint64_t mine = 0;  // lane i: the warp's i-th best entry so far
-    for (int q0 = 0; q0 < nq; q0 += 32) {
-      uint64_t kth = __shfl_sync(0xffffffffu, mine, K - 1);
-      const int item = q0 + lane < nq ? queue[q0 + lane] : -1;
-      const int ig = item >> 5, it = (item & 31) + warp * 32;
-      bool act = item >= 0;
-      const bool is_single = act && ig == g;
-      const int first = act && !is_single ? v0 + ig * per * kLgUnroll * kLgThreads + it : 0;
-      // nothing in the group can enter when its maximum at its lowest index would not
-      if (act && !is_single)
-        act = top_key(gmax[ig * kLgThreads + it], uint32_t(nh + first * kN)) > kth;
-      if (!__any_sync(0xffffffffu, act)) continue;
-      // the single elements: one entry per thread
-      {
-        const int tsingle = it < nh ? it : nv * kN + it;
-        const float v = is_single ? gmax[g * kLgThreads + it] : -INFINITY;
-        const uint64_t key = top_key(v, uint32_t(tsingle));
-        uint32_t b = __ballot_sync(0xffffffffu, is_single && uint32_t(key >> 32) >= thr && v > -INFINITY && key > kth);
-        while (b) {
+    uint64_t kth = 0;
+    auto offer = [&](float v, uint32_t idx, bool in) {
+      const uint64_t key = top_key(v, idx);
+      uint32_t b = __ballot_sync(0xffffffffu, in && v > -INFINITY && uint32_t(key >> 32) >= thr && key > kth);
+      if (b) {
+        do {
           const int src = __ffs(b) - 1;
           b &= b - 1;
           top_insert(mine, __shfl_sync(0xffffffffu, key, src), lane);
-        }
+        } while (b);
         kth = __shfl_sync(0xffffffffu, mine, K - 1);
       }
-      act = act && !is_single;
-      for (int u = 0; u < per * kLgUnroll; u += kLgUnroll) {
-        uint4 v[kLgUnroll];
+    };
+    if (warp == 0 && rank == nc - 1) offer(zs, uint32_t(tid < q.nh ? tid : q.nv * kN + tid), tid < nsingle);
+    uint16_t* queue = gmax + p.slots * kLgThreads + warp * kLgQueue;
+    int nq = 0;
+    for (int k = 0; k < g || nq > 0;) {
+      while (k < g && nq <= kLgQueue - 32) {
+        const bool in = gmax[k * kLgThreads + tid] >= thr16;
+        const uint32_t b = __ballot_sync(0xffffffffu, in);
+        if (in) queue[nq + __popc(b & ((1u << lane) - 1u))] = uint16_t(k * 32 + lane);
+        nq += __popc(b);
+        ++k;
+      }
+      __syncwarp();
+      const int take = min(nq, 32);
+      const int item = lane < take ? queue[nq - take + lane] : -1;
+      nq -= take;
+      const int ig = item >> 5, il = item & 31;
+      const int b0 = ig * per, b1 = min(b0 + per, nb);
+      const int first = q.v0 + warp * 32 + il;  // vector u of batch b: first + (b * kLgUnroll + u) * kLgThreads
+      bool act = item >= 0;
+      if (act) {
+        // nothing in the group can enter when its largest possible value at its lowest index would not
+        const uint32_t o16 = gmax[ig * kLgThreads + warp * 32 + il];
+        const uint32_t low = E::kNegInf == 0xFF80FF80u && (o16 & 0x8000u) ? 0u : 0xFFFFu;
+        const uint32_t at = uint32_t(q.nh + (first + b0 * kLgUnroll * kLgThreads) * kN);
+        act = ((uint64_t((o16 << 16) | low) << 32) | (0xFFFFFFFFu - at)) > kth;
+      }
+      if (__any_sync(0xffffffffu, act)) {
+        for (int b = b0; __any_sync(0xffffffffu, act && b < b1); ++b) {
+          uint4 v[kLgUnroll];
 #pragma unroll
-        for (int w = 0; w < kLgUnroll; ++w) {
-          const int i = first + (u + w) * kLgThreads;
-          v[w] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
-          if (act && i < v1) v[w] = ldg_stream(zv + i);
-        }
+          for (int w = 0; w < kLgUnroll; ++w) {
+            const int i = first + (b * kLgUnroll + w) * kLgThreads;
+            v[w] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
+            if (act && b < b1 && i < q.v1) v[w] = ldg_stream(q.zv + i);
+          }
 #pragma unroll
-        for (int w = 0; w < kLgUnroll; ++w) {
-          const float vm = E::pmax_final(E::pmax(E::pmax(v[w].x, v[w].y), E::pmax(v[w].z, v[w].w)));
-          const uint32_t om = uint32_t(top_key(vm, 0) >> 32);
-          if (!__any_sync(0xffffffffu, om >= thr && om > none)) continue;
-          float f[kN];
-          E::widen(v[w], f);
-          const uint32_t i0 = uint32_t(nh + (first + (u + w) * kLgThreads) * kN);
+          for (int w = 0; w < kLgUnroll; ++w) {
+            const float vm = E::pmax_final(E::pmax(E::pmax(v[w].x, v[w].y), E::pmax(v[w].z, v[w].w)));
+            if (!__any_sync(0xffffffffu, uint32_t(top_key(vm, 0) >> 32) >= thr)) continue;
+            float f[kN];
+            E::widen(v[w], f);
+            const int i = first + (b * kLgUnroll + w) * kLgThreads;
 #pragma unroll
-          for (int e = 0; e < kN; ++e) {
-            const uint64_t key = top_key(f[e], i0 + e);
-            uint32_t b = __ballot_sync(0xffffffffu, uint32_t(key >> 32) >= thr && f[e] > -INFINITY && key > kth);
-            if (b) {
-              do {
-                const int src = __ffs(b) - 1;
-                b &= b - 1;
-                top_insert(mine, __shfl_sync(0xffffffffu, key, src), lane);
-              } while (b);
-              kth = __shfl_sync(0xffffffffu, mine, K - 1);
-            }
+            for (int e = 0; e < kN; ++e) offer(f[e], uint32_t(q.nh + i * kN + e), true);
           }
         }
       }
+      __syncwarp();
     }
     // the warps' lists one behind the other; their order does not matter
     const int have = __popc(__ballot_sync(0xffffffffu, lane < K && mine != 0));
@@ -541,22 +620,23 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   }
   tot = sh_tot[0];
 #pragma unroll
-  for (int w = 1; w < kLgWarps; ++w) tot = row_join(tot, sh_tot[w], c);
+  for (int w = 1; w < kLgWarps; ++w) tot = row_join(tot, sh_tot[w]);
 
   // ---- join the CTAs of the row in CTA 0
   if (nc > 1) {
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (tid == 0) {
       const uint32_t to = mapa_shared(smem_u32(&sh_cl[rank]), 0);
-      st_cluster_u32(to, __float_as_uint(tot.m));
+      st_cluster_u32(to, __float_as_uint(tot.R));
       st_cluster_u32(to + 4, __float_as_uint(tot.s));
       st_cluster_u32(to + 8, __float_as_uint(tot.t));
+      st_cluster_u32(to + 12, __float_as_uint(tot.m));
     }
     if (TOP && tid < K) st_cluster_u64(mapa_shared(smem_u32(&sh_cl_list[rank * K + tid]), 0), sh_best[tid]);
     cluster_sync_all();
     if (rank != 0) return;
     tot = sh_cl[0];
-    for (uint32_t q = 1; q < nc; ++q) tot = row_join(tot, sh_cl[q], c);
+    for (uint32_t w = 1; w < nc; ++w) tot = row_join(tot, sh_cl[w]);
     if (TOP) {
       if (tid < kLgMaxTop) sh_best[tid] = 0;
       __syncthreads();
@@ -566,28 +646,32 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   }
 
   // ---- results
+  const float ln2 = 0.6931471805599453f;
+  const bool plain = fabsf(tot.m * c) < kLgPlainX && (tot.m - p.clamp) * c > 1000.f;  // the same for all threads
+  if (!plain) tot = row_slow<T>(zrow, V, c, sh_tot);
   // no finite logit: every probability is 0, lse = -inf, nothing to choose from
   const bool empty = tot.m == -INFINITY && tot.s == 0.f;
   const bool broken = !empty && !(tot.m > -INFINITY && tot.m < INFINITY && tot.s > 0.f && tot.s < INFINITY);
   const float nan = __int_as_float(0x7FC00000);
   const float ln_s = logf(tot.s);
-  const float lse = broken ? nan : (empty ? -INFINITY : fmaf(p.scale, tot.m, ln_s));
+  // ln p of a logit, relative to the reference, so that a large common offset does not cost digits
+  auto ln_p = [&](float z) {
+    if (broken) return nan;
+    if (empty || z == -INFINITY) return -INFINITY;
+    if (!plain) return p.scale * (z - tot.m) - ln_s;
+    return z > p.clamp ? fmaf(fmaf(z, c, -tot.R), ln2, -ln_s) : fmaf(p.scale, z, -fmaf(tot.R, ln2, ln_s));
+  };
   if (tid == 0) {
-    if (p.token_lse) p.token_lse[row] = lse;
-    if (p.token_entropy)
-      p.token_entropy[row] = broken ? nan : (empty ? 0.f : fmaxf(0.f, ln_s - 0.6931471805599453f * (tot.t / tot.s)));
-    if (p.token_logp) {
-      // relative to the reference, so that a large common offset does not cost digits
-      const float lp = bad_target || broken ? nan : (empty ? -INFINITY : p.scale * (z_target - tot.m) - ln_s);
-      p.token_logp[row] = lp;
-    }
+    if (p.token_lse)
+      p.token_lse[row] = broken ? nan : (empty ? -INFINITY : (plain ? fmaf(tot.R, ln2, ln_s) : fmaf(p.scale, tot.m, ln_s)));
+    if (p.token_entropy) p.token_entropy[row] = broken ? nan : (empty ? 0.f : fmaxf(0.f, ln_s - ln2 * (tot.t / tot.s)));
+    if (p.token_logp) p.token_logp[row] = bad_target ? nan : ln_p(z_target);
     if (p.status && (bad_target || broken)) atomicCAS(p.status, 0, bad_target ? kErrBadTarget : kErrNonfinite);
   }
   if (TOP && tid < K) {
     const uint64_t key = sh_best[tid];
     if (p.top_id) p.top_id[row * K + tid] = key ? int32_t(0xFFFFFFFFu - uint32_t(key)) : -1;
-    if (p.top_logp)
-      p.top_logp[row * K + tid] = broken ? nan : (key ? p.scale * (top_value(key) - tot.m) - ln_s : -INFINITY);
+    if (p.top_logp) p.top_logp[row * K + tid] = broken ? nan : (key ? ln_p(top_value(key)) : -INFINITY);
   }
 }
 

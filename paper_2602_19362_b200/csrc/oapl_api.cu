@@ -637,7 +637,7 @@ static int check_logits(const oapl_logits* L) {
   if (!L || !L->logits || L->N <= 0 || L->V <= 0 || L->ld < L->V) return OAPL_ERR_INVALID_ARG;
   const int es = logits_type_size(L->type);
   if (!es) return OAPL_ERR_INVALID_ARG;
-  if (!(L->scale > 0.f) || !std::isfinite(L->scale)) return OAPL_ERR_INVALID_ARG;
+  if (!(L->scale > 0.f) || !(L->scale <= 1e6f)) return OAPL_ERR_INVALID_ARG;  // the forward's clamp
   if ((uintptr_t)L->logits % es) return OAPL_ERR_MISALIGNED;
   if (L->N > (int64_t)2000000000 || (int64_t)L->V > (int64_t)2000000000) return OAPL_ERR_UNSUPPORTED_SHAPE;
   return OAPL_OK;
@@ -653,35 +653,45 @@ static LogitsParams logits_params(const oapl_logits* L) {
   lp.targets = L->targets;
   lp.mask = L->mask;
   lp.scale = L->scale;
+  // where scale * log2(e) * z = -2^27, rounded towards zero to the type (fp16 stops at -65504)
+  lp.clamp = -134217728.f / (L->scale * 1.4426950408889634f);
+  uint32_t u;
+  memcpy(&u, &lp.clamp, 4);
+  if (L->type == OAPL_TYPE_BF16) {
+    u &= 0xFFFF0000u;
+    lp.clamp_pk = u | (u >> 16);
+  } else if (L->type == OAPL_TYPE_F16) {
+    const float lo = lp.clamp < -65504.f ? -65504.f : lp.clamp;
+    const __half h = __float2half_rz(lo);
+    const float back = __half2float(h);
+    uint16_t w;
+    memcpy(&w, &h, 2);
+    memcpy(&u, &back, 4);
+    lp.clamp_pk = w | ((uint32_t)w << 16);
+  } else {
+    lp.clamp_pk = u;
+  }
+  memcpy(&lp.clamp, &u, 4);
   return lp;
 }
 
 template <typename T, bool TOP>
 static int launch_logits_fwd(LogitsParams lp, cudaStream_t st) {
   const int n_sm = sm_count();
-  int dev = -1;
-  if (n_sm <= 0 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return OAPL_ERR_CUDA;
-  // CTAs of a row: split it while the split rows still fit the SMs twice and every thread keeps a load
+  if (n_sm <= 0) return OAPL_ERR_CUDA;
+  // CTAs of a row: split it while the split rows still fit the SMs twice and every thread keeps a vector
   const int nv = lp.V / Elem<T>::kN;
   int nc = 1;
   while (nc < kLgMaxCluster && (int64_t)lp.N * nc * 2 <= 2 * n_sm && nv / (nc * 2) >= kLgThreads) nc *= 2;
-  if ((int64_t)lp.N * nc > (int64_t)2147483647) return OAPL_ERR_UNSUPPORTED_SHAPE;
   size_t smem = 0;
   if (TOP) {
-    const int span = kLgThreads * kLgUnroll;
-    const int nb = (nv / nc + 1 + span - 1) / span;  // the largest part of a row has one vector more
-    const int per = (nb + kLgMaxGroups - 1) / kLgMaxGroups;
-    lp.slots = (nb + per - 1) / per + 1;
-    smem = (size_t)lp.slots * (kLgThreads * 4 + kLgWarps * 32 * 2);
+    // batches of the largest part of a row, which has one vector more
+    const int span = kLgThreads * kLgUnroll, nb = (nv / nc + 1 + span - 1) / span;
+    lp.per = nb > kLgMaxGroups ? (nb + kLgMaxGroups - 1) / kLgMaxGroups : 1;
+    lp.slots = (nb + lp.per - 1) / lp.per;
+    smem = (size_t)lp.slots * kLgThreads * 2 + kLgWarps * kLgQueue * 2;
   }
   auto kern = logits_fwd_kernel<T, TOP>;
-  static bool attr_set[kMaxDevices] = {false};
-  if (TOP && !attr_set[dev]) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (kLgMaxGroups + 1) * (kLgThreads * 4 + kLgWarps * 32 * 2)) != cudaSuccess)
-      return OAPL_ERR_CUDA;
-    attr_set[dev] = true;
-  }
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3((unsigned)(lp.N * (int64_t)nc));
