@@ -278,15 +278,24 @@ __device__ __forceinline__ void top_insert(uint64_t& mine, uint64_t key, int lan
   if (lane > pos) mine = up;
 }
 
-// out[rank] = the K best of entries[0..M); keys are distinct apart from empty ones.  All threads.
-__device__ __forceinline__ void top_rank(const uint64_t* entries, int M, int K, uint64_t* out) {
+// out[rank] = the K best of entries[0..M); keys are distinct apart from empty ones (0).  All threads;
+// entries is 16-byte aligned and has room for a multiple of four.
+__device__ __forceinline__ void top_rank(uint64_t* entries, int M, int K, uint64_t* out) {
+  if (threadIdx.x < 4 && (M & 3) && threadIdx.x < 4 - (M & 3)) entries[M + threadIdx.x] = 0;
+  __syncthreads();
+  const ulonglong2* two = reinterpret_cast<const ulonglong2*>(entries);
   for (int i = threadIdx.x; i < M; i += kLgThreads) {
     const uint64_t k = entries[i];
     if (k == 0) continue;
     int r = 0;
-    for (int j = 0; j < M; ++j) r += entries[j] > k;
+#pragma unroll 4
+    for (int j = 0; j < (M + 3) / 4; ++j) {
+      const ulonglong2 a = two[2 * j], b = two[2 * j + 1];
+      r += (a.x > k) + (a.y > k) + (b.x > k) + (b.y > k);
+    }
     if (r < K) out[r] = k;
   }
+  __syncthreads();
 }
 
 __device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
@@ -307,11 +316,13 @@ __device__ __forceinline__ void st_cluster_u64(uint32_t addr, uint64_t v) {
 // the upper half of the ordered value, a lower bound).  Each of the w warps with data has j = ceil(K / w)
 // threads whose maximum is at least the warp's own j-th largest thread maximum; the smallest of these over
 // the warps, thr, therefore has at least K logits at or above it.  Only groups whose maximum reaches thr
-// can hold an alternative: a few dozen of a few thousand.  They are read once more (a warp takes 32 at a
-// time, one per lane), and their entries at or above thr go through a list kept sorted over the warp's
-// lanes.  The lists are joined by counting ranks.  Order and ties are decided by distinct keys, so the
-// result does not depend on the order of work.
-constexpr int kLgQueue = 64;  // groups a warp has waiting
+// can hold an alternative: a few dozen of a few thousand.  They are read once more, a vector per thread,
+// and their entries at or above thr are ranked by counting.  Order and ties are decided by distinct keys,
+// so the result does not depend on the order of work.  Rows with too many equal logits for the two small
+// lists go through sorted lists instead (top_by_lists).
+constexpr int kLgQueue = 64;    // top_by_lists: groups a warp has waiting
+constexpr int kLgItems = 256;   // groups to read again
+constexpr int kLgCands = 256;   // entries at or above thr
 constexpr float kLgPlainX = 67108864.f;    // 2^26
 
 // Where a row's part lies: nh single elements, vectors [v0, v1) of this CTA behind them.
@@ -383,18 +394,104 @@ __device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* 
   return r;
 }
 
+// The K best entries of every warp's part of the row through lists that are kept sorted over the lanes,
+// whatever the ties: `out` gets the lists one behind the other, *count their length.  All threads.
+template <typename T>
+__device__ __noinline__ void top_by_lists(const LogitsParams& p, const RowPart& q, int nb, int g, uint32_t thr,
+                                          uint32_t thr16, float zs, bool has_single, const uint16_t* gmax,
+                                          uint64_t* out, int* count) {
+  using E = Elem<T>;
+  constexpr int kN = E::kN;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, K = p.K, per = p.per;
+  __shared__ uint16_t sh_queue[kLgWarps * kLgQueue];
+  uint16_t* queue = sh_queue + warp * kLgQueue;
+  __syncthreads();  // everybody has read the count
+  if (tid == 0) *count = 0;
+  uint64_t mine = 0;  // lane i: the warp's i-th best entry so far
+  uint64_t kth = 0;
+  auto offer = [&](float v, uint32_t idx, bool in) {
+    const uint64_t key = top_key(v, idx);
+    uint32_t b = __ballot_sync(0xffffffffu, in && v > -INFINITY && uint32_t(key >> 32) >= thr && key > kth);
+    if (b) {
+      do {
+        const int src = __ffs(b) - 1;
+        b &= b - 1;
+        top_insert(mine, __shfl_sync(0xffffffffu, key, src), lane);
+      } while (b);
+      kth = __shfl_sync(0xffffffffu, mine, K - 1);
+    }
+  };
+  if (warp == 0) offer(zs, uint32_t(tid < q.nh ? tid : q.nv * kN + tid), has_single);
+  int nq = 0;
+  for (int k = 0; k < g || nq > 0;) {
+    while (k < g && nq <= kLgQueue - 32) {
+      const bool in = gmax[k * kLgThreads + tid] >= thr16;
+      const uint32_t b = __ballot_sync(0xffffffffu, in);
+      if (in) queue[nq + __popc(b & ((1u << lane) - 1u))] = uint16_t(k * 32 + lane);
+      nq += __popc(b);
+      ++k;
+    }
+    __syncwarp();
+    const int take = min(nq, 32);
+    const int item = lane < take ? queue[nq - take + lane] : -1;
+    nq -= take;
+    const int ig = item >> 5, il = item & 31;
+    const int b0 = ig * per, b1 = min(b0 + per, nb);
+    const int first = q.v0 + warp * 32 + il;  // vector u of batch b: first + (b * kLgUnroll + u) * kLgThreads
+    bool act = item >= 0;
+    if (act) {
+      // nothing in the group can enter when its largest possible value at its lowest index would not
+      const uint32_t o16 = gmax[ig * kLgThreads + warp * 32 + il];
+      const uint32_t low = E::kNegInf == 0xFF80FF80u && (o16 & 0x8000u) ? 0u : 0xFFFFu;
+      const uint32_t at = uint32_t(q.nh + (first + b0 * kLgUnroll * kLgThreads) * kN);
+      act = ((uint64_t((o16 << 16) | low) << 32) | (0xFFFFFFFFu - at)) > kth;
+    }
+    if (__any_sync(0xffffffffu, act)) {
+      for (int b = b0; __any_sync(0xffffffffu, act && b < b1); ++b) {
+        uint4 v[kLgUnroll];
+#pragma unroll
+        for (int w = 0; w < kLgUnroll; ++w) {
+          const int i = first + (b * kLgUnroll + w) * kLgThreads;
+          v[w] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
+          if (act && b < b1 && i < q.v1) v[w] = ldg_stream(q.zv + i);
+        }
+#pragma unroll
+        for (int w = 0; w < kLgUnroll; ++w) {
+          const float vm = E::pmax_final(E::pmax(E::pmax(v[w].x, v[w].y), E::pmax(v[w].z, v[w].w)));
+          if (!__any_sync(0xffffffffu, uint32_t(top_key(vm, 0) >> 32) >= thr)) continue;
+          float f[kN];
+          E::widen(v[w], f);
+          const int i = first + (b * kLgUnroll + w) * kLgThreads;
+#pragma unroll
+          for (int e = 0; e < kN; ++e) offer(f[e], uint32_t(q.nh + i * kN + e), true);
+        }
+      }
+    }
+    __syncwarp();
+  }
+  __syncthreads();  // the count is 0
+  // the warps' lists one behind the other; their order does not matter
+  const int have = __popc(__ballot_sync(0xffffffffu, lane < K && mine != 0));
+  int to = 0;
+  if (lane == 0 && have) to = atomicAdd(count, have);
+  to = __shfl_sync(0xffffffffu, to, 0);
+  if (lane < have) out[to + lane] = mine;
+  __syncthreads();
+}
+
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsParams p) {
   using E = Elem<T>;
   constexpr int kN = E::kN;
-  extern __shared__ __align__(16) uint16_t gmax[];  // TOP: [slots][kLgThreads] group maxima, the warps' queues
+  extern __shared__ __align__(16) uint16_t gmax[];  // TOP: [slots][kLgThreads] group maxima, the items
   __shared__ RowTotal sh_tot[kLgWarps];
   __shared__ RowTotal sh_cl[kLgMaxCluster];
-  __shared__ uint64_t sh_list[kLgWarps * kLgMaxTop];
-  __shared__ uint64_t sh_cl_list[kLgMaxCluster * kLgMaxTop];
+  __shared__ __align__(16) uint64_t sh_list[kLgCands];  // kLgCands = kLgWarps * kLgMaxTop
+  __shared__ __align__(16) uint64_t sh_cl_list[kLgMaxCluster * kLgMaxTop];
   __shared__ uint64_t sh_best[kLgMaxTop];
   __shared__ uint32_t sh_thr[kLgWarps];
-  __shared__ int sh_count;
+  __shared__ int sh_count, sh_items;
+  uint16_t* items = gmax + p.slots * kLgThreads;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t nc, rank;
@@ -534,7 +631,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
       }
     }
     if (lane == 0) sh_thr[warp] = jth;
-    if (tid == 0) sh_count = 0;
+    if (tid == 0) sh_count = sh_items = 0;
     if (tid < kLgMaxTop) sh_best[tid] = 0;
     __syncthreads();
     uint32_t thr = with ? 0xFFFFFFFFu : 0u;
@@ -543,79 +640,42 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     if (thr <= uint32_t(top_key(p.clamp, 0) >> 32)) thr = none + 1;
     const uint32_t thr16 = thr > none + 1 ? thr >> 16 : 0;
 
-    uint64_t mine = 0;  // lane i: the warp's i-th best entry so far
-    uint64_t kth = 0;
-    auto offer = [&](float v, uint32_t idx, bool in) {
+    // groups to read again
+    for (int k = 0; k < g; ++k) {
+      if (gmax[k * kLgThreads + tid] >= thr16) {
+        const int at = atomicAdd(&sh_items, 1);
+        if (at < kLgItems) items[at] = uint16_t(k * kLgThreads + tid);
+      }
+    }
+    auto offer = [&](float v, uint32_t idx) {
       const uint64_t key = top_key(v, idx);
-      uint32_t b = __ballot_sync(0xffffffffu, in && v > -INFINITY && uint32_t(key >> 32) >= thr && key > kth);
-      if (b) {
-        do {
-          const int src = __ffs(b) - 1;
-          b &= b - 1;
-          top_insert(mine, __shfl_sync(0xffffffffu, key, src), lane);
-        } while (b);
-        kth = __shfl_sync(0xffffffffu, mine, K - 1);
+      if (uint32_t(key >> 32) >= thr && v > -INFINITY) {
+        const int at = atomicAdd(&sh_count, 1);
+        if (at < kLgCands) sh_list[at] = key;
       }
     };
-    if (warp == 0 && rank == nc - 1) offer(zs, uint32_t(tid < q.nh ? tid : q.nv * kN + tid), tid < nsingle);
-    uint16_t* queue = gmax + p.slots * kLgThreads + warp * kLgQueue;
-    int nq = 0;
-    for (int k = 0; k < g || nq > 0;) {
-      while (k < g && nq <= kLgQueue - 32) {
-        const bool in = gmax[k * kLgThreads + tid] >= thr16;
-        const uint32_t b = __ballot_sync(0xffffffffu, in);
-        if (in) queue[nq + __popc(b & ((1u << lane) - 1u))] = uint16_t(k * 32 + lane);
-        nq += __popc(b);
-        ++k;
-      }
-      __syncwarp();
-      const int take = min(nq, 32);
-      const int item = lane < take ? queue[nq - take + lane] : -1;
-      nq -= take;
-      const int ig = item >> 5, il = item & 31;
-      const int b0 = ig * per, b1 = min(b0 + per, nb);
-      const int first = q.v0 + warp * 32 + il;  // vector u of batch b: first + (b * kLgUnroll + u) * kLgThreads
-      bool act = item >= 0;
-      if (act) {
-        // nothing in the group can enter when its largest possible value at its lowest index would not
-        const uint32_t o16 = gmax[ig * kLgThreads + warp * 32 + il];
-        const uint32_t low = E::kNegInf == 0xFF80FF80u && (o16 & 0x8000u) ? 0u : 0xFFFFu;
-        const uint32_t at = uint32_t(q.nh + (first + b0 * kLgUnroll * kLgThreads) * kN);
-        act = ((uint64_t((o16 << 16) | low) << 32) | (0xFFFFFFFFu - at)) > kth;
-      }
-      if (__any_sync(0xffffffffu, act)) {
-        for (int b = b0; __any_sync(0xffffffffu, act && b < b1); ++b) {
-          uint4 v[kLgUnroll];
+    if (rank == nc - 1 && tid < nsingle) offer(zs, uint32_t(tid < q.nh ? tid : q.nv * kN + tid));
+    __syncthreads();
+    const int n_items = sh_items;
+    if (n_items <= kLgItems) {
+      const int vecs = per * kLgUnroll;  // of a group
+      for (int i = tid; i < n_items * vecs; i += kLgThreads) {
+        const int it = items[i / vecs], n = (it / kLgThreads) * vecs + i % vecs;
+        const int at = q.v0 + n * kLgThreads + it % kLgThreads;
+        if (at < q.v1) {
+          float f[kN];
+          E::widen(ldg_stream(q.zv + at), f);
 #pragma unroll
-          for (int w = 0; w < kLgUnroll; ++w) {
-            const int i = first + (b * kLgUnroll + w) * kLgThreads;
-            v[w] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
-            if (act && b < b1 && i < q.v1) v[w] = ldg_stream(q.zv + i);
-          }
-#pragma unroll
-          for (int w = 0; w < kLgUnroll; ++w) {
-            const float vm = E::pmax_final(E::pmax(E::pmax(v[w].x, v[w].y), E::pmax(v[w].z, v[w].w)));
-            if (!__any_sync(0xffffffffu, uint32_t(top_key(vm, 0) >> 32) >= thr)) continue;
-            float f[kN];
-            E::widen(v[w], f);
-            const int i = first + (b * kLgUnroll + w) * kLgThreads;
-#pragma unroll
-            for (int e = 0; e < kN; ++e) offer(f[e], uint32_t(q.nh + i * kN + e), true);
-          }
+          for (int e = 0; e < kN; ++e) offer(f[e], uint32_t(q.nh + at * kN + e));
         }
       }
-      __syncwarp();
     }
-    // the warps' lists one behind the other; their order does not matter
-    const int have = __popc(__ballot_sync(0xffffffffu, lane < K && mine != 0));
-    int to = 0;
-    if (lane == 0 && have) to = atomicAdd(&sh_count, have);
-    to = __shfl_sync(0xffffffffu, to, 0);
-    if (lane < have) sh_list[to + lane] = mine;
-  }
-  __syncthreads();
-  if (TOP) {
+    __syncthreads();
+    if (n_items > kLgItems || sh_count > kLgCands) {
+      top_by_lists<T>(p, q, nb, g, thr, thr16, zs, rank == nc - 1 && tid < nsingle, gmax, sh_list, &sh_count);
+    }
     top_rank(sh_list, sh_count, K, sh_best);
+  } else {
     __syncthreads();
   }
   tot = sh_tot[0];
@@ -639,9 +699,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     for (uint32_t w = 1; w < nc; ++w) tot = row_join(tot, sh_cl[w]);
     if (TOP) {
       if (tid < kLgMaxTop) sh_best[tid] = 0;
-      __syncthreads();
       top_rank(sh_cl_list, int(nc) * K, K, sh_best);
-      __syncthreads();
     }
   }
 

@@ -689,7 +689,7 @@ static int launch_logits_fwd(LogitsParams lp, cudaStream_t st) {
     const int span = kLgThreads * kLgUnroll, nb = (nv / nc + 1 + span - 1) / span;
     lp.per = nb > kLgMaxGroups ? (nb + kLgMaxGroups - 1) / kLgMaxGroups : 1;
     lp.slots = (nb + lp.per - 1) / lp.per;
-    smem = (size_t)lp.slots * kLgThreads * 2 + kLgWarps * kLgQueue * 2;
+    smem = ((size_t)lp.slots * kLgThreads + kLgItems) * 2;
   }
   auto kern = logits_fwd_kernel<T, TOP>;
   cudaLaunchConfig_t cfg;
