@@ -247,27 +247,49 @@ __device__ __forceinline__ void row_add(RowSums& r, const float (&f)[KN], float 
   }
 }
 
-__device__ __forceinline__ RowTotal row_join(const RowTotal& a, const RowTotal& b) {
-  RowTotal o;
-  o.R = fmaxf(a.R, b.R);
-  o.m = fmaxf(a.m, b.m);
-  const float da = fmaxf(a.R - o.R, kLgFloor), db = fmaxf(b.R - o.R, kLgFloor);
-  const float fa = ex2_approx(da), fb = ex2_approx(db);
-  o.s = fa * a.s + fb * b.s;
-  o.t = fa * fmaf(da, a.s, a.t) + fb * fmaf(db, b.s, b.t);
-  return o;
+// A float as a whole number of the same order.
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(uint32_t o) {
+  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+}
+__device__ __forceinline__ float warp_max(float v) {  // no NaN
+  return from_ordered(__reduce_max_sync(0xffffffffu, ordered(v)));
+}
+
+// Sums brought to the reference R.
+__device__ __forceinline__ void row_to(RowTotal& a, float R) {
+  const float d = fmaxf(a.R - R, kLgFloor), f = ex2_approx(d);
+  a.t = f * fmaf(d, a.s, a.t);
+  a.s = f * a.s;
+  a.R = R;
+}
+// The lanes' sums joined; every lane adds the same pairs, so all get the same bits.
+__device__ __forceinline__ RowTotal row_join_warp(RowTotal a) {
+  row_to(a, warp_max(a.R));
+  a.m = warp_max(a.m);
+#pragma unroll 1
+  for (int o = 16; o > 0; o >>= 1) {
+    a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
+    a.t += __shfl_xor_sync(0xffffffffu, a.t, o);
+  }
+  return a;
+}
+// The first n <= 32 sums of a list joined, by every warp.
+__device__ __forceinline__ RowTotal row_join_list(const RowTotal* list, int n) {
+  const int lane = threadIdx.x & 31;
+  RowTotal a = list[lane < n ? lane : 0];
+  if (lane >= n) a.s = a.t = 0.f;
+  return row_join_warp(a);
 }
 
 // Order of the alternatives: larger logit first, then the lower index.  0 = no entry.
 __device__ __forceinline__ uint64_t top_key(float v, uint32_t idx) {
-  const uint32_t u = __float_as_uint(v + 0.f);  // -0 counts as +0
-  const uint32_t o = u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
-  return (uint64_t(o) << 32) | (0xFFFFFFFFu - idx);
+  return (uint64_t(ordered(v + 0.f)) << 32) | (0xFFFFFFFFu - idx);  // -0 counts as +0
 }
-__device__ __forceinline__ float top_value(uint64_t key) {
-  const uint32_t o = uint32_t(key >> 32);
-  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
-}
+__device__ __forceinline__ float top_value(uint64_t key) { return from_ordered(uint32_t(key >> 32)); }
 
 // A warp's best entries, lane i the i-th best: insert `key` (uniform over the warp).
 __device__ __forceinline__ void top_insert(uint64_t& mine, uint64_t key, int lane) {
@@ -278,23 +300,27 @@ __device__ __forceinline__ void top_insert(uint64_t& mine, uint64_t key, int lan
   if (lane > pos) mine = up;
 }
 
-// out[rank] = the K best of entries[0..M); keys are distinct apart from empty ones (0).  All threads;
-// entries is 16-byte aligned and has room for a multiple of four.
+// out[rank] = the K best of entries[0..M), M <= 256, whose keys are distinct; the rest of out is 0.  Four
+// threads count for an entry while there are enough.  All threads; two barriers, the first before anything
+// is read.  entries has room for M + 3.
 __device__ __forceinline__ void top_rank(uint64_t* entries, int M, int K, uint64_t* out) {
-  if (threadIdx.x < 4 && (M & 3) && threadIdx.x < 4 - (M & 3)) entries[M + threadIdx.x] = 0;
+  const int tid = threadIdx.x;
+  if (tid < 3) entries[M + tid] = 0;
+  if (tid < kLgMaxTop) out[tid] = 0;
   __syncthreads();
-  const ulonglong2* two = reinterpret_cast<const ulonglong2*>(entries);
-  for (int i = threadIdx.x; i < M; i += kLgThreads) {
-    const uint64_t k = entries[i];
-    if (k == 0) continue;
-    int r = 0;
-#pragma unroll 4
-    for (int j = 0; j < (M + 3) / 4; ++j) {
-      const ulonglong2 a = two[2 * j], b = two[2 * j + 1];
-      r += (a.x > k) + (a.y > k) + (b.x > k) + (b.y > k);
-    }
-    if (r < K) out[r] = k;
+  const int ways = M <= kLgThreads / 4 ? 4 : 1;
+  const int i = tid / ways, part = tid % ways;
+  const uint64_t k = i < M ? entries[i] : 0;
+  int r = 0;
+  if (i < M) {
+#pragma unroll 2
+    for (int j = part; j < M; j += ways) r += entries[j] > k;
   }
+  if (ways == 4) {
+    r += __shfl_xor_sync(0xffffffffu, r, 1);
+    r += __shfl_xor_sync(0xffffffffu, r, 2);
+  }
+  if (i < M && part == 0 && r < K) out[r] = k;
   __syncthreads();
 }
 
@@ -339,8 +365,9 @@ __device__ __forceinline__ RowPart row_part(const LogitsParams& p, int64_t row, 
   if (q.nh > p.V) q.nh = p.V;
   q.nv = (p.V - q.nh) / kN;
   q.zv = reinterpret_cast<const uint4*>(zrow + q.nh);
-  q.v0 = int(int64_t(q.nv) * rank / nc);
-  q.v1 = int(int64_t(q.nv) * (rank + 1) / nc);
+  const int shift = 31 - __clz(nc);  // nc is a power of two
+  q.v0 = int((int64_t(q.nv) * rank) >> shift);
+  q.v1 = int((int64_t(q.nv) * (rank + 1)) >> shift);
   return q;
 }
 
@@ -486,8 +513,8 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   extern __shared__ __align__(16) uint16_t gmax[];  // TOP: [slots][kLgThreads] group maxima, the items
   __shared__ RowTotal sh_tot[kLgWarps];
   __shared__ RowTotal sh_cl[kLgMaxCluster];
-  __shared__ __align__(16) uint64_t sh_list[kLgCands];  // kLgCands = kLgWarps * kLgMaxTop
-  __shared__ __align__(16) uint64_t sh_cl_list[kLgMaxCluster * kLgMaxTop];
+  __shared__ uint64_t sh_list[kLgCands + 3];  // kLgCands = kLgWarps * kLgMaxTop = kLgMaxCluster * kLgMaxTop
+  __shared__ uint64_t sh_cl_list[kLgMaxCluster * kLgMaxTop];
   __shared__ uint64_t sh_best[kLgMaxTop];
   __shared__ uint32_t sh_thr[kLgWarps];
   __shared__ int sh_count, sh_items;
@@ -499,7 +526,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int K = p.K, V = p.V;
   const float c = p.scale * 1.4426950408889634f;
-  const int64_t row = blockIdx.x / nc;
+  const int64_t row = blockIdx.x >> (31 - __clz(nc));
   if (p.mask && p.mask[row] == 0) {
     if (rank == 0) {
       if (tid == 0) {
@@ -519,13 +546,8 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   if (nc > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 
   const T* zrow = reinterpret_cast<const T*>(p.z) + row * p.ld;
-  float z_target = 0.f;
-  bool bad_target = false;
-  if (rank == 0 && tid == 0 && p.token_logp) {
-    const int target = p.targets[row];
-    bad_target = target < 0 || target >= V;
-    if (!bad_target) z_target = E::one(zrow, target);
-  }
+  int target = 0;
+  if (rank == 0 && tid == 0 && p.token_logp) target = p.targets[row];
   const RowPart q = row_part<T>(p, row, rank, nc);
   const int nsingle = V - q.nv * kN;  // head and tail elements: the last CTA takes them
   const int nb = (q.v1 - q.v0 + kLgThreads * kLgUnroll - 1) / (kLgThreads * kLgUnroll);
@@ -548,6 +570,9 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     }
   };
   if (nb > 0) load(0, cur);
+  const bool bad_target = target < 0 || target >= V;
+  float z_target = 0.f;
+  if (rank == 0 && tid == 0 && p.token_logp && !bad_target) z_target = E::one(zrow, target);  // behind the first loads
   for (int b = 0; b < nb; ++b) {
     if (b + 1 < nb) load(b + 1, nxt);
     uint32_t pm = 0;
@@ -604,35 +629,22 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     tot.t = t0 + t1;
     tot.m = wmax;
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    RowTotal other;
-    other.R = __shfl_xor_sync(0xffffffffu, tot.R, o);
-    other.s = __shfl_xor_sync(0xffffffffu, tot.s, o);
-    other.t = __shfl_xor_sync(0xffffffffu, tot.t, o);
-    other.m = __shfl_xor_sync(0xffffffffu, tot.m, o);
-    // both partners form the same sum in the same order
-    tot = (lane & o) ? row_join(other, tot) : row_join(tot, other);
-  }
+  tot = row_join_warp(tot);
   if (lane == 0) sh_tot[warp] = tot;
 
   // ---- top alternatives of this CTA's part
   if (TOP) {
     const uint32_t none = uint32_t(top_key(-INFINITY, 0) >> 32);  // -inf is no alternative
     const int with = min((q.v1 - q.v0 + 31) / 32, kLgWarps);      // warps with data
-    float left = tmax;
-    uint32_t jth = 0;
+    uint32_t left = ordered(tmax + 0.f), jth = 0;
     if (warp < with) {
       for (int n = (K + with - 1) / with; n > 0; --n) {
-        const uint32_t o = uint32_t(top_key(left, 0) >> 32);
-        jth = __reduce_max_sync(0xffffffffu, o);
-        const uint32_t who = __ballot_sync(0xffffffffu, o == jth);
-        if (lane == __ffs(who) - 1) left = -INFINITY;
+        jth = __reduce_max_sync(0xffffffffu, left);
+        if (left == jth) left = 0;  // equal ones together: the next is lower, which is safe
       }
     }
     if (lane == 0) sh_thr[warp] = jth;
     if (tid == 0) sh_count = sh_items = 0;
-    if (tid < kLgMaxTop) sh_best[tid] = 0;
     __syncthreads();
     uint32_t thr = with ? 0xFFFFFFFFu : 0u;
     for (int w = 0; w < with; ++w) thr = min(thr, sh_thr[w]);
@@ -678,9 +690,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   } else {
     __syncthreads();
   }
-  tot = sh_tot[0];
-#pragma unroll
-  for (int w = 1; w < kLgWarps; ++w) tot = row_join(tot, sh_tot[w]);
+  tot = row_join_list(sh_tot, kLgWarps);
 
   // ---- join the CTAs of the row in CTA 0
   if (nc > 1) {
@@ -695,11 +705,18 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     if (TOP && tid < K) st_cluster_u64(mapa_shared(smem_u32(&sh_cl_list[rank * K + tid]), 0), sh_best[tid]);
     cluster_sync_all();
     if (rank != 0) return;
-    tot = sh_cl[0];
-    for (uint32_t w = 1; w < nc; ++w) tot = row_join(tot, sh_cl[w]);
+    tot = row_join_list(sh_cl, int(nc));
     if (TOP) {
-      if (tid < kLgMaxTop) sh_best[tid] = 0;
-      top_rank(sh_cl_list, int(nc) * K, K, sh_best);
+      // as with the warps: at least K entries reach the smallest of the CTAs' j-th bests, j = ceil(K / nc)
+      uint64_t bound = ~0ull;
+      const int j = (K + int(nc) - 1) >> (31 - __clz(nc));
+      for (uint32_t w = 0; w < nc; ++w) bound = min(bound, sh_cl_list[w * K + j - 1]);
+      const uint64_t key = tid < int(nc) * K ? sh_cl_list[tid] : 0;
+      if (tid == 0) sh_count = 0;
+      __syncthreads();
+      if (key != 0 && key >= bound) sh_list[atomicAdd(&sh_count, 1)] = key;
+      __syncthreads();
+      top_rank(sh_list, sh_count, K, sh_best);
     }
   }
 
