@@ -26,7 +26,6 @@
 namespace oapl {
 
 constexpr int kLgThreads = 256;
-constexpr int kLgWarps = kLgThreads / 32;
 constexpr int kLgUnroll = 4;       // 16-byte vectors that a thread loads together (a batch)
 constexpr int kLgMaxGroups = 32;   // groups of a thread whose maxima are kept for the top alternatives
 constexpr int kLgMaxTop = 32;
@@ -303,24 +302,29 @@ __device__ __forceinline__ void top_insert(uint64_t& mine, uint64_t key, int lan
 // out[rank] = the K best of entries[0..M), M <= 256, whose keys are distinct; the rest of out is 0.  Four
 // threads count for an entry while there are enough.  All threads; two barriers, the first before anything
 // is read.  entries has room for M + 3.
+template <int NT>
 __device__ __forceinline__ void top_rank(uint64_t* entries, int M, int K, uint64_t* out) {
   const int tid = threadIdx.x;
   if (tid < 3) entries[M + tid] = 0;
   if (tid < kLgMaxTop) out[tid] = 0;
   __syncthreads();
-  const int ways = M <= kLgThreads / 4 ? 4 : 1;
-  const int i = tid / ways, part = tid % ways;
-  const uint64_t k = i < M ? entries[i] : 0;
-  int r = 0;
-  if (i < M) {
+  const int ways = M <= NT / 4 ? 4 : 1;
+  const int part = tid % ways;
+#pragma unroll 1
+  for (int i0 = 0; i0 < M; i0 += NT / ways) {
+    const int i = i0 + tid / ways;
+    const uint64_t k = i < M ? entries[i] : 0;
+    int r = 0;
+    if (i < M) {
 #pragma unroll 2
-    for (int j = part; j < M; j += ways) r += entries[j] > k;
+      for (int j = part; j < M; j += ways) r += entries[j] > k;
+    }
+    if (ways == 4) {
+      r += __shfl_xor_sync(0xffffffffu, r, 1);
+      r += __shfl_xor_sync(0xffffffffu, r, 2);
+    }
+    if (i < M && part == 0 && r < K) out[r] = k;
   }
-  if (ways == 4) {
-    r += __shfl_xor_sync(0xffffffffu, r, 1);
-    r += __shfl_xor_sync(0xffffffffu, r, 2);
-  }
-  if (i < M && part == 0 && r < K) out[r] = k;
   __syncthreads();
 }
 
@@ -372,13 +376,13 @@ __device__ __forceinline__ RowPart row_part(const LogitsParams& p, int64_t row, 
 }
 
 // A whole row by one CTA, any logits: the exact maximum m first, then x = c (z - m).  All threads get
-// {m, sum 2^x, sum 2^x x}; sh: kLgWarps entries.
-template <typename T>
+// {m, sum 2^x, sum 2^x x}; sh: NT / 32 entries.
+template <typename T, int NT>
 __device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* sh) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   float m = -INFINITY;
   bool nan = false;
-  for (int i = tid; i < V; i += kLgThreads) {
+  for (int i = tid; i < V; i += NT) {
     const float v = Elem<T>::one(z, i);
     nan |= v != v;
     m = fmaxf(m, v);
@@ -388,13 +392,13 @@ __device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* 
   __syncthreads();
   if (lane == 0) sh[warp].m = m;
   nan = __syncthreads_or(nan);
-  for (int w = 0; w < kLgWarps; ++w) m = fmaxf(m, sh[w].m);
+  for (int w = 0; w < (NT / 32); ++w) m = fmaxf(m, sh[w].m);
   RowTotal r;
   r.R = 0.f;
   r.m = m;
   r.s = r.t = 0.f;
   if (!nan && m > -INFINITY) {
-    for (int i = tid; i < V; i += kLgThreads) {
+    for (int i = tid; i < V; i += NT) {
       const float x = max_nan((Elem<T>::one(z, i) - m) * c, kLgFloor);
       const float e = ex2_approx(x);
       r.s += e;
@@ -413,7 +417,7 @@ __device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* 
   if (lane == 0) sh[warp] = r;
   __syncthreads();
   r = sh[0];
-  for (int w = 1; w < kLgWarps; ++w) {
+  for (int w = 1; w < (NT / 32); ++w) {
     r.s += sh[w].s;
     r.t += sh[w].t;
   }
@@ -423,14 +427,14 @@ __device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* 
 
 // The K best entries of every warp's part of the row through lists that are kept sorted over the lanes,
 // whatever the ties: `out` gets the lists one behind the other, *count their length.  All threads.
-template <typename T>
+template <typename T, int NT>
 __device__ __noinline__ void top_by_lists(const LogitsParams& p, const RowPart& q, int nb, int g, uint32_t thr,
                                           uint32_t thr16, float zs, bool has_single, const uint16_t* gmax,
                                           uint64_t* out, int* count) {
   using E = Elem<T>;
   constexpr int kN = E::kN;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, K = p.K, per = p.per;
-  __shared__ uint16_t sh_queue[kLgWarps * kLgQueue];
+  __shared__ uint16_t sh_queue[(NT / 32) * kLgQueue];
   uint16_t* queue = sh_queue + warp * kLgQueue;
   __syncthreads();  // everybody has read the count
   if (tid == 0) *count = 0;
@@ -452,7 +456,7 @@ __device__ __noinline__ void top_by_lists(const LogitsParams& p, const RowPart& 
   int nq = 0;
   for (int k = 0; k < g || nq > 0;) {
     while (k < g && nq <= kLgQueue - 32) {
-      const bool in = gmax[k * kLgThreads + tid] >= thr16;
+      const bool in = gmax[k * NT + tid] >= thr16;
       const uint32_t b = __ballot_sync(0xffffffffu, in);
       if (in) queue[nq + __popc(b & ((1u << lane) - 1u))] = uint16_t(k * 32 + lane);
       nq += __popc(b);
@@ -464,13 +468,13 @@ __device__ __noinline__ void top_by_lists(const LogitsParams& p, const RowPart& 
     nq -= take;
     const int ig = item >> 5, il = item & 31;
     const int b0 = ig * per, b1 = min(b0 + per, nb);
-    const int first = q.v0 + warp * 32 + il;  // vector u of batch b: first + (b * kLgUnroll + u) * kLgThreads
+    const int first = q.v0 + warp * 32 + il;  // vector u of batch b: first + (b * kLgUnroll + u) * NT
     bool act = item >= 0;
     if (act) {
       // nothing in the group can enter when its largest possible value at its lowest index would not
-      const uint32_t o16 = gmax[ig * kLgThreads + warp * 32 + il];
+      const uint32_t o16 = gmax[ig * NT + warp * 32 + il];
       const uint32_t low = E::kNegInf == 0xFF80FF80u && (o16 & 0x8000u) ? 0u : 0xFFFFu;
-      const uint32_t at = uint32_t(q.nh + (first + b0 * kLgUnroll * kLgThreads) * kN);
+      const uint32_t at = uint32_t(q.nh + (first + b0 * kLgUnroll * NT) * kN);
       act = ((uint64_t((o16 << 16) | low) << 32) | (0xFFFFFFFFu - at)) > kth;
     }
     if (__any_sync(0xffffffffu, act)) {
@@ -478,7 +482,7 @@ __device__ __noinline__ void top_by_lists(const LogitsParams& p, const RowPart& 
         uint4 v[kLgUnroll];
 #pragma unroll
         for (int w = 0; w < kLgUnroll; ++w) {
-          const int i = first + (b * kLgUnroll + w) * kLgThreads;
+          const int i = first + (b * kLgUnroll + w) * NT;
           v[w] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
           if (act && b < b1 && i < q.v1) v[w] = ldg_stream(q.zv + i);
         }
@@ -488,7 +492,7 @@ __device__ __noinline__ void top_by_lists(const LogitsParams& p, const RowPart& 
           if (!__any_sync(0xffffffffu, uint32_t(top_key(vm, 0) >> 32) >= thr)) continue;
           float f[kN];
           E::widen(v[w], f);
-          const int i = first + (b * kLgUnroll + w) * kLgThreads;
+          const int i = first + (b * kLgUnroll + w) * NT;
 #pragma unroll
           for (int e = 0; e < kN; ++e) offer(f[e], uint32_t(q.nh + i * kN + e), true);
         }
@@ -506,19 +510,19 @@ __device__ __noinline__ void top_by_lists(const LogitsParams& p, const RowPart& 
   __syncthreads();
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsParams p) {
+template <typename T, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) logits_fwd_kernel(const LogitsParams p) {
   using E = Elem<T>;
   constexpr int kN = E::kN;
-  extern __shared__ __align__(16) uint16_t gmax[];  // TOP: [slots][kLgThreads] group maxima, the items
-  __shared__ RowTotal sh_tot[kLgWarps];
+  extern __shared__ __align__(16) uint16_t gmax[];  // TOP: [slots][NT] group maxima, the items
+  __shared__ RowTotal sh_tot[(NT / 32)];
   __shared__ RowTotal sh_cl[kLgMaxCluster];
-  __shared__ uint64_t sh_list[kLgCands + 3];  // kLgCands = kLgWarps * kLgMaxTop = kLgMaxCluster * kLgMaxTop
+  __shared__ uint64_t sh_list[kLgCands + 3];  // kLgCands = kLgMaxCluster * kLgMaxTop, no less than NT / 32 * kLgMaxTop
   __shared__ uint64_t sh_cl_list[kLgMaxCluster * kLgMaxTop];
   __shared__ uint64_t sh_best[kLgMaxTop];
-  __shared__ uint32_t sh_thr[kLgWarps];
+  __shared__ uint32_t sh_thr[(NT / 32)];
   __shared__ int sh_count, sh_items;
-  uint16_t* items = gmax + p.slots * kLgThreads;
+  uint16_t* items = gmax + p.slots * NT;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t nc, rank;
@@ -550,7 +554,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   if (rank == 0 && tid == 0 && p.token_logp) target = p.targets[row];
   const RowPart q = row_part<T>(p, row, rank, nc);
   const int nsingle = V - q.nv * kN;  // head and tail elements: the last CTA takes them
-  const int nb = (q.v1 - q.v0 + kLgThreads * kLgUnroll - 1) / (kLgThreads * kLgUnroll);
+  const int nb = (q.v1 - q.v0 + NT * kLgUnroll - 1) / (NT * kLgUnroll);
   const int per = p.per;
   float zs = -INFINITY;
   if (rank == nc - 1 && tid < nsingle) zs = E::one(zrow, tid < q.nh ? tid : q.nv * kN + tid);
@@ -564,7 +568,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   auto load = [&](int b, uint4 (&v)[kLgUnroll]) {
 #pragma unroll
     for (int u = 0; u < kLgUnroll; ++u) {
-      const int i = q.v0 + (b * kLgUnroll + u) * kLgThreads + tid;
+      const int i = q.v0 + (b * kLgUnroll + u) * NT + tid;
       v[u] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
       if (i < q.v1) v[u] = ldg_stream(q.zv + i);
     }
@@ -589,7 +593,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     if (TOP) {
       gm = fmaxf(gm, bm);
       if (++in_group == per) {
-        gmax[g * kLgThreads + tid] = uint16_t(top_key(gm, 0) >> 48);
+        gmax[g * NT + tid] = uint16_t(top_key(gm, 0) >> 48);
         gm = p.clamp;
         in_group = 0;
         ++g;
@@ -606,7 +610,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     for (int u = 0; u < kLgUnroll; ++u) cur[u] = nxt[u];
   }
   if (TOP && in_group) {
-    gmax[g * kLgThreads + tid] = uint16_t(top_key(gm, 0) >> 48);
+    gmax[g * NT + tid] = uint16_t(top_key(gm, 0) >> 48);
     ++g;
   }
   float wmax = tmax;
@@ -635,7 +639,7 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
   // ---- top alternatives of this CTA's part
   if (TOP) {
     const uint32_t none = uint32_t(top_key(-INFINITY, 0) >> 32);  // -inf is no alternative
-    const int with = min((q.v1 - q.v0 + 31) / 32, kLgWarps);      // warps with data
+    const int with = min((q.v1 - q.v0 + 31) / 32, (NT / 32));      // warps with data
     uint32_t left = ordered(tmax + 0.f), jth = 0;
     if (warp < with) {
       for (int n = (K + with - 1) / with; n > 0; --n) {
@@ -653,11 +657,13 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     const uint32_t thr16 = thr > none + 1 ? thr >> 16 : 0;
 
     // groups to read again
-    for (int k = 0; k < g; ++k) {
-      if (gmax[k * kLgThreads + tid] >= thr16) {
-        const int at = atomicAdd(&sh_items, 1);
-        if (at < kLgItems) items[at] = uint16_t(k * kLgThreads + tid);
-      }
+    uint32_t hot = 0;
+#pragma unroll 8
+    for (int k = 0; k < g; ++k) hot |= uint32_t(gmax[k * NT + tid] >= thr16) << k;
+    while (hot) {
+      const int k = __ffs(hot) - 1, at = atomicAdd(&sh_items, 1);
+      hot &= hot - 1;
+      if (at < kLgItems) items[at] = uint16_t(k * NT + tid);
     }
     auto offer = [&](float v, uint32_t idx) {
       const uint64_t key = top_key(v, idx);
@@ -671,9 +677,9 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     const int n_items = sh_items;
     if (n_items <= kLgItems) {
       const int vecs = per * kLgUnroll;  // of a group
-      for (int i = tid; i < n_items * vecs; i += kLgThreads) {
-        const int it = items[i / vecs], n = (it / kLgThreads) * vecs + i % vecs;
-        const int at = q.v0 + n * kLgThreads + it % kLgThreads;
+      for (int i = tid; i < n_items * vecs; i += NT) {
+        const int it = items[i / vecs], n = (it / NT) * vecs + i % vecs;
+        const int at = q.v0 + n * NT + it % NT;
         if (at < q.v1) {
           float f[kN];
           E::widen(ldg_stream(q.zv + at), f);
@@ -684,13 +690,13 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
     }
     __syncthreads();
     if (n_items > kLgItems || sh_count > kLgCands) {
-      top_by_lists<T>(p, q, nb, g, thr, thr16, zs, rank == nc - 1 && tid < nsingle, gmax, sh_list, &sh_count);
+      top_by_lists<T, NT>(p, q, nb, g, thr, thr16, zs, rank == nc - 1 && tid < nsingle, gmax, sh_list, &sh_count);
     }
-    top_rank(sh_list, sh_count, K, sh_best);
+    top_rank<NT>(sh_list, sh_count, K, sh_best);
   } else {
     __syncthreads();
   }
-  tot = row_join_list(sh_tot, kLgWarps);
+  tot = row_join_list(sh_tot, (NT / 32));
 
   // ---- join the CTAs of the row in CTA 0
   if (nc > 1) {
@@ -716,14 +722,14 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_fwd_kernel(const LogitsP
       __syncthreads();
       if (key != 0 && key >= bound) sh_list[atomicAdd(&sh_count, 1)] = key;
       __syncthreads();
-      top_rank(sh_list, sh_count, K, sh_best);
+      top_rank<NT>(sh_list, sh_count, K, sh_best);
     }
   }
 
   // ---- results
   const float ln2 = 0.6931471805599453f;
   const bool plain = fabsf(tot.m * c) < kLgPlainX && (tot.m - p.clamp) * c > 1000.f;  // the same for all threads
-  if (!plain) tot = row_slow<T>(zrow, V, c, sh_tot);
+  if (!plain) tot = row_slow<T, NT>(zrow, V, c, sh_tot);
   // no finite logit: every probability is 0, lse = -inf, nothing to choose from
   const bool empty = tot.m == -INFINITY && tot.s == 0.f;
   const bool broken = !empty && !(tot.m > -INFINITY && tot.m < INFINITY && tot.s > 0.f && tot.s < INFINITY);
