@@ -760,7 +760,7 @@ static int launch_quantize(const QuantParams& qp, bool e5, bool block, bool turn
     case 6: kern = quantize_kernel<T, 1, true, false>; break;
     default: kern = quantize_kernel<T, 1, true, true>; break;
   }
-  kern<<<(unsigned)grid, kQtThreads, 0, st>>>(qp);
+  kern<<<(unsigned)grid, kQtGroups * kQtTile / Elem<T>::kN, 0, st>>>(qp);
   CKL();
   return OAPL_OK;
 }
