@@ -12,7 +12,7 @@
 // 128 x 256 accumulators: per warp 8 loads of 16 columns and 64 two-wide multiply-adds, so they fit
 // with room for scales that differ per column.
 // Warp 0 issues TMA loads, warp 1 owns TMEM and (in the leader) issues the MMAs, warp 2 copies the
-// scales of each K block to shared memory with cp.async, warps 3 to 10 are the epilogue: quadrant
+// scales of each K block to shared memory with cp.async, warps 4 to 11 are the epilogue: quadrant
 // warp & 3 of the TMEM lanes, one half of the columns each.
 #pragma once
 #include <cuda.h>
@@ -32,7 +32,11 @@ constexpr int kSmStageBytes = 2 * kSmHalf * kSmKB;
 constexpr int kSmScaleStages = 8;
 constexpr int kSmScaleFloats = kSmHalf + kSmTile;  // row scales of this CTA, column scales of the tile
 constexpr int kSmEpiWarps = 8;
-constexpr int kSmThreads = 32 * (3 + kSmEpiWarps);
+constexpr int kSmThreads = 32 * (4 + kSmEpiWarps);
+// Registers of a thread: 168 at launch (what 384 threads can have), then 56 for the four warps that move
+// data and 224 for the epilogue: 128 * 56 + 256 * 224 = 384 * 168.
+constexpr int kSmRegs = 168, kSmRegsLow = 56, kSmRegsHigh = 224;
+static_assert(128 * kSmRegsLow + 256 * kSmRegsHigh == kSmThreads * kSmRegs, "register split");
 constexpr int kSmOutPitch = 33;    // words per row of a warp's 32 x 32 output piece
 constexpr int kSmOutBytes = kSmEpiWarps * 32 * kSmOutPitch * 4;
 constexpr size_t kSmSmemBytes = size_t(kSmStages) * kSmStageBytes + kSmScaleStages * kSmScaleFloats * 4 +
@@ -71,15 +75,6 @@ __device__ __forceinline__ uint32_t make_idesc_f8(int m, int n, int e5_a, int e5
          | (uint32_t(e5_a) << 7)    // A format: 0 e4m3, 1 e5m2
          | (uint32_t(e5_b) << 10)   // B format
          | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
 }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool in) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
@@ -188,6 +183,8 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   const int nk = (p.K + kSmKB - 1) / kSmKB;
   int m0, n0;
 
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kSmRegsLow));
   if (warp == 0) {
     // ------------------------------------------------------------ operand loads
     if (lane == 0) {
@@ -271,12 +268,14 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+  }
   } else {
     // ------------------------------------------------------------ epilogue
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSmRegsHigh));
     const int quad = warp & 3;
-    const int half = (warp - 3) >> 2;  // columns [128 half, 128 half + 128)
+    const int half = (warp - 4) >> 2;  // columns [128 half, 128 half + 128)
     const uint32_t tlane = tmem_base + (uint32_t(quad * 32) << 16) + half * 128;
-    float* piece = reinterpret_cast<float*>(smem + kOutOff) + (warp - 3) * 32 * kSmOutPitch;
+    float* piece = reinterpret_cast<float*>(smem + kOutOff) + (warp - 4) * 32 * kSmOutPitch;
     uint32_t it = 0;
     bool ok = true;
     for (int j = 0; ok && scaled_tile(p, j, m0, n0); ++j) {
@@ -297,30 +296,33 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         const float f = PERCOL ? fa : fa * sc[kSmHalf + half];
         const uint64_t f2 = pack2(f, f);
         const uint32_t ta = tlane + buf * kSmTile;
-        uint32_t r[2][16];
-        tmem_ld16(ta, r[0]);
+        uint32_t ra[32], rb[32];
+        auto add = [&](const uint32_t (&r)[32], int c) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          tmem_ld_wait();
-          if (c < 7) {
-            tmem_ld16(ta + (c + 1) * 16, r[(c + 1) & 1]);
-          } else {
-            // the accumulator is in registers: hand it back
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(mapa_shared(tempty_bar(buf), 0));
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint64_t v = pack2(__uint_as_float(r[c & 1][2 * i]), __uint_as_float(r[c & 1][2 * i + 1]));
+          for (int i = 0; i < 16; ++i) {
+            const uint64_t v = pack2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
             if (PERCOL) {
-              const uint64_t g = *reinterpret_cast<const uint64_t*>(sc + kSmHalf + half * 128 + c * 16 + 2 * i);
-              acc[c * 8 + i] = fma2(v, mul2(f2, g), acc[c * 8 + i]);
+              const uint64_t g = *reinterpret_cast<const uint64_t*>(sc + kSmHalf + half * 128 + c * 32 + 2 * i);
+              acc[c * 16 + i] = fma2(v, mul2(f2, g), acc[c * 16 + i]);
             } else {
-              acc[c * 8 + i] = fma2(v, f2, acc[c * 8 + i]);
+              acc[c * 16 + i] = fma2(v, f2, acc[c * 16 + i]);
             }
           }
-        }
+        };
+        tmem_ld32(ta, ra);
+        tmem_ld32(ta + 32, rb);
+        tmem_ld_wait();
+        add(ra, 0);
+        tmem_ld32(ta + 64, ra);
+        add(rb, 1);
+        tmem_ld32(ta + 96, rb);
+        tmem_ld_wait();
+        // the accumulator is in registers: hand it back
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(mapa_shared(tempty_bar(buf), 0));
+        add(ra, 2);
+        add(rb, 3);
         __syncwarp();
         if (lane == 0) mbar_arrive(sempty_bar(s));
       }
