@@ -8,12 +8,13 @@
 // tensor cores fill the other accumulator.
 //
 // CTA pairs (cta_group::2) share a 256 x 256 tile; a K block is 128 bytes, one swizzle row, and takes
-// the tensor cores about 512 cycles per pair.  In that time the eight epilogue warps of a CTA move
-// 128 x 256 accumulators: per warp 8 loads of 16 columns and 64 two-wide multiply-adds, so they fit
-// with room for scales that differ per column.
-// Warp 0 issues TMA loads, warp 1 owns TMEM and (in the leader) issues the MMAs, warp 2 copies the
-// scales of each K block to shared memory with cp.async, warps 4 to 11 are the epilogue: quadrant
-// warp & 3 of the TMEM lanes, one half of the columns each.
+// the tensor cores about 512 cycles per pair.  Two things bound it: the hand-over of the two accumulators
+// (a K block every 670 cycles with an epilogue that does nothing) and the epilogue warps' way through a block,
+// a chain of waits that more warps with fewer columns each shorten; in long calls, the power limit.
+// Warp 0 issues TMA loads, warp 1 owns TMEM and (in the leader) issues the MMAs, warp 2 copies the scales to
+// shared memory a few K blocks ahead (cp.async).  It arrives on the accumulator's barrier as the tensor cores
+// do, so the epilogue waits once per block.  Warps 4 to 11 are the epilogue: quadrant warp & 3 of the TMEM
+// lanes, one half of the columns each.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -29,19 +30,28 @@ constexpr int kSmHalf = 128;       // rows of A, and of B, that a CTA loads
 constexpr int kSmKB = 128;         // K values (bytes) of a block
 constexpr int kSmStages = 5;
 constexpr int kSmStageBytes = 2 * kSmHalf * kSmKB;
-constexpr int kSmScaleStages = 8;
-constexpr int kSmScaleFloats = kSmHalf + kSmTile;  // row scales of this CTA, column scales of the tile
+constexpr int kSmSlots = 16;       // K blocks whose scales have room in shared memory
+constexpr int kSmAhead = 6;        // K blocks that their copies run ahead
+constexpr int kSmSlotFloats = kSmHalf + kSmTile;  // row scales of this CTA, column scales of the tile
+constexpr int kSmFree = 4;         // the epilogue frees slots in fours
 constexpr int kSmEpiWarps = 8;
 constexpr int kSmThreads = 32 * (4 + kSmEpiWarps);
-// Registers of a thread: 168 at launch (what 384 threads can have), then 56 for the four warps that move
-// data and 224 for the epilogue: 128 * 56 + 256 * 224 = 384 * 168.
-constexpr int kSmRegs = 168, kSmRegsLow = 56, kSmRegsHigh = 224;
-static_assert(128 * kSmRegsLow + 256 * kSmRegsHigh == kSmThreads * kSmRegs, "register split");
-constexpr int kSmOutPitch = 33;    // words per row of a warp's 32 x 32 output piece
+constexpr int kSmOutCols = 32;     // columns of a warp's output piece
+constexpr int kSmOutPitch = kSmOutCols + 1;
 constexpr int kSmOutBytes = kSmEpiWarps * 32 * kSmOutPitch * 4;
-constexpr size_t kSmSmemBytes = size_t(kSmStages) * kSmStageBytes + kSmScaleStages * kSmScaleFloats * 4 +
+constexpr size_t kSmSmemBytes = size_t(kSmStages) * kSmStageBytes + kSmSlots * kSmSlotFloats * 4 +
                                 kSmOutBytes + 1024 /*align*/ + 512 /*barriers*/;
 static_assert(kSmSmemBytes <= 227 * 1024, "shared memory of a CTA");
+// Registers of a thread: 168 at launch (what 384 threads can have), then few for the four warps that move data
+// and the rest for the epilogue, whose loop holds 192 values: 128 low + 256 high = 384 * 168.  Scales per column
+// need more in warp 2.  (4096 x 152064 x 3584: 2.15 ms with 24 / 240, 2.27 with 40 / 232, 2.5 with 56 / 224, where
+// the loop spills; 8192^3 with a scale per column 0.78 and 0.74 ms.)
+constexpr int kSmRegs = 168;
+constexpr int sm_regs_low(bool percol) { return percol ? 40 : 24; }
+constexpr int sm_regs_high(bool percol) { return percol ? 232 : 240; }
+static_assert(128 * sm_regs_low(true) + 256 * sm_regs_high(true) == kSmThreads * kSmRegs &&
+                  128 * sm_regs_low(false) + 256 * sm_regs_high(false) == kSmThreads * kSmRegs,
+              "register split");
 
 enum { OUT_BF16 = 0, OUT_F16 = 1, OUT_F32 = 2 };
 
@@ -70,18 +80,24 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+// mbar_wait by a whole warp, with one answer for all lanes
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
 __device__ __forceinline__ uint32_t make_idesc_f8(int m, int n, int e5_a, int e5_b) {
   return (1u << 4)                  // D format f32
          | (uint32_t(e5_a) << 7)    // A format: 0 e4m3, 1 e5m2
          | (uint32_t(e5_b) << 10)   // B format
          | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
 }
-__device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool in) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(in ? 4 : 0) : "memory");
-}
-// one arrival on `bar` once all cp.async of this thread so far have landed
-__device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void cp_async4(uint32_t dst, const float* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
 // Tile number t: groups of `group` tiles along M, inside a group M fastest, so that the tiles in work at
@@ -138,18 +154,17 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (base - raw);
   constexpr uint32_t kScaleOff = kSmStages * kSmStageBytes;
-  constexpr uint32_t kOutOff = kScaleOff + kSmScaleStages * kSmScaleFloats * 4;
+  constexpr uint32_t kOutOff = kScaleOff + kSmSlots * kSmSlotFloats * 4;
   constexpr uint32_t kBarOff = kOutOff + kSmOutBytes;
   float* scales = reinterpret_cast<float*>(smem + kScaleOff);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kBarOff);
   const uint32_t bar0 = base + kBarOff;
   auto full_bar = [&](int s) { return bar0 + 8u * s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (kSmStages + s); };
-  auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * kSmStages + b); };
-  auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * kSmStages + 2 + b); };
-  auto sfull_bar = [&](int s) { return bar0 + 8u * (2 * kSmStages + 4 + s); };
-  auto sempty_bar = [&](int s) { return bar0 + 8u * (2 * kSmStages + 4 + kSmScaleStages + s); };
-  constexpr int kBars = 2 * kSmStages + 4 + 2 * kSmScaleStages;
+  auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * kSmStages + b); };       // accumulator and scales ready
+  auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * kSmStages + 2 + b); };  // accumulator handed back
+  auto sempty_bar = [&](int h) { return bar0 + 8u * (2 * kSmStages + 4 + h); };  // slots free again
+  constexpr int kBars = 2 * kSmStages + 4 + kSmSlots / kSmFree;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kBars + 1);
 
@@ -162,13 +177,10 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       mbar_init(empty_bar(s), 1);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(tfull_bar(b), 1);
+      mbar_init(tfull_bar(b), 2);                 // the tensor cores and warp 2
       mbar_init(tempty_bar(b), 2 * kSmEpiWarps);  // the leader's copy counts the warps of both CTAs
     }
-    for (int s = 0; s < kSmScaleStages; ++s) {
-      mbar_init(sfull_bar(s), 32);
-      mbar_init(sempty_bar(s), kSmEpiWarps);
-    }
+    for (int h = 0; h < kSmSlots / kSmFree; ++h) mbar_init(sempty_bar(h), kSmEpiWarps);
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tmA);
@@ -184,7 +196,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   int m0, n0;
 
   if (warp < 4) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kSmRegsLow));
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(sm_regs_low(PERCOL)));
   if (warp == 0) {
     // ------------------------------------------------------------ operand loads
     if (lane == 0) {
@@ -207,110 +219,136 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMAs (leader CTA)
-    if (lane == 0 && rank == 0) {
+    // the whole warp walks the loop and one elected lane issues, so that the descriptors stay uniform
+    if (rank == 0) {
       const uint32_t idesc = make_idesc_f8(kSmTile, kSmTile, p.e5_a, p.e5_b);
+      const uint64_t da0 = smem_desc_sw128(base, 16, 1024), db0 = smem_desc_sw128(base + kSmHalf * kSmKB, 16, 1024);
       uint32_t it = 0;
       bool ok = true;
       for (int j = 0; ok && scaled_tile(p, j, m0, n0); ++j) {
         for (int kb = 0; kb < nk; ++kb, ++it) {
           const int s = it % kSmStages, buf = it & 1;
-          if (!mbar_wait(tempty_bar(buf), ((it >> 1) & 1u) ^ 1u, abort_flag) ||
-              !mbar_wait(full_bar(s), (it / kSmStages) & 1u, abort_flag)) {
-            ok = false;
-            break;
-          }
+          ok = warp_wait(full_bar(s), (it / kSmStages) & 1u, abort_flag) &&
+               warp_wait(tempty_bar(buf), ((it >> 1) & 1u) ^ 1u, abort_flag);
+          if (!ok) break;
           tc_fence_after();
-          const uint32_t sa = base + s * kSmStageBytes, sb = sa + kSmHalf * kSmKB;
+          if (elect_one()) {
+            const uint64_t da = da0 + uint32_t(s * (kSmStageBytes >> 4)), db = db0 + uint32_t(s * (kSmStageBytes >> 4));
 #pragma unroll
-          for (int kk = 0; kk < kSmKB / 32; ++kk)
-            umma_f8(tmem_base + buf * kSmTile, smem_desc_sw128(sa + kk * 32, 16, 1024),
-                    smem_desc_sw128(sb + kk * 32, 16, 1024), idesc, kk ? 1u : 0u);
-          umma_commit_pair(empty_bar(s));
-          umma_commit_pair(tfull_bar(buf));
+            for (int kk = 0; kk < kSmKB / 32; ++kk)
+              umma_f8(tmem_base + buf * kSmTile, da + 2 * kk, db + 2 * kk, idesc, kk ? 1u : 0u);
+            umma_commit_pair(tfull_bar(buf));
+            umma_commit_pair(empty_bar(s));
+          }
+          __syncwarp();
         }
       }
     }
   } else if (warp == 2) {
     // ------------------------------------------------------------ scales
-    uint32_t it = 0;
+    constexpr int kCols = PERCOL ? kSmTile / 32 : 1;  // copies per lane for the columns
+    const int64_t da = p.ga == 1 ? 32 * p.sa_row : 0, db = 32 * p.sb_row;
+    const uint32_t dst0 = smem_u32(scales) + 4 * lane;
+    const float *pa = p.sa, *pb = p.sb;
+    int pj = 0, pkb = 0, left_m = 0, left_n = 0;  // left: rows of A and of B from this lane's first one on
+    auto seek = [&]() {
+      if (!scaled_tile(p, pj, m0, n0)) {
+        left_m = left_n = 0;
+        return;
+      }
+      const int r = m0 + int(rank) * kSmHalf + lane, c = n0 + (PERCOL ? lane : lane * 128);
+      left_m = p.M - r;
+      left_n = PERCOL || lane < 2 ? p.N - c : 0;
+      pa = p.sa + int64_t(p.ga == 1 ? r : r >> 7) * p.sa_row;
+      pb = p.sb + int64_t(PERCOL ? c : c >> 7) * p.sb_row;
+    };
+    auto copy = [&](uint32_t t) {  // of the next K block, number t; rows behind the last keep what was there
+      const uint32_t dst = dst0 + (t % kSmSlots) * (kSmSlotFloats * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i * 32 < left_m) cp_async4(dst + i * 128, pa + i * da);
+#pragma unroll
+      for (int i = 0; i < kCols; ++i)
+        if (i * 32 < left_n) cp_async4(dst + kSmHalf * 4 + i * 128, pb + i * db);
+      pa += p.sa_col;
+      pb += p.sb_col;
+      if (++pkb == nk) {
+        pkb = 0;
+        ++pj;
+        seek();
+      }
+    };
+    seek();
     bool ok = true;
-    for (int j = 0; ok && scaled_tile(p, j, m0, n0); ++j) {
-      const int mrow = m0 + int(rank) * kSmHalf;
+#pragma unroll 1
+    for (uint32_t t = 0; t < kSmAhead; ++t) {
+      copy(t);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    uint32_t it = 0;
+    for (int j = 0, m, n; ok && scaled_tile(p, j, m, n); ++j) {
       for (int kb = 0; kb < nk; ++kb, ++it) {
-        const int s = it % kSmScaleStages;
-        ok = mbar_wait(sempty_bar(s), ((it / kSmScaleStages) & 1u) ^ 1u, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
+        const uint32_t t = it + kSmAhead;
+        if (t % kSmFree == 0) {
+          ok = warp_wait(sempty_bar(t % kSmSlots / kSmFree), ((t / kSmSlots) & 1u) ^ 1u, abort_flag);
+          if (!ok) break;
         }
-        const uint32_t dst = smem_u32(scales + s * kSmScaleFloats);
-        const float* sa = p.sa + kb * p.sa_col;
-        const float* sb = p.sb + kb * p.sb_col;
-#pragma unroll
-        for (int i = 0; i < kSmHalf / 32; ++i) {
-          const int r = mrow + i * 32 + lane;
-          const bool in = r < p.M;
-          cp_async4(dst + 4 * (i * 32 + lane), in ? sa + int64_t(p.ga == 1 ? r : r >> 7) * p.sa_row : sa, in);
+        copy(t);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(kSmAhead) : "memory");  // this block's have landed
+        __syncwarp();
+        // the barrier's phase of two blocks before has to be over, or this arrival would count for it
+        if (it >= 2) {
+          ok = warp_wait(tfull_bar(it & 1), ((it >> 1) & 1u) ^ 1u, abort_flag);
+          if (!ok) break;
         }
-        if (PERCOL) {
-#pragma unroll
-          for (int i = 0; i < kSmTile / 32; ++i) {
-            const int c = n0 + i * 32 + lane;
-            const bool in = c < p.N;
-            cp_async4(dst + 4 * (kSmHalf + i * 32 + lane), in ? sb + int64_t(c) * p.sb_row : sb, in);
-          }
-        } else if (lane < 2) {
-          const int c = n0 + lane * 128;
-          const bool in = c < p.N;
-          cp_async4(dst + 4 * (kSmHalf + lane), in ? sb + int64_t(c >> 7) * p.sb_row : sb, in);
-        }
-        cp_async_arrive(sfull_bar(s));
+        if (lane == 0) mbar_arrive(tfull_bar(it & 1));
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
   }
   } else {
     // ------------------------------------------------------------ epilogue
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSmRegsHigh));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(sm_regs_high(PERCOL)));
     const int quad = warp & 3;
     const int half = (warp - 4) >> 2;  // columns [128 half, 128 half + 128)
     const uint32_t tlane = tmem_base + (uint32_t(quad * 32) << 16) + half * 128;
     float* piece = reinterpret_cast<float*>(smem + kOutOff) + (warp - 4) * 32 * kSmOutPitch;
-    uint32_t it = 0;
+    const uint32_t back0 = mapa_shared(tempty_bar(0), 0);
+    const float* sc_row = scales + quad * 32 + lane;
+    const float* sc_col = scales + kSmHalf + (PERCOL ? half * 128 : half);
+    uint32_t buf = 0, parity = 0, slot = 0;
     bool ok = true;
     for (int j = 0; ok && scaled_tile(p, j, m0, n0); ++j) {
-      uint64_t acc[64];
+      float2 acc[64];
 #pragma unroll
-      for (int i = 0; i < 64; ++i) acc[i] = 0;
-      for (int kb = 0; kb < nk; ++kb, ++it) {
-        const int s = it % kSmScaleStages, buf = it & 1;
-        ok = mbar_wait(sfull_bar(s), (it / kSmScaleStages) & 1u, abort_flag);
-        ok = ok && mbar_wait(tfull_bar(buf), (it >> 1) & 1u, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) {
-          ok = false;
-          break;
-        }
+      for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.f, 0.f);
+#pragma unroll 1
+      for (int kb = 0; kb < nk; ++kb) {
+        ok = warp_wait(tfull_bar(buf), parity, abort_flag);
+        if (!ok) break;
         tc_fence_after();
-        const float* sc = scales + s * kSmScaleFloats;
-        const float fa = sc[quad * 32 + lane];
-        const float f = PERCOL ? fa : fa * sc[kSmHalf + half];
-        const uint64_t f2 = pack2(f, f);
         const uint32_t ta = tlane + buf * kSmTile;
         uint32_t ra[32], rb[32];
-        auto add = [&](const uint32_t (&r)[32], int c) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint64_t v = pack2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
-            if (PERCOL) {
-              const uint64_t g = *reinterpret_cast<const uint64_t*>(sc + kSmHalf + half * 128 + c * 32 + 2 * i);
-              acc[c * 16 + i] = fma2(v, mul2(f2, g), acc[c * 16 + i]);
-            } else {
-              acc[c * 16 + i] = fma2(v, f2, acc[c * 16 + i]);
-            }
-          }
-        };
         tmem_ld32(ta, ra);
         tmem_ld32(ta + 32, rb);
+        const float* sc = sc_col + slot * kSmSlotFloats;
+        const float fa = sc_row[slot * kSmSlotFloats], f = PERCOL ? fa : fa * sc[0];
+        auto add = [&](const uint32_t (&r)[32], int c) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float2 v0 = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+            const float2 v1 = make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+            float2 g0 = make_float2(f, f), g1 = g0;
+            if (PERCOL) {
+              const float4 g = *reinterpret_cast<const float4*>(sc + c * 32 + i);
+              g0 = __fmul2_rn(g0, make_float2(g.x, g.y));
+              g1 = __fmul2_rn(g1, make_float2(g.z, g.w));
+            }
+            acc[c * 16 + i / 2] = __ffma2_rn(v0, g0, acc[c * 16 + i / 2]);
+            acc[c * 16 + i / 2 + 1] = __ffma2_rn(v1, g1, acc[c * 16 + i / 2 + 1]);
+          }
+        };
         tmem_ld_wait();
         add(ra, 0);
         tmem_ld32(ta + 64, ra);
@@ -320,11 +358,16 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         // the accumulator is in registers: hand it back
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(mapa_shared(tempty_bar(buf), 0));
+        if (lane == 0) mbar_arrive_cluster(back0 + 8u * buf);
         add(ra, 2);
         add(rb, 3);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sempty_bar(s));
+        parity ^= buf;
+        buf ^= 1;
+        if ((++slot & (kSmFree - 1)) == 0) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sempty_bar(slot / kSmFree - 1));
+          slot &= kSmSlots - 1;
+        }
       }
       if (!ok) break;
 
@@ -342,18 +385,13 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              float lo, hi;
               if (OUT == OUT_F32) {
-                unpack2(acc[q * 4 + i / 2], lo, hi);
-                w[i] = __float_as_uint(i & 1 ? hi : lo);
+                w[i] = __float_as_uint(i & 1 ? acc[q * 4 + i / 2].y : acc[q * 4 + i / 2].x);
+              } else if (OUT == OUT_BF16) {
+                w[i] = pack_bf16x2(acc[q * 8 + i].x, acc[q * 8 + i].y);
               } else {
-                unpack2(acc[q * 8 + i], lo, hi);
-                if (OUT == OUT_BF16) {
-                  w[i] = pack_bf16x2(lo, hi);
-                } else {
-                  const __half2 h = __floats2half2_rn(lo, hi);
-                  w[i] = *reinterpret_cast<const uint32_t*>(&h);
-                }
+                const __half2 h = __floats2half2_rn(acc[q * 8 + i].x, acc[q * 8 + i].y);
+                w[i] = *reinterpret_cast<const uint32_t*>(&h);
               }
             }
             st32b(dst + q * kPer, w);
@@ -361,24 +399,22 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         }
       } else {
         // any alignment, edges, accumulation: 32 x 32 pieces through shared memory, a row at a time
+        const int rows = min(32, p.M - row0);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < 128 / kSmOutCols; ++q) {
           __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float lo, hi;
-            unpack2(acc[q * 16 + i], lo, hi);
-            piece[lane * kSmOutPitch + 2 * i] = lo;
-            piece[lane * kSmOutPitch + 2 * i + 1] = hi;
+          for (int i = 0; i < kSmOutCols / 2; ++i) {
+            piece[lane * kSmOutPitch + 2 * i] = acc[q * (kSmOutCols / 2) + i].x;
+            piece[lane * kSmOutPitch + 2 * i + 1] = acc[q * (kSmOutCols / 2) + i].y;
           }
           __syncwarp();
-          const int col = col0 + q * 32 + lane;
+          const int c = lane % kSmOutCols, col = col0 + q * kSmOutCols + c;
           if (col < p.N) {
-            const int rows = min(32, p.M - row0);
             OT* dst = C + int64_t(row0) * p.ldc + col;
 #pragma unroll 4
-            for (int i = 0; i < rows; ++i) {
-              float x = piece[i * kSmOutPitch + lane];
+            for (int i = lane / kSmOutCols; i < rows; i += 32 / kSmOutCols) {
+              float x = piece[i * kSmOutPitch + c];
               if (p.accumulate) x += O::get(dst[i * p.ldc]);
               dst[i * p.ldc] = O::put(x);
             }
