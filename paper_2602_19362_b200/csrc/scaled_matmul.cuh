@@ -47,11 +47,11 @@ static_assert(kSmSmemBytes <= 227 * 1024, "shared memory of a CTA");
 // need more in warp 2.  (4096 x 152064 x 3584: 2.15 ms with 24 / 240, 2.27 with 40 / 232, 2.5 with 56 / 224, where
 // the loop spills; 8192^3 with a scale per column 0.78 and 0.74 ms.)
 constexpr int kSmRegs = 168;
-constexpr int sm_regs_low(bool percol) { return percol ? 40 : 24; }
-constexpr int sm_regs_high(bool percol) { return percol ? 232 : 240; }
-static_assert(128 * sm_regs_low(true) + 256 * sm_regs_high(true) == kSmThreads * kSmRegs &&
-                  128 * sm_regs_low(false) + 256 * sm_regs_high(false) == kSmThreads * kSmRegs,
-              "register split");
+template <bool PERCOL>
+struct SmRegs {
+  static constexpr int kLow = PERCOL ? 40 : 24, kHigh = PERCOL ? 232 : 240;
+  static_assert(128 * kLow + 256 * kHigh == kSmThreads * kSmRegs, "register split");
+};
 
 enum { OUT_BF16 = 0, OUT_F16 = 1, OUT_F32 = 2 };
 
@@ -196,7 +196,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   int m0, n0;
 
   if (warp < 4) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(sm_regs_low(PERCOL)));
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(SmRegs<PERCOL>::kLow));
   if (warp == 0) {
     // ------------------------------------------------------------ operand loads
     if (lane == 0) {
@@ -309,7 +309,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   }
   } else {
     // ------------------------------------------------------------ epilogue
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(sm_regs_high(PERCOL)));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SmRegs<PERCOL>::kHigh));
     const int quad = warp & 3;
     const int half = (warp - 4) >> 2;  // columns [128 half, 128 half + 128)
     const uint32_t tlane = tmem_base + (uint32_t(quad * 32) << 16) + half * 128;
