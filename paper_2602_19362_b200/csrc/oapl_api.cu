@@ -198,14 +198,15 @@ static bool make_map_f32(CUtensorMap* m, const void* base, uint64_t rows, uint64
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Matrix of 8-bit values [rows, cols], leading dimension ld bytes, seen through 128 x 128 boxes (128-byte
-// rows, 128-byte swizzle): an operand half of the block-scaled product.  What lies outside reads as 0.
-static bool make_map_u8(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t ld) {
+// Matrix of 8-bit values [rows, cols], leading dimension ld bytes, seen through boxes of 128-byte rows (128-byte
+// swizzle): an operand of the block-scaled product.  What lies outside reads as 0.
+static bool make_map_u8(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t ld,
+                        uint32_t box_rows = 128) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {cols, rows};
   const cuuint64_t strides[1] = {ld};
-  const cuuint32_t box[2] = {128, 128};
+  const cuuint32_t box[2] = {128, box_rows};
   const cuuint32_t estr[2] = {1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -783,6 +784,65 @@ static int launch_scaled_matmul(const CUtensorMap& a, const CUtensorMap& b, cons
   kern<<<grid, kSmThreads, kSmSmemBytes, st>>>(a, b, sp);
   CKL();
   return OAPL_OK;
+}
+
+
+template <int OUT, int NT>
+static int launch_scaled_few(const oapl_scaled* A, const oapl_scaled* B, const FewParams& fp, int n_sm, cudaStream_t st) {
+  CUtensorMap tw, tt;
+  if (!make_map_u8(&tw, B->data, (uint64_t)B->rows, (uint64_t)B->cols, (uint64_t)B->ld, (uint32_t)fp.rows) ||
+      !make_map_u8(&tt, A->data, (uint64_t)A->rows, (uint64_t)A->cols, (uint64_t)A->ld, NT))
+    return OAPL_ERR_CUDA;
+  static bool attr_set[kMaxDevices] = {false};
+  auto kern = scaled_few_kernel<OUT, NT>;
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return OAPL_ERR_CUDA;
+  if (!attr_set[dev]) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FewCfg<NT>::kSmemBytes) !=
+        cudaSuccess)
+      return OAPL_ERR_CUDA;
+    attr_set[dev] = true;
+  }
+  kern<<<fp.tiles < n_sm ? fp.tiles : n_sm, kFwThreads, FewCfg<NT>::kSmemBytes, st>>>(tw, tt, fp);
+  CKL();
+  return OAPL_OK;
+}
+
+template <int OUT>
+static int route_scaled_few(const oapl_scaled* A, const oapl_scaled* B, const FewParams& fp, int n_sm, cudaStream_t st) {
+  if (fp.M <= 16) return launch_scaled_few<OUT, 16>(A, B, fp, n_sm, st);
+  if (fp.M <= 32) return launch_scaled_few<OUT, 32>(A, B, fp, n_sm, st);
+  return launch_scaled_few<OUT, 64>(A, B, fp, n_sm, st);
+}
+
+// At most 64 rows of A: the roles swapped, B's rows shared out over the SMs (see scaled_few_kernel).
+static int scaled_few(const oapl_scaled* A, const oapl_scaled* B, void* C, int32_t c_type, int64_t ldc, int accumulate,
+                      int32_t* device_status, int n_sm, cudaStream_t st) {
+  FewParams fp;
+  memset(&fp, 0, sizeof(fp));
+  fp.sw = B->scale;
+  fp.st = A->scale;
+  fp.sw_row = B->scale_row_stride;
+  fp.sw_col = B->scale_col_stride;
+  fp.st_row = A->scale_row_stride;
+  fp.st_col = A->scale_col_stride;
+  fp.gw = B->block_rows;
+  fp.gt = A->block_rows;
+  fp.M = (int32_t)A->rows;
+  fp.N = (int32_t)B->rows;
+  fp.K = (int32_t)A->cols;
+  fp.C = C;
+  fp.ldc = ldc;
+  fp.accumulate = accumulate != 0;
+  fp.e5_w = B->type == OAPL_TYPE_E5M2;
+  fp.e5_t = A->type == OAPL_TYPE_E5M2;
+  const int64_t per_round = (int64_t)kFwRows * n_sm, rounds = (B->rows + per_round - 1) / per_round;
+  fp.rows = (int32_t)((B->rows + rounds * n_sm - 1) / (rounds * n_sm));
+  fp.tiles = (int32_t)((B->rows + fp.rows - 1) / fp.rows);
+  fp.err = device_status;
+  if (c_type == OAPL_TYPE_BF16) return route_scaled_few<OUT_BF16>(A, B, fp, n_sm, st);
+  if (c_type == OAPL_TYPE_F16) return route_scaled_few<OUT_F16>(A, B, fp, n_sm, st);
+  return route_scaled_few<OUT_F32>(A, B, fp, n_sm, st);
 }
 
 }  // namespace oapl
@@ -1421,6 +1481,8 @@ int oapl_scaled_matmul(const oapl_scaled* A, const oapl_scaled* B, void* C, int3
   if ((uintptr_t)C % es) return OAPL_ERR_MISALIGNED;
   const int n_sm = sm_count();
   if (n_sm < 2) return OAPL_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (A->rows <= 64) return scaled_few(A, B, C, c_type, ldc, accumulate, device_status, n_sm, st);
   CUtensorMap ta, tb;
   if (!make_map_u8(&ta, A->data, (uint64_t)A->rows, (uint64_t)A->cols, (uint64_t)A->ld) ||
       !make_map_u8(&tb, B->data, (uint64_t)B->rows, (uint64_t)B->cols, (uint64_t)B->ld))
@@ -1450,7 +1512,6 @@ int oapl_scaled_matmul(const oapl_scaled* A, const oapl_scaled* B, void* C, int3
   sp.err = device_status;
   const int64_t tiles = (int64_t)sp.mt * sp.nt;
   const int grid = 2 * (int)(tiles < n_sm / 2 ? tiles : n_sm / 2);
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool percol = sp.gb == 1;
   if (c_type == OAPL_TYPE_BF16)
     return percol ? launch_scaled_matmul<OUT_BF16, true>(ta, tb, sp, grid, st)

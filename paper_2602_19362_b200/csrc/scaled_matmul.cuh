@@ -443,4 +443,323 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   }
 }
 
+// ------------------------------------------------------------------------------------ few rows
+// The same product for at most 64 rows of A (decoded tokens): HBM-bound by B, the weight.  The roles are
+// swapped: rows of B fill the 128 lanes of the accumulator and the rows of A are its NT = 16, 32 or 64 columns,
+// so a token costs what it needs and the 512 TMEM columns hold 512 / NT accumulators (at most 16): the hand-over
+// of an accumulator, about 900 cycles, is spread over as many K blocks.  (152064 x 3584, one token to 64: 97 to
+// 114 us against 144 to 129 with the kernel above; 128 tokens: 165 against 143, which therefore takes them.)  B's rows are shared out evenly: with
+// S SMs and k = ceil(N / (128 S)) rounds a CTA takes tiles of ceil(N / (k S)) rows, 25 of 3584 and 115 of 152064
+// on 148 SMs, so that a small weight keeps every SM busy and a large one ends everywhere at the same time.
+// No pairs: one CTA per SM, all its shared memory as stages of the weight stream.
+constexpr int kFwRows = 128;
+constexpr int kFwEpiWarps = 4;
+constexpr int kFwThreads = 32 * (4 + kFwEpiWarps);
+
+template <int NT>
+struct FewCfg {
+  static constexpr int kStageBytes = (kFwRows + NT) * kSmKB;
+  static constexpr int kStages = NT <= 32 ? 9 : 7;
+  static constexpr int kBufs = 512 / NT < 16 ? 512 / NT : 16;
+  static constexpr int kTmemCols = kBufs * NT;  // a power of two, at least 32
+  static constexpr int kSlots = 32;             // K blocks whose scales have room
+  static constexpr int kAhead = 16;
+  static constexpr int kFree = 8;
+  static constexpr int kSlotFloats = kFwRows + NT;
+  static constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + kSlots * kSlotFloats * 4 + 1024 + 1024;
+  static_assert(kSmemBytes <= 227 * 1024, "shared memory of a CTA");
+};
+
+struct FewParams {
+  const float* sw;  // scales of B's rows, then of A's
+  const float* st;
+  int64_t sw_row, sw_col, st_row, st_col;
+  int32_t gw, gt;
+  int32_t M, N, K;  // A's rows, B's rows
+  void* C;
+  int64_t ldc;
+  int32_t accumulate;
+  int32_t e5_w, e5_t;
+  int32_t rows, tiles;  // rows of B in a tile (at most 128), tiles
+  int32_t* err;
+};
+
+__device__ __forceinline__ void tma_load_2d_one(uint32_t dst, const void* tmap, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void umma_f8_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_one(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[N], int at) {
+  static_assert(N % 16 == 0, "whole loads");
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[at]), "=r"(r[at + 1]), "=r"(r[at + 2]), "=r"(r[at + 3]), "=r"(r[at + 4]), "=r"(r[at + 5]),
+        "=r"(r[at + 6]), "=r"(r[at + 7]), "=r"(r[at + 8]), "=r"(r[at + 9]), "=r"(r[at + 10]), "=r"(r[at + 11]),
+        "=r"(r[at + 12]), "=r"(r[at + 13]), "=r"(r[at + 14]), "=r"(r[at + 15])
+      : "r"(taddr)
+      : "memory");
+}
+
+template <int OUT, int NT>
+__global__ void __launch_bounds__(kFwThreads, 1)
+scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmT, const FewParams p) {
+  using Cfg = FewCfg<NT>;
+  using O = OutElem<OUT>;
+  using OT = typename O::T;
+  constexpr int kStages = Cfg::kStages, kBufs = Cfg::kBufs;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (base - raw);
+  constexpr uint32_t kScaleOff = kStages * Cfg::kStageBytes;
+  constexpr uint32_t kBarOff = kScaleOff + Cfg::kSlots * Cfg::kSlotFloats * 4;
+  float* scales = reinterpret_cast<float*>(smem + kScaleOff);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kBarOff);
+  const uint32_t bar0 = base + kBarOff;
+  auto full_bar = [&](int s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
+  auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
+  auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * kStages + kBufs + b); };
+  auto sempty_bar = [&](int h) { return bar0 + 8u * (2 * kStages + 2 * kBufs + h); };
+  constexpr int kBars = 2 * kStages + 2 * kBufs + Cfg::kSlots / Cfg::kFree;
+  static_assert(8 * (kBars + 2) <= 1024, "barriers");
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bars + kBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kBars + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 1);
+    }
+    for (int b = 0; b < kBufs; ++b) {
+      mbar_init(tfull_bar(b), 2);  // the tensor cores and warp 2
+      mbar_init(tempty_bar(b), kFwEpiWarps);
+    }
+    for (int h = 0; h < Cfg::kSlots / Cfg::kFree; ++h) mbar_init(sempty_bar(h), kFwEpiWarps);
+    *abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tmW);
+    tma_prefetch_desc(&tmT);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)tmem_slot)),
+                 "r"((uint32_t)Cfg::kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  const int nk = (p.K + kSmKB - 1) / kSmKB;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------ operand loads
+    if (lane == 0) {
+      const uint32_t bytes = uint32_t(p.rows + NT) * kSmKB;  // whole boxes, whatever lies outside
+      uint32_t it = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+        for (int kb = 0; kb < nk; ++kb, ++it) {
+          const int s = it % kStages;
+          if (!mbar_wait(empty_bar(s), ((it / kStages) & 1u) ^ 1u, abort_flag)) {
+            ok = false;
+            break;
+          }
+          const uint32_t sa = base + s * Cfg::kStageBytes;
+          mbar_expect_tx(full_bar(s), bytes);
+          tma_load_2d_one(sa, &tmW, full_bar(s), kb * kSmKB, t * p.rows);
+          tma_load_2d_one(sa + kFwRows * kSmKB, &tmT, full_bar(s), kb * kSmKB, 0);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMAs
+    const uint32_t idesc = make_idesc_f8(kFwRows, NT, p.e5_w, p.e5_t);
+    const uint64_t da0 = smem_desc_sw128(base, 16, 1024), db0 = smem_desc_sw128(base + kFwRows * kSmKB, 16, 1024);
+    uint32_t it = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+      for (int kb = 0; kb < nk; ++kb, ++it) {
+        const int s = it % kStages, buf = it % kBufs;
+        ok = warp_wait(full_bar(s), (it / kStages) & 1u, abort_flag) &&
+             warp_wait(tempty_bar(buf), ((it / kBufs) & 1u) ^ 1u, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t off = uint32_t(s * (Cfg::kStageBytes >> 4));
+#pragma unroll
+          for (int kk = 0; kk < kSmKB / 32; ++kk)
+            umma_f8_one(tmem_base + buf * NT, da0 + off + 2 * kk, db0 + off + 2 * kk, idesc, kk ? 1u : 0u);
+          umma_commit_one(tfull_bar(buf));
+          umma_commit_one(empty_bar(s));
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp == 2) {
+    // ------------------------------------------------------------ scales
+    const int64_t dw = p.gw == 1 ? 32 * p.sw_row : 0, dt = p.gt == 1 ? 32 * p.st_row : 0;
+    const uint32_t dst0 = smem_u32(scales) + 4 * lane;
+    const float *pw = p.sw, *pt = p.st;
+    int pj = blockIdx.x, pkb = 0, left_w = 0, left_t = 0;
+    // rows of B in a tile need not lie in one block of 128: every row's scale is looked up by itself
+    int r0 = 0;
+    auto seek = [&]() {
+      left_w = left_t = 0;
+      if (pj >= p.tiles) return;
+      r0 = pj * p.rows + lane;
+      left_w = min(p.N - r0, p.rows - lane);
+      left_t = p.M - lane;
+      pw = p.sw + int64_t(p.gw == 1 ? r0 : 0) * p.sw_row;
+      pt = p.st + int64_t(p.gt == 1 ? lane : 0) * p.st_row;
+    };
+    auto copy = [&](uint32_t n) {
+      const uint32_t dst = dst0 + (n % Cfg::kSlots) * (Cfg::kSlotFloats * 4);
+#pragma unroll
+      for (int i = 0; i < kFwRows / 32; ++i)
+        if (i * 32 < left_w)
+          cp_async4(dst + i * 128, p.gw == 1 ? pw + i * dw : pw + int64_t((r0 + i * 32) >> 7) * p.sw_row);
+#pragma unroll
+      for (int i = 0; i < (NT + 31) / 32; ++i)
+        if (i * 32 < left_t && i * 32 + lane < NT) cp_async4(dst + kFwRows * 4 + i * 128, pt + i * dt);
+      pw += p.sw_col;
+      pt += p.st_col;
+      if (++pkb == nk) {
+        pkb = 0;
+        pj += gridDim.x;
+        seek();
+      }
+    };
+    seek();
+    bool ok = true;
+#pragma unroll 1
+    for (uint32_t n = 0; n < Cfg::kAhead; ++n) {
+      copy(n);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    uint32_t it = 0;
+    for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+      for (int kb = 0; kb < nk; ++kb, ++it) {
+        const uint32_t n = it + Cfg::kAhead;
+        if (n % Cfg::kFree == 0) {
+          ok = warp_wait(sempty_bar(n % Cfg::kSlots / Cfg::kFree), ((n / Cfg::kSlots) & 1u) ^ 1u, abort_flag);
+          if (!ok) break;
+        }
+        copy(n);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(Cfg::kAhead) : "memory");  // this block's have landed
+        __syncwarp();
+        // the barrier's phase of one round before has to be over, or this arrival would count for it
+        if (it >= kBufs) {
+          ok = warp_wait(tfull_bar(it % kBufs), ((it / kBufs) & 1u) ^ 1u, abort_flag);
+          if (!ok) break;
+        }
+        if (lane == 0) mbar_arrive(tfull_bar(it % kBufs));
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp >= 4) {
+    // ------------------------------------------------------------ epilogue
+    constexpr int kPiece = NT < 32 ? NT : 32;  // columns taken from TMEM together
+    const int quad = warp & 3, r = quad * 32 + lane;
+    const uint32_t tlane = tmem_base + (uint32_t(quad * 32) << 16);
+    uint32_t buf = 0, parity = 0, slot = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+      float2 acc[NT / 2];
+#pragma unroll
+      for (int i = 0; i < NT / 2; ++i) acc[i] = make_float2(0.f, 0.f);
+#pragma unroll 1
+      for (int kb = 0; kb < nk; ++kb) {
+        ok = warp_wait(tfull_bar(buf), parity, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        const float* sc = scales + slot * Cfg::kSlotFloats;
+        const float f = sc[r];
+        const float2 f2 = make_float2(f, f);
+        const uint32_t ta = tlane + buf * NT;
+#pragma unroll
+        for (int c = 0; c < NT / kPiece; ++c) {
+          uint32_t v[kPiece];
+#pragma unroll
+          for (int i = 0; i < kPiece; i += 16) tmem_ld16(ta + c * kPiece + i, v, i);
+          tmem_ld_wait();
+          if (c == NT / kPiece - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tempty_bar(buf));
+          }
+#pragma unroll
+          for (int i = 0; i < kPiece; i += 4) {
+            const float4 g = *reinterpret_cast<const float4*>(sc + kFwRows + c * kPiece + i);
+            const int k = (c * kPiece + i) / 2;
+            acc[k] = __ffma2_rn(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])),
+                                __fmul2_rn(f2, make_float2(g.x, g.y)), acc[k]);
+            acc[k + 1] = __ffma2_rn(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])),
+                                    __fmul2_rn(f2, make_float2(g.z, g.w)), acc[k + 1]);
+          }
+        }
+        if (++buf == kBufs) {
+          buf = 0;
+          parity ^= 1u;
+        }
+        if ((++slot & (Cfg::kFree - 1)) == 0) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sempty_bar(slot / Cfg::kFree - 1));
+          slot &= Cfg::kSlots - 1;
+        }
+      }
+      if (!ok) break;
+      // this thread's row of B is a column of C: a warp stores 32 of them next to one another
+      const int col = t * p.rows + r;
+      if (r < p.rows && col < p.N) {
+        OT* C = reinterpret_cast<OT*>(p.C) + col;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          if (i < p.M) {
+            float x = i & 1 ? acc[i / 2].y : acc[i / 2].x;
+            if (p.accumulate) x += O::get(C[i * p.ldc]);
+            C[i * p.ldc] = O::put(x);
+          }
+        }
+      }
+    }
+  }
+
+  // ---------------------------------------------------------------- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (threadIdx.x == 0) {
+      if (p.err) atomicCAS(p.err, 0, -8 /*OAPL_ERR_DEVICE_TIMEOUT*/);
+      const long long t0 = clock64();  // loads in flight land before shared memory is released
+      while (clock64() - t0 < 2000000LL) {
+      }
+    }
+    __syncthreads();
+  }
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)Cfg::kTmemCols)
+                 : "memory");
+  }
+}
+
 }  // namespace oapl
