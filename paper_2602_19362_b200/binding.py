@@ -371,12 +371,14 @@ MAX_TOP = 32
 
 
 def _rows(t, types, name):
-    """Check a [rows, cols] CUDA tensor with contiguous rows; its leading dimension."""
-    if t.dtype not in types or t.dim() != 2 or not t.is_cuda:
+    """Check a [rows, cols] CUDA tensor with contiguous rows: its type code, rows, cols and leading dimension."""
+    code = types.get(t.dtype)
+    if code is None or t.dim() != 2 or not t.is_cuda:
         raise TypeError(f"{name}: expected a 2-D CUDA tensor of one of {[str(x) for x in types]}")
-    if t.stride(1) != 1 and t.shape[1] > 1:
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    if step != 1 and cols > 1:
         raise TypeError(f"{name}: elements of a row must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return code, rows, cols, (ld if rows > 1 else max(ld, cols))
 
 
 def _vec(t, dtype, shape, device, name):
@@ -384,13 +386,13 @@ def _vec(t, dtype, shape, device, name):
     if t is None:
         return None
     if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
-        raise TypeError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on the logits' device")
+        raise TypeError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{device}")
     return t.data_ptr()
 
 
 def _stream_of(device):
     """The current stream of `device`, which has to be the current device."""
-    if device != torch.cuda.current_device():
+    if device != torch._C._cuda_getDevice():
         raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
     return torch._C._cuda_getCurrentRawStream(device)
 
@@ -398,12 +400,11 @@ def _stream_of(device):
 def make_logits(logits, targets=None, mask=None, scale: float = 1.0) -> OaplLogits:
     """Fill oapl_logits.  logits: [N, V] bf16, fp16 or fp32, rows any stride apart; targets: int32 [N];
     mask: uint8 [N].  The struct keeps the tensors alive."""
-    ld = _rows(logits, FLOAT_TYPES, "logits")
-    N, V = logits.shape
+    code, N, V, ld = _rows(logits, FLOAT_TYPES, "logits")
     dev = logits.get_device()
-    L = OaplLogits(logits.data_ptr(), N, ld, V, FLOAT_TYPES[logits.dtype], _vec(targets, torch.int32, (N,), dev, "targets"),
+    L = OaplLogits(logits.data_ptr(), N, ld, V, code, _vec(targets, torch.int32, (N,), dev, "targets"),
                    _vec(mask, torch.uint8, (N,), dev, "mask"), scale)
-    L.tensors = (logits, targets, mask)
+    L.tensors, L.device = (logits, targets, mask), dev
     return L
 
 
@@ -411,7 +412,7 @@ def oapl_logits_logprobs(L, token_logp=None, token_entropy=None, token_lse=None,
                          device_status=None):
     """Log-probability of the targets, entropy, log-sum-exp [N] and the top K alternatives [N, K]; each
     output may be None.  device_status: int32 [1], zero before the call."""
-    dev, N = L.tensors[0].get_device(), L.N
+    dev, N = L.device, L.N
     first = top_id if top_id is not None else top_logp
     K = 0 if first is None else first.shape[-1]
     f32 = torch.float32
@@ -427,13 +428,12 @@ def oapl_logits_logprobs(L, token_logp=None, token_entropy=None, token_lse=None,
 def oapl_logits_logprobs_bwd(L, token_lse, token_entropy, g_logp, g_entropy, g_top, top_id, dlogits):
     """Gradient of the logits from the gradients of token_logp, token_entropy (each [N] or None) and of the
     log-probabilities of the ids top_id ([N, K] or None).  dlogits may be the logits themselves."""
-    logits = L.tensors[0]
-    dev, N = logits.get_device(), L.N
+    dev, N = L.device, L.N
     K = 0 if g_top is None else g_top.shape[-1]
     f32 = torch.float32
-    ld_d = _rows(dlogits, (logits.dtype,), "dlogits")
-    if dlogits.shape != logits.shape or dlogits.get_device() != dev:
-        raise TypeError("dlogits: expected the logits' shape and device")
+    code, rows, cols, ld_d = _rows(dlogits, FLOAT_TYPES, "dlogits")
+    if code != L.type or rows != N or cols != L.V or dlogits.get_device() != dev:
+        raise TypeError("dlogits: expected the logits' type, shape and device")
     rc = lib().oapl_logits_logprobs_bwd(
         L, _vec(token_lse, f32, (N,), dev, "token_lse"), _vec(token_entropy, f32, (N,), dev, "token_entropy"),
         _vec(g_logp, f32, (N,), dev, "g_logp"), _vec(g_entropy, f32, (N,), dev, "g_entropy"), K,
@@ -447,18 +447,17 @@ def make_scaled(data, scale, block_rows: int) -> OaplScaled:
     """Fill oapl_scaled.  data: [rows, cols] float8_e4m3fn or float8_e5m2, rows a multiple of 16 bytes apart;
     scale: fp32 [ceil(rows / block_rows), ceil(cols / 128)] of any strides; block_rows 1 or 128.  The struct
     keeps the tensors alive."""
-    ld = _rows(data, SCALED_TYPES, "data")
-    rows, cols = data.shape
-    if data.shape[0] == 1:
+    code, rows, cols, ld = _rows(data, SCALED_TYPES, "data")
+    if rows == 1:
         ld = -(-ld // 16) * 16      # one row: no second one to find
-    if block_rows not in (1, 128):
+    if block_rows != 1 and block_rows != 128:
         raise ValueError("block_rows: 1 or 128")
-    if (scale.dtype != torch.float32 or scale.get_device() != data.get_device()
-            or scale.shape != (-(-rows // block_rows), -(-cols // 128))):
+    dev = data.get_device()
+    if (scale.dtype != torch.float32 or scale.shape != ((rows + block_rows - 1) // block_rows, (cols + 127) // 128)
+            or scale.get_device() != dev):
         raise TypeError("scale: expected fp32 [ceil(rows / block_rows), ceil(cols / 128)] on the data's device")
-    m = OaplScaled(data.data_ptr(), scale.data_ptr(), rows, cols, ld, scale.stride(0), scale.stride(1),
-                   SCALED_TYPES[data.dtype], block_rows)
-    m.tensors = (data, scale)
+    m = OaplScaled(data.data_ptr(), scale.data_ptr(), rows, cols, ld, *scale.stride(), code, block_rows)
+    m.tensors, m.device = (data, scale), dev
     return m
 
 
@@ -472,26 +471,25 @@ def alloc_scaled(rows: int, cols: int, block_rows: int, dtype=torch.float8_e4m3f
 
 def oapl_quantize(x, out: OaplScaled, transpose: bool = False, pow2: bool = False):
     """Quantise x [rows, cols] (bf16, fp16, fp32) into `out`, turned when transpose is set."""
-    ld = _rows(x, FLOAT_TYPES, "x")
-    dev = x.get_device()
-    if out.tensors[0].get_device() != dev:
+    code, rows, cols, ld = _rows(x, FLOAT_TYPES, "x")
+    if x.get_device() != out.device:
         raise TypeError("out: expected x's device")
-    rc = lib().oapl_quantize(x.data_ptr(), FLOAT_TYPES[x.dtype], x.shape[0], x.shape[1], ld, out,
+    rc = lib().oapl_quantize(x.data_ptr(), code, rows, cols, ld, out,
                              (OAPL_QUANT_TRANSPOSE if transpose else 0) | (OAPL_QUANT_POW2 if pow2 else 0),
-                             _stream_of(dev))
+                             _stream_of(out.device))
     if rc != OAPL_OK:
         raise OaplError(rc, "oapl_quantize")
 
 
 def oapl_scaled_matmul(A: OaplScaled, B: OaplScaled, C, accumulate: bool = False, device_status=None):
     """C [A.rows, B.rows] (bf16, fp16, fp32) = A . B^T, or C += A . B^T."""
-    ldc = _rows(C, FLOAT_TYPES, "C")
-    dev = C.get_device()
-    if C.shape != (A.rows, B.rows):
+    code, rows, cols, ldc = _rows(C, FLOAT_TYPES, "C")
+    if rows != A.rows or cols != B.rows:
         raise TypeError(f"C: expected shape {(A.rows, B.rows)}")
-    if A.tensors[0].get_device() != dev or B.tensors[0].get_device() != dev:
+    dev = C.get_device()
+    if A.device != dev or B.device != dev:
         raise TypeError("A, B: expected C's device")
-    rc = lib().oapl_scaled_matmul(A, B, C.data_ptr(), FLOAT_TYPES[C.dtype], ldc, int(accumulate),
+    rc = lib().oapl_scaled_matmul(A, B, C.data_ptr(), code, ldc, accumulate,
                                   _vec(device_status, torch.int32, (1,), dev, "device_status"), _stream_of(dev))
     if rc != OAPL_OK:
         raise OaplError(rc, "oapl_scaled_matmul")
