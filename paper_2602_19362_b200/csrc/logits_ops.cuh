@@ -65,29 +65,6 @@ struct LogitsParams {
 };
 
 // ------------------------------------------------------------------------------------ small pieces
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -211,7 +188,7 @@ struct Elem<float> {
 // of log2, not a rounded product that stands for a logit, so one multiply-add gives x with one rounding.
 struct RowSums {
   float R;
-  uint64_t s, t;  // two lanes each: sum 2^x and sum 2^x x
+  float2 s, t;  // two lanes each: sum 2^x and sum 2^x x
 };
 struct RowTotal {
   float R, s, t, m;  // m: the largest logit, clamped
@@ -224,25 +201,21 @@ __device__ __forceinline__ void row_move(RowSums& r, float to) {
   // x + d in place of x: 2^x turns into 2^x 2^d, and 2^x x into (x + d) 2^x 2^d
   const float d = fmaxf(r.R - to, kLgFloor);
   const float f = ex2_approx(d);
-  float s0, s1, t0, t1;
-  unpack2(r.s, s0, s1);
-  unpack2(r.t, t0, t1);
-  r.t = pack2(f * fmaf(d, s0, t0), f * fmaf(d, s1, t1));
-  r.s = pack2(f * s0, f * s1);
+  r.t = make_float2(f * fmaf(d, r.s.x, r.t.x), f * fmaf(d, r.s.y, r.t.y));
+  r.s = make_float2(f * r.s.x, f * r.s.y);
   r.R = to;
 }
 
+// The two-wide forms are the compiler's own: with 64-bit asm operands it copied every pair.
 template <int KN>
 __device__ __forceinline__ void row_add(RowSums& r, const float (&f)[KN], float c) {
-  const uint64_t nr = pack2(-r.R, -r.R), cc = pack2(c, c);
+  const float2 nr = make_float2(-r.R, -r.R), cc = make_float2(c, c);
 #pragma unroll
   for (int i = 0; i < KN; i += 2) {
-    const uint64_t x2 = fma2(pack2(f[i], f[i + 1]), cc, nr);
-    float x0, x1;
-    unpack2(x2, x0, x1);
-    const uint64_t e2 = pack2(ex2_approx(x0), ex2_approx(x1));
-    r.s = add2(r.s, e2);
-    r.t = fma2(e2, x2, r.t);
+    const float2 x = __ffma2_rn(make_float2(f[i], f[i + 1]), cc, nr);
+    const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+    r.s = __fadd2_rn(r.s, e);
+    r.t = __ffma2_rn(e, x, r.t);
   }
 }
 
@@ -561,7 +534,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logits_fwd_kernel(const LogitsP
 
   RowSums r;
   r.R = fmaf(p.clamp, c, 1000.f);  // a clamped logit counts for nothing
-  r.s = r.t = pack2(0.f, 0.f);
+  r.s = r.t = make_float2(0.f, 0.f);
   float tmax = p.clamp, gm = p.clamp;
   int g = 0, in_group = 0;
   uint4 cur[kLgUnroll], nxt[kLgUnroll];
@@ -625,12 +598,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logits_fwd_kernel(const LogitsP
   // ---- join the sums: lanes, warps
   RowTotal tot;
   {
-    float s0, s1, t0, t1;
-    unpack2(r.s, s0, s1);
-    unpack2(r.t, t0, t1);
     tot.R = r.R;
-    tot.s = s0 + s1;
-    tot.t = t0 + t1;
+    tot.s = r.s.x + r.s.y;
+    tot.t = r.t.x + r.t.y;
     tot.m = wmax;
   }
   tot = row_join_warp(tot);
@@ -759,29 +729,29 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logits_fwd_kernel(const LogitsP
 // ------------------------------------------------------------------------------------ backward
 // dz_v = a ( -p_v (G + g_H (ln p_v + H)) + g_lp [v = t] + sum_k g_k [v = id_k] ),  G = g_lp + sum_k g_k,
 // p_v = e^(a z_v - lse).  One read and one write per logit, HBM-bound; dz may be the logits themselves.
-// A CTA takes kLgSpan logits of a row; the few entries with a point term are written again after the
+// A CTA takes kLgSpanVecs 16-byte vectors of a row; the few entries with a point term are written again after the
 // CTA's stores, from logits read before them.
 constexpr int kLgSpanVecs = kLgThreads * kLgUnroll;
 
 struct RowGrad {
-  float scale, lse, G, ge, H;
+  float a, nlse;  // ln p = a z + nlse
+  float A, B;     // dz = p (A ln p + B)
 };
-__device__ __forceinline__ float grad_smooth(float z, const RowGrad& r) {
-  const float lp = fmaf(z, r.scale, -r.lse);
-  const float pr = ex2_approx(lp * 1.4426950408889634f);
-  // p = 0: nothing flows, whatever ln p is (0 * inf must not turn into NaN)
-  const float w = fmaf(r.ge, lp + r.H, r.G);
-  const float v = -r.scale * (pr * w);
-  return pr == 0.f ? 0.f : v;
+// Logits are clamped as in the forward, so that ln p is finite and p = 0 gives 0.
+__device__ __forceinline__ float2 grad_smooth(float2 z, const RowGrad& r) {
+  const float2 lp = __ffma2_rn(z, make_float2(r.a, r.a), make_float2(r.nlse, r.nlse));
+  const float2 x = __fmul2_rn(lp, make_float2(1.4426950408889634f, 1.4426950408889634f));
+  const float2 w = __ffma2_rn(lp, make_float2(r.A, r.A), make_float2(r.B, r.B));
+  return __fmul2_rn(make_float2(ex2_approx(x.x), ex2_approx(x.y)), w);
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kLgThreads, 4) logits_bwd_kernel(const LogitsParams p, int spans) {
   using E = Elem<T>;
   constexpr int kN = E::kN;
-  const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x / spans;
-  const int span = blockIdx.x % spans;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int64_t row = blockIdx.x / unsigned(spans);
+  const int span = int(blockIdx.x % unsigned(spans));
   const int V = p.V, K = p.K;
   const T* zrow = reinterpret_cast<const T*>(p.z) + row * p.ld;
   T* drow = reinterpret_cast<T*>(p.dz) + row * p.ld_d;
@@ -804,74 +774,94 @@ __global__ void __launch_bounds__(kLgThreads, 4) logits_bwd_kernel(const LogitsP
     return;
   }
 
-  RowGrad r;
-  r.scale = p.scale;
-  r.lse = p.lse[row];
-  r.ge = p.g_entropy ? p.g_entropy[row] : 0.f;
-  r.H = p.g_entropy ? p.entropy[row] : 0.f;
-  const int target = p.g_logp ? p.targets[row] : -1;
-  r.G = target >= 0 && target < V ? p.g_logp[row] : 0.f;  // indexes outside [0, V) count for nothing
-  // a row without a finite logit, or with nothing but a type's lowest value as a mask: every p is 0
-  if (r.lse < -1e30f) r.lse = INFINITY;
-  if (p.g_top)
-    for (int k = 0; k < K; ++k) {
-      const int id = p.ids[row * K + k];
-      r.G += id >= 0 && id < V ? p.g_top[row * K + k] : 0.f;
-    }
+  uint4 v[kLgUnroll];
+#pragma unroll
+  for (int u = 0; u < kLgUnroll; ++u) {
+    const int i = w0 + u * kLgThreads + tid;
+    v[u] = make_uint4(0, 0, 0, 0);
+    if (together && i < w1) v[u] = *(reinterpret_cast<const uint4*>(zrow + nh) + i);
+  }
+  float zs = 0.f;
+  const int single = tid < nh ? tid : nv * kN + tid;
+  if (span == 0 && tid < nsingle) zs = E::one(zrow, single);
 
-  // the entries with a point term: thread 0 the target, thread 1 + k alternative k
+  // the row's factors; lane k of every warp holds alternative k
+  const int target = p.g_logp ? p.targets[row] : -1;
+  const bool target_in = target >= 0 && target < V;  // indexes outside [0, V) count for nothing
+  const float g_target = target_in ? p.g_logp[row] : 0.f;
+  int id = -1;
+  float g_id = 0.f;
+  if (lane < K) {
+    id = p.ids[row * K + lane];
+    if (id < 0 || id >= V) id = -1;
+    if (id >= 0) g_id = p.g_top[row * K + lane];
+  }
+  float G = g_target;
+  if (K) {
+    float sum = g_id;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    G += sum;
+  }
+  const float ge = p.g_entropy ? p.g_entropy[row] : 0.f;
+  const float H = p.g_entropy ? p.entropy[row] : 0.f;
+  float lse = p.lse[row];
+  // a row without a finite logit, or with nothing but a type's lowest value as a mask: every p is 0
+  if (lse < -1e30f) lse = 1e30f;
+  const RowGrad r = {p.scale, -lse, -p.scale * ge, -p.scale * fmaf(ge, H, G)};
+
+  // the entries with a point term: warp 0 the alternatives, warp 1 the target; each with all terms at its
+  // entry, so that equal indexes write the same value
   int at = -1;
-  float point = 0.f, z_at = 0.f;
-  if (tid == 0) at = target;
-  if (tid >= 1 && tid <= K && p.g_top) at = p.ids[row * K + tid - 1];
-  if (at >= V) at = -1;
-  if (at >= 0) {
-    // owned by the CTA that stores it
+  float point = 0.f;
+  if (warp == 0 && K) {
+    at = id;
+    if (id == target) point = g_target;
+    for (int k = 0; k < K; ++k) {
+      const int other = __shfl_sync(0xffffffffu, id, k);
+      const float g = __shfl_sync(0xffffffffu, g_id, k);
+      if (other == id) point += g;
+    }
+  } else if (warp == 1 && target_in) {
+    point = id == target ? g_id : 0.f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) point += __shfl_xor_sync(0xffffffffu, point, o);
+    point += g_target;
+    at = lane == 0 ? target : -1;
+  }
+  if (at >= 0) {  // owned by the CTA that stores it
     const int vec = (at - nh) / kN;
     const bool is_single = at < nh || at >= nh + nv * kN;
     if (is_single ? span != 0 : (vec < w0 || vec >= w1)) at = -1;
   }
-  if (at >= 0) {
-    z_at = E::one(zrow, at);
-    // every term at this entry, so that equal indexes write the same value
-    if (target == at) point += p.g_logp[row];
-    if (p.g_top)
-      for (int k = 0; k < K; ++k)
-        if (p.ids[row * K + k] == at) point += p.g_top[row * K + k];
-  }
-  const bool any_point = __syncthreads_or(at >= 0);
+  const float z_at = at >= 0 ? E::one(zrow, at) : 0.f;
+  const bool any_point = __syncthreads_or(at >= 0);  // the logits at these entries have been read
 
-  uint4 v[kLgUnroll];
-  if (together) {
-#pragma unroll
-    for (int u = 0; u < kLgUnroll; ++u) {
-      const int i = w0 + u * kLgThreads + tid;
-      if (i < w1) v[u] = *(reinterpret_cast<const uint4*>(zrow + nh) + i);
-    }
-  }
 #pragma unroll
   for (int u = 0; u < kLgUnroll; ++u) {
     const int i = w0 + u * kLgThreads + tid;
     if (i < w1) {
       float f[kN];
       if (together) {
-        E::widen(v[u], f);
+        E::widen(make_uint4(E::pclamp(v[u].x, p.clamp_pk), E::pclamp(v[u].y, p.clamp_pk),
+                            E::pclamp(v[u].z, p.clamp_pk), E::pclamp(v[u].w, p.clamp_pk)), f);
       } else {
 #pragma unroll
-        for (int e = 0; e < kN; ++e) f[e] = E::one(zrow, nh + int64_t(i) * kN + e);
+        for (int e = 0; e < kN; ++e) f[e] = max_nan(E::one(zrow, nh + int64_t(i) * kN + e), p.clamp);
       }
 #pragma unroll
-      for (int e = 0; e < kN; ++e) f[e] = grad_smooth(f[e], r);
+      for (int e = 0; e < kN; e += 2) {
+        const float2 d = grad_smooth(make_float2(f[e], f[e + 1]), r);
+        f[e] = d.x;
+        f[e + 1] = d.y;
+      }
       *reinterpret_cast<uint4*>(drow + nh + int64_t(i) * kN) = E::narrow(f);
     }
   }
-  if (span == 0 && tid < nsingle) {
-    const int i = tid < nh ? tid : nv * kN + tid;
-    E::put(drow, i, grad_smooth(E::one(zrow, i), r));
-  }
+  if (span == 0 && tid < nsingle) E::put(drow, single, grad_smooth(make_float2(max_nan(zs, p.clamp), 0.f), r).x);
   if (any_point) {
     __syncthreads();
-    if (at >= 0) E::put(drow, at, fmaf(r.scale, point, grad_smooth(z_at, r)));
+    if (at >= 0) E::put(drow, at, fmaf(r.a, point, grad_smooth(make_float2(max_nan(z_at, p.clamp), 0.f), r).x));
   }
 }
 
