@@ -213,6 +213,22 @@ static bool make_map_u8(CUtensorMap* m, const void* base, uint64_t rows, uint64_
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Matrix of 2- or 4-byte elements seen through boxes of 32 rows x 64 bytes (64-byte swizzle): how the block-scaled
+// product stores its result.
+static bool make_map_out(CUtensorMap* m, void* base, int32_t type, uint64_t rows, uint64_t cols, uint64_t ld) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const bool f32 = type == OAPL_TYPE_F32;
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {ld * (f32 ? 4 : 2)};
+  const cuuint32_t box[2] = {f32 ? 16u : 32u, 32};
+  const cuuint32_t estr[2] = {1, 1};
+  const CUtensorMapDataType t = f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                    : (type == OAPL_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
+  return fn(m, t, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static int sm_count() {
   static int n[kMaxDevices] = {0};
   int dev = 0;
@@ -767,8 +783,8 @@ static int launch_quantize(const QuantParams& qp, bool e5, bool block, bool turn
 }
 
 template <int OUT, bool PERCOL>
-static int launch_scaled_matmul(const CUtensorMap& a, const CUtensorMap& b, const ScaledParams& sp, int grid,
-                                cudaStream_t st) {
+static int launch_scaled_matmul(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& c, const ScaledParams& sp,
+                                int grid, cudaStream_t st) {
   static bool attr_set[kMaxDevices] = {false};
   auto kern = scaled_matmul_kernel<OUT, PERCOL>;
   int dev = -1;
@@ -781,7 +797,7 @@ static int launch_scaled_matmul(const CUtensorMap& a, const CUtensorMap& b, cons
       return OAPL_ERR_CUDA;
     attr_set[dev] = true;
   }
-  kern<<<grid, kSmThreads, kSmSmemBytes, st>>>(a, b, sp);
+  kern<<<grid, kSmThreads, kSmSmemBytes, st>>>(a, b, c, sp);
   CKL();
   return OAPL_OK;
 }
@@ -1503,7 +1519,11 @@ int oapl_scaled_matmul(const oapl_scaled* A, const oapl_scaled* B, void* C, int3
   sp.C = C;
   sp.ldc = ldc;
   sp.accumulate = accumulate != 0;
-  sp.wide = (((uintptr_t)C | (uintptr_t)(ldc * es)) & 31) == 0;
+  CUtensorMap tc = ta;
+  if (((uintptr_t)C & 15) == 0 && (ldc * es) % 16 == 0 && (!accumulate || c_type == OAPL_TYPE_F32)) {
+    if (!make_map_out(&tc, C, c_type, (uint64_t)A->rows, (uint64_t)B->rows, (uint64_t)ldc)) return OAPL_ERR_CUDA;
+    sp.bulk = accumulate ? 2 : 1;
+  }
   sp.e5_a = A->type == OAPL_TYPE_E5M2;
   sp.e5_b = B->type == OAPL_TYPE_E5M2;
   sp.mt = (sp.M + kSmTile - 1) / kSmTile;
@@ -1514,13 +1534,13 @@ int oapl_scaled_matmul(const oapl_scaled* A, const oapl_scaled* B, void* C, int3
   const int grid = 2 * (int)(tiles < n_sm / 2 ? tiles : n_sm / 2);
   const bool percol = sp.gb == 1;
   if (c_type == OAPL_TYPE_BF16)
-    return percol ? launch_scaled_matmul<OUT_BF16, true>(ta, tb, sp, grid, st)
-                  : launch_scaled_matmul<OUT_BF16, false>(ta, tb, sp, grid, st);
+    return percol ? launch_scaled_matmul<OUT_BF16, true>(ta, tb, tc, sp, grid, st)
+                  : launch_scaled_matmul<OUT_BF16, false>(ta, tb, tc, sp, grid, st);
   if (c_type == OAPL_TYPE_F16)
-    return percol ? launch_scaled_matmul<OUT_F16, true>(ta, tb, sp, grid, st)
-                  : launch_scaled_matmul<OUT_F16, false>(ta, tb, sp, grid, st);
-  return percol ? launch_scaled_matmul<OUT_F32, true>(ta, tb, sp, grid, st)
-                : launch_scaled_matmul<OUT_F32, false>(ta, tb, sp, grid, st);
+    return percol ? launch_scaled_matmul<OUT_F16, true>(ta, tb, tc, sp, grid, st)
+                  : launch_scaled_matmul<OUT_F16, false>(ta, tb, tc, sp, grid, st);
+  return percol ? launch_scaled_matmul<OUT_F32, true>(ta, tb, tc, sp, grid, st)
+                : launch_scaled_matmul<OUT_F32, false>(ta, tb, tc, sp, grid, st);
 }
 
 }  // extern "C"

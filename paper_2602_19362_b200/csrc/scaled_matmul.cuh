@@ -64,7 +64,7 @@ struct ScaledParams {
   void* C;
   int64_t ldc;
   int32_t accumulate;
-  int32_t wide;  // every row of C starts on a 32-byte boundary
+  int32_t bulk;  // C leaves by TMA: 1 store, 2 add (fp32), 0 not (rows off 16-byte boundaries, 16-bit sums)
   int32_t e5_a, e5_b;
   int32_t mt, nt, group;  // tiles along M and N; m tiles that are walked together
   int32_t* err;
@@ -135,10 +135,11 @@ struct OutElem<OUT_F32> {
   static __device__ __forceinline__ T put(float x) { return x; }
 };
 
-// 32 bytes to or from global memory in one access
-__device__ __forceinline__ void st32b(void* p, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+// Tile store from shared memory (bulk group); what lies outside the tensor is clipped.
+__device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(tmap)),
+               "r"(src), "r"(x), "r"(y)
                : "memory");
 }
 
@@ -146,7 +147,7 @@ __device__ __forceinline__ void st32b(void* p, const uint32_t (&w)[8]) {
 template <int OUT, bool PERCOL>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kSmThreads, 1)
 scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                     const ScaledParams p) {
+                     const __grid_constant__ CUtensorMap tmC, const ScaledParams p) {
   using O = OutElem<OUT>;
   using OT = typename O::T;
   extern __shared__ uint8_t smem_raw[];
@@ -376,29 +377,52 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       const int col0 = n0 + half * 128;
       if (row0 >= p.M || col0 >= p.N) continue;
       OT* C = reinterpret_cast<OT*>(p.C);
-      if (p.wide && !p.accumulate && col0 + 128 <= p.N) {
-        if (row0 + lane < p.M) {
-          OT* dst = C + int64_t(row0 + lane) * p.ldc + col0;
-          constexpr int kPer = 32 / sizeof(OT);  // elements of a 32-byte store
+      if (p.bulk) {
+        // 64 bytes of every row at a time through one of two swizzled 2 KB pieces; the stores run on under the
+        // next tile
+        constexpr int kCols = 64 / sizeof(OT);
+        uint8_t* two = smem + kOutOff + (warp - 4) * 4096;
 #pragma unroll
-          for (int q = 0; q < 128 / kPer; ++q) {
-            uint32_t w[8];
+        for (int q = 0; q < 128 / kCols; ++q) {
+          uint8_t* out = two + (q & 1) * 2048;
+          if (lane == 0) tma_store_wait_read<1>();
+          __syncwarp();
+          uint4* line = reinterpret_cast<uint4*>(out + lane * 64);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+          for (int c = 0; c < 4; ++c) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
               if (OUT == OUT_F32) {
-                w[i] = __float_as_uint(i & 1 ? acc[q * 4 + i / 2].y : acc[q * 4 + i / 2].x);
-              } else if (OUT == OUT_BF16) {
-                w[i] = pack_bf16x2(acc[q * 8 + i].x, acc[q * 8 + i].y);
+                const float2 x = acc[q * 8 + c * 2 + i / 2];
+                w[i] = __float_as_uint(i & 1 ? x.y : x.x);
               } else {
-                const __half2 h = __floats2half2_rn(acc[q * 8 + i].x, acc[q * 8 + i].y);
-                w[i] = *reinterpret_cast<const uint32_t*>(&h);
+                const float2 x = acc[q * 16 + c * 4 + i];
+                if (OUT == OUT_BF16) {
+                  w[i] = pack_bf16x2(x.x, x.y);
+                } else {
+                  const __half2 h = __floats2half2_rn(x.x, x.y);
+                  w[i] = *reinterpret_cast<const uint32_t*>(&h);
+                }
               }
             }
-            st32b(dst + q * kPer, w);
+            line[c ^ ((lane >> 1) & 3)] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            const int x = col0 + q * kCols;
+            if (x < p.N) {
+              if (p.bulk == 2)
+                tma_reduce_add_2d(&tmC, smem_u32(out), x, row0);
+              else
+                tma_store_2d(&tmC, smem_u32(out), x, row0);
+            }
+            tma_store_commit();
           }
         }
       } else {
-        // any alignment, edges, accumulation: 32 x 32 pieces through shared memory, a row at a time
+        // any alignment, sums in 16 bits: 32 x 32 pieces through shared memory, a row at a time
         const int rows = min(32, p.M - row0);
 #pragma unroll
         for (int q = 0; q < 128 / kSmOutCols; ++q) {
@@ -422,6 +446,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         }
       }
     }
+    if (lane == 0) tma_store_wait_all();  // before shared memory is released
   }
 
   // ---------------------------------------------------------------- teardown
