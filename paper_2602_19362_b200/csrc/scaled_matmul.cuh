@@ -11,9 +11,9 @@
 // the tensor cores about 512 cycles per pair.  Two things bound it: the hand-over of the two accumulators
 // (a K block every 670 cycles with an epilogue that does nothing) and the epilogue warps' way through a block,
 // a chain of waits that more warps with fewer columns each shorten; in long calls, the power limit.
-// Warp 0 issues TMA loads, warp 1 owns TMEM and (in the leader) issues the MMAs, warp 2 copies the scales to
-// shared memory a few K blocks ahead (cp.async).  It arrives on the accumulator's barrier as the tensor cores
-// do, so the epilogue waits once per block.  Warps 4 to 11 are the epilogue: quadrant warp & 3 of the TMEM
+// Warp 0 issues TMA loads, warp 1 owns TMEM and (in the leader) issues the MMAs, warps 2 and 3 copy the scales
+// of rows and columns to shared memory a few K blocks ahead (cp.async).  They arrive on the accumulator's
+// barrier as the tensor cores do, so the epilogue waits once per block.  Warps 4 to 11 are the epilogue: quadrant warp & 3 of the TMEM
 // lanes, one half of the columns each.
 #pragma once
 #include <cuda.h>
@@ -42,16 +42,11 @@ constexpr int kSmOutBytes = kSmEpiWarps * 32 * kSmOutPitch * 4;
 constexpr size_t kSmSmemBytes = size_t(kSmStages) * kSmStageBytes + kSmSlots * kSmSlotFloats * 4 +
                                 kSmOutBytes + 1024 /*align*/ + 512 /*barriers*/;
 static_assert(kSmSmemBytes <= 227 * 1024, "shared memory of a CTA");
-// Registers of a thread: 168 at launch (what 384 threads can have), then few for the four warps that move data
-// and the rest for the epilogue, whose loop holds 192 values: 128 low + 256 high = 384 * 168.  Scales per column
-// need more in warp 2.  (4096 x 152064 x 3584: 2.15 ms with 24 / 240, 2.27 with 40 / 232, 2.5 with 56 / 224, where
-// the loop spills; 8192^3 with a scale per column 0.78 and 0.74 ms.)
-constexpr int kSmRegs = 168;
-template <bool PERCOL>
-struct SmRegs {
-  static constexpr int kLow = PERCOL ? 40 : 24, kHigh = PERCOL ? 232 : 240;
-  static_assert(128 * kLow + 256 * kHigh == kSmThreads * kSmRegs, "register split");
-};
+// Registers of a thread: 168 at launch (what 384 threads can have), then 24 for the four warps that move data
+// and 240 for the epilogue, whose loop holds 192 values: 128 * 24 + 256 * 240 = 384 * 168.  (4096 x 152064 x 3584:
+// 2.15 ms, 2.27 with 40 / 232, 2.5 with 56 / 224, where the loop spills.)
+constexpr int kSmRegs = 168, kSmRegsLow = 24, kSmRegsHigh = 240;
+static_assert(128 * kSmRegsLow + 256 * kSmRegsHigh == kSmThreads * kSmRegs, "register split");
 
 enum { OUT_BF16 = 0, OUT_F16 = 1, OUT_F32 = 2 };
 
@@ -178,7 +173,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       mbar_init(empty_bar(s), 1);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(tfull_bar(b), 2);                 // the tensor cores and warp 2
+      mbar_init(tfull_bar(b), 3);                 // the tensor cores, warps 2 and 3
       mbar_init(tempty_bar(b), 2 * kSmEpiWarps);  // the leader's copy counts the warps of both CTAs
     }
     for (int h = 0; h < kSmSlots / kSmFree; ++h) mbar_init(sempty_bar(h), kSmEpiWarps);
@@ -197,7 +192,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   int m0, n0;
 
   if (warp < 4) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(SmRegs<PERCOL>::kLow));
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kSmRegsLow));
   if (warp == 0) {
     // ------------------------------------------------------------ operand loads
     if (lane == 0) {
@@ -245,34 +240,33 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         }
       }
     }
-  } else if (warp == 2) {
-    // ------------------------------------------------------------ scales
-    constexpr int kCols = PERCOL ? kSmTile / 32 : 1;  // copies per lane for the columns
-    const int64_t da = p.ga == 1 ? 32 * p.sa_row : 0, db = 32 * p.sb_row;
-    const uint32_t dst0 = smem_u32(scales) + 4 * lane;
-    const float *pa = p.sa, *pb = p.sb;
-    int pj = 0, pkb = 0, left_m = 0, left_n = 0;  // left: rows of A and of B from this lane's first one on
+  } else {
+    // ------------------------------------------------------------ scales: warp 2 the rows', warp 3 the columns'
+    const bool cols = warp == 3;
+    const int64_t step = cols ? (PERCOL ? 32 * p.sb_row : 0) : (p.ga == 1 ? 32 * p.sa_row : 0);
+    const int64_t ahead = cols ? p.sb_col : p.sa_col;
+    const uint32_t dst0 = smem_u32(scales) + 4 * (lane + (cols ? kSmHalf : 0));
+    const float* at = p.sa;
+    int pj = 0, pkb = 0, left = 0;  // left: rows from this lane's first one on; 32 apart, as far as they go
     auto seek = [&]() {
-      if (!scaled_tile(p, pj, m0, n0)) {
-        left_m = left_n = 0;
-        return;
+      left = 0;
+      if (!scaled_tile(p, pj, m0, n0)) return;
+      if (cols) {
+        const int c = n0 + (PERCOL ? lane : lane * 128);
+        if (PERCOL || lane < 2) left = PERCOL ? p.N - c : min(p.N - c, 1);
+        at = p.sb + int64_t(PERCOL ? c : c >> 7) * p.sb_row;
+      } else {
+        const int r = m0 + int(rank) * kSmHalf + lane;
+        left = min(p.M - r, kSmHalf - lane);
+        at = p.sa + int64_t(p.ga == 1 ? r : r >> 7) * p.sa_row;
       }
-      const int r = m0 + int(rank) * kSmHalf + lane, c = n0 + (PERCOL ? lane : lane * 128);
-      left_m = p.M - r;
-      left_n = PERCOL || lane < 2 ? p.N - c : 0;
-      pa = p.sa + int64_t(p.ga == 1 ? r : r >> 7) * p.sa_row;
-      pb = p.sb + int64_t(PERCOL ? c : c >> 7) * p.sb_row;
     };
     auto copy = [&](uint32_t t) {  // of the next K block, number t; rows behind the last keep what was there
       const uint32_t dst = dst0 + (t % kSmSlots) * (kSmSlotFloats * 4);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i * 32 < left_m) cp_async4(dst + i * 128, pa + i * da);
-#pragma unroll
-      for (int i = 0; i < kCols; ++i)
-        if (i * 32 < left_n) cp_async4(dst + kSmHalf * 4 + i * 128, pb + i * db);
-      pa += p.sa_col;
-      pb += p.sb_col;
+      for (int i = 0; i < kSmTile / 32; ++i)
+        if (i * 32 < left) cp_async4(dst + i * 128, at + i * step);
+      at += ahead;
       if (++pkb == nk) {
         pkb = 0;
         ++pj;
@@ -310,7 +304,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
   }
   } else {
     // ------------------------------------------------------------ epilogue
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SmRegs<PERCOL>::kHigh));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSmRegsHigh));
     const int quad = warp & 3;
     const int half = (warp - 4) >> 2;  // columns [128 half, 128 half + 128)
     const uint32_t tlane = tmem_base + (uint32_t(quad * 32) << 16) + half * 128;
