@@ -12,7 +12,7 @@
 // finite values 0 and itself NaN.
 //
 // HBM-bound: x is read once and q written once.  A CTA takes a 128 x 128 tile, which it holds in registers
-// between the maximum and the rounding: 8 rows x 16 bytes a thread, all loads in flight together, four CTAs
+// between the maximum and the rounding: 8 rows x 16 bytes a thread, all loads in flight together, five CTAs
 // (16-bit types) per SM.  Maxima are taken on packed words; what rounding needs of a block is computed once
 // and shared.  Rows that do not start on a 16-byte boundary are read as the aligned 16-byte blocks that hold
 // them (a block without an element of the row is not touched) and shifted in registers.  A turned tile goes
@@ -126,7 +126,7 @@ __device__ __forceinline__ uint4 shift_bytes(const uint4& lo, const uint4& hi, u
 }
 
 template <typename T, int E5M2, bool BLOCK, bool TURN>
-__global__ void __launch_bounds__(kQtGroups * kQtTile / Elem<T>::kN, sizeof(T) == 4 ? 2 : 4)
+__global__ void __launch_bounds__(kQtGroups * kQtTile / Elem<T>::kN, sizeof(T) == 4 ? 2 : 5)
 quantize_kernel(const QuantParams p) {
   using E = Elem<T>;
   constexpr int kN = E::kN;                    // columns of a thread
@@ -246,62 +246,57 @@ quantize_kernel(const QuantParams p) {
   __syncthreads();
 
   // ---- round and store
-  QuantScale qs[TURN && !BLOCK ? kN : 1];
-  if (TURN && !BLOCK) {
+  if (!TURN) {
+    QuantScale qs = sh_qs[0];
 #pragma unroll
-    for (int e = 0; e < kN; ++e) qs[e] = sh_qs[lane * kN + e];
-  } else {
-    qs[0] = sh_qs[0];
-  }
+    for (int i = 0; i < kQtRows; ++i) {
+      if (!BLOCK) qs = sh_qs[group * kQtRows + i];
+      float f[kN];
+      E::widen(v[i], f);
 #pragma unroll
-  for (int i = 0; i < kQtRows; ++i) {
-    if (!BLOCK && !TURN) qs[0] = sh_qs[group * kQtRows + i];
-    float f[kN];
-    E::widen(v[i], f);
+      for (int e = 0; e < kN; ++e) f[e] = quant_one(f[e], qs);
+      uint32_t w[kN / 4];
 #pragma unroll
-    for (int e = 0; e < kN; ++e) f[e] = quant_one(f[e], qs[TURN && !BLOCK ? e : 0]);
-    uint32_t w[kN / 4];
+      for (int e = 0; e < kN; e += 4)
+        w[e / 4] = cvt_fp8x2<E5M2>(f[e], f[e + 1]) | (cvt_fp8x2<E5M2>(f[e + 2], f[e + 3]) << 16);
+      if (row + i < p.R) {
+        uint8_t* q = p.q + int64_t(row + i) * p.ldq + col;
+        if (col + kN <= p.C) {
+          if (kN == 8)
+            *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+          else
+            *reinterpret_cast<uint32_t*>(q) = w[0];
+        } else {
 #pragma unroll
-    for (int e = 0; e < kN; e += 4)
-      w[e / 4] = cvt_fp8x2<E5M2>(f[e], f[e + 1]) | (cvt_fp8x2<E5M2>(f[e + 2], f[e + 3]) << 16);
-    if (TURN) {
-      v[i].x = w[0];
-      if (kN == 8) v[i].y = w[1];
-    } else if (row + i < p.R) {
-      uint8_t* q = p.q + int64_t(row + i) * p.ldq + col;
-      if (col + kN <= p.C) {
-        if (kN == 8)
-          *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
-        else
-          *reinterpret_cast<uint32_t*>(q) = w[0];
-      } else {
-#pragma unroll
-        for (int e = 0; e < kN; ++e)
-          if (col + e < p.C) q[e] = uint8_t(w[e / 4] >> (8 * (e & 3)));
+          for (int e = 0; e < kN; ++e)
+            if (col + e < p.C) q[e] = uint8_t(w[e / 4] >> (8 * (e & 3)));
+        }
       }
     }
-  }
-  if (TURN) {
-    // Four bytes of a column from four rows: a 4 x 4 byte transposition per word.  8-byte unit u of row c
-    // sits at u ^ (c / kN), which spreads a warp's stores over all banks.
+  } else {
+    // Two columns at a time, so that their words and factors are done with: eight rows of the pair, rounded,
+    // are turned into eight bytes of each column.  8-byte unit u of row c of the turned tile sits at
+    // u ^ (c / kN), which spreads a warp's stores over all banks.
 #pragma unroll
-    for (int h = 0; h < kN / 4; ++h) {
-      uint32_t t[2][4];
+    for (int e = 0; e < kN; e += 2) {
+      const QuantScale s0 = sh_qs[BLOCK ? 0 : lane * kN + e], s1 = sh_qs[BLOCK ? 0 : lane * kN + e + 1];
+      uint32_t r[kQtRows];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t a = h ? v[4 * k].y : v[4 * k].x, b = h ? v[4 * k + 1].y : v[4 * k + 1].x;
-        const uint32_t c = h ? v[4 * k + 2].y : v[4 * k + 2].x, d = h ? v[4 * k + 3].y : v[4 * k + 3].x;
-        const uint32_t ab0 = __byte_perm(a, b, 0x5140), ab1 = __byte_perm(a, b, 0x7362);
-        const uint32_t cd0 = __byte_perm(c, d, 0x5140), cd1 = __byte_perm(c, d, 0x7362);
-        t[k][0] = __byte_perm(ab0, cd0, 0x5410);
-        t[k][1] = __byte_perm(ab0, cd0, 0x7632);
-        t[k][2] = __byte_perm(ab1, cd1, 0x5410);
-        t[k][3] = __byte_perm(ab1, cd1, 0x7632);
+      for (int i = 0; i < kQtRows; ++i) {
+        float f[kN];
+        E::widen(v[i], f);
+        r[i] = cvt_fp8x2<E5M2>(quant_one(f[e], s0), quant_one(f[e + 1], s1));
       }
+      uint32_t lo[2], hi[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<uint2*>(sh_tile + (lane * kN + h * 4 + e) * kQtTile + ((group ^ (lane & 15)) * 8)) =
-            make_uint2(t[0][e], t[1][e]);
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t a = __byte_perm(r[4 * h], r[4 * h + 1], 0x5140), c = __byte_perm(r[4 * h + 2], r[4 * h + 3], 0x5140);
+        lo[h] = __byte_perm(a, c, 0x5410);
+        hi[h] = __byte_perm(a, c, 0x7632);
+      }
+      uint8_t* to = sh_tile + (lane * kN + e) * kQtTile + ((group ^ (lane & 15)) * 8);
+      *reinterpret_cast<uint2*>(to) = make_uint2(lo[0], lo[1]);
+      *reinterpret_cast<uint2*>(to + kQtTile) = make_uint2(hi[0], hi[1]);
     }
     __syncthreads();
 #pragma unroll
