@@ -138,8 +138,10 @@ quantize_kernel(const QuantParams p) {
   __shared__ __align__(16) uint8_t sh_tile[TURN ? kQtTile * kQtTile : 16];
 
   const int tid = threadIdx.x, lane = tid % kLanes, group = tid / kLanes;
-  const int tiles_c = (p.C + kQtTile - 1) / kQtTile;
-  const int r0 = int(blockIdx.x / tiles_c) * kQtTile, c0 = int(blockIdx.x % tiles_c) * kQtTile;
+  // neighbours in the order of the result's rows, whose lines they share (1999 x 50021 turned: 66 us against 73)
+  const unsigned inner = (unsigned(TURN ? p.R : p.C) + kQtTile - 1) / kQtTile;
+  const int a0 = int(blockIdx.x / inner) * kQtTile, b0 = int(blockIdx.x % inner) * kQtTile;
+  const int r0 = TURN ? b0 : a0, c0 = TURN ? a0 : b0;
   const int row = r0 + group * kQtRows, col = c0 + lane * kN;
 
   // ---- the thread's 8 x kN values
