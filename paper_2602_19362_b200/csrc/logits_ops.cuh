@@ -311,7 +311,7 @@ __device__ __forceinline__ void st_cluster_u64(uint32_t addr, uint64_t v) {
 // ------------------------------------------------------------------------------------ forward
 // The pass clamps logits where c z = -2^27 (a packed maximum), so that -inf and large negative masks give
 // 2^x = 0 and a finite x: below 2^27 in magnitude, x is off from c z - R by at most 8.  (fp16 ends at
-// -65504: there only -inf is clamped.)  That is exact for every row whose largest logit m lies 1000 / c
+// -65504: there only -inf is clamped.)  That is exact for every row whose largest logit m lies 512 / c
 // above the clamp, with |c m| < 2^26.  The others are done again by row_slow, which is only careful: rows
 // that hold nothing but masked logits, an infinity, or a huge common offset.
 //
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
   if (rank == nc - 1 && tid < nsingle) zs = E::one(zrow, tid < q.nh ? tid : q.nv * kN + tid);
 
   RowSums r;
-  r.R = fmaf(p.clamp, c, 1000.f);  // a clamped logit counts for nothing
+  r.R = fmaf(p.clamp, c, 256.f);  // a clamped logit counts for nothing
   r.s = r.t = make_float2(0.f, 0.f);
   float tmax = p.clamp, gm = p.clamp;
   int g = 0, in_group = 0;
@@ -706,7 +706,7 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
 
   // ---- results
   const float ln2 = 0.6931471805599453f;
-  const bool plain = fabsf(tot.m * c) < kLgPlainX && (tot.m - p.clamp) * c > 1000.f;  // the same for all threads
+  const bool plain = fabsf(tot.m * c) < kLgPlainX && (tot.m - p.clamp) * c > 512.f;  // the same for all threads
   if (!plain) tot = row_slow<T, NT>(zrow, V, c, sh_tot);
   // no finite logit: every probability is 0, lse = -inf, nothing to choose from
   const bool empty = tot.m == -INFINITY && tot.s == 0.f;
@@ -745,9 +745,10 @@ struct RowGrad {
   float a, nlse;  // ln p = a z + nlse
   float A, B;     // dz = p (A ln p + B)
 };
-// Logits are clamped as in the forward, so that ln p is finite and p = 0 gives 0.
+// ln p is kept finite, so that p = 0 gives 0.
 __device__ __forceinline__ float2 grad_smooth(float2 z, const RowGrad& r) {
-  const float2 lp = __ffma2_rn(z, make_float2(r.a, r.a), make_float2(r.nlse, r.nlse));
+  float2 lp = __ffma2_rn(z, make_float2(r.a, r.a), make_float2(r.nlse, r.nlse));
+  lp = make_float2(max_nan(lp.x, -1e5f), max_nan(lp.y, -1e5f));
   const float2 x = __fmul2_rn(lp, make_float2(1.4426950408889634f, 1.4426950408889634f));
   const float2 w = __ffma2_rn(lp, make_float2(r.A, r.A), make_float2(r.B, r.B));
   return __fmul2_rn(make_float2(ex2_approx(x.x), ex2_approx(x.y)), w);
@@ -851,11 +852,10 @@ __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsP
     if (i < w1) {
       float f[kN];
       if (together) {
-        E::widen(make_uint4(E::pclamp(v[u].x, p.clamp_pk), E::pclamp(v[u].y, p.clamp_pk),
-                            E::pclamp(v[u].z, p.clamp_pk), E::pclamp(v[u].w, p.clamp_pk)), f);
+        E::widen(v[u], f);
       } else {
 #pragma unroll
-        for (int e = 0; e < kN; ++e) f[e] = max_nan(E::one(zrow, nh + int64_t(i) * kN + e), p.clamp);
+        for (int e = 0; e < kN; ++e) f[e] = E::one(zrow, nh + int64_t(i) * kN + e);
       }
 #pragma unroll
       for (int e = 0; e < kN; e += 2) {
@@ -866,10 +866,10 @@ __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsP
       *reinterpret_cast<uint4*>(drow + nh + int64_t(i) * kN) = E::narrow(f);
     }
   }
-  if (span == 0 && tid < nsingle) E::put(drow, single, grad_smooth(make_float2(max_nan(zs, p.clamp), 0.f), r).x);
+  if (span == 0 && tid < nsingle) E::put(drow, single, grad_smooth(make_float2(zs, 0.f), r).x);
   if (any_point) {
     __syncthreads();
-    if (at >= 0) E::put(drow, at, fmaf(r.a, point, grad_smooth(make_float2(max_nan(z_at, p.clamp), 0.f), r).x));
+    if (at >= 0) E::put(drow, at, fmaf(r.a, point, grad_smooth(make_float2(z_at, 0.f), r).x));
   }
 }
 

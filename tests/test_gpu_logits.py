@@ -153,6 +153,36 @@ def test_forward_masked_and_extreme_logits(t, V):
     check_fwd(z, targets, None, 6)
 
 
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("scale", [1e-30, 0.003, 0.02, 40.0, 3000.0])
+def test_forward_and_gradient_over_scales(t, scale):
+    z, targets, mask = make(30, 5003, t, 3)
+    z = z.clone()
+    z[1, ::2] = -math.inf
+    z[2, 1:] = torch.finfo(z.dtype).min
+    targets[1], targets[2] = 1, 0
+    _, _, lse, _, _ = check_fwd(z, targets, mask, 4, scale)
+    g = torch.randn(30, device="cuda")
+    check_bwd(z, targets, mask, g, g, None, None, scale)
+
+
+@pytest.mark.parametrize("t,low", [("bf16", -1e4), ("bf16", -1e9), ("f32", -1e9), ("f16", -6e4), ("f32", -1e20), ("f16", -65504.0)])
+def test_rows_of_finite_mask_values(t, low):
+    z, targets, _ = make(6, 3001, t, 8)
+    z = z.clone()
+    z[0, 7:] = low                          # a few tokens left
+    z[1] = low                              # none left: uniform
+    z[2] = low
+    z[2, ::2] = -math.inf                   # and some excluded altogether
+    z[3, :-1] = low
+    targets[:4] = torch.tensor([3, 5, 1, 3000])
+    _, _, lse, _, _ = check_fwd(z, targets, None, 4)
+    g = torch.randn(6, device="cuda")
+    ok = lse.abs() < 2.0 ** 24              # beyond, fp32 log-sum-exps carry no probabilities
+    zz, tt, gg = z[ok].contiguous(), targets[ok].contiguous(), g[ok].contiguous()
+    check_bwd(zz, tt, None, gg, gg, None, None)
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf])
 @pytest.mark.parametrize("V", [6, 4096, 30011])
 def test_forward_rows_with_nan_or_inf(bad, V):
@@ -238,9 +268,10 @@ def ref_bwd(z, targets, mask, lse, ent, gl, ge, gt, ids, scale):
         part = ge.double()[:, None] * (torch.where(p > 0, lp, torch.zeros_like(lp)) + ent.double()[:, None])
     d = scale * (-torch.where(p > 0, p * (inner + part), torch.zeros_like(p)) + point)
     live = mask.bool()[:, None]
-    size = scale * p * (inner.abs() + part.abs() * 2 + (ge.double().abs()[:, None] if ge is not None else 0.0))
+    factor = scale * (inner.abs() + part.abs() * 2 + (ge.double().abs()[:, None] if ge is not None else 0.0))
     dist = (z.double() * scale).abs().nan_to_num(0, 0, 0) + lse.double().abs().nan_to_num(0, 0, 0)[:, None]
-    return torch.where(live, d, 0.0), torch.where(live, size, 0.0), dist, torch.where(live, point.abs() * scale, 0.0)
+    zero = torch.zeros_like(d)
+    return tuple(torch.where(live, x, zero) for x in (d, factor * p, dist, point.abs() * scale, factor))
 
 
 def check_bwd(z, targets, mask, gl, ge, gt, ids, scale=1.0, pad=0, offset=0):
@@ -252,12 +283,13 @@ def check_bwd(z, targets, mask, gl, ge, gt, ids, scale=1.0, pad=0, offset=0):
     d = flat[offset:].view(N, V + pad)[:, :V]
     B.oapl_logits_logprobs_bwd(L, lse, ent, gl, ge, gt, ids, d)
     m = mask if mask is not None else torch.ones(N, device="cuda")
-    want, size, dist, point = ref_bwd(z, targets, m, lse, ent, gl, ge, gt, ids, scale)
+    want, size, dist, point, factor = ref_bwd(z, targets, m, lse, ent, gl, ge, gt, ids, scale)
     fi = torch.finfo(z.dtype)
     # one rounding to the type; p: 2^-22 of the exponential and three roundings of an exponent of size dist;
     # a few roundings of the factors and of the sum with the point term
     tol = fi.eps / 2 * want.abs() + size * (2.0 ** -22 + (3 * dist + 8 + gt_terms(gt)) * U) * (1 + fi.eps) + (4 + gt_terms(gt)) * U * point
-    tol = tol + fi.smallest_normal * fi.eps + 1e-37
+    # p below the smallest normal fp32 number, 2^-126, is 0 there: off by no more than that times its factor
+    tol = tol + fi.smallest_normal * fi.eps + 1e-37 + factor * 2.0 ** -126
     close(d, want, tol, "dlogits")
     if pad:
         assert bool((flat[offset:].view(N, V + pad)[:, V:] == 5.0).all())

@@ -258,6 +258,55 @@ def test_matmul_repeats_bit_for_bit_and_on_two_streams():
     assert all(torch.equal(x, y) for x, y in zip(outs, want))
 
 
+def test_captured_and_replayed():
+    x, w = torch.randn(300, 700, device="cuda"), torch.randn(500, 700, device="cuda").to(torch.bfloat16)
+    A, W = B.alloc_scaled(300, 700, 1), B.alloc_scaled(500, 700, 128)
+    few = B.alloc_scaled(9, 700, 1)
+    C, D = torch.zeros(300, 500, device="cuda"), torch.zeros(9, 500, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        B.oapl_quantize(x, A)
+        B.oapl_quantize(x[:9], few)
+        B.oapl_quantize(w, W)
+        B.oapl_scaled_matmul(A, W, C)
+        B.oapl_scaled_matmul(few, W, D)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    x.normal_()
+    graph.replay()
+    torch.cuda.synchronize()
+    got = C.clone(), D.clone()
+    C.zero_()
+    D.zero_()
+    step()
+    assert torch.equal(got[0], C) and torch.equal(got[1], D)
+    assert float((C.double() - widen(A) @ widen(W).t()).abs().max()) < 1e-3
+
+
+def test_matmul_row_offsets_beyond_32_bits():
+    # the last rows of the weight, and of the result, start past 2^31 bytes and elements
+    N, K = 18000, 131072
+    W = B.make_scaled(torch.zeros(N, K, dtype=torch.uint8, device="cuda").view(F8["e4m3"]),
+                      torch.ones(-(-N // 128), K // 128, device="cuda"), 128)
+    W.tensors[0][N - 3:] = torch.randn(3, K, device="cuda").to(F8["e4m3"])
+    for M in (2, 70):
+        A = rand_scaled(M, K, 1, "e4m3", 1)
+        C = torch.full((M, N), 7.0, device="cuda")
+        B.oapl_scaled_matmul(A, W, C)
+        want = widen(A) @ W.tensors[0][N - 3:].double().t()
+        assert float((C[:, N - 3:].double() - want).abs().max()) <= 1e-5 * float(widen(A).abs().sum(1).max()) * 4
+        assert bool((C[:, :N - 3] == 0).all())
+    del W
+    M, N = 70000, 32768
+    C = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    A, W = rand_scaled(M, 128, 1, "e4m3", 1), rand_scaled(N, 128, 128, "e4m3", 2)
+    B.oapl_scaled_matmul(A, W, C)
+    want = widen(A)[-5:] @ widen(W).t()
+    assert float((C[-5:].double() - want).norm() / want.norm()) < 2.0 ** -8
+    assert not bool((C == 7.0).all(1).any())
+
+
 def test_binding_refusals():
     A, W = rand_scaled(4, 256, 1, "e4m3", 1), rand_scaled(64, 256, 128, "e4m3", 2)
     with pytest.raises(TypeError):
