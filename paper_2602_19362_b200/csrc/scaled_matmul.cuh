@@ -465,9 +465,11 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 // ------------------------------------------------------------------------------------ few rows
 // The same product for at most 64 rows of A (decoded tokens): HBM-bound by B, the weight.  The roles are
 // swapped: rows of B fill the 128 lanes of the accumulator and the rows of A are its NT = 16, 32 or 64 columns,
-// so a token costs what it needs and the 512 TMEM columns hold 512 / NT accumulators (at most 16): the hand-over
-// of an accumulator, about 900 cycles, is spread over as many K blocks.  (152064 x 3584, one token to 64: 97 to
-// 114 us against 144 to 129 with the kernel above; 128 tokens: 165 against 143, which therefore takes them.)  B's rows are shared out evenly: with
+// so a token costs what it needs.  Everything that the warps hand to one another (stages, accumulators, scales)
+// goes in batches of kBatch K blocks, because each hand-over costs its warp some 300 to 500 cycles, more than a
+// block of a small tile takes to load.  (152064 x 3584, one token to 64: 83 to
+// 100 us, 97 to 114 with batches of one, 144 to 129 with the kernel above; 3584 x 3584, one token: 7.8 us, 8.6 with
+// batches of two, 12.0 with one.  128 tokens: 146 against 137, which therefore takes them.)  B's rows are shared out evenly: with
 // S SMs and k = ceil(N / (128 S)) rounds a CTA takes tiles of ceil(N / (k S)) rows, 25 of 3584 and 115 of 152064
 // on 148 SMs, so that a small weight keeps every SM busy and a large one ends everywhere at the same time.
 // No pairs: one CTA per SM, all its shared memory as stages of the weight stream.
@@ -477,15 +479,15 @@ constexpr int kFwThreads = 32 * (4 + kFwEpiWarps);
 
 template <int NT>
 struct FewCfg {
-  static constexpr int kStageBytes = (kFwRows + NT) * kSmKB;
-  static constexpr int kStages = NT <= 32 ? 9 : 7;
-  static constexpr int kBufs = 512 / NT < 16 ? 512 / NT : 16;
-  static constexpr int kTmemCols = kBufs * NT;  // a power of two, at least 32
-  static constexpr int kSlots = 32;             // K blocks whose scales have room
-  static constexpr int kAhead = 16;
-  static constexpr int kFree = 8;
-  static constexpr int kSlotFloats = kFwRows + NT;
-  static constexpr size_t kSmemBytes = size_t(kStages) * kStageBytes + kSlots * kSlotFloats * 4 + 1024 + 1024;
+  static constexpr int kBatch = NT <= 16 ? 4 : 2;  // K blocks handed over together
+  static constexpr int kBlockBytes = (kFwRows + NT) * kSmKB;
+  static constexpr int kStages = NT <= 16 ? 2 : (NT <= 32 ? 5 : 4);
+  static constexpr int kBufs = 4;               // batches of accumulators
+  static constexpr int kTmemCols = kBufs * kBatch * NT;  // 256 or 512
+  static constexpr int kSlots = 8;              // batches whose scales have room
+  static constexpr int kAhead = 5;
+  static constexpr int kSlotFloats = kBatch * (kFwRows + NT);
+  static constexpr size_t kSmemBytes = size_t(kStages) * kBatch * kBlockBytes + kSlots * kSlotFloats * 4 + 1024 + 512;
   static_assert(kSmemBytes <= 227 * 1024, "shared memory of a CTA");
 };
 
@@ -545,7 +547,9 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* smem = smem_raw + (base - raw);
-  constexpr uint32_t kScaleOff = kStages * Cfg::kStageBytes;
+  constexpr int kBatch = Cfg::kBatch;
+  constexpr uint32_t kStageBytes = kBatch * Cfg::kBlockBytes;
+  constexpr uint32_t kScaleOff = kStages * kStageBytes;
   constexpr uint32_t kBarOff = kScaleOff + Cfg::kSlots * Cfg::kSlotFloats * 4;
   float* scales = reinterpret_cast<float*>(smem + kScaleOff);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kBarOff);
@@ -555,8 +559,8 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
   auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * kStages + kBufs + b); };
   auto sempty_bar = [&](int h) { return bar0 + 8u * (2 * kStages + 2 * kBufs + h); };
-  constexpr int kBars = 2 * kStages + 2 * kBufs + Cfg::kSlots / Cfg::kFree;
-  static_assert(8 * (kBars + 2) <= 1024, "barriers");
+  constexpr int kBars = 2 * kStages + 2 * kBufs + Cfg::kSlots;
+  static_assert(8 * (kBars + 2) <= 512, "barriers");
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kBars + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -570,7 +574,7 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       mbar_init(tfull_bar(b), 2);  // the tensor cores and warp 2
       mbar_init(tempty_bar(b), kFwEpiWarps);
     }
-    for (int h = 0; h < Cfg::kSlots / Cfg::kFree; ++h) mbar_init(sempty_bar(h), kFwEpiWarps);
+    for (int h = 0; h < Cfg::kSlots; ++h) mbar_init(sempty_bar(h), kFwEpiWarps);
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tmW);
@@ -586,25 +590,30 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  const int nk = (p.K + kSmKB - 1) / kSmKB;
+  const int nk = (p.K + kSmKB - 1) / kSmKB, nb = (nk + kBatch - 1) / kBatch;  // K blocks, batches of them
 
   if (warp == 0) {
     // ------------------------------------------------------------ operand loads
     if (lane == 0) {
-      const uint32_t bytes = uint32_t(p.rows + NT) * kSmKB;  // whole boxes, whatever lies outside
+      const uint32_t bytes = uint32_t(p.rows + NT) * kSmKB * kBatch;  // whole boxes, whatever lies outside
       uint32_t it = 0;
       bool ok = true;
       for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-        for (int kb = 0; kb < nk; ++kb, ++it) {
+        for (int b = 0; b < nb; ++b, ++it) {
           const int s = it % kStages;
           if (!mbar_wait(empty_bar(s), ((it / kStages) & 1u) ^ 1u, abort_flag)) {
             ok = false;
             break;
           }
-          const uint32_t sa = base + s * Cfg::kStageBytes;
           mbar_expect_tx(full_bar(s), bytes);
-          tma_load_2d_one(sa, &tmW, full_bar(s), kb * kSmKB, t * p.rows);
-          tma_load_2d_one(sa + kFwRows * kSmKB, &tmT, full_bar(s), kb * kSmKB, 0);
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            // blocks behind the last lie outside the matrix and read as 0; x stays a small multiple of 128
+            const uint32_t sa = base + s * kStageBytes + i * Cfg::kBlockBytes;
+            const int x = min(b * kBatch + i, nk) * kSmKB;
+            tma_load_2d_one(sa, &tmW, full_bar(s), x, t * p.rows);
+            tma_load_2d_one(sa + kFwRows * kSmKB, &tmT, full_bar(s), x, 0);
+          }
         }
       }
     }
@@ -615,17 +624,20 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     uint32_t it = 0;
     bool ok = true;
     for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-      for (int kb = 0; kb < nk; ++kb, ++it) {
+      for (int b = 0; b < nb; ++b, ++it) {
         const int s = it % kStages, buf = it % kBufs;
         ok = warp_wait(full_bar(s), (it / kStages) & 1u, abort_flag) &&
              warp_wait(tempty_bar(buf), ((it / kBufs) & 1u) ^ 1u, abort_flag);
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
-          const uint64_t off = uint32_t(s * (Cfg::kStageBytes >> 4));
 #pragma unroll
-          for (int kk = 0; kk < kSmKB / 32; ++kk)
-            umma_f8_one(tmem_base + buf * NT, da0 + off + 2 * kk, db0 + off + 2 * kk, idesc, kk ? 1u : 0u);
+          for (int i = 0; i < kBatch; ++i) {
+            const uint64_t off = uint32_t((s * kStageBytes + i * Cfg::kBlockBytes) >> 4);
+#pragma unroll
+            for (int kk = 0; kk < kSmKB / 32; ++kk)
+              umma_f8_one(tmem_base + (buf * kBatch + i) * NT, da0 + off + 2 * kk, db0 + off + 2 * kk, idesc, kk ? 1u : 0u);
+          }
           umma_commit_one(tfull_bar(buf));
           umma_commit_one(empty_bar(s));
         }
@@ -649,18 +661,21 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       pw = p.sw + int64_t(p.gw == 1 ? r0 : 0) * p.sw_row;
       pt = p.st + int64_t(p.gt == 1 ? lane : 0) * p.st_row;
     };
-    auto copy = [&](uint32_t n) {
-      const uint32_t dst = dst0 + (n % Cfg::kSlots) * (Cfg::kSlotFloats * 4);
+    auto copy = [&](uint32_t n) {  // of the next batch, number n
+      uint32_t dst = dst0 + (n % Cfg::kSlots) * (Cfg::kSlotFloats * 4);
+#pragma unroll 1
+      for (int k = 0; k < kBatch && pkb < nk; ++k, ++pkb, dst += (kFwRows + NT) * 4) {
 #pragma unroll
-      for (int i = 0; i < kFwRows / 32; ++i)
-        if (i * 32 < left_w)
-          cp_async4(dst + i * 128, p.gw == 1 ? pw + i * dw : pw + int64_t((r0 + i * 32) >> 7) * p.sw_row);
+        for (int i = 0; i < kFwRows / 32; ++i)
+          if (i * 32 < left_w)
+            cp_async4(dst + i * 128, p.gw == 1 ? pw + i * dw : pw + int64_t((r0 + i * 32) >> 7) * p.sw_row);
 #pragma unroll
-      for (int i = 0; i < (NT + 31) / 32; ++i)
-        if (i * 32 < left_t && i * 32 + lane < NT) cp_async4(dst + kFwRows * 4 + i * 128, pt + i * dt);
-      pw += p.sw_col;
-      pt += p.st_col;
-      if (++pkb == nk) {
+        for (int i = 0; i < (NT + 31) / 32; ++i)
+          if (i * 32 < left_t && i * 32 + lane < NT) cp_async4(dst + kFwRows * 4 + i * 128, pt + i * dt);
+        pw += p.sw_col;
+        pt += p.st_col;
+      }
+      if (pkb == nk) {
         pkb = 0;
         pj += gridDim.x;
         seek();
@@ -675,15 +690,13 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     }
     uint32_t it = 0;
     for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
-      for (int kb = 0; kb < nk; ++kb, ++it) {
+      for (int b = 0; b < nb; ++b, ++it) {
         const uint32_t n = it + Cfg::kAhead;
-        if (n % Cfg::kFree == 0) {
-          ok = warp_wait(sempty_bar(n % Cfg::kSlots / Cfg::kFree), ((n / Cfg::kSlots) & 1u) ^ 1u, abort_flag);
-          if (!ok) break;
-        }
+        ok = warp_wait(sempty_bar(n % Cfg::kSlots), ((n / Cfg::kSlots) & 1u) ^ 1u, abort_flag);
+        if (!ok) break;
         copy(n);
         asm volatile("cp.async.commit_group;" ::: "memory");
-        asm volatile("cp.async.wait_group %0;" ::"n"(Cfg::kAhead) : "memory");  // this block's have landed
+        asm volatile("cp.async.wait_group %0;" ::"n"(Cfg::kAhead) : "memory");  // this batch's have landed
         __syncwarp();
         // the barrier's phase of one round before has to be over, or this arrival would count for it
         if (it >= kBufs) {
@@ -696,7 +709,8 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp >= 4) {
     // ------------------------------------------------------------ epilogue
-    constexpr int kPiece = NT < 32 ? NT : 32;  // columns taken from TMEM together
+    constexpr int kCols = kBatch * NT;                // accumulator columns of a batch
+    constexpr int kPiece = kCols < 64 ? kCols : 64;   // columns taken from TMEM together
     const int quad = warp & 3, r = quad * 32 + lane;
     const uint32_t tlane = tmem_base + (uint32_t(quad * 32) << 16);
     uint32_t buf = 0, parity = 0, slot = 0;
@@ -706,44 +720,48 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
 #pragma unroll
       for (int i = 0; i < NT / 2; ++i) acc[i] = make_float2(0.f, 0.f);
 #pragma unroll 1
-      for (int kb = 0; kb < nk; ++kb) {
+      for (int b = 0; b < nb; ++b) {
         ok = warp_wait(tfull_bar(buf), parity, abort_flag);
         if (!ok) break;
         tc_fence_after();
+        const uint32_t ta = tlane + buf * kCols;
         const float* sc = scales + slot * Cfg::kSlotFloats;
-        const float f = sc[r];
-        const float2 f2 = make_float2(f, f);
-        const uint32_t ta = tlane + buf * NT;
 #pragma unroll
-        for (int c = 0; c < NT / kPiece; ++c) {
+        for (int c = 0; c < kCols; c += kPiece) {
           uint32_t v[kPiece];
 #pragma unroll
-          for (int i = 0; i < kPiece; i += 16) tmem_ld16(ta + c * kPiece + i, v, i);
+          for (int i = 0; i < kPiece; i += 16) tmem_ld16(ta + c + i, v, i);
           tmem_ld_wait();
-          if (c == NT / kPiece - 1) {
+          if (c + kPiece == kCols) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(tempty_bar(buf));
           }
 #pragma unroll
-          for (int i = 0; i < kPiece; i += 4) {
-            const float4 g = *reinterpret_cast<const float4*>(sc + kFwRows + c * kPiece + i);
-            const int k = (c * kPiece + i) / 2;
-            acc[k] = __ffma2_rn(make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])),
-                                __fmul2_rn(f2, make_float2(g.x, g.y)), acc[k]);
-            acc[k + 1] = __ffma2_rn(make_float2(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3])),
-                                    __fmul2_rn(f2, make_float2(g.z, g.w)), acc[k + 1]);
+          for (int j = 0; j < kPiece; j += NT < kPiece ? NT : kPiece) {
+            const int block = (c + j) / NT, c0 = (c + j) % NT;  // K block of the batch, first column
+            if (b * kBatch + block >= nk) continue;             // behind the last: its scales were not copied
+            const float* sb = sc + block * (kFwRows + NT);
+            const float f = sb[r];
+            const float2 f2 = make_float2(f, f);
+#pragma unroll
+            for (int i = 0; i < (NT < kPiece ? NT : kPiece); i += 4) {
+              const float4 g = *reinterpret_cast<const float4*>(sb + kFwRows + c0 + i);
+              const int k = (c0 + i) / 2;
+              acc[k] = __ffma2_rn(make_float2(__uint_as_float(v[j + i]), __uint_as_float(v[j + i + 1])),
+                                  __fmul2_rn(f2, make_float2(g.x, g.y)), acc[k]);
+              acc[k + 1] = __ffma2_rn(make_float2(__uint_as_float(v[j + i + 2]), __uint_as_float(v[j + i + 3])),
+                                      __fmul2_rn(f2, make_float2(g.z, g.w)), acc[k + 1]);
+            }
           }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sempty_bar(slot));
         if (++buf == kBufs) {
           buf = 0;
           parity ^= 1u;
         }
-        if ((++slot & (Cfg::kFree - 1)) == 0) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(sempty_bar(slot / Cfg::kFree - 1));
-          slot &= Cfg::kSlots - 1;
-        }
+        if (++slot == Cfg::kSlots) slot = 0;
       }
       if (!ok) break;
       // this thread's row of B is a column of C: a warp stores 32 of them next to one another
