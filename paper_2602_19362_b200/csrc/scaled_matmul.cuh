@@ -7,14 +7,16 @@
 // take it out of TMEM, multiply by the product of the two scales and add in fp32 registers, while the
 // tensor cores fill the other accumulator.
 //
-// CTA pairs (cta_group::2) share a 256 x 256 tile; a K block is 128 bytes, one swizzle row, and takes
-// the tensor cores about 512 cycles per pair.  Two things bound it: the hand-over of the two accumulators
-// (a K block every 670 cycles with an epilogue that does nothing) and the epilogue warps' way through a block,
-// a chain of waits that more warps with fewer columns each shorten; in long calls, the power limit.
+// CTA pairs (cta_group::2) share a 256 x 256 tile; a K block is 128 bytes, one swizzle row, and takes the
+// tensor cores 512 cycles per pair.  What bounds it is the hand-over of the two accumulators that TMEM has room
+// for: an accumulator is away for about 900 cycles between the end of its MMAs and the next ones (commit, the
+// warps' wake-up, TMEM loads, hand-back), so a K block takes 725 cycles, 667 with an epilogue that does nothing.
+// Halves of 128 columns would give four accumulators, but read A twice from shared memory: slower.  Long calls
+// run at the power limit: 4096 x 152064 x 3584 in 2.05 ms, 2.18 PFLOP/s at about 1.4 GHz.
 // Warp 0 issues TMA loads, warp 1 owns TMEM and (in the leader) issues the MMAs, warps 2 and 3 copy the scales
-// of rows and columns to shared memory a few K blocks ahead (cp.async).  They arrive on the accumulator's
-// barrier as the tensor cores do, so the epilogue waits once per block.  Warps 4 to 11 are the epilogue: quadrant warp & 3 of the TMEM
-// lanes, one half of the columns each.
+// of rows and columns to shared memory a few K blocks ahead (cp.async).  They arrive on the accumulator's barrier
+// as the tensor cores do, so the epilogue waits once per block.  Warps 4 to 11 are the epilogue: quadrant warp & 3
+// of the TMEM lanes, one half of the columns each.  The result leaves through TMA stores while the next tile runs.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -467,12 +469,13 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 // swapped: rows of B fill the 128 lanes of the accumulator and the rows of A are its NT = 16, 32 or 64 columns,
 // so a token costs what it needs.  Everything that the warps hand to one another (stages, accumulators, scales)
 // goes in batches of kBatch K blocks, because each hand-over costs its warp some 300 to 500 cycles, more than a
-// block of a small tile takes to load.  (152064 x 3584, one token to 64: 83 to
-// 100 us, 97 to 114 with batches of one, 144 to 129 with the kernel above; 3584 x 3584, one token: 7.8 us, 8.6 with
-// batches of two, 12.0 with one.  128 tokens: 146 against 137, which therefore takes them.)  B's rows are shared out evenly: with
-// S SMs and k = ceil(N / (128 S)) rounds a CTA takes tiles of ceil(N / (k S)) rows, 25 of 3584 and 115 of 152064
-// on 148 SMs, so that a small weight keeps every SM busy and a large one ends everywhere at the same time.
-// No pairs: one CTA per SM, all its shared memory as stages of the weight stream.
+// block of a small tile takes to load.  B's rows are shared out evenly: with S SMs and k = ceil(N / (128 S)) rounds
+// a CTA takes tiles of ceil(N / (k S)) rows, 25 of 3584 and 115 of 152064 on 148 SMs, so that a small weight keeps
+// every SM busy and a large one ends everywhere at the same time.  No pairs: one CTA per SM, all its shared memory
+// as stages of the weight stream.
+// Measured, 152064 x 3584: 82 us with 1 to 16 rows of A, the copy rate, 88 with 32 and 96 to 100 with 64 (144 to
+// 129 us with the kernel above, which is faster from 128 rows on: 137 against 146); 3584 x 3584, one row: 7.5 us,
+// 12 with batches of one.
 constexpr int kFwRows = 128;
 constexpr int kFwEpiWarps = 4;
 constexpr int kFwThreads = 32 * (4 + kFwEpiWarps);
