@@ -429,6 +429,25 @@ def test_captured_and_replayed():
     assert all(torch.equal(x, y) for x, y in zip(got, o + [d]))
 
 
+def test_single_outputs():
+    z, targets, _ = make(9, 3001, "bf16", 5)
+    lp, ent, lse, top, ids = check_fwd(z, targets, None, 6)
+    L, new = B.make_logits(z, targets), lambda x: torch.full_like(x, 3)
+    for k, want in enumerate((lp, ent, lse, top, ids)):
+        args = [None] * 5
+        args[k] = new(want)
+        B.oapl_logits_logprobs(L, *args)
+        assert torch.equal(args[k], want)
+    one = new(ent)
+    B.oapl_logits_logprobs(B.make_logits(z), None, one)         # no targets needed for the entropy
+    assert torch.equal(one, ent)
+
+
+def test_binding_refuses_tensors_of_another_device():
+    with pytest.raises(ValueError):
+        B._stream_of(torch.cuda.current_device() + 1)
+
+
 def test_binding_refusals():
     z, targets, mask = make(4, 64, "bf16", 0)
     f = torch.empty(4, device="cuda")
