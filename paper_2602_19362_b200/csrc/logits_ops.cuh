@@ -550,21 +550,13 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
   const bool bad_target = target < 0 || target >= V;
   float z_target = 0.f;
   if (rank == 0 && tid == 0 && p.token_logp && !bad_target) z_target = E::one(zrow, target);  // behind the first loads
-  for (int b = 0; b < nb; ++b) {
-    // Without alternatives five CTAs per SM hide each other's loads; with them, registers allow four, which
-    // load a batch ahead (4096 x 152064 bf16: 190 and 213 us; the other way round 206 and 232).
-    if (TOP) {
-      if (b + 1 < nb) load(b + 1, nxt);
-    } else if (b) {
-      load(b, cur);
-    }
+  auto take = [&](uint4* v) {
     uint32_t pm = 0;
 #pragma unroll
     for (int u = 0; u < kLgUnroll; ++u) {
-      uint4& v = cur[u];
-      v = make_uint4(E::pclamp(v.x, p.clamp_pk), E::pclamp(v.y, p.clamp_pk), E::pclamp(v.z, p.clamp_pk),
-                     E::pclamp(v.w, p.clamp_pk));
-      const uint32_t a = E::pmax(E::pmax(v.x, v.y), E::pmax(v.z, v.w));
+      v[u] = make_uint4(E::pclamp(v[u].x, p.clamp_pk), E::pclamp(v[u].y, p.clamp_pk), E::pclamp(v[u].z, p.clamp_pk),
+                        E::pclamp(v[u].w, p.clamp_pk));
+      const uint32_t a = E::pmax(E::pmax(v[u].x, v[u].y), E::pmax(v[u].z, v[u].w));
       pm = u ? E::pmax(pm, a) : a;
     }
     const float bm = E::pmax_final(pm);
@@ -582,12 +574,25 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
 #pragma unroll
     for (int u = 0; u < kLgUnroll; ++u) {
       float f[kN];
-      E::widen(cur[u], f);
+      E::widen(v[u], f);
       row_add<kN>(r, f, c);
     }
-    if (TOP) {
-#pragma unroll
-      for (int u = 0; u < kLgUnroll; ++u) cur[u] = nxt[u];
+  };
+  // Without alternatives five CTAs per SM hide each other's loads; with them, registers allow four, which load a
+  // batch ahead (4096 x 152064 bf16: 190 and 213 us; the other way round 206 and 232).
+  if (TOP) {
+#pragma unroll 1
+    for (int b = 0; b < nb; b += 2) {
+      if (b + 1 < nb) load(b + 1, nxt);
+      take(cur);
+      if (b + 1 == nb) break;
+      if (b + 2 < nb) load(b + 2, cur);
+      take(nxt);
+    }
+  } else {
+    for (int b = 0; b < nb; ++b) {
+      if (b) load(b, cur);
+      take(cur);
     }
   }
   if (TOP && in_group) {
