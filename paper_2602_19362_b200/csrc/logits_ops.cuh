@@ -538,12 +538,25 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
   float tmax = p.clamp, gm = p.clamp;
   int g = 0, in_group = 0;
   uint4 cur[kLgUnroll], nxt[TOP ? kLgUnroll : 1];
+  // Whole batches of all threads need neither bounds nor a filling (4096 x 152064 bf16 in repeated calls, with and
+  // without alternatives: 228 and 211 us, 235 and 217 with one form for all); the variant for few rows has one
+  // form, since the first pass through the code is its time (64 rows of 152064: 11.3 us, 11.8 with two).
+  constexpr bool kWhole = !TOP || NT < kLgThreads;
+  const int whole = kWhole ? (q.v1 - q.v0) / (NT * kLgUnroll) : 0;
+  const uint4* mine = q.zv + q.v0 + tid;
   auto load = [&](int b, uint4* v) {
+    const uint4* at = mine + b * (NT * kLgUnroll);
+    if (kWhole && b < whole) {
 #pragma unroll
-    for (int u = 0; u < kLgUnroll; ++u) {
-      const int i = q.v0 + (b * kLgUnroll + u) * NT + tid;
-      v[u] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
-      if (i < q.v1) v[u] = ldg_stream(q.zv + i);
+      for (int u = 0; u < kLgUnroll; ++u) v[u] = ldg_stream(at + u * NT);
+    } else {
+      const int i0 = q.v0 + b * (NT * kLgUnroll) + tid;
+#pragma unroll
+      for (int u = 0; u < kLgUnroll; ++u) {
+        const int i = i0 + u * NT;
+        v[u] = make_uint4(E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf);
+        if (i < q.v1) v[u] = ldg_stream(kWhole ? at + u * NT : q.zv + i);
+      }
     }
   };
   if (nb > 0) load(0, cur);
@@ -742,11 +755,12 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
 // ------------------------------------------------------------------------------------ backward
 // dz_v = a ( -p_v (G + g_H (ln p_v + H)) + g_lp [v = t] + sum_k g_k [v = id_k] ),  G = g_lp + sum_k g_k,
 // p_v = e^(a z_v - lse).  One read and one write per logit, HBM-bound; dz may be the logits themselves.
-// A CTA takes kLgSpanVecs 16-byte vectors of a row, six CTAs per SM (4096 x 152064 bf16: 387 us, 98 % of the copy
-// rate; four CTAs 433 us); the few entries with a point term are written again after the
-// CTA's stores, from logits read before them.
-constexpr int kLgSpanVecs = kLgThreads * kLgUnroll;
-
+// Six CTAs per SM (four: 12 % slower).  A CTA takes a span of a row, one batch of loads or, where there are rows
+// enough (kMany), four, which share the row's factors and the scan of its entries: these are half of the
+// instructions otherwise, and under the power limit fewer instructions are a higher clock.  4096 x 152064 bf16 in
+// repeated calls: 382 us with four batches, the copy rate; 403 us with one.  257 x 32003 fp32 with 8 entries a row:
+// 12.8 us with one.  The few entries with a point term are written again after the CTA's stores, from logits read
+// before them.
 struct RowGrad {
   float a, nlse;  // ln p = a z + nlse
   float A, B;     // dz = p (A ln p + B)
@@ -760,7 +774,7 @@ __device__ __forceinline__ float2 grad_smooth(float2 z, const RowGrad& r) {
   return __fmul2_rn(make_float2(ex2_approx(x.x), ex2_approx(x.y)), w);
 }
 
-template <typename T>
+template <typename T, bool kMany>
 __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsParams p, int spans) {
   using E = Elem<T>;
   constexpr int kN = E::kN;
@@ -779,8 +793,11 @@ __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsP
   const int nsingle = V - nv * kN;
   const bool together = az == ad;  // loads and stores share the vector boundaries
   const bool live = !p.mask || p.mask[row] != 0;
-  const int w0 = span * kLgSpanVecs;
-  const int w1 = min(nv, w0 + kLgSpanVecs);
+  // a batch, or equal spans of whole rounds of the CTA
+  const int per_span =
+      kMany ? (nv + spans * kLgThreads - 1) / (spans * kLgThreads) * kLgThreads : kLgThreads * kLgUnroll;
+  const int w0 = min(nv, span * per_span);
+  const int w1 = min(nv, w0 + per_span);
 
   if (!live) {
     for (int i = w0 + tid; i < w1; i += kLgThreads)
@@ -790,12 +807,14 @@ __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsP
   }
 
   uint4 v[kLgUnroll];
+  auto load = [&](int at) {
 #pragma unroll
-  for (int u = 0; u < kLgUnroll; ++u) {
-    const int i = w0 + u * kLgThreads + tid;
-    v[u] = make_uint4(0, 0, 0, 0);
-    if (together && i < w1) v[u] = *(reinterpret_cast<const uint4*>(zrow + nh) + i);
-  }
+    for (int u = 0; u < kLgUnroll; ++u) {
+      const int i = at + u * kLgThreads + tid;
+      if (together && i < w1) v[u] = *(reinterpret_cast<const uint4*>(zrow + nh) + i);
+    }
+  };
+  load(w0);
   float zs = 0.f;
   const int single = tid < nh ? tid : nv * kN + tid;
   if (span == 0 && tid < nsingle) zs = E::one(zrow, single);
@@ -852,25 +871,29 @@ __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsP
   const float z_at = at >= 0 ? E::one(zrow, at) : 0.f;
   const bool any_point = __syncthreads_or(at >= 0);  // the logits at these entries have been read
 
+  for (int at = w0; at < w1; at += kLgThreads * kLgUnroll) {
+    if (kMany && at != w0) load(at);
 #pragma unroll
-  for (int u = 0; u < kLgUnroll; ++u) {
-    const int i = w0 + u * kLgThreads + tid;
-    if (i < w1) {
-      float f[kN];
-      if (together) {
-        E::widen(v[u], f);
-      } else {
+    for (int u = 0; u < kLgUnroll; ++u) {
+      const int i = at + u * kLgThreads + tid;
+      if (i < w1) {
+        float f[kN];
+        if (together) {
+          E::widen(v[u], f);
+        } else {
 #pragma unroll
-        for (int e = 0; e < kN; ++e) f[e] = E::one(zrow, nh + int64_t(i) * kN + e);
+          for (int e = 0; e < kN; ++e) f[e] = E::one(zrow, nh + int64_t(i) * kN + e);
+        }
+#pragma unroll
+        for (int e = 0; e < kN; e += 2) {
+          const float2 d = grad_smooth(make_float2(f[e], f[e + 1]), r);
+          f[e] = d.x;
+          f[e + 1] = d.y;
+        }
+        *reinterpret_cast<uint4*>(drow + nh + int64_t(i) * kN) = E::narrow(f);
       }
-#pragma unroll
-      for (int e = 0; e < kN; e += 2) {
-        const float2 d = grad_smooth(make_float2(f[e], f[e + 1]), r);
-        f[e] = d.x;
-        f[e + 1] = d.y;
-      }
-      *reinterpret_cast<uint4*>(drow + nh + int64_t(i) * kN) = E::narrow(f);
     }
+    if (!kMany) break;
   }
   if (span == 0 && tid < nsingle) E::put(drow, single, grad_smooth(make_float2(zs, 0.f), r).x);
   if (any_point) {
