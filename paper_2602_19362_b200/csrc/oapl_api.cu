@@ -221,11 +221,11 @@ static bool make_map_out(CUtensorMap* m, void* base, int32_t type, uint64_t rows
   const bool f32 = type == OAPL_TYPE_F32;
   const cuuint64_t dims[2] = {cols, rows};
   const cuuint64_t strides[1] = {ld * (f32 ? 4 : 2)};
-  const cuuint32_t box[2] = {f32 ? 16u : 32u, 32};
+  const cuuint32_t box[2] = {f32 ? 32u : 64u, 32};
   const cuuint32_t estr[2] = {1, 1};
   const CUtensorMapDataType t = f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                     : (type == OAPL_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
-  return fn(m, t, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+  return fn(m, t, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

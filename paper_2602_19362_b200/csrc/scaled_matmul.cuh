@@ -30,7 +30,7 @@ namespace oapl {
 constexpr int kSmTile = 256;       // rows and columns of a pair's tile
 constexpr int kSmHalf = 128;       // rows of A, and of B, that a CTA loads
 constexpr int kSmKB = 128;         // K values (bytes) of a block
-constexpr int kSmStages = 5;
+constexpr int kSmStages = 4;
 constexpr int kSmStageBytes = 2 * kSmHalf * kSmKB;
 constexpr int kSmSlots = 16;       // K blocks whose scales have room in shared memory
 constexpr int kSmAhead = 6;        // K blocks that their copies run ahead
@@ -40,7 +40,9 @@ constexpr int kSmEpiWarps = 8;
 constexpr int kSmThreads = 32 * (4 + kSmEpiWarps);
 constexpr int kSmOutCols = 32;     // columns of a warp's output piece
 constexpr int kSmOutPitch = kSmOutCols + 1;
-constexpr int kSmOutBytes = kSmEpiWarps * 32 * kSmOutPitch * 4;
+constexpr int kSmOutWarp = 8192;   // of an epilogue warp: two pieces of 32 rows x 128 bytes, or one of 32 x 33 floats
+constexpr int kSmOutBytes = kSmEpiWarps * kSmOutWarp;
+static_assert(32 * kSmOutPitch * 4 <= kSmOutWarp, "a padded piece fits");
 constexpr size_t kSmSmemBytes = size_t(kSmStages) * kSmStageBytes + kSmSlots * kSmSlotFloats * 4 +
                                 kSmOutBytes + 1024 /*align*/ + 512 /*barriers*/;
 static_assert(kSmSmemBytes <= 227 * 1024, "shared memory of a CTA");
@@ -310,7 +312,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
     const int quad = warp & 3;
     const int half = (warp - 4) >> 2;  // columns [128 half, 128 half + 128)
     const uint32_t tlane = tmem_base + (uint32_t(quad * 32) << 16) + half * 128;
-    float* piece = reinterpret_cast<float*>(smem + kOutOff) + (warp - 4) * 32 * kSmOutPitch;
+    float* piece = reinterpret_cast<float*>(smem + kOutOff + (warp - 4) * kSmOutWarp);
     const uint32_t back0 = mapa_shared(tempty_bar(0), 0);
     const float* sc_row = scales + quad * 32 + lane;
     const float* sc_col = scales + kSmHalf + (PERCOL ? half * 128 : half);
@@ -374,26 +376,26 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       if (row0 >= p.M || col0 >= p.N) continue;
       OT* C = reinterpret_cast<OT*>(p.C);
       if (p.bulk) {
-        // 64 bytes of every row at a time through one of two swizzled 2 KB pieces; the stores run on under the
+        // 128 bytes of every row at a time through one of two swizzled 4 KB pieces; the stores run on under the
         // next tile
-        constexpr int kCols = 64 / sizeof(OT);
-        uint8_t* two = smem + kOutOff + (warp - 4) * 4096;
+        constexpr int kCols = 128 / sizeof(OT);
+        uint8_t* two = smem + kOutOff + (warp - 4) * kSmOutWarp;
 #pragma unroll
         for (int q = 0; q < 128 / kCols; ++q) {
-          uint8_t* out = two + (q & 1) * 2048;
+          uint8_t* out = two + (q & 1) * 4096;
           if (lane == 0) tma_store_wait_read<1>();
           __syncwarp();
-          uint4* line = reinterpret_cast<uint4*>(out + lane * 64);
+          uint4* line = reinterpret_cast<uint4*>(out + lane * 128);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 8; ++c) {
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               if (OUT == OUT_F32) {
-                const float2 x = acc[q * 8 + c * 2 + i / 2];
+                const float2 x = acc[q * 16 + c * 2 + i / 2];
                 w[i] = __float_as_uint(i & 1 ? x.y : x.x);
               } else {
-                const float2 x = acc[q * 16 + c * 4 + i];
+                const float2 x = acc[q * 32 + c * 4 + i];
                 if (OUT == OUT_BF16) {
                   w[i] = pack_bf16x2(x.x, x.y);
                 } else {
@@ -402,7 +404,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
                 }
               }
             }
-            line[c ^ ((lane >> 1) & 3)] = make_uint4(w[0], w[1], w[2], w[3]);
+            line[c ^ (lane & 7)] = make_uint4(w[0], w[1], w[2], w[3]);
           }
           fence_proxy_async_smem();
           __syncwarp();
