@@ -69,6 +69,26 @@ struct ScaledParams {
   int32_t* err;
 };
 
+// Waits for the warp's loads from TMEM; naming the registers keeps their uses behind it.
+__device__ __forceinline__ void tmem_ld_wait_on(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
+                 "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
+                 "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]),
+                 "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]),
+                 "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait_on(uint32_t (&a)[32], uint32_t (&b)[32]) {
+  tmem_ld_wait_on(a);
+  asm volatile("" : "+r"(b[0]), "+r"(b[1]), "+r"(b[2]), "+r"(b[3]), "+r"(b[4]), "+r"(b[5]), "+r"(b[6]), "+r"(b[7]),
+               "+r"(b[8]), "+r"(b[9]), "+r"(b[10]), "+r"(b[11]), "+r"(b[12]), "+r"(b[13]), "+r"(b[14]),
+               "+r"(b[15]), "+r"(b[16]), "+r"(b[17]), "+r"(b[18]), "+r"(b[19]), "+r"(b[20]), "+r"(b[21]),
+               "+r"(b[22]), "+r"(b[23]), "+r"(b[24]), "+r"(b[25]), "+r"(b[26]), "+r"(b[27]), "+r"(b[28]),
+               "+r"(b[29]), "+r"(b[30]), "+r"(b[31]) : : "memory");
+}
+
 // D[tmem] (+)= A B^T, 8-bit floating point operands, K = 32 per instruction, for both CTAs of the pair
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                         uint32_t accumulate) {
@@ -333,27 +353,44 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         tmem_ld32(ta + 32, rb);
         const float* sc = sc_col + slot * kSmSlotFloats;
         const float fa = sc_row[slot * kSmSlotFloats], f = PERCOL ? fa : fa * sc[0];
-        auto add = [&](const uint32_t (&r)[32], int c) {
+        float4 g[4];  // scales of the next 16 columns
+        auto scales_of = [&](int c) {
+          if (PERCOL) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const float2 v0 = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
-            const float2 v1 = make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-            float2 g0 = make_float2(f, f), g1 = g0;
-            if (PERCOL) {
-              const float4 g = *reinterpret_cast<const float4*>(sc + c * 32 + i);
-              g0 = __fmul2_rn(g0, make_float2(g.x, g.y));
-              g1 = __fmul2_rn(g1, make_float2(g.z, g.w));
-            }
-            acc[c * 16 + i / 2] = __ffma2_rn(v0, g0, acc[c * 16 + i / 2]);
-            acc[c * 16 + i / 2 + 1] = __ffma2_rn(v1, g1, acc[c * 16 + i / 2 + 1]);
+            for (int i = 0; i < 4; ++i) g[i] = *reinterpret_cast<const float4*>(sc + c + 4 * i);
           }
         };
-        tmem_ld_wait();
+        auto add = [&](const uint32_t (&r)[32], int c) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float4 now[4];
+            if (PERCOL) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) now[i] = g[i];
+              if (c + h < 4) scales_of(c * 32 + h * 16 + 16);
+            }
+#pragma unroll
+            for (int i = h * 16; i < h * 16 + 16; i += 4) {
+              const float2 v0 = make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1]));
+              const float2 v1 = make_float2(__uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+              float2 g0 = make_float2(f, f), g1 = g0;
+              if (PERCOL) {
+                const float4 s4 = now[(i & 15) / 4];
+                g0 = __fmul2_rn(g0, make_float2(s4.x, s4.y));
+                g1 = __fmul2_rn(g1, make_float2(s4.z, s4.w));
+              }
+              acc[c * 16 + i / 2] = __ffma2_rn(v0, g0, acc[c * 16 + i / 2]);
+              acc[c * 16 + i / 2 + 1] = __ffma2_rn(v1, g1, acc[c * 16 + i / 2 + 1]);
+            }
+          }
+        };
+        scales_of(0);
+        tmem_ld_wait_on(ra, rb);
         add(ra, 0);
         tmem_ld32(ta + 64, ra);
         add(rb, 1);
         tmem_ld32(ta + 96, rb);
-        tmem_ld_wait();
+        tmem_ld_wait_on(ra, rb);
         // the accumulator is in registers: hand it back
         tc_fence_before();
         __syncwarp();
