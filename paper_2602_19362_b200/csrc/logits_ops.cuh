@@ -13,7 +13,7 @@
 // at a time, and sums and products are two wide.  The top alternatives cost the pass nothing but the group
 // maxima that it needs anyway: see top-K below.
 // Measured, 4096 rows of 152064 bf16 logits (1.25 GB): 190 us without alternatives, the copy rate; 212 us with
-// eight, where every row ends in a chain of short waits; one row with twenty 9.6 us.
+// eight, where every row ends in a chain of short waits; one row with twenty 8.2 us.
 //
 // A row goes to a cluster of 1, 2, 4 or 8 CTAs (few rows: the row is split and joined through
 // distributed shared memory, so a call is always a single launch without a workspace).
@@ -274,27 +274,32 @@ __device__ __forceinline__ void top_insert(uint64_t& mine, uint64_t key, int lan
   if (lane > pos) mine = up;
 }
 
-// out[rank] = the K best of entries[0..M), whose keys are distinct; the rest of out is 0.  Four threads count
-// for an entry while there are enough.  All threads; two barriers, the first before anything is read.
+// out[rank] = the K best of entries[0..M), whose keys are distinct; the rest of out is 0.  Up to eight threads
+// count for an entry, four keys at a time.  All threads; two barriers, the first before anything is read.
 template <int NT>
 __device__ __forceinline__ void top_rank(const uint64_t* entries, int M, int K, uint64_t* out) {
   const int tid = threadIdx.x;
   if (tid < kLgMaxTop) out[tid] = 0;
   __syncthreads();
-  const int ways = M <= NT / 4 ? 4 : 1;
-  const int part = tid % ways;
+  const int log = M <= NT / 8 ? 3 : (M <= NT / 4 ? 2 : (M <= NT / 2 ? 1 : 0));
+  const int ways = 1 << log, part = tid & (ways - 1);
 #pragma unroll 1
-  for (int i0 = 0; i0 < M; i0 += NT / ways) {
-    const int i = i0 + tid / ways;
-    const uint64_t k = i < M ? entries[i] : 0;
+  for (int i0 = 0; i0 < M; i0 += NT >> log) {
+    const int i = i0 + (tid >> log);
+    const uint64_t k = i < M ? entries[i] : ~0ull;
     int r = 0;
-    if (i < M) {
-#pragma unroll 2
-      for (int j = part; j < M; j += ways) r += entries[j] > k;
+#pragma unroll 1
+    for (int j = part; j < M; j += 4 * ways) {
+      uint64_t o[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[u] = j + u * ways < M ? entries[j + u * ways] : 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) r += o[u] > k;
     }
-    if (ways == 4) {
-      r += __shfl_xor_sync(0xffffffffu, r, 1);
-      r += __shfl_xor_sync(0xffffffffu, r, 2);
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      const int other = __shfl_xor_sync(0xffffffffu, r, 1 << u);
+      if (u < log) r += other;
     }
     if (i < M && part == 0 && r < K) out[r] = k;
   }
@@ -636,7 +641,7 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
   if (TOP) {
     const uint32_t none = uint32_t(top_key(-INFINITY, 0) >> 32);  // -inf is no alternative
     const int with = min((q.v1 - q.v0 + 31) / 32, (NT / 32));      // warps with data
-    uint32_t left = ordered(tmax + 0.f), jth = 0;
+    uint32_t left = ordered(tmax + 0.f), jth = 0xFFFFFFFFu;
     if (warp < with) {
       for (int n = (K + with - 1) / with; n > 0; --n) {
         jth = __reduce_max_sync(0xffffffffu, left);
@@ -646,41 +651,64 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
     if (lane == 0) sh_thr[warp] = jth;
     if (tid == 0) sh_count = sh_items = 0;
     __syncthreads();
-    uint32_t thr = with ? 0xFFFFFFFFu : 0u;
-    for (int w = 0; w < with; ++w) thr = min(thr, sh_thr[w]);
+    uint32_t thr = with ? __reduce_min_sync(0xffffffffu, sh_thr[lane % (NT / 32)]) : 0u;
     // at the clamp the maxima say nothing: everything above -inf is to be looked at
     if (thr <= uint32_t(top_key(p.clamp, 0) >> 32)) thr = none + 1;
     const uint32_t thr16 = thr > none + 1 ? thr >> 16 : 0;
+    const float thr_f = from_ordered(thr);  // NaN is no alternative
 
     // groups to read again
     uint32_t hot = 0;
 #pragma unroll 8
     for (int k = 0; k < g; ++k) hot |= uint32_t(gmax[k * NT + tid] >= thr16) << k;
-    while (hot) {
-      const int k = __ffs(hot) - 1, at = atomicAdd(&sh_items, 1);
-      hot &= hot - 1;
-      if (at < kLgItems) items[at] = uint16_t(k * NT + tid);
+    if (hot) {
+      int at = atomicAdd(&sh_items, __popc(hot));
+      do {
+        if (at < kLgItems) items[at] = uint16_t((__ffs(hot) - 1) * NT + tid);
+        ++at;
+        hot &= hot - 1;
+      } while (hot);
     }
-    auto offer = [&](float v, uint32_t idx) {
-      const uint64_t key = top_key(v, idx);
-      if (uint32_t(key >> 32) >= thr && v > -INFINITY) {
+    if (rank == nc - 1 && tid < nsingle) {
+      if (zs >= thr_f) {
         const int at = atomicAdd(&sh_count, 1);
-        if (at < kLgCands) sh_list[at] = key;
+        if (at < kLgCands) sh_list[at] = top_key(zs, uint32_t(tid < q.nh ? tid : q.nv * kN + tid));
       }
-    };
-    if (rank == nc - 1 && tid < nsingle) offer(zs, uint32_t(tid < q.nh ? tid : q.nv * kN + tid));
+    }
     __syncthreads();
     const int n_items = sh_items;
     if (n_items <= kLgItems) {
       const int vecs = per * kLgUnroll;  // of a group
-      for (int i = tid; i < n_items * vecs; i += NT) {
-        const int it = items[i / vecs], n = (it / NT) * vecs + i % vecs;
-        const int at = q.v0 + n * NT + it % NT;
-        if (at < q.v1) {
-          float f[kN];
-          E::widen(ldg_stream(q.zv + at), f);
+      const int n_vecs = n_items * vecs;
+#pragma unroll 1
+      for (int i0 = tid; i0 < n_vecs; i0 += 2 * NT) {
+        uint4 v[2];  // two under way
+        int at[2];
 #pragma unroll
-          for (int e = 0; e < kN; ++e) offer(f[e], uint32_t(q.nh + at * kN + e));
+        for (int u = 0; u < 2; ++u) {
+          const int i = i0 + u * NT, it = i < n_vecs ? items[i / vecs] : 0;
+          at[u] = i < n_vecs ? q.v0 + ((it / NT) * vecs + i % vecs) * NT + it % NT : q.v1;
+          if (at[u] < q.v1) v[u] = ldg_stream(q.zv + at[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          if (at[u] < q.v1) {
+            float f[kN];
+            E::widen(v[u], f);
+            uint32_t in = 0;
+#pragma unroll
+            for (int e = 0; e < kN; ++e) in |= uint32_t(f[e] >= thr_f) << e;
+            if (in) {
+              int to = atomicAdd(&sh_count, __popc(in));
+#pragma unroll
+              for (int e = 0; e < kN; ++e) {
+                if (in >> e & 1) {
+                  if (to < kLgCands) sh_list[to] = top_key(f[e], uint32_t(q.nh + at[u] * kN + e));
+                  ++to;
+                }
+              }
+            }
+          }
         }
       }
     }
@@ -712,7 +740,9 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
       // as with the warps: at least K entries reach the smallest of the CTAs' j-th bests, j = ceil(K / nc)
       uint64_t bound = ~0ull;
       const int j = (K + int(nc) - 1) >> (31 - __clz(nc));
-      for (uint32_t w = 0; w < nc; ++w) bound = min(bound, sh_cl_list[w * K + j - 1]);
+#pragma unroll
+      for (uint32_t w = 0; w < kLgMaxCluster; ++w)
+        if (w < nc) bound = min(bound, sh_cl_list[w * K + j - 1]);
       const uint64_t key = tid < int(nc) * K ? sh_cl_list[tid] : 0;
       if (tid == 0) sh_count = 0;
       __syncthreads();
