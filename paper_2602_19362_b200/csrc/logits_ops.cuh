@@ -12,8 +12,9 @@
 // when a batch's maximum exceeds it by 2^8 (no rescaling in the steady state), masked logits are dealt with two
 // at a time, and sums and products are two wide.  The top alternatives cost the pass nothing but the group
 // maxima that it needs anyway: see top-K below.
-// Measured, 4096 rows of 152064 bf16 logits (1.25 GB): 190 us without alternatives, the copy rate; 212 us with
-// eight, where every row ends in a chain of short waits; one row with twenty 8.2 us.
+// Measured, 4096 rows of 152064 bf16 logits (1.25 GB), a single call: 189 us without alternatives, the copy rate;
+// 207 us with eight, where every row ends in a chain of short waits.  In repeated calls, at the power limit, 211
+// and 228.  One row with twenty: 8.2 us.
 //
 // A row goes to a cluster of 1, 2, 4 or 8 CTAs (few rows: the row is split and joined through
 // distributed shared memory, so a call is always a single launch without a workspace).

@@ -728,8 +728,9 @@ static int launch_logits_fwd(LogitsParams lp, int nc, cudaStream_t st) {
 // CTAs of a row: it is split while the parts are no more than three per SM and every thread keeps a vector
 // (100 rows of 152064 bf16: 9.6 us, 12.2 with two per SM; 64 rows 7.2 us, 8.0 with four).
 // Many rows with alternatives go to CTAs of 128 threads, eight per SM: a row's end is a chain of short waits
-// (about 14,000 cycles on a busy SM), which weighs half as much behind a pass that takes twice as long.
-// 4096 rows of 152064: 214 us against 226; 256 rows, which leave SMs half empty: 38 us against 27.
+// (about 10,000 cycles on a busy SM), which weighs half as much behind a pass that takes twice as long.
+// 4096 rows of 152064: 214 us against 226; 1531 rows of 50021: 28 against 31; 256 rows, which leave SMs half
+// empty: 38 us against 27.
 template <typename T>
 static int route_logits_fwd(const LogitsParams& lp, cudaStream_t st) {
   const int n_sm = sm_count();
