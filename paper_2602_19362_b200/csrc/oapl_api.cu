@@ -746,13 +746,13 @@ template <typename T>
 static int launch_logits_bwd(const LogitsParams& lp, cudaStream_t st) {
   // A CTA's span of a row: four batches of loads, so that the row's factors and the scan of its entries are
   // shared, where that still leaves four waves of CTAs; one batch otherwise.
-  const int n_sm = sm_count();
-  if (n_sm <= 0) return OAPL_ERR_CUDA;
   const int64_t nv = (int64_t)lp.V / Elem<T>::kN, batch = kLgThreads * kLgUnroll;
   int64_t spans = (nv + 4 * batch) / (4 * batch);
+  if (spans * lp.N > (int64_t)2147483647) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  const int n_sm = sm_count();
+  if (n_sm <= 0) return OAPL_ERR_CUDA;
   const bool many = spans * lp.N >= 4 * 6 * (int64_t)n_sm;
   if (!many) spans = (nv + batch) / batch;
-  if (spans * lp.N > (int64_t)2147483647) return OAPL_ERR_UNSUPPORTED_SHAPE;
   auto kern = many ? logits_bwd_kernel<T, true> : logits_bwd_kernel<T, false>;
   kern<<<(unsigned)(spans * lp.N), kLgThreads, 0, st>>>(lp, (int)spans);
   CKL();
