@@ -110,6 +110,15 @@ def test_forward_rows_split_over_ctas(t, N):
     check_fwd(z, targets, None, 5, scale=1 / 0.7)
 
 
+@pytest.mark.parametrize("t,V,offset,pad", [("bf16", 9, 1, 2), ("f16", 1024, 0, 0), ("bf16", 4096, 0, 8), ("f16", 12295, 3, 4),
+                                            ("f32", 8209, 1, 0), ("bf16", 50021, 0, 2)])
+def test_forward_more_rows_than_sms_hold(t, V, offset, pad):
+    # narrow CTAs with alternatives, whole batches and a last one, rows on and off 16-byte boundaries
+    z, targets, mask = make(1201, V, t, V, offset, pad)
+    check_fwd(z, targets, mask, 7)
+    check_fwd(z, targets, None, 0)
+
+
 def test_forward_vocabulary_larger_than_the_kept_group_maxima():
     # more than 32 batches of a thread: a group holds several
     z, targets, _ = make(200, 600011, "bf16", 3)
@@ -316,6 +325,21 @@ def test_gradient_sizes(t, V, offset, pad, doff, dpad):
         check_bwd(z, targets, None, None, ge, None, None, 0.5, dpad, doff)
         if K:
             check_bwd(z, None if K == 5 else targets, None, None, None, gt, ids, 1.0, dpad, doff)
+
+
+@pytest.mark.parametrize("t,N,V,pad,dpad", [("bf16", 3700, 5, 0, 3), ("f16", 3700, 2056, 0, 0), ("bf16", 3700, 8200, 3, 3),
+                                            ("f32", 1900, 20003, 1, 5), ("bf16", 1800, 40009, 7, 7), ("f16", 901, 131100, 4, 4)])
+def test_gradient_many_rows(t, N, V, pad, dpad):
+    # a CTA takes several batches of a row; entries with a point term in any of them
+    z, targets, mask = make(N, V, t, V, 0, pad)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    gl, ge = (torch.randn(N, device="cuda", generator=g) for _ in range(2))
+    gt = torch.rand(N, 9, device="cuda", generator=g)
+    ids = torch.randint(-1, V, (N, 9), device="cuda", generator=g).to(torch.int32)
+    L, lse, ent, d = check_bwd(z, targets, mask, gl, ge, gt, ids, 1.0, dpad)
+    d = d.clone()
+    B.oapl_logits_logprobs_bwd(L, lse, ent, gl, ge, gt, ids, z)        # over the logits
+    assert torch.equal(d, z)
 
 
 def test_gradient_target_among_the_alternatives_and_ids_outside():
