@@ -875,8 +875,9 @@ __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsP
   if (lse < -1e30f) lse = 1e30f;
   const RowGrad r = {p.scale, -lse, -p.scale * ge, -p.scale * fmaf(ge, H, G)};
 
-  // the entries with a point term: warp 0 the alternatives, warp 1 the target; each with all terms at its
-  // entry, so that equal indexes write the same value
+  // the entries with a point term, each with all terms at its entry and written by one warp: warp 0 the
+  // alternatives, whose lanes of equal index add the same terms in the same order (the target's first, then by k);
+  // warp 1 the target where it is none of them
   int at = -1;
   float point = 0.f;
   if (warp == 0 && K) {
@@ -887,11 +888,8 @@ __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsP
       const float g = __shfl_sync(0xffffffffu, g_id, k);
       if (other == id) point += g;
     }
-  } else if (warp == 1 && target_in) {
-    point = id == target ? g_id : 0.f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) point += __shfl_xor_sync(0xffffffffu, point, o);
-    point += g_target;
+  } else if (warp == 1 && target_in && !__any_sync(0xffffffffu, id == target)) {
+    point = g_target;
     at = lane == 0 ? target : -1;
   }
   if (at >= 0) {  // owned by the CTA that stores it

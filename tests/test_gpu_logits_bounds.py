@@ -1,0 +1,49 @@
+"""oapl_logits_logprobs and its gradient where order, magnitude or cancellation decide: ids that repeat the
+target."""
+import math
+
+import pytest
+import torch
+
+from paper_2602_19362_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+def forward(z, targets, mask=None, scale=1.0):
+    """lse and entropy as the forward leaves them."""
+    N = z.shape[0]
+    L = B.make_logits(z, targets, mask, scale)
+    lp, ent, lse = (torch.empty(N, device="cuda") for _ in range(3))
+    B.oapl_logits_logprobs(L, lp, ent, lse)
+    return L, lp, ent, lse
+
+
+@pytest.mark.parametrize("K", [2, 3, 32])
+@pytest.mark.parametrize("N", [3, 900])
+def test_gradient_of_a_target_repeated_among_the_ids_has_one_order(N, K):
+    V = 1000
+    g = torch.Generator(device="cuda").manual_seed(K)
+    z = torch.randn(N, V, device="cuda", generator=g)
+    targets = torch.randint(0, V, (N,), device="cuda", generator=g).to(torch.int32)
+    # p of the target is 0, so the entry is the sum of its point terms, bit for bit
+    z.scatter_(1, targets.long()[:, None], -math.inf)
+    ids = targets[:, None].repeat(1, K).contiguous()
+    gl, gt = torch.randn(N, device="cuda", generator=g), torch.randn(N, K, device="cuda", generator=g)
+    gl[0], gt[0] = 1.0, 2.0 ** -24          # 1 from the left, 1 + K 2^-24 when the small ones are added first
+    gl[1], gt[1] = 2.0 ** -24, 1.0
+    want = gl.clone()
+    for k in range(K):
+        want = want + gt[:, k]              # the target's term first, then by k
+    L, _, ent, lse = forward(z, targets)
+    first = None
+    for _ in range(8):
+        d = torch.empty_like(z)
+        B.oapl_logits_logprobs_bwd(L, lse, ent, gl, None, gt, ids, d)
+        assert torch.equal(d.gather(1, targets.long()[:, None])[:, 0], want)
+        first = d if first is None else first
+        assert torch.equal(d, first)
+    B.oapl_logits_logprobs_bwd(L, lse, ent, gl, None, gt, ids, z)      # over the logits
+    assert torch.equal(z, first)
