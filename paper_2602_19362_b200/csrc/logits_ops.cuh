@@ -360,7 +360,7 @@ __device__ __forceinline__ RowPart row_part(const LogitsParams& p, int64_t row, 
 // A whole row by one CTA, any logits: the exact maximum m first, then x = c (z - m).  All threads get
 // {m, sum 2^x, sum 2^x x}; sh: NT / 32 entries.
 template <typename T, int NT>
-__device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* sh) {
+__device__ __forceinline__ RowTotal row_careful(const T* z, int V, float c, RowTotal* sh) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   float m = -INFINITY;
   bool nan = false;
@@ -405,6 +405,11 @@ __device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* 
   }
   __syncthreads();
   return r;
+}
+
+template <typename T, int NT>
+__device__ __noinline__ RowTotal row_slow(const T* z, int V, float c, RowTotal* sh) {
+  return row_careful<T, NT>(z, V, c, sh);
 }
 
 // The K best entries of every warp's part of the row through lists that are kept sorted over the lanes,
@@ -789,12 +794,12 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
 // ------------------------------------------------------------------------------------ backward
 // dz_v = a ( -p_v (G + g_H (ln p_v + H)) + g_lp [v = t] + sum_k g_k [v = id_k] ),  G = g_lp + sum_k g_k,
 // p_v = e^(a z_v - lse).  One read and one write per logit, HBM-bound; dz may be the logits themselves.
-// Six CTAs per SM (four: 12 % slower).  A CTA takes a span of a row, one batch of loads or, where there are rows
-// enough (kMany), four, which share the row's factors and the scan of its entries: these are half of the
-// instructions otherwise, and under the power limit fewer instructions are a higher clock.  4096 x 152064 bf16 in
-// repeated calls: 382 us with four batches, the copy rate; 403 us with one.  257 x 32003 fp32 with 8 entries a row:
-// 12.8 us with one.  The few entries with a point term are written again after the CTA's stores, from logits read
-// before them.
+// Six CTAs per SM (four: 12 % slower), five with one batch a CTA (64 x 152064 bf16 with 32 entries a row: 8.5 us, 9.0
+// with six).  A CTA takes a span of a row, one batch of loads or, where there are rows enough (kMany), four, which
+// share the row's factors and the scan of its entries: these are half of the instructions otherwise, and under the
+// power limit fewer instructions are a higher clock.  4096 x 152064 bf16 in repeated calls: 382 us with four batches,
+// the copy rate; 403 us with one.  257 x 32003 fp32 with 8 entries a row: 15.4 us with one.  The few entries with a
+// point term are written again after the CTA's stores, from logits read before them.
 struct RowGrad {
   float a, nlse;  // ln p = a z + nlse
   float A, B;     // dz = p (A ln p + B)
@@ -808,11 +813,91 @@ __device__ __forceinline__ float2 grad_smooth(float2 z, const RowGrad& r) {
   return __fmul2_rn(make_float2(ex2_approx(x.x), ex2_approx(x.y)), w);
 }
 
+// What the gradient needs of a row; lane k of every warp holds alternative k.
+struct RowTerms {
+  int target, id;  // -1 where there is none, or outside [0, V): they count for nothing
+  float g_target, g_id, G, ge, H, lse;
+};
+__device__ __forceinline__ RowTerms row_terms(const LogitsParams& p, int64_t row) {
+  const int lane = threadIdx.x & 31, K = p.K, V = p.V;
+  RowTerms t;
+  t.lse = p.lse[row];
+  t.target = p.g_logp ? p.targets[row] : -1;
+  if (t.target < 0 || t.target >= V) t.target = -1;
+  t.g_target = t.target >= 0 ? p.g_logp[row] : 0.f;
+  t.id = -1;
+  t.g_id = 0.f;
+  if (lane < K) {
+    t.id = p.ids[row * K + lane];
+    if (t.id < 0 || t.id >= V) t.id = -1;
+    if (t.id >= 0) t.g_id = p.g_top[row * K + lane];
+  }
+  t.G = t.g_target;
+  if (K) {
+    float sum = t.g_id;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    t.G += sum;
+  }
+  t.ge = p.g_entropy ? p.g_entropy[row] : 0.f;
+  t.H = p.g_entropy ? p.entropy[row] : 0.f;
+  return t;
+}
+__device__ __forceinline__ RowGrad row_grad(const LogitsParams& p, const RowTerms& t, float lse) {
+  return {p.scale, -lse, -p.scale * t.ge, -p.scale * fmaf(t.ge, t.H, t.G)};
+}
+// The entry with a point term that this thread writes (-1: none), with all terms of that entry.  An entry is written
+// by one warp: warp 0 the alternatives, whose lanes of equal index add the same terms in the same order (the target's
+// first, then by k); warp 1 the target where it is none of them.
+__device__ __forceinline__ int row_point(const RowTerms& t, int K, float& point) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  point = 0.f;
+  if (warp == 0 && K) {
+    if (t.id == t.target) point = t.g_target;
+    for (int k = 0; k < K; ++k) {
+      const int other = __shfl_sync(0xffffffffu, t.id, k);
+      const float g = __shfl_sync(0xffffffffu, t.g_id, k);
+      if (other == t.id) point += g;
+    }
+    return t.id;
+  }
+  if (warp == 1 && t.target >= 0 && !__any_sync(0xffffffffu, t.id == t.target)) {
+    point = t.g_target;
+    return lane == 0 ? t.target : -1;
+  }
+  return -1;
+}
+
+// Beyond this |lse| its fp32 digits do not resolve p (half a step of 1024 is 2^-14 of p; at 1e9 it is e^32).  Such a
+// row (a large common offset, or nothing but a finite mask value) is done by one CTA, which forms the maximum m and
+// the sum S again and takes ln p = a (z - m) - ln S.  It is only careful: three passes, an
+// element at a time (one row of 152064 bf16: 142 us; 4096 of them 1.98 ms, against 0.38 for other rows).
+constexpr float kLgResolved = 1024.f;
+template <typename T>
+__device__ __forceinline__ void grad_row_apart(const LogitsParams& p, int64_t row) {
+  using E = Elem<T>;
+  __shared__ RowTotal sh_tot[kLgThreads / 32];
+  const T* z = reinterpret_cast<const T*>(p.z) + row * p.ld;
+  T* d = reinterpret_cast<T*>(p.dz) + row * p.ld_d;
+  const RowTotal tot = row_careful<T, kLgThreads>(z, p.V, p.scale * 1.4426950408889634f, sh_tot);
+  const bool none = tot.m == -INFINITY && tot.s == 0.f;  // not the row that this lse is of: p = 0
+  const float m = none ? 0.f : tot.m;
+  const RowTerms t = row_terms(p, row);
+  const RowGrad r = row_grad(p, t, none ? 1e30f : logf(tot.s));
+  float point;
+  const int at = row_point(t, p.K, point);
+  const float z_at = at >= 0 ? E::one(z, at) : 0.f;
+  __syncthreads();  // the logits at these entries have been read
+  for (int i = threadIdx.x; i < p.V; i += kLgThreads) E::put(d, i, grad_smooth(make_float2(E::one(z, i) - m, 0.f), r).x);
+  __syncthreads();
+  if (at >= 0) E::put(d, at, fmaf(r.a, point, grad_smooth(make_float2(z_at - m, 0.f), r).x));
+}
+
 template <typename T, bool kMany>
-__global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsParams p, int spans) {
+__global__ void __launch_bounds__(kLgThreads, kMany ? 6 : 5) logits_bwd_kernel(const __grid_constant__ LogitsParams p, int spans) {
   using E = Elem<T>;
   constexpr int kN = E::kN;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x;
   const int64_t row = blockIdx.x / unsigned(spans);
   const int span = int(blockIdx.x % unsigned(spans));
   const int V = p.V, K = p.K;
@@ -853,48 +938,20 @@ __global__ void __launch_bounds__(kLgThreads, 6) logits_bwd_kernel(const LogitsP
   const int single = tid < nh ? tid : nv * kN + tid;
   if (span == 0 && tid < nsingle) zs = E::one(zrow, single);
 
-  // the row's factors; lane k of every warp holds alternative k
-  const int target = p.g_logp ? p.targets[row] : -1;
-  const bool target_in = target >= 0 && target < V;  // indexes outside [0, V) count for nothing
-  const float g_target = target_in ? p.g_logp[row] : 0.f;
-  int id = -1;
-  float g_id = 0.f;
-  if (lane < K) {
-    id = p.ids[row * K + lane];
-    if (id < 0 || id >= V) id = -1;
-    if (id >= 0) g_id = p.g_top[row * K + lane];
-  }
-  float G = g_target;
-  if (K) {
-    float sum = g_id;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    G += sum;
-  }
-  const float ge = p.g_entropy ? p.g_entropy[row] : 0.f;
-  const float H = p.g_entropy ? p.entropy[row] : 0.f;
-  float lse = p.lse[row];
+  const RowTerms t = row_terms(p, row);
+  float lse = t.lse;
   // a row without a finite logit, or with nothing but a type's lowest value as a mask: every p is 0
-  if (lse < -1e30f) lse = 1e30f;
-  const RowGrad r = {p.scale, -lse, -p.scale * ge, -p.scale * fmaf(ge, H, G)};
-
-  // the entries with a point term, each with all terms at its entry and written by one warp: warp 0 the
-  // alternatives, whose lanes of equal index add the same terms in the same order (the target's first, then by k);
-  // warp 1 the target where it is none of them
-  int at = -1;
-  float point = 0.f;
-  if (warp == 0 && K) {
-    at = id;
-    if (id == target) point = g_target;
-    for (int k = 0; k < K; ++k) {
-      const int other = __shfl_sync(0xffffffffu, id, k);
-      const float g = __shfl_sync(0xffffffffu, g_id, k);
-      if (other == id) point += g;
-    }
-  } else if (warp == 1 && target_in && !__any_sync(0xffffffffu, id == target)) {
-    point = g_target;
-    at = lane == 0 ? target : -1;
+  if (lse < -1e30f) {
+    lse = 1e30f;
+  } else if (fabsf(lse) > kLgResolved) {  // the same for all threads of the row
+    unsigned block;  // read anew: nothing that only these rows need is held in registers
+    asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(block));
+    if (block % unsigned(spans) == 0) grad_row_apart<T>(p, block / unsigned(spans));
+    return;
   }
+  const RowGrad r = row_grad(p, t, lse);
+  float point;
+  int at = row_point(t, K, point);
   if (at >= 0) {  // owned by the CTA that stores it
     const int vec = (at - nh) / kN;
     const bool is_single = at < nh || at >= nh + nv * kN;

@@ -1,5 +1,5 @@
-"""oapl_logits_logprobs and its gradient where order, magnitude or cancellation decide: ids that repeat the
-target, peaked rows."""
+"""oapl_logits_logprobs and its gradient where order, magnitude or cancellation decide: ids that repeat the target,
+peaked rows, rows whose log-sum-exp is too large for its digits to say anything of a probability."""
 import math
 
 import pytest
@@ -74,3 +74,74 @@ def test_entropy_of_peaked_rows(t, V, N):
         top = torch.empty(N, K, device="cuda") if K else None
         B.oapl_logits_logprobs(B.make_logits(z), None, ent, None, top)
         assert bool(((ent.double() - want).abs() <= tol).all()), (ent, want)
+
+
+def exact_gradient(z, targets, gl, ge, gt, ids, scale):
+    """From the logits alone, in 64 bits: ln p relative to the row's maximum.  Also the size that roundings scale with."""
+    x = z.double()
+    d = scale * (x - x.amax(1, keepdim=True))
+    lp = torch.log_softmax(d, 1)
+    p = lp.exp()
+    plp = torch.where(p > 0, p * lp, torch.zeros_like(p))
+    H = -plp.sum(1, keepdim=True)
+    G = gl.double() + gt.double().sum(1)
+    point = torch.zeros_like(x).scatter_add_(1, targets.long()[:, None], gl.double()[:, None])
+    point.scatter_add_(1, ids.long(), gt.double())
+    out = scale * (-(p * G[:, None] + ge.double()[:, None] * (plp + p * H)) + point)
+    terms = torch.zeros_like(x).scatter_add_(1, targets.long()[:, None], gl.double().abs()[:, None])
+    terms.scatter_add_(1, ids.long(), gt.double().abs())
+    size = scale * (p * (gl.double().abs() + gt.double().abs().sum(1))[:, None] + ge.double().abs()[:, None] * (plp.abs() + p * H + p))
+    dist = torch.where(p > 0, d.abs(), torch.zeros_like(d))
+    return out, size, dist, scale * terms
+
+
+@pytest.mark.parametrize("t,low", [("bf16", -1e9), ("f32", -1e9), ("f32", -1e20), ("bf16", -1e20), ("f16", -65504.0),
+                                   ("bf16", -3000.0), ("f32", 1e9), ("f32", 1e5), ("bf16", 4e4), ("f16", 6e4)])
+@pytest.mark.parametrize("scale,N,V", [(1.0, 6, 3001), (1 / 0.7, 700, 3001), (1.3, 6, 152064), (1 / 0.7, 60, 50021),
+                                       (1.0, 1200, 70001)])
+def test_gradient_of_rows_with_a_large_offset(t, low, scale, N, V):
+    g = torch.Generator(device="cuda").manual_seed(V)
+    kinds = 6
+    z = torch.randn(kinds, V, device="cuda", generator=g)
+    z[0] = low                                    # nothing but a finite mask value, or the offset alone: uniform
+    z[1] = low
+    z[1, ::2] = -math.inf                         # some excluded altogether
+    z[2] = low + z[2] * abs(low) * 2.0 ** -6      # an offset, and logits as far apart as the type tells them
+    z[3] = low
+    z[3, V // 2] = low + abs(low) / 8             # one above the rest
+    if t == "f16":
+        z[2:4].clamp_(-65504.0, 65504.0)
+    z = z.to(TYPES[t]).repeat(-(-N // kinds), 1)[:N].contiguous()      # rows 4, 5: ordinary ones beside them
+    targets = torch.full((N,), 1, dtype=torch.int32, device="cuda")
+    targets[0] = V - 1
+    gl, ge = torch.randn(N, device="cuda", generator=g), torch.randn(N, device="cuda", generator=g)
+    gt = torch.rand(N, 3, device="cuda", generator=g)
+    ids = torch.tensor([[1, V // 2, V - 1]], dtype=torch.int32, device="cuda").repeat(N, 1)
+    L, _, ent, lse = forward(z, targets, None, scale)
+    d = torch.empty(N, V + 3, dtype=z.dtype, device="cuda")[:, :V]
+    B.oapl_logits_logprobs_bwd(L, lse, ent, gl, ge, gt, ids, d)
+    want, size, dist, point = exact_gradient(z, targets, gl, ge, gt, ids, scale)
+    fi = torch.finfo(z.dtype)
+    # One rounding to the type.  p: 2^-22 of the exponential; ln p: behind an lse of up to 1024 its half step 2^-15 and
+    # its product with ln 2, 2^-14; otherwise ln S as a sum of V / 128 terms a thread and a tree of 13; and five
+    # roundings of a distance (scale, difference, multiply-add, two of the change of base).  The forward's entropy: its
+    # two sums of as many terms.  The rest: roundings of factors and terms.
+    rel = 2.0 ** -22 + 2.0 ** -13 + (5 * dist + V / 128 + 100) * U
+    tol = fi.eps / 2 * want.abs() + size * rel * (1 + fi.eps) + 12 * U * point + fi.smallest_normal * fi.eps + 1e-35
+    bad = ~((d.double() - want).abs() <= tol)
+    assert not bool(bad.any()), (bad.nonzero()[:4], d[bad][:4], want[bad][:4], tol[bad][:4])
+    again = z.clone()
+    L2 = B.make_logits(again, targets, None, scale)
+    B.oapl_logits_logprobs_bwd(L2, lse, ent, gl, ge, gt, ids, again)       # over the logits
+    assert torch.equal(again, d)
+
+
+def test_gradient_of_a_row_that_does_not_belong_to_its_lse_is_bounded():
+    # no finite logit, but an lse that says otherwise: p is 0, the point term is left
+    z = torch.full((2, 700), -math.inf, device="cuda")
+    targets = torch.tensor([3, 5], dtype=torch.int32, device="cuda")
+    d = torch.empty_like(z)
+    B.oapl_logits_logprobs_bwd(B.make_logits(z, targets), torch.tensor([2e3, -5e9], device="cuda"), None,
+                               torch.ones(2, device="cuda"), None, None, None, d)
+    want = torch.zeros_like(z).scatter_(1, targets.long()[:, None], 1.0)
+    assert torch.equal(d, want)
