@@ -371,6 +371,7 @@ typedef struct {
  * OAPL_QUANT_POW2: scale = 2^ceil(log2(amax / top)) instead.  OAPL_QUANT_TRANSPOSE: out is x turned,
  * [cols, rows], with blocks of the turned matrix.  Only rows x cols values are written, never the padding
  * behind a row.  A NaN makes its block's scale and values NaN, an infinity the scale infinite.
+ * Strides of out's scales that give two blocks one place (0 over several blocks, for instance) are refused.
  */
 #define OAPL_QUANT_TRANSPOSE 1
 #define OAPL_QUANT_POW2 2

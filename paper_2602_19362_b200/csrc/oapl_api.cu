@@ -772,6 +772,22 @@ static int check_scaled(const oapl_scaled* m) {
   return OAPL_OK;
 }
 
+// Whether every scale of the matrix has a place of its own, which an output needs.  Two blocks (di, dj) apart share
+// one where di * row stride = dj * column stride; the smallest such pair is the strides over their common divisor,
+// crosswise.
+static bool scales_apart(const oapl_scaled* m) {
+  const int64_t nr = (m->rows + m->block_rows - 1) / m->block_rows, nc = (m->cols + 127) / 128;
+  int64_t a = m->scale_row_stride, b = m->scale_col_stride;
+  if (nr == 1 || nc == 1) return (nr == 1 || a > 0) && (nc == 1 || b > 0);
+  if (a == 0 || b == 0) return false;
+  while (b) {
+    const int64_t r = a % b;
+    a = b;
+    b = r;
+  }
+  return m->scale_col_stride / a >= nr || m->scale_row_stride / a >= nc;
+}
+
 template <typename T>
 static int launch_quantize(const QuantParams& qp, bool e5, bool block, bool turn, cudaStream_t st) {
   const int64_t grid = (((int64_t)qp.R + 127) / 128) * (((int64_t)qp.C + 127) / 128);
@@ -1477,6 +1493,7 @@ int oapl_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int
   if (flags & ~(OAPL_QUANT_TRANSPOSE | OAPL_QUANT_POW2)) return OAPL_ERR_INVALID_ARG;
   const bool turn = (flags & OAPL_QUANT_TRANSPOSE) != 0;
   if (out->rows != (turn ? cols : rows) || out->cols != (turn ? rows : cols)) return OAPL_ERR_INVALID_ARG;
+  if (!scales_apart(out)) return OAPL_ERR_INVALID_ARG;
   if ((uintptr_t)x % es) return OAPL_ERR_MISALIGNED;
   QuantParams qp;
   memset(&qp, 0, sizeof(qp));

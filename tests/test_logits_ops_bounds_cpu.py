@@ -1,0 +1,37 @@
+"""Further refusals of the calls on logits in memory and on 8-bit matrices, made on the host before any CUDA call
+(the addresses are never dereferenced)."""
+import ctypes
+import itertools
+
+import pytest
+
+from paper_2602_19362_b200 import binding as B, build
+
+OUT, ST = ctypes.c_void_p(0x2000), ctypes.c_void_p(0)
+INVALID = -1
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build()
+    return B.lib()
+
+
+def test_quantize_refuses_scales_that_share_a_place(L):
+    """Every layout of 1 to 4 by 1 to 4 scales with strides up to 6, against a count of the places.  A call that is not
+    refused for its scales is refused for the alignment of x, which is looked at last."""
+    for nr, nc, sr, sc in itertools.product(range(1, 5), range(1, 5), range(7), range(7)):
+        apart = len({i * sr + j * sc for i in range(nr) for j in range(nc)}) == nr * nc
+        for b in (1, 128):
+            rows, cols = (nr if b == 1 else 128 * nr - 5), 128 * nc - 1
+            m = B.OaplScaled(0x1000, 0x2000, rows, cols, 1024, sr, sc, 3, b)
+            rc = L.oapl_quantize(ctypes.c_void_p(0x2001), 0, rows, cols, 2000, m, 0, ST)
+            assert rc == (-2 if apart else INVALID), (nr, nc, sr, sc, b)
+            rc = L.oapl_quantize(ctypes.c_void_p(0x2001), 0, cols, rows, 2000, m, B.OAPL_QUANT_TRANSPOSE, ST)
+            assert rc == (-2 if apart else INVALID), (nr, nc, sr, sc, b)
+
+
+def test_scales_of_operands_may_share_a_place(L):
+    # one scale for all rows of a column block is a legal operand: refused here only for C's alignment
+    m = B.OaplScaled(0x1000, 0x2000, 256, 512, 512, 0, 1, 3, 1)
+    assert L.oapl_scaled_matmul(m, m, ctypes.c_void_p(0x2001), 0, 256, 0, None, ST) == -2
