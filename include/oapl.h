@@ -338,7 +338,8 @@ int oapl_logits_logprobs(const oapl_logits* logits /*host*/, float* token_logp, 
  *   (K = 0 without): any K token ids, not only the forward's; an id may occur twice.  Ids and targets
  *   outside [0,V) count for nothing (their share of G included).
  *   dlogits [N,V], the logits' type, rows ld_d elements apart; rows with mask==0 are written as 0.
- *   It may be the logits' own memory (then ld_d == ld), but must not overlap them otherwise.
+ *   It may be the logits' own memory (then ld_d == ld) or, with ld_d == ld, lie between their rows; any other
+ *   overlap is refused.
  * ln p_v is scale * z_v - token_lse in fp32, whose rounding costs |token_lse| 2^-24 of a probability.  A row whose
  * |token_lse| exceeds 1024 (a large common offset; nothing but a finite mask value such as -1e9) would lose its
  * probabilities that way: there the row's maximum and sum are formed again from its logits, by one CTA, several times

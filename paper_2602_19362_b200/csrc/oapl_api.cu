@@ -742,6 +742,18 @@ static int route_logits_fwd(const LogitsParams& lp, cudaStream_t st) {
   return lp.N <= 4 * n_sm ? launch_logits_fwd<T, true, 256>(lp, nc, st) : launch_logits_fwd<T, true, 128>(lp, 1, st);
 }
 
+// Whether no logit is written that is still to be read: the result over the logits row by row, in memory of its own, or
+// between the logits' rows.  Other overlaps are refused, also the few with different strides that would be harmless.
+static bool gradient_place(const LogitsParams& lp, int es) {
+  using Wide = unsigned __int128;
+  const Wide z = reinterpret_cast<uintptr_t>(lp.z), d = reinterpret_cast<uintptr_t>(lp.dz), row = (Wide)lp.V * es;
+  const Wide z_end = z + (Wide)(lp.N - 1) * lp.ld * es + row, d_end = d + (Wide)(lp.N - 1) * lp.ld_d * es + row;
+  if (d >= z_end || z >= d_end) return true;
+  if (lp.ld != lp.ld_d) return false;
+  const Wide pitch = (Wide)lp.ld * es, off = z < d ? (d - z) % pitch : pitch - 1 - (z - d - 1) % pitch;
+  return z == d || (off >= row && pitch - off >= row);
+}
+
 template <typename T>
 static int launch_logits_bwd(const LogitsParams& lp, cudaStream_t st) {
   // A CTA's span of a row: four batches of loads, so that the row's factors and the scan of its entries are
@@ -749,6 +761,7 @@ static int launch_logits_bwd(const LogitsParams& lp, cudaStream_t st) {
   const int64_t nv = (int64_t)lp.V / Elem<T>::kN, batch = kLgThreads * kLgUnroll;
   int64_t spans = (nv + 4 * batch) / (4 * batch);
   if (spans * lp.N > (int64_t)2147483647) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  if (!gradient_place(lp, sizeof(T))) return OAPL_ERR_INVALID_ARG;
   const int n_sm = sm_count();
   if (n_sm <= 0) return OAPL_ERR_CUDA;
   const bool many = spans * lp.N >= 4 * 6 * (int64_t)n_sm;

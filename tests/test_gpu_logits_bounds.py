@@ -145,3 +145,22 @@ def test_gradient_of_a_row_that_does_not_belong_to_its_lse_is_bounded():
                                torch.ones(2, device="cuda"), None, None, None, d)
     want = torch.zeros_like(z).scatter_(1, targets.long()[:, None], 1.0)
     assert torch.equal(d, want)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("first", [True, False])
+def test_gradient_between_the_rows_of_the_logits(t, first):
+    # [logits | gradient] or [gradient | logits] in one buffer, rows side by side
+    N, V = 70, 5003
+    g = torch.Generator(device="cuda").manual_seed(1)
+    buf = torch.randn(N, 2 * V, device="cuda", generator=g).to(TYPES[t])
+    z, d = (buf[:, :V], buf[:, V:]) if first else (buf[:, V:], buf[:, :V])
+    targets = torch.randint(0, V, (N,), device="cuda", generator=g).to(torch.int32)
+    gl = torch.randn(N, device="cuda", generator=g)
+    old = z.clone()
+    L, _, ent, lse = forward(z, targets)
+    B.oapl_logits_logprobs_bwd(L, lse, ent, gl, gl, None, None, d)
+    assert torch.equal(z, old)
+    want = torch.empty_like(old)
+    B.oapl_logits_logprobs_bwd(B.make_logits(old, targets), lse, ent, gl, gl, None, None, want)
+    assert torch.equal(d, want)

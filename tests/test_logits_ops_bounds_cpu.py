@@ -35,3 +35,13 @@ def test_scales_of_operands_may_share_a_place(L):
     # one scale for all rows of a column block is a legal operand: refused here only for C's alignment
     m = B.OaplScaled(0x1000, 0x2000, 256, 512, 512, 0, 1, 3, 1)
     assert L.oapl_scaled_matmul(m, m, ctypes.c_void_p(0x2001), 0, 256, 0, None, ST) == -2
+
+
+@pytest.mark.parametrize("off, ld_d", [(2, 2100), (-2, 2100), (1000, 2100), (1998, 2100), (-1998, 2100), (2 * 2100 + 500, 2100),
+                                       (-2 * 2100 * 7 - 4, 2100), (2 * 2100 * 63 + 1998, 2100), (2 * 2100 - 1000, 2100),
+                                       (4000, 2099), (-4000, 2101), (2, 1 << 40)])
+def test_gradient_refuses_a_place_that_overlaps_the_logits(L, off, ld_d):
+    """64 rows of 1000 bf16 logits, 2100 elements apart: bytes that a row of the result shares with any row of them."""
+    p = B.OaplLogits(0x100000, 64, 2100, 1000, 0, 0x3000, 0x4000, 1.0)
+    d = ctypes.c_void_p(p.logits + off)
+    assert L.oapl_logits_logprobs_bwd(p, OUT, OUT, OUT, OUT, 0, None, None, d, ld_d, ST) == INVALID
