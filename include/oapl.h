@@ -384,6 +384,8 @@ int oapl_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int
  * block_rows of A and B may differ.  C: bf16, f16 or f32 (c_type), rows ldc elements apart, natural
  * alignment.  Products of a block of 128 are summed by the tensor cores in fp32, scaled blocks in fp32;
  * one rounding to c_type at the end (accumulate: of the sum with the old C).  Bitwise reproducible.
+ * A pipeline wait that runs out (its limit is far above any healthy wait) sets OAPL_ERR_DEVICE_TIMEOUT in
+ * device_status, and what was not computed is NaN in C, so that it shows without a status word too.
  *   logits = H . W^T:  A = H, B = W (128 x 128 blocks);
  *   dH = g . W:        A = g, B = W quantised with OAPL_QUANT_TRANSPOSE;
  *   dW = g^T . H:      A = g, B = H, both with OAPL_QUANT_TRANSPOSE (block_rows 1), accumulate.
@@ -493,6 +495,15 @@ int oapl_profile_applies(int enabled_device, int current_device);
  */
 int oapl_debug_gemm(const void* A, const void* B, float* C, int M, int N, int K, int a_mn,
                     int b_mn, int wide, long long wait_cycles, int skip_step, int* err, void* stream);
+
+/*
+ * oapl_scaled_matmul with the two arguments of the give-up path's test, as above: wait_cycles > 0 (at most 4e9, the
+ * product limit) replaces the limit of every pipeline wait, and skip_step = k > 0 (with 0 < wait_cycles <= 1e8) leaves out the loads of every CTA's
+ * pipeline step k - 1: a block of 128 of K, for at most 64 rows of A two or four of them.  device_status is needed.
+ */
+int oapl_debug_scaled_matmul(const oapl_scaled* A /*host*/, const oapl_scaled* B /*host*/, void* C, int32_t c_type,
+                             int64_t ldc, int accumulate, int32_t* device_status, long long wait_cycles,
+                             int skip_step, void* stream);
 
 #ifdef __cplusplus
 }

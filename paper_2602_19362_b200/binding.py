@@ -26,7 +26,8 @@ EXPORTS = ["oapl_workspace_bytes", "oapl_token_logprobs", "oapl_value_estimate",
            "oapl_token_logprobs_static", "oapl_loss_fwd_bwd", "oapl_profile_read_clocks", "oapl_entropy", "oapl_group_advantage",
            "oapl_grpo_loss_fwd_bwd", "oapl_adamw_workspace_bytes", "oapl_adamw_step", "oapl_loss_fwd_bwd_ex",
            "oapl_get_range_count", "oapl_profile_applies", "oapl_range_slots", "oapl_batch_stats",
-           "oapl_logits_logprobs", "oapl_logits_logprobs_bwd", "oapl_quantize", "oapl_scaled_matmul"]
+           "oapl_logits_logprobs", "oapl_logits_logprobs_bwd", "oapl_quantize", "oapl_scaled_matmul",
+           "oapl_debug_scaled_matmul"]
 
 
 class OaplProblem(ctypes.Structure):
@@ -128,6 +129,8 @@ def lib() -> ctypes.CDLL:
         L.oapl_quantize.argtypes = [vp, ctypes.c_int32, i64, i64, i64, ps, i32, vp]
         L.oapl_scaled_matmul.restype = i32
         L.oapl_scaled_matmul.argtypes = [ps, ps, vp, ctypes.c_int32, i64, i32, vp, vp]
+        L.oapl_debug_scaled_matmul.restype = i32
+        L.oapl_debug_scaled_matmul.argtypes = [ps, ps, vp, ctypes.c_int32, i64, i32, vp, ctypes.c_longlong, i32, vp]
         L.oapl_profile_enable.restype = i32
         L.oapl_profile_enable.argtypes = [i32]
         L.oapl_profile_read.restype = i32
@@ -481,15 +484,27 @@ def oapl_quantize(x, out: OaplScaled, transpose: bool = False, pow2: bool = Fals
         raise OaplError(rc, "oapl_quantize")
 
 
-def oapl_scaled_matmul(A: OaplScaled, B: OaplScaled, C, accumulate: bool = False, device_status=None):
-    """C [A.rows, B.rows] (bf16, fp16, fp32) = A . B^T, or C += A . B^T."""
+def _product_args(A, B, C, accumulate, device_status):
     code, rows, cols, ldc = _rows(C, FLOAT_TYPES, "C")
     if rows != A.rows or cols != B.rows:
         raise TypeError(f"C: expected shape {(A.rows, B.rows)}")
     dev = C.get_device()
     if A.device != dev or B.device != dev:
         raise TypeError("A, B: expected C's device")
-    rc = lib().oapl_scaled_matmul(A, B, C.data_ptr(), code, ldc, accumulate,
-                                  _vec(device_status, torch.int32, (1,), dev, "device_status"), _stream_of(dev))
+    return A, B, C.data_ptr(), code, ldc, accumulate, _vec(device_status, torch.int32, (1,), dev, "device_status")
+
+
+def oapl_scaled_matmul(A: OaplScaled, B: OaplScaled, C, accumulate: bool = False, device_status=None):
+    """C [A.rows, B.rows] (bf16, fp16, fp32) = A . B^T, or C += A . B^T.  NaN where a pipeline wait ran out, and
+    OAPL_ERR_DEVICE_TIMEOUT in device_status (int32 [1], zero before the call)."""
+    rc = lib().oapl_scaled_matmul(*_product_args(A, B, C, accumulate, device_status), _stream_of(C.get_device()))
     if rc != OAPL_OK:
         raise OaplError(rc, "oapl_scaled_matmul")
+
+
+def oapl_debug_scaled_matmul(A: OaplScaled, B: OaplScaled, C, device_status, accumulate: bool = False, wait_cycles=0,
+                             skip_step=0):
+    rc = lib().oapl_debug_scaled_matmul(*_product_args(A, B, C, accumulate, device_status), int(wait_cycles),
+                                        int(skip_step), _stream_of(C.get_device()))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_debug_scaled_matmul")

@@ -873,7 +873,7 @@ static int route_scaled_few(const oapl_scaled* A, const oapl_scaled* B, const Fe
 
 // At most 64 rows of A: the roles swapped, B's rows shared out over the SMs (see scaled_few_kernel).
 static int scaled_few(const oapl_scaled* A, const oapl_scaled* B, void* C, int32_t c_type, int64_t ldc, int accumulate,
-                      int32_t* device_status, int n_sm, cudaStream_t st) {
+                      int32_t* device_status, uint32_t wait_cycles, uint32_t skip_step, int n_sm, cudaStream_t st) {
   FewParams fp;
   memset(&fp, 0, sizeof(fp));
   fp.sw = B->scale;
@@ -896,9 +896,69 @@ static int scaled_few(const oapl_scaled* A, const oapl_scaled* B, void* C, int32
   fp.rows = (int32_t)((B->rows + rounds * n_sm - 1) / (rounds * n_sm));
   fp.tiles = (int32_t)((B->rows + fp.rows - 1) / fp.rows);
   fp.err = device_status;
+  fp.wait_cycles = wait_cycles;
+  fp.skip_step = skip_step;
   if (c_type == OAPL_TYPE_BF16) return route_scaled_few<OUT_BF16>(A, B, fp, n_sm, st);
   if (c_type == OAPL_TYPE_F16) return route_scaled_few<OUT_F16>(A, B, fp, n_sm, st);
   return route_scaled_few<OUT_F32>(A, B, fp, n_sm, st);
+}
+
+static int scaled_product(const oapl_scaled* A, const oapl_scaled* B, void* C, int32_t c_type, int64_t ldc,
+                          int accumulate, int32_t* device_status, uint32_t wait_cycles, uint32_t skip_step, void* stream) {
+  int rc = check_scaled(A);
+  if (rc == OAPL_OK) rc = check_scaled(B);
+  if (rc != OAPL_OK) return rc;
+  const int es = logits_type_size(c_type);
+  if (!C || !es || A->cols != B->cols || ldc < B->rows) return OAPL_ERR_INVALID_ARG;
+  if ((uintptr_t)C % es) return OAPL_ERR_MISALIGNED;
+  const int n_sm = sm_count();
+  if (n_sm < 2) return OAPL_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (A->rows <= 64) return scaled_few(A, B, C, c_type, ldc, accumulate, device_status, wait_cycles, skip_step, n_sm, st);
+  CUtensorMap ta, tb;
+  if (!make_map_u8(&ta, A->data, (uint64_t)A->rows, (uint64_t)A->cols, (uint64_t)A->ld) ||
+      !make_map_u8(&tb, B->data, (uint64_t)B->rows, (uint64_t)B->cols, (uint64_t)B->ld))
+    return OAPL_ERR_CUDA;
+  ScaledParams sp;
+  memset(&sp, 0, sizeof(sp));
+  sp.sa = A->scale;
+  sp.sb = B->scale;
+  sp.sa_row = A->scale_row_stride;
+  sp.sa_col = A->scale_col_stride;
+  sp.sb_row = B->scale_row_stride;
+  sp.sb_col = B->scale_col_stride;
+  sp.ga = A->block_rows;
+  sp.gb = B->block_rows;
+  sp.M = (int32_t)A->rows;
+  sp.N = (int32_t)B->rows;
+  sp.K = (int32_t)A->cols;
+  sp.C = C;
+  sp.ldc = ldc;
+  sp.accumulate = accumulate != 0;
+  CUtensorMap tc = ta;
+  if (((uintptr_t)C & 15) == 0 && (ldc * es) % 16 == 0 && (!accumulate || c_type == OAPL_TYPE_F32)) {
+    if (!make_map_out(&tc, C, c_type, (uint64_t)A->rows, (uint64_t)B->rows, (uint64_t)ldc)) return OAPL_ERR_CUDA;
+    sp.bulk = accumulate ? 2 : 1;
+  }
+  sp.e5_a = A->type == OAPL_TYPE_E5M2;
+  sp.e5_b = B->type == OAPL_TYPE_E5M2;
+  sp.mt = (sp.M + kSmTile - 1) / kSmTile;
+  sp.nt = (sp.N + kSmTile - 1) / kSmTile;
+  sp.group = sp.mt < 16 ? sp.mt : 16;
+  sp.err = device_status;
+  sp.wait_cycles = wait_cycles;
+  sp.skip_step = skip_step;
+  const int64_t tiles = (int64_t)sp.mt * sp.nt;
+  const int grid = 2 * (int)(tiles < n_sm / 2 ? tiles : n_sm / 2);
+  const bool percol = sp.gb == 1;
+  if (c_type == OAPL_TYPE_BF16)
+    return percol ? launch_scaled_matmul<OUT_BF16, true>(ta, tb, tc, sp, grid, st)
+                  : launch_scaled_matmul<OUT_BF16, false>(ta, tb, tc, sp, grid, st);
+  if (c_type == OAPL_TYPE_F16)
+    return percol ? launch_scaled_matmul<OUT_F16, true>(ta, tb, tc, sp, grid, st)
+                  : launch_scaled_matmul<OUT_F16, false>(ta, tb, tc, sp, grid, st);
+  return percol ? launch_scaled_matmul<OUT_F32, true>(ta, tb, tc, sp, grid, st)
+                : launch_scaled_matmul<OUT_F32, false>(ta, tb, tc, sp, grid, st);
 }
 
 }  // namespace oapl
@@ -1530,58 +1590,17 @@ int oapl_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int
 
 int oapl_scaled_matmul(const oapl_scaled* A, const oapl_scaled* B, void* C, int32_t c_type, int64_t ldc,
                        int accumulate, int32_t* device_status, void* stream) {
-  int rc = check_scaled(A);
-  if (rc == OAPL_OK) rc = check_scaled(B);
-  if (rc != OAPL_OK) return rc;
-  const int es = logits_type_size(c_type);
-  if (!C || !es || A->cols != B->cols || ldc < B->rows) return OAPL_ERR_INVALID_ARG;
-  if ((uintptr_t)C % es) return OAPL_ERR_MISALIGNED;
-  const int n_sm = sm_count();
-  if (n_sm < 2) return OAPL_ERR_CUDA;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (A->rows <= 64) return scaled_few(A, B, C, c_type, ldc, accumulate, device_status, n_sm, st);
-  CUtensorMap ta, tb;
-  if (!make_map_u8(&ta, A->data, (uint64_t)A->rows, (uint64_t)A->cols, (uint64_t)A->ld) ||
-      !make_map_u8(&tb, B->data, (uint64_t)B->rows, (uint64_t)B->cols, (uint64_t)B->ld))
-    return OAPL_ERR_CUDA;
-  ScaledParams sp;
-  memset(&sp, 0, sizeof(sp));
-  sp.sa = A->scale;
-  sp.sb = B->scale;
-  sp.sa_row = A->scale_row_stride;
-  sp.sa_col = A->scale_col_stride;
-  sp.sb_row = B->scale_row_stride;
-  sp.sb_col = B->scale_col_stride;
-  sp.ga = A->block_rows;
-  sp.gb = B->block_rows;
-  sp.M = (int32_t)A->rows;
-  sp.N = (int32_t)B->rows;
-  sp.K = (int32_t)A->cols;
-  sp.C = C;
-  sp.ldc = ldc;
-  sp.accumulate = accumulate != 0;
-  CUtensorMap tc = ta;
-  if (((uintptr_t)C & 15) == 0 && (ldc * es) % 16 == 0 && (!accumulate || c_type == OAPL_TYPE_F32)) {
-    if (!make_map_out(&tc, C, c_type, (uint64_t)A->rows, (uint64_t)B->rows, (uint64_t)ldc)) return OAPL_ERR_CUDA;
-    sp.bulk = accumulate ? 2 : 1;
-  }
-  sp.e5_a = A->type == OAPL_TYPE_E5M2;
-  sp.e5_b = B->type == OAPL_TYPE_E5M2;
-  sp.mt = (sp.M + kSmTile - 1) / kSmTile;
-  sp.nt = (sp.N + kSmTile - 1) / kSmTile;
-  sp.group = sp.mt < 16 ? sp.mt : 16;
-  sp.err = device_status;
-  const int64_t tiles = (int64_t)sp.mt * sp.nt;
-  const int grid = 2 * (int)(tiles < n_sm / 2 ? tiles : n_sm / 2);
-  const bool percol = sp.gb == 1;
-  if (c_type == OAPL_TYPE_BF16)
-    return percol ? launch_scaled_matmul<OUT_BF16, true>(ta, tb, tc, sp, grid, st)
-                  : launch_scaled_matmul<OUT_BF16, false>(ta, tb, tc, sp, grid, st);
-  if (c_type == OAPL_TYPE_F16)
-    return percol ? launch_scaled_matmul<OUT_F16, true>(ta, tb, tc, sp, grid, st)
-                  : launch_scaled_matmul<OUT_F16, false>(ta, tb, tc, sp, grid, st);
-  return percol ? launch_scaled_matmul<OUT_F32, true>(ta, tb, tc, sp, grid, st)
-                : launch_scaled_matmul<OUT_F32, false>(ta, tb, tc, sp, grid, st);
+  return scaled_product(A, B, C, c_type, ldc, accumulate, device_status, (uint32_t)kWaitCycles, 0, stream);
+}
+
+int oapl_debug_scaled_matmul(const oapl_scaled* A, const oapl_scaled* B, void* C, int32_t c_type, int64_t ldc,
+                             int accumulate, int32_t* device_status, long long wait_cycles, int skip_step, void* stream) {
+  // as for oapl_debug_gemm: a step is left out only under a short limit, so that the launch ends soon
+  if (!device_status || wait_cycles < 0 || wait_cycles > kWaitCycles || skip_step < 0) return OAPL_ERR_INVALID_ARG;
+  if (skip_step > 0 && (wait_cycles == 0 || wait_cycles > 100000000LL)) return OAPL_ERR_INVALID_ARG;
+  return scaled_product(A, B, C, c_type, ldc, accumulate, device_status,
+                        (uint32_t)(wait_cycles ? wait_cycles : kWaitCycles),
+                        (uint32_t)skip_step, stream);
 }
 
 }  // extern "C"

@@ -56,6 +56,10 @@ static_assert(128 * kSmRegsLow + 256 * kSmRegsHigh == kSmThreads * kSmRegs, "reg
 
 enum { OUT_BF16 = 0, OUT_F16 = 1, OUT_F32 = 2 };
 
+// Both kernels' give-up path.  wait_cycles: limit of every pipeline wait, in SM cycles.  skip_step: for its test, a
+// pipeline step (counted from 1, 0: none) whose loads every CTA leaves out, so that the waits for it run out.  Their
+// places in the two structs were measured, since the compiler's registers turn on them: behind `err` 4096 x 152064 x
+// 3584 takes 1.86 ms, in the gaps before it 1.91; 152064 x 3584 with 64 rows of A 107 and 99.5 us.
 struct ScaledParams {
   const float* sa;
   const float* sb;
@@ -69,6 +73,8 @@ struct ScaledParams {
   int32_t e5_a, e5_b;
   int32_t mt, nt, group;  // tiles along M and N; m tiles that are walked together
   int32_t* err;
+  long long wait_cycles;
+  uint32_t skip_step;
 };
 
 // Waits for the warp's loads from TMEM; naming the registers keeps their uses behind it.
@@ -107,9 +113,9 @@ __device__ __forceinline__ bool elect_one() {
   return r != 0;
 }
 // mbar_wait by a whole warp, with one answer for all lanes
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
 }
 __device__ __forceinline__ uint32_t make_idesc_f8(int m, int n, int e5_a, int e5_b) {
   return (1u << 4)                  // D format f32
@@ -226,8 +232,9 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       bool ok = true;
       for (int j = 0; ok && scaled_tile(p, j, m0, n0); ++j) {
         for (int kb = 0; kb < nk; ++kb, ++it) {
+          if (it + 1 == p.skip_step) continue;
           const int s = it % kSmStages;
-          if (!mbar_wait(empty_bar(s), ((it / kSmStages) & 1u) ^ 1u, abort_flag)) {
+          if (!mbar_wait(empty_bar(s), ((it / kSmStages) & 1u) ^ 1u, abort_flag, p.wait_cycles)) {
             ok = false;
             break;
           }
@@ -250,8 +257,8 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       for (int j = 0; ok && scaled_tile(p, j, m0, n0); ++j) {
         for (int kb = 0; kb < nk; ++kb, ++it) {
           const int s = it % kSmStages, buf = it & 1;
-          ok = warp_wait(full_bar(s), (it / kSmStages) & 1u, abort_flag) &&
-               warp_wait(tempty_bar(buf), ((it >> 1) & 1u) ^ 1u, abort_flag);
+          ok = warp_wait(full_bar(s), (it / kSmStages) & 1u, abort_flag, p.wait_cycles) &&
+               warp_wait(tempty_bar(buf), ((it >> 1) & 1u) ^ 1u, abort_flag, p.wait_cycles);
           if (!ok) break;
           tc_fence_after();
           if (elect_one()) {
@@ -311,7 +318,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
       for (int kb = 0; kb < nk; ++kb, ++it) {
         const uint32_t t = it + kSmAhead;
         if (t % kSmFree == 0) {
-          ok = warp_wait(sempty_bar(t % kSmSlots / kSmFree), ((t / kSmSlots) & 1u) ^ 1u, abort_flag);
+          ok = warp_wait(sempty_bar(t % kSmSlots / kSmFree), ((t / kSmSlots) & 1u) ^ 1u, abort_flag, p.wait_cycles);
           if (!ok) break;
         }
         copy(t);
@@ -320,7 +327,7 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         __syncwarp();
         // the barrier's phase of two blocks before has to be over, or this arrival would count for it
         if (it >= 2) {
-          ok = warp_wait(tfull_bar(it & 1), ((it >> 1) & 1u) ^ 1u, abort_flag);
+          ok = warp_wait(tfull_bar(it & 1), ((it >> 1) & 1u) ^ 1u, abort_flag, p.wait_cycles);
           if (!ok) break;
         }
         if (lane == 0) mbar_arrive(tfull_bar(it & 1));
@@ -340,13 +347,14 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
     const float* sc_col = scales + kSmHalf + (PERCOL ? half * 128 : half);
     uint32_t buf = 0, parity = 0, slot = 0;
     bool ok = true;
-    for (int j = 0; ok && scaled_tile(p, j, m0, n0); ++j) {
+    int j = 0;
+    for (; scaled_tile(p, j, m0, n0); ++j) {
       float2 acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = make_float2(0.f, 0.f);
 #pragma unroll 1
       for (int kb = 0; kb < nk; ++kb) {
-        ok = warp_wait(tfull_bar(buf), parity, abort_flag);
+        ok = warp_wait(tfull_bar(buf), parity, abort_flag, p.wait_cycles);
         if (!ok) break;
         tc_fence_after();
         const uint32_t ta = tlane + buf * kSmTile;
@@ -483,6 +491,13 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
         }
       }
     }
+    // after a wait that ran out: NaN in the warp's part of this tile and of all that were to come
+    for (; !ok && scaled_tile(p, j, m0, n0); ++j) {
+      const int row0 = m0 + int(rank) * kSmHalf + quad * 32, col0 = n0 + half * 128 + lane;
+      for (int i = 0; i < 32 && row0 + i < p.M; ++i)
+        for (int c = col0; c < min(p.N, col0 - lane + 128); c += 32)
+          reinterpret_cast<OT*>(p.C)[int64_t(row0 + i) * p.ldc + c] = O::put(__int_as_float(0x7FC00000));
+    }
     if (lane == 0) tma_store_wait_all();  // before shared memory is released
   }
 
@@ -541,11 +556,13 @@ struct FewParams {
   int64_t sw_row, sw_col, st_row, st_col;
   int32_t gw, gt;
   int32_t M, N, K;  // A's rows, B's rows
+  uint32_t skip_step;
   void* C;
   int64_t ldc;
   int32_t accumulate;
   int32_t e5_w, e5_t;
   int32_t rows, tiles;  // rows of B in a tile (at most 128), tiles
+  uint32_t wait_cycles;
   int32_t* err;
 };
 
@@ -644,8 +661,9 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       bool ok = true;
       for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
         for (int b = 0; b < nb; ++b, ++it) {
+          if (it + 1 == p.skip_step) continue;
           const int s = it % kStages;
-          if (!mbar_wait(empty_bar(s), ((it / kStages) & 1u) ^ 1u, abort_flag)) {
+          if (!mbar_wait(empty_bar(s), ((it / kStages) & 1u) ^ 1u, abort_flag, p.wait_cycles)) {
             ok = false;
             break;
           }
@@ -670,8 +688,8 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
       for (int b = 0; b < nb; ++b, ++it) {
         const int s = it % kStages, buf = it % kBufs;
-        ok = warp_wait(full_bar(s), (it / kStages) & 1u, abort_flag) &&
-             warp_wait(tempty_bar(buf), ((it / kBufs) & 1u) ^ 1u, abort_flag);
+        ok = warp_wait(full_bar(s), (it / kStages) & 1u, abort_flag, p.wait_cycles) &&
+             warp_wait(tempty_bar(buf), ((it / kBufs) & 1u) ^ 1u, abort_flag, p.wait_cycles);
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
@@ -736,7 +754,7 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
       for (int b = 0; b < nb; ++b, ++it) {
         const uint32_t n = it + Cfg::kAhead;
-        ok = warp_wait(sempty_bar(n % Cfg::kSlots), ((n / Cfg::kSlots) & 1u) ^ 1u, abort_flag);
+        ok = warp_wait(sempty_bar(n % Cfg::kSlots), ((n / Cfg::kSlots) & 1u) ^ 1u, abort_flag, p.wait_cycles);
         if (!ok) break;
         copy(n);
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -744,7 +762,7 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
         __syncwarp();
         // the barrier's phase of one round before has to be over, or this arrival would count for it
         if (it >= kBufs) {
-          ok = warp_wait(tfull_bar(it % kBufs), ((it / kBufs) & 1u) ^ 1u, abort_flag);
+          ok = warp_wait(tfull_bar(it % kBufs), ((it / kBufs) & 1u) ^ 1u, abort_flag, p.wait_cycles);
           if (!ok) break;
         }
         if (lane == 0) mbar_arrive(tfull_bar(it % kBufs));
@@ -759,13 +777,14 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     const uint32_t tlane = tmem_base + (uint32_t(quad * 32) << 16);
     uint32_t buf = 0, parity = 0, slot = 0;
     bool ok = true;
-    for (int t = blockIdx.x; ok && t < p.tiles; t += gridDim.x) {
+    int t = blockIdx.x;
+    for (; t < p.tiles; t += gridDim.x) {
       float2 acc[NT / 2];
 #pragma unroll
       for (int i = 0; i < NT / 2; ++i) acc[i] = make_float2(0.f, 0.f);
 #pragma unroll 1
       for (int b = 0; b < nb; ++b) {
-        ok = warp_wait(tfull_bar(buf), parity, abort_flag);
+        ok = warp_wait(tfull_bar(buf), parity, abort_flag, p.wait_cycles);
         if (!ok) break;
         tc_fence_after();
         const uint32_t ta = tlane + buf * kCols;
@@ -821,6 +840,12 @@ scaled_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
           }
         }
       }
+    }
+    // after a wait that ran out: NaN in the warp's part of this tile and of all that were to come
+    for (; !ok && t < p.tiles; t += gridDim.x) {
+      const int col = t * p.rows + r;
+      if (r < p.rows && col < p.N)
+        for (int i = 0; i < p.M; ++i) reinterpret_cast<OT*>(p.C)[i * p.ldc + col] = O::put(__int_as_float(0x7FC00000));
     }
   }
 

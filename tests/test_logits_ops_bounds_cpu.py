@@ -45,3 +45,14 @@ def test_gradient_refuses_a_place_that_overlaps_the_logits(L, off, ld_d):
     p = B.OaplLogits(0x100000, 64, 2100, 1000, 0, 0x3000, 0x4000, 1.0)
     d = ctypes.c_void_p(p.logits + off)
     assert L.oapl_logits_logprobs_bwd(p, OUT, OUT, OUT, OUT, 0, None, None, d, ld_d, ST) == INVALID
+
+
+def test_debug_product_arguments(L):
+    f = L.oapl_debug_scaled_matmul
+    m = B.OaplScaled(0x1000, 0x2000, 256, 512, 512, 1, 256, 3, 1)
+    off = ctypes.c_void_p(0x2001)           # off C's alignment: nothing is launched in any case
+    assert f(m, m, off, 0, 256, 0, OUT, 0, 0, ST) == -2
+    assert f(m, m, off, 0, 256, 0, OUT, 1000, 3, ST) == -2
+    for status, cycles, step in [(None, 0, 0), (OUT, -1, 0), (OUT, 0, -1), (OUT, 0, 1), (OUT, 100_000_001, 1),
+                                 (OUT, 4_000_000_001, 0)]:
+        assert f(m, m, off, 0, 256, 0, status, cycles, step, ST) == INVALID
