@@ -368,11 +368,14 @@ typedef struct {
 /*
  * Quantise x [rows, cols] (bf16, f16 or f32; rows ld_x elements apart) into `out`:
  *   amax = max(largest |x| of the block, 2^-100), scale = amax / top (top: the type's largest value),
- *   values = x * top / amax, correctly rounded to fp32 and then to the 8-bit type (nearest even).
- * OAPL_QUANT_POW2: scale = 2^ceil(log2(amax / top)) instead.  OAPL_QUANT_TRANSPOSE: out is x turned,
- * [cols, rows], with blocks of the turned matrix.  Only rows x cols values are written, never the padding
- * behind a row.  A NaN makes its block's scale and values NaN, an infinity the scale infinite.
- * Strides of out's scales that give two blocks one place (0 over several blocks, for instance) are refused.
+ *   values = x * top / amax, correctly rounded to fp32 and then to the 8-bit type (nearest even).  top is 0.875 times
+ *   a power of two, and fp32 inputs are multiplied by 0.875 in fp32 first: a quotient within 2^-23 of the middle between
+ *   two 8-bit numbers may go to either of them.  16-bit inputs have no such rounding.
+ * OAPL_QUANT_POW2: scale = 2^ceil(log2(amax / top)) instead, values = x / scale, rounded once.
+ * OAPL_QUANT_TRANSPOSE: out is x turned, [cols, rows], with blocks of the turned matrix.
+ * Only rows x cols values are written, never the padding behind a row.  A NaN makes its block's scale and values NaN,
+ * an infinity the scale infinite.  Strides of out's scales that give two blocks one place (0 over several blocks, for
+ * instance) are refused.
  */
 #define OAPL_QUANT_TRANSPOSE 1
 #define OAPL_QUANT_POW2 2

@@ -5,9 +5,11 @@
 //   scale = amax / top                              (top = 448 for e4m3, 57344 for e5m2)
 //   q     = round((0.875 x) / (0.875 amax / top))   to the 8-bit type, nearest even
 // top is 0.875 times a power of two, so for 16-bit inputs both sides of that quotient are exact and a
-// value half way between two 8-bit numbers is seen as such.  The quotient is correctly rounded: a
-// product with the rounded reciprocal, and one residual step (Markstein's theorem on division by
-// multiply-add).  With power-of-two scales, scale = 2^ceil(log2(amax / top)) and x / scale is exact.
+// value half way between two 8-bit numbers is seen as such.  For fp32 inputs 0.875 x is rounded first, which can move a
+// quotient that lies within 2^-23 of such a value onto it or across.  The quotient is correctly rounded: a product
+// with the rounded reciprocal, and one residual step (Markstein's theorem on division by multiply-add).  With
+// power-of-two scales, scale = 2^ceil(log2(amax / top)) and the result is that of x / scale, which is exact: the
+// rounding of 0.875 x keeps the order of values and moves none onto another one of fewer than 20 bits.
 // A NaN in a block makes its scale and all its values NaN; an infinity makes the scale infinite, the
 // finite values 0 and itself NaN.
 //
