@@ -164,3 +164,37 @@ def test_gradient_between_the_rows_of_the_logits(t, first):
     want = torch.empty_like(old)
     B.oapl_logits_logprobs_bwd(B.make_logits(old, targets), lse, ent, gl, gl, None, None, want)
     assert torch.equal(d, want)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+@pytest.mark.parametrize("N,K", [(3, 0), (3, 7), (700, 0), (700, 7)])
+@pytest.mark.parametrize("offset", [0.0, 1e8])
+def test_forward_sums_of_every_variant(t, N, K, offset):
+    """CTAs of 256 and of 128 threads, whole rows and split ones, and (with the offset) the careful pass over a row."""
+    V = 50021
+    g = torch.Generator(device="cuda").manual_seed(N + K)
+    z = (torch.randn(N, V, device="cuda", generator=g) * 3).to(TYPES[t])
+    if offset:
+        step = offset * torch.finfo(z.dtype).eps          # neighbouring numbers of the type beside the offset
+        z = (offset + (z.float() / 4).round().double() * step).to(TYPES[t])
+    targets = torch.randint(0, V, (N,), device="cuda", generator=g).to(torch.int32)
+    scale = 1.0 if not offset else 0.7 / step
+    top = torch.empty(N, K, device="cuda") if K else None
+    lp, ent = torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+    B.oapl_logits_logprobs(B.make_logits(z, targets, None, scale), lp, ent, None, top)
+    s32 = float(torch.tensor(scale, dtype=torch.float32))
+    x = s32 * (z.double() - z.double().amax(1, keepdim=True))
+    ln_p = torch.log_softmax(x, 1)
+    p = ln_p.exp()
+    want, mean = -(p * ln_p).sum(1), -(p * x).sum(1)
+    at = x.gather(1, targets.long()[:, None])[:, 0].abs()
+    # A running sum takes at most V / 128 terms (128 threads, one lane per sum: the careful pass and narrow CTAs bound all
+    # others), then a tree of 13; 2^-22 of the exponential; x: a multiply-add or a difference and a product, the
+    # factor's own rounding, at a distance of `mean` on average.  ln p of the target: its distance and ln S likewise.
+    rel = (V / 128 + 13) * U + 2.0 ** -22 + 4 * U * (mean + 1)
+    assert bool(((ent.double() - want).abs() <= (2 * rel + 8 * U) * (mean + 1)).all())
+    got = ln_p.gather(1, targets.long()[:, None])[:, 0]
+    assert bool(((lp.double() - got).abs() <= rel + 4 * U * (at + got.abs() + 8)).all())
+    if K:
+        best = ln_p.sort(1, descending=True).values[:, :K]
+        assert bool(((top.double() - best).abs() <= (rel + 4 * U * (best.abs().amax(1) + 8))[:, None]).all())
