@@ -357,6 +357,31 @@ __device__ __forceinline__ RowPart row_part(const LogitsParams& p, int64_t row, 
   return q;
 }
 
+// f(x) for every logit of a row by one CTA: 16-byte loads, four under way, and single elements at both ends.
+template <typename T, int NT, typename F>
+__device__ __forceinline__ void row_each(const T* z, int V, F f) {
+  const int tid = threadIdx.x;
+  int nh = int(((16u - (uint32_t(reinterpret_cast<uintptr_t>(z)) & 15u)) & 15u) / sizeof(T));
+  if (nh > V) nh = V;
+  const int nv = (V - nh) / Elem<T>::kN, nsingle = V - nv * Elem<T>::kN;
+  const uint4* zv = reinterpret_cast<const uint4*>(z + nh);
+  for (int i0 = tid; i0 < nv; i0 += 4 * NT) {
+    uint4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i0 + u * NT < nv) v[u] = zv[i0 + u * NT];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (i0 + u * NT >= nv) break;
+      float x[Elem<T>::kN];
+      Elem<T>::widen(v[u], x);
+#pragma unroll
+      for (int e = 0; e < Elem<T>::kN; ++e) f(x[e]);
+    }
+  }
+  if (tid < nsingle) f(Elem<T>::one(z, tid < nh ? tid : nv * Elem<T>::kN + tid));
+}
+
 // A whole row by one CTA, any logits: the exact maximum m first, then x = c (z - m).  All threads get
 // {m, sum 2^x, sum 2^x x}; sh: NT / 32 entries.
 template <typename T, int NT>
@@ -364,11 +389,10 @@ __device__ __forceinline__ RowTotal row_careful(const T* z, int V, float c, RowT
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   float m = -INFINITY;
   bool nan = false;
-  for (int i = tid; i < V; i += NT) {
-    const float v = Elem<T>::one(z, i);
+  row_each<T, NT>(z, V, [&](float v) {
     nan |= v != v;
     m = fmaxf(m, v);
-  }
+  });
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   __syncthreads();
@@ -380,12 +404,12 @@ __device__ __forceinline__ RowTotal row_careful(const T* z, int V, float c, RowT
   r.m = m;
   r.s = r.t = 0.f;
   if (!nan && m > -INFINITY) {
-    for (int i = tid; i < V; i += NT) {
-      const float x = max_nan((Elem<T>::one(z, i) - m) * c, kLgFloor);
+    row_each<T, NT>(z, V, [&](float v) {
+      const float x = max_nan((v - m) * c, kLgFloor);
       const float e = ex2_approx(x);
       r.s += e;
       r.t = fmaf(e, x, r.t);
-    }
+    });
   } else if (nan) {
     r.s = __int_as_float(0x7FC00000);
   }
@@ -794,11 +818,11 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
 // ------------------------------------------------------------------------------------ backward
 // dz_v = a ( -p_v (G + g_H (ln p_v + H)) + g_lp [v = t] + sum_k g_k [v = id_k] ),  G = g_lp + sum_k g_k,
 // p_v = e^(a z_v - lse).  One read and one write per logit, HBM-bound; dz may be the logits themselves.
-// Six CTAs per SM (four: 12 % slower), five with one batch a CTA (64 x 152064 bf16 with 32 entries a row: 8.5 us, 9.0
+// Six CTAs per SM (four: 12 % slower), five with one batch a CTA (64 x 152064 bf16 with 32 entries a row: 7.8 us, 8.5
 // with six).  A CTA takes a span of a row, one batch of loads or, where there are rows enough (kMany), four, which
 // share the row's factors and the scan of its entries: these are half of the instructions otherwise, and under the
 // power limit fewer instructions are a higher clock.  4096 x 152064 bf16 in repeated calls: 382 us with four batches,
-// the copy rate; 403 us with one.  257 x 32003 fp32 with 8 entries a row: 15.4 us with one.  The few entries with a
+// the copy rate; 403 us with one.  257 x 32003 fp32 with 8 entries a row: 13.2 us with one.  The few entries with a
 // point term are written again after the CTA's stores, from logits read before them.
 struct RowGrad {
   float a, nlse;  // ln p = a z + nlse
@@ -821,16 +845,21 @@ struct RowTerms {
 __device__ __forceinline__ RowTerms row_terms(const LogitsParams& p, int64_t row) {
   const int lane = threadIdx.x & 31, K = p.K, V = p.V;
   RowTerms t;
+  // all loads first: none waits for another
   t.lse = p.lse[row];
   t.target = p.g_logp ? p.targets[row] : -1;
-  if (t.target < 0 || t.target >= V) t.target = -1;
-  t.g_target = t.target >= 0 ? p.g_logp[row] : 0.f;
-  t.id = -1;
-  t.g_id = 0.f;
-  if (lane < K) {
-    t.id = p.ids[row * K + lane];
-    if (t.id < 0 || t.id >= V) t.id = -1;
-    if (t.id >= 0) t.g_id = p.g_top[row * K + lane];
+  t.g_target = p.g_logp ? p.g_logp[row] : 0.f;
+  t.id = lane < K ? p.ids[row * K + lane] : -1;
+  t.g_id = lane < K ? p.g_top[row * K + lane] : 0.f;
+  t.ge = p.g_entropy ? p.g_entropy[row] : 0.f;
+  t.H = p.g_entropy ? p.entropy[row] : 0.f;
+  if (t.target < 0 || t.target >= V) {
+    t.target = -1;
+    t.g_target = 0.f;
+  }
+  if (t.id < 0 || t.id >= V) {
+    t.id = -1;
+    t.g_id = 0.f;
   }
   t.G = t.g_target;
   if (K) {
@@ -839,8 +868,6 @@ __device__ __forceinline__ RowTerms row_terms(const LogitsParams& p, int64_t row
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     t.G += sum;
   }
-  t.ge = p.g_entropy ? p.g_entropy[row] : 0.f;
-  t.H = p.g_entropy ? p.entropy[row] : 0.f;
   return t;
 }
 __device__ __forceinline__ RowGrad row_grad(const LogitsParams& p, const RowTerms& t, float lse) {
@@ -870,8 +897,8 @@ __device__ __forceinline__ int row_point(const RowTerms& t, int K, float& point)
 
 // Beyond this |lse| its fp32 digits do not resolve p (half a step of 1024 is 2^-14 of p; at 1e9 it is e^32).  Such a
 // row (a large common offset, or nothing but a finite mask value) is done by one CTA, which forms the maximum m and
-// the sum S again and takes ln p = a (z - m) - ln S.  It is only careful: three passes, an
-// element at a time (one row of 152064 bf16: 142 us; 4096 of them 1.98 ms, against 0.38 for other rows).
+// the sum S again and takes ln p = a (z - m) - ln S, in three passes over the row: 34 us for one of 152064 bf16, 0.77 ms
+// for 4096 of them against 0.38 for other rows.
 constexpr float kLgResolved = 1024.f;
 template <typename T>
 __device__ __forceinline__ void grad_row_apart(const LogitsParams& p, int64_t row) {
@@ -881,14 +908,45 @@ __device__ __forceinline__ void grad_row_apart(const LogitsParams& p, int64_t ro
   T* d = reinterpret_cast<T*>(p.dz) + row * p.ld_d;
   const RowTotal tot = row_careful<T, kLgThreads>(z, p.V, p.scale * 1.4426950408889634f, sh_tot);
   const bool none = tot.m == -INFINITY && tot.s == 0.f;  // not the row that this lse is of: p = 0
-  const float m = none ? 0.f : tot.m;
+  const float m = none ? 0.f : tot.m, ln_s = none ? 1e30f : logf(tot.s);
   const RowTerms t = row_terms(p, row);
-  const RowGrad r = row_grad(p, t, none ? 1e30f : logf(tot.s));
+  const RowGrad r = row_grad(p, t, ln_s);
   float point;
   const int at = row_point(t, p.K, point);
   const float z_at = at >= 0 ? E::one(z, at) : 0.f;
   __syncthreads();  // the logits at these entries have been read
-  for (int i = threadIdx.x; i < p.V; i += kLgThreads) E::put(d, i, grad_smooth(make_float2(E::one(z, i) - m, 0.f), r).x);
+  if (((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(d)) & 15) == 0) {
+    // single elements up to a 16-byte boundary and behind the last one, vectors between
+    int nh = int(((16u - (uint32_t(reinterpret_cast<uintptr_t>(d)) & 15u)) & 15u) / sizeof(T));
+    if (nh > p.V) nh = p.V;
+    const int nv = (p.V - nh) / E::kN, nsingle = p.V - nv * E::kN;
+    const uint4* zv = reinterpret_cast<const uint4*>(z + nh);
+    uint4* dv = reinterpret_cast<uint4*>(d + nh);
+    for (int i0 = threadIdx.x; i0 < nv; i0 += 2 * kLgThreads) {
+      uint4 v[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (i0 + u * kLgThreads < nv) v[u] = zv[i0 + u * kLgThreads];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (i0 + u * kLgThreads >= nv) break;
+        float f[E::kN];
+        E::widen(v[u], f);
+#pragma unroll
+        for (int e = 0; e < E::kN; e += 2) {
+          const float2 g = grad_smooth(make_float2(f[e] - m, f[e + 1] - m), r);
+          f[e] = g.x;
+          f[e + 1] = g.y;
+        }
+        dv[i0 + u * kLgThreads] = E::narrow(f);
+      }
+    }
+    const int i = int(threadIdx.x) < nh ? threadIdx.x : nv * E::kN + threadIdx.x;
+    if (int(threadIdx.x) < nsingle) E::put(d, i, grad_smooth(make_float2(E::one(z, i) - m, 0.f), r).x);
+  } else {
+    for (int i = threadIdx.x; i < p.V; i += kLgThreads)
+      E::put(d, i, grad_smooth(make_float2(E::one(z, i) - m, 0.f), r).x);
+  }
   __syncthreads();
   if (at >= 0) E::put(d, at, fmaf(r.a, point, grad_smooth(make_float2(z_at - m, 0.f), r).x));
 }
@@ -940,14 +998,12 @@ __global__ void __launch_bounds__(kLgThreads, kMany ? 6 : 5) logits_bwd_kernel(c
 
   const RowTerms t = row_terms(p, row);
   float lse = t.lse;
-  // a row without a finite logit, or with nothing but a type's lowest value as a mask: every p is 0
-  if (lse < -1e30f) {
-    lse = 1e30f;
-  } else if (fabsf(lse) > kLgResolved) {  // the same for all threads of the row
-    unsigned block;  // read anew: nothing that only these rows need is held in registers
-    asm volatile("mov.u32 %0, %%ctaid.x;" : "=r"(block));
-    if (block % unsigned(spans) == 0) grad_row_apart<T>(p, block / unsigned(spans));
-    return;
+  if (fabsf(lse) > kLgResolved) {  // the same for all threads of the row
+    if (lse >= -1e30f) {
+      if (span == 0) grad_row_apart<T>(p, row);
+      return;
+    }
+    lse = 1e30f;  // no finite logit, or nothing but a type's lowest value as a mask: every p is 0
   }
   const RowGrad r = row_grad(p, t, lse);
   float point;
