@@ -15,9 +15,11 @@
 // when a batch's maximum exceeds it by 2^8 (no rescaling in the steady state), masked logits are dealt with two
 // at a time, and sums and products are two wide.  The top alternatives cost the pass nothing but the group
 // maxima that it needs anyway: see top-K below.
-// Measured, 4096 rows of 152064 bf16 logits (1.25 GB), a single call: 189 us without alternatives, the copy rate;
-// 207 us with eight, where every row ends in a chain of short waits.  In repeated calls, at the power limit, 211
-// and 228.  One row with twenty: 8.2 us.
+// Measured, 4096 rows of 152064 bf16 logits (1.25 GB), single calls: 189 us without alternatives, the copy rate;
+// 209 us with eight, where every row ends in a chain of short waits.  Calls in a row, at the power limit: 216 and
+// 236.  One row with twenty: 8.0 us.  Rows with fewer finite logits than alternatives (constrained decoding) are read
+// twice, see top_by_lists: 4096 such rows 403 us; 64 rows of 128256 fp32 with five, 19.4 us against 10.9, and as much
+// when a hundred logits are finite, since no part of a split row then holds enough.
 //
 // A row goes to a cluster of 1, 2, 4 or 8 CTAs (few rows: the row is split and joined through
 // distributed shared memory, so a call is always a single launch without a workspace).
@@ -576,9 +578,9 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
   float tmax = p.clamp, gm = p.clamp;
   int g = 0, in_group = 0;
   uint4 cur[kLgUnroll], nxt[TOP ? kLgUnroll : 1];
-  // Whole batches of all threads need neither bounds nor a filling (4096 x 152064 bf16 in repeated calls, with and
-  // without alternatives: 228 and 211 us, 235 and 217 with one form for all); the variant for few rows has one
-  // form, since the first pass through the code is its time (64 rows of 152064: 11.3 us, 11.8 with two).
+  // Whole batches of all threads need neither bounds nor a filling (4096 x 152064 bf16 with and without alternatives,
+  // single calls 209 and 189 us, 212 and 192 with one form for all; in a row 236 and 216, 243 and 222); the variant for
+  // few rows has one form, since the first pass through the code is its time (256 rows: 22.8 us, 24.2 with two).
   constexpr bool kWhole = !TOP || NT < kLgThreads;
   const int whole = kWhole ? (q.v1 - q.v0) / (NT * kLgUnroll) : 0;
   const uint4* mine = q.zv + q.v0 + tid;
@@ -630,7 +632,7 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
     }
   };
   // Without alternatives five CTAs per SM hide each other's loads; with them, registers allow four, which load a
-  // batch ahead (4096 x 152064 bf16: 190 and 213 us; the other way round 206 and 232).
+  // batch ahead (4096 x 152064 bf16: the other way round both take 8 % more).
   if (TOP) {
 #pragma unroll 1
     for (int b = 0; b < nb; b += 2) {
@@ -821,9 +823,10 @@ __global__ void __launch_bounds__(NT, (TOP ? 1024 : 1280) / NT) logits_fwd_kerne
 // Six CTAs per SM (four: 12 % slower), five with one batch a CTA (64 x 152064 bf16 with 32 entries a row: 7.8 us, 8.5
 // with six).  A CTA takes a span of a row, one batch of loads or, where there are rows enough (kMany), four, which
 // share the row's factors and the scan of its entries: these are half of the instructions otherwise, and under the
-// power limit fewer instructions are a higher clock.  4096 x 152064 bf16 in repeated calls: 382 us with four batches,
-// the copy rate; 403 us with one.  257 x 32003 fp32 with 8 entries a row: 13.2 us with one.  The few entries with a
-// point term are written again after the CTA's stores, from logits read before them.
+// power limit fewer instructions are a higher clock.  4096 x 152064 bf16 in repeated calls: 383 us with four batches,
+// the copy rate; 404 us with one.  257 x 32003 fp32 with 8 entries a row: 13.1 us with one, 15.1 with four.  Rows of
+// the result at another offset from 16 bytes than the logits' rows are read an element at a time: 503 us against 380.
+// The few entries with a point term are written again after the CTA's stores, from logits read before them.
 struct RowGrad {
   float a, nlse;  // ln p = a z + nlse
   float A, B;     // dz = p (A ln p + B)

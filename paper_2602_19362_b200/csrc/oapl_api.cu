@@ -213,7 +213,7 @@ static bool make_map_u8(CUtensorMap* m, const void* base, uint64_t rows, uint64_
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Matrix of 2- or 4-byte elements seen through boxes of 32 rows x 64 bytes (64-byte swizzle): how the block-scaled
+// Matrix of 2- or 4-byte elements seen through boxes of 32 rows x 128 bytes (128-byte swizzle): how the block-scaled
 // product stores its result.
 static bool make_map_out(CUtensorMap* m, void* base, int32_t type, uint64_t rows, uint64_t cols, uint64_t ld) {
   EncodeTiledFn fn = encode_fn();
@@ -726,11 +726,11 @@ static int launch_logits_fwd(LogitsParams lp, int nc, cudaStream_t st) {
 }
 
 // CTAs of a row: it is split while the parts are no more than three per SM and every thread keeps a vector
-// (100 rows of 152064 bf16: 9.6 us, 12.2 with two per SM; 64 rows 7.2 us, 8.0 with four).
+// (100 rows of 152064 bf16, eight alternatives: 13.9 us, 15.0 with two per SM; 64 rows 11.4 us, 12.6 with four).
 // Many rows with alternatives go to CTAs of 128 threads, eight per SM: a row's end is a chain of short waits
 // (about 10,000 cycles on a busy SM), which weighs half as much behind a pass that takes twice as long.
-// 4096 rows of 152064: 214 us against 226; 1531 rows of 50021: 28 against 31; 256 rows, which leave SMs half
-// empty: 38 us against 27.
+// 4096 rows of 152064: 209 us against 219; 1531 rows of 50021: 39 against 43; 600 rows 45.2 against 45.9; 256 rows,
+// which leave SMs half empty: 33.5 us against 22.8.
 template <typename T>
 static int route_logits_fwd(const LogitsParams& lp, cudaStream_t st) {
   const int n_sm = sm_count();

@@ -17,8 +17,10 @@
 // between the maximum and the rounding: 8 rows x 16 bytes a thread, all loads in flight together, five CTAs
 // (16-bit types) per SM.  Maxima are taken on packed words; what rounding needs of a block is computed once
 // and shared.  Rows that do not start on a 16-byte boundary are read as the aligned 16-byte blocks that hold
-// them (a block without an element of the row is not touched) and shifted in registers.  A turned tile goes
-// through 16 KB of swizzled shared memory, so that it too leaves in 16-byte stores.
+// them (a block without an element of the row is not touched) and shifted in registers: 8192 x 3585 bf16 29.4 us,
+// 8192 x 3584 15.9; turned, 1999 x 50021 95.5 and 65 us.  A turned tile goes through 16 KB of swizzled shared memory, so
+// that it too leaves in 16-byte stores.  Five CTAs cost the form with 128 x 128 blocks five words of local memory a
+// thread, 1.3 % of its instructions (152064 x 3584 bf16: 247 us, the copy rate).
 #pragma once
 #include "logits_ops.cuh"
 

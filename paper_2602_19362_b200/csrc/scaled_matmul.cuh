@@ -12,9 +12,9 @@
 // for: an accumulator is away for about 900 cycles between the end of its MMAs and the next ones (commit, the
 // warps' wake-up, TMEM loads, hand-back), so a K block takes 725 cycles, 667 with an epilogue that does nothing.
 // Halves of 128 columns would give four accumulators, but read A twice from shared memory: slower.  Long calls
-// run at the power limit: 4096 x 152064 x 3584 in 2.05 ms (single calls; 2.16 ms repeated), 2.18 PFLOP/s at about
-// 1.4 GHz.  With a scale per column the epilogue has two operations per pair of values in place of one and 32 more
-// reads of shared memory: 1200 cycles per K block, 8192^3 716 us against 516.
+// run at the power limit: 4096 x 152064 x 3584 in 1.87 ms (single calls after a pause; 2.2 ms in a row), 2.0 to 2.4
+// PFLOP/s, in a row at about 1.4 GHz.  With a scale per column the epilogue has two operations per pair of values in place of one and 32 more
+// reads of shared memory: 1200 cycles per K block, 8192^3 621 us against 443.
 // Warp 0 issues TMA loads, warp 1 owns TMEM and (in the leader) issues the MMAs, warps 2 and 3 copy the scales
 // of rows and columns to shared memory a few K blocks ahead (cp.async).  They arrive on the accumulator's barrier
 // as the tensor cores do, so the epilogue waits once per block.  Warps 4 to 11 are the epilogue: quadrant warp & 3
@@ -49,8 +49,9 @@ constexpr size_t kSmSmemBytes = size_t(kSmStages) * kSmStageBytes + kSmSlots * k
                                 kSmOutBytes + 1024 /*align*/ + 512 /*barriers*/;
 static_assert(kSmSmemBytes <= 227 * 1024, "shared memory of a CTA");
 // Registers of a thread: 168 at launch (what 384 threads can have), then 24 for the four warps that move data
-// and 240 for the epilogue, whose loop holds 192 values: 128 * 24 + 256 * 240 = 384 * 168.  (4096 x 152064 x 3584:
-// 2.15 ms, 2.27 with 40 / 232, 2.5 with 56 / 224, where the loop spills.)
+// and 240 for the epilogue, whose loop holds 192 values: 128 * 24 + 256 * 240 = 384 * 168.  (In a row 5 % slower with
+// 40 / 232 and 16 % with 56 / 224, where the loop spills its values.  With this split the compiler still keeps some 20
+// words in local memory, of which a warp reads two per K block, 1.4 % of its instructions.)
 constexpr int kSmRegs = 168, kSmRegsLow = 24, kSmRegsHigh = 240;
 static_assert(128 * kSmRegsLow + 256 * kSmRegsHigh == kSmThreads * kSmRegs, "register split");
 
@@ -529,8 +530,9 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 // a CTA takes tiles of ceil(N / (k S)) rows, 25 of 3584 and 115 of 152064 on 148 SMs, so that a small weight keeps
 // every SM busy and a large one ends everywhere at the same time.  No pairs: one CTA per SM, all its shared memory
 // as stages of the weight stream.
-// Measured, 152064 x 3584: 82 us with 1 to 16 rows of A, the copy rate, 88 with 32 and 96 to 100 with 64 (144 to
-// 129 us with the kernel above, which is faster from 128 rows on: 137 against 146); 3584 x 3584, one row: 7.5 us,
+// Measured, 152064 x 3584: 84 to 86 us with 1 to 16 rows of A, the copy rate, 88 with 32 and 99 with 64 (131 with the
+// kernel above; 128 columns, when tried, took 146 us with 128 rows, 137 above).  64 rows of other weights, here and above:
+// 3584 x 3584 13.4 and 15.3 us, 18944 x 3584 17.3 and 20.0, 8192 x 8192 23.4 and 31.7.  3584 x 3584, one row: 7.7 us,
 // 12 with batches of one.
 constexpr int kFwRows = 128;
 constexpr int kFwEpiWarps = 4;
