@@ -46,20 +46,21 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    new = LIB + ".new"      # takes the library's place once the check has passed
+    # takes the library's place once the check has passed; each process builds one of its own
+    new = os.path.join(HERE, f".liboapl-{os.getpid()}.so")
     cmd = [nvcc, "-shared", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo", "-Xptxas", "-v",
            "-gencode", "arch=compute_100a,code=sm_100a", "-o", new]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    done = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
-    if verbose or done.returncode:
-        sys.stderr.write(done.stderr)
-    done.check_returncode()
     try:
+        done = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
+        if verbose or done.returncode:
+            sys.stderr.write(done.stderr)
+        done.check_returncode()
         check_registers(done.stderr, _split_constant())
-    except RuntimeError:
-        os.remove(new)
-        raise
-    os.replace(new, LIB)
+        os.replace(new, LIB)
+    finally:
+        if os.path.exists(new):
+            os.remove(new)
     return LIB
 
 
