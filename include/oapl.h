@@ -501,8 +501,9 @@ int oapl_debug_gemm(const void* A, const void* B, float* C, int M, int N, int K,
 
 /*
  * oapl_scaled_matmul with the two arguments of the give-up path's test, as above: wait_cycles > 0 (at most 4e9, the
- * product limit) replaces the limit of every pipeline wait, and skip_step = k > 0 (with 0 < wait_cycles <= 1e8) leaves out the loads of every CTA's
- * pipeline step k - 1: a block of 128 of K, for at most 64 rows of A two or four of them.  device_status is needed.
+ * product limit) replaces the limit of every pipeline wait, and skip_step = k > 0 (with 0 < wait_cycles <= 1e8) leaves
+ * out the loads of every CTA's pipeline step k - 1: a block of 128 of K, for at most 64 rows of A two or four of them.
+ * device_status is needed.
  */
 int oapl_debug_scaled_matmul(const oapl_scaled* A /*host*/, const oapl_scaled* B /*host*/, void* C, int32_t c_type,
                              int64_t ldc, int accumulate, int32_t* device_status, long long wait_cycles,

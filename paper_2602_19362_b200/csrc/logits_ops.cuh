@@ -4,11 +4,11 @@
 // Forward, one pass over a row (z: the row's logits, a: the caller's factor):
 //     x_v = a log2(e) z_v - R,  S = sum_v 2^x_v,  T = sum_v 2^x_v x_v      (R: a reference near the maximum)
 //     lse = R ln 2 + ln S,   ln p_t = x_t ln 2 - ln S,   entropy = ln S - ln 2 T / S.
-// The entropy is formed from sums relative to R.  R is a logit of the row at most 2^8 below the maximum: where it
-// is k bits below, the row holds a second logit of 2^-k and an entropy to match, and where the maximum stands alone
-// R is the maximum and neither ln S nor ln 2 T / S is large.  What is left is an absolute error of a few 2^-24 (two
-// logits 0.5 to 40 bits apart: at most 1.2e-7), so an entropy below about 1e-6 keeps no digits.  Sums are fp32: a
-// thread adds up to V / 256 terms to each of two lanes, the rest are trees.
+// The entropy is formed from sums relative to R.  R is a logit of the row, at most 8 bits below the maximum: where it
+// is k bits below, the row holds a second logit with 2^-k of the largest one's weight and an entropy to match, and
+// where the maximum stands alone R is the maximum and neither ln S nor ln 2 T / S is large.  What is left is an
+// absolute error of a few 2^-24 (two logits 0.5 to 40 bits apart: at most 1.2e-7), so an entropy below about 1e-6 keeps
+// no digits.  Sums are fp32: a thread adds up to V / 256 terms to each of two lanes, the rest are trees.
 //
 // What bounds it: HBM.  At the copy rate an SM has to take 11.5 16-bit logits a cycle and can issue 128 lane
 // instructions, 16 of them exponentials; the pass takes about seven per logit.  So the reference R is moved only
@@ -955,7 +955,8 @@ __device__ __forceinline__ void grad_row_apart(const LogitsParams& p, int64_t ro
 }
 
 template <typename T, bool kMany>
-__global__ void __launch_bounds__(kLgThreads, kMany ? 6 : 5) logits_bwd_kernel(const __grid_constant__ LogitsParams p, int spans) {
+__global__ void __launch_bounds__(kLgThreads, kMany ? 6 : 5)
+logits_bwd_kernel(const __grid_constant__ LogitsParams p, int spans) {
   using E = Elem<T>;
   constexpr int kN = E::kN;
   const int tid = threadIdx.x;

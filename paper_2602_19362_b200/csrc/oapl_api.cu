@@ -904,7 +904,8 @@ static int scaled_few(const oapl_scaled* A, const oapl_scaled* B, void* C, int32
 }
 
 static int scaled_product(const oapl_scaled* A, const oapl_scaled* B, void* C, int32_t c_type, int64_t ldc,
-                          int accumulate, int32_t* device_status, uint32_t wait_cycles, uint32_t skip_step, void* stream) {
+                          int accumulate, int32_t* device_status, uint32_t wait_cycles, uint32_t skip_step,
+                          void* stream) {
   int rc = check_scaled(A);
   if (rc == OAPL_OK) rc = check_scaled(B);
   if (rc != OAPL_OK) return rc;

@@ -11,10 +11,10 @@
 // tensor cores 512 cycles per pair.  What bounds it is the hand-over of the two accumulators that TMEM has room
 // for: an accumulator is away for about 900 cycles between the end of its MMAs and the next ones (commit, the
 // warps' wake-up, TMEM loads, hand-back), so a K block takes 725 cycles, 667 with an epilogue that does nothing.
-// Halves of 128 columns would give four accumulators, but read A twice from shared memory: slower.  Long calls
-// run at the power limit: 4096 x 152064 x 3584 in 1.87 ms (single calls after a pause; 2.2 ms in a row), 2.0 to 2.4
-// PFLOP/s, in a row at about 1.4 GHz.  With a scale per column the epilogue has two operations per pair of values in place of one and 32 more
-// reads of shared memory: 1200 cycles per K block, 8192^3 621 us against 443.
+// Halves of 128 columns would give four accumulators, but read A twice from shared memory: slower.  Long calls run at
+// the power limit: 4096 x 152064 x 3584 in 1.87 ms (single calls after a pause; 2.2 ms in a row), 2.0 to 2.4 PFLOP/s, in
+// a row at about 1.4 GHz.  With a scale per column the epilogue has two operations per pair of values in place of one
+// and 32 more reads of shared memory: 1200 cycles per K block, 8192^3 621 us against 443.
 // Warp 0 issues TMA loads, warp 1 owns TMEM and (in the leader) issues the MMAs, warps 2 and 3 copy the scales
 // of rows and columns to shared memory a few K blocks ahead (cp.async).  They arrive on the accumulator's barrier
 // as the tensor cores do, so the epilogue waits once per block.  Warps 4 to 11 are the epilogue: quadrant warp & 3
@@ -531,9 +531,9 @@ scaled_matmul_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_const
 // every SM busy and a large one ends everywhere at the same time.  No pairs: one CTA per SM, all its shared memory
 // as stages of the weight stream.
 // Measured, 152064 x 3584: 84 to 86 us with 1 to 16 rows of A, the copy rate, 88 with 32 and 99 with 64 (131 with the
-// kernel above; 128 columns, when tried, took 146 us with 128 rows, 137 above).  64 rows of other weights, here and above:
-// 3584 x 3584 13.4 and 15.3 us, 18944 x 3584 17.3 and 20.0, 8192 x 8192 23.4 and 31.7.  3584 x 3584, one row: 7.7 us,
-// 12 with batches of one.
+// kernel above; 128 columns, when tried, took 146 us with 128 rows, 137 above).  64 rows of other weights, here and
+// above: 3584 x 3584 13.4 and 15.3 us, 18944 x 3584 17.3 and 20.0, 8192 x 8192 23.4 and 31.7.  3584 x 3584, one row:
+// 7.7 us, 12 with batches of one.
 constexpr int kFwRows = 128;
 constexpr int kFwEpiWarps = 4;
 constexpr int kFwThreads = 32 * (4 + kFwEpiWarps);
