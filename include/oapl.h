@@ -396,6 +396,172 @@ int oapl_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int
 int oapl_scaled_matmul(const oapl_scaled* A /*host*/, const oapl_scaled* B /*host*/, void* C, int32_t c_type,
                        int64_t ldc, int accumulate, int32_t* device_status, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * The two sides of the LM head in a model that trains: the embedding (whose table is the head's W where the two are
+ * tied), the norms around a block, the last of which makes H, and the gradient norm over all parameters.  With tied
+ * weights a step is oapl_embedding, the blocks with oapl_residual_norm, oapl_loss_fwd_bwd, oapl_residual_norm_bwd,
+ * oapl_embedding_bwd with accumulate into dW, oapl_grad_norm over dW and the rest, oapl_adamw_step.
+ * Matrices are row-major with rows ld elements apart and need only the natural alignment of their type; rows that start on
+ * 16-byte boundaries are faster.  Results are the same in every run on one kind of GPU.  device_status as above.
+ * ------------------------------------------------------------------------------------------ */
+
+/* N token ids of a vocabulary of V. */
+typedef struct {
+  const int32_t* ids;  /* [N]; in [0,V) where mask==1                                        */
+  const uint8_t* mask; /* [N] or NULL (all rows count); ids of rows with mask==0 are not read */
+  int64_t N;
+  int32_t V;
+  float scale;         /* finite; a scaled embedding's factor, otherwise 1                   */
+} oapl_lookup;
+
+/*
+ * out[n] = scale * table[ids[n]], rounded once; table [V,d] and out [N,d] of any of the three types.  Rows with mask==0
+ * become 0.  An id outside [0,V) on a row that counts: 0, status OAPL_ERR_BAD_TARGET.  out does not overlap the table.
+ */
+int oapl_embedding(const oapl_lookup* lookup /*host*/, const void* table, int32_t table_type, int64_t ld_table, int32_t d,
+                   void* out, int32_t out_type, int64_t ld_out, int32_t* device_status, void* stream);
+
+/*
+ * dtable[v] = scale * sum of dout[n] over the rows with ids[n] == v that count, or that added to dtable when
+ * accumulate != 0 (rows of dtable without such a row are then not touched; they become 0 otherwise).
+ * dout [N,d] bf16, f16 or f32; dtable [V,d] f32, apart from dout.  Sums are fp32, in the order of the rows, cut into
+ * stretches of a batch.  An id outside [0,V) on a row that counts adds nothing and sets OAPL_ERR_BAD_TARGET.
+ * N <= 2e9, d <= 2e9.  ws: oapl_embedding_workspace_bytes(N, V, d) bytes (0 for sizes that are refused), 16-byte aligned.
+ */
+size_t oapl_embedding_workspace_bytes(int64_t N, int32_t V, int32_t d);
+int oapl_embedding_bwd(const oapl_lookup* lookup /*host*/, const void* dout, int32_t type, int64_t ld_dout, int32_t d,
+                       float* dtable, int64_t ld_dtable, int accumulate, int32_t* device_status, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/* kinds of a gate */
+#define OAPL_GATE_NONE 0
+#define OAPL_GATE_ROW 1    /* one factor per row: [N], ld_gate elements apart                     */
+#define OAPL_GATE_COLUMN 2 /* one per channel: [d]                                                */
+#define OAPL_GATE_FULL 3   /* [N,d], of the rows' type, rows ld_gate elements apart               */
+
+/*
+ * The end of a block with result y on the residual stream x, and the norm before what follows:
+ *   u = w_post * y / rms(y) (u = y without w_post),   x' = residual_scale * x + branch_scale * gate * u,
+ *   h = w_pre * x' / rms(x'),                         rms(v) = sqrt(mean v^2 + eps).
+ * Without y: x' = residual_scale * x, the norm alone.  A weight counts as weight + weight_offset (1 where a model stores
+ * the difference from 1).
+ */
+typedef struct {
+  int64_t N;
+  int32_t d;               /* 1 .. 16384                                                          */
+  int32_t type;            /* of x, y, a full gate and all matrices below                         */
+  const void* x;           /* [N,d]                                                               */
+  int64_t ld_x;
+  const void* y;           /* [N,d] or NULL                                                       */
+  int64_t ld_y;
+  const void* gate;        /* NULL with OAPL_GATE_NONE; otherwise needs y                         */
+  int64_t ld_gate;         /* row and full gates                                                  */
+  int32_t gate_kind;
+  int32_t gate_type;       /* any of the three types; a full gate: the rows' type                 */
+  const void* w_post;      /* [d] or NULL: no norm of y.  Needs y                                 */
+  const void* w_pre;       /* [d] or NULL: no norm of x'                                          */
+  int32_t weight_type;
+  float weight_offset;
+  float eps;               /* >= 0, finite                                                        */
+  float residual_scale;    /* finite                                                              */
+  float branch_scale;      /* finite                                                              */
+} oapl_residual;
+
+/*
+ * Forward.  x_out [N,d]: x', or NULL; h [N,d]: with w_pre, NULL without; rstd_post [N], rstd_pre [N] f32 or NULL:
+ * 1 / rms of y and of x' (with w_post, w_pre), which the gradient reads.  h and the statistics are formed from x' in
+ * fp32, before it is rounded to its type.  x_out and h may each lie exactly over x, y or a full gate (the same rows);
+ * other overlaps are refused.
+ */
+int oapl_residual_norm(const oapl_residual* residual /*host*/, void* x_out, int64_t ld_x_out, void* h, int64_t ld_h,
+                       float* rstd_post, float* rstd_pre, void* stream);
+
+/*
+ * Gradient.  x_out (with w_pre), rstd_post (with w_post), rstd_pre (with w_pre): as the forward left them; x is not read
+ * and may be NULL.  dh [N,d] (with w_pre) and dx_out [N,d] or NULL (0; needed without w_pre): the gradients of h and x'.
+ *   dx [N,d], dy [N,d] (with y), or NULL; they may each lie exactly over x_out, dh, dx_out, y or a full gate;
+ *   dgate or NULL: a row gate's [N] f32, ld_dgate elements apart; a channel gate's [d] f32; a full gate's [N,d], like dy;
+ *   dw_post, dw_pre [d] f32 or NULL.
+ * accumulate != 0: dw_post, dw_pre and a channel gate's dgate are added to what is there.
+ * ws: oapl_residual_norm_workspace_bytes(N, d) bytes, 16-byte aligned; needed where one of those three sums is asked for.
+ */
+size_t oapl_residual_norm_workspace_bytes(int64_t N, int32_t d);
+int oapl_residual_norm_bwd(const oapl_residual* residual /*host*/, const void* x_out, int64_t ld_x_out,
+                           const float* rstd_post, const float* rstd_pre, const void* dh, int64_t ld_dh,
+                           const void* dx_out, int64_t ld_dx_out, void* dx, int64_t ld_dx, void* dy, int64_t ld_dy,
+                           void* dgate, int64_t ld_dgate, float* dw_post, float* dw_pre, int accumulate, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* One tensor of a list: n elements in a row. */
+typedef struct {
+  const void* data;  /* bf16, f16 or f32, natural alignment (16-byte alignment of data and out is faster) */
+  void* out;         /* where the scaled elements go: data itself, memory of its own, or NULL for the norm alone */
+  int64_t n;         /* >= 0; a tensor of none is passed over                                         */
+  int32_t type;
+  int32_t out_type;  /* type where out is data                                                       */
+} oapl_tensor;
+
+/*
+ * sq_norm [1] f32 = sum of (scale * g)^2 over all elements of the list, norm [1] f32 its square root; one of them may be
+ * NULL.  Sums are fp64, so norm is right where sq_norm leaves the range of fp32.  A norm that is not finite:
+ * OAPL_ERR_NONFINITE_INPUT.  The list is read during the call only.  ws: oapl_grad_norm_workspace_bytes(count) bytes,
+ * 16-byte aligned.  sq_norm is what oapl_adamw_step takes as other_sq_norm.
+ */
+size_t oapl_grad_norm_workspace_bytes(int32_t count);
+int oapl_grad_norm(const oapl_tensor* tensors /*host*/, int32_t count, float scale, float* sq_norm, float* norm,
+                   int32_t* device_status, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * out = g * scale * min(1, clip_norm / (sqrt(*sq_norm) + 1e-6)) for every tensor of the list, rounded once.  sq_norm: of
+ * oapl_grad_norm with the same scale, or such a sum over several ranks.  Where it is not finite the factor is scale
+ * alone: the caller leaves out the step.  Elements that the factor 1 would leave in place are not read.
+ * No out overlaps a tensor other than its own.
+ */
+int oapl_grad_clip(const oapl_tensor* tensors /*host*/, int32_t count, float scale, const float* sq_norm,
+                   float clip_norm, void* stream);
+
+/*
+ * What a sampler does to logits before it samples, which a trainer that re-scores its tokens has to repeat.  For a token v
+ * of row n, c: how often it is in the row's answer, seen: whether it is in the row's prompt or answer,
+ *   z1 = seen ? (z > 0 ? z / repetition : z * repetition) : z,
+ *   z2 = z1 - frequency * c - presence * [c > 0],   z3 = z2 + the sum of its biases,   result = allowed ? z3 : -inf.
+ */
+typedef struct {
+  const int32_t* tokens;    /* [T] or NULL: token ids of all rows' prompts and answers; ids outside [0,V) count for nothing */
+  int64_t T;
+  const int64_t* spans;     /* [N,3], with tokens: row n's prompt is tokens[s0 .. s1), its answer tokens[s1 .. s2);
+                               rows may share tokens.  At most 2^30 - 1 tokens in an answer                             */
+  const float* repetition;  /* [N] or NULL: > 0                                                                         */
+  const float* frequency;   /* [N] or NULL                                                                              */
+  const float* presence;    /* [N] or NULL                                                                              */
+  const int64_t* bias_start;/* [N+1] or NULL: row n's biases are entries bias_start[n] .. bias_start[n+1) of the next two */
+  const int32_t* bias_id;   /* [biases]; an id may occur several times in a row, ids outside [0,V) count for nothing     */
+  const float* bias;        /* [biases]                                                                                 */
+  int64_t biases;
+  const uint32_t* allowed;  /* [allowed_rows, ld_allowed] or NULL: token v is allowed where bit v % 32 of word v / 32 is set */
+  int64_t ld_allowed;       /* >= ceil(V / 32), words                                                                   */
+  int64_t allowed_rows;
+  const int32_t* allowed_row; /* [N] or NULL (row n of allowed, which then has N rows): a row of allowed; negative: all tokens */
+} oapl_adjust;
+
+/*
+ * out [N,V], the logits' type, rows ld_out elements apart: the logits' own memory (then ld_out == ld, and only what
+ * changes is touched) or memory apart.  Rows with the logits' mask==0 are neither read nor written; targets and scale of
+ * `logits` are not used.  Unchanged logits keep their bits.  Spans that decrease or leave [0,T], biases that leave
+ * [0,biases]: none for that row, status OAPL_ERR_BAD_SEQ_ORDER; an allowed_row past allowed_rows: no mask for that row,
+ * OAPL_ERR_BAD_TARGET.
+ */
+int oapl_logits_adjust(const oapl_logits* logits /*host*/, const oapl_adjust* adjust /*host*/, void* out, int64_t ld_out,
+                       int32_t* device_status, void* stream);
+
+/*
+ * Gradient: dlogits_v = allowed ? (seen ? (z > 0 ? d_out / repetition : d_out * repetition) : d_out) : 0.  `logits`: as
+ * they were before the adjustment (read only at tokens that are seen).  d_out, dlogits [N,V] of the logits' type; dlogits
+ * may lie exactly over d_out or the logits.  Rows with mask==0 are written as 0.
+ */
+int oapl_logits_adjust_bwd(const oapl_logits* logits /*host*/, const oapl_adjust* adjust /*host*/, const void* d_out,
+                           int64_t ld_d_out, void* dlogits, int64_t ld_dlogits, int32_t* device_status, void* stream);
+
 /* Synchronises `stream` and returns the status word the device recorded in `ws`
  * since the last forward call (OAPL_OK if none). */
 int oapl_get_last_status(void* ws, void* stream);

@@ -27,7 +27,10 @@ EXPORTS = ["oapl_workspace_bytes", "oapl_token_logprobs", "oapl_value_estimate",
            "oapl_grpo_loss_fwd_bwd", "oapl_adamw_workspace_bytes", "oapl_adamw_step", "oapl_loss_fwd_bwd_ex",
            "oapl_get_range_count", "oapl_profile_applies", "oapl_range_slots", "oapl_batch_stats",
            "oapl_logits_logprobs", "oapl_logits_logprobs_bwd", "oapl_quantize", "oapl_scaled_matmul",
-           "oapl_debug_scaled_matmul"]
+           "oapl_debug_scaled_matmul", "oapl_embedding", "oapl_embedding_workspace_bytes", "oapl_embedding_bwd",
+           "oapl_residual_norm", "oapl_residual_norm_workspace_bytes", "oapl_residual_norm_bwd",
+           "oapl_grad_norm_workspace_bytes", "oapl_grad_norm", "oapl_grad_clip", "oapl_logits_adjust",
+           "oapl_logits_adjust_bwd"]
 
 
 class OaplProblem(ctypes.Structure):
@@ -54,6 +57,33 @@ class OaplScaled(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64),
                 ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("scale_row_stride", ctypes.c_int64),
                 ("scale_col_stride", ctypes.c_int64), ("type", ctypes.c_int32), ("block_rows", ctypes.c_int32)]
+
+
+class OaplLookup(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("N", ctypes.c_int64), ("V", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class OaplResidual(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("d", ctypes.c_int32), ("type", ctypes.c_int32), ("x", ctypes.c_void_p),
+                ("ld_x", ctypes.c_int64), ("y", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("gate", ctypes.c_void_p),
+                ("ld_gate", ctypes.c_int64), ("gate_kind", ctypes.c_int32), ("gate_type", ctypes.c_int32),
+                ("w_post", ctypes.c_void_p), ("w_pre", ctypes.c_void_p), ("weight_type", ctypes.c_int32),
+                ("weight_offset", ctypes.c_float), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("branch_scale", ctypes.c_float)]
+
+
+class OaplTensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("out_type", ctypes.c_int32)]
+
+
+class OaplAdjust(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("T", ctypes.c_int64), ("spans", ctypes.c_void_p),
+                ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                ("bias_start", ctypes.c_void_p), ("bias_id", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("biases", ctypes.c_int64), ("allowed", ctypes.c_void_p), ("ld_allowed", ctypes.c_int64),
+                ("allowed_rows", ctypes.c_int64), ("allowed_row", ctypes.c_void_p)]
 
 
 class OaplError(RuntimeError):
@@ -131,6 +161,31 @@ def lib() -> ctypes.CDLL:
         L.oapl_scaled_matmul.argtypes = [ps, ps, vp, ctypes.c_int32, i64, i32, vp, vp]
         L.oapl_debug_scaled_matmul.restype = i32
         L.oapl_debug_scaled_matmul.argtypes = [ps, ps, vp, ctypes.c_int32, i64, i32, vp, ctypes.c_longlong, i32, vp]
+        pk, pr, pt, pa = (ctypes.POINTER(t) for t in (OaplLookup, OaplResidual, OaplTensor, OaplAdjust))
+        c32 = ctypes.c_int32
+        L.oapl_embedding.restype = i32
+        L.oapl_embedding.argtypes = [pk, vp, c32, i64, c32, vp, c32, i64, vp, vp]
+        L.oapl_embedding_workspace_bytes.restype = sz
+        L.oapl_embedding_workspace_bytes.argtypes = [i64, c32, c32]
+        L.oapl_embedding_bwd.restype = i32
+        L.oapl_embedding_bwd.argtypes = [pk, vp, c32, i64, c32, vp, i64, i32, vp, vp, sz, vp]
+        L.oapl_residual_norm.restype = i32
+        L.oapl_residual_norm.argtypes = [pr, vp, i64, vp, i64, vp, vp, vp]
+        L.oapl_residual_norm_workspace_bytes.restype = sz
+        L.oapl_residual_norm_workspace_bytes.argtypes = [i64, c32]
+        L.oapl_residual_norm_bwd.restype = i32
+        L.oapl_residual_norm_bwd.argtypes = [pr, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp,
+                                             i32, vp, sz, vp]
+        L.oapl_grad_norm_workspace_bytes.restype = sz
+        L.oapl_grad_norm_workspace_bytes.argtypes = [c32]
+        L.oapl_grad_norm.restype = i32
+        L.oapl_grad_norm.argtypes = [pt, c32, f32, vp, vp, vp, vp, sz, vp]
+        L.oapl_grad_clip.restype = i32
+        L.oapl_grad_clip.argtypes = [pt, c32, f32, vp, f32, vp]
+        L.oapl_logits_adjust.restype = i32
+        L.oapl_logits_adjust.argtypes = [pl, pa, vp, i64, vp, vp]
+        L.oapl_logits_adjust_bwd.restype = i32
+        L.oapl_logits_adjust_bwd.argtypes = [pl, pa, vp, i64, vp, i64, vp, vp]
         L.oapl_profile_enable.restype = i32
         L.oapl_profile_enable.argtypes = [i32]
         L.oapl_profile_read.restype = i32
@@ -508,3 +563,251 @@ def oapl_debug_scaled_matmul(A: OaplScaled, B: OaplScaled, C, device_status, acc
                                         int(skip_step), _stream_of(C.get_device()))
     if rc != OAPL_OK:
         raise OaplError(rc, "oapl_debug_scaled_matmul")
+
+
+# ---- the embedding, the norms around a block, the gradient norm, adjustments of logits ---------------------
+
+OAPL_GATE_NONE, OAPL_GATE_ROW, OAPL_GATE_COLUMN, OAPL_GATE_FULL = 0, 1, 2, 3
+
+
+def _ws(ws, device):
+    """Address and size of a workspace: a contiguous uint8 tensor of that device, or None."""
+    if ws is None:
+        return None, 0
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.get_device() != device:
+        raise TypeError(f"ws: expected a contiguous uint8 tensor on cuda:{device}")
+    return ws.data_ptr(), ws.numel()
+
+
+def make_lookup(ids, V: int, mask=None, scale: float = 1.0) -> OaplLookup:
+    """Fill oapl_lookup.  ids: int32 [N]; mask: uint8 [N].  The struct keeps the tensors alive."""
+    if not ids.is_cuda or ids.dim() != 1:
+        raise TypeError("ids: expected a 1-D CUDA tensor")
+    dev, N = ids.get_device(), ids.shape[0]
+    k = OaplLookup(_vec(ids, torch.int32, (N,), dev, "ids"), _vec(mask, torch.uint8, (N,), dev, "mask"), N, V, scale)
+    k.tensors, k.device = (ids, mask), dev
+    return k
+
+
+def oapl_embedding(k: OaplLookup, table, out, device_status=None):
+    """out [N, d] = scale * table[ids]; table [V, d]; each bf16, fp16 or fp32, rows any stride apart."""
+    dev = k.device
+    ct, V, d, ld_t = _rows(table, FLOAT_TYPES, "table")
+    co, N, do, ld_o = _rows(out, FLOAT_TYPES, "out")
+    if V != k.V or N != k.N or d != do or table.get_device() != dev or out.get_device() != dev:
+        raise TypeError(f"table, out: expected shapes {(k.V, d)} and {(k.N, d)} on cuda:{dev}")
+    rc = lib().oapl_embedding(k, table.data_ptr(), ct, ld_t, d, out.data_ptr(), co, ld_o,
+                              _vec(device_status, torch.int32, (1,), dev, "device_status"), _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_embedding")
+
+
+def oapl_embedding_workspace_bytes(N: int, V: int, d: int) -> int:
+    return int(lib().oapl_embedding_workspace_bytes(N, V, d))
+
+
+def oapl_embedding_bwd(k: OaplLookup, dout, dtable, accumulate: bool, ws, device_status=None):
+    """dtable [V, d] fp32 = (or +=) scale * the rows of dout [N, d] added up by token.  ws: uint8,
+    oapl_embedding_workspace_bytes(N, V, d)."""
+    dev = k.device
+    ct, N, d, ld = _rows(dout, FLOAT_TYPES, "dout")
+    c32, V, dt, ld_t = _rows(dtable, FLOAT_TYPES, "dtable")
+    if V != k.V or N != k.N or d != dt or c32 != 2 or dout.get_device() != dev or dtable.get_device() != dev:
+        raise TypeError(f"dout, dtable: expected shapes {(k.N, d)} and {(k.V, d)}, the latter fp32, on cuda:{dev}")
+    at, size = _ws(ws, dev)
+    rc = lib().oapl_embedding_bwd(k, dout.data_ptr(), ct, ld, d, dtable.data_ptr(), ld_t, int(accumulate),
+                                  _vec(device_status, torch.int32, (1,), dev, "device_status"), at, size, _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_embedding_bwd")
+
+
+def make_residual(x, y=None, gate=None, w_post=None, w_pre=None, eps: float = 1e-6, residual_scale: float = 1.0,
+                  branch_scale: float = 1.0, weight_offset: float = 0.0) -> OaplResidual:
+    """Fill oapl_residual.  x, y: [N, d] of one type; gate: [N, 1] a factor per row, [d] one per channel, [N, d] one per
+    element (of x's type); w_post, w_pre: [d] of one type.  The struct keeps the tensors alive."""
+    code, N, d, ld_x = _rows(x, FLOAT_TYPES, "x")
+    dev, ld_y, at_y = x.get_device(), 0, None
+    if y is not None:
+        cy, ny, dy, ld_y = _rows(y, FLOAT_TYPES, "y")
+        if cy != code or ny != N or dy != d or y.get_device() != dev:
+            raise TypeError("y: expected x's type, shape and device")
+        at_y = y.data_ptr()
+    kind = gate_type = ld_gate = 0
+    at_gate = None
+    if gate is not None:
+        gate_type = FLOAT_TYPES.get(gate.dtype)
+        if gate_type is None or gate.get_device() != dev:
+            raise TypeError("gate: expected bf16, fp16 or fp32 on x's device")
+        if gate.dim() == 1 and gate.shape[0] == d and gate.is_contiguous():
+            kind = OAPL_GATE_COLUMN
+        elif gate.dim() == 2 and gate.shape == (N, d) and (d > 1 or gate_type == code):
+            kind, ld_gate = OAPL_GATE_FULL, _rows(gate, {x.dtype: code}, "gate")[3]
+        elif gate.dim() == 2 and gate.shape == (N, 1):
+            kind, ld_gate = OAPL_GATE_ROW, (gate.stride(0) if N > 1 else 1)
+        else:
+            raise TypeError("gate: expected [N, 1], a contiguous [d], or [N, d]")
+        at_gate = gate.data_ptr()
+    weight = w_pre if w_pre is not None else w_post
+    weight_type = 0
+    if weight is not None:
+        weight_type = FLOAT_TYPES.get(weight.dtype)
+        if weight_type is None:
+            raise TypeError("w_post, w_pre: expected bf16, fp16 or fp32")
+    r = OaplResidual(N, d, code, x.data_ptr(), ld_x, at_y, ld_y, at_gate, ld_gate, kind, gate_type,
+                     None if w_post is None else _vec(w_post, weight.dtype, (d,), dev, "w_post"),
+                     None if w_pre is None else _vec(w_pre, weight.dtype, (d,), dev, "w_pre"), weight_type, weight_offset,
+                     eps, residual_scale, branch_scale)
+    r.tensors, r.device = (x, y, gate, w_post, w_pre), dev
+    return r
+
+
+def _like(r, t, name):
+    """Address and leading dimension of a matrix of the residual's type, shape and device; None and 0 for None."""
+    if t is None:
+        return None, 0
+    code, N, d, ld = _rows(t, FLOAT_TYPES, name)
+    if code != r.type or N != r.N or d != r.d or t.get_device() != r.device:
+        raise TypeError(f"{name}: expected x's type, shape and device")
+    return t.data_ptr(), ld
+
+
+def oapl_residual_norm(r: OaplResidual, x_out, h=None, rstd_post=None, rstd_pre=None):
+    """x_out [N, d] = residual_scale x + branch_scale gate norm(y), h [N, d] = norm(x_out); rstd_post, rstd_pre: fp32
+    [N], what the gradient reads.  x_out and h may be x, y or a full gate."""
+    dev, N = r.device, r.N
+    f32 = torch.float32
+    rc = lib().oapl_residual_norm(r, *_like(r, x_out, "x_out"), *_like(r, h, "h"),
+                                  _vec(rstd_post, f32, (N,), dev, "rstd_post"), _vec(rstd_pre, f32, (N,), dev, "rstd_pre"),
+                                  _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_residual_norm")
+
+
+def oapl_residual_norm_workspace_bytes(N: int, d: int) -> int:
+    return int(lib().oapl_residual_norm_workspace_bytes(N, d))
+
+
+def oapl_residual_norm_bwd(r: OaplResidual, x_out, rstd_post, rstd_pre, dh, dx_out, dx=None, dy=None, dgate=None,
+                           dw_post=None, dw_pre=None, accumulate: bool = False, ws=None):
+    """Gradients of x, y, the gate and the weights from dh and dx_out (None: 0).  dgate: fp32 [N, 1] or [d], or [N, d]
+    like y.  ws: uint8, oapl_residual_norm_workspace_bytes(N, d), for dw_post, dw_pre and a channel gate's dgate."""
+    dev, N, d = r.device, r.N, r.d
+    f32 = torch.float32
+    at_dg, ld_dg = None, 0
+    if dgate is not None:
+        if r.gate_kind == OAPL_GATE_FULL:
+            at_dg, ld_dg = _like(r, dgate, "dgate")
+        elif r.gate_kind == OAPL_GATE_ROW:
+            if dgate.dtype != f32 or dgate.shape != (N, 1) or dgate.get_device() != dev:
+                raise TypeError(f"dgate: expected fp32 {(N, 1)} on cuda:{dev}")
+            at_dg, ld_dg = dgate.data_ptr(), dgate.stride(0) if N > 1 else 1
+        else:
+            at_dg = _vec(dgate, f32, (d,), dev, "dgate")
+    rc = lib().oapl_residual_norm_bwd(
+        r, *_like(r, x_out, "x_out"), _vec(rstd_post, f32, (N,), dev, "rstd_post"),
+        _vec(rstd_pre, f32, (N,), dev, "rstd_pre"), *_like(r, dh, "dh"), *_like(r, dx_out, "dx_out"), *_like(r, dx, "dx"),
+        *_like(r, dy, "dy"), at_dg, ld_dg, _vec(dw_post, f32, (d,), dev, "dw_post"), _vec(dw_pre, f32, (d,), dev, "dw_pre"),
+        int(accumulate), *_ws(ws, dev), _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_residual_norm_bwd")
+
+
+class TensorList:
+    """A host array of oapl_tensor for the tensors of a model, which it keeps alive.  Made once for gradients that keep
+    their memory."""
+
+    def __init__(self, tensors, outs=None):
+        if not tensors:
+            raise ValueError("tensors: expected at least one")
+        if outs is not None and len(outs) != len(tensors):
+            raise ValueError("outs: expected one for each tensor")
+        self.device = tensors[0].get_device()
+        self.array = (OaplTensor * len(tensors))()
+        for t, o, e in zip(tensors, tensors if outs is None else outs, self.array):
+            for x in (t, o):
+                if x.dtype not in FLOAT_TYPES or not x.is_cuda or not x.is_contiguous() or x.get_device() != self.device:
+                    raise TypeError("tensors, outs: expected contiguous CUDA tensors of bf16, fp16 or fp32 on one device")
+            if t.numel() != o.numel():
+                raise TypeError("outs: expected as many elements as the tensor has")
+            e.data, e.out, e.n = t.data_ptr(), o.data_ptr(), t.numel()
+            e.type, e.out_type = FLOAT_TYPES[t.dtype], FLOAT_TYPES[o.dtype]
+        self.count, self.tensors = len(tensors), (list(tensors), None if outs is None else list(outs))
+
+
+def make_tensor_list(tensors, outs=None) -> TensorList:
+    """The list that oapl_grad_norm and oapl_grad_clip take.  outs: where clipped elements go (None: in place)."""
+    return TensorList(tensors, outs)
+
+
+def oapl_grad_norm_workspace_bytes(count: int) -> int:
+    return int(lib().oapl_grad_norm_workspace_bytes(count))
+
+
+def oapl_grad_norm(tensors: TensorList, sq_norm, norm, ws, scale: float = 1.0, device_status=None):
+    """sq_norm, norm: fp32 [1] or None: the squared norm of scale * all tensors, and the norm.  ws: uint8,
+    oapl_grad_norm_workspace_bytes(count).  sq_norm serves oapl_adamw_step as other_sq_norm."""
+    dev, f32 = tensors.device, torch.float32
+    rc = lib().oapl_grad_norm(tensors.array, tensors.count, scale, _vec(sq_norm, f32, (1,), dev, "sq_norm"),
+                              _vec(norm, f32, (1,), dev, "norm"),
+                              _vec(device_status, torch.int32, (1,), dev, "device_status"), *_ws(ws, dev), _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_grad_norm")
+
+
+def oapl_grad_clip(tensors: TensorList, sq_norm, clip_norm: float, scale: float = 1.0):
+    """Every tensor times scale * min(1, clip_norm / (sqrt(sq_norm) + 1e-6)), into the list's outs."""
+    dev = tensors.device
+    if sq_norm is None:
+        raise TypeError("sq_norm: expected the fp32 [1] of oapl_grad_norm")
+    rc = lib().oapl_grad_clip(tensors.array, tensors.count, scale, _vec(sq_norm, torch.float32, (1,), dev, "sq_norm"),
+                              clip_norm, _stream_of(dev))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_grad_clip")
+
+
+def make_adjust(L: OaplLogits, tokens=None, spans=None, repetition=None, frequency=None, presence=None, bias_start=None,
+                bias_id=None, bias=None, allowed=None, allowed_row=None) -> OaplAdjust:
+    """Fill oapl_adjust for the rows of L.  tokens: int32 [T]; spans: int64 [N, 3], begin of a row's prompt, of its answer,
+    and the answer's end in tokens; repetition, frequency, presence: fp32 [N]; bias_start: int64 [N + 1] into bias_id
+    (int32) and bias (fp32); allowed: int32 [rows, words], bit v % 32 of word v / 32 set where token v is allowed, row n
+    of it for row n or row allowed_row[n] (int32 [N], negative: all tokens).  The struct keeps the tensors alive."""
+    dev, N, f32, i32 = L.device, L.N, torch.float32, torch.int32
+    T = 0 if tokens is None else tokens.numel()
+    biases = 0 if bias_id is None else bias_id.numel()
+    at_allowed, ld, rows = None, 0, 0
+    if allowed is not None:
+        _, rows, words, ld = _rows(allowed, {i32: 0}, "allowed")
+        if words * 32 < L.V or allowed.get_device() != dev or (allowed_row is None and rows != N):
+            raise TypeError(f"allowed: expected int32 [{N}, at least {-(-L.V // 32)}] on cuda:{dev}")
+        at_allowed = allowed.data_ptr()
+    a = OaplAdjust(_vec(tokens, i32, (T,), dev, "tokens"), T, _vec(spans, torch.int64, (N, 3), dev, "spans"),
+                   _vec(repetition, f32, (N,), dev, "repetition"), _vec(frequency, f32, (N,), dev, "frequency"),
+                   _vec(presence, f32, (N,), dev, "presence"), _vec(bias_start, torch.int64, (N + 1,), dev, "bias_start"),
+                   _vec(bias_id, i32, (biases,), dev, "bias_id"), _vec(bias, f32, (biases,), dev, "bias"), biases, at_allowed,
+                   ld, rows, _vec(allowed_row, i32, (N,), dev, "allowed_row"))
+    a.tensors = (tokens, spans, repetition, frequency, presence, bias_start, bias_id, bias, allowed, allowed_row)
+    return a
+
+
+def _of_logits(L, t, name):
+    code, N, V, ld = _rows(t, FLOAT_TYPES, name)
+    if code != L.type or N != L.N or V != L.V or t.get_device() != L.device:
+        raise TypeError(f"{name}: expected the logits' type, shape and device")
+    return t.data_ptr(), ld
+
+
+def oapl_logits_adjust(L: OaplLogits, a: OaplAdjust, out, device_status=None):
+    """out = the logits with penalties, biases and the mask applied; it may be the logits themselves."""
+    rc = lib().oapl_logits_adjust(L, a, *_of_logits(L, out, "out"),
+                                  _vec(device_status, torch.int32, (1,), L.device, "device_status"), _stream_of(L.device))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_logits_adjust")
+
+
+def oapl_logits_adjust_bwd(L: OaplLogits, a: OaplAdjust, d_out, dlogits, device_status=None):
+    """Gradient of the logits that L holds (before the adjustment) from that of the adjusted ones; dlogits may be d_out."""
+    rc = lib().oapl_logits_adjust_bwd(L, a, *_of_logits(L, d_out, "d_out"), *_of_logits(L, dlogits, "dlogits"),
+                                      _vec(device_status, torch.int32, (1,), L.device, "device_status"),
+                                      _stream_of(L.device))
+    if rc != OAPL_OK:
+        raise OaplError(rc, "oapl_logits_adjust_bwd")

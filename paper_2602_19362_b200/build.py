@@ -5,13 +5,15 @@ import os
 import re
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liboapl.so")
-SOURCES = ["oapl_api.cu"]
+SOURCES = ["oapl_api.cu", "step_api.cu"]
 DEPS = ["oapl_api.cu", "gemm_sm100.cuh", "small_kernels.cuh", "sm100_ptx.cuh", "sweep_schedule.cuh", "adamw.cuh",
-        "logits_ops.cuh", "quantize.cuh", "scaled_matmul.cuh",
+        "logits_ops.cuh", "quantize.cuh", "scaled_matmul.cuh", "step_api.cu", "elements.cuh", "host_common.cuh",
+        "embedding.cuh", "residual_norm.cuh", "grad_clip.cuh", "logits_adjust.cuh",
         os.path.join("..", "..", "include", "oapl.h")]
 
 
@@ -41,26 +43,35 @@ def _stale() -> bool:
     return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in DEPS)
 
 
+def _run(commands: list, verbose: bool) -> str:
+    """Run the commands side by side; what they reported, one after the other.  Raises if one of them fails."""
+    running = [subprocess.Popen(c, stderr=subprocess.PIPE, text=True) for c in commands]
+    logs = [p.communicate()[1] for p in running]
+    for p, c, log in zip(running, commands, logs):
+        if verbose or p.returncode:
+            sys.stderr.write(log)
+    for p, c in zip(running, commands):
+        if p.returncode:
+            raise subprocess.CalledProcessError(p.returncode, c)
+    return "".join(logs)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Build liboapl.so if missing or older than its sources; return its path."""
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    flags = ["-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo", "-Xptxas", "-v",
+             "-gencode", "arch=compute_100a,code=sm_100a"]
     # takes the library's place once the check has passed; each process builds one of its own
-    new = os.path.join(HERE, f".liboapl-{os.getpid()}.so")
-    cmd = [nvcc, "-shared", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo", "-Xptxas", "-v",
-           "-gencode", "arch=compute_100a,code=sm_100a", "-o", new]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    try:
-        done = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
-        if verbose or done.returncode:
-            sys.stderr.write(done.stderr)
-        done.check_returncode()
-        check_registers(done.stderr, _split_constant())
+    with tempfile.TemporaryDirectory(prefix=".build-", dir=HERE) as work:
+        new = os.path.join(work, "liboapl.so")
+        objects = [os.path.join(work, s + ".o") for s in SOURCES]
+        steps = [[nvcc, "-c", *flags, "-o", o, os.path.join(CSRC, s)] for s, o in zip(SOURCES, objects)]
+        log = _run(steps, verbose)
+        _run([[nvcc, "-shared", *flags, "-o", new, *objects]], verbose)
+        check_registers(log, _split_constant())
         os.replace(new, LIB)
-    finally:
-        if os.path.exists(new):
-            os.remove(new)
     return LIB
 
 

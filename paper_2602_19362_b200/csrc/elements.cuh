@@ -1,0 +1,178 @@
+// Element types of matrices in memory: 16-byte vectors widened to fp32 and narrowed again, and a few
+// instructions that the kernels on such matrices share.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "sm100_ptx.cuh"
+
+namespace oapl {
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint4 ldg_stream(const uint4* p) {
+  uint4 v;
+  asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+      : "l"(p));
+  return v;
+}
+
+// Element type: kN elements per 16 bytes, widening to fp32 (exact), the packed -inf word.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<__nv_bfloat16> {
+  static constexpr int kN = 8;
+  static constexpr uint32_t kNegInf = 0xFF80FF80u;
+  static __device__ __forceinline__ void widen(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ float one(const void* p, int64_t i) {
+    return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
+  }
+  static __device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ uint32_t pclamp(uint32_t a, uint32_t low) {  // a NaN stays
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(low));
+    return r;
+  }
+  static __device__ __forceinline__ float pmax_final(uint32_t a) {
+    return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint4 narrow(const float (&f)[8]) {
+    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                      pack_bf16x2(f[6], f[7]));
+  }
+  static __device__ __forceinline__ void put(void* p, int64_t i, float x) {
+    reinterpret_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
+  }
+};
+template <>
+struct Elem<__half> {
+  static constexpr int kN = 8;
+  static constexpr uint32_t kNegInf = 0xFC00FC00u;
+  static __device__ __forceinline__ void widen(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[2 * i] = t.x;
+      f[2 * i + 1] = t.y;
+    }
+  }
+  static __device__ __forceinline__ float one(const void* p, int64_t i) {
+    return __half2float(reinterpret_cast<const __half*>(p)[i]);
+  }
+  static __device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ uint32_t pclamp(uint32_t a, uint32_t low) {
+    uint32_t r;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(low));
+    return r;
+  }
+  static __device__ __forceinline__ float pmax_final(uint32_t a) {
+    const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&a));
+    return fmaxf(t.x, t.y);
+  }
+  static __device__ __forceinline__ uint32_t pk(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ uint4 narrow(const float (&f)[8]) {
+    return make_uint4(pk(f[0], f[1]), pk(f[2], f[3]), pk(f[4], f[5]), pk(f[6], f[7]));
+  }
+  static __device__ __forceinline__ void put(void* p, int64_t i, float x) {
+    reinterpret_cast<__half*>(p)[i] = __float2half_rn(x);
+  }
+};
+template <>
+struct Elem<float> {
+  static constexpr int kN = 4;
+  static constexpr uint32_t kNegInf = 0xFF800000u;
+  static __device__ __forceinline__ void widen(const uint4& v, float (&f)[4]) {
+    f[0] = __uint_as_float(v.x);
+    f[1] = __uint_as_float(v.y);
+    f[2] = __uint_as_float(v.z);
+    f[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ float one(const void* p, int64_t i) {
+    return reinterpret_cast<const float*>(p)[i];
+  }
+  static __device__ __forceinline__ uint32_t pmax(uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }
+  static __device__ __forceinline__ uint32_t pclamp(uint32_t a, uint32_t low) {
+    return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(low)));
+  }
+  static __device__ __forceinline__ float pmax_final(uint32_t a) { return __uint_as_float(a); }
+  static __device__ __forceinline__ uint4 narrow(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+  static __device__ __forceinline__ void put(void* p, int64_t i, float x) { reinterpret_cast<float*>(p)[i] = x; }
+};
+
+// KE neighbouring elements of a row: whole 16-byte vectors, or one element at its natural alignment.  Loading and
+// widening are apart, so that several loads can be in flight.
+template <typename T, int KE>
+struct Raw {
+  static constexpr int kV = KE / Elem<T>::kN;
+  uint4 v[kV];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) v[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void load_stream(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kV; ++i) v[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+  }
+  __device__ __forceinline__ void put(T* p) const {  // the bits as they are
+#pragma unroll
+    for (int i = 0; i < kV; ++i) reinterpret_cast<uint4*>(p)[i] = v[i];
+  }
+  __device__ __forceinline__ void widen(float (&f)[KE]) const {
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+      Elem<T>::widen(v[i], *reinterpret_cast<float(*)[Elem<T>::kN]>(&f[i * Elem<T>::kN]));
+  }
+  static __device__ __forceinline__ void store(T* p, const float (&f)[KE]) {
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+      reinterpret_cast<uint4*>(p)[i] =
+          Elem<T>::narrow(*reinterpret_cast<const float(*)[Elem<T>::kN]>(&f[i * Elem<T>::kN]));
+  }
+  static __device__ __forceinline__ void store_stream(T* p, const float (&f)[KE]) {
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+      __stcs(reinterpret_cast<uint4*>(p) + i,
+             Elem<T>::narrow(*reinterpret_cast<const float(*)[Elem<T>::kN]>(&f[i * Elem<T>::kN])));
+  }
+};
+template <typename T>
+struct Raw<T, 1> {
+  T v;
+  __device__ __forceinline__ void load(const T* p) { v = *p; }
+  __device__ __forceinline__ void load_stream(const T* p) { v = *p; }
+  __device__ __forceinline__ void put(T* p) const { *p = v; }
+  __device__ __forceinline__ void widen(float (&f)[1]) const { f[0] = Elem<T>::one(&v, 0); }
+  static __device__ __forceinline__ void store(T* p, const float (&f)[1]) { Elem<T>::put(p, 0, f[0]); }
+};
+
+}  // namespace oapl

@@ -1,0 +1,408 @@
+// Embedding lookup, and the gradient of its table.
+//
+//     out[n] = s table[id_n],       dtable[v] (+)= s sum_{n: id_n = v} dout[n]
+//
+// Both are bound by HBM: the lookup moves each row once in and once out; the gradient reads dout once and, when it does
+// not add to what is there, writes every row of the table's gradient, most of them zeros.
+//
+// The gradient adds rows in the order of their positions, without atomics on sums, so it is the same in every run:
+//   1. the positions are sorted by token (stable): up to kEbCountMax of them by counting, for each, the keys before it;
+//      more by a radix sort of two or three passes, each a histogram per tile, prefix sums per digit and a move;
+//   2. the sorted list is cut into chunks.  A CTA adds up a chunk's rows; a run of equal tokens that lies within the
+//      chunk goes straight to the table, the two that may reach over the chunk's ends leave partial sums;
+//   3. the CTA of the chunk where a run begins that reaches further adds up its partial sums.
+// A token that holds a tenth of the batch is thus spread over many CTAs.  Sums are fp32: up to kEbMaxChunk terms in a
+// chunk, then the chunks' partial sums.
+// Rows without a token are cleared by further CTAs of the launch of step 2, which find out by searching the sorted list.
+#pragma once
+#include <type_traits>
+
+#include "elements.cuh"
+
+namespace oapl {
+
+constexpr int kEbThreads = 256;
+constexpr int kEbCountMax = 8192;   // positions sorted by counting: work grows with their square
+constexpr int kEbTile = 2048;       // positions of a CTA of the radix sort
+constexpr int kEbMaxBits = 10;      // digit of a pass
+constexpr int kEbMinChunk = 32, kEbMaxChunk = 256;
+constexpr int kEbZeroRows = 32;     // rows of the table of a CTA that clears
+constexpr int kErrBadId = -5;       // OAPL_ERR_BAD_TARGET
+
+struct LookupParams {
+  const int32_t* ids;
+  const uint8_t* mask;
+  int64_t N;
+  int32_t V, d;
+  float scale;
+  int32_t* status;
+  const void* in;  // table, or dout
+  int64_t ld_in;
+  void* out;       // looked-up rows, or the table's gradient
+  int64_t ld_out;
+  // gradient
+  uint2* sorted;   // (token, position); tokens of rows that do not count are V
+  float* part;     // [chunks][2][d]: sums of a chunk's first run, when it came from before, and of its last one
+  int32_t chunk, chunks, slabs;
+  int32_t accumulate;
+};
+
+// The token of position n, V where it does not count.
+__device__ __forceinline__ uint32_t lookup_key(const LookupParams& p, int64_t n) {
+  if (p.mask && !p.mask[n]) return (uint32_t)p.V;
+  const uint32_t id = (uint32_t)p.ids[n];
+  return id < (uint32_t)p.V ? id : (uint32_t)p.V;
+}
+__device__ __forceinline__ void lookup_check(const LookupParams& p, int64_t n) {
+  if (p.status && !(p.mask && !p.mask[n]) && (uint32_t)p.ids[n] >= (uint32_t)p.V) atomicCAS(p.status, 0, kErrBadId);
+}
+
+// ------------------------------------------------------------------------------------------------ lookup
+// A thread: KE elements of R rows, all loads in flight; blockDim.x threads along a row, blockDim.y rows beside one
+// another, blockIdx.y pieces of a row.
+template <typename TI, typename TO, int KE, int R>
+__global__ void __launch_bounds__(kEbThreads) embedding_kernel(LookupParams p) {
+  const int c = ((int)blockIdx.y * (int)blockDim.x + (int)threadIdx.x) * KE;
+  const int64_t n0 = ((int64_t)blockIdx.x * R) * blockDim.y + threadIdx.y;
+  uint32_t key[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t n = n0 + (int64_t)r * blockDim.y;
+    key[r] = n < p.N ? lookup_key(p, n) : (uint32_t)p.V;
+    if (n < p.N && blockIdx.y == 0 && threadIdx.x == 0) lookup_check(p, n);
+  }
+  if (c >= p.d) return;
+  Raw<TI, KE> v[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (key[r] < (uint32_t)p.V) v[r].load(static_cast<const TI*>(p.in) + (int64_t)key[r] * p.ld_in + c);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t n = n0 + (int64_t)r * blockDim.y;
+    if (n >= p.N) break;
+    float f[KE];
+    if (key[r] < (uint32_t)p.V) {
+      if constexpr (std::is_same<TI, TO>::value) {
+        if (p.scale == 1.f) {  // the bits as they are, a NaN's too
+          v[r].put(static_cast<TO*>(p.out) + n * p.ld_out + c);
+          continue;
+        }
+      }
+      v[r].widen(f);
+#pragma unroll
+      for (int i = 0; i < KE; ++i) f[i] *= p.scale;
+    } else {
+#pragma unroll
+      for (int i = 0; i < KE; ++i) f[i] = 0.f;
+    }
+    Raw<TO, KE>::store(static_cast<TO*>(p.out) + n * p.ld_out + c, f);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ sorting
+// A warp ranks kEbCountRows positions: lanes share out the keys, each compared with all of the warp's positions.
+constexpr int kEbCountRows = 8;
+__global__ void __launch_bounds__(kEbThreads) embedding_count_sort_kernel(LookupParams p) {
+  const int N = (int)p.N, lane = threadIdx.x & 31;
+  const int n0 = ((int)blockIdx.x * (kEbThreads / 32) + (threadIdx.x >> 5)) * kEbCountRows;
+  if (n0 >= N) return;
+  uint32_t key[kEbCountRows];
+  int rank[kEbCountRows];
+#pragma unroll
+  for (int r = 0; r < kEbCountRows; ++r) {
+    key[r] = n0 + r < N ? lookup_key(p, n0 + r) : 0u;
+    rank[r] = 0;
+  }
+  if (lane < kEbCountRows && n0 + lane < N) lookup_check(p, n0 + lane);
+  for (int m0 = 0; m0 < N; m0 += 128) {
+    uint32_t k[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int m = m0 + j * 32 + lane;
+      k[j] = m < N ? lookup_key(p, m) : 0xFFFFFFFFu;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int m = m0 + j * 32 + lane;
+#pragma unroll
+      for (int r = 0; r < kEbCountRows; ++r) rank[r] += k[j] < key[r] + (m < n0 + r);  // equal keys keep their order
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kEbCountRows; ++r) {
+    const int at = __reduce_add_sync(0xffffffffu, rank[r]);
+    if (lane == 0 && n0 + r < N) p.sorted[at] = make_uint2(key[r], (uint32_t)(n0 + r));
+  }
+}
+
+struct RadixParams {
+  const uint2* in;   // nullptr: the first pass, keys from the ids
+  uint2* out;
+  uint32_t* hist;    // [bins][tiles], then its prefix sums within a bin
+  uint32_t* total;   // [bins]
+  int32_t shift, bits, tiles;
+};
+
+__device__ __forceinline__ uint2 radix_load(const LookupParams& p, const RadixParams& r, int64_t n) {
+  return r.in ? r.in[n] : make_uint2(lookup_key(p, n), (uint32_t)n);
+}
+
+__global__ void __launch_bounds__(kEbThreads) embedding_radix_hist_kernel(LookupParams p, RadixParams r) {
+  __shared__ uint32_t h[1 << kEbMaxBits];
+  const int bins = 1 << r.bits;
+  for (int i = threadIdx.x; i < bins; i += kEbThreads) h[i] = 0;
+  __syncthreads();
+  const int64_t n0 = (int64_t)blockIdx.x * kEbTile;
+#pragma unroll
+  for (int i = 0; i < kEbTile / kEbThreads; ++i) {
+    const int64_t n = n0 + i * kEbThreads + threadIdx.x;
+    if (n < p.N) {
+      if (!r.in) lookup_check(p, n);
+      atomicAdd(&h[(radix_load(p, r, n).x >> r.shift) & (bins - 1)], 1u);
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < bins; i += kEbThreads) r.hist[(int64_t)i * r.tiles + blockIdx.x] = h[i];
+}
+
+// A warp: exclusive prefix sums of one digit over the tiles.
+__global__ void __launch_bounds__(kEbThreads) embedding_radix_scan_kernel(RadixParams r) {
+  const int bin = (int)blockIdx.x * (kEbThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (bin >= (1 << r.bits)) return;
+  uint32_t* h = r.hist + (int64_t)bin * r.tiles;
+  uint32_t run = 0;
+  for (int t0 = 0; t0 < r.tiles; t0 += 32) {
+    const uint32_t v = t0 + lane < r.tiles ? h[t0 + lane] : 0u;
+    uint32_t s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t u = __shfl_up_sync(0xffffffffu, s, o);
+      if (lane >= o) s += u;
+    }
+    if (t0 + lane < r.tiles) h[t0 + lane] = run + s - v;
+    run += __shfl_sync(0xffffffffu, s, 31);
+  }
+  if (lane == 0) r.total[bin] = run;
+}
+
+// Moves a tile's positions to their places.  A warp holds successive positions, 32 at a time in order, so that equal
+// digits keep their order: before them come the smaller digits, the tiles before, the warps before and the lanes before.
+__global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(LookupParams p, RadixParams r) {
+  constexpr int kWarps = kEbThreads / 32, kRounds = kEbTile / kEbThreads;
+  __shared__ uint32_t at[1 << kEbMaxBits];               // first place of a digit of this tile
+  __shared__ uint16_t cnt[kWarps][1 << kEbMaxBits];
+  __shared__ uint32_t wsum[kWarps];
+  const int bins = 1 << r.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int i = threadIdx.x; i < kWarps << kEbMaxBits; i += kEbThreads) (&cnt[0][0])[i] = 0;
+  // the digits' first places: prefix sums over all digits, kPer neighbouring ones a thread
+  constexpr int kPer = (1 << kEbMaxBits) / kEbThreads;
+  uint32_t v[kPer], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int b = (int)threadIdx.x * kPer + i;
+    v[i] = b < bins ? r.total[b] : 0u;
+    sum += v[i];
+  }
+  uint32_t inc = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t u = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += u;
+  }
+  if (lane == 31) wsum[warp] = inc;
+  __syncthreads();
+  uint32_t before = inc - sum;
+  for (int w = 0; w < warp; ++w) before += wsum[w];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int b = (int)threadIdx.x * kPer + i;
+    if (b < bins) at[b] = before + r.hist[(int64_t)b * r.tiles + blockIdx.x];
+    before += v[i];
+  }
+  const int64_t n0 = (int64_t)blockIdx.x * kEbTile + warp * 32 * kRounds + lane;
+  uint2 e[kRounds];
+  uint16_t rank[kRounds];
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i)
+    if (n0 + i * 32 < p.N) e[i] = radix_load(p, r, n0 + i * 32);
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) {
+    const bool in = n0 + i * 32 < p.N;
+    const uint32_t digit = in ? (e[i].x >> r.shift) & (bins - 1) : 0xFFFFFFFFu;
+    const uint32_t same = __match_any_sync(0xffffffffu, digit);
+    const uint32_t earlier = __popc(same & ((1u << lane) - 1));
+    uint16_t had = 0;
+    if (in) had = cnt[warp][digit];
+    __syncwarp();
+    rank[i] = uint16_t(had + earlier);
+    if (in && earlier == 0) cnt[warp][digit] = uint16_t(had + __popc(same));
+    __syncwarp();
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += kEbThreads) {
+    uint32_t run = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      const uint32_t c = cnt[w][b];
+      cnt[w][b] = uint16_t(run);
+      run += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i)
+    if (n0 + i * 32 < p.N) {
+      const uint32_t digit = (e[i].x >> r.shift) & (bins - 1);
+      r.out[at[digit] + cnt[warp][digit] + rank[i]] = e[i];
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ sums
+// First place in the sorted list whose token is at least `key`.
+__device__ __forceinline__ int64_t sorted_lower(const uint2* s, int64_t n, uint32_t key) {
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (s[mid].x < key) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+template <int KE>
+__device__ __forceinline__ void table_put(const LookupParams& p, uint32_t v, int c, const float (&acc)[KE]) {
+  float* t = static_cast<float*>(p.out) + (int64_t)v * p.ld_out + c;
+  float f[KE];
+  if (p.accumulate) {
+    Raw<float, KE> old;
+    old.load(t);
+    old.widen(f);
+#pragma unroll
+    for (int i = 0; i < KE; ++i) f[i] = fmaf(p.scale, acc[i], f[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < KE; ++i) f[i] = p.scale * acc[i];
+  }
+  Raw<float, KE>::store(t, f);
+}
+
+// Grid: (chunks + CTAs that clear) x slabs of columns, the slabs of a chunk next to one another.
+template <typename T, int KE>
+__global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams p) {
+  constexpr int kAhead = 8;  // rows whose loads are in flight together
+  __shared__ uint2 e[kEbMaxChunk];
+  __shared__ uint32_t live;
+  const int slab = (int)(blockIdx.x % (unsigned)p.slabs);
+  const int64_t item = blockIdx.x / (unsigned)p.slabs;
+  const int c = (slab * (int)blockDim.x + (int)threadIdx.x) * KE;
+  if (item >= p.chunks) {
+    // clear the rows that no position names
+    const int64_t v0 = (item - p.chunks) * kEbZeroRows;
+    if (threadIdx.x < 32) {
+      const int64_t v = v0 + threadIdx.x;
+      bool has = true;
+      if (v < p.V) {
+        const int64_t at = sorted_lower(p.sorted, p.N, (uint32_t)v);
+        has = at < p.N && p.sorted[at].x == (uint32_t)v;
+      }
+      const uint32_t m = __ballot_sync(0xffffffffu, has);
+      if (threadIdx.x == 0) live = m;
+    }
+    __syncthreads();
+    if (c >= p.d) return;
+    const uint32_t m = live;
+    float zero[KE];
+#pragma unroll
+    for (int i = 0; i < KE; ++i) zero[i] = 0.f;
+    for (int r = 0; r < kEbZeroRows; ++r)
+      if (!(m >> r & 1)) Raw<float, KE>::store(static_cast<float*>(p.out) + (v0 + r) * p.ld_out + c, zero);
+    return;
+  }
+  const int64_t first = item * p.chunk;
+  const int n = (int)(p.N - first < p.chunk ? p.N - first : p.chunk);
+  for (int i = threadIdx.x; i < n; i += blockDim.x) e[i] = p.sorted[first + i];
+  const uint32_t none = 0xFFFFFFFFu;
+  const uint32_t prev = first ? p.sorted[first - 1].x : none;
+  const uint32_t next = first + n < p.N ? p.sorted[first + n].x : none;
+  __syncthreads();
+  if (c >= p.d) return;
+  float acc[KE];
+#pragma unroll
+  for (int i = 0; i < KE; ++i) acc[i] = 0.f;
+  const T* in = static_cast<const T*>(p.in) + c;
+  uint32_t key = e[0].x;
+  if (key >= (uint32_t)p.V) return;
+  bool from_before = key == prev;
+  for (int i0 = 0; i0 < n; i0 += kAhead) {
+    Raw<T, KE> v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (i0 + j < n && e[i0 + j].x < (uint32_t)p.V) v[j].load_stream(in + (int64_t)e[i0 + j].y * p.ld_in);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i0 + j >= n) break;
+      const uint32_t k = e[i0 + j].x;
+      if (k != key) {  // the run before this one has ended; the same for all threads
+        if (from_before) {
+          Raw<float, KE>::store(p.part + (item * 2) * p.d + c, acc);
+        } else {
+          table_put<KE>(p, key, c, acc);
+        }
+#pragma unroll
+        for (int i = 0; i < KE; ++i) acc[i] = 0.f;
+        key = k;
+        from_before = false;
+        if (k >= (uint32_t)p.V) return;
+      }
+      float f[KE];
+      v[j].widen(f);
+#pragma unroll
+      for (int i = 0; i < KE; ++i) acc[i] += f[i];
+    }
+  }
+  if (from_before) {
+    Raw<float, KE>::store(p.part + (item * 2) * p.d + c, acc);
+  } else if (next == key) {
+    Raw<float, KE>::store(p.part + (item * 2 + 1) * p.d + c, acc);
+  } else {
+    table_put<KE>(p, key, c, acc);
+  }
+}
+
+// Runs that reach over the end of the chunk where they begin: their partial sums, in order.
+template <int KE>
+__global__ void __launch_bounds__(kEbThreads) embedding_join_kernel(LookupParams p) {
+  constexpr int kAhead = 8;
+  const int slab = (int)(blockIdx.x % (unsigned)p.slabs);
+  const int64_t item = blockIdx.x / (unsigned)p.slabs;
+  const int c = (slab * (int)blockDim.x + (int)threadIdx.x) * KE;
+  const int64_t first = item * p.chunk, end = first + p.chunk;
+  if (end >= p.N) return;
+  const uint32_t key = p.sorted[end - 1].x;
+  if (key >= (uint32_t)p.V || p.sorted[end].x != key) return;
+  if (p.sorted[first].x == key && first && p.sorted[first - 1].x == key) return;  // it began before
+  if (c >= p.d) return;
+  float acc[KE];
+  Raw<float, KE> t;
+  t.load(p.part + (item * 2 + 1) * p.d + c);
+  t.widen(acc);
+  for (int64_t j0 = item + 1; j0 < p.chunks; j0 += kAhead) {
+    Raw<float, KE> v[kAhead];
+    bool in[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      in[j] = j0 + j < p.chunks && p.sorted[(j0 + j) * p.chunk].x == key;
+      if (j0 + j < p.chunks) v[j].load(p.part + ((j0 + j) * 2) * p.d + c);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (in[j]) {
+        float f[KE];
+        v[j].widen(f);
+#pragma unroll
+        for (int i = 0; i < KE; ++i) acc[i] += f[i];
+      }
+    if (!in[kAhead - 1]) break;
+  }
+  table_put<KE>(p, key, c, acc);
+}
+
+}  // namespace oapl

@@ -14,15 +14,13 @@
 #include "../../include/oapl.h"
 #include "adamw.cuh"
 #include "gemm_sm100.cuh"
+#include "host_common.cuh"
 #include "logits_ops.cuh"
 #include "quantize.cuh"
 #include "scaled_matmul.cuh"
 #include "small_kernels.cuh"
 
 namespace oapl {
-
-static std::atomic<uint64_t> g_launches{0};
-#define OAPL_LAUNCHED() (g_launches.fetch_add(1, std::memory_order_relaxed))
 
 // rows of one g chunk of the two-call backward: 74 row blocks of 256, so that on 74 CTA pairs the
 // chunk's dH tiles (74 x d/512) fill whole rounds and its sweep two whole waves of 37 row blocks
@@ -31,7 +29,6 @@ constexpr int kChunkRowsDefault = 74 * 256;
 // the ranges, the fewer partial rounds of dH tiles, passes over dW and tail waves of the sweep
 constexpr int kStageRowsDefault = 65536;
 constexpr int kSyncSlots = 4096;             // lock-step counters in the workspace, one per contraction launch
-constexpr int kMaxDevices = 64;              // per-device host-side caches
 
 static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -229,14 +226,6 @@ static bool make_map_out(CUtensorMap* m, void* base, int32_t type, uint64_t rows
             CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static int sm_count() {
-  static int n[kMaxDevices] = {0};
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 0;
-  if (!n[dev] && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n[dev] = 0;
-  return n[dev];
-}
-
 // Sweep schedule: a wave is R row blocks (256 rows, one CTA pair each) x C vocabulary
 // splits, R*C <= number of CTA pairs.  C is the smallest power of two that keeps the wave's
 // H row blocks within an L2 budget; a short row range is handled by the tail-wave
@@ -374,16 +363,6 @@ static int check_problem(const oapl_problem* p, bool need_loss_inputs) {
   }
   return OAPL_OK;
 }
-
-#define CK(call)                                   \
-  do {                                             \
-    if ((call) != cudaSuccess) return OAPL_ERR_CUDA; \
-  } while (0)
-#define CKL()                                                  \
-  do {                                                         \
-    OAPL_LAUNCHED();                                           \
-    if (cudaGetLastError() != cudaSuccess) return OAPL_ERR_CUDA; \
-  } while (0)
 
 // Live-row compaction shared by every forward: state word, compacted per-row arrays,
 // compacted-sequence bounds and the dense copy of the live rows of H.
@@ -646,20 +625,6 @@ static int staged_fwd_bwd(const oapl_problem* p, const Objective& ob, float* los
 
 // ---------------------------------------------------------------------------------------
 // Logits in memory: log-probabilities, entropy, top alternatives, and their gradient.
-static int logits_type_size(int32_t type) {
-  return type == OAPL_TYPE_BF16 || type == OAPL_TYPE_F16 ? 2 : (type == OAPL_TYPE_F32 ? 4 : 0);
-}
-
-static int check_logits(const oapl_logits* L) {
-  if (!L || !L->logits || L->N <= 0 || L->V <= 0 || L->ld < L->V) return OAPL_ERR_INVALID_ARG;
-  const int es = logits_type_size(L->type);
-  if (!es) return OAPL_ERR_INVALID_ARG;
-  if (!(L->scale > 0.f) || !(L->scale <= 1e6f)) return OAPL_ERR_INVALID_ARG;  // the forward's clamp
-  if ((uintptr_t)L->logits % es) return OAPL_ERR_MISALIGNED;
-  if (L->N > (int64_t)2000000000 || (int64_t)L->V > (int64_t)2000000000) return OAPL_ERR_UNSUPPORTED_SHAPE;
-  return OAPL_OK;
-}
-
 static LogitsParams logits_params(const oapl_logits* L) {
   LogitsParams lp;
   memset(&lp, 0, sizeof(lp));
@@ -909,7 +874,7 @@ static int scaled_product(const oapl_scaled* A, const oapl_scaled* B, void* C, i
   int rc = check_scaled(A);
   if (rc == OAPL_OK) rc = check_scaled(B);
   if (rc != OAPL_OK) return rc;
-  const int es = logits_type_size(c_type);
+  const int es = type_size(c_type);
   if (!C || !es || A->cols != B->cols || ldc < B->rows) return OAPL_ERR_INVALID_ARG;
   if ((uintptr_t)C % es) return OAPL_ERR_MISALIGNED;
   const int n_sm = sm_count();
@@ -1541,7 +1506,7 @@ int oapl_logits_logprobs_bwd(const oapl_logits* L, const float* token_lse, const
   if (g_entropy && !token_entropy) return OAPL_ERR_INVALID_ARG;
   if ((g_top != nullptr) != (K > 0) || (g_top && !top_id)) return OAPL_ERR_INVALID_ARG;
   if (dlogits == L->logits && ld_d != L->ld) return OAPL_ERR_INVALID_ARG;  // in place means the same rows
-  if ((uintptr_t)dlogits % logits_type_size(L->type)) return OAPL_ERR_MISALIGNED;
+  if ((uintptr_t)dlogits % type_size(L->type)) return OAPL_ERR_MISALIGNED;
   LogitsParams lp = logits_params(L);
   lp.K = K;
   lp.lse = token_lse;
@@ -1562,7 +1527,7 @@ int oapl_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int
                   int flags, void* stream) {
   const int rc = check_scaled(out);
   if (rc != OAPL_OK) return rc;
-  const int es = logits_type_size(x_type);
+  const int es = type_size(x_type);
   if (!x || !es || rows <= 0 || cols <= 0 || ld_x < cols) return OAPL_ERR_INVALID_ARG;
   if (flags & ~(OAPL_QUANT_TRANSPOSE | OAPL_QUANT_POW2)) return OAPL_ERR_INVALID_ARG;
   const bool turn = (flags & OAPL_QUANT_TRANSPOSE) != 0;
