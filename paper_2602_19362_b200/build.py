@@ -10,9 +10,9 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liboapl.so")
-SOURCES = ["oapl_api.cu", "step_api.cu"]
+SOURCES = ["oapl_api.cu", "step_api.cu", "residual_api.cu"]
 DEPS = ["oapl_api.cu", "gemm_sm100.cuh", "small_kernels.cuh", "sm100_ptx.cuh", "sweep_schedule.cuh", "adamw.cuh",
-        "logits_ops.cuh", "quantize.cuh", "scaled_matmul.cuh", "step_api.cu", "elements.cuh", "host_common.cuh",
+        "logits_ops.cuh", "quantize.cuh", "scaled_matmul.cuh", "step_api.cu", "residual_api.cu", "elements.cuh", "host_common.cuh",
         "embedding.cuh", "residual_norm.cuh", "grad_clip.cuh", "logits_adjust.cuh",
         os.path.join("..", "..", "include", "oapl.h")]
 

@@ -47,11 +47,11 @@ struct LookupParams {
   int32_t accumulate;
 };
 
-// The token of position n, V where it does not count.
+// The token of position n, V where it does not count.  Both loads are in flight together.
 __device__ __forceinline__ uint32_t lookup_key(const LookupParams& p, int64_t n) {
-  if (p.mask && !p.mask[n]) return (uint32_t)p.V;
   const uint32_t id = (uint32_t)p.ids[n];
-  return id < (uint32_t)p.V ? id : (uint32_t)p.V;
+  const uint32_t live = p.mask ? p.mask[n] : 1u;
+  return live && id < (uint32_t)p.V ? id : (uint32_t)p.V;
 }
 __device__ __forceinline__ void lookup_check(const LookupParams& p, int64_t n) {
   if (p.status && !(p.mask && !p.mask[n]) && (uint32_t)p.ids[n] >= (uint32_t)p.V) atomicCAS(p.status, 0, kErrBadId);
@@ -100,33 +100,42 @@ __global__ void __launch_bounds__(kEbThreads) embedding_kernel(LookupParams p) {
 }
 
 // ------------------------------------------------------------------------------------------------ sorting
-// A warp ranks kEbCountRows positions: lanes share out the keys, each compared with all of the warp's positions.
+// A warp ranks kEbCountRows positions: the CTA brings all keys into shared memory, lanes share them out and compare each
+// with the warp's positions.  Of equal keys the earlier position comes first.
 constexpr int kEbCountRows = 8;
 __global__ void __launch_bounds__(kEbThreads) embedding_count_sort_kernel(LookupParams p) {
+  __shared__ uint32_t keys[kEbCountMax];
   const int N = (int)p.N, lane = threadIdx.x & 31;
+#pragma unroll 8
+  for (int m = threadIdx.x; m < N; m += kEbThreads) keys[m] = lookup_key(p, m);
+  __syncthreads();
   const int n0 = ((int)blockIdx.x * (kEbThreads / 32) + (threadIdx.x >> 5)) * kEbCountRows;
   if (n0 >= N) return;
   uint32_t key[kEbCountRows];
   int rank[kEbCountRows];
 #pragma unroll
   for (int r = 0; r < kEbCountRows; ++r) {
-    key[r] = n0 + r < N ? lookup_key(p, n0 + r) : 0u;
+    key[r] = n0 + r < N ? keys[n0 + r] : 0u;
     rank[r] = 0;
   }
   if (lane < kEbCountRows && n0 + lane < N) lookup_check(p, n0 + lane);
-  for (int m0 = 0; m0 < N; m0 += 128) {
-    uint32_t k[4];
+  // n0 is a multiple of 8 and the positions of a step are 32: before them all, at them, or behind them all
+  int m0 = 0;
+  for (; m0 + 32 <= n0; m0 += 32) {
+    const uint32_t k = keys[m0 + lane];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + j * 32 + lane;
-      k[j] = m < N ? lookup_key(p, m) : 0xFFFFFFFFu;
-    }
+    for (int r = 0; r < kEbCountRows; ++r) rank[r] += k <= key[r];
+  }
+  for (; m0 < N && m0 < n0 + kEbCountRows; m0 += 32) {
+    const int m = m0 + lane;
+    const uint32_t k = m < N ? keys[m] : 0xFFFFFFFFu;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + j * 32 + lane;
+    for (int r = 0; r < kEbCountRows; ++r) rank[r] += k < key[r] || (k == key[r] && m < n0 + r);
+  }
+  for (; m0 < N; m0 += 32) {
+    const uint32_t k = m0 + lane < N ? keys[m0 + lane] : 0xFFFFFFFFu;
 #pragma unroll
-      for (int r = 0; r < kEbCountRows; ++r) rank[r] += k[j] < key[r] + (m < n0 + r);  // equal keys keep their order
-    }
+    for (int r = 0; r < kEbCountRows; ++r) rank[r] += k < key[r];
   }
 #pragma unroll
   for (int r = 0; r < kEbCountRows; ++r) {
@@ -152,15 +161,19 @@ __global__ void __launch_bounds__(kEbThreads) embedding_radix_hist_kernel(Lookup
   const int bins = 1 << r.bits;
   for (int i = threadIdx.x; i < bins; i += kEbThreads) h[i] = 0;
   __syncthreads();
-  const int64_t n0 = (int64_t)blockIdx.x * kEbTile;
+  const int64_t n0 = (int64_t)blockIdx.x * kEbTile + threadIdx.x;
+  uint32_t key[kEbTile / kEbThreads];
 #pragma unroll
   for (int i = 0; i < kEbTile / kEbThreads; ++i) {
-    const int64_t n = n0 + i * kEbThreads + threadIdx.x;
-    if (n < p.N) {
-      if (!r.in) lookup_check(p, n);
-      atomicAdd(&h[(radix_load(p, r, n).x >> r.shift) & (bins - 1)], 1u);
-    }
+    const int64_t n = n0 + i * kEbThreads;
+    key[i] = n < p.N ? radix_load(p, r, n).x : 0u;
   }
+#pragma unroll
+  for (int i = 0; i < kEbTile / kEbThreads; ++i)
+    if (n0 + i * kEbThreads < p.N) {
+      atomicAdd(&h[(key[i] >> r.shift) & (bins - 1)], 1u);
+      if (!r.in && key[i] == (uint32_t)p.V) lookup_check(p, n0 + i * kEbThreads);
+    }
   __syncthreads();
   for (int i = threadIdx.x; i < bins; i += kEbThreads) r.hist[(int64_t)i * r.tiles + blockIdx.x] = h[i];
 }
@@ -224,7 +237,7 @@ __global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(Lookup
   uint16_t rank[kRounds];
 #pragma unroll
   for (int i = 0; i < kRounds; ++i)
-    if (n0 + i * 32 < p.N) e[i] = radix_load(p, r, n0 + i * 32);
+    e[i] = n0 + i * 32 < p.N ? radix_load(p, r, n0 + i * 32) : make_uint2(0u, 0u);
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) {
     const bool in = n0 + i * 32 < p.N;
@@ -284,7 +297,7 @@ __device__ __forceinline__ void table_put(const LookupParams& p, uint32_t v, int
   Raw<float, KE>::store(t, f);
 }
 
-// Grid: (chunks + CTAs that clear) x slabs of columns, the slabs of a chunk next to one another.
+// Grid: chunks x slabs of columns, the slabs of a chunk next to one another, then the CTAs that clear.
 template <typename T, int KE>
 __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams p) {
   constexpr int kAhead = 8;  // rows whose loads are in flight together
@@ -295,7 +308,7 @@ __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams 
   const int c = (slab * (int)blockDim.x + (int)threadIdx.x) * KE;
   if (item >= p.chunks) {
     // clear the rows that no position names
-    const int64_t v0 = (item - p.chunks) * kEbZeroRows;
+    const int64_t v0 = ((int64_t)blockIdx.x - (int64_t)p.chunks * p.slabs) * kEbZeroRows;
     if (threadIdx.x < 32) {
       const int64_t v = v0 + threadIdx.x;
       bool has = true;
@@ -307,13 +320,24 @@ __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams 
       if (threadIdx.x == 0) live = m;
     }
     __syncthreads();
-    if (c >= p.d) return;
     const uint32_t m = live;
-    float zero[KE];
-#pragma unroll
-    for (int i = 0; i < KE; ++i) zero[i] = 0.f;
+    const int w = p.d;
     for (int r = 0; r < kEbZeroRows; ++r)
-      if (!(m >> r & 1)) Raw<float, KE>::store(static_cast<float*>(p.out) + (v0 + r) * p.ld_out + c, zero);
+      if (!(m >> r & 1)) {
+        float* row = static_cast<float*>(p.out) + (v0 + r) * p.ld_out;
+        if constexpr (KE > 1) {
+          for (int i = threadIdx.x; i < w / 4; i += blockDim.x) reinterpret_cast<float4*>(row)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+          // up to the first 16-byte boundary, vectors, and the rest
+          int head = (int)(-(reinterpret_cast<uintptr_t>(row) >> 2) & 3);
+          head = head < w ? head : w;
+          const int vecs = (w - head) / 4;
+          float4* body = reinterpret_cast<float4*>(row + head);
+          for (int i = threadIdx.x; i < vecs; i += blockDim.x) body[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          const int i = (int)threadIdx.x < head ? (int)threadIdx.x : head + vecs * 4 + (int)threadIdx.x - head;
+          if (i < w && ((int)threadIdx.x < head || (int)threadIdx.x < head + (w - head) % 4)) row[i] = 0.f;
+        }
+      }
     return;
   }
   const int64_t first = item * p.chunk;
@@ -367,41 +391,58 @@ __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams 
   }
 }
 
-// Runs that reach over the end of the chunk where they begin: their partial sums, in order.
+// Runs that reach over the end of the chunk where they begin: their partial sums.  blockDim.y threads of a column share
+// out the chunks and are added up in their order.
+constexpr int kEbJoinShares = 4;
 template <int KE>
-__global__ void __launch_bounds__(kEbThreads) embedding_join_kernel(LookupParams p) {
-  constexpr int kAhead = 8;
+__global__ void __launch_bounds__(64 * kEbJoinShares) embedding_join_kernel(LookupParams p) {
+  constexpr int kAhead = 4;
+  __shared__ float sh[kEbJoinShares][64 * KE];
   const int slab = (int)(blockIdx.x % (unsigned)p.slabs);
   const int64_t item = blockIdx.x / (unsigned)p.slabs;
-  const int c = (slab * (int)blockDim.x + (int)threadIdx.x) * KE;
+  const int c = (slab * 64 + (int)threadIdx.x) * KE;
   const int64_t first = item * p.chunk, end = first + p.chunk;
   if (end >= p.N) return;
-  const uint32_t key = p.sorted[end - 1].x;
-  if (key >= (uint32_t)p.V || p.sorted[end].x != key) return;
-  if (p.sorted[first].x == key && first && p.sorted[first - 1].x == key) return;  // it began before
-  if (c >= p.d) return;
+  const uint32_t key = p.sorted[end - 1].x, next = p.sorted[end].x;
+  const uint32_t start = p.sorted[first].x, prev = first ? p.sorted[first - 1].x : 0xFFFFFFFFu;
+  if (key >= (uint32_t)p.V || next != key || (start == key && prev == key)) return;  // the last: it began before
   float acc[KE];
-  Raw<float, KE> t;
-  t.load(p.part + (item * 2 + 1) * p.d + c);
-  t.widen(acc);
-  for (int64_t j0 = item + 1; j0 < p.chunks; j0 += kAhead) {
-    Raw<float, KE> v[kAhead];
-    bool in[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      in[j] = j0 + j < p.chunks && p.sorted[(j0 + j) * p.chunk].x == key;
-      if (j0 + j < p.chunks) v[j].load(p.part + ((j0 + j) * 2) * p.d + c);
+  for (int i = 0; i < KE; ++i) acc[i] = 0.f;
+  if (c < p.d) {
+    if (threadIdx.y == 0) {
+      Raw<float, KE> t;
+      t.load(p.part + (item * 2 + 1) * p.d + c);
+      t.widen(acc);
     }
+    for (int64_t j0 = item + 1 + threadIdx.y; j0 < p.chunks; j0 += kAhead * kEbJoinShares) {
+      Raw<float, KE> v[kAhead];
+      bool in[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (in[j]) {
-        float f[KE];
-        v[j].widen(f);
-#pragma unroll
-        for (int i = 0; i < KE; ++i) acc[i] += f[i];
+      for (int j = 0; j < kAhead; ++j) {
+        const int64_t at = j0 + j * kEbJoinShares;
+        in[j] = at < p.chunks && p.sorted[at * p.chunk].x == key;
+        if (at < p.chunks) v[j].load(p.part + (at * 2) * p.d + c);
       }
-    if (!in[kAhead - 1]) break;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (in[j]) {
+          float f[KE];
+          v[j].widen(f);
+#pragma unroll
+          for (int i = 0; i < KE; ++i) acc[i] += f[i];
+        }
+      if (!in[kAhead - 1]) break;
+    }
   }
+#pragma unroll
+  for (int i = 0; i < KE; ++i) sh[threadIdx.y][threadIdx.x + i * 64] = acc[i];
+  __syncthreads();
+  if (threadIdx.y || c >= p.d) return;
+#pragma unroll
+  for (int y = 1; y < kEbJoinShares; ++y)
+#pragma unroll
+    for (int i = 0; i < KE; ++i) acc[i] += sh[y][threadIdx.x + i * 64];
   table_put<KE>(p, key, c, acc);
 }
 

@@ -4,9 +4,9 @@
 //
 // Bound by HBM: the norm reads every element once; no element can be scaled before that, so the second call reads them
 // again and writes the result.  The list goes to the kernel as its argument, so a call copies nothing to the device.  The
-// elements are cut into chunks of kGcChunk, a CTA takes a stretch of successive chunks; the second call takes each
-// stretch from its end, where the first one left off, which finds up to an L2 full of elements there.
-// Squares are added in fp32 over a thread's 32 elements of a chunk and in fp64 from there, in an order that only the
+// elements are cut into chunks of 16 KB that the CTAs take in turn; the second call begins at the end, where the first
+// one left off, and finds up to an L2 full of elements there.
+// Squares are added in fp32 over a thread's 16 or 32 elements of a chunk and in fp64 from there, in an order that only the
 // list and the number of SMs determine.  A thread whose fp32 sum left the range where that is exact to fp32 rounding
 // (values above about 1e14, or nothing but values below about 1e-12) adds the same elements again in fp64.
 #pragma once
@@ -15,7 +15,8 @@
 namespace oapl {
 
 constexpr int kGcThreads = 256;
-constexpr int kGcChunk = 8192;
+constexpr int kGcVecs = 4;                                  // 16-byte vectors of a thread that are read together
+constexpr int kGcBytes = kGcVecs * kGcThreads * 16;         // of a chunk, in the wider one of its two types
 constexpr int kGcList = 480;       // tensors of a launch
 constexpr int kGcSumsPerSm = 8;    // CTAs, each with one partial sum
 constexpr int kErrNonfiniteGrad = -7;  // OAPL_ERR_NONFINITE_INPUT
@@ -25,7 +26,7 @@ struct GradTensor {
   void* out;
   int64_t n;
   int32_t first;       // chunks of the list before this tensor's
-  uint8_t in_type, out_type, vec;
+  uint8_t in_type, out_type, vec, shift;  // shift: log2 of the elements of a chunk
 };
 struct GradList {
   GradTensor t[kGcList];
@@ -43,77 +44,69 @@ __device__ __forceinline__ int grad_find(const GradList& l, int chunk) {
 }
 
 // ------------------------------------------------------------------------------------------------ norm
-// Sum of squares of a thread's share of a chunk: W words of elements in registers.
-template <typename T, int KE, int U>
-__device__ __forceinline__ double grad_squares(const T* g, int n) {
-  Raw<T, KE> v[U];
-  float s = 0.f, top = 0.f;
+// Sum of squares of a thread's vectors, whatever their type: fp32 where it is exact to fp32 rounding, fp64 otherwise.
+template <typename T>
+__device__ __forceinline__ double grad_squares(const uint4 (&v)[kGcVecs]) {
+  constexpr int KE = Elem<T>::kN;
+  float2 s = make_float2(0.f, 0.f);
+  float top = 0.f;
 #pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int i = (j * kGcThreads + (int)threadIdx.x) * KE;
-    if (i + KE <= n) v[j].load(g + i);
-  }
+  for (int j = 0; j < kGcVecs; ++j) {
+    float f[KE];
+    Elem<T>::widen(v[j], f);
 #pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int i = (j * kGcThreads + (int)threadIdx.x) * KE;
-    if (i + KE <= n) {
-      float f[KE];
-      v[j].widen(f);
-#pragma unroll
-      for (int k = 0; k < KE; ++k) {
-        s = fmaf(f[k], f[k], s);
-        top = fmaxf(top, fabsf(f[k]));
-      }
+    for (int k = 0; k < KE; k += 2) {
+      const float2 x = make_float2(f[k], f[k + 1]);
+      s = __ffma2_rn(x, x, s);
+      top = fmaxf(top, fmaxf(fabsf(x.x), fabsf(x.y)));
     }
   }
-  if (s < 1e29f && (s > 1e-23f || top == 0.f)) return (double)s;
+  const float sum = s.x + s.y;
+  if (sum < 1e29f && (sum > 1e-23f || top == 0.f)) return (double)sum;
   double w = 0.0;
+#pragma unroll 1
+  for (int j = 0; j < kGcVecs; ++j) {
+    const uint4 q = j == 0 ? v[0] : j == 1 ? v[1] : j == 2 ? v[2] : v[3];
+    float f[KE];
+    Elem<T>::widen(q, f);
 #pragma unroll
-  for (int j = 0; j < U; ++j) {
-    const int i = (j * kGcThreads + (int)threadIdx.x) * KE;
-    if (i + KE <= n) {
-      float f[KE];
-      v[j].widen(f);
-#pragma unroll
-      for (int k = 0; k < KE; ++k) w = fma((double)f[k], (double)f[k], w);
-    }
+    for (int k = 0; k < KE; ++k) w = fma((double)f[k], (double)f[k], w);
   }
   return w;
 }
-
-template <typename T>
-__device__ __forceinline__ double grad_chunk_squares(const GradTensor& t, int64_t at) {
-  const T* g = static_cast<const T*>(t.in) + at;
-  const int n = (int)(t.n - at < kGcChunk ? t.n - at : kGcChunk);
-  constexpr int KE = Elem<T>::kN;
-  double s = 0.0;
-  if (t.vec) {
-    // four vectors of 16-bit elements or eight of fp32, all in flight
-    s = grad_squares<T, KE, kGcChunk / kGcThreads / KE>(g, n);
-    const int rest = n / KE * KE + (int)threadIdx.x;
-    if (rest < n) {
-      const double x = Elem<T>::one(g, rest);
-      s = fma(x, x, s);
-    }
-  } else {
-    for (int i = 0; i < n; i += 8 * kGcThreads) s += grad_squares<T, 1, 8>(g + i, n - i);
-  }
-  return s;
+__device__ __forceinline__ float grad_one(const void* p, int type, int64_t i) {
+  return type == 0 ? Elem<__nv_bfloat16>::one(p, i) : (type == 1 ? Elem<__half>::one(p, i) : Elem<float>::one(p, i));
 }
 
-__global__ void __launch_bounds__(kGcThreads, 4) grad_norm_kernel(const __grid_constant__ GradList l, double* part) {
+__global__ void __launch_bounds__(kGcThreads, 5) grad_norm_kernel(const __grid_constant__ GradList l, double* part) {
   __shared__ double sh[kGcThreads / 32];
-  const int64_t b = blockIdx.x, nb = gridDim.x;
-  const int lo = (int)(b * l.chunks / nb), hi = (int)((b + 1) * l.chunks / nb);
   double s = 0.0;
-  int k = lo < hi ? grad_find(l, lo) : 0;
-  for (int c = lo; c < hi; ++c) {
+  int k = grad_find(l, (int)blockIdx.x);
+  for (int c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     while (k + 1 < l.count && l.t[k + 1].first <= c) ++k;
     const GradTensor& t = l.t[k];
-    const int64_t at = (int64_t)(c - t.first) * kGcChunk;
-    if (t.in_type == 0) s += grad_chunk_squares<__nv_bfloat16>(t, at);
-    else if (t.in_type == 1) s += grad_chunk_squares<__half>(t, at);
-    else s += grad_chunk_squares<float>(t, at);
+    const int64_t at = (int64_t)(c - t.first) << t.shift;
+    const int size = 1 << t.shift, n = t.n - at < size ? (int)(t.n - at) : size;
+    int done = 0;
+    if (t.vec) {
+      const int per = t.in_type == 2 ? 4 : 8;
+      const uint4* g = reinterpret_cast<const uint4*>(static_cast<const char*>(t.in) + at * (t.in_type == 2 ? 4 : 2));
+      const int vecs = n / per;
+      done = vecs * per;
+      uint4 v[kGcVecs];
+#pragma unroll
+      for (int j = 0; j < kGcVecs; ++j) {
+        const int i = j * kGcThreads + (int)threadIdx.x;
+        v[j] = i < vecs ? g[i] : make_uint4(0, 0, 0, 0);
+      }
+      if (t.in_type == 0) s += grad_squares<__nv_bfloat16>(v);
+      else if (t.in_type == 1) s += grad_squares<__half>(v);
+      else s += grad_squares<float>(v);
+    }
+    for (int i = done + (int)threadIdx.x; i < n; i += kGcThreads) {
+      const double x = grad_one(t.in, t.in_type, at + i);
+      s = fma(x, x, s);
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
@@ -122,7 +115,7 @@ __global__ void __launch_bounds__(kGcThreads, 4) grad_norm_kernel(const __grid_c
   if (threadIdx.x == 0) {
     double t = 0.0;
     for (int w = 0; w < kGcThreads / 32; ++w) t += sh[w];
-    part[b] = t;
+    part[blockIdx.x] = t;
   }
 }
 
@@ -148,45 +141,45 @@ __global__ void __launch_bounds__(kGcThreads) grad_norm_join_kernel(const double
 
 // ------------------------------------------------------------------------------------------------ clipping
 template <typename TI, typename TO>
-__device__ __forceinline__ void grad_scale_chunk(const GradTensor& t, int64_t at, float factor) {
+__device__ __forceinline__ void grad_scale_chunk(const GradTensor& t, int64_t at, int n, float factor) {
   const TI* g = static_cast<const TI*>(t.in) + at;
   TO* o = static_cast<TO*>(t.out) + at;
-  const int n = (int)(t.n - at < kGcChunk ? t.n - at : kGcChunk);
   constexpr int KE = Elem<TI>::kN > Elem<TO>::kN ? Elem<TI>::kN : Elem<TO>::kN;
+  constexpr int U = kGcBytes / kGcThreads / KE / (sizeof(TI) > sizeof(TO) ? (int)sizeof(TI) : (int)sizeof(TO));
   int done = 0;
   if (t.vec) {
-    constexpr int U = kGcChunk / kGcThreads / KE;
+    const int vecs = n / KE;
+    done = vecs * KE;
     Raw<TI, KE> v[U];
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      const int i = (j * kGcThreads + (int)threadIdx.x) * KE;
-      if (i + KE <= n) v[j].load_stream(g + i);
+      const int i = j * kGcThreads + (int)threadIdx.x;
+      if (i < vecs) v[j].load_stream(g + i * KE);
     }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      const int i = (j * kGcThreads + (int)threadIdx.x) * KE;
-      if (i + KE <= n) {
+      const int i = j * kGcThreads + (int)threadIdx.x;
+      if (i < vecs) {
         float f[KE];
         v[j].widen(f);
 #pragma unroll
         for (int k = 0; k < KE; ++k) f[k] *= factor;
-        Raw<TO, KE>::store_stream(o + i, f);
+        Raw<TO, KE>::store_stream(o + i * KE, f);
       }
     }
-    done = n / KE * KE;
   }
-#pragma unroll 4
+#pragma unroll 1
   for (int i = done + (int)threadIdx.x; i < n; i += kGcThreads) Elem<TO>::put(o, i, Elem<TI>::one(g, i) * factor);
 }
 
 template <typename TI>
-__device__ __forceinline__ void grad_scale_types(const GradTensor& t, int64_t at, float factor) {
-  if (t.out_type == 0) grad_scale_chunk<TI, __nv_bfloat16>(t, at, factor);
-  else if (t.out_type == 1) grad_scale_chunk<TI, __half>(t, at, factor);
-  else grad_scale_chunk<TI, float>(t, at, factor);
+__device__ __forceinline__ void grad_scale_types(const GradTensor& t, int64_t at, int n, float factor) {
+  if (t.out_type == 0) grad_scale_chunk<TI, __nv_bfloat16>(t, at, n, factor);
+  else if (t.out_type == 1) grad_scale_chunk<TI, __half>(t, at, n, factor);
+  else grad_scale_chunk<TI, float>(t, at, n, factor);
 }
 
-__global__ void __launch_bounds__(kGcThreads, 4) grad_clip_kernel(const __grid_constant__ GradList l, const float* sq_norm,
+__global__ void __launch_bounds__(kGcThreads, 3) grad_clip_kernel(const __grid_constant__ GradList l, const float* sq_norm,
                                                                float clip, float scale) {
   __shared__ float sh;
   if (threadIdx.x == 0) {
@@ -197,17 +190,17 @@ __global__ void __launch_bounds__(kGcThreads, 4) grad_clip_kernel(const __grid_c
   }
   __syncthreads();
   const float factor = sh;
-  const int64_t b = blockIdx.x, nb = gridDim.x;
-  const int lo = (int)(b * l.chunks / nb), hi = (int)((b + 1) * l.chunks / nb);
-  int k = lo < hi ? grad_find(l, hi - 1) : 0;
-  for (int c = hi - 1; c >= lo; --c) {
+  const int last = l.chunks - 1 - (int)blockIdx.x;
+  int k = grad_find(l, last);
+  for (int c = last; c >= 0; c -= gridDim.x) {
     while (l.t[k].first > c) --k;
     const GradTensor& t = l.t[k];
     if (factor == 1.f && t.in == t.out) continue;  // in place, and nothing changes
-    const int64_t at = (int64_t)(c - t.first) * kGcChunk;
-    if (t.in_type == 0) grad_scale_types<__nv_bfloat16>(t, at, factor);
-    else if (t.in_type == 1) grad_scale_types<__half>(t, at, factor);
-    else grad_scale_types<float>(t, at, factor);
+    const int64_t at = (int64_t)(c - t.first) << t.shift;
+    const int size = 1 << t.shift, n = t.n - at < size ? (int)(t.n - at) : size;
+    if (t.in_type == 0) grad_scale_types<__nv_bfloat16>(t, at, n, factor);
+    else if (t.in_type == 1) grad_scale_types<__half>(t, at, n, factor);
+    else grad_scale_types<float>(t, at, n, factor);
   }
 }
 

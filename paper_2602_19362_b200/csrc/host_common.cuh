@@ -47,4 +47,31 @@ inline int check_logits(const oapl_logits* L) {
   return OAPL_OK;
 }
 
+constexpr int64_t kMaxRows = 2000000000;
+constexpr int64_t kMaxGrid = 2147483647;
+
+inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// A matrix in memory, to see what overlaps.
+struct Place {
+  const void* base;
+  int64_t rows, cols, ld;
+  int es;
+};
+enum Overlap { kApart, kSameRows, kMixed };
+// kSameRows: the same rows of the same elements.  Matrices of one row pitch may lie between one another's rows.
+inline Overlap overlap(const Place& p, const Place& q) {
+  using Wide = unsigned __int128;
+  if (!p.base || !q.base) return kApart;
+  const Wide a = (uintptr_t)p.base, b = (uintptr_t)q.base, ra = (Wide)p.cols * p.es, rb = (Wide)q.cols * q.es;
+  const Wide pa = (Wide)p.ld * p.es, pb = (Wide)q.ld * q.es;
+  const Wide ea = a + (Wide)(p.rows - 1) * pa + ra, eb = b + (Wide)(q.rows - 1) * pb + rb;
+  if (a >= eb || b >= ea) return kApart;
+  if (a == b && p.es == q.es && p.rows == q.rows && p.cols == q.cols && (pa == pb || p.rows == 1)) return kSameRows;
+  if (pa != pb) return kMixed;
+  const Wide off = b >= a ? (b - a) % pa : (pa - (a - b) % pa) % pa;  // q's rows in p's pitch
+  return off >= ra && pa - off >= rb ? kApart : kMixed;
+}
+
 }  // namespace oapl

@@ -44,7 +44,7 @@ struct ResidualParams {
   int64_t ld_dx, ld_dy, ld_dg;
   float* part;      // [kinds][workers][d]
   int32_t kind_pre, kind_post, kind_gate;  // where a kind's partial rows are, -1 without
-  int32_t stages;   // rows that are in flight
+  int32_t stages, pitch;  // rows of an array in shared memory, bytes from one to the next
 };
 
 // KE elements of a weight of any type, as fp32.
@@ -95,6 +95,7 @@ __device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.com
 // Until the copies of all but the last `ahead` rows are there.
 __device__ __forceinline__ void copy_async_wait(int ahead) {
   if (ahead == 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+  else if (ahead == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
   else if (ahead == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
   else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
@@ -102,12 +103,11 @@ __device__ __forceinline__ void copy_async_wait(int ahead) {
 // The threads of a row: a warp, or the whole CTA.
 template <bool WARP>
 struct RowGroup {
+  static constexpr int kSlot = 3 * 16;  // three sums of at most 16 warps
   int t, nt;
   int64_t first, step;
-  float* red;   // [2][kMaxSums][32]
-  int turn;
-  static constexpr int kMaxSums = 3;
-  __device__ __forceinline__ RowGroup(float* red_) : red(red_), turn(0) {
+  float* red;  // two slots
+  __device__ __forceinline__ explicit RowGroup(float* red_) : red(red_) {
     if (WARP) {
       const int warps = (int)blockDim.x >> 5;
       t = threadIdx.x & 31;
@@ -119,345 +119,530 @@ struct RowGroup {
       nt = blockDim.x;
       first = blockIdx.x;
       step = gridDim.x;
+      for (int i = t; i < 64 + kSlot; i += nt) red[i] = 0.f;  // the places of warps that there are not
+      __syncthreads();
     }
   }
-  template <int M>
-  __device__ __forceinline__ void sum(float (&v)[M]) {
+  __device__ __forceinline__ void sync() const {
+    if (WARP) __syncwarp();
+    else __syncthreads();
+  }
+  // Sum over the row's threads, the same bits in each of them.
+  __device__ __forceinline__ float sum(float v) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (WARP) return v;
+    if ((t & 31) == 0) red[t >> 5] = v;
+    __syncthreads();
+    const float4* r = reinterpret_cast<const float4*>(red);
+    const float4 p = r[0], q = r[1], x = r[2], y = r[3];
+    swap();
+    return (((p.x + p.y) + (p.z + p.w)) + ((q.x + q.y) + (q.z + q.w))) +
+           (((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w)));
+  }
+  // Three sums: lanes share them out as they halve, six exchanges for the three.
+  __device__ __forceinline__ void sum3(float (&v)[3]) {
+    const int lane = threadIdx.x & 31;
+    const bool h16 = lane & 16, h8 = lane & 8;
+    float x = (h16 ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, h16 ? v[0] : v[1], 16);
+    const float z = v[2] + __shfl_xor_sync(0xffffffffu, v[2], 16);
+    x = (h8 ? z : x) + __shfl_xor_sync(0xffffffffu, h8 ? x : z, 8);
 #pragma unroll
-      for (int m = 0; m < M; ++m) v[m] += __shfl_xor_sync(0xffffffffu, v[m], o);
-    if (WARP) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
-    float* to = red + turn * kMaxSums * 32;  // the sums after next are two barriers away
-    turn ^= 1;
-    if (lane == 0)
-#pragma unroll
-      for (int m = 0; m < M; ++m) to[m * 32 + warp] = v[m];
+    for (int o = 4; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    // lanes 0 .. 7 hold the first sum, 16 .. 23 the second, 8 .. 15 and 24 .. 31 the third
+    if (WARP) {
+      v[0] = __shfl_sync(0xffffffffu, x, 0);
+      v[1] = __shfl_sync(0xffffffffu, x, 16);
+      v[2] = __shfl_sync(0xffffffffu, x, 8);
+      return;
+    }
+    if ((lane & 7) == 0 && lane < 24) red[(lane == 0 ? 0 : lane == 16 ? 16 : 32) + (t >> 5)] = x;
     __syncthreads();
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-      float s = lane < warps ? to[m * 32 + lane] : 0.f;
+    for (int m = 0; m < 3; ++m) v[m] = red[m * 16 + (lane & 15)];
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);  // at most 16 warps
-      v[m] = __shfl_sync(0xffffffffu, s, 0);
-    }
+    for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+      for (int m = 0; m < 3; ++m) v[m] += __shfl_xor_sync(0xffffffffu, v[m], o);
+    swap();
   }
+  // Sums use the two slots in turn: a slot is written again two barriers after it was.
+  __device__ __forceinline__ void swap() { red = reinterpret_cast<float*>(reinterpret_cast<uintptr_t>(red) ^ 256u); }
 };
+// The slots lie 256 bytes apart in 512 aligned bytes.
+constexpr int kRsRedFloats = 64 + RowGroup<false>::kSlot;
 
-// Rows on their way: with KE > 1 through shared memory, `arrays` rows to a stage; with KE == 1 read where they are.
+// Rows on their way through shared memory, `arrays` of them to a stage.
+// KE > 1: rows of whole 16-byte vectors.  A thread copies the vectors that it will read, so a wait for its own copies is
+// all that a stage needs.
+// KE == 1: rows at any alignment.  The aligned 16-byte blocks that hold a row are copied as they are, whoever reads them,
+// and a barrier follows the wait; elements are then read one at a time, neighbouring ones by neighbouring threads.
+// kDirect: fp32 rows above 8192 elements, five of which shared memory has no room for, are read where they are.
+extern __shared__ __align__(16) unsigned char rs_ring[];
+
 template <typename T, int KE, int K>
 struct RowFeed {
-  static constexpr bool kStaged = KE > 1;
-  const T* base[5];
-  int64_t ld[5];
-  uint32_t addr;            // shared memory of this row group
-  const unsigned char* mem;
-  int arrays, units, stages;
-  __device__ __forceinline__ int unit(int t, int nt, int k) const { return t + k * nt; }
-  __device__ __forceinline__ void fetch(int64_t row, int64_t N, int stage, int t, int nt) {
-    if (!kStaged) return;
-    if (row < N) {
+  static constexpr bool kDirect = sizeof(T) == 4 && KE * K == 32;
+  const T* next[5];        // the row that is fetched next, at this thread's first element (KE > 1) or its beginning
+  const T* here[5];        // KE == 1: the row that is read
+  int64_t hop[5];          // elements from one of the group's rows to the next
+  uint32_t offset, pitch;  // of this row group's part of the ring, of a row
+  int arrays, units, t, nt;
+  int64_t left;            // rows that are still to be fetched
+  template <bool WARP>
+  __device__ __forceinline__ void init(const ResidualParams& p, int arrays_, const RowGroup<WARP>& g) {
+    arrays = arrays_;
+    units = p.d / KE;
+    pitch = (uint32_t)p.pitch;
+    offset = WARP ? (uint32_t)(threadIdx.x >> 5) * (uint32_t)(p.stages * arrays) * pitch : 0u;
+    t = g.t;
+    nt = g.nt;
+    left = g.first < p.N ? (p.N - 1 - g.first) / g.step + 1 : 0;
+  }
+  template <bool WARP>
+  __device__ __forceinline__ void array(int a, const void* base, int64_t ld, const RowGroup<WARP>& g) {
+    next[a] = static_cast<const T*>(base) + g.first * ld + (KE > 1 ? t * KE : 0);
+    here[a] = next[a];
+    hop[a] = g.step * ld;
+  }
+  // Starts the copies of the next row into a stage; one group of copies whether there is a row or not.
+  __device__ __forceinline__ void fetch(int stage) {
+    if constexpr (kDirect) return;
+    if (left > 0) {
+      --left;
 #pragma unroll
       for (int a = 0; a < 5; ++a)
         if (a < arrays) {
-          const T* src = base[a] + row * ld[a];
-          const uint32_t dst = addr + (uint32_t)((stage * arrays + a) * units) * 16u;
+          const uint32_t dst = smem_u32(rs_ring) + offset + (uint32_t)(stage * arrays + a) * pitch + (uint32_t)t * 16u;
+          if constexpr (KE > 1) {
 #pragma unroll
-          for (int k = 0; k < K; ++k) {
-            const int u = unit(t, nt, k);
-            if (u < units) copy_async_16(dst + (uint32_t)u * 16u, src + (int64_t)u * KE);
+            for (int k = 0; k < K; ++k)
+              if (t + k * nt < units) copy_async_16(dst + (uint32_t)(k * nt) * 16u, next[a] + k * nt * KE);
+          } else {
+            const uintptr_t from = reinterpret_cast<uintptr_t>(next[a]) & ~(uintptr_t)15;
+            const int blocks = (int)((reinterpret_cast<uintptr_t>(next[a] + units) - from + 15) >> 4);
+            for (int u = t; u < blocks; u += nt)
+              copy_async_16(dst + (uint32_t)(u - t) * 16u, reinterpret_cast<const void*>(from + (uintptr_t)u * 16));
           }
+          next[a] += hop[a];
         }
     }
     copy_async_commit();
   }
-  __device__ __forceinline__ void read(int a, int64_t row, int stage, int u, float (&f)[KE]) const {
-    if constexpr (kStaged) {
-      Elem<T>::widen(*reinterpret_cast<const uint4*>(mem + ((size_t)(stage * arrays + a) * units + u) * 16), f);
+  // Waits for the row of `stage` and starts the copies of the row that is `ahead` of it into the slot that was read in
+  // the round before.
+  template <bool WARP>
+  __device__ __forceinline__ void turn(int stage, int ahead, const RowGroup<WARP>& g) {
+    if constexpr (kDirect) {
+    } else if constexpr (KE > 1) {
+      fetch(stage == 0 ? ahead : stage - 1);
+      copy_async_wait(ahead);
+    } else if (ahead) {
+      copy_async_wait(ahead - 1);
+      g.sync();
+      fetch(stage == 0 ? ahead : stage - 1);
     } else {
-      f[0] = Elem<T>::one(base[a] + row * ld[a], u);
+      g.sync();
+      fetch(0);
+      copy_async_wait(0);
+      g.sync();
+    }
+  }
+  // This thread's first element of an array's row of a stage.
+  __device__ __forceinline__ const unsigned char* place(int a, int stage) const {
+    const unsigned char* p = nullptr;
+    if constexpr (KE == 1) {
+#pragma unroll
+      for (int i = 0; i < 5; ++i)
+        if (i == a) p = reinterpret_cast<const unsigned char*>(here[i]);
+      if constexpr (kDirect) return p + t * sizeof(T);
+      return rs_ring + offset + (uint32_t)(stage * arrays + a) * pitch + (reinterpret_cast<uintptr_t>(p) & 15) + t * sizeof(T);
+    }
+    return rs_ring + offset + (uint32_t)(stage * arrays + a) * pitch + (uint32_t)t * 16u;
+  }
+  __device__ __forceinline__ void advance() {
+    if constexpr (KE == 1) {
+#pragma unroll
+      for (int a = 0; a < 5; ++a)
+        if (a < arrays) here[a] += hop[a];
+    }
+  }
+  __device__ __forceinline__ void read(const unsigned char* place, int k, float (&f)[KE]) const {
+    if constexpr (KE > 1) {
+      Elem<T>::widen(reinterpret_cast<const uint4*>(place)[k * nt], f);
+    } else {
+      f[0] = Elem<T>::one(place, k * nt);
     }
   }
 };
 
-template <typename T, int KE, int K, bool WARP>
-__device__ __forceinline__ RowFeed<T, KE, K> row_feed(const ResidualParams& p, unsigned char* ring, int arrays) {
-  RowFeed<T, KE, K> f;
-  f.arrays = arrays;
-  f.units = p.d / KE;
-  f.stages = p.stages;
-  f.mem = ring + (WARP ? (size_t)(threadIdx.x >> 5) * p.stages * arrays * f.units * 16 : 0);
-  f.addr = smem_u32(f.mem);
-  return f;
+// Arithmetic on a vector's elements, two wide.
+template <int KE>
+__device__ __forceinline__ void v_fma(float (&o)[KE], const float (&a)[KE], const float (&b)[KE], const float (&c)[KE]) {
+  if constexpr (KE == 1) {
+    o[0] = fmaf(a[0], b[0], c[0]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < KE; i += 2) {
+      const float2 r = __ffma2_rn(make_float2(a[i], a[i + 1]), make_float2(b[i], b[i + 1]), make_float2(c[i], c[i + 1]));
+      o[i] = r.x;
+      o[i + 1] = r.y;
+    }
+  }
+}
+template <int KE>
+__device__ __forceinline__ void v_fma(float (&o)[KE], const float (&a)[KE], float b, const float (&c)[KE]) {
+  if constexpr (KE == 1) {
+    o[0] = fmaf(a[0], b, c[0]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < KE; i += 2) {
+      const float2 r = __ffma2_rn(make_float2(a[i], a[i + 1]), make_float2(b, b), make_float2(c[i], c[i + 1]));
+      o[i] = r.x;
+      o[i + 1] = r.y;
+    }
+  }
+}
+template <int KE>
+__device__ __forceinline__ void v_mul(float (&o)[KE], const float (&a)[KE], const float (&b)[KE]) {
+  if constexpr (KE == 1) {
+    o[0] = a[0] * b[0];
+  } else {
+#pragma unroll
+    for (int i = 0; i < KE; i += 2) {
+      const float2 r = __fmul2_rn(make_float2(a[i], a[i + 1]), make_float2(b[i], b[i + 1]));
+      o[i] = r.x;
+      o[i + 1] = r.y;
+    }
+  }
+}
+template <int KE>
+__device__ __forceinline__ void v_mul(float (&o)[KE], const float (&a)[KE], float b) {
+  if constexpr (KE == 1) {
+    o[0] = a[0] * b;
+  } else {
+#pragma unroll
+    for (int i = 0; i < KE; i += 2) {
+      const float2 r = __fmul2_rn(make_float2(a[i], a[i + 1]), make_float2(b, b));
+      o[i] = r.x;
+      o[i + 1] = r.y;
+    }
+  }
+}
+template <int KE>
+__device__ __forceinline__ void v_dot(float2& s, const float (&a)[KE], const float (&b)[KE]) {
+  if constexpr (KE == 1) {
+    s.x = fmaf(a[0], b[0], s.x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < KE; i += 2) s = __ffma2_rn(make_float2(a[i], a[i + 1]), make_float2(b[i], b[i + 1]), s);
+  }
+}
+template <int KE>
+__device__ __forceinline__ void v_set(float (&o)[KE], float v) {
+#pragma unroll
+  for (int i = 0; i < KE; ++i) o[i] = v;
+}
+
+// Weights of a thread's columns, kept in registers over its rows, or (KEEP false: rows so wide that the registers are
+// needed elsewhere) formed again for each.
+template <int KE, int K, bool KEEP>
+struct ColumnFactor {
+  float w[KEEP ? K : 1][KE];
+  template <typename F>
+  __device__ __forceinline__ void init(int t, int nt, int units, F form) {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (t + k * nt < units) form(t + k * nt, w[k]);
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ const float (&get(int k, int u, F form))[KE] {
+    if constexpr (KEEP) {
+      return w[k];
+    } else {
+      form(u, w[0]);
+      return w[0];
+    }
+  }
+};
+
+// What a call has.  COMMON: the form that blocks with both norms have, known when the kernel is compiled (16384 x 3584
+// bf16, gradient: %COMMON%).
+template <bool COMMON>
+struct ResidualHas {
+  bool y, post, pre, full, dx_out;
+  __device__ __forceinline__ explicit ResidualHas(const ResidualParams& p) {
+    y = COMMON || p.y != nullptr;
+    post = COMMON || p.w_post != nullptr;
+    pre = COMMON || p.w_pre != nullptr;
+    full = !COMMON && p.gate_kind == kGateFull;
+    dx_out = COMMON || p.dx_out != nullptr;
+  }
+};
+
+// A column's factors: of h, and of y (b w_post, and a channel's gate).
+template <int KE>
+__device__ __forceinline__ void form_pre(const ResidualParams& p, bool pre, int c, float (&w)[KE]) {
+  if (pre) load_weight<KE>(p.w_pre, p.weight_type, c, p.weight_offset, w);
+  else v_set(w, 0.f);
+}
+template <int KE>
+__device__ __forceinline__ void form_y(const ResidualParams& p, bool post, int c, float (&w)[KE]) {
+  if (post) load_weight<KE>(p.w_post, p.weight_type, c, p.weight_offset, w);
+  else v_set(w, 1.f);
+  v_mul(w, w, p.b);
+  if (p.gate_kind == kGateColumn) {
+    float g[KE];
+    load_weight<KE>(p.gate, p.gate_type, c, 0.f, g);
+    v_mul(w, w, g);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ forward
-template <typename T, int KE, int K, bool WARP>
+template <typename T, int KE, int K, bool WARP, bool COMMON>
 __global__ void __launch_bounds__(WARP ? 256 : kRsMaxThreads) residual_fwd_kernel(ResidualParams p) {
-  extern __shared__ __align__(16) unsigned char ring[];
-  __shared__ float red[2 * RowGroup<WARP>::kMaxSums * 32];
+  __shared__ __align__(512) float red[kRsRedFloats];
   RowGroup<WARP> grp(red);
-  const bool has_y = p.y != nullptr, post = p.w_post != nullptr, pre = p.w_pre != nullptr;
-  const int arrays = 1 + has_y + (p.gate_kind == kGateFull);
-  RowFeed<T, KE, K> feed = row_feed<T, KE, K, WARP>(p, ring, arrays);
-  feed.base[0] = static_cast<const T*>(p.x);
-  feed.ld[0] = p.ld_x;
-  feed.base[1] = static_cast<const T*>(p.y);
-  feed.ld[1] = p.ld_y;
-  feed.base[2] = static_cast<const T*>(p.gate);
-  feed.ld[2] = p.ld_gate;
-  const int t = grp.t, nt = grp.nt;
-  for (int s = 0; s + 1 < p.stages; ++s) feed.fetch(grp.first + s * grp.step, p.N, s, t, nt);
+  const ResidualHas<COMMON> has(p);
+  RowFeed<T, KE, K> feed;
+  feed.init(p, 1 + has.y + has.full, grp);
+  feed.array(0, p.x, p.ld_x, grp);
+  feed.array(1, p.y, p.ld_y, grp);
+  feed.array(2, p.gate, p.ld_gate, grp);
+  feed.array(3, nullptr, 0, grp);
+  feed.array(4, nullptr, 0, grp);
+  const int t = grp.t, nt = grp.nt, units = feed.units, ahead = p.stages - 1;
+  for (int s = 0; s < ahead; ++s) feed.fetch(s);
+  constexpr bool kKeep = KE * K <= 16;
+  ColumnFactor<KE, K, kKeep> f_pre, f_y;
+  auto make_pre = [&](int u, float (&w)[KE]) { form_pre<KE>(p, has.pre, u * KE, w); };
+  auto make_y = [&](int u, float (&w)[KE]) { form_y<KE>(p, has.post, u * KE, w); };
+  f_pre.init(t, nt, units, make_pre);
+  f_y.init(t, nt, units, make_y);
   const float inv_d = 1.f / (float)p.d;
-  int stage = 0, ahead = p.stages - 1;
+  T* x_out = static_cast<T*>(p.x_out) + grp.first * p.ld_xo + t * KE;
+  T* h = static_cast<T*>(p.h) + grp.first * p.ld_h + t * KE;
+  int stage = 0;
   for (int64_t row = grp.first; row < p.N; row += grp.step) {
-    // the slot that this fetch fills was read in the round before
-    feed.fetch(row + (int64_t)ahead * grp.step, p.N, stage == 0 ? p.stages - 1 : stage - 1, t, nt);
-    float g_row = p.b;
-    if (p.gate_kind == kGateRow) g_row *= load_one(p.gate, p.gate_type, row * p.ld_gate);
-    if (feed.kStaged) copy_async_wait(ahead);
-    if (post) {
-      float ss[1] = {0.f};
+    float g_row = 1.f;
+    if (p.gate_kind == kGateRow) g_row = load_one(p.gate, p.gate_type, row * p.ld_gate);
+    feed.turn(stage, ahead, grp);
+    const unsigned char *at_x = feed.place(0, stage), *at_y = feed.place(1, stage), *at_g = feed.place(2, stage);
+    float v[K][KE];
+    float2 ss = make_float2(0.f, 0.f);
+    if (has.y) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int u = feed.unit(t, nt, k);
-        if (u < feed.units) {
-          float f[KE];
-          feed.read(1, row, stage, u, f);
-#pragma unroll
-          for (int i = 0; i < KE; ++i) ss[0] = fmaf(f[i], f[i], ss[0]);
+      for (int k = 0; k < K; ++k)
+        if (t + k * nt < units) {
+          feed.read(at_y, k, v[k]);
+          v_dot(ss, v[k], v[k]);
         }
+      if (has.post) {
+        const float r = 1.f / sqrtf(fmaf(grp.sum(ss.x + ss.y), inv_d, p.eps));
+        if (t == 0 && p.rstd_post) p.rstd_post[row] = r;
+        g_row *= r;
       }
-      grp.sum(ss);
-      const float r = 1.f / sqrtf(fmaf(ss[0], inv_d, p.eps));
-      if (t == 0 && p.rstd_post) p.rstd_post[row] = r;
-      g_row *= r;
     }
-    float v[K][KE], ss[1] = {0.f};
+    ss = make_float2(0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int u = feed.unit(t, nt, k);
-      if (u < feed.units) {
-        const int c = u * KE;
-        feed.read(0, row, stage, u, v[k]);
-#pragma unroll
-        for (int i = 0; i < KE; ++i) v[k][i] *= p.a;
-        if (has_y) {
-          float f[KE], w[KE];
-          feed.read(1, row, stage, u, f);
-#pragma unroll
-          for (int i = 0; i < KE; ++i) f[i] *= g_row;
-          if (post) {
-            load_weight<KE>(p.w_post, p.weight_type, c, p.weight_offset, w);
-#pragma unroll
-            for (int i = 0; i < KE; ++i) f[i] *= w[i];
+      const int u = t + k * nt;
+      if (u < units) {
+        float x[KE];
+        feed.read(at_x, k, x);
+        if (has.y) {
+          v_mul(v[k], v[k], g_row);
+          v_mul(v[k], v[k], f_y.get(k, u, make_y));
+          if (has.full) {
+            float g[KE];
+            feed.read(at_g, k, g);
+            v_mul(v[k], v[k], g);
           }
-          if (p.gate_kind >= kGateColumn) {
-            if (p.gate_kind == kGateColumn) load_weight<KE>(p.gate, p.gate_type, c, 0.f, w);
-            else feed.read(2, row, stage, u, w);
-#pragma unroll
-            for (int i = 0; i < KE; ++i) f[i] *= w[i];
-          }
-#pragma unroll
-          for (int i = 0; i < KE; ++i) v[k][i] += f[i];
+          v_fma(v[k], x, p.a, v[k]);
+        } else {
+          v_mul(v[k], x, p.a);
         }
-#pragma unroll
-        for (int i = 0; i < KE; ++i) ss[0] = fmaf(v[k][i], v[k][i], ss[0]);
-        if (p.x_out) Raw<T, KE>::store(static_cast<T*>(p.x_out) + row * p.ld_xo + c, v[k]);
+        v_dot(ss, v[k], v[k]);
+        if (COMMON || p.x_out) Raw<T, KE>::store(x_out + k * nt * KE, v[k]);
       }
     }
-    if (pre) {
-      grp.sum(ss);
-      const float r = 1.f / sqrtf(fmaf(ss[0], inv_d, p.eps));
+    if (has.pre) {
+      const float r = 1.f / sqrtf(fmaf(grp.sum(ss.x + ss.y), inv_d, p.eps));
       if (t == 0 && p.rstd_pre) p.rstd_pre[row] = r;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const int u = feed.unit(t, nt, k);
-        if (u < feed.units) {
-          float w[KE];
-          load_weight<KE>(p.w_pre, p.weight_type, u * KE, p.weight_offset, w);
-#pragma unroll
-          for (int i = 0; i < KE; ++i) w[i] *= v[k][i] * r;
-          Raw<T, KE>::store(static_cast<T*>(p.h) + row * p.ld_h + u * KE, w);
+        const int u = t + k * nt;
+        if (u < units) {
+          v_mul(v[k], v[k], r);
+          v_mul(v[k], v[k], f_pre.get(k, u, make_pre));
+          Raw<T, KE>::store(h + k * nt * KE, v[k]);
         }
       }
     }
-    stage = stage + 1 == p.stages ? 0 : stage + 1;
+    x_out += grp.step * p.ld_xo;
+    h += grp.step * p.ld_h;
+    feed.advance();
+    stage = stage == ahead ? 0 : stage + 1;
   }
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-template <typename T, int KE, int K, bool WARP>
+// Of a column only two sums are needed: dw_pre, and S = sum_n t yh (times a row's or an element's gate).  Without these
+// gates dw_post = b g S and dg = b w_post S, both per channel; with them dw_post = b S.
+template <typename T, int KE, int K, bool WARP, bool COMMON>
 __global__ void __launch_bounds__(WARP ? 256 : kRsMaxThreads) residual_bwd_kernel(ResidualParams p) {
-  extern __shared__ __align__(16) unsigned char ring[];
-  __shared__ float red[2 * RowGroup<WARP>::kMaxSums * 32];
+  __shared__ __align__(512) float red[kRsRedFloats];
   RowGroup<WARP> grp(red);
-  const bool has_y = p.y != nullptr, post = p.w_post != nullptr, pre = p.w_pre != nullptr, has_dx = p.dx_out != nullptr;
+  const ResidualHas<COMMON> has(p);
   // the arrays of a stage, in this order, those that there are
-  const int at_xo = 0, at_dh = 1, at_dx = pre ? 2 : 0, at_y = at_dx + has_dx, at_g = at_y + has_y;
-  const int arrays = at_g + (p.gate_kind == kGateFull);
-  RowFeed<T, KE, K> feed = row_feed<T, KE, K, WARP>(p, ring, arrays);
-  auto put = [&](int at, const void* base, int64_t ld) {
+  const int i_dx = has.pre ? 2 : 0, i_y = i_dx + has.dx_out, i_g = i_y + has.y;
+  RowFeed<T, KE, K> feed;
+  feed.init(p, i_g + has.full, grp);
 #pragma unroll
-    for (int a = 0; a < 5; ++a)
-      if (a == at) {
-        feed.base[a] = static_cast<const T*>(base);
-        feed.ld[a] = ld;
-      }
-  };
-  if (pre) {
-    put(at_xo, p.x_out, p.ld_xo);
-    put(at_dh, p.dh, p.ld_dh);
+  for (int a = 0; a < 5; ++a) {
+    const void* from = nullptr;
+    int64_t ld = 0;
+    if (has.pre && a == 0) { from = p.x_out; ld = p.ld_xo; }
+    if (has.pre && a == 1) { from = p.dh; ld = p.ld_dh; }
+    if (has.dx_out && a == i_dx) { from = p.dx_out; ld = p.ld_dxo; }
+    if (has.y && a == i_y) { from = p.y; ld = p.ld_y; }
+    if (has.full && a == i_g) { from = p.gate; ld = p.ld_gate; }
+    feed.array(a, from, ld, grp);
   }
-  if (has_dx) put(at_dx, p.dx_out, p.ld_dxo);
-  if (has_y) put(at_y, p.y, p.ld_y);
-  if (p.gate_kind == kGateFull) put(at_g, p.gate, p.ld_gate);
-  const int t = grp.t, nt = grp.nt;
-  for (int s = 0; s + 1 < p.stages; ++s) feed.fetch(grp.first + s * grp.step, p.N, s, t, nt);
+  const int t = grp.t, nt = grp.nt, units = feed.units, ahead = p.stages - 1;
+  for (int s = 0; s < ahead; ++s) feed.fetch(s);
+  constexpr bool kKeep = KE * K <= 16;
+  ColumnFactor<KE, K, kKeep> f_pre, f_y;
+  auto make_pre = [&](int u, float (&w)[KE]) { form_pre<KE>(p, has.pre, u * KE, w); };
+  auto make_y = [&](int u, float (&w)[KE]) { form_y<KE>(p, has.post, u * KE, w); };
+  f_pre.init(t, nt, units, make_pre);
+  f_y.init(t, nt, units, make_y);
   const float inv_d = 1.f / (float)p.d;
-  float a_pre[K][KE], a_post[K][KE], a_gate[K][KE];
+  const bool second = has.y && (has.post || p.gate_kind == kGateRow);
+  T* dx = static_cast<T*>(p.dx) + grp.first * p.ld_dx + t * KE;
+  T* dy = static_cast<T*>(p.dy) + grp.first * p.ld_dy + t * KE;
+  float a_pre[K][KE], a_y[K][KE];
 #pragma unroll
-  for (int k = 0; k < K; ++k)
-#pragma unroll
-    for (int i = 0; i < KE; ++i) a_pre[k][i] = a_post[k][i] = a_gate[k][i] = 0.f;
-  int stage = 0, ahead = p.stages - 1;
+  for (int k = 0; k < K; ++k) {
+    v_set(a_pre[k], 0.f);
+    v_set(a_y[k], 0.f);
+  }
+  int stage = 0;
   for (int64_t row = grp.first; row < p.N; row += grp.step) {
-    feed.fetch(row + (int64_t)ahead * grp.step, p.N, stage == 0 ? p.stages - 1 : stage - 1, t, nt);
-    const float r_x = pre ? p.rstd_pre[row] : 0.f, r_y = post ? p.rstd_post[row] : 1.f;
+    const float r_x = has.pre ? p.rstd_pre[row] : 0.f, r_y = has.post ? p.rstd_post[row] : 1.f;
     const float g_row = p.gate_kind == kGateRow ? load_one(p.gate, p.gate_type, row * p.ld_gate) : 1.f;
-    if (feed.kStaged) copy_async_wait(ahead);
-    // b w_post g r_y of a column: what y is multiplied with to give A (a row's gate comes later)
-    auto branch = [&](int u, float (&e)[KE]) {
+    feed.turn(stage, ahead, grp);
+    const unsigned char *at_xo = feed.place(0, stage), *at_dh = feed.place(1, stage), *at_dx = feed.place(i_dx, stage),
+                        *at_y = feed.place(i_y, stage), *at_g = feed.place(i_g, stage);
+    // c = dx' + r_x w_pre dh, and the sums of (w_pre dh) xh, A c and A xh
+    float c[K][KE];
+    float2 s0 = make_float2(0.f, 0.f), s1 = s0, s2 = s0;
 #pragma unroll
-      for (int i = 0; i < KE; ++i) e[i] = p.b;
-      float w[KE];
-      if (post) {
-        load_weight<KE>(p.w_post, p.weight_type, u * KE, p.weight_offset, w);
-#pragma unroll
-        for (int i = 0; i < KE; ++i) e[i] *= w[i];
-      }
-      if (p.gate_kind >= kGateColumn) {
-        if (p.gate_kind == kGateColumn) load_weight<KE>(p.gate, p.gate_type, u * KE, 0.f, w);
-        else feed.read(at_g, row, stage, u, w);
-#pragma unroll
-        for (int i = 0; i < KE; ++i) e[i] *= w[i];
-      }
-    };
-    const bool second = has_y && (post || p.gate_kind == kGateRow);
-    float s[3] = {0.f, 0.f, 0.f};
-    if (pre || second) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int u = feed.unit(t, nt, k);
-        if (u < feed.units) {
-          float q[KE], xo[KE], tt[KE];
-#pragma unroll
-          for (int i = 0; i < KE; ++i) q[i] = xo[i] = tt[i] = 0.f;
-          if (pre) {
-            float w[KE];
-            feed.read(at_dh, row, stage, u, q);
-            feed.read(at_xo, row, stage, u, xo);
-            load_weight<KE>(p.w_pre, p.weight_type, u * KE, p.weight_offset, w);
-#pragma unroll
-            for (int i = 0; i < KE; ++i) {
-              q[i] *= w[i];
-              xo[i] *= r_x;
-              s[0] = fmaf(q[i], xo[i], s[0]);
-            }
+    for (int k = 0; k < K; ++k) {
+      const int u = t + k * nt;
+      if (u < units) {
+        float xh[KE];
+        if (has.dx_out) feed.read(at_dx, k, c[k]);
+        else v_set(c[k], 0.f);
+        if (has.pre) {
+          float dh[KE];
+          feed.read(at_dh, k, dh);
+          feed.read(at_xo, k, xh);
+          v_mul(xh, xh, r_x);
+          v_fma(a_pre[k], dh, xh, a_pre[k]);
+          v_mul(dh, dh, f_pre.get(k, u, make_pre));
+          v_dot(s0, dh, xh);
+          v_fma(c[k], dh, r_x, c[k]);
+        } else {
+          v_set(xh, 0.f);
+        }
+        if (second) {
+          float A[KE];
+          feed.read(at_y, k, A);
+          v_mul(A, A, f_y.get(k, u, make_y));
+          if (has.full) {
+            float g[KE];
+            feed.read(at_g, k, g);
+            v_mul(A, A, g);
           }
-          if (second) {
-            float e[KE], y[KE];
-            if (has_dx) feed.read(at_dx, row, stage, u, tt);
-            feed.read(at_y, row, stage, u, y);
-            branch(u, e);
-#pragma unroll
-            for (int i = 0; i < KE; ++i) {
-              const float A = e[i] * (y[i] * r_y);
-              s[1] = fmaf(A, fmaf(r_x, q[i], tt[i]), s[1]);
-              s[2] = fmaf(A, xo[i], s[2]);
-            }
-          }
+          v_dot(s1, A, c[k]);
+          v_dot(s2, A, xh);
         }
       }
-      grp.sum(s);
     }
-    const float m1 = r_x * s[0] * inv_d;                 // t = dx' + r_x q - m1 xh
-    const float dg_row = fmaf(-m1, s[2], s[1]);          // sum of A t without a row's gate
-    const float m2 = g_row * dg_row * inv_d;
+    float s[3] = {s0.x + s0.y, (s1.x + s1.y) * r_y, (s2.x + s2.y) * r_y};
+    if (has.pre || second) grp.sum3(s);
+    const float m1 = r_x * s[0] * inv_d;         // t = c - m1 xh
+    const float dg_row = fmaf(-m1, s[2], s[1]);  // sum of A t without a row's gate
+    const float m2 = g_row * dg_row * inv_d, e_row = g_row * r_y;
+    const float m1x = -m1 * r_x, m2y = -m2 * r_y * r_y;  // with x' and y as they were stored
     if (p.gate_kind == kGateRow && t == 0 && p.dgate) static_cast<float*>(p.dgate)[row * p.ld_dg] = dg_row;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int u = feed.unit(t, nt, k);
-      if (u < feed.units) {
-        const int c = u * KE;
-        float tt[KE];
-#pragma unroll
-        for (int i = 0; i < KE; ++i) tt[i] = 0.f;
-        if (has_dx) feed.read(at_dx, row, stage, u, tt);
-        if (pre) {
-          float q[KE], xo[KE], w[KE];
-          feed.read(at_dh, row, stage, u, q);
-          feed.read(at_xo, row, stage, u, xo);
-          load_weight<KE>(p.w_pre, p.weight_type, c, p.weight_offset, w);
-#pragma unroll
-          for (int i = 0; i < KE; ++i) {
-            xo[i] *= r_x;
-            a_pre[k][i] = fmaf(q[i], xo[i], a_pre[k][i]);
-            tt[i] = fmaf(-m1, xo[i], fmaf(r_x, q[i] * w[i], tt[i]));
-          }
+      const int u = t + k * nt;
+      if (u < units) {
+        if (has.pre) {
+          float xo[KE];
+          feed.read(at_xo, k, xo);
+          v_fma(c[k], xo, m1x, c[k]);
         }
-        float o_dx[KE];
-#pragma unroll
-        for (int i = 0; i < KE; ++i) o_dx[i] = p.a * tt[i];
-        if (has_y) {
-          float y[KE], w[KE], g[KE];
-          feed.read(at_y, row, stage, u, y);
-#pragma unroll
-          for (int i = 0; i < KE; ++i) {
-            y[i] *= r_y;
-            w[i] = 1.f;
-            g[i] = g_row;
-            tt[i] *= p.b;
-          }
-          if (post) load_weight<KE>(p.w_post, p.weight_type, c, p.weight_offset, w);
-          if (p.gate_kind >= kGateColumn) {
-            if (p.gate_kind == kGateColumn) load_weight<KE>(p.gate, p.gate_type, c, 0.f, g);
-            else feed.read(at_g, row, stage, u, g);
-            float o[KE];
-#pragma unroll
-            for (int i = 0; i < KE; ++i) {
-              o[i] = tt[i] * y[i] * w[i];
-              a_gate[k][i] += o[i];
-            }
-            if (p.gate_kind == kGateFull && p.dgate)
-              Raw<T, KE>::store(static_cast<T*>(p.dgate) + row * p.ld_dg + c, o);
-          }
-#pragma unroll
-          for (int i = 0; i < KE; ++i) {
-            tt[i] *= g[i];
-            if (post) {
-              a_post[k][i] = fmaf(tt[i], y[i], a_post[k][i]);
-              tt[i] = r_y * fmaf(-m2, y[i], tt[i] * w[i]);
-            }
-          }
-          if (p.dy) Raw<T, KE>::store(static_cast<T*>(p.dy) + row * p.ld_dy + c, tt);
+        float y[KE], g[KE], o[KE];
+        if (has.y) feed.read(at_y, k, y);
+        if (has.full) feed.read(at_g, k, g);
+        if (COMMON || p.dx) {
+          v_mul(o, c[k], p.a);
+          Raw<T, KE>::store(dx + k * nt * KE, o);
         }
-        if (p.dx) Raw<T, KE>::store(static_cast<T*>(p.dx) + row * p.ld_dx + c, o_dx);
+        if (has.y) {
+          v_mul(o, c[k], f_y.get(k, u, make_y));  // b w_post g t
+          if (has.full) {
+            float e[KE];
+            v_mul(c[k], c[k], g);
+            v_mul(e, y, r_y);
+            v_fma(a_y[k], c[k], e, a_y[k]);
+            v_mul(e, e, o);
+            if (p.dgate) Raw<T, KE>::store(static_cast<T*>(p.dgate) + row * p.ld_dg + u * KE, e);
+            v_mul(o, o, g);
+          } else {
+            v_mul(c[k], c[k], e_row);
+            v_fma(a_y[k], c[k], y, a_y[k]);
+          }
+          v_mul(o, o, e_row);
+          if (has.post) v_fma(o, y, m2y, o);
+          if (COMMON || p.dy) Raw<T, KE>::store(dy + k * nt * KE, o);
+        }
       }
     }
-    stage = stage + 1 == p.stages ? 0 : stage + 1;
+    dx += grp.step * p.ld_dx;
+    dy += grp.step * p.ld_dy;
+    feed.advance();
+    stage = stage == ahead ? 0 : stage + 1;
   }
   // this worker's sums over its rows
-  const int64_t workers = grp.step;
+  const int64_t kind = grp.step * p.d;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const int u = feed.unit(t, nt, k);
-    if (u < feed.units) {
-      const int64_t at = grp.first * p.d + u * KE, kind = workers * p.d;
-      if (p.kind_pre >= 0) Raw<float, KE>::store(p.part + p.kind_pre * kind + at, a_pre[k]);
-      if (p.kind_post >= 0) Raw<float, KE>::store(p.part + p.kind_post * kind + at, a_post[k]);
-      if (p.kind_gate >= 0) Raw<float, KE>::store(p.part + p.kind_gate * kind + at, a_gate[k]);
+    const int u = t + k * nt;
+    if (u < units) {
+      float* to = p.part + grp.first * p.d + u * KE;
+      if (p.kind_pre >= 0) Raw<float, KE>::store(to + p.kind_pre * kind, a_pre[k]);
+      float w[KE], g[KE];
+#pragma unroll
+      for (int i = 0; i < KE; ++i) w[i] = g[i] = 1.f;
+      if (p.kind_post >= 0) {
+        if (p.gate_kind == kGateColumn) load_weight<KE>(p.gate, p.gate_type, u * KE, 0.f, g);
+#pragma unroll
+        for (int i = 0; i < KE; ++i) g[i] *= p.b * a_y[k][i];
+        Raw<float, KE>::store(to + p.kind_post * kind, g);
+      }
+      if (p.kind_gate >= 0) {
+        if (has.post) load_weight<KE>(p.w_post, p.weight_type, u * KE, p.weight_offset, w);
+#pragma unroll
+        for (int i = 0; i < KE; ++i) w[i] *= p.b * a_y[k][i];
+        Raw<float, KE>::store(to + p.kind_gate * kind, w);
+      }
     }
   }
 }

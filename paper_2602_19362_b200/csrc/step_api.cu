@@ -1,5 +1,5 @@
-// Host side of the operators around the LM head declared in include/oapl.h: the embedding, the residual norm, the
-// gradient norm and clipping, and the adjustments of logits.  Checks, workspaces and launches.
+// Host side of operators around the LM head declared in include/oapl.h: the embedding, the gradient norm and clipping,
+// and the adjustments of logits.  Checks, workspaces and launches.
 #include <cuda_runtime.h>
 
 #include <cmath>
@@ -9,36 +9,8 @@
 #include "grad_clip.cuh"
 #include "host_common.cuh"
 #include "logits_adjust.cuh"
-#include "residual_norm.cuh"
 
 namespace oapl {
-
-constexpr int64_t kMaxRows = 2000000000;
-constexpr int64_t kMaxGrid = 2147483647;
-
-static size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-static bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
-// A matrix in memory, to see what overlaps.
-struct Place {
-  const void* base;
-  int64_t rows, cols, ld;
-  int es;
-};
-enum Overlap { kApart, kSameRows, kMixed };
-// kSameRows: the same rows of the same elements.  Matrices of one row pitch may lie between one another's rows.
-static Overlap overlap(const Place& p, const Place& q) {
-  using Wide = unsigned __int128;
-  if (!p.base || !q.base) return kApart;
-  const Wide a = (uintptr_t)p.base, b = (uintptr_t)q.base, ra = (Wide)p.cols * p.es, rb = (Wide)q.cols * q.es;
-  const Wide pa = (Wide)p.ld * p.es, pb = (Wide)q.ld * q.es;
-  const Wide ea = a + (Wide)(p.rows - 1) * pa + ra, eb = b + (Wide)(q.rows - 1) * pb + rb;
-  if (a >= eb || b >= ea) return kApart;
-  if (a == b && p.es == q.es && p.rows == q.rows && p.cols == q.cols && (pa == pb || p.rows == 1)) return kSameRows;
-  if (pa != pb) return kMixed;
-  const Wide off = b >= a ? (b - a) % pa : (pa - (a - b) % pa) % pa;  // q's rows in p's pitch
-  return off >= ra && pa - off >= rb ? kApart : kMixed;
-}
 
 // ---------------------------------------------------------------------------------------
 // Embedding.
@@ -139,12 +111,15 @@ static int launch_embedding_sum(LookupParams p, cudaStream_t st) {
   const int64_t slabs = (units + kEbThreads - 1) / kEbThreads;
   const int threads = (int)round_up((size_t)((units + slabs - 1) / slabs), 32);
   const int64_t zero = p.accumulate ? 0 : ((int64_t)p.V + kEbZeroRows - 1) / kEbZeroRows;
-  if ((p.chunks + zero) * slabs > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  if (p.chunks * slabs + zero > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
   p.slabs = (int32_t)slabs;
-  embedding_sum_kernel<T, KE><<<(unsigned)((p.chunks + zero) * slabs), threads, 0, st>>>(p);
+  embedding_sum_kernel<T, KE><<<(unsigned)(p.chunks * slabs + zero), threads, 0, st>>>(p);
   CKL();
   if (p.chunks > 1) {
-    embedding_join_kernel<KE><<<(unsigned)(p.chunks * slabs), threads, 0, st>>>(p);
+    constexpr int JE = KE > 4 ? 4 : KE;
+    p.slabs = (int32_t)((p.d / JE + 63) / 64);
+    if ((int64_t)p.chunks * p.slabs > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
+    embedding_join_kernel<JE><<<(unsigned)(p.chunks * (int64_t)p.slabs), dim3(64, kEbJoinShares), 0, st>>>(p);
     CKL();
   }
   return OAPL_OK;
@@ -158,159 +133,6 @@ static int route_embedding_sum(const LookupParams& p, cudaStream_t st) {
 }
 
 // ---------------------------------------------------------------------------------------
-// Residual norm.
-constexpr int kRsWarpD = 512;          // rows of a warp: 16 elements a lane
-constexpr int64_t kRsWarpWorkers = 8192, kRsCtaWorkers = 1024;
-constexpr size_t kRsSmem = 200 * 1024; // shared memory of an SM that rows on their way may take
-
-static int64_t residual_workers(int64_t N, int32_t d) {
-  const int64_t most = d <= kRsWarpD ? kRsWarpWorkers : kRsCtaWorkers;
-  return N < most ? N : most;
-}
-
-static int check_residual(const oapl_residual* r, bool forward) {
-  if (!r || r->N <= 0 || r->d <= 0) return OAPL_ERR_INVALID_ARG;
-  const int es = type_size(r->type);
-  if (!es) return OAPL_ERR_INVALID_ARG;
-  if (forward && !r->x) return OAPL_ERR_INVALID_ARG;
-  if (r->x && r->ld_x < r->d) return OAPL_ERR_INVALID_ARG;
-  if (r->y && r->ld_y < r->d) return OAPL_ERR_INVALID_ARG;
-  if (!r->y && (r->w_post || r->gate_kind != OAPL_GATE_NONE)) return OAPL_ERR_INVALID_ARG;
-  if (!r->y && !r->w_pre) return OAPL_ERR_INVALID_ARG;  // nothing but a scaled copy
-  if ((r->w_post || r->w_pre) && !type_size(r->weight_type)) return OAPL_ERR_INVALID_ARG;
-  if (r->gate_kind < OAPL_GATE_NONE || r->gate_kind > OAPL_GATE_FULL) return OAPL_ERR_INVALID_ARG;
-  if ((r->gate_kind != OAPL_GATE_NONE) != (r->gate != nullptr)) return OAPL_ERR_INVALID_ARG;
-  if (r->gate && !type_size(r->gate_type)) return OAPL_ERR_INVALID_ARG;
-  if (r->gate_kind == OAPL_GATE_ROW && r->ld_gate < 1) return OAPL_ERR_INVALID_ARG;
-  if (r->gate_kind == OAPL_GATE_FULL && (r->ld_gate < r->d || r->gate_type != r->type)) return OAPL_ERR_INVALID_ARG;
-  if (!(r->eps >= 0.f) || !std::isfinite(r->eps) || !std::isfinite(r->weight_offset) ||
-      !std::isfinite(r->residual_scale) || !std::isfinite(r->branch_scale))
-    return OAPL_ERR_INVALID_ARG;
-  if ((uintptr_t)r->x % es || (uintptr_t)r->y % es) return OAPL_ERR_MISALIGNED;
-  if (r->gate && (uintptr_t)r->gate % type_size(r->gate_type)) return OAPL_ERR_MISALIGNED;
-  if ((r->w_post || r->w_pre) && ((uintptr_t)r->w_post | (uintptr_t)r->w_pre) % type_size(r->weight_type))
-    return OAPL_ERR_MISALIGNED;
-  if (r->N > kMaxRows || r->d > kRsMaxD) return OAPL_ERR_UNSUPPORTED_SHAPE;
-  return OAPL_OK;
-}
-
-static ResidualParams residual_params(const oapl_residual* r) {
-  ResidualParams p;
-  memset(&p, 0, sizeof(p));
-  p.N = r->N;
-  p.d = r->d;
-  p.x = r->x;
-  p.y = r->y;
-  p.gate = r->gate;
-  p.w_post = r->w_post;
-  p.w_pre = r->w_pre;
-  p.ld_x = r->ld_x;
-  p.ld_y = r->ld_y;
-  p.ld_gate = r->ld_gate;
-  p.gate_kind = r->gate_kind;
-  p.gate_type = r->gate_type;
-  p.weight_type = r->weight_type;
-  p.weight_offset = r->weight_offset;
-  p.eps = r->eps;
-  p.a = r->residual_scale;
-  p.b = r->branch_scale;
-  p.kind_pre = p.kind_post = p.kind_gate = -1;
-  return p;
-}
-
-// Whether rows start on 16-byte boundaries: of matrices and, where there are any, of the weights.
-// The few widest fp32 rows do not fit into shared memory together: they are read where they are.
-static bool residual_vec(const ResidualParams& p, int es, int arrays, const Place* m, int count) {
-  if (p.d % (16 / es) || (size_t)arrays * p.d * es > kRsSmem) return false;
-  for (int i = 0; i < count; ++i)
-    if (m[i].base && (!on16(m[i].base) || (m[i].rows > 1 && m[i].ld * m[i].es % 16))) return false;
-  return on16(p.w_post) && on16(p.w_pre) && (p.gate_kind != OAPL_GATE_COLUMN || on16(p.gate));
-}
-
-// The launch: rows per SM, rows in flight, workers.
-struct ResidualShape {
-  int threads, grid, smem;
-  int64_t workers;
-};
-static ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int ke, bool warp, int arrays, int per_sm) {
-  ResidualShape s;
-  const int units = p.d / ke;
-  const size_t row = ke > 1 ? (size_t)arrays * units * 16 : 0;
-  if (warp) {
-    s.threads = 256;
-    per_sm = per_sm * (int)kRsMaxThreads / 256;
-    p.stages = 4;
-    while (p.stages > 1 && row * p.stages * 8 * per_sm > kRsSmem) p.stages /= 2;
-    s.workers = (p.N + 7) / 8 < (int64_t)n_sm * per_sm ? (p.N + 7) / 8 * 8 : (int64_t)n_sm * per_sm * 8;
-    if (s.workers > kRsWarpWorkers) s.workers = kRsWarpWorkers;
-    s.grid = (int)(s.workers / 8);
-    s.smem = (int)(row * p.stages * 8);
-  } else {
-    const int k = elems / ke;
-    s.threads = (int)round_up((size_t)((units + k - 1) / k), 32);
-    per_sm = per_sm * (int)kRsMaxThreads / s.threads;
-    if (per_sm < 1) per_sm = 1;
-    p.stages = 4;
-    while (p.stages > 1 && row * p.stages * per_sm > kRsSmem) p.stages /= 2;
-    while (per_sm > 1 && row * p.stages * per_sm > kRsSmem) --per_sm;
-    s.workers = p.N < (int64_t)n_sm * per_sm ? p.N : (int64_t)n_sm * per_sm;
-    if (s.workers > kRsCtaWorkers) s.workers = kRsCtaWorkers;
-    s.grid = (int)s.workers;
-    s.smem = (int)(row * p.stages);
-  }
-  return s;
-}
-
-template <typename F>
-static int residual_smem(F kern, int bytes, bool (&done)[kMaxDevices]) {
-  if (bytes <= 40 * 1024) return OAPL_OK;
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return OAPL_ERR_CUDA;
-  if (!done[dev]) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) != cudaSuccess)
-      return OAPL_ERR_CUDA;
-    done[dev] = true;
-  }
-  return OAPL_OK;
-}
-
-template <typename T, int KE, int K, bool WARP, bool FWD>
-static int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  static bool done[kMaxDevices] = {false};
-  auto kern = FWD ? residual_fwd_kernel<T, KE, K, WARP> : residual_bwd_kernel<T, KE, K, WARP>;
-  // threads of an SM in units of 512: what the registers allow
-  const ResidualShape s = residual_shape(p, n_sm, KE * K, KE, WARP, arrays, FWD ? 2 : 1);
-  const int rc = residual_smem(kern, s.smem, done);
-  if (rc != OAPL_OK) return rc;
-  *workers = s.workers;
-  kern<<<s.grid, s.threads, s.smem, st>>>(p);
-  CKL();
-  return OAPL_OK;
-}
-
-template <typename T, int KE, bool FWD>
-static int route_residual(const ResidualParams& p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  // elements a thread: as few as give a CTA at most 256 threads, 32 beyond that
-  if (p.d <= kRsWarpD) return launch_residual<T, KE, 16 / KE, true, FWD>(p, arrays, n_sm, workers, st);
-  if (p.d <= 2048) return launch_residual<T, KE, 8 / KE, false, FWD>(p, arrays, n_sm, workers, st);
-  if (p.d <= 4096) return launch_residual<T, KE, 16 / KE, false, FWD>(p, arrays, n_sm, workers, st);
-  return launch_residual<T, KE, 32 / KE, false, FWD>(p, arrays, n_sm, workers, st);
-}
-
-template <bool FWD>
-static int route_residual_type(const ResidualParams& p, int32_t type, bool vec, int arrays, int n_sm, int64_t* workers,
-                               cudaStream_t st) {
-  if (type == OAPL_TYPE_BF16)
-    return vec ? route_residual<__nv_bfloat16, 8, FWD>(p, arrays, n_sm, workers, st)
-               : route_residual<__nv_bfloat16, 1, FWD>(p, arrays, n_sm, workers, st);
-  if (type == OAPL_TYPE_F16)
-    return vec ? route_residual<__half, 8, FWD>(p, arrays, n_sm, workers, st)
-               : route_residual<__half, 1, FWD>(p, arrays, n_sm, workers, st);
-  return vec ? route_residual<float, 4, FWD>(p, arrays, n_sm, workers, st)
-             : route_residual<float, 1, FWD>(p, arrays, n_sm, workers, st);
-}
-
-// ---------------------------------------------------------------------------------------
 // Gradient norm and clipping.
 static int check_tensors(const oapl_tensor* t, int32_t count, bool clip) {
   if (!t || count <= 0) return OAPL_ERR_INVALID_ARG;
@@ -321,7 +143,7 @@ static int check_tensors(const oapl_tensor* t, int32_t count, bool clip) {
     if (!t[i].n) continue;
     if (!t[i].data) return OAPL_ERR_INVALID_ARG;
     if ((uintptr_t)t[i].data % es) return OAPL_ERR_MISALIGNED;
-    chunks += (t[i].n - 1) / kGcChunk + 1;
+    chunks += (t[i].n - 1) / (kGcBytes / 4) + 1;  // the most that its types can give
     if (chunks > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
     if (!clip) continue;
     if (!t[i].out || !os) return OAPL_ERR_INVALID_ARG;
@@ -349,7 +171,10 @@ static int32_t fill_list(const oapl_tensor* t, int32_t count, bool clip, GradLis
     g.in_type = (uint8_t)t[i].type;
     g.out_type = (uint8_t)(clip ? t[i].out_type : 0);
     g.vec = on16(t[i].data) && (!clip || on16(t[i].out));
-    l->chunks += (int32_t)((t[i].n - 1) / kGcChunk + 1);
+    const int wide = type_size(t[i].type) == 4 || (clip && type_size(t[i].out_type) == 4) ? 4 : 2;
+    g.shift = wide == 4 ? 12 : 13;
+    static_assert(kGcBytes == 4 << 12, "a chunk's elements");
+    l->chunks += (int32_t)((t[i].n - 1 >> g.shift) + 1);
   }
   return i;
 }
@@ -414,7 +239,7 @@ static int launch_adjust(AdjustParams p, cudaStream_t st) {
   if (slices * p.N > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
   p.slices = (int32_t)slices;
   auto kern = adjust_kernel<T, KE, VPT, GRAD, OVER>;
-  const int smem = p.counters ? (int)kSlice * 4 : 0;
+  const int smem = p.history || p.biased ? AdjustShared::bytes((int)kSlice) : 0;
   if (smem > 40 * 1024) {
     static bool done[kMaxDevices] = {false};
     int dev = -1;
@@ -432,9 +257,9 @@ static int launch_adjust(AdjustParams p, cudaStream_t st) {
 
 template <typename T, int KE, bool GRAD, bool OVER>
 static int route_adjust_size(const AdjustParams& p, int n_sm, cudaStream_t st) {
-  // slices of eight vectors a thread where they give every SM a few, of two otherwise
-  constexpr int kMany = KE == 1 ? 32 : 8, kFew = KE == 1 ? 8 : 2;
-  const int64_t many = (int64_t)p.N * p.V / (KE * kMany * kAdThreads);
+  // slices of 8192 tokens where they give every SM four, of 2048 otherwise
+  constexpr int kMany = 32 / KE, kFew = 8 / KE;
+  const int64_t many = (int64_t)p.N * p.V / 8192;
   return many >= 4 * (int64_t)n_sm ? launch_adjust<T, KE, kMany, GRAD, OVER>(p, st)
                                    : launch_adjust<T, KE, kFew, GRAD, OVER>(p, st);
 }
@@ -446,7 +271,7 @@ static int route_adjust(const AdjustParams& p, bool grad, cudaStream_t st) {
   constexpr int KE = Elem<T>::kN;
   const bool over = !grad && p.out == p.z;
   auto rows16 = [&](const void* b, int64_t ld) { return on16(b) && (p.N == 1 || ld * sizeof(T) % 16 == 0); };
-  const bool vec = rows16(p.out, p.ld_o) && rows16(grad ? p.d : p.z, grad ? p.ld_d : p.ld_z);
+  const bool vec = rows16(p.out, p.ld_o) && rows16(p.z, p.ld_z) && (!grad || rows16(p.d, p.ld_d));
   if (grad)
     return vec ? route_adjust_size<T, KE, true, false>(p, n_sm, st) : route_adjust_size<T, 1, true, false>(p, n_sm, st);
   if (over)
@@ -547,116 +372,6 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
   return route_embedding_sum<float>(p, st);
 }
 
-int oapl_residual_norm(const oapl_residual* r, void* x_out, int64_t ld_x_out, void* h, int64_t ld_h, float* rstd_post,
-                       float* rstd_pre, void* stream) {
-  const int rc = check_residual(r, true);
-  if (rc != OAPL_OK) return rc;
-  const int es = type_size(r->type);
-  if ((h != nullptr) != (r->w_pre != nullptr) || (!x_out && !h)) return OAPL_ERR_INVALID_ARG;
-  if ((x_out && ld_x_out < r->d) || (h && ld_h < r->d)) return OAPL_ERR_INVALID_ARG;
-  if ((rstd_post && !r->w_post) || (rstd_pre && !r->w_pre)) return OAPL_ERR_INVALID_ARG;
-  if ((uintptr_t)x_out % es || (uintptr_t)h % es || (((uintptr_t)rstd_post | (uintptr_t)rstd_pre) & 3))
-    return OAPL_ERR_MISALIGNED;
-  const bool full = r->gate_kind == OAPL_GATE_FULL;
-  const Place m[5] = {{x_out, r->N, r->d, ld_x_out, es}, {h, r->N, r->d, ld_h, es}, {r->x, r->N, r->d, r->ld_x, es},
-                      {r->y, r->N, r->d, r->ld_y, es}, {full ? r->gate : nullptr, r->N, r->d, r->ld_gate, es}};
-  if (overlap(m[0], m[1]) != kApart) return OAPL_ERR_INVALID_ARG;
-  for (int o = 0; o < 2; ++o)
-    for (int i = 2; i < 5; ++i)
-      if (overlap(m[o], m[i]) == kMixed) return OAPL_ERR_INVALID_ARG;
-  const int n_sm = sm_count();
-  if (n_sm <= 0) return OAPL_ERR_CUDA;
-  ResidualParams p = residual_params(r);
-  p.x_out = x_out;
-  p.ld_xo = ld_x_out;
-  p.h = h;
-  p.ld_h = ld_h;
-  p.rstd_post = rstd_post;
-  p.rstd_pre = rstd_pre;
-  int64_t workers = 0;
-  const int arrays = 1 + (r->y != nullptr) + full;
-  return route_residual_type<true>(p, r->type, residual_vec(p, es, arrays, m, 5), arrays, n_sm, &workers,
-                                   static_cast<cudaStream_t>(stream));
-}
-
-size_t oapl_residual_norm_workspace_bytes(int64_t N, int32_t d) {
-  if (N <= 0 || d <= 0 || N > kMaxRows || d > kRsMaxD) return 0;
-  // a warp's rows come eight at a time
-  return 3 * sizeof(float) * (size_t)d * round_up((size_t)residual_workers(N, d), 8);
-}
-
-int oapl_residual_norm_bwd(const oapl_residual* r, const void* x_out, int64_t ld_x_out, const float* rstd_post,
-                           const float* rstd_pre, const void* dh, int64_t ld_dh, const void* dx_out, int64_t ld_dx_out,
-                           void* dx, int64_t ld_dx, void* dy, int64_t ld_dy, void* dgate, int64_t ld_dgate,
-                           float* dw_post, float* dw_pre, int accumulate, void* ws, size_t ws_bytes, void* stream) {
-  const int rc = check_residual(r, false);
-  if (rc != OAPL_OK) return rc;
-  const int es = type_size(r->type);
-  const bool pre = r->w_pre != nullptr, post = r->w_post != nullptr, full = r->gate_kind == OAPL_GATE_FULL;
-  const bool row = r->gate_kind == OAPL_GATE_ROW, column = r->gate_kind == OAPL_GATE_COLUMN;
-  if (pre && (!x_out || !rstd_pre || !dh)) return OAPL_ERR_INVALID_ARG;
-  if ((!pre && (dh || dw_pre || !dx_out)) || (post && !rstd_post) || (!post && dw_post)) return OAPL_ERR_INVALID_ARG;
-  if ((dy && !r->y) || (dgate && !r->gate)) return OAPL_ERR_INVALID_ARG;
-  if (!dx && !dy && !dgate && !dw_post && !dw_pre) return OAPL_ERR_INVALID_ARG;
-  if ((pre && (ld_x_out < r->d || ld_dh < r->d)) || (dx_out && ld_dx_out < r->d) || (dx && ld_dx < r->d) ||
-      (dy && ld_dy < r->d) || (dgate && full && ld_dgate < r->d) || (dgate && row && ld_dgate < 1))
-    return OAPL_ERR_INVALID_ARG;
-  const int gs = full ? es : 4;
-  if ((pre && ((uintptr_t)x_out % es || (uintptr_t)dh % es)) || (uintptr_t)dx_out % es || (uintptr_t)dx % es ||
-      (uintptr_t)dy % es || (uintptr_t)dgate % gs ||
-      (((uintptr_t)dw_post | (uintptr_t)dw_pre | (uintptr_t)rstd_post | (uintptr_t)rstd_pre) & 3))
-    return OAPL_ERR_MISALIGNED;
-  const Place m[8] = {{dx, r->N, r->d, ld_dx, es}, {dy, r->N, r->d, ld_dy, es},
-                      {full ? dgate : nullptr, r->N, r->d, ld_dgate, es},
-                      {pre ? x_out : nullptr, r->N, r->d, ld_x_out, es}, {dh, r->N, r->d, ld_dh, es},
-                      {dx_out, r->N, r->d, ld_dx_out, es}, {r->y, r->N, r->d, r->ld_y, es},
-                      {full ? r->gate : nullptr, r->N, r->d, r->ld_gate, es}};
-  for (int o = 0; o < 3; ++o)
-    for (int i = o + 1; i < 8; ++i) {
-      const Overlap v = overlap(m[o], m[i]);
-      if (v == kMixed || (i < 3 && v != kApart)) return OAPL_ERR_INVALID_ARG;
-    }
-  ResidualParams p = residual_params(r);
-  int kinds = 0;
-  ResidualJoinParams j;
-  memset(&j, 0, sizeof(j));
-  if (dw_pre) { j.out[kinds] = dw_pre; p.kind_pre = kinds++; }
-  if (dw_post) { j.out[kinds] = dw_post; p.kind_post = kinds++; }
-  if (dgate && column) { j.out[kinds] = static_cast<float*>(dgate); p.kind_gate = kinds++; }
-  if (kinds) {
-    if (!ws) return OAPL_ERR_INVALID_ARG;
-    if (!on16(ws)) return OAPL_ERR_MISALIGNED;
-    if (ws_bytes < oapl_residual_norm_workspace_bytes(r->N, r->d)) return OAPL_ERR_WORKSPACE_TOO_SMALL;
-  }
-  const int n_sm = sm_count();
-  if (n_sm <= 0) return OAPL_ERR_CUDA;
-  p.x_out = const_cast<void*>(x_out);
-  p.ld_xo = ld_x_out;
-  p.rstd_post = const_cast<float*>(rstd_post);
-  p.rstd_pre = const_cast<float*>(rstd_pre);
-  p.dh = dh;
-  p.ld_dh = ld_dh;
-  p.dx_out = dx_out;
-  p.ld_dxo = ld_dx_out;
-  p.dx = dx;
-  p.ld_dx = ld_dx;
-  p.dy = dy;
-  p.ld_dy = ld_dy;
-  p.dgate = dgate;
-  p.ld_dg = ld_dgate;
-  p.part = static_cast<float*>(ws);
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int arrays = 2 * pre + (dx_out != nullptr) + (r->y != nullptr) + full;
-  const int run = route_residual_type<false>(p, r->type, residual_vec(p, es, arrays, m, 8), arrays, n_sm, &j.workers, st);
-  if (run != OAPL_OK || !kinds) return run;
-  j.part = p.part;
-  j.d = r->d;
-  j.accumulate = accumulate != 0;
-  residual_join_kernel<<<dim3((unsigned)((r->d + 31) / 32), (unsigned)kinds), dim3(32, 8), 0, st>>>(j);
-  CKL();
-  return OAPL_OK;
-}
-
 size_t oapl_grad_norm_workspace_bytes(int32_t count) {
   return count <= 0 ? 0 : sizeof(double) * kGcMaxSums * (size_t)((count + kGcList - 1) / kGcList);
 }
@@ -718,8 +433,8 @@ int oapl_logits_adjust(const oapl_logits* L, const oapl_adjust* a, void* out, in
   if (overlap({L->logits, L->N, L->V, L->ld, es}, {out, L->N, L->V, ld_out, es}) == kMixed) return OAPL_ERR_INVALID_ARG;
   AdjustParams p = adjust_params(L, a, out, ld_out, device_status);
   const bool history = a->spans && (a->repetition || a->frequency || a->presence);
-  if (!history) p.spans = nullptr;
-  p.counters = history || a->bias_start;
+  p.history = history;
+  p.biased = a->bias_start && a->biases > 0;
   return route_adjust_type(p, L->type, false, static_cast<cudaStream_t>(stream));
 }
 
@@ -736,8 +451,7 @@ int oapl_logits_adjust_bwd(const oapl_logits* L, const oapl_adjust* a, const voi
   AdjustParams p = adjust_params(L, a, dlogits, ld_dlogits, device_status);
   p.d = d_out;
   p.ld_d = ld_d_out;
-  p.counters = a->repetition != nullptr;
-  if (!p.counters) p.spans = nullptr;
+  p.history = a->repetition != nullptr;
   return route_adjust_type(p, L->type, true, static_cast<cudaStream_t>(stream));
 }
 
