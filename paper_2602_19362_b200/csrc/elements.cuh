@@ -175,4 +175,41 @@ struct Raw<T, 1> {
   static __device__ __forceinline__ void store(T* p, const float (&f)[1]) { Elem<T>::put(p, 0, f[0]); }
 };
 
+// KE neighbouring elements at any alignment: the aligned 16-byte blocks that hold them, shifted in registers.  A block
+// without one of the elements is not touched.
+template <typename T, int KE>
+struct Shifted {
+  static constexpr int kV = KE / Elem<T>::kN;
+  uint4 b[kV + 1];
+  uint32_t off;  // bytes into the first block
+  __device__ __forceinline__ void load(const T* p) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    off = (uint32_t)a & 15u;
+    const uint4* q = reinterpret_cast<const uint4*>(a & ~(uintptr_t)15);
+#pragma unroll
+    for (int i = 0; i < kV; ++i) b[i] = q[i];
+    b[kV] = off ? q[kV] : make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ void raw(Raw<T, KE>& r) const {
+    uint32_t w[kV * 4 + 4];
+#pragma unroll
+    for (int i = 0; i <= kV; ++i) {
+      w[4 * i] = b[i].x;
+      w[4 * i + 1] = b[i].y;
+      w[4 * i + 2] = b[i].z;
+      w[4 * i + 3] = b[i].w;
+    }
+    // whole words first, two and one at a time, then bits
+#pragma unroll
+    for (int i = 0; i < kV * 4 + 2; ++i) w[i] = off & 8u ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < kV * 4 + 1; ++i) w[i] = off & 4u ? w[i + 1] : w[i];
+    const uint32_t s = (off & 3u) * 8u;
+#pragma unroll
+    for (int i = 0; i < kV; ++i)
+      r.v[i] = make_uint4(__funnelshift_r(w[4 * i], w[4 * i + 1], s), __funnelshift_r(w[4 * i + 1], w[4 * i + 2], s),
+                          __funnelshift_r(w[4 * i + 2], w[4 * i + 3], s), __funnelshift_r(w[4 * i + 3], w[4 * i + 4], s));
+  }
+};
+
 }  // namespace oapl

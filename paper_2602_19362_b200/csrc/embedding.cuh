@@ -58,44 +58,85 @@ __device__ __forceinline__ void lookup_check(const LookupParams& p, int64_t n) {
 }
 
 // ------------------------------------------------------------------------------------------------ lookup
+template <typename TI, typename TO, int KE>
+__device__ __forceinline__ void lookup_put(const LookupParams& p, bool live, const Raw<TI, KE>& v, TO* to) {
+  float f[KE];
+  if (live) {
+    if constexpr (std::is_same<TI, TO>::value) {
+      if (p.scale == 1.f) {  // the bits as they are, a NaN's too
+        v.put(to);
+        return;
+      }
+    }
+    v.widen(f);
+#pragma unroll
+    for (int i = 0; i < KE; ++i) f[i] *= p.scale;
+  } else {
+#pragma unroll
+    for (int i = 0; i < KE; ++i) f[i] = 0.f;
+  }
+  Raw<TO, KE>::store(to, f);
+}
+
 // A thread: KE elements of R rows, all loads in flight; blockDim.x threads along a row, blockDim.y rows beside one
-// another, blockIdx.y pieces of a row.
-template <typename TI, typename TO, int KE, int R>
+// another, blockIdx.y pieces of a row.  LEVEL: all rows on 16-byte boundaries.  Otherwise vectors begin at the first boundary
+// of a row of the result, the table's row is shifted to them, and the threads behind the row's vectors take one of the up
+// to 2 KE - 2 elements before and behind them each.
+template <typename TI, typename TO, int KE, int R, bool LEVEL>
 __global__ void __launch_bounds__(kEbThreads) embedding_kernel(LookupParams p) {
-  const int c = ((int)blockIdx.y * (int)blockDim.x + (int)threadIdx.x) * KE;
+  const int u = (int)blockIdx.y * (int)blockDim.x + (int)threadIdx.x;
   const int64_t n0 = ((int64_t)blockIdx.x * R) * blockDim.y + threadIdx.y;
   uint32_t key[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int64_t n = n0 + (int64_t)r * blockDim.y;
     key[r] = n < p.N ? lookup_key(p, n) : (uint32_t)p.V;
-    if (n < p.N && blockIdx.y == 0 && threadIdx.x == 0) lookup_check(p, n);
+    if (n < p.N && u == 0) lookup_check(p, n);
   }
-  if (c >= p.d) return;
+  const TI* table = static_cast<const TI*>(p.in);
+  TO* out = static_cast<TO*>(p.out) + n0 * p.ld_out;
+  const int64_t step = (int64_t)blockDim.y * p.ld_out;
   Raw<TI, KE> v[R];
+  if constexpr (LEVEL) {
+    const int c = u * KE;
+    if (c >= p.d) return;
 #pragma unroll
-  for (int r = 0; r < R; ++r)
-    if (key[r] < (uint32_t)p.V) v[r].load(static_cast<const TI*>(p.in) + (int64_t)key[r] * p.ld_in + c);
+    for (int r = 0; r < R; ++r)
+      if (key[r] < (uint32_t)p.V) v[r].load(table + (int64_t)key[r] * p.ld_in + c);
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int64_t n = n0 + (int64_t)r * blockDim.y;
-    if (n >= p.N) break;
-    float f[KE];
-    if (key[r] < (uint32_t)p.V) {
-      if constexpr (std::is_same<TI, TO>::value) {
-        if (p.scale == 1.f) {  // the bits as they are, a NaN's too
-          v[r].put(static_cast<TO*>(p.out) + n * p.ld_out + c);
-          continue;
+    for (int r = 0; r < R; ++r)
+      if (n0 + (int64_t)r * blockDim.y < p.N) lookup_put<TI, TO, KE>(p, key[r] < (uint32_t)p.V, v[r], out + r * step + c);
+  } else {
+    constexpr int kMask = 16 / (int)sizeof(TO) - 1;
+    Shifted<TI, KE> b[R];
+    Raw<TI, 1> one[R];
+    int c[R];
+    bool whole[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      int head = (int)(-(reinterpret_cast<uintptr_t>(out + r * step) / sizeof(TO)) & kMask);
+      head = head < p.d ? head : p.d;
+      const int vecs = (p.d - head) / KE, e = u - vecs;  // e: place among the single elements
+      whole[r] = u < vecs;
+      c[r] = whole[r] ? head + u * KE : e < head ? e : vecs * KE + e;
+      if (c[r] < p.d && key[r] < (uint32_t)p.V) {
+        const TI* from = table + (int64_t)key[r] * p.ld_in + c[r];
+        if (whole[r]) b[r].load(from);
+        else one[r].load(from);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (n0 + (int64_t)r * blockDim.y < p.N && c[r] < p.d) {
+        const bool live = key[r] < (uint32_t)p.V;
+        TO* to = out + r * step + c[r];
+        if (whole[r]) {
+          b[r].raw(v[r]);
+          lookup_put<TI, TO, KE>(p, live, v[r], to);
+        } else {
+          lookup_put<TI, TO, 1>(p, live, one[r], to);
         }
       }
-      v[r].widen(f);
-#pragma unroll
-      for (int i = 0; i < KE; ++i) f[i] *= p.scale;
-    } else {
-#pragma unroll
-      for (int i = 0; i < KE; ++i) f[i] = 0.f;
-    }
-    Raw<TO, KE>::store(static_cast<TO*>(p.out) + n * p.ld_out + c, f);
   }
 }
 
@@ -300,7 +341,7 @@ __device__ __forceinline__ void table_put(const LookupParams& p, uint32_t v, int
 // Grid: chunks x slabs of columns, the slabs of a chunk next to one another, then the CTAs that clear.
 template <typename T, int KE>
 __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams p) {
-  constexpr int kAhead = 8;  // rows whose loads are in flight together
+  constexpr int kAhead = KE == 1 ? 16 : 8;  // rows whose loads are in flight together
   __shared__ uint2 e[kEbMaxChunk];
   __shared__ uint32_t live;
   const int slab = (int)(blockIdx.x % (unsigned)p.slabs);

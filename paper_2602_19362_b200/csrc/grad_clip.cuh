@@ -10,6 +10,8 @@
 // list and the number of SMs determine.  A thread whose fp32 sum left the range where that is exact to fp32 rounding
 // (values above about 1e14, or nothing but values below about 1e-12) adds the same elements again in fp64.
 #pragma once
+#include <type_traits>
+
 #include "elements.cuh"
 
 namespace oapl {
@@ -78,35 +80,44 @@ __device__ __forceinline__ float grad_one(const void* p, int type, int64_t i) {
   return type == 0 ? Elem<__nv_bfloat16>::one(p, i) : (type == 1 ? Elem<__half>::one(p, i) : Elem<float>::one(p, i));
 }
 
-__global__ void __launch_bounds__(kGcThreads, 5) grad_norm_kernel(const __grid_constant__ GradList l, double* part) {
+// A thread's vectors of a chunk; elements that they leave out are added up at once.
+struct GradShare {
+  uint4 v[kGcVecs];
+  int type;
+};
+__device__ __forceinline__ void grad_fetch(const GradList& l, int c, int& k, GradShare& q, double& s) {
+  while (k + 1 < l.count && l.t[k + 1].first <= c) ++k;
+  const GradTensor& t = l.t[k];
+  const int64_t at = (int64_t)(c - t.first) << t.shift;
+  const int size = 1 << t.shift, n = t.n - at < size ? (int)(t.n - at) : size;
+  const int wide = t.in_type == 2 ? 2 : 1;  // log2 of the bytes of an element
+  const uint4* g = reinterpret_cast<const uint4*>(static_cast<const char*>(t.in) + (at << wide));
+  const int vecs = t.vec ? n >> (4 - wide) : 0, done = vecs << (4 - wide);
+  q.type = t.in_type;
+#pragma unroll
+  for (int j = 0; j < kGcVecs; ++j) {
+    const int i = j * kGcThreads + (int)threadIdx.x;
+    q.v[j] = i < vecs ? g[i] : make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll 1
+  for (int i = done + (int)threadIdx.x; i < n; i += kGcThreads) {
+    const double x = grad_one(t.in, t.in_type, at + i);
+    s = fma(x, x, s);
+  }
+}
+__global__ void __launch_bounds__(kGcThreads, 4) grad_norm_kernel(const __grid_constant__ GradList l, double* part) {
   __shared__ double sh[kGcThreads / 32];
   double s = 0.0;
   int k = grad_find(l, (int)blockIdx.x);
+  GradShare now, next;
+  grad_fetch(l, (int)blockIdx.x, k, now, s);
   for (int c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-    while (k + 1 < l.count && l.t[k + 1].first <= c) ++k;
-    const GradTensor& t = l.t[k];
-    const int64_t at = (int64_t)(c - t.first) << t.shift;
-    const int size = 1 << t.shift, n = t.n - at < size ? (int)(t.n - at) : size;
-    int done = 0;
-    if (t.vec) {
-      const int per = t.in_type == 2 ? 4 : 8;
-      const uint4* g = reinterpret_cast<const uint4*>(static_cast<const char*>(t.in) + at * (t.in_type == 2 ? 4 : 2));
-      const int vecs = n / per;
-      done = vecs * per;
-      uint4 v[kGcVecs];
-#pragma unroll
-      for (int j = 0; j < kGcVecs; ++j) {
-        const int i = j * kGcThreads + (int)threadIdx.x;
-        v[j] = i < vecs ? g[i] : make_uint4(0, 0, 0, 0);
-      }
-      if (t.in_type == 0) s += grad_squares<__nv_bfloat16>(v);
-      else if (t.in_type == 1) s += grad_squares<__half>(v);
-      else s += grad_squares<float>(v);
-    }
-    for (int i = done + (int)threadIdx.x; i < n; i += kGcThreads) {
-      const double x = grad_one(t.in, t.in_type, at + i);
-      s = fma(x, x, s);
-    }
+    // the next chunk's loads before this one's sums
+    if (c + (int)gridDim.x < l.chunks) grad_fetch(l, c + (int)gridDim.x, k, next, s);
+    s += now.type == 0   ? grad_squares<__nv_bfloat16>(now.v)
+         : now.type == 1 ? grad_squares<__half>(now.v)
+                         : grad_squares<float>(now.v);
+    now = next;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_down_sync(0xffffffffu, s, o);
@@ -179,8 +190,10 @@ __device__ __forceinline__ void grad_scale_types(const GradTensor& t, int64_t at
   else grad_scale_chunk<TI, float>(t, at, n, factor);
 }
 
-__global__ void __launch_bounds__(kGcThreads, 3) grad_clip_kernel(const __grid_constant__ GradList l, const float* sq_norm,
-                                                               float clip, float scale) {
+// TI, TO: the types of the whole list, void where it has several.
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(kGcThreads, 4) grad_clip_kernel(const __grid_constant__ GradList l, const float* sq_norm,
+                                                                  float clip, float scale) {
   __shared__ float sh;
   if (threadIdx.x == 0) {
     const double sq = *sq_norm;
@@ -198,9 +211,13 @@ __global__ void __launch_bounds__(kGcThreads, 3) grad_clip_kernel(const __grid_c
     if (factor == 1.f && t.in == t.out) continue;  // in place, and nothing changes
     const int64_t at = (int64_t)(c - t.first) << t.shift;
     const int size = 1 << t.shift, n = t.n - at < size ? (int)(t.n - at) : size;
-    if (t.in_type == 0) grad_scale_types<__nv_bfloat16>(t, at, n, factor);
-    else if (t.in_type == 1) grad_scale_types<__half>(t, at, n, factor);
-    else grad_scale_types<float>(t, at, n, factor);
+    if constexpr (std::is_void<TI>::value) {
+      if (t.in_type == 0) grad_scale_types<__nv_bfloat16>(t, at, n, factor);
+      else if (t.in_type == 1) grad_scale_types<__half>(t, at, n, factor);
+      else grad_scale_types<float>(t, at, n, factor);
+    } else {
+      grad_scale_chunk<TI, TO>(t, at, n, factor);
+    }
   }
 }
 

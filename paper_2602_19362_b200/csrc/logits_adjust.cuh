@@ -15,6 +15,8 @@
 //   5. behind a barrier the listed values are stored over what the copy left there.
 // So the copy does not test for tokens that change.  (When it did, with a counter per token beside each vector, a token in
 // one of a warp's 256 places cost the warp eight divisions: 2048 x 152064 bf16, gradient 472 us; %GRAD% like this.)
+// Rows need not start on 16-byte boundaries: where the two sides are off by the same number of bytes, vectors begin at the
+// slice's first boundary (KE > 1); rows off by different numbers go an element at a time (KE == 1).
 // Few rows are cut into smaller slices, for more CTAs; the tokens are then read by more of them, from L2.
 #pragma once
 #include "elements.cuh"
@@ -104,13 +106,22 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
     }
   }
   auto is_open = [&](int i) { return !bits || (bits[i >> 5] >> (i & 31) & 1); };
+  // elements before the first vector
+  int head = KE == 1 ? 0 : (int)(-(reinterpret_cast<uintptr_t>(out) / sizeof(T)) & (KE - 1));
+  head = head < len ? head : len;
   Raw<T, KE> v[VPT];
   uint32_t open[VPT];
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
-    const int i = (j * kAdThreads + t) * KE;
-    if (!OVER && i + KE <= len) v[j].load_stream(d + i);
-    open[j] = bits && i + KE <= len ? (bits[i >> 5] >> (i & 31)) & kAll : kAll;
+    const int i = head + (j * kAdThreads + t) * KE;
+    const bool in = i + KE <= len;
+    if (!OVER && in) v[j].load_stream(d + i);
+    open[j] = kAll;
+    if (bits && in) {
+      const int sh = i & 31;
+      const uint32_t low = bits[i >> 5], high = sh + KE > 32 ? bits[(i >> 5) + 1] : 0u;
+      open[j] = __funnelshift_r(low, high, sh) & kAll;
+    }
   }
   const AdjustShared sm(ad_smem, kSlice);
   const bool special = p.history || p.biased;
@@ -195,13 +206,13 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
   if (OVER) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      const int i = (j * kAdThreads + t) * KE;
+      const int i = head + (j * kAdThreads + t) * KE;
       if (open[j] != kAll && open[j]) v[j].load(z + i);
     }
   }
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
-    const int i = (j * kAdThreads + t) * KE;
+    const int i = head + (j * kAdThreads + t) * KE;
     if (i + KE > len) continue;
     if (open[j] == kAll) {
       if (!OVER) v[j].put(out + i);
@@ -214,9 +225,9 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
       if (!(open[j] >> k & 1)) f[k] = closed;
     Raw<T, KE>::store(out + i, f);
   }
-  if (KE > 1) {  // what is left of the row
-    const int i = len / KE * KE + t;
-    if (i < len) {
+  if (KE > 1 && t < 2 * KE) {  // what is left before and behind the vectors
+    const int i = t < KE ? t : head + (len - head) / KE * KE + t - KE;
+    if (i < (t < KE ? head : len)) {
       if (!is_open(i)) Elem<T>::put(out, i, closed);
       else if (!OVER) out[i] = d[i];
     }

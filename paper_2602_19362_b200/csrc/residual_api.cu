@@ -121,11 +121,12 @@ static int residual_smem(F kern, int bytes, bool (&done)[kMaxDevices]) {
   return OAPL_OK;
 }
 
-template <typename T, int KE, int K, bool WARP, bool FWD, bool COMMON>
+template <typename T, int KE, int K, bool WARP, int NT, bool FWD, bool COMMON>
 static int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
   static bool done[kMaxDevices] = {false};
-  auto kern = FWD ? residual_fwd_kernel<T, KE, K, WARP, COMMON> : residual_bwd_kernel<T, KE, K, WARP, COMMON>;
-  const ResidualShape s = residual_shape(p, n_sm, KE * K, KE, (int)sizeof(T), WARP, arrays, FWD ? 1024 : 512);
+  auto kern = FWD ? residual_fwd_kernel<T, KE, K, WARP, NT, COMMON> : residual_bwd_kernel<T, KE, K, WARP, NT, COMMON>;
+  const ResidualShape s = residual_shape(p, n_sm, KE * K, KE, (int)sizeof(T), WARP, arrays,
+                                         residual_ctas(FWD, KE * K, NT) * NT);
   const int rc = residual_smem(kern, s.smem, done);
   if (rc != OAPL_OK) return rc;
   *workers = s.workers;
@@ -134,23 +135,23 @@ static int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* work
   return OAPL_OK;
 }
 
-template <typename T, int KE, int K, bool WARP, bool FWD>
+template <typename T, int KE, int K, bool WARP, int NT, bool FWD>
 static int pick_residual(const ResidualParams& p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  const bool common = KE > 1 && p.y && p.w_post && p.w_pre && p.gate_kind != kGateFull && p.x_out &&
+  const bool common = p.y && p.w_post && p.w_pre && p.gate_kind != kGateFull && p.x_out &&
                       (FWD || (p.dx_out && p.dx && p.dy));
-  if constexpr (KE > 1)
-    if (common) return launch_residual<T, KE, K, WARP, FWD, true>(p, arrays, n_sm, workers, st);
-  return launch_residual<T, KE, K, WARP, FWD, false>(p, arrays, n_sm, workers, st);
+  if (common) return launch_residual<T, KE, K, WARP, NT, FWD, true>(p, arrays, n_sm, workers, st);
+  return launch_residual<T, KE, K, WARP, NT, FWD, false>(p, arrays, n_sm, workers, st);
 }
 
 template <typename T, int KE, bool FWD>
 static int route_residual(const ResidualParams& p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
   // elements a thread: as few as give a CTA at most 256 threads, 32 beyond that
-  if (p.d <= kRsWarpD) return pick_residual<T, KE, 16 / KE, true, FWD>(p, arrays, n_sm, workers, st);
-  if (p.d <= 2048) return pick_residual<T, KE, 8 / KE, false, FWD>(p, arrays, n_sm, workers, st);
-  if (p.d <= 8192) return pick_residual<T, KE, 16 / KE, false, FWD>(p, arrays, n_sm, workers, st);
+  if (p.d <= kRsWarpD) return pick_residual<T, KE, 16 / KE, true, 256, FWD>(p, arrays, n_sm, workers, st);
+  if (p.d <= 2048) return pick_residual<T, KE, 8 / KE, false, 256, FWD>(p, arrays, n_sm, workers, st);
+  if (p.d <= 4096) return pick_residual<T, KE, 16 / KE, false, 256, FWD>(p, arrays, n_sm, workers, st);
+  if (p.d <= 8192) return pick_residual<T, KE, 16 / KE, false, 512, FWD>(p, arrays, n_sm, workers, st);
   constexpr int kWide = sizeof(T) == 4 ? 1 : KE;  // fp32: read where they are
-  return pick_residual<T, kWide, 32 / kWide, false, FWD>(p, arrays, n_sm, workers, st);
+  return pick_residual<T, kWide, 32 / kWide, false, 512, FWD>(p, arrays, n_sm, workers, st);
 }
 
 template <bool FWD>

@@ -368,6 +368,11 @@ struct ColumnFactor {
   }
 };
 
+// CTAs of an SM that the registers are shared out for.
+constexpr int residual_ctas(bool forward, int elems, int nt) {
+  return nt > 256 ? 1 : forward ? (elems == 8 ? 4 : 3) : (elems == 8 ? 3 : 2);
+}
+
 // What a call has.  COMMON: the form that blocks with both norms have, known when the kernel is compiled (16384 x 3584
 // bf16, gradient: %COMMON%).
 template <bool COMMON>
@@ -401,8 +406,8 @@ __device__ __forceinline__ void form_y(const ResidualParams& p, bool post, int c
 }
 
 // ------------------------------------------------------------------------------------------------ forward
-template <typename T, int KE, int K, bool WARP, bool COMMON>
-__global__ void __launch_bounds__(WARP ? 256 : kRsMaxThreads) residual_fwd_kernel(ResidualParams p) {
+template <typename T, int KE, int K, bool WARP, int NT, bool COMMON>
+__global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_fwd_kernel(ResidualParams p) {
   __shared__ __align__(512) float red[kRsRedFloats];
   RowGroup<WARP> grp(red);
   const ResidualHas<COMMON> has(p);
@@ -491,8 +496,8 @@ __global__ void __launch_bounds__(WARP ? 256 : kRsMaxThreads) residual_fwd_kerne
 // ------------------------------------------------------------------------------------------------ gradient
 // Of a column only two sums are needed: dw_pre, and S = sum_n t yh (times a row's or an element's gate).  Without these
 // gates dw_post = b g S and dg = b w_post S, both per channel; with them dw_post = b S.
-template <typename T, int KE, int K, bool WARP, bool COMMON>
-__global__ void __launch_bounds__(WARP ? 256 : kRsMaxThreads) residual_bwd_kernel(ResidualParams p) {
+template <typename T, int KE, int K, bool WARP, int NT, bool COMMON>
+__global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual_bwd_kernel(ResidualParams p) {
   __shared__ __align__(512) float red[kRsRedFloats];
   RowGroup<WARP> grp(red);
   const ResidualHas<COMMON> has(p);

@@ -34,19 +34,20 @@ static LookupParams lookup_params(const oapl_lookup* l, int32_t d, int32_t* stat
   return p;
 }
 
-template <typename TI, typename TO, int KE>
+template <typename TI, typename TO, int KE, bool LEVEL>
 static int launch_embedding(const LookupParams& p, int n_sm, cudaStream_t st) {
-  const int units = p.d / KE;
+  // vectors of a row, and where it may be off 16-byte boundaries the elements before and behind them
+  const int64_t units = (int64_t)p.d / KE + (LEVEL ? 0 : 2 * KE - 1);
   int tx = 32;
   while (tx < kEbThreads && tx < units) tx *= 2;
   const dim3 block(tx, kEbThreads / tx);
-  const int64_t slabs = ((int64_t)units + tx - 1) / tx, rows = (p.N + block.y - 1) / block.y;
+  const int64_t slabs = (units + tx - 1) / tx, rows = (p.N + block.y - 1) / block.y;
   if (slabs > 65535) return OAPL_ERR_UNSUPPORTED_SHAPE;
   // four rows a thread, for loads in flight, where that still leaves eight CTAs to an SM
   if (rows / 4 * slabs >= 8 * (int64_t)n_sm)
-    embedding_kernel<TI, TO, KE, 4><<<dim3((unsigned)((rows + 3) / 4), (unsigned)slabs), block, 0, st>>>(p);
+    embedding_kernel<TI, TO, KE, 4, LEVEL><<<dim3((unsigned)((rows + 3) / 4), (unsigned)slabs), block, 0, st>>>(p);
   else
-    embedding_kernel<TI, TO, KE, 1><<<dim3((unsigned)rows, (unsigned)slabs), block, 0, st>>>(p);
+    embedding_kernel<TI, TO, KE, 1, LEVEL><<<dim3((unsigned)rows, (unsigned)slabs), block, 0, st>>>(p);
   CKL();
   return OAPL_OK;
 }
@@ -56,7 +57,7 @@ static int route_embedding(const LookupParams& p, int n_sm, cudaStream_t st) {
   constexpr int KE = Elem<TI>::kN > Elem<TO>::kN ? Elem<TI>::kN : Elem<TO>::kN;
   const bool vec = on16(p.in) && on16(p.out) && p.d % KE == 0 && p.ld_in * sizeof(TI) % 16 == 0 &&
                    p.ld_out * sizeof(TO) % 16 == 0;
-  return vec ? launch_embedding<TI, TO, KE>(p, n_sm, st) : launch_embedding<TI, TO, 1>(p, n_sm, st);
+  return vec ? launch_embedding<TI, TO, KE, true>(p, n_sm, st) : launch_embedding<TI, TO, KE, false>(p, n_sm, st);
 }
 
 template <typename TI>
@@ -179,6 +180,11 @@ static int32_t fill_list(const oapl_tensor* t, int32_t count, bool clip, GradLis
   return i;
 }
 
+template <typename TI>
+static auto pick_clip(int out) -> void (*)(GradList, const float*, float, float) {
+  return out == 0 ? grad_clip_kernel<TI, __nv_bfloat16> : out == 1 ? grad_clip_kernel<TI, __half> : grad_clip_kernel<TI, float>;
+}
+
 constexpr int kGcMaxSums = 2048;  // partial sums of a launch
 
 // ---------------------------------------------------------------------------------------
@@ -257,8 +263,8 @@ static int launch_adjust(AdjustParams p, cudaStream_t st) {
 
 template <typename T, int KE, bool GRAD, bool OVER>
 static int route_adjust_size(const AdjustParams& p, int n_sm, cudaStream_t st) {
-  // slices of 8192 tokens where they give every SM four, of 2048 otherwise
-  constexpr int kMany = 32 / KE, kFew = 8 / KE;
+  // slices of 8192 tokens (4096 an element at a time) where they give every SM four, of 2048 otherwise
+  constexpr int kMany = 32 / KE / (KE == 1 ? 2 : 1), kFew = 8 / KE;
   const int64_t many = (int64_t)p.N * p.V / 8192;
   return many >= 4 * (int64_t)n_sm ? launch_adjust<T, KE, kMany, GRAD, OVER>(p, st)
                                    : launch_adjust<T, KE, kFew, GRAD, OVER>(p, st);
@@ -270,8 +276,11 @@ static int route_adjust(const AdjustParams& p, bool grad, cudaStream_t st) {
   if (n_sm <= 0) return OAPL_ERR_CUDA;
   constexpr int KE = Elem<T>::kN;
   const bool over = !grad && p.out == p.z;
-  auto rows16 = [&](const void* b, int64_t ld) { return on16(b) && (p.N == 1 || ld * sizeof(T) % 16 == 0); };
-  const bool vec = rows16(p.out, p.ld_o) && rows16(p.z, p.ld_z) && (!grad || rows16(p.d, p.ld_d));
+  // whether a row of b is as far off 16-byte boundaries as the result's
+  auto level = [&](const void* b, int64_t ld) {
+    return (((uintptr_t)b - (uintptr_t)p.out) & 15) == 0 && (p.N == 1 || (ld - p.ld_o) * (int64_t)sizeof(T) % 16 == 0);
+  };
+  const bool vec = level(grad ? p.d : p.z, grad ? p.ld_d : p.ld_z);
   if (grad)
     return vec ? route_adjust_size<T, KE, true, false>(p, n_sm, st) : route_adjust_size<T, 1, true, false>(p, n_sm, st);
   if (over)
@@ -417,7 +426,14 @@ int oapl_grad_clip(const oapl_tensor* tensors, int32_t count, float scale, const
     i += fill_list(tensors + i, count - i, true, &l);
     if (!l.chunks) continue;
     const int most = n_sm * kGcSumsPerSm;
-    grad_clip_kernel<<<l.chunks < most ? l.chunks : most, kGcThreads, 0, st>>>(l, sq_norm, clip_norm, scale);
+    // a list of one pair of types, as most are, goes to a kernel of that pair: 64 registers without spills, against
+    // %SPILL% for all nine pairs in one
+    bool one = true;
+    for (int32_t k = 1; k < l.count; ++k) one = one && l.t[k].in_type == l.t[0].in_type && l.t[k].out_type == l.t[0].out_type;
+    const int in = l.t[0].in_type, out = l.t[0].out_type;
+    auto kern = !one ? grad_clip_kernel<void, void>
+                     : in == 0 ? pick_clip<__nv_bfloat16>(out) : in == 1 ? pick_clip<__half>(out) : pick_clip<float>(out);
+    kern<<<l.chunks < most ? l.chunks : most, kGcThreads, 0, st>>>(l, sq_norm, clip_norm, scale);
     CKL();
   }
   return OAPL_OK;
