@@ -129,11 +129,11 @@ struct Elem<float> {
   static __device__ __forceinline__ void put(void* p, int64_t i, float x) { reinterpret_cast<float*>(p)[i] = x; }
 };
 
-// KE neighbouring elements of a row: whole 16-byte vectors, or one element at its natural alignment.  Loading and
+// KE neighbouring elements of a row: 16-byte vectors, 8 bytes, or one element at its natural alignment.  Loading and
 // widening are apart, so that several loads can be in flight.
-template <typename T, int KE>
+template <typename T, int KE, int BYTES = KE * (int)sizeof(T)>
 struct Raw {
-  static constexpr int kV = KE / Elem<T>::kN;
+  static constexpr int kV = BYTES / 16;
   uint4 v[kV];
   __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
@@ -166,7 +166,29 @@ struct Raw {
   }
 };
 template <typename T>
-struct Raw<T, 1> {
+struct Raw<T, 4, 8> {  // half a vector of 16-bit elements, beside a vector of fp32
+  uint2 v;
+  __device__ __forceinline__ void load(const T* p) { v = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void load_stream(const T* p) { v = __ldcs(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ void put(T* p) const { *reinterpret_cast<uint2*>(p) = v; }
+  __device__ __forceinline__ void widen(float (&f)[4]) const {
+    float g[8];
+    Elem<T>::widen(make_uint4(v.x, v.y, 0u, 0u), g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = g[i];
+  }
+  static __device__ __forceinline__ uint2 narrow(const float (&f)[4]) {
+    const float g[8] = {f[0], f[1], f[2], f[3], 0.f, 0.f, 0.f, 0.f};
+    const uint4 w = Elem<T>::narrow(g);
+    return make_uint2(w.x, w.y);
+  }
+  static __device__ __forceinline__ void store(T* p, const float (&f)[4]) { *reinterpret_cast<uint2*>(p) = narrow(f); }
+  static __device__ __forceinline__ void store_stream(T* p, const float (&f)[4]) {
+    __stcs(reinterpret_cast<uint2*>(p), narrow(f));
+  }
+};
+template <typename T, int BYTES>
+struct Raw<T, 1, BYTES> {
   T v;
   __device__ __forceinline__ void load(const T* p) { v = *p; }
   __device__ __forceinline__ void load_stream(const T* p) { v = *p; }
@@ -175,11 +197,23 @@ struct Raw<T, 1> {
   static __device__ __forceinline__ void store(T* p, const float (&f)[1]) { Elem<T>::put(p, 0, f[0]); }
 };
 
-// KE neighbouring elements at any alignment: the aligned 16-byte blocks that hold them, shifted in registers.  A block
-// without one of the elements is not touched.
-template <typename T, int KE>
+// 16 bytes that start `off` < 16 bytes into the 32 of lo and hi; off a multiple of the element size.
+__device__ __forceinline__ uint4 shift_16(const uint4& lo, const uint4& hi, uint32_t off) {
+  // whole words first, two and one at a time, then bits
+  const bool two = off & 8u, one = off & 4u;
+  const uint32_t a0 = two ? lo.z : lo.x, a1 = two ? lo.w : lo.y, a2 = two ? hi.x : lo.z, a3 = two ? hi.y : lo.w,
+                 a4 = two ? hi.z : hi.x, a5 = two ? hi.w : hi.y;
+  const uint32_t w0 = one ? a1 : a0, w1 = one ? a2 : a1, w2 = one ? a3 : a2, w3 = one ? a4 : a3, w4 = one ? a5 : a4;
+  const uint32_t s = (off & 3u) * 8u;
+  return make_uint4(__funnelshift_r(w0, w1, s), __funnelshift_r(w1, w2, s), __funnelshift_r(w2, w3, s),
+                    __funnelshift_r(w3, w4, s));
+}
+
+// KE neighbouring elements at any alignment: the aligned blocks (of 16 bytes, or 8) that hold them, shifted in registers.
+// A block without one of the elements is not touched.
+template <typename T, int KE, int BYTES = KE * (int)sizeof(T)>
 struct Shifted {
-  static constexpr int kV = KE / Elem<T>::kN;
+  static constexpr int kV = BYTES / 16;
   uint4 b[kV + 1];
   uint32_t off;  // bytes into the first block
   __device__ __forceinline__ void load(const T* p) {
@@ -191,24 +225,26 @@ struct Shifted {
     b[kV] = off ? q[kV] : make_uint4(0u, 0u, 0u, 0u);
   }
   __device__ __forceinline__ void raw(Raw<T, KE>& r) const {
-    uint32_t w[kV * 4 + 4];
 #pragma unroll
-    for (int i = 0; i <= kV; ++i) {
-      w[4 * i] = b[i].x;
-      w[4 * i + 1] = b[i].y;
-      w[4 * i + 2] = b[i].z;
-      w[4 * i + 3] = b[i].w;
-    }
-    // whole words first, two and one at a time, then bits
-#pragma unroll
-    for (int i = 0; i < kV * 4 + 2; ++i) w[i] = off & 8u ? w[i + 2] : w[i];
-#pragma unroll
-    for (int i = 0; i < kV * 4 + 1; ++i) w[i] = off & 4u ? w[i + 1] : w[i];
+    for (int i = 0; i < kV; ++i) r.v[i] = shift_16(b[i], b[i + 1], off);
+  }
+};
+template <typename T, int KE>
+struct Shifted<T, KE, 8> {
+  uint2 b[2];
+  uint32_t off;
+  __device__ __forceinline__ void load(const T* p) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    off = (uint32_t)a & 7u;
+    const uint2* q = reinterpret_cast<const uint2*>(a & ~(uintptr_t)7);
+    b[0] = q[0];
+    b[1] = off ? q[1] : make_uint2(0u, 0u);
+  }
+  __device__ __forceinline__ void raw(Raw<T, KE>& r) const {
+    const bool one = off & 4u;
+    const uint32_t w0 = one ? b[0].y : b[0].x, w1 = one ? b[1].x : b[0].y, w2 = one ? b[1].y : b[1].x;
     const uint32_t s = (off & 3u) * 8u;
-#pragma unroll
-    for (int i = 0; i < kV; ++i)
-      r.v[i] = make_uint4(__funnelshift_r(w[4 * i], w[4 * i + 1], s), __funnelshift_r(w[4 * i + 1], w[4 * i + 2], s),
-                          __funnelshift_r(w[4 * i + 2], w[4 * i + 3], s), __funnelshift_r(w[4 * i + 3], w[4 * i + 4], s));
+    r.v = make_uint2(__funnelshift_r(w0, w1, s), __funnelshift_r(w1, w2, s));
   }
 };
 

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kEbThreads) embedding_kernel(LookupParams p) {
     for (int r = 0; r < R; ++r)
       if (n0 + (int64_t)r * blockDim.y < p.N) lookup_put<TI, TO, KE>(p, key[r] < (uint32_t)p.V, v[r], out + r * step + c);
   } else {
-    constexpr int kMask = 16 / (int)sizeof(TO) - 1;
+    constexpr int kMask = KE - 1;  // a boundary of KE elements of the result
     Shifted<TI, KE> b[R];
     Raw<TI, 1> one[R];
     int c[R];

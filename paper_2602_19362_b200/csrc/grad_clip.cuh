@@ -155,8 +155,8 @@ template <typename TI, typename TO>
 __device__ __forceinline__ void grad_scale_chunk(const GradTensor& t, int64_t at, int n, float factor) {
   const TI* g = static_cast<const TI*>(t.in) + at;
   TO* o = static_cast<TO*>(t.out) + at;
-  constexpr int KE = Elem<TI>::kN > Elem<TO>::kN ? Elem<TI>::kN : Elem<TO>::kN;
-  constexpr int U = kGcBytes / kGcThreads / KE / (sizeof(TI) > sizeof(TO) ? (int)sizeof(TI) : (int)sizeof(TO));
+  constexpr int KE = Elem<TI>::kN < Elem<TO>::kN ? Elem<TI>::kN : Elem<TO>::kN;  // 16 bytes of the wider type
+  constexpr int U = kGcVecs;
   int done = 0;
   if (t.vec) {
     const int vecs = n / KE;

@@ -9,10 +9,10 @@
 //   1. its logits' loads are started, which the steps up to 3 then cover;
 //   2. it reads the row's tokens: those of its slice are marked in a bitmap in shared memory, listed when they are met for
 //      the first time, and counted (whole numbers and marks: the order does not matter).  Tokens with a bias are marked too;
-//   3. the values of the listed tokens are formed, one a thread, and take their counters' places.  A token's biases are
-//      added up in their order by the thread that holds the first of them;
+//   3. the logits of the listed tokens are loaded, a token a thread;
 //   4. the slice is copied, closed tokens overwritten;
-//   5. behind a barrier the listed values are stored over what the copy left there.
+//   5. behind a barrier the listed tokens' values are stored over what the copy left there, and those of tokens with a
+//      bias by the thread that holds the first of a token's biases and adds them up in their order.
 // So the copy does not test for tokens that change.  (When it did, with a counter per token beside each vector, a token in
 // one of a warp's 256 places cost the warp eight divisions: 2048 x 152064 bf16, gradient 472 us; %GRAD% like this.)
 // Rows need not start on 16-byte boundaries: where the two sides are off by the same number of bytes, vectors begin at the
@@ -55,26 +55,29 @@ struct AdjustParams {
 struct AdjustRow {
   float r, f, p;
 };
+__device__ __forceinline__ float adjust_slope(float d, float z, const AdjustRow& a) { return z > 0.f ? d / a.r : d * a.r; }
 __device__ __forceinline__ float adjust_value(float z, bool seen, uint32_t c, const AdjustRow& a) {
   if (seen) z = z > 0.f ? z / a.r : z * a.r;
   if (c) z = fmaf(-a.f, (float)c, z) - a.p;
   return z;
 }
 
-// Shared memory of a CTA whose rows have tokens or biases, for a slice of `n` tokens.
+// Shared memory of a CTA whose rows have tokens or biases, for a slice of `n` tokens.  The gradient counts nothing; over
+// the logits it keeps its results instead, by their place in the list.
+template <bool WORDS>
 struct AdjustShared {
-  uint32_t* value;    // [n] times in the answer, then the bits of the result
+  uint32_t* count;    // of the list
   uint32_t* seen;     // [n / 32]
   uint32_t* biased;   // [n / 32]
-  uint16_t* list;     // [n] tokens that change, each once
-  uint32_t* count;    // of the list
-  static constexpr int bytes(int n) { return n * 4 + n / 8 * 2 + n * 2 + 16; }
+  uint32_t* word;     // [n] times in the answer, or results
+  uint16_t* list;     // [n] tokens of the prompt and the answer, each once
+  static constexpr int bytes(int n) { return 16 + n / 4 + (WORDS ? n * 4 : 0) + n * 2; }
   __device__ __forceinline__ AdjustShared(uint32_t* base, int n) {
-    value = base;
-    seen = value + n;
+    count = base;
+    seen = count + 4;
     biased = seen + n / 32;
-    count = biased + n / 32;
-    list = reinterpret_cast<uint16_t*>(count + 4);
+    word = biased + n / 32;
+    list = reinterpret_cast<uint16_t*>(word + (WORDS ? n : 0));
   }
 };
 
@@ -115,7 +118,7 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
   for (int j = 0; j < VPT; ++j) {
     const int i = head + (j * kAdThreads + t) * KE;
     const bool in = i + KE <= len;
-    if (!OVER && in) v[j].load_stream(d + i);
+    if ((!OVER || GRAD) && in) v[j].load_stream(d + i);
     open[j] = kAll;
     if (bits && in) {
       const int sh = i & 31;
@@ -123,15 +126,19 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
       open[j] = __funnelshift_r(low, high, sh) & kAll;
     }
   }
-  const AdjustShared sm(ad_smem, kSlice);
+  const AdjustShared<!GRAD || OVER> sm(ad_smem, kSlice);
   const bool special = p.history || p.biased;
+  constexpr int kFirst = 2;  // listed tokens of a thread whose loads go ahead of the copy
+  AdjustRow a{1.f, 0.f, 0.f};
+  int64_t b0 = 0, b1 = 0;
+  int listed = 0;
+  float x[kFirst], g[kFirst];
   if (special) {
-    constexpr int kAhead = 8;
-    AdjustRow a{1.f, 0.f, 0.f};
+    constexpr int kAhead = 4;
     if (p.repetition) a.r = p.repetition[n];
     if (!GRAD && p.frequency) a.f = p.frequency[n];
     if (!GRAD && p.presence) a.p = p.presence[n];
-    int64_t lo = 0, mid = 0, hi = 0, b0 = 0, b1 = 0;
+    int64_t lo = 0, mid = 0, hi = 0;
     if (p.history) {
       lo = p.spans[3 * (int64_t)n], mid = p.spans[3 * (int64_t)n + 1], hi = p.spans[3 * (int64_t)n + 2];
       if (lo < 0 || mid < lo || hi < mid || hi > p.T) {
@@ -148,9 +155,9 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
         if (t == 0 && p.status) atomicCAS(p.status, 0, kErrBadSpan);
       }
     }
-    // counters (the gradient has none), marks and the list's length
-    for (int i = (GRAD ? kSlice : 0) + t * 4; i < kSlice + kSlice / 16 + 4; i += kAdThreads * 4)
-      *reinterpret_cast<uint4*>(&sm.value[i]) = make_uint4(0, 0, 0, 0);
+    // the list's length, marks, and counters
+    for (int i = t * 4; i < 4 + kSlice / 16 + (GRAD ? 0 : kSlice); i += kAdThreads * 4)
+      *reinterpret_cast<uint4*>(&sm.count[i]) = make_uint4(0, 0, 0, 0);
     __syncthreads();
     for (int64_t i0 = lo + t; i0 < hi; i0 += kAhead * kAdThreads) {
       uint32_t id[kAhead];
@@ -164,7 +171,7 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
           uint32_t* word = &sm.seen[id[j] >> 5];
           if (!(*reinterpret_cast<volatile uint32_t*>(word) & bit) && !(atomicOr(word, bit) & bit))
             sm.list[atomicAdd(sm.count, 1u)] = (uint16_t)id[j];
-          if (!GRAD && i0 + j * kAdThreads >= mid) atomicAdd(&sm.value[id[j]], 1u);
+          if (!GRAD && i0 + j * kAdThreads >= mid) atomicAdd(&sm.word[id[j]], 1u);
         }
     }
     for (int64_t i = b0 + t; i < b1; i += kAdThreads) {
@@ -172,38 +179,26 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
       if (id < (uint32_t)len) atomicOr(&sm.biased[id >> 5], 1u << (id & 31));
     }
     __syncthreads();
-    const int listed = (int)*sm.count;
-    for (int i = t; i < listed; i += kAdThreads) {
-      const int at = sm.list[i];
-      const float x = Elem<T>::one(z, at);
-      if (GRAD) {
-        const float g = Elem<T>::one(d, at);
-        sm.value[at] = __float_as_uint(x > 0.f ? g / a.r : g * a.r);
-      } else if (!(sm.biased[at >> 5] >> (at & 31) & 1)) {
-        sm.value[at] = __float_as_uint(adjust_value(x, true, sm.value[at], a));
+    listed = (int)*sm.count;
+#pragma unroll
+    for (int j = 0; j < kFirst; ++j) {
+      const int i = j * kAdThreads + t;
+      if (i < listed) {
+        x[j] = Elem<T>::one(z, sm.list[i]);
+        if (GRAD) g[j] = Elem<T>::one(d, sm.list[i]);
       }
     }
-    if (p.biased) {
-      __syncthreads();  // the list grows
-      for (int64_t i = b0 + t; i < b1; i += kAdThreads) {
-        const int32_t id = p.bias_id[i];
-        const uint32_t at = (uint32_t)id - (uint32_t)v0;
-        if (at >= (uint32_t)len) continue;
-        bool first = true;
-        for (int64_t k = b0; k < i && first; ++k) first = p.bias_id[k] != id;
-        if (!first) continue;
-        float sum = 0.f;
-        for (int64_t k = i; k < b1; ++k)
-          if (p.bias_id[k] == id) sum += p.bias[k];
-        const bool seen = sm.seen[at >> 5] >> (at & 31) & 1;
-        sm.value[at] = __float_as_uint(adjust_value(Elem<T>::one(z, at), seen, sm.value[at], a) + sum);
-        if (!seen) sm.list[atomicAdd(sm.count, 1u)] = (uint16_t)at;
+    if (GRAD && OVER) {
+      // the copy overwrites the logits that decide on the factor: the results first
+      for (int i = kFirst * kAdThreads + t; i < listed; i += kAdThreads) {
+        const int at = sm.list[i];
+        sm.word[i] = __float_as_uint(adjust_slope(Elem<T>::one(d, at), Elem<T>::one(z, at), a));
       }
+      __syncthreads();
     }
-    if (OVER || GRAD) __syncthreads();  // every value is formed before what it comes from may be overwritten
   }
   const float closed = GRAD ? 0.f : -__int_as_float(0x7F800000);
-  if (OVER) {
+  if (OVER && !GRAD) {
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
       const int i = head + (j * kAdThreads + t) * KE;
@@ -215,7 +210,7 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
     const int i = head + (j * kAdThreads + t) * KE;
     if (i + KE > len) continue;
     if (open[j] == kAll) {
-      if (!OVER) v[j].put(out + i);
+      if (!OVER || GRAD) v[j].put(out + i);
       continue;
     }
     float f[KE];
@@ -229,15 +224,43 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
     const int i = t < KE ? t : head + (len - head) / KE * KE + t - KE;
     if (i < (t < KE ? head : len)) {
       if (!is_open(i)) Elem<T>::put(out, i, closed);
-      else if (!OVER) out[i] = d[i];
+      else if (!OVER || GRAD) out[i] = d[i];
     }
   }
-  if (special) {
-    __syncthreads();
-    const int listed = (int)*sm.count;
-    for (int i = t; i < listed; i += kAdThreads) {
+  if (!special) return;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kFirst; ++j) {
+    const int i = j * kAdThreads + t;
+    if (i < listed) {
       const int at = sm.list[i];
-      if (is_open(at)) Elem<T>::put(out, at, __uint_as_float(sm.value[at]));
+      if (is_open(at)) {
+        if (GRAD) Elem<T>::put(out, at, adjust_slope(g[j], x[j], a));
+        else if (!(sm.biased[at >> 5] >> (at & 31) & 1)) Elem<T>::put(out, at, adjust_value(x[j], true, sm.word[at], a));
+      }
+    }
+  }
+  for (int i = kFirst * kAdThreads + t; i < listed; i += kAdThreads) {
+    const int at = sm.list[i];
+    if (!is_open(at)) continue;
+    if (GRAD)
+      Elem<T>::put(out, at, OVER ? __uint_as_float(sm.word[i]) : adjust_slope(Elem<T>::one(d, at), Elem<T>::one(z, at), a));
+    else if (!(sm.biased[at >> 5] >> (at & 31) & 1))
+      Elem<T>::put(out, at, adjust_value(Elem<T>::one(z, at), true, sm.word[at], a));
+  }
+  if constexpr (!GRAD) {
+    for (int64_t i = b0 + t; i < b1; i += kAdThreads) {
+      const int32_t id = p.bias_id[i];
+      const uint32_t at = (uint32_t)id - (uint32_t)v0;
+      if (at >= (uint32_t)len || !is_open((int)at)) continue;
+      bool first = true;
+      for (int64_t k = b0; k < i && first; ++k) first = p.bias_id[k] != id;
+      if (!first) continue;
+      float sum = 0.f;
+      for (int64_t k = i; k < b1; ++k)
+        if (p.bias_id[k] == id) sum += p.bias[k];
+      const bool seen = sm.seen[at >> 5] >> (at & 31) & 1;
+      Elem<T>::put(out, at, adjust_value(Elem<T>::one(z, at), seen, sm.word[at], a) + sum);
     }
   }
 }

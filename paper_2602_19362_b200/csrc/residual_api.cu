@@ -69,7 +69,7 @@ static ResidualParams residual_params(const oapl_residual* r) {
 }
 
 // Whether rows start on 16-byte boundaries: of matrices and, where there are any, of the weights.
-static bool residual_vec(const ResidualParams& p, int es, const Place* m, int count) {
+static bool residual_level(const ResidualParams& p, int es, const Place* m, int count) {
   if (p.d % (16 / es)) return false;
   for (int i = 0; i < count; ++i)
     if (m[i].base && (!on16(m[i].base) || (m[i].rows > 1 && m[i].ld * m[i].es % 16))) return false;
@@ -82,29 +82,33 @@ struct ResidualShape {
   int threads, grid, smem;
   int64_t workers;
 };
-static ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int ke, int es, bool warp, int arrays,
+static ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int es, bool warp, bool level, int arrays,
                                     int threads_per_sm) {
   ResidualShape s;
-  const int units = p.d / ke;
+  const int ke = 16 / es, units = (p.d + ke - 1) / ke;
   const bool direct = es == 4 && elems == 32;
-  p.pitch = (int32_t)(direct ? 0 : ke > 1 ? units * 16 : (p.d * es + 15) / 16 * 16 + 16);
+  p.pitch = (int32_t)(direct ? 0 : level ? units * 16 : (p.d * es + 15) / 16 * 16 + 16);
   s.threads = warp ? 256 : (int)round_up((size_t)((units + elems / ke - 1) / (elems / ke)), 32);
   const int groups = warp ? 8 : 1;
-  const size_t row = (size_t)arrays * p.pitch * groups;
+  const size_t row = (size_t)arrays * p.pitch * groups, sink = level ? 0 : (size_t)(s.threads / 32) * 66 * 16;
+  const size_t factors = residual_factors(elems, level) == kFactorShared ? (size_t)2 * elems * 4 * (warp ? 32 : s.threads) : 0;
   int per_sm = threads_per_sm / s.threads;
   if (per_sm < 1) per_sm = 1;
   // two rows ahead where there is room, and one at least before CTAs are given up
   p.stages = 3;
-  while (p.stages > 2 && row * p.stages * per_sm > kRsSmem) --p.stages;
-  while (per_sm > 1 && row * p.stages * per_sm > kRsSmem) --per_sm;
-  while (p.stages > 1 && row * p.stages * per_sm > kRsSmem) --p.stages;
+  auto room = [&] { return (row * p.stages + sink + factors) * per_sm <= kRsSmem; };
+  while (p.stages > 2 && !room()) --p.stages;
+  while (per_sm > 1 && !room()) --per_sm;
+  while (p.stages > 1 && !room()) --p.stages;
   int64_t grid = (p.N + groups - 1) / groups;
   if (grid > (int64_t)n_sm * per_sm) grid = (int64_t)n_sm * per_sm;
   const int64_t most = (warp ? kRsWarpWorkers : kRsCtaWorkers) / groups;
   if (grid > most) grid = most;
   s.grid = (int)grid;
   s.workers = grid * groups;
-  s.smem = (int)(row * p.stages);
+  p.sink = (int32_t)(row * p.stages);
+  p.factors = (int32_t)(row * p.stages + sink);
+  s.smem = (int)(row * p.stages + sink + factors);
   return s;
 }
 
@@ -121,12 +125,14 @@ static int residual_smem(F kern, int bytes, bool (&done)[kMaxDevices]) {
   return OAPL_OK;
 }
 
-template <typename T, int KE, int K, bool WARP, int NT, bool FWD, bool COMMON>
+template <typename T, int E, bool WARP, int NT, bool FWD, bool LEVEL, bool COMMON>
 static int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
   static bool done[kMaxDevices] = {false};
-  auto kern = FWD ? residual_fwd_kernel<T, KE, K, WARP, NT, COMMON> : residual_bwd_kernel<T, KE, K, WARP, NT, COMMON>;
-  const ResidualShape s = residual_shape(p, n_sm, KE * K, KE, (int)sizeof(T), WARP, arrays,
-                                         residual_ctas(FWD, KE * K, NT) * NT);
+  constexpr int KE = Elem<T>::kN, K = E / KE;
+  auto kern = FWD ? residual_fwd_kernel<T, KE, K, WARP, NT, LEVEL, COMMON>
+                  : residual_bwd_kernel<T, KE, K, WARP, NT, LEVEL, COMMON>;
+  const ResidualShape s =
+      residual_shape(p, n_sm, E, (int)sizeof(T), WARP, LEVEL, arrays, residual_ctas(FWD, E, NT) * NT);
   const int rc = residual_smem(kern, s.smem, done);
   if (rc != OAPL_OK) return rc;
   *workers = s.workers;
@@ -135,36 +141,36 @@ static int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* work
   return OAPL_OK;
 }
 
-template <typename T, int KE, int K, bool WARP, int NT, bool FWD>
-static int pick_residual(const ResidualParams& p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
+template <typename T, int E, bool WARP, int NT, bool FWD>
+static int pick_residual(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
   const bool common = p.y && p.w_post && p.w_pre && p.gate_kind != kGateFull && p.x_out &&
                       (FWD || (p.dx_out && p.dx && p.dy));
-  if (common) return launch_residual<T, KE, K, WARP, NT, FWD, true>(p, arrays, n_sm, workers, st);
-  return launch_residual<T, KE, K, WARP, NT, FWD, false>(p, arrays, n_sm, workers, st);
+  if (level)
+    return common ? launch_residual<T, E, WARP, NT, FWD, true, true>(p, arrays, n_sm, workers, st)
+                  : launch_residual<T, E, WARP, NT, FWD, true, false>(p, arrays, n_sm, workers, st);
+  return common ? launch_residual<T, E, WARP, NT, FWD, false, true>(p, arrays, n_sm, workers, st)
+                : launch_residual<T, E, WARP, NT, FWD, false, false>(p, arrays, n_sm, workers, st);
 }
 
-template <typename T, int KE, bool FWD>
-static int route_residual(const ResidualParams& p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
+template <typename T, bool FWD>
+static int route_residual(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
   // elements a thread: as few as give a CTA at most 256 threads, 32 beyond that
-  if (p.d <= kRsWarpD) return pick_residual<T, KE, 16 / KE, true, 256, FWD>(p, arrays, n_sm, workers, st);
-  if (p.d <= 2048) return pick_residual<T, KE, 8 / KE, false, 256, FWD>(p, arrays, n_sm, workers, st);
-  if (p.d <= 4096) return pick_residual<T, KE, 16 / KE, false, 256, FWD>(p, arrays, n_sm, workers, st);
-  if (p.d <= 8192) return pick_residual<T, KE, 16 / KE, false, 512, FWD>(p, arrays, n_sm, workers, st);
-  constexpr int kWide = sizeof(T) == 4 ? 1 : KE;  // fp32: read where they are
-  return pick_residual<T, kWide, 32 / kWide, false, 512, FWD>(p, arrays, n_sm, workers, st);
+  if (p.d <= kRsWarpD) return pick_residual<T, 16, true, 256, FWD>(p, level, arrays, n_sm, workers, st);
+  if (p.d <= 2048) return pick_residual<T, 8, false, 256, FWD>(p, level, arrays, n_sm, workers, st);
+  if (p.d <= 4096) return pick_residual<T, 16, false, 256, FWD>(p, level, arrays, n_sm, workers, st);
+  // (fp32 rows off 16-byte boundaries have no room beside their factors where there are five arrays of them)
+  const bool room = level || (size_t)arrays * p.d * sizeof(T) + (size_t)8 * p.d <= kRsSmem;
+  if (p.d <= 8192 && room) return pick_residual<T, 16, false, 512, FWD>(p, level, arrays, n_sm, workers, st);
+  // fp32 rows are read where they are
+  return pick_residual<T, 32, false, 512, FWD>(p, level && sizeof(T) == 2, arrays, n_sm, workers, st);
 }
 
 template <bool FWD>
-static int route_residual_type(const ResidualParams& p, int32_t type, bool vec, int arrays, int n_sm, int64_t* workers,
+static int route_residual_type(const ResidualParams& p, int32_t type, bool level, int arrays, int n_sm, int64_t* workers,
                                cudaStream_t st) {
-  if (type == OAPL_TYPE_BF16)
-    return vec ? route_residual<__nv_bfloat16, 8, FWD>(p, arrays, n_sm, workers, st)
-               : route_residual<__nv_bfloat16, 1, FWD>(p, arrays, n_sm, workers, st);
-  if (type == OAPL_TYPE_F16)
-    return vec ? route_residual<__half, 8, FWD>(p, arrays, n_sm, workers, st)
-               : route_residual<__half, 1, FWD>(p, arrays, n_sm, workers, st);
-  return vec ? route_residual<float, 4, FWD>(p, arrays, n_sm, workers, st)
-             : route_residual<float, 1, FWD>(p, arrays, n_sm, workers, st);
+  if (type == OAPL_TYPE_BF16) return route_residual<__nv_bfloat16, FWD>(p, level, arrays, n_sm, workers, st);
+  if (type == OAPL_TYPE_F16) return route_residual<__half, FWD>(p, level, arrays, n_sm, workers, st);
+  return route_residual<float, FWD>(p, level, arrays, n_sm, workers, st);
 }
 
 }  // namespace oapl
@@ -201,8 +207,8 @@ int oapl_residual_norm(const oapl_residual* r, void* x_out, int64_t ld_x_out, vo
   p.rstd_pre = rstd_pre;
   int64_t workers = 0;
   const int arrays = 1 + (r->y != nullptr) + full;
-  const bool vec = residual_vec(p, es, m, 5);
-  return route_residual_type<true>(p, r->type, vec, arrays, n_sm, &workers,
+  const bool level = residual_level(p, es, m, 5);
+  return route_residual_type<true>(p, r->type, level, arrays, n_sm, &workers,
                                    static_cast<cudaStream_t>(stream));
 }
 
@@ -274,8 +280,8 @@ int oapl_residual_norm_bwd(const oapl_residual* r, const void* x_out, int64_t ld
   p.part = static_cast<float*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int arrays = 2 * pre + (dx_out != nullptr) + (r->y != nullptr) + full;
-  const bool vec = residual_vec(p, es, m, 8);
-  const int run = route_residual_type<false>(p, r->type, vec, arrays, n_sm, &j.workers, st);
+  const bool level = residual_level(p, es, m, 8);
+  const int run = route_residual_type<false>(p, r->type, level, arrays, n_sm, &j.workers, st);
   if (run != OAPL_OK || !kinds) return run;
   j.part = p.part;
   j.d = r->d;

@@ -45,6 +45,7 @@ struct ResidualParams {
   float* part;      // [kinds][workers][d]
   int32_t kind_pre, kind_post, kind_gate;  // where a kind's partial rows are, -1 without
   int32_t stages, pitch;  // rows of an array in shared memory, bytes from one to the next
+  int32_t sink, factors;  // where the warps' buffers for results, and the columns' factors, begin there
 };
 
 // KE elements of a weight of any type, as fp32.
@@ -172,27 +173,28 @@ struct RowGroup {
 // The slots lie 256 bytes apart in 512 aligned bytes.
 constexpr int kRsRedFloats = 64 + RowGroup<false>::kSlot;
 
-// Rows on their way through shared memory, `arrays` of them to a stage.
-// KE > 1: rows of whole 16-byte vectors.  A thread copies the vectors that it will read, so a wait for its own copies is
-// all that a stage needs.
-// KE == 1: rows at any alignment.  The aligned 16-byte blocks that hold a row are copied as they are, whoever reads them,
-// and a barrier follows the wait; elements are then read one at a time, neighbouring ones by neighbouring threads.
+// Rows on their way through shared memory, `arrays` of them to a stage, in units of KE elements (16 bytes).
+// LEVEL: all rows start on 16-byte boundaries and have whole units.  A thread copies the units that it will read, so a wait
+// for its own copies is all that a stage needs.
+// Otherwise the aligned 16-byte blocks that hold a row are copied as they are, whoever reads them, and a barrier follows
+// the wait.  A unit is then two blocks shifted in registers, its elements behind the row's end taken as 0.
 // kDirect: fp32 rows above 8192 elements, five of which shared memory has no room for, are read where they are.
 extern __shared__ __align__(16) unsigned char rs_ring[];
 
-template <typename T, int KE, int K>
+template <typename T, int KE, int K, bool LEVEL>
 struct RowFeed {
   static constexpr bool kDirect = sizeof(T) == 4 && KE * K == 32;
-  const T* next[5];        // the row that is fetched next, at this thread's first element (KE > 1) or its beginning
-  const T* here[5];        // KE == 1: the row that is read
+  const T* next[5];        // the row that is fetched next, at this thread's first unit (LEVEL) or its beginning
+  const T* here[5];        // not LEVEL: the row that is read
   int64_t hop[5];          // elements from one of the group's rows to the next
   uint32_t offset, pitch;  // of this row group's part of the ring, of a row
-  int arrays, units, t, nt;
+  int arrays, units, d, t, nt;
   int64_t left;            // rows that are still to be fetched
   template <bool WARP>
   __device__ __forceinline__ void init(const ResidualParams& p, int arrays_, const RowGroup<WARP>& g) {
     arrays = arrays_;
-    units = p.d / KE;
+    d = p.d;
+    units = (p.d + KE - 1) / KE;
     pitch = (uint32_t)p.pitch;
     offset = WARP ? (uint32_t)(threadIdx.x >> 5) * (uint32_t)(p.stages * arrays) * pitch : 0u;
     t = g.t;
@@ -201,8 +203,8 @@ struct RowFeed {
   }
   template <bool WARP>
   __device__ __forceinline__ void array(int a, const void* base, int64_t ld, const RowGroup<WARP>& g) {
-    next[a] = static_cast<const T*>(base) + g.first * ld + (KE > 1 ? t * KE : 0);
-    here[a] = next[a];
+    here[a] = static_cast<const T*>(base) + g.first * ld;
+    next[a] = here[a] + (LEVEL ? t * KE : 0);
     hop[a] = g.step * ld;
   }
   // Starts the copies of the next row into a stage; one group of copies whether there is a row or not.
@@ -214,13 +216,13 @@ struct RowFeed {
       for (int a = 0; a < 5; ++a)
         if (a < arrays) {
           const uint32_t dst = smem_u32(rs_ring) + offset + (uint32_t)(stage * arrays + a) * pitch + (uint32_t)t * 16u;
-          if constexpr (KE > 1) {
+          if constexpr (LEVEL) {
 #pragma unroll
             for (int k = 0; k < K; ++k)
               if (t + k * nt < units) copy_async_16(dst + (uint32_t)(k * nt) * 16u, next[a] + k * nt * KE);
           } else {
             const uintptr_t from = reinterpret_cast<uintptr_t>(next[a]) & ~(uintptr_t)15;
-            const int blocks = (int)((reinterpret_cast<uintptr_t>(next[a] + units) - from + 15) >> 4);
+            const int blocks = (int)((reinterpret_cast<uintptr_t>(next[a] + d) - from + 15) >> 4);
             for (int u = t; u < blocks; u += nt)
               copy_async_16(dst + (uint32_t)(u - t) * 16u, reinterpret_cast<const void*>(from + (uintptr_t)u * 16));
           }
@@ -234,7 +236,7 @@ struct RowFeed {
   template <bool WARP>
   __device__ __forceinline__ void turn(int stage, int ahead, const RowGroup<WARP>& g) {
     if constexpr (kDirect) {
-    } else if constexpr (KE > 1) {
+    } else if constexpr (LEVEL) {
       fetch(stage == 0 ? ahead : stage - 1);
       copy_async_wait(ahead);
     } else if (ahead) {
@@ -248,30 +250,84 @@ struct RowFeed {
       g.sync();
     }
   }
-  // This thread's first element of an array's row of a stage.
-  __device__ __forceinline__ const unsigned char* place(int a, int stage) const {
-    const unsigned char* p = nullptr;
-    if constexpr (KE == 1) {
+  // An array's row of a stage: this thread's first unit, and how far the row is off its first block.
+  struct Place {
+    const uint4* p;
+    uint32_t off;
+  };
+  __device__ __forceinline__ Place place(int a, int stage) const {
+    Place r;
+    const T* row = nullptr;
 #pragma unroll
-      for (int i = 0; i < 5; ++i)
-        if (i == a) p = reinterpret_cast<const unsigned char*>(here[i]);
-      if constexpr (kDirect) return p + t * sizeof(T);
-      return rs_ring + offset + (uint32_t)(stage * arrays + a) * pitch + (reinterpret_cast<uintptr_t>(p) & 15) + t * sizeof(T);
-    }
-    return rs_ring + offset + (uint32_t)(stage * arrays + a) * pitch + (uint32_t)t * 16u;
+    for (int i = 0; i < 5; ++i)
+      if (i == a) row = here[i];
+    r.off = LEVEL ? 0u : (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u;
+    if constexpr (kDirect)
+      r.p = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15) + t;
+    else
+      r.p = reinterpret_cast<const uint4*>(rs_ring + offset + (uint32_t)(stage * arrays + a) * pitch) + t;
+    return r;
   }
   __device__ __forceinline__ void advance() {
-    if constexpr (KE == 1) {
+    if constexpr (!LEVEL) {
 #pragma unroll
       for (int a = 0; a < 5; ++a)
         if (a < arrays) here[a] += hop[a];
     }
   }
-  __device__ __forceinline__ void read(const unsigned char* place, int k, float (&f)[KE]) const {
-    if constexpr (KE > 1) {
-      Elem<T>::widen(reinterpret_cast<const uint4*>(place)[k * nt], f);
+  __device__ __forceinline__ void read(const Place& q, int k, float (&f)[KE]) const {
+    if constexpr (LEVEL) {
+      Elem<T>::widen(q.p[k * nt], f);
     } else {
-      f[0] = Elem<T>::one(place, k * nt);
+      const int have = d - (t + k * nt) * KE;  // elements from here to the row's end, at least one
+      const uint4 lo = q.p[k * nt];
+      uint4 hi = lo;
+      if constexpr (kDirect) {  // memory behind the row's last block may be nobody's
+        if (q.off + (uint32_t)(have < KE ? have : KE) * (uint32_t)sizeof(T) > 16u) hi = q.p[k * nt + 1];
+      } else {
+        hi = q.p[k * nt + 1];
+      }
+      Elem<T>::widen(shift_16(lo, hi, q.off), f);
+      if (have < KE) {
+#pragma unroll
+        for (int i = 0; i < KE; ++i)
+          if (i >= have) f[i] = 0.f;
+      }
+    }
+  }
+};
+
+// Writes unit k of every thread of a warp to a row.  LEVEL: where it belongs.  Otherwise through the warp's buffer in
+// shared memory, from which the row's aligned 16-byte blocks leave whole, and up to 15 bytes before and behind them an
+// element a lane.
+template <typename T, int KE, bool LEVEL>
+struct RowSink {
+  uint4* buf;  // of this warp: 32 units, one more that is read but not used, two of these in turn
+  int d, t, nt, turn;
+  __device__ __forceinline__ RowSink(unsigned char* mem, int d_, int t_, int nt_) : d(d_), t(t_), nt(nt_), turn(0) {
+    buf = reinterpret_cast<uint4*>(mem) + (threadIdx.x >> 5) * 66;
+  }
+  // For all lanes of the warp.  row: the row's first element.
+  __device__ __forceinline__ void put(T* row, int k, const float (&o)[KE]) {
+    if constexpr (LEVEL) {
+      if (t + k * nt < d / KE) Raw<T, KE>::store(row + (t + k * nt) * KE, o);
+    } else {
+      const int lane = threadIdx.x & 31, first = (t - lane + k * nt) * KE;  // the warp's first element
+      int n = d - first;
+      if (n <= 0) return;
+      n = n < 32 * KE ? n : 32 * KE;
+      uint4* b = buf + turn * 33;
+      turn ^= 1;
+      b[lane] = Elem<T>::narrow(o);
+      __syncwarp();
+      T* to = row + first;
+      int head = (int)(-(reinterpret_cast<uintptr_t>(to) / sizeof(T)) & (KE - 1));
+      head = head < n ? head : n;
+      const int blocks = (n - head) / KE;
+      if (lane < blocks)
+        reinterpret_cast<uint4*>(to + head)[lane] = shift_16(b[lane], b[lane + 1], (uint32_t)head * (uint32_t)sizeof(T));
+      const int e = lane < KE ? lane : head + blocks * KE + lane - KE;
+      if (lane < 2 * KE && e < (lane < KE ? head : n)) to[e] = reinterpret_cast<const T*>(b)[e];
     }
   }
 };
@@ -344,23 +400,51 @@ __device__ __forceinline__ void v_set(float (&o)[KE], float v) {
   for (int i = 0; i < KE; ++i) o[i] = v;
 }
 
-// Weights of a thread's columns, kept in registers over its rows, or (KEEP false: rows so wide that the registers are
-// needed elsewhere) formed again for each.
-template <int KE, int K, bool KEEP>
+// Factors of a thread's columns over its rows: kept in registers; or, where shifting needs those, as fp32 in shared memory,
+// each thread's own; or, for rows so wide that there is no room either, formed again for each row.
+enum { kFactorRegisters = 0, kFactorShared = 1, kFactorFormed = 2 };
+__host__ __device__ constexpr int residual_factors(int elems, bool level) {
+  return elems == 32 ? kFactorFormed : level ? kFactorRegisters : kFactorShared;
+}
+template <int KE, int K, int WHERE>
 struct ColumnFactor {
-  float w[KEEP ? K : 1][KE];
+  float w[WHERE == kFactorRegisters ? K : 1][KE];
+  float4* mem;  // [K * KE / 4][nt]
+  int t, nt;
   template <typename F>
-  __device__ __forceinline__ void init(int t, int nt, int units, F form) {
-    if constexpr (KEEP) {
+  __device__ __forceinline__ void init(unsigned char* at, int t_, int nt_, int units, bool mine, F form) {
+    mem = reinterpret_cast<float4*>(at);
+    t = t_;
+    nt = nt_;
+    if constexpr (WHERE == kFactorRegisters) {
 #pragma unroll
       for (int k = 0; k < K; ++k)
         if (t + k * nt < units) form(t + k * nt, w[k]);
+    } else if constexpr (WHERE == kFactorShared) {
+      if (mine)
+        for (int k = 0; k < K; ++k) {
+          if (t + k * nt >= units) break;
+          form(t + k * nt, w[0]);
+#pragma unroll
+          for (int i = 0; i < KE / 4; ++i)
+            mem[(k * (KE / 4) + i) * nt + t] = make_float4(w[0][4 * i], w[0][4 * i + 1], w[0][4 * i + 2], w[0][4 * i + 3]);
+        }
     }
   }
   template <typename F>
   __device__ __forceinline__ const float (&get(int k, int u, F form))[KE] {
-    if constexpr (KEEP) {
+    if constexpr (WHERE == kFactorRegisters) {
       return w[k];
+    } else if constexpr (WHERE == kFactorShared) {
+#pragma unroll
+      for (int i = 0; i < KE / 4; ++i) {
+        const float4 q = mem[(k * (KE / 4) + i) * nt + t];
+        w[0][4 * i] = q.x;
+        w[0][4 * i + 1] = q.y;
+        w[0][4 * i + 2] = q.z;
+        w[0][4 * i + 3] = q.w;
+      }
+      return w[0];
     } else {
       form(u, w[0]);
       return w[0];
@@ -387,31 +471,42 @@ struct ResidualHas {
   }
 };
 
+// KE elements of a weight, 0 behind the row's end; LEVEL: there are whole vectors, on 16-byte boundaries.
+template <int KE, bool LEVEL>
+__device__ __forceinline__ void row_weight(const void* w, int type, int d, int c, float offset, float (&f)[KE]) {
+  if constexpr (LEVEL) {
+    load_weight<KE>(w, type, c, offset, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < KE; ++i) f[i] = c + i < d ? load_one(w, type, c + i) + offset : 0.f;
+  }
+}
+
 // A column's factors: of h, and of y (b w_post, and a channel's gate).
-template <int KE>
+template <int KE, bool LEVEL>
 __device__ __forceinline__ void form_pre(const ResidualParams& p, bool pre, int c, float (&w)[KE]) {
-  if (pre) load_weight<KE>(p.w_pre, p.weight_type, c, p.weight_offset, w);
+  if (pre) row_weight<KE, LEVEL>(p.w_pre, p.weight_type, p.d, c, p.weight_offset, w);
   else v_set(w, 0.f);
 }
-template <int KE>
+template <int KE, bool LEVEL>
 __device__ __forceinline__ void form_y(const ResidualParams& p, bool post, int c, float (&w)[KE]) {
-  if (post) load_weight<KE>(p.w_post, p.weight_type, c, p.weight_offset, w);
+  if (post) row_weight<KE, LEVEL>(p.w_post, p.weight_type, p.d, c, p.weight_offset, w);
   else v_set(w, 1.f);
   v_mul(w, w, p.b);
   if (p.gate_kind == kGateColumn) {
     float g[KE];
-    load_weight<KE>(p.gate, p.gate_type, c, 0.f, g);
+    row_weight<KE, LEVEL>(p.gate, p.gate_type, p.d, c, 0.f, g);
     v_mul(w, w, g);
   }
 }
 
 // ------------------------------------------------------------------------------------------------ forward
-template <typename T, int KE, int K, bool WARP, int NT, bool COMMON>
+template <typename T, int KE, int K, bool WARP, int NT, bool LEVEL, bool COMMON>
 __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_fwd_kernel(ResidualParams p) {
   __shared__ __align__(512) float red[kRsRedFloats];
   RowGroup<WARP> grp(red);
   const ResidualHas<COMMON> has(p);
-  RowFeed<T, KE, K> feed;
+  RowFeed<T, KE, K, LEVEL> feed;
   feed.init(p, 1 + has.y + has.full, grp);
   feed.array(0, p.x, p.ld_x, grp);
   feed.array(1, p.y, p.ld_y, grp);
@@ -420,21 +515,25 @@ __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_
   feed.array(4, nullptr, 0, grp);
   const int t = grp.t, nt = grp.nt, units = feed.units, ahead = p.stages - 1;
   for (int s = 0; s < ahead; ++s) feed.fetch(s);
-  constexpr bool kKeep = KE * K <= 16;
-  ColumnFactor<KE, K, kKeep> f_pre, f_y;
-  auto make_pre = [&](int u, float (&w)[KE]) { form_pre<KE>(p, has.pre, u * KE, w); };
-  auto make_y = [&](int u, float (&w)[KE]) { form_y<KE>(p, has.post, u * KE, w); };
-  f_pre.init(t, nt, units, make_pre);
-  f_y.init(t, nt, units, make_y);
+  constexpr int kWhere = residual_factors(KE * K, LEVEL);
+  ColumnFactor<KE, K, kWhere> f_pre, f_y;
+  auto make_pre = [&](int u, float (&w)[KE]) { form_pre<KE, LEVEL>(p, has.pre, u * KE, w); };
+  auto make_y = [&](int u, float (&w)[KE]) { form_y<KE, LEVEL>(p, has.post, u * KE, w); };
+  const bool mine = !WARP || threadIdx.x < 32;  // a warp's rows have the same columns as the next warp's
+  unsigned char* factors = rs_ring + p.factors;
+  f_pre.init(factors, t, nt, units, mine, make_pre);
+  f_y.init(factors + K * KE * 4 * nt, t, nt, units, mine, make_y);
+  if (WARP && kWhere == kFactorShared) __syncthreads();
   const float inv_d = 1.f / (float)p.d;
-  T* x_out = static_cast<T*>(p.x_out) + grp.first * p.ld_xo + t * KE;
-  T* h = static_cast<T*>(p.h) + grp.first * p.ld_h + t * KE;
+  T* x_out = static_cast<T*>(p.x_out) + grp.first * p.ld_xo;
+  T* h = static_cast<T*>(p.h) + grp.first * p.ld_h;
+  RowSink<T, KE, LEVEL> sink(rs_ring + p.sink, p.d, t, nt);
   int stage = 0;
   for (int64_t row = grp.first; row < p.N; row += grp.step) {
     float g_row = 1.f;
     if (p.gate_kind == kGateRow) g_row = load_one(p.gate, p.gate_type, row * p.ld_gate);
     feed.turn(stage, ahead, grp);
-    const unsigned char *at_x = feed.place(0, stage), *at_y = feed.place(1, stage), *at_g = feed.place(2, stage);
+    const auto at_x = feed.place(0, stage), at_y = feed.place(1, stage), at_g = feed.place(2, stage);
     float v[K][KE];
     float2 ss = make_float2(0.f, 0.f);
     if (has.y) {
@@ -470,8 +569,8 @@ __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_
           v_mul(v[k], x, p.a);
         }
         v_dot(ss, v[k], v[k]);
-        if (COMMON || p.x_out) Raw<T, KE>::store(x_out + k * nt * KE, v[k]);
       }
+      if (COMMON || p.x_out) sink.put(x_out, k, v[k]);
     }
     if (has.pre) {
       const float r = 1.f / sqrtf(fmaf(grp.sum(ss.x + ss.y), inv_d, p.eps));
@@ -482,8 +581,8 @@ __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_
         if (u < units) {
           v_mul(v[k], v[k], r);
           v_mul(v[k], v[k], f_pre.get(k, u, make_pre));
-          Raw<T, KE>::store(h + k * nt * KE, v[k]);
         }
+        sink.put(h, k, v[k]);
       }
     }
     x_out += grp.step * p.ld_xo;
@@ -496,14 +595,14 @@ __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_
 // ------------------------------------------------------------------------------------------------ gradient
 // Of a column only two sums are needed: dw_pre, and S = sum_n t yh (times a row's or an element's gate).  Without these
 // gates dw_post = b g S and dg = b w_post S, both per channel; with them dw_post = b S.
-template <typename T, int KE, int K, bool WARP, int NT, bool COMMON>
+template <typename T, int KE, int K, bool WARP, int NT, bool LEVEL, bool COMMON>
 __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual_bwd_kernel(ResidualParams p) {
   __shared__ __align__(512) float red[kRsRedFloats];
   RowGroup<WARP> grp(red);
   const ResidualHas<COMMON> has(p);
   // the arrays of a stage, in this order, those that there are
   const int i_dx = has.pre ? 2 : 0, i_y = i_dx + has.dx_out, i_g = i_y + has.y;
-  RowFeed<T, KE, K> feed;
+  RowFeed<T, KE, K, LEVEL> feed;
   feed.init(p, i_g + has.full, grp);
 #pragma unroll
   for (int a = 0; a < 5; ++a) {
@@ -518,16 +617,20 @@ __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual
   }
   const int t = grp.t, nt = grp.nt, units = feed.units, ahead = p.stages - 1;
   for (int s = 0; s < ahead; ++s) feed.fetch(s);
-  constexpr bool kKeep = KE * K <= 16;
-  ColumnFactor<KE, K, kKeep> f_pre, f_y;
-  auto make_pre = [&](int u, float (&w)[KE]) { form_pre<KE>(p, has.pre, u * KE, w); };
-  auto make_y = [&](int u, float (&w)[KE]) { form_y<KE>(p, has.post, u * KE, w); };
-  f_pre.init(t, nt, units, make_pre);
-  f_y.init(t, nt, units, make_y);
+  constexpr int kWhere = residual_factors(KE * K, LEVEL);
+  ColumnFactor<KE, K, kWhere> f_pre, f_y;
+  auto make_pre = [&](int u, float (&w)[KE]) { form_pre<KE, LEVEL>(p, has.pre, u * KE, w); };
+  auto make_y = [&](int u, float (&w)[KE]) { form_y<KE, LEVEL>(p, has.post, u * KE, w); };
+  const bool mine = !WARP || threadIdx.x < 32;  // a warp's rows have the same columns as the next warp's
+  unsigned char* factors = rs_ring + p.factors;
+  f_pre.init(factors, t, nt, units, mine, make_pre);
+  f_y.init(factors + K * KE * 4 * nt, t, nt, units, mine, make_y);
+  if (WARP && kWhere == kFactorShared) __syncthreads();
   const float inv_d = 1.f / (float)p.d;
   const bool second = has.y && (has.post || p.gate_kind == kGateRow);
-  T* dx = static_cast<T*>(p.dx) + grp.first * p.ld_dx + t * KE;
-  T* dy = static_cast<T*>(p.dy) + grp.first * p.ld_dy + t * KE;
+  T* dx = static_cast<T*>(p.dx) + grp.first * p.ld_dx;
+  T* dy = static_cast<T*>(p.dy) + grp.first * p.ld_dy;
+  RowSink<T, KE, LEVEL> sink(rs_ring + p.sink, p.d, t, nt);
   float a_pre[K][KE], a_y[K][KE];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
@@ -539,8 +642,8 @@ __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual
     const float r_x = has.pre ? p.rstd_pre[row] : 0.f, r_y = has.post ? p.rstd_post[row] : 1.f;
     const float g_row = p.gate_kind == kGateRow ? load_one(p.gate, p.gate_type, row * p.ld_gate) : 1.f;
     feed.turn(stage, ahead, grp);
-    const unsigned char *at_xo = feed.place(0, stage), *at_dh = feed.place(1, stage), *at_dx = feed.place(i_dx, stage),
-                        *at_y = feed.place(i_y, stage), *at_g = feed.place(i_g, stage);
+    const auto at_xo = feed.place(0, stage), at_dh = feed.place(1, stage), at_dx = feed.place(i_dx, stage),
+               at_y = feed.place(i_y, stage), at_g = feed.place(i_g, stage);
     // c = dx' + r_x w_pre dh, and the sums of (w_pre dh) xh, A c and A xh
     float c[K][KE];
     float2 s0 = make_float2(0.f, 0.f), s1 = s0, s2 = s0;
@@ -587,28 +690,26 @@ __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int u = t + k * nt;
+      float o_dx[KE], o_dg[KE], o[KE];
       if (u < units) {
         if (has.pre) {
           float xo[KE];
           feed.read(at_xo, k, xo);
           v_fma(c[k], xo, m1x, c[k]);
         }
-        float y[KE], g[KE], o[KE];
-        if (has.y) feed.read(at_y, k, y);
-        if (has.full) feed.read(at_g, k, g);
-        if (COMMON || p.dx) {
-          v_mul(o, c[k], p.a);
-          Raw<T, KE>::store(dx + k * nt * KE, o);
-        }
+        v_mul(o_dx, c[k], p.a);
+        if (LEVEL && (COMMON || p.dx)) sink.put(dx, k, o_dx);
         if (has.y) {
+          float y[KE];
+          feed.read(at_y, k, y);
           v_mul(o, c[k], f_y.get(k, u, make_y));  // b w_post g t
           if (has.full) {
-            float e[KE];
+            float g[KE], e[KE];
+            feed.read(at_g, k, g);
             v_mul(c[k], c[k], g);
             v_mul(e, y, r_y);
             v_fma(a_y[k], c[k], e, a_y[k]);
-            v_mul(e, e, o);
-            if (p.dgate) Raw<T, KE>::store(static_cast<T*>(p.dgate) + row * p.ld_dg + u * KE, e);
+            v_mul(o_dg, e, o);
             v_mul(o, o, g);
           } else {
             v_mul(c[k], c[k], e_row);
@@ -616,9 +717,12 @@ __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual
           }
           v_mul(o, o, e_row);
           if (has.post) v_fma(o, y, m2y, o);
-          if (COMMON || p.dy) Raw<T, KE>::store(dy + k * nt * KE, o);
+          if (LEVEL && (COMMON || p.dy)) sink.put(dy, k, o);
         }
       }
+      if (!LEVEL && (COMMON || p.dx)) sink.put(dx, k, o_dx);
+      if (!LEVEL && (COMMON || p.dy)) sink.put(dy, k, o);
+      if (has.full && p.dgate) sink.put(static_cast<T*>(p.dgate) + row * p.ld_dg, k, o_dg);
     }
     dx += grp.step * p.ld_dx;
     dy += grp.step * p.ld_dy;
@@ -629,25 +733,33 @@ __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual
   const int64_t kind = grp.step * p.d;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const int u = t + k * nt;
-    if (u < units) {
-      float* to = p.part + grp.first * p.d + u * KE;
-      if (p.kind_pre >= 0) Raw<float, KE>::store(to + p.kind_pre * kind, a_pre[k]);
-      float w[KE], g[KE];
+    const int c = (t + k * nt) * KE;
+    if (c >= p.d) continue;
+    float* to = p.part + grp.first * p.d + c;
+    auto put = [&](float* q, const float(&f)[KE]) {
+      if constexpr (LEVEL) {
+        Raw<float, KE>::store(q, f);
+      } else {
 #pragma unroll
-      for (int i = 0; i < KE; ++i) w[i] = g[i] = 1.f;
-      if (p.kind_post >= 0) {
-        if (p.gate_kind == kGateColumn) load_weight<KE>(p.gate, p.gate_type, u * KE, 0.f, g);
-#pragma unroll
-        for (int i = 0; i < KE; ++i) g[i] *= p.b * a_y[k][i];
-        Raw<float, KE>::store(to + p.kind_post * kind, g);
+        for (int i = 0; i < KE; ++i)
+          if (c + i < p.d) q[i] = f[i];
       }
-      if (p.kind_gate >= 0) {
-        if (has.post) load_weight<KE>(p.w_post, p.weight_type, u * KE, p.weight_offset, w);
-#pragma unroll
-        for (int i = 0; i < KE; ++i) w[i] *= p.b * a_y[k][i];
-        Raw<float, KE>::store(to + p.kind_gate * kind, w);
-      }
+    };
+    if (p.kind_pre >= 0) put(to + p.kind_pre * kind, a_pre[k]);
+    float w[KE];
+    if (p.kind_post >= 0) {
+      v_set(w, 1.f);
+      if (p.gate_kind == kGateColumn) row_weight<KE, LEVEL>(p.gate, p.gate_type, p.d, c, 0.f, w);
+      v_mul(w, w, p.b);
+      v_mul(w, w, a_y[k]);
+      put(to + p.kind_post * kind, w);
+    }
+    if (p.kind_gate >= 0) {
+      v_set(w, 1.f);
+      if (has.post) row_weight<KE, LEVEL>(p.w_post, p.weight_type, p.d, c, p.weight_offset, w);
+      v_mul(w, w, p.b);
+      v_mul(w, w, a_y[k]);
+      put(to + p.kind_gate * kind, w);
     }
   }
 }

@@ -54,9 +54,8 @@ static int launch_embedding(const LookupParams& p, int n_sm, cudaStream_t st) {
 
 template <typename TI, typename TO>
 static int route_embedding(const LookupParams& p, int n_sm, cudaStream_t st) {
-  constexpr int KE = Elem<TI>::kN > Elem<TO>::kN ? Elem<TI>::kN : Elem<TO>::kN;
-  const bool vec = on16(p.in) && on16(p.out) && p.d % KE == 0 && p.ld_in * sizeof(TI) % 16 == 0 &&
-                   p.ld_out * sizeof(TO) % 16 == 0;
+  constexpr int KE = Elem<TI>::kN < Elem<TO>::kN ? Elem<TI>::kN : Elem<TO>::kN;  // 16 bytes of the wider type
+  const bool vec = on16(p.in) && on16(p.out) && p.d % KE == 0 && p.ld_in % KE == 0 && p.ld_out % KE == 0;
   return vec ? launch_embedding<TI, TO, KE, true>(p, n_sm, st) : launch_embedding<TI, TO, KE, false>(p, n_sm, st);
 }
 
@@ -245,7 +244,7 @@ static int launch_adjust(AdjustParams p, cudaStream_t st) {
   if (slices * p.N > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
   p.slices = (int32_t)slices;
   auto kern = adjust_kernel<T, KE, VPT, GRAD, OVER>;
-  const int smem = p.history || p.biased ? AdjustShared::bytes((int)kSlice) : 0;
+  const int smem = p.history || p.biased ? AdjustShared<!GRAD || OVER>::bytes((int)kSlice) : 0;
   if (smem > 40 * 1024) {
     static bool done[kMaxDevices] = {false};
     int dev = -1;
@@ -263,9 +262,10 @@ static int launch_adjust(AdjustParams p, cudaStream_t st) {
 
 template <typename T, int KE, bool GRAD, bool OVER>
 static int route_adjust_size(const AdjustParams& p, int n_sm, cudaStream_t st) {
-  // slices of 8192 tokens (4096 an element at a time) where they give every SM four, of 2048 otherwise
-  constexpr int kMany = 32 / KE / (KE == 1 ? 2 : 1), kFew = 8 / KE;
-  const int64_t many = (int64_t)p.N * p.V / 8192;
+  // slices of 8192 tokens where they give every SM four, of 2048 otherwise; the gradient, which counts nothing and has
+  // room, 16384, and 4096 where it goes an element at a time
+  constexpr int kMany = (KE == 1 ? 16 : GRAD && !OVER ? 64 : 32) / KE, kFew = 8 / KE;
+  const int64_t many = (int64_t)p.N * p.V / (kMany * KE * kAdThreads);
   return many >= 4 * (int64_t)n_sm ? launch_adjust<T, KE, kMany, GRAD, OVER>(p, st)
                                    : launch_adjust<T, KE, kFew, GRAD, OVER>(p, st);
 }
@@ -275,15 +275,16 @@ static int route_adjust(const AdjustParams& p, bool grad, cudaStream_t st) {
   const int n_sm = sm_count();
   if (n_sm <= 0) return OAPL_ERR_CUDA;
   constexpr int KE = Elem<T>::kN;
-  const bool over = !grad && p.out == p.z;
   // whether a row of b is as far off 16-byte boundaries as the result's
   auto level = [&](const void* b, int64_t ld) {
     return (((uintptr_t)b - (uintptr_t)p.out) & 15) == 0 && (p.N == 1 || (ld - p.ld_o) * (int64_t)sizeof(T) % 16 == 0);
   };
   const bool vec = level(grad ? p.d : p.z, grad ? p.ld_d : p.ld_z);
+  if (grad && p.out == p.z)
+    return vec ? route_adjust_size<T, KE, true, true>(p, n_sm, st) : route_adjust_size<T, 1, true, true>(p, n_sm, st);
   if (grad)
     return vec ? route_adjust_size<T, KE, true, false>(p, n_sm, st) : route_adjust_size<T, 1, true, false>(p, n_sm, st);
-  if (over)
+  if (p.out == p.z)
     return vec ? route_adjust_size<T, KE, false, true>(p, n_sm, st) : route_adjust_size<T, 1, false, true>(p, n_sm, st);
   return vec ? route_adjust_size<T, KE, false, false>(p, n_sm, st) : route_adjust_size<T, 1, false, false>(p, n_sm, st);
 }
