@@ -7,7 +7,7 @@
 //
 // The gradient adds rows in the order of their positions, without atomics on sums, so it is the same in every run:
 //   1. the positions are sorted by token (stable): up to kEbCountMax of them by counting, for each, the keys before it;
-//      more by a radix sort of two or three passes, each a histogram per tile, prefix sums per digit and a move;
+//      more by a radix sort of one to four passes, each a move of a tile's positions that also counts the next digits;
 //   2. the sorted list is cut into chunks.  A CTA adds up a chunk's rows; a run of equal tokens that lies within the
 //      chunk goes straight to the table, the two that may reach over the chunk's ends leave partial sums;
 //   3. the CTA of the chunk where a run begins that reaches further adds up its partial sums.
@@ -45,6 +45,7 @@ struct LookupParams {
   float* part;     // [chunks][2][d]: sums of a chunk's first run, when it came from before, and of its last one
   int32_t chunk, chunks, slabs;
   int32_t accumulate;
+  uint32_t* joins; // chunks whose last run reaches further: how many, then which
 };
 
 // The token of position n, V where it does not count.  Both loads are in flight together.
@@ -143,10 +144,11 @@ __global__ void __launch_bounds__(kEbThreads) embedding_kernel(LookupParams p) {
 // ------------------------------------------------------------------------------------------------ sorting
 // A warp ranks kEbCountRows positions: the CTA brings all keys into shared memory, lanes share them out and compare each
 // with the warp's positions.  Of equal keys the earlier position comes first.
-constexpr int kEbCountRows = 8;
+constexpr int kEbCountRows = 4;
 __global__ void __launch_bounds__(kEbThreads) embedding_count_sort_kernel(LookupParams p) {
   __shared__ uint32_t keys[kEbCountMax];
   const int N = (int)p.N, lane = threadIdx.x & 31;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.joins = 0;
 #pragma unroll 8
   for (int m = threadIdx.x; m < N; m += kEbThreads) keys[m] = lookup_key(p, m);
   __syncthreads();
@@ -160,8 +162,9 @@ __global__ void __launch_bounds__(kEbThreads) embedding_count_sort_kernel(Lookup
     rank[r] = 0;
   }
   if (lane < kEbCountRows && n0 + lane < N) lookup_check(p, n0 + lane);
-  // n0 is a multiple of 8 and the positions of a step are 32: before them all, at them, or behind them all
+  // n0 is a multiple of 4 and the positions of a step are 32: before them all, at them, or behind them all
   int m0 = 0;
+#pragma unroll 4
   for (; m0 + 32 <= n0; m0 += 32) {
     const uint32_t k = keys[m0 + lane];
 #pragma unroll
@@ -173,6 +176,7 @@ __global__ void __launch_bounds__(kEbThreads) embedding_count_sort_kernel(Lookup
 #pragma unroll
     for (int r = 0; r < kEbCountRows; ++r) rank[r] += k < key[r] || (k == key[r] && m < n0 + r);
   }
+#pragma unroll 4
   for (; m0 < N; m0 += 32) {
     const uint32_t k = m0 + lane < N ? keys[m0 + lane] : 0xFFFFFFFFu;
 #pragma unroll
@@ -188,75 +192,115 @@ __global__ void __launch_bounds__(kEbThreads) embedding_count_sort_kernel(Lookup
 struct RadixParams {
   const uint2* in;   // nullptr: the first pass, keys from the ids
   uint2* out;
-  uint32_t* hist;    // [bins][tiles], then its prefix sums within a bin
-  uint32_t* total;   // [bins]
-  int32_t shift, bits, tiles;
+  uint32_t* hist;    // [tiles][bins] of this pass; with `scanned`, prefix sums over the tiles
+  uint32_t* next;    // [tiles][bins] of the next pass, nullptr: the last one
+  uint32_t* total;   // [bins], with `scanned`
+  uint32_t* clear;   // the first pass: words that the others count in
+  int64_t clear_words;
+  int32_t shift, bits, tiles, scanned;
 };
 
 __device__ __forceinline__ uint2 radix_load(const LookupParams& p, const RadixParams& r, int64_t n) {
   return r.in ? r.in[n] : make_uint2(lookup_key(p, n), (uint32_t)n);
 }
 
-__global__ void __launch_bounds__(kEbThreads) embedding_radix_hist_kernel(LookupParams p, RadixParams r) {
+// The digits of the first pass, counted by tile.
+__global__ void __launch_bounds__(kEbThreads) embedding_radix_count_kernel(LookupParams p, RadixParams r) {
   __shared__ uint32_t h[1 << kEbMaxBits];
   const int bins = 1 << r.bits;
-  for (int i = threadIdx.x; i < bins; i += kEbThreads) h[i] = 0;
-  __syncthreads();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.joins = 0;
   const int64_t n0 = (int64_t)blockIdx.x * kEbTile + threadIdx.x;
   uint32_t key[kEbTile / kEbThreads];
 #pragma unroll
   for (int i = 0; i < kEbTile / kEbThreads; ++i) {
     const int64_t n = n0 + i * kEbThreads;
-    key[i] = n < p.N ? radix_load(p, r, n).x : 0u;
+    key[i] = n < p.N ? lookup_key(p, n) : 0u;
   }
+  for (int i = threadIdx.x; i < bins; i += kEbThreads) h[i] = 0;
+  for (int64_t i = (int64_t)blockIdx.x * kEbThreads + threadIdx.x; i < r.clear_words; i += (int64_t)gridDim.x * kEbThreads)
+    r.clear[i] = 0;
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < kEbTile / kEbThreads; ++i)
     if (n0 + i * kEbThreads < p.N) {
-      atomicAdd(&h[(key[i] >> r.shift) & (bins - 1)], 1u);
-      if (!r.in && key[i] == (uint32_t)p.V) lookup_check(p, n0 + i * kEbThreads);
+      atomicAdd(&h[key[i] & (bins - 1)], 1u);
+      if (key[i] == (uint32_t)p.V) lookup_check(p, n0 + i * kEbThreads);
     }
   __syncthreads();
-  for (int i = threadIdx.x; i < bins; i += kEbThreads) r.hist[(int64_t)i * r.tiles + blockIdx.x] = h[i];
+  for (int i = threadIdx.x; i < bins; i += kEbThreads) r.hist[(int64_t)blockIdx.x * bins + i] = h[i];
 }
 
-// A warp: exclusive prefix sums of one digit over the tiles.
-__global__ void __launch_bounds__(kEbThreads) embedding_radix_scan_kernel(RadixParams r) {
-  const int bin = (int)blockIdx.x * (kEbThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (bin >= (1 << r.bits)) return;
-  uint32_t* h = r.hist + (int64_t)bin * r.tiles;
-  uint32_t run = 0;
-  for (int t0 = 0; t0 < r.tiles; t0 += 32) {
-    const uint32_t v = t0 + lane < r.tiles ? h[t0 + lane] : 0u;
-    uint32_t s = v;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t u = __shfl_up_sync(0xffffffffu, s, o);
-      if (lane >= o) s += u;
-    }
-    if (t0 + lane < r.tiles) h[t0 + lane] = run + s - v;
-    run += __shfl_sync(0xffffffffu, s, 31);
+// Many tiles: exclusive prefix sums of 32 digits over the tiles, 32 threads to a digit.
+__global__ void __launch_bounds__(1024) embedding_radix_scan_kernel(RadixParams r) {
+  __shared__ uint32_t sh[32][33];
+  const int bins = 1 << r.bits, bin = (int)blockIdx.x * 32 + (int)threadIdx.x, g = threadIdx.y;
+  const int per = (r.tiles + 31) / 32, t0 = g * per, t1 = t0 + per < r.tiles ? t0 + per : r.tiles;
+  uint32_t* h = r.hist + bin;
+  uint32_t sum = 0;
+  if (bin < bins) {
+#pragma unroll 8
+    for (int t = t0; t < t1; ++t) sum += h[(int64_t)t * bins];
   }
-  if (lane == 0) r.total[bin] = run;
+  sh[g][threadIdx.x] = sum;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+  for (int i = 0; i < 32; ++i) {
+    const uint32_t v = sh[i][threadIdx.x];
+    before += i < g ? v : 0u;
+    all += v;
+  }
+  if (bin >= bins) return;
+  if (g == 0) r.total[bin] = all;
+#pragma unroll 8
+  for (int t = t0; t < t1; ++t) {
+    const uint32_t v = h[(int64_t)t * bins];
+    h[(int64_t)t * bins] = before;
+    before += v;
+  }
 }
 
 // Moves a tile's positions to their places.  A warp holds successive positions, 32 at a time in order, so that equal
 // digits keep their order: before them come the smaller digits, the tiles before, the warps before and the lanes before.
+// Each then counts its next digit for the tile that it has moved to.
 __global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(LookupParams p, RadixParams r) {
   constexpr int kWarps = kEbThreads / 32, kRounds = kEbTile / kEbThreads;
   __shared__ uint32_t at[1 << kEbMaxBits];               // first place of a digit of this tile
   __shared__ uint16_t cnt[kWarps][1 << kEbMaxBits];
   __shared__ uint32_t wsum[kWarps];
   const int bins = 1 << r.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < kWarps << kEbMaxBits; i += kEbThreads) (&cnt[0][0])[i] = 0;
-  // the digits' first places: prefix sums over all digits, kPer neighbouring ones a thread
-  constexpr int kPer = (1 << kEbMaxBits) / kEbThreads;
-  uint32_t v[kPer], sum = 0;
+  const int64_t n0 = (int64_t)blockIdx.x * kEbTile + warp * 32 * kRounds + lane;
+  uint2 e[kRounds];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int b = (int)threadIdx.x * kPer + i;
-    v[i] = b < bins ? r.total[b] : 0u;
-    sum += v[i];
+  for (int i = 0; i < kRounds; ++i) e[i] = n0 + i * 32 < p.N ? radix_load(p, r, n0 + i * 32) : make_uint2(0u, 0u);
+  for (int i = threadIdx.x; i < kWarps << (kEbMaxBits - 1); i += kEbThreads) reinterpret_cast<uint32_t*>(&cnt[0][0])[i] = 0;
+  // of each of a thread's kPer neighbouring digits: all positions, and those of the tiles before
+  constexpr int kPer = (1 << kEbMaxBits) / kEbThreads;
+  const int per = bins / kEbThreads > 0 ? bins / kEbThreads : 1, b0 = (int)threadIdx.x * per;
+  uint32_t v[kPer], ahead[kPer], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) v[i] = ahead[i] = 0;
+  if (b0 < bins) {
+    if (r.scanned) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (i < per) {
+          v[i] = r.total[b0 + i];
+          ahead[i] = r.hist[(int64_t)blockIdx.x * bins + b0 + i];
+        }
+    } else {
+#pragma unroll 8
+      for (int t = 0; t < r.tiles; ++t)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (i < per) {
+            const uint32_t c = r.hist[(int64_t)t * bins + b0 + i];
+            v[i] += c;
+            ahead[i] += t < (int)blockIdx.x ? c : 0u;
+          }
+    }
   }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) sum += v[i];
   uint32_t inc = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -269,16 +313,10 @@ __global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(Lookup
   for (int w = 0; w < warp; ++w) before += wsum[w];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int b = (int)threadIdx.x * kPer + i;
-    if (b < bins) at[b] = before + r.hist[(int64_t)b * r.tiles + blockIdx.x];
+    if (i < per && b0 < bins) at[b0 + i] = before + ahead[i];
     before += v[i];
   }
-  const int64_t n0 = (int64_t)blockIdx.x * kEbTile + warp * 32 * kRounds + lane;
-  uint2 e[kRounds];
   uint16_t rank[kRounds];
-#pragma unroll
-  for (int i = 0; i < kRounds; ++i)
-    e[i] = n0 + i * 32 < p.N ? radix_load(p, r, n0 + i * 32) : make_uint2(0u, 0u);
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) {
     const bool in = n0 + i * 32 < p.N;
@@ -302,12 +340,24 @@ __global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(Lookup
     }
   }
   __syncthreads();
+  uint32_t place[kRounds];
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) place[i] = 0xFFFFFFFFu;
 #pragma unroll
   for (int i = 0; i < kRounds; ++i)
     if (n0 + i * 32 < p.N) {
       const uint32_t digit = (e[i].x >> r.shift) & (bins - 1);
-      r.out[at[digit] + cnt[warp][digit] + rank[i]] = e[i];
+      const uint32_t to = at[digit] + cnt[warp][digit] + rank[i];
+      r.out[to] = e[i];
+      place[i] = (to / kEbTile) << r.bits | ((e[i].x >> (r.shift + r.bits)) & (bins - 1));
     }
+  if (!r.next) return;
+  // one addition for all lanes that count at the same place: half of a text's tokens share their upper digit
+#pragma unroll
+  for (int i = 0; i < kRounds; ++i) {
+    const uint32_t same = __match_any_sync(0xffffffffu, place[i]);
+    if (place[i] != 0xFFFFFFFFu && (same & ((1u << lane) - 1)) == 0) atomicAdd(&r.next[place[i]], (uint32_t)__popc(same));
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ sums
@@ -427,64 +477,70 @@ __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams 
     Raw<float, KE>::store(p.part + (item * 2) * p.d + c, acc);
   } else if (next == key) {
     Raw<float, KE>::store(p.part + (item * 2 + 1) * p.d + c, acc);
+    if (slab == 0 && threadIdx.x == 0) p.joins[1 + atomicAdd(p.joins, 1u)] = (uint32_t)item;
   } else {
     table_put<KE>(p, key, c, acc);
   }
 }
 
-// Runs that reach over the end of the chunk where they begin: their partial sums.  blockDim.y threads of a column share
-// out the chunks and are added up in their order.
-constexpr int kEbJoinShares = 4;
+// Runs that reach over the end of the chunk where they begin, as the sums listed them: their partial sums.  blockDim.y
+// threads of a column share out the chunks and are added up in their order, so the list's order does not matter.
+constexpr int kEbJoinCols = 128, kEbJoinShares = 2;
 template <int KE>
-__global__ void __launch_bounds__(64 * kEbJoinShares) embedding_join_kernel(LookupParams p) {
-  constexpr int kAhead = 4;
-  __shared__ float sh[kEbJoinShares][64 * KE];
-  const int slab = (int)(blockIdx.x % (unsigned)p.slabs);
-  const int64_t item = blockIdx.x / (unsigned)p.slabs;
-  const int c = (slab * 64 + (int)threadIdx.x) * KE;
-  const int64_t first = item * p.chunk, end = first + p.chunk;
-  if (end >= p.N) return;
-  const uint32_t key = p.sorted[end - 1].x, next = p.sorted[end].x;
-  const uint32_t start = p.sorted[first].x, prev = first ? p.sorted[first - 1].x : 0xFFFFFFFFu;
-  if (key >= (uint32_t)p.V || next != key || (start == key && prev == key)) return;  // the last: it began before
-  float acc[KE];
+__global__ void __launch_bounds__(kEbJoinCols * kEbJoinShares) embedding_join_kernel(LookupParams p) {
+  constexpr int kAhead = 8;
+  __shared__ float sh[kEbJoinShares][kEbJoinCols * KE];
+  const int64_t items = (int64_t)*p.joins * p.slabs;
+  for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
+    const int64_t item = p.joins[1 + w / p.slabs];
+    const int c = ((int)(w % p.slabs) * kEbJoinCols + (int)threadIdx.x) * KE;
+    const uint32_t key = p.sorted[(item + 1) * p.chunk].x;
+    float acc[KE];
 #pragma unroll
-  for (int i = 0; i < KE; ++i) acc[i] = 0.f;
-  if (c < p.d) {
-    if (threadIdx.y == 0) {
-      Raw<float, KE> t;
-      t.load(p.part + (item * 2 + 1) * p.d + c);
-      t.widen(acc);
-    }
-    for (int64_t j0 = item + 1 + threadIdx.y; j0 < p.chunks; j0 += kAhead * kEbJoinShares) {
-      Raw<float, KE> v[kAhead];
-      bool in[kAhead];
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int64_t at = j0 + j * kEbJoinShares;
-        in[j] = at < p.chunks && p.sorted[at * p.chunk].x == key;
-        if (at < p.chunks) v[j].load(p.part + (at * 2) * p.d + c);
+    for (int i = 0; i < KE; ++i) acc[i] = 0.f;
+    if (c < p.d) {
+      if (threadIdx.y == 0) {
+        Raw<float, KE> t;
+        t.load(p.part + (item * 2 + 1) * p.d + c);
+        t.widen(acc);
       }
+      for (int64_t j0 = item + 1 + threadIdx.y; j0 < p.chunks; j0 += kAhead * kEbJoinShares) {
+        // keys and sums together: which of the sums count shows when they are there
+        uint32_t k[kAhead];
+        Raw<float, KE> v[kAhead];
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j)
-        if (in[j]) {
+        for (int j = 0; j < kAhead; ++j) {
+          int64_t at = j0 + j * kEbJoinShares;
+          at = at < p.chunks ? at : p.chunks - 1;
+          k[j] = load_here(&p.sorted[at * p.chunk].x);
+          const float* from = p.part + (at * 2) * p.d + c;
+          if constexpr (KE == 1) v[j].v = __uint_as_float(load_here(reinterpret_cast<const uint32_t*>(from)));
+          else v[j].v[0] = load_here(reinterpret_cast<const uint4*>(from));
+        }
+        bool in[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          in[j] = j0 + j * kEbJoinShares < p.chunks && k[j] == key;
           float f[KE];
           v[j].widen(f);
 #pragma unroll
-          for (int i = 0; i < KE; ++i) acc[i] += f[i];
+          for (int i = 0; i < KE; ++i) acc[i] += in[j] ? f[i] : 0.f;
         }
-      if (!in[kAhead - 1]) break;
+        if (!in[kAhead - 1]) break;
+      }
     }
+#pragma unroll
+    for (int i = 0; i < KE; ++i) sh[threadIdx.y][threadIdx.x + i * kEbJoinCols] = acc[i];
+    __syncthreads();
+    if (threadIdx.y == 0 && c < p.d) {
+#pragma unroll
+      for (int y = 1; y < kEbJoinShares; ++y)
+#pragma unroll
+        for (int i = 0; i < KE; ++i) acc[i] += sh[y][threadIdx.x + i * kEbJoinCols];
+      table_put<KE>(p, key, c, acc);
+    }
+    __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < KE; ++i) sh[threadIdx.y][threadIdx.x + i * 64] = acc[i];
-  __syncthreads();
-  if (threadIdx.y || c >= p.d) return;
-#pragma unroll
-  for (int y = 1; y < kEbJoinShares; ++y)
-#pragma unroll
-    for (int i = 0; i < KE; ++i) acc[i] += sh[y][threadIdx.x + i * 64];
-  table_put<KE>(p, key, c, acc);
 }
 
 }  // namespace oapl

@@ -62,29 +62,57 @@ __device__ __forceinline__ float adjust_value(float z, bool seen, uint32_t c, co
   return z;
 }
 
-// Shared memory of a CTA whose rows have tokens or biases, for a slice of `n` tokens.  The gradient counts nothing; over
-// the logits it keeps its results instead, by their place in the list.
-template <bool WORDS>
+// Shared memory of a CTA whose rows have tokens or biases, for a slice of `n` tokens: n / 2 words to count in, 16 bits a
+// token, or 32 bits for half of the slice at a time where an answer is too long for that.  The gradient counts nothing;
+// over the logits it keeps its results instead, by their place in the list, a word each.
+constexpr int kAdBiases = 256;  // biases of a row that are kept in shared memory; more are read again where they are
+template <int WORDS>
 struct AdjustShared {
-  uint32_t* count;    // of the list
+  uint32_t* listed;   // length of the list
   uint32_t* seen;     // [n / 32]
   uint32_t* biased;   // [n / 32]
-  uint32_t* word;     // [n] times in the answer, or results
+  uint32_t* word;     // [WORDS n / 2]
   uint16_t* list;     // [n] tokens of the prompt and the answer, each once
-  static constexpr int bytes(int n) { return 16 + n / 4 + (WORDS ? n * 4 : 0) + n * 2; }
+  int32_t* bias_id;   // [kAdBiases] the row's first biases
+  float* bias;
+  static constexpr int bytes(int n) { return 16 + n / 4 + WORDS * n * 2 + n * 2 + kAdBiases * 8; }
   __device__ __forceinline__ AdjustShared(uint32_t* base, int n) {
-    count = base;
-    seen = count + 4;
+    listed = base;
+    seen = listed + 4;
     biased = seen + n / 32;
     word = biased + n / 32;
-    list = reinterpret_cast<uint16_t*>(word + (WORDS ? n : 0));
+    list = reinterpret_cast<uint16_t*>(word + WORDS * n / 2);
+    bias_id = reinterpret_cast<int32_t*>(list + n);
+    bias = reinterpret_cast<float*>(bias_id + kAdBiases);
   }
 };
+constexpr int64_t kAdShort = 65535;  // tokens of an answer that 16 bits can count
+
+// Overwrites the elements of a vector that are not open, as words: `what` holds the closing value in each element.
+template <typename T, int KE>
+__device__ __forceinline__ void adjust_close(Raw<T, KE>& v, uint32_t open, uint32_t what) {
+  if constexpr (KE == 1) {
+    if (!(open & 1u)) {
+      const uint16_t half = (uint16_t)what;
+      v.v = sizeof(T) == 2 ? *reinterpret_cast<const T*>(&half) : *reinterpret_cast<const T*>(&what);
+    }
+  } else {
+    uint32_t* w = reinterpret_cast<uint32_t*>(&v.v[0]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4) {
+        w[k] = open >> k & 1 ? w[k] : what;
+      } else {
+        const uint32_t keep = (open >> (2 * k) & 1 ? 0x0000FFFFu : 0u) | (open >> (2 * k + 1) & 1 ? 0xFFFF0000u : 0u);
+        w[k] = (w[k] & keep) | (what & ~keep);
+      }
+    }
+  }
+}
 
 // GRAD: the gradient.  OVER: the result goes over the logits.
 template <typename T, int KE, int VPT, bool GRAD, bool OVER>
 __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
-  extern __shared__ __align__(16) uint32_t ad_smem[];
   constexpr int kSlice = KE * VPT * kAdThreads;
   static_assert(kSlice <= 65536, "a place in the list has 16 bits");
   constexpr uint32_t kAll = (1u << KE) - 1;
@@ -108,37 +136,31 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
       bits = p.allowed + at * p.ld_allowed + (v0 >> 5);
     }
   }
-  auto is_open = [&](int i) { return !bits || (bits[i >> 5] >> (i & 31) & 1); };
+  // the slice's part of it, in shared memory
+  extern __shared__ __align__(16) uint32_t ad_smem[];
+  if (bits) {
+    for (int i = t; i < (len + 31) / 32; i += kAdThreads) copy_async_4(smem_u32(&ad_smem[i]), bits + i);
+    copy_async_commit();
+  }
+  auto is_open = [&](int i) { return !bits || (ad_smem[i >> 5] >> (i & 31) & 1); };
   // elements before the first vector
   int head = KE == 1 ? 0 : (int)(-(reinterpret_cast<uintptr_t>(out) / sizeof(T)) & (KE - 1));
   head = head < len ? head : len;
   Raw<T, KE> v[VPT];
-  uint32_t open[VPT];
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     const int i = head + (j * kAdThreads + t) * KE;
-    const bool in = i + KE <= len;
-    if ((!OVER || GRAD) && in) v[j].load_stream(d + i);
-    open[j] = kAll;
-    if (bits && in) {
-      const int sh = i & 31;
-      const uint32_t low = bits[i >> 5], high = sh + KE > 32 ? bits[(i >> 5) + 1] : 0u;
-      open[j] = __funnelshift_r(low, high, sh) & kAll;
-    }
+    if ((!OVER || GRAD) && i + KE <= len) v[j].load_stream(d + i);
   }
-  const AdjustShared<!GRAD || OVER> sm(ad_smem, kSlice);
+  constexpr int kWords = !GRAD ? 1 : OVER ? 2 : 0;
+  const AdjustShared<kWords> sm(ad_smem + kSlice / 32 + 4, kSlice);
   const bool special = p.history || p.biased;
-  constexpr int kFirst = 2;  // listed tokens of a thread whose loads go ahead of the copy
   AdjustRow a{1.f, 0.f, 0.f};
-  int64_t b0 = 0, b1 = 0;
-  int listed = 0;
-  float x[kFirst], g[kFirst];
+  int64_t lo = 0, mid = 0, hi = 0, b0 = 0, b1 = 0;
   if (special) {
-    constexpr int kAhead = 4;
     if (p.repetition) a.r = p.repetition[n];
     if (!GRAD && p.frequency) a.f = p.frequency[n];
     if (!GRAD && p.presence) a.p = p.presence[n];
-    int64_t lo = 0, mid = 0, hi = 0;
     if (p.history) {
       lo = p.spans[3 * (int64_t)n], mid = p.spans[3 * (int64_t)n + 1], hi = p.spans[3 * (int64_t)n + 2];
       if (lo < 0 || mid < lo || hi < mid || hi > p.T) {
@@ -155,37 +177,100 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
         if (t == 0 && p.status) atomicCAS(p.status, 0, kErrBadSpan);
       }
     }
-    // the list's length, marks, and counters
-    for (int i = t * 4; i < 4 + kSlice / 16 + (GRAD ? 0 : kSlice); i += kAdThreads * 4)
-      *reinterpret_cast<uint4*>(&sm.count[i]) = make_uint4(0, 0, 0, 0);
+  }
+  const bool narrow = GRAD || hi - mid <= kAdShort;
+  // Marks, lists and counts the row's tokens among those at from .. from + size of the slice.
+  auto gather = [&](int from, int size) {
+    constexpr int kAhead = 4;
+    const uint32_t base = (uint32_t)v0 + (uint32_t)from;
+    for (int i = t * 4; i < 4 + kSlice / 16 + (GRAD ? 0 : kSlice / 2); i += kAdThreads * 4)
+      *reinterpret_cast<uint4*>(&sm.listed[i]) = make_uint4(0, 0, 0, 0);
     __syncthreads();
     for (int64_t i0 = lo + t; i0 < hi; i0 += kAhead * kAdThreads) {
       uint32_t id[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j)
-        id[j] = i0 + j * kAdThreads < hi ? (uint32_t)(p.tokens[i0 + j * kAdThreads]) - (uint32_t)v0 : 0xFFFFFFFFu;
+        id[j] = i0 + j * kAdThreads < hi ? (uint32_t)(p.tokens[i0 + j * kAdThreads]) - base : 0xFFFFFFFFu;
 #pragma unroll
       for (int j = 0; j < kAhead; ++j)
-        if (id[j] < (uint32_t)len) {
+        if (id[j] < (uint32_t)size) {
           const uint32_t bit = 1u << (id[j] & 31);
           uint32_t* word = &sm.seen[id[j] >> 5];
           if (!(*reinterpret_cast<volatile uint32_t*>(word) & bit) && !(atomicOr(word, bit) & bit))
-            sm.list[atomicAdd(sm.count, 1u)] = (uint16_t)id[j];
-          if (!GRAD && i0 + j * kAdThreads >= mid) atomicAdd(&sm.word[id[j]], 1u);
+            sm.list[atomicAdd(sm.listed, 1u)] = (uint16_t)id[j];
+          if (!GRAD && i0 + j * kAdThreads >= mid) {
+            if (narrow) atomicAdd(&sm.word[id[j] >> 1], id[j] & 1 ? 65536u : 1u);
+            else atomicAdd(&sm.word[id[j]], 1u);
+          }
         }
     }
     for (int64_t i = b0 + t; i < b1; i += kAdThreads) {
-      const uint32_t id = (uint32_t)p.bias_id[i] - (uint32_t)v0;
-      if (id < (uint32_t)len) atomicOr(&sm.biased[id >> 5], 1u << (id & 31));
+      const int32_t token = p.bias_id[i];
+      const uint32_t id = (uint32_t)token - base;
+      if (id < (uint32_t)size) atomicOr(&sm.biased[id >> 5], 1u << (id & 31));
+      if (i - b0 < kAdBiases) {
+        sm.bias_id[i - b0] = token;
+        sm.bias[i - b0] = p.bias[i];
+      }
     }
     __syncthreads();
-    listed = (int)*sm.count;
+    return (int)*sm.listed;
+  };
+  auto counted = [&](int at) { return narrow ? (sm.word[at >> 1] >> (at & 1) * 16) & 0xFFFFu : sm.word[at]; };
+  // Stores the value of a token of the list, x and g: its logit and its gradient.
+  auto settle = [&](int from, int at, float x, float g) {
+    if (!is_open(from + at)) return;
+    if (GRAD) Elem<T>::put(out, from + at, adjust_slope(g, x, a));
+    else if (!(sm.biased[at >> 5] >> (at & 31) & 1)) Elem<T>::put(out, from + at, adjust_value(x, true, counted(at), a));
+  };
+  auto settle_rest = [&](int from, int size, int first, int listed) {
+    for (int i = first + t; i < listed; i += kAdThreads) {
+      const int at = sm.list[i];
+      if (GRAD && OVER) {
+        if (is_open(from + at)) Elem<T>::put(out, from + at, __uint_as_float(sm.word[i]));
+      } else {
+        settle(from, at, Elem<T>::one(z, from + at), GRAD ? Elem<T>::one(d, from + at) : 0.f);
+      }
+    }
+    if constexpr (!GRAD) {
+      const int count = (int)(b1 - b0), kept = count < kAdBiases ? count : kAdBiases;
+      for (int i = t; i < count; i += kAdThreads) {
+        const int32_t id = i < kAdBiases ? sm.bias_id[i] : p.bias_id[b0 + i];
+        const uint32_t at = (uint32_t)id - (uint32_t)v0 - (uint32_t)from;
+        if (at >= (uint32_t)size) continue;
+        const float logit = Elem<T>::one(z, from + at);
+        const bool shown = is_open(from + (int)at);
+        // whether an entry before this one has the token, and the sum of this one and those behind it
+        bool first_entry = true;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < kept; ++k) {
+          const bool same = sm.bias_id[k] == id;
+          first_entry = first_entry && !(same && k < i);
+          if (same && k >= i) sum += sm.bias[k];
+        }
+        for (int k = kAdBiases; k < count; ++k)
+          if (p.bias_id[b0 + k] == id) {
+            first_entry = first_entry && k >= i;
+            if (k >= i) sum += p.bias[b0 + k];
+          }
+        if (!first_entry || !shown) continue;
+        const bool seen = sm.seen[at >> 5] >> (at & 31) & 1;
+        Elem<T>::put(out, from + at, adjust_value(logit, seen, counted((int)at), a) + sum);
+      }
+    }
+  };
+  constexpr int kFirst = 2;  // listed tokens of a thread whose loads go ahead of the copy
+  int listed = 0;
+  float x[kFirst], g[kFirst];
+  if (special && narrow) {
+    listed = gather(0, len);
 #pragma unroll
     for (int j = 0; j < kFirst; ++j) {
       const int i = j * kAdThreads + t;
       if (i < listed) {
         x[j] = Elem<T>::one(z, sm.list[i]);
-        if (GRAD) g[j] = Elem<T>::one(d, sm.list[i]);
+        g[j] = GRAD ? Elem<T>::one(d, sm.list[i]) : 0.f;
       }
     }
     if (GRAD && OVER) {
@@ -198,11 +283,19 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
     }
   }
   const float closed = GRAD ? 0.f : -__int_as_float(0x7F800000);
-  if (OVER && !GRAD) {
+  if (bits) {
+    copy_async_wait_all();
+    __syncthreads();
+  }
+  uint32_t open[VPT];
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      const int i = head + (j * kAdThreads + t) * KE;
-      if (open[j] != kAll && open[j]) v[j].load(z + i);
+  for (int j = 0; j < VPT; ++j) {
+    const int i = head + (j * kAdThreads + t) * KE;
+    open[j] = kAll;
+    if (bits && i + KE <= len) {
+      // (the word behind the slice's last one is there, whatever it holds)
+      open[j] = __funnelshift_r(ad_smem[i >> 5], ad_smem[(i >> 5) + 1], i & 31) & kAll;
+      if (OVER && !GRAD && open[j] != kAll && open[j]) v[j].load(z + i);
     }
   }
 #pragma unroll
@@ -213,12 +306,8 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
       if (!OVER || GRAD) v[j].put(out + i);
       continue;
     }
-    float f[KE];
-    if (open[j]) v[j].widen(f);
-#pragma unroll
-    for (int k = 0; k < KE; ++k)
-      if (!(open[j] >> k & 1)) f[k] = closed;
-    Raw<T, KE>::store(out + i, f);
+    adjust_close<T, KE>(v[j], open[j], GRAD ? 0u : Elem<T>::kNegInf);
+    v[j].put(out + i);
   }
   if (KE > 1 && t < 2 * KE) {  // what is left before and behind the vectors
     const int i = t < KE ? t : head + (len - head) / KE * KE + t - KE;
@@ -229,38 +318,17 @@ __global__ void __launch_bounds__(kAdThreads) adjust_kernel(AdjustParams p) {
   }
   if (!special) return;
   __syncthreads();
+  if (narrow) {
 #pragma unroll
-  for (int j = 0; j < kFirst; ++j) {
-    const int i = j * kAdThreads + t;
-    if (i < listed) {
-      const int at = sm.list[i];
-      if (is_open(at)) {
-        if (GRAD) Elem<T>::put(out, at, adjust_slope(g[j], x[j], a));
-        else if (!(sm.biased[at >> 5] >> (at & 31) & 1)) Elem<T>::put(out, at, adjust_value(x[j], true, sm.word[at], a));
-      }
-    }
-  }
-  for (int i = kFirst * kAdThreads + t; i < listed; i += kAdThreads) {
-    const int at = sm.list[i];
-    if (!is_open(at)) continue;
-    if (GRAD)
-      Elem<T>::put(out, at, OVER ? __uint_as_float(sm.word[i]) : adjust_slope(Elem<T>::one(d, at), Elem<T>::one(z, at), a));
-    else if (!(sm.biased[at >> 5] >> (at & 31) & 1))
-      Elem<T>::put(out, at, adjust_value(Elem<T>::one(z, at), true, sm.word[at], a));
-  }
-  if constexpr (!GRAD) {
-    for (int64_t i = b0 + t; i < b1; i += kAdThreads) {
-      const int32_t id = p.bias_id[i];
-      const uint32_t at = (uint32_t)id - (uint32_t)v0;
-      if (at >= (uint32_t)len || !is_open((int)at)) continue;
-      bool first = true;
-      for (int64_t k = b0; k < i && first; ++k) first = p.bias_id[k] != id;
-      if (!first) continue;
-      float sum = 0.f;
-      for (int64_t k = i; k < b1; ++k)
-        if (p.bias_id[k] == id) sum += p.bias[k];
-      const bool seen = sm.seen[at >> 5] >> (at & 31) & 1;
-      Elem<T>::put(out, at, adjust_value(Elem<T>::one(z, at), seen, sm.word[at], a) + sum);
+    for (int j = 0; j < kFirst; ++j)
+      if (j * kAdThreads + t < listed) settle(0, sm.list[j * kAdThreads + t], x[j], g[j]);
+    settle_rest(0, len, kFirst * kAdThreads, listed);
+  } else {
+    for (int from = 0; from < len; from += kSlice / 2) {
+      const int size = len - from < kSlice / 2 ? len - from : kSlice / 2;
+      listed = gather(from, size);
+      settle_rest(from, size, 0, listed);
+      __syncthreads();
     }
   }
 }

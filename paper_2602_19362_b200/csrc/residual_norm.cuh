@@ -89,10 +89,6 @@ __device__ __forceinline__ float load_one(const void* p, int type, int64_t i) {
   return type == 0 ? Elem<__nv_bfloat16>::one(p, i) : (type == 1 ? Elem<__half>::one(p, i) : Elem<float>::one(p, i));
 }
 
-__device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // Until the copies of all but the last `ahead` rows are there.
 __device__ __forceinline__ void copy_async_wait(int ahead) {
   if (ahead == 3) asm volatile("cp.async.wait_group 3;" ::: "memory");

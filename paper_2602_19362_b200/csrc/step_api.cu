@@ -70,7 +70,7 @@ static int route_embedding_out(const LookupParams& p, int32_t out_type, int n_sm
 // partial sums of a row's width for each chunk.
 struct LookupCarve {
   int32_t chunk, chunks, bits, passes, tiles;
-  size_t sorted, other, hist, totals, part, total;
+  size_t sorted, other, hist, totals, joins, part, total;
 };
 static bool lookup_carve(int64_t N, int32_t V, int32_t d, LookupCarve* c) {
   if (N <= 0 || V <= 0 || d <= 0 || N > kMaxRows || (int64_t)V > kMaxRows || (int64_t)d > kMaxRows) return false;
@@ -97,16 +97,17 @@ static bool lookup_carve(int64_t N, int32_t V, int32_t d, LookupCarve* c) {
     c->bits = (bits + c->passes - 1) / c->passes;
     c->tiles = (int32_t)((N + kEbTile - 1) / kEbTile);
     c->other = take(8 * (size_t)N);
-    c->hist = take(4 * ((size_t)c->tiles << c->bits));
+    c->hist = take(4 * (size_t)c->passes * ((size_t)c->tiles << c->bits));
     c->totals = take(4 * ((size_t)1 << c->bits));
   }
+  c->joins = take(4 * ((size_t)chunks + 1));
   c->part = take(8 * (size_t)chunks * (size_t)d);
   c->total = off;
   return true;
 }
 
 template <typename T, int KE>
-static int launch_embedding_sum(LookupParams p, cudaStream_t st) {
+static int launch_embedding_sum(LookupParams p, int n_sm, cudaStream_t st) {
   const int64_t units = p.d / KE;
   const int64_t slabs = (units + kEbThreads - 1) / kEbThreads;
   const int threads = (int)round_up((size_t)((units + slabs - 1) / slabs), 32);
@@ -117,41 +118,47 @@ static int launch_embedding_sum(LookupParams p, cudaStream_t st) {
   CKL();
   if (p.chunks > 1) {
     constexpr int JE = KE > 4 ? 4 : KE;
-    p.slabs = (int32_t)((p.d / JE + 63) / 64);
-    if ((int64_t)p.chunks * p.slabs > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
-    embedding_join_kernel<JE><<<(unsigned)(p.chunks * (int64_t)p.slabs), dim3(64, kEbJoinShares), 0, st>>>(p);
+    p.slabs = (int32_t)((p.d / JE + kEbJoinCols - 1) / kEbJoinCols);
+    const int64_t most = (int64_t)p.chunks * p.slabs, grid = 8 * (int64_t)n_sm;  // how many there are, the device knows
+    embedding_join_kernel<JE><<<(unsigned)(most < grid ? most : grid), dim3(kEbJoinCols, kEbJoinShares), 0, st>>>(p);
     CKL();
   }
   return OAPL_OK;
 }
 
 template <typename T>
-static int route_embedding_sum(const LookupParams& p, cudaStream_t st) {
+static int route_embedding_sum(const LookupParams& p, int n_sm, cudaStream_t st) {
   constexpr int KE = Elem<T>::kN;
   const bool vec = on16(p.in) && on16(p.out) && p.d % KE == 0 && p.ld_in * sizeof(T) % 16 == 0 && p.ld_out % 4 == 0;
-  return vec ? launch_embedding_sum<T, KE>(p, st) : launch_embedding_sum<T, 1>(p, st);
+  return vec ? launch_embedding_sum<T, KE>(p, n_sm, st) : launch_embedding_sum<T, 1>(p, n_sm, st);
 }
 
 // ---------------------------------------------------------------------------------------
 // Gradient norm and clipping.
+// log2 of an element's size, -1 for no type.  A list has hundreds of tensors: no divisions here.
+static int type_shift(int32_t type) {
+  return type == OAPL_TYPE_BF16 || type == OAPL_TYPE_F16 ? 1 : (type == OAPL_TYPE_F32 ? 2 : -1);
+}
 static int check_tensors(const oapl_tensor* t, int32_t count, bool clip) {
   if (!t || count <= 0) return OAPL_ERR_INVALID_ARG;
   int64_t chunks = 0;
   for (int32_t i = 0; i < count; ++i) {
-    const int es = type_size(t[i].type), os = type_size(t[i].out_type);
-    if (t[i].n < 0 || !es) return OAPL_ERR_INVALID_ARG;
+    const int es = type_shift(t[i].type);
+    if (t[i].n < 0 || es < 0) return OAPL_ERR_INVALID_ARG;
     if (!t[i].n) continue;
-    if (!t[i].data) return OAPL_ERR_INVALID_ARG;
-    if ((uintptr_t)t[i].data % es) return OAPL_ERR_MISALIGNED;
+    const uintptr_t in = (uintptr_t)t[i].data, out = (uintptr_t)t[i].out;
+    if (!in) return OAPL_ERR_INVALID_ARG;
+    if (in & ((1u << es) - 1)) return OAPL_ERR_MISALIGNED;
     chunks += (t[i].n - 1) / (kGcBytes / 4) + 1;  // the most that its types can give
     if (chunks > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
     if (!clip) continue;
-    if (!t[i].out || !os) return OAPL_ERR_INVALID_ARG;
-    if ((uintptr_t)t[i].out % os) return OAPL_ERR_MISALIGNED;
-    if (t[i].out == t[i].data) {
+    const int os = type_shift(t[i].out_type);
+    if (!out || os < 0) return OAPL_ERR_INVALID_ARG;
+    if (out & ((1u << os) - 1)) return OAPL_ERR_MISALIGNED;
+    if (in == out) {
       if (t[i].type != t[i].out_type) return OAPL_ERR_INVALID_ARG;
-    } else if (overlap({t[i].data, 1, t[i].n, t[i].n, es}, {t[i].out, 1, t[i].n, t[i].n, os}) != kApart) {
-      return OAPL_ERR_INVALID_ARG;
+    } else if (in < out + ((uintptr_t)t[i].n << os) && out < in + ((uintptr_t)t[i].n << es)) {
+      return OAPL_ERR_INVALID_ARG;  // partly over itself
     }
   }
   return OAPL_OK;
@@ -171,8 +178,7 @@ static int32_t fill_list(const oapl_tensor* t, int32_t count, bool clip, GradLis
     g.in_type = (uint8_t)t[i].type;
     g.out_type = (uint8_t)(clip ? t[i].out_type : 0);
     g.vec = on16(t[i].data) && (!clip || on16(t[i].out));
-    const int wide = type_size(t[i].type) == 4 || (clip && type_size(t[i].out_type) == 4) ? 4 : 2;
-    g.shift = wide == 4 ? 12 : 13;
+    g.shift = t[i].type == OAPL_TYPE_F32 || (clip && t[i].out_type == OAPL_TYPE_F32) ? 12 : 13;
     static_assert(kGcBytes == 4 << 12, "a chunk's elements");
     l->chunks += (int32_t)((t[i].n - 1 >> g.shift) + 1);
   }
@@ -244,13 +250,15 @@ static int launch_adjust(AdjustParams p, cudaStream_t st) {
   if (slices * p.N > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
   p.slices = (int32_t)slices;
   auto kern = adjust_kernel<T, KE, VPT, GRAD, OVER>;
-  const int smem = p.history || p.biased ? AdjustShared<!GRAD || OVER>::bytes((int)kSlice) : 0;
+  const int smem = (p.allowed || p.history || p.biased ? (int)kSlice / 8 + 16 : 0) +
+                   (p.history || p.biased ? AdjustShared<!GRAD ? 1 : OVER ? 2 : 0>::bytes((int)kSlice) : 0);
+  constexpr int kMost = (int)kSlice / 8 + 16 + AdjustShared<!GRAD ? 1 : OVER ? 2 : 0>::bytes((int)kSlice);
   if (smem > 40 * 1024) {
     static bool done[kMaxDevices] = {false};
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return OAPL_ERR_CUDA;
     if (!done[dev]) {
-      if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+      if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) != cudaSuccess)
         return OAPL_ERR_CUDA;
       done[dev] = true;
     }
@@ -262,12 +270,13 @@ static int launch_adjust(AdjustParams p, cudaStream_t st) {
 
 template <typename T, int KE, bool GRAD, bool OVER>
 static int route_adjust_size(const AdjustParams& p, int n_sm, cudaStream_t st) {
-  // slices of 8192 tokens where they give every SM four, of 2048 otherwise; the gradient, which counts nothing and has
-  // room, 16384, and 4096 where it goes an element at a time
-  constexpr int kMany = (KE == 1 ? 16 : GRAD && !OVER ? 64 : 32) / KE, kFew = 8 / KE;
+  // Slices of 16384 tokens (8192 for the gradient over the logits, which needs the room, and 4096 an element at a time)
+  // where they give every SM four CTAs, else half of that where they do, else 2048.
+  constexpr int kMany = (KE == 1 ? 16 : GRAD && OVER ? 32 : 64) / KE, kSome = kMany / 2, kFew = 8 / KE;
   const int64_t many = (int64_t)p.N * p.V / (kMany * KE * kAdThreads);
-  return many >= 4 * (int64_t)n_sm ? launch_adjust<T, KE, kMany, GRAD, OVER>(p, st)
-                                   : launch_adjust<T, KE, kFew, GRAD, OVER>(p, st);
+  if (many >= 4 * (int64_t)n_sm) return launch_adjust<T, KE, kMany, GRAD, OVER>(p, st);
+  if (2 * many >= 4 * (int64_t)n_sm) return launch_adjust<T, KE, kSome, GRAD, OVER>(p, st);
+  return launch_adjust<T, KE, kFew, GRAD, OVER>(p, st);
 }
 
 template <typename T>
@@ -341,6 +350,8 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
   LookupCarve c;
   if (!lookup_carve(lookup->N, lookup->V, d, &c)) return OAPL_ERR_UNSUPPORTED_SHAPE;
   if (ws_bytes < c.total) return OAPL_ERR_WORKSPACE_TOO_SMALL;
+  const int n_sm = sm_count();
+  if (n_sm <= 0) return OAPL_ERR_CUDA;
   uint8_t* w = static_cast<uint8_t*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   LookupParams p = lookup_params(lookup, d, device_status);
@@ -353,6 +364,7 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
   p.chunks = c.chunks;
   p.sorted = reinterpret_cast<uint2*>(w + c.sorted);
   p.part = reinterpret_cast<float*>(w + c.part);
+  p.joins = reinterpret_cast<uint32_t*>(w + c.joins);
   if (!c.passes) {
     const int per = kEbThreads / 32 * kEbCountRows;
     embedding_count_sort_kernel<<<(unsigned)((p.N + per - 1) / per), kEbThreads, 0, st>>>(p);
@@ -361,25 +373,36 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
     uint2* lists[2] = {p.sorted, reinterpret_cast<uint2*>(w + c.other)};
     RadixParams r;
     memset(&r, 0, sizeof(r));
-    r.hist = reinterpret_cast<uint32_t*>(w + c.hist);
+    uint32_t* hist = reinterpret_cast<uint32_t*>(w + c.hist);
+    const int64_t words = (int64_t)c.tiles << c.bits;
     r.total = reinterpret_cast<uint32_t*>(w + c.totals);
     r.bits = c.bits;
     r.tiles = c.tiles;
+    r.hist = hist;
+    r.clear = hist + words;
+    r.clear_words = (c.passes - 1) * words;
+    // Each tile's CTA adds up all tiles' counts itself while they are few; a launch in between costs 2 us (40960 rows:
+    // 20 tiles, %SCAN%).
+    r.scanned = c.tiles > 64;
+    embedding_radix_count_kernel<<<(unsigned)c.tiles, kEbThreads, 0, st>>>(p, r);
+    CKL();
     for (int k = 0; k < c.passes; ++k) {
+      r.hist = hist + k * words;
+      r.next = k + 1 < c.passes ? r.hist + words : nullptr;
       r.shift = k * c.bits;
       r.out = lists[(c.passes - 1 - k) & 1];  // the last pass into `sorted`
-      embedding_radix_hist_kernel<<<(unsigned)c.tiles, kEbThreads, 0, st>>>(p, r);
-      CKL();
-      embedding_radix_scan_kernel<<<(unsigned)(((1 << c.bits) + 7) / 8), kEbThreads, 0, st>>>(r);
-      CKL();
+      if (r.scanned) {
+        embedding_radix_scan_kernel<<<(unsigned)(((1 << c.bits) + 31) / 32), dim3(32, 32), 0, st>>>(r);
+        CKL();
+      }
       embedding_radix_move_kernel<<<(unsigned)c.tiles, kEbThreads, 0, st>>>(p, r);
       CKL();
       r.in = r.out;
     }
   }
-  if (type == OAPL_TYPE_BF16) return route_embedding_sum<__nv_bfloat16>(p, st);
-  if (type == OAPL_TYPE_F16) return route_embedding_sum<__half>(p, st);
-  return route_embedding_sum<float>(p, st);
+  if (type == OAPL_TYPE_BF16) return route_embedding_sum<__nv_bfloat16>(p, n_sm, st);
+  if (type == OAPL_TYPE_F16) return route_embedding_sum<__half>(p, n_sm, st);
+  return route_embedding_sum<float>(p, n_sm, st);
 }
 
 size_t oapl_grad_norm_workspace_bytes(int32_t count) {

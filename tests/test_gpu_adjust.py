@@ -184,6 +184,25 @@ def test_histories_of_length_zero_and_one_and_shared_tokens():
     check_fwd(c)
 
 
+@pytest.mark.parametrize("over", [False, True])
+@pytest.mark.parametrize("N,V", [(2, 20000), (700, 8300)])
+def test_answers_too_long_to_count_in_16_bits(N, V, over):
+    # 66000 times one token, 65535 and 65536 tokens beside it
+    g = torch.Generator().manual_seed(17)
+    toks = torch.cat([torch.full((66000,), 5), torch.randint(0, V, (9000,), generator=g), torch.full((4,), V - 1)])
+    c = make(N, V, "f32", 17, prompt=0, answer=0)
+    c["tokens"] = toks.to(torch.int32).cuda()
+    ends = torch.tensor([toks.numel(), 65535, 65536, 66001, 100, 70000])
+    spans = torch.zeros(N, 3, dtype=torch.long)
+    spans[:, 2] = ends[torch.arange(N) % 6]
+    spans[3::6, 1] = 3
+    c.update(spans=spans.cuda(), repetition=torch.full((N,), 1.25, device="cuda"), frequency=torch.full((N,), 0.001, device="cuda"),
+             presence=torch.full((N,), -0.5, device="cuda"))
+    if not over:
+        check_bwd(c)
+    check_fwd(c, over=over)
+
+
 def test_empty_bias_list():
     c = make(4, 300, "bf16", 6, bias=0)
     c.update(bias_start=torch.zeros(5, dtype=torch.long, device="cuda"), bias_id=torch.zeros(0, dtype=torch.int32, device="cuda"),

@@ -66,10 +66,10 @@ def test_embedding_gradient_arguments(L):
 def test_embedding_workspace(L):
     w = L.oapl_embedding_workspace_bytes
     assert w(0, 10, 10) == w(10, 0, 10) == w(10, 10, 0) == w(3 * 10 ** 9, 10, 10) == 0
-    # two rows of partial sums for each chunk, the list, and for many rows a second list and the digits' counts
+    # two rows of partial sums and a word for each chunk, the list, and for many rows a second list and the digits' counts
     assert w(1, 10, 64) <= 256 + 512 + 256
     for N, chunk in ((8192, 32), (40960, 32), (300000, 128), (4000000, 256)):
-        assert w(N, 152064, 64) <= 16 * N + 512 * (N // chunk + 1) + 4 * 1024 * (N // 2048 + 2) + 2048
+        assert w(N, 152064, 64) <= 16 * N + 516 * (N // chunk + 1) + 4 * 1024 * (N // 2048 + 2) + 2048
 
 
 def _residual(**kw):
