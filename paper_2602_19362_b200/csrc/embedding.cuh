@@ -24,6 +24,7 @@ namespace oapl {
 constexpr int kEbThreads = 256;
 constexpr int kEbCountMax = 8192;   // positions sorted by counting: work grows with their square
 constexpr int kEbTile = 2048;       // positions of a CTA of the radix sort
+constexpr int kEbMoveThreads = 512;
 constexpr int kEbMaxBits = 10;      // digit of a pass
 constexpr int kEbMinChunk = 32, kEbMaxChunk = 256;
 constexpr int kEbZeroRows = 32;     // rows of the table of a CTA that clears
@@ -56,6 +57,19 @@ __device__ __forceinline__ uint32_t lookup_key(const LookupParams& p, int64_t n)
 }
 __device__ __forceinline__ void lookup_check(const LookupParams& p, int64_t n) {
   if (p.status && !(p.mask && !p.mask[n]) && (uint32_t)p.ids[n] >= (uint32_t)p.V) atomicCAS(p.status, 0, kErrBadId);
+}
+
+// Clears a row of the table's gradient, by a whole CTA.
+__device__ __forceinline__ void clear_row(const LookupParams& p, int64_t v) {
+  float* row = static_cast<float*>(p.out) + v * p.ld_out;
+  // up to the first 16-byte boundary, vectors, and the rest
+  int head = (int)(-(reinterpret_cast<uintptr_t>(row) >> 2) & 3);
+  head = head < p.d ? head : p.d;
+  const int vecs = (p.d - head) / 4, tail = (p.d - head) % 4, t = threadIdx.x;
+  float4* body = reinterpret_cast<float4*>(row + head);
+  for (int i = t; i < vecs; i += blockDim.x) body[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (t < head) row[t] = 0.f;
+  else if (t < head + tail) row[vecs * 4 + t] = 0.f;
 }
 
 // ------------------------------------------------------------------------------------------------ lookup
@@ -262,9 +276,9 @@ __global__ void __launch_bounds__(1024) embedding_radix_scan_kernel(RadixParams 
 // Moves a tile's positions to their places.  A warp holds successive positions, 32 at a time in order, so that equal
 // digits keep their order: before them come the smaller digits, the tiles before, the warps before and the lanes before.
 // Each then counts its next digit for the tile that it has moved to.
-__global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(LookupParams p, RadixParams r) {
-  constexpr int kWarps = kEbThreads / 32, kRounds = kEbTile / kEbThreads;
-  __shared__ uint32_t at[1 << kEbMaxBits];               // first place of a digit of this tile
+__global__ void __launch_bounds__(kEbMoveThreads) embedding_radix_move_kernel(LookupParams p, RadixParams r) {
+  constexpr int kWarps = kEbMoveThreads / 32, kRounds = kEbTile / kEbMoveThreads;
+  __shared__ uint32_t at[1 << kEbMaxBits], total[1 << kEbMaxBits];  // first place of a digit of this tile, and all of it
   __shared__ uint16_t cnt[kWarps][1 << kEbMaxBits];
   __shared__ uint32_t wsum[kWarps];
   const int bins = 1 << r.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -272,35 +286,38 @@ __global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(Lookup
   uint2 e[kRounds];
 #pragma unroll
   for (int i = 0; i < kRounds; ++i) e[i] = n0 + i * 32 < p.N ? radix_load(p, r, n0 + i * 32) : make_uint2(0u, 0u);
-  for (int i = threadIdx.x; i < kWarps << (kEbMaxBits - 1); i += kEbThreads) reinterpret_cast<uint32_t*>(&cnt[0][0])[i] = 0;
-  // of each of a thread's kPer neighbouring digits: all positions, and those of the tiles before
-  constexpr int kPer = (1 << kEbMaxBits) / kEbThreads;
-  const int per = bins / kEbThreads > 0 ? bins / kEbThreads : 1, b0 = (int)threadIdx.x * per;
-  uint32_t v[kPer], ahead[kPer], sum = 0;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) v[i] = ahead[i] = 0;
-  if (b0 < bins) {
+  for (int i = threadIdx.x; i < kWarps << (kEbMaxBits - 1); i += kEbMoveThreads) reinterpret_cast<uint32_t*>(&cnt[0][0])[i] = 0;
+  // of each digit: all positions, and those of the tiles before
+  for (int b = threadIdx.x; b < bins; b += kEbMoveThreads) {
+    uint32_t all = 0, ahead = 0;
     if (r.scanned) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (i < per) {
-          v[i] = r.total[b0 + i];
-          ahead[i] = r.hist[(int64_t)blockIdx.x * bins + b0 + i];
-        }
+      all = r.total[b];
+      ahead = r.hist[(int64_t)blockIdx.x * bins + b];
     } else {
-#pragma unroll 8
-      for (int t = 0; t < r.tiles; ++t)
+      for (int t0 = 0; t0 < r.tiles; t0 += 16) {
+        uint32_t c[16];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (i < per) {
-            const uint32_t c = r.hist[(int64_t)t * bins + b0 + i];
-            v[i] += c;
-            ahead[i] += t < (int)blockIdx.x ? c : 0u;
-          }
+        for (int t = 0; t < 16; ++t) c[t] = t0 + t < r.tiles ? r.hist[(t0 + t) * bins + b] : 0u;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+          all += c[t];
+          ahead += t0 + t < (int)blockIdx.x ? c[t] : 0u;
+        }
+      }
     }
+    total[b] = all;
+    at[b] = ahead;
   }
+  __syncthreads();
+  // the digits' first places: prefix sums, neighbouring digits a thread
+  constexpr int kPer = (1 << kEbMaxBits) / kEbMoveThreads;
+  uint32_t v[kPer], sum = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) sum += v[i];
+  for (int i = 0; i < kPer; ++i) {
+    const int b = (int)threadIdx.x * kPer + i;
+    v[i] = b < bins ? total[b] : 0u;
+    sum += v[i];
+  }
   uint32_t inc = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -313,7 +330,8 @@ __global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(Lookup
   for (int w = 0; w < warp; ++w) before += wsum[w];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    if (i < per && b0 < bins) at[b0 + i] = before + ahead[i];
+    const int b = (int)threadIdx.x * kPer + i;
+    if (b < bins) at[b] += before;
     before += v[i];
   }
   uint16_t rank[kRounds];
@@ -331,7 +349,7 @@ __global__ void __launch_bounds__(kEbThreads) embedding_radix_move_kernel(Lookup
     __syncwarp();
   }
   __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += kEbThreads) {
+  for (int b = threadIdx.x; b < bins; b += kEbMoveThreads) {
     uint32_t run = 0;
     for (int w = 0; w < kWarps; ++w) {
       const uint32_t c = cnt[w][b];
@@ -412,23 +430,8 @@ __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams 
     }
     __syncthreads();
     const uint32_t m = live;
-    const int w = p.d;
     for (int r = 0; r < kEbZeroRows; ++r)
-      if (!(m >> r & 1)) {
-        float* row = static_cast<float*>(p.out) + (v0 + r) * p.ld_out;
-        if constexpr (KE > 1) {
-          for (int i = threadIdx.x; i < w / 4; i += blockDim.x) reinterpret_cast<float4*>(row)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        } else {
-          // up to the first 16-byte boundary, vectors, and the rest
-          int head = (int)(-(reinterpret_cast<uintptr_t>(row) >> 2) & 3);
-          head = head < w ? head : w;
-          const int vecs = (w - head) / 4;
-          float4* body = reinterpret_cast<float4*>(row + head);
-          for (int i = threadIdx.x; i < vecs; i += blockDim.x) body[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-          const int i = (int)threadIdx.x < head ? (int)threadIdx.x : head + vecs * 4 + (int)threadIdx.x - head;
-          if (i < w && ((int)threadIdx.x < head || (int)threadIdx.x < head + (w - head) % 4)) row[i] = 0.f;
-        }
-      }
+      if (!(m >> r & 1)) clear_row(p, v0 + r);
     return;
   }
   const int64_t first = item * p.chunk;
@@ -490,10 +493,12 @@ template <int KE>
 __global__ void __launch_bounds__(kEbJoinCols * kEbJoinShares) embedding_join_kernel(LookupParams p) {
   constexpr int kAhead = 8;
   __shared__ float sh[kEbJoinShares][kEbJoinCols * KE];
-  const int64_t items = (int64_t)*p.joins * p.slabs;
-  for (int64_t w = blockIdx.x; w < items; w += gridDim.x) {
-    const int64_t item = p.joins[1 + w / p.slabs];
-    const int c = ((int)(w % p.slabs) * kEbJoinCols + (int)threadIdx.x) * KE;
+  __shared__ __align__(16) float ring[kAhead][kEbJoinCols * kEbJoinShares * KE];  // each thread's own places
+  const int mine = ((int)threadIdx.y * kEbJoinCols + (int)threadIdx.x) * KE;
+  const uint32_t slabs = (uint32_t)p.slabs, items = *p.joins * slabs;
+  for (uint32_t w = blockIdx.x; w < items; w += gridDim.x) {
+    const int64_t item = p.joins[1 + w / slabs];
+    const int c = ((int)(w % slabs) * kEbJoinCols + (int)threadIdx.x) * KE;
     const uint32_t key = p.sorted[(item + 1) * p.chunk].x;
     float acc[KE];
 #pragma unroll
@@ -506,27 +511,28 @@ __global__ void __launch_bounds__(kEbJoinCols * kEbJoinShares) embedding_join_ke
       }
       for (int64_t j0 = item + 1 + threadIdx.y; j0 < p.chunks; j0 += kAhead * kEbJoinShares) {
         // keys and sums together: which of the sums count shows when they are there
-        uint32_t k[kAhead];
-        Raw<float, KE> v[kAhead];
+        uint32_t in = 0;
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
           int64_t at = j0 + j * kEbJoinShares;
           at = at < p.chunks ? at : p.chunks - 1;
-          k[j] = load_here(&p.sorted[at * p.chunk].x);
           const float* from = p.part + (at * 2) * p.d + c;
-          if constexpr (KE == 1) v[j].v = __uint_as_float(load_here(reinterpret_cast<const uint32_t*>(from)));
-          else v[j].v[0] = load_here(reinterpret_cast<const uint4*>(from));
+          if constexpr (KE == 1) copy_async_4(smem_u32(&ring[j][mine]), from);
+          else copy_async_16(smem_u32(&ring[j][mine]), from);
         }
-        bool in[kAhead];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-          in[j] = j0 + j * kEbJoinShares < p.chunks && k[j] == key;
-          float f[KE];
-          v[j].widen(f);
-#pragma unroll
-          for (int i = 0; i < KE; ++i) acc[i] += in[j] ? f[i] : 0.f;
+          const int64_t at = j0 + j * kEbJoinShares;
+          in |= (uint32_t)(at < p.chunks && p.sorted[at * p.chunk].x == key) << j;
         }
-        if (!in[kAhead - 1]) break;
+        copy_async_wait_all();
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+          if (in >> j & 1) {
+#pragma unroll
+            for (int i = 0; i < KE; ++i) acc[i] += ring[j][mine + i];
+          }
+        if (!(in >> (kAhead - 1) & 1)) break;
       }
     }
 #pragma unroll

@@ -19,7 +19,7 @@ namespace oapl {
 constexpr int kGcThreads = 256;
 constexpr int kGcVecs = 4;                                  // 16-byte vectors of a thread that are read together
 constexpr int kGcBytes = kGcVecs * kGcThreads * 16;         // of a chunk, in the wider one of its two types
-constexpr int kGcList = 480;       // tensors of a launch
+constexpr int kGcList = 960;       // tensors of a launch: 30 KB of its 32 KB of arguments
 constexpr int kGcSumsPerSm = 8;    // CTAs, each with one partial sum
 constexpr int kErrNonfiniteGrad = -7;  // OAPL_ERR_NONFINITE_INPUT
 

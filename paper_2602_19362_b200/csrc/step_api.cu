@@ -74,10 +74,10 @@ struct LookupCarve {
 };
 static bool lookup_carve(int64_t N, int32_t V, int32_t d, LookupCarve* c) {
   if (N <= 0 || V <= 0 || d <= 0 || N > kMaxRows || (int64_t)V > kMaxRows || (int64_t)d > kMaxRows) return false;
-  // Chunks: short ones give a CTA to each few rows, long ones few partial sums to join where one token is frequent.
-  // 4096 of them are more than the GPU holds at a time.
+  // Chunks: short ones give a CTA to each few rows, long ones few partial sums to join where one token is frequent
+  // (a token's join takes 0.16 us per chunk).  640 of them are four per SM.
   int64_t chunk = kEbMinChunk;
-  while (chunk < kEbMaxChunk && chunk * 4096 < N) chunk *= 2;
+  while (chunk < kEbMaxChunk && chunk * 640 < N) chunk *= 2;
   const int64_t chunks = (N + chunk - 1) / chunk;
   c->chunk = (int32_t)chunk;
   c->chunks = (int32_t)chunks;
@@ -119,7 +119,9 @@ static int launch_embedding_sum(LookupParams p, int n_sm, cudaStream_t st) {
   if (p.chunks > 1) {
     constexpr int JE = KE > 4 ? 4 : KE;
     p.slabs = (int32_t)((p.d / JE + kEbJoinCols - 1) / kEbJoinCols);
-    const int64_t most = (int64_t)p.chunks * p.slabs, grid = 8 * (int64_t)n_sm;  // how many there are, the device knows
+    const int64_t most = (int64_t)p.chunks * p.slabs;
+    if (most > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
+    const int64_t grid = 8 * (int64_t)n_sm;  // how many there are, the device knows
     embedding_join_kernel<JE><<<(unsigned)(most < grid ? most : grid), dim3(kEbJoinCols, kEbJoinShares), 0, st>>>(p);
     CKL();
   }
@@ -272,7 +274,7 @@ template <typename T, int KE, bool GRAD, bool OVER>
 static int route_adjust_size(const AdjustParams& p, int n_sm, cudaStream_t st) {
   // Slices of 16384 tokens (8192 for the gradient over the logits, which needs the room, and 4096 an element at a time)
   // where they give every SM four CTAs, else half of that where they do, else 2048.
-  constexpr int kMany = (KE == 1 ? 16 : GRAD && OVER ? 32 : 64) / KE, kSome = kMany / 2, kFew = 8 / KE;
+  constexpr int kMany = (KE == 1 ? 16 : GRAD && !OVER ? 64 : 32) / KE, kSome = kMany / 2, kFew = 8 / KE;
   const int64_t many = (int64_t)p.N * p.V / (kMany * KE * kAdThreads);
   if (many >= 4 * (int64_t)n_sm) return launch_adjust<T, KE, kMany, GRAD, OVER>(p, st);
   if (2 * many >= 4 * (int64_t)n_sm) return launch_adjust<T, KE, kSome, GRAD, OVER>(p, st);
@@ -395,7 +397,7 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
         embedding_radix_scan_kernel<<<(unsigned)(((1 << c.bits) + 31) / 32), dim3(32, 32), 0, st>>>(r);
         CKL();
       }
-      embedding_radix_move_kernel<<<(unsigned)c.tiles, kEbThreads, 0, st>>>(p, r);
+      embedding_radix_move_kernel<<<(unsigned)c.tiles, kEbMoveThreads, 0, st>>>(p, r);
       CKL();
       r.in = r.out;
     }

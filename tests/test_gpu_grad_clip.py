@@ -75,7 +75,7 @@ def test_types_sizes_and_alignment(t, to, offset):
     check([x.clone() for x in tensors], None, 0.5 * full, 3.0)      # in place
 
 
-@pytest.mark.parametrize("count", [1, 479, 480, 481, 1300])
+@pytest.mark.parametrize("count", [1, 480, 481, 959, 960, 961, 2100])
 def test_lists_longer_than_a_launch(count):
     sizes = [1 + (i * 37) % 900 for i in range(count)]
     tensors = make(sizes, "f32", count)
