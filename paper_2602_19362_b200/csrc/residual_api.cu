@@ -82,8 +82,7 @@ struct ResidualShape {
   int threads, grid, smem;
   int64_t workers;
 };
-static ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int es, bool warp, bool level, int arrays,
-                                    int threads_per_sm) {
+static ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int es, bool warp, bool level, int arrays, int regs) {
   ResidualShape s;
   const int ke = 16 / es, units = (p.d + ke - 1) / ke;
   const bool direct = es == 4 && elems == 32;
@@ -92,8 +91,10 @@ static ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int 
   const int groups = warp ? 8 : 1;
   const size_t row = (size_t)arrays * p.pitch * groups, sink = level ? 0 : (size_t)(s.threads / 32) * 66 * 16;
   const size_t factors = residual_factors(elems, level) == kFactorShared ? (size_t)2 * elems * 4 * (warp ? 32 : s.threads) : 0;
-  int per_sm = threads_per_sm / s.threads;
+  // 65536 registers, handed to warps eight a lane at a time
+  int per_sm = 65536 / ((regs + 7) / 8 * 8 * 32) / (s.threads / 32);
   if (per_sm < 1) per_sm = 1;
+  if (per_sm > 2048 / s.threads) per_sm = 2048 / s.threads;
   // two rows ahead where there is room, and one at least before CTAs are given up
   p.stages = 3;
   auto room = [&] { return (row * p.stages + sink + factors) * per_sm <= kRsSmem; };
@@ -112,29 +113,32 @@ static ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int 
   return s;
 }
 
+// A kernel's registers, with its shared memory allowed, looked up once for each device.
 template <typename F>
-static int residual_smem(F kern, int bytes, bool (&done)[kMaxDevices]) {
-  if (bytes <= 40 * 1024) return OAPL_OK;
+static int residual_registers(F kern, int (&known)[kMaxDevices], int* regs) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return OAPL_ERR_CUDA;
-  if (!done[dev]) {
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) != cudaSuccess)
+  if (!known[dev]) {
+    cudaFuncAttributes fa;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) != cudaSuccess ||
+        cudaFuncGetAttributes(&fa, kern) != cudaSuccess)
       return OAPL_ERR_CUDA;
-    done[dev] = true;
+    known[dev] = fa.numRegs;
   }
+  *regs = known[dev];
   return OAPL_OK;
 }
 
 template <typename T, int E, bool WARP, int NT, bool FWD, bool LEVEL, bool COMMON>
 static int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  static bool done[kMaxDevices] = {false};
+  static int known[kMaxDevices] = {0};
   constexpr int KE = Elem<T>::kN, K = E / KE;
   auto kern = FWD ? residual_fwd_kernel<T, KE, K, WARP, NT, LEVEL, COMMON>
                   : residual_bwd_kernel<T, KE, K, WARP, NT, LEVEL, COMMON>;
-  const ResidualShape s =
-      residual_shape(p, n_sm, E, (int)sizeof(T), WARP, LEVEL, arrays, residual_ctas(FWD, E, NT) * NT);
-  const int rc = residual_smem(kern, s.smem, done);
+  int regs = 0;
+  const int rc = residual_registers(kern, known, &regs);
   if (rc != OAPL_OK) return rc;
+  const ResidualShape s = residual_shape(p, n_sm, E, (int)sizeof(T), WARP, LEVEL, arrays, regs);
   *workers = s.workers;
   kern<<<s.grid, s.threads, s.smem, st>>>(p);
   CKL();
@@ -155,6 +159,7 @@ static int pick_residual(const ResidualParams& p, bool level, int arrays, int n_
 template <typename T, bool FWD>
 static int route_residual(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
   // elements a thread: as few as give a CTA at most 256 threads, 32 beyond that
+  if (p.d <= kRsWarpD / 2) return pick_residual<T, 8, true, 256, FWD>(p, level, arrays, n_sm, workers, st);
   if (p.d <= kRsWarpD) return pick_residual<T, 16, true, 256, FWD>(p, level, arrays, n_sm, workers, st);
   if (p.d <= 2048) return pick_residual<T, 8, false, 256, FWD>(p, level, arrays, n_sm, workers, st);
   if (p.d <= 4096) return pick_residual<T, 16, false, 256, FWD>(p, level, arrays, n_sm, workers, st);
@@ -286,7 +291,7 @@ int oapl_residual_norm_bwd(const oapl_residual* r, const void* x_out, int64_t ld
   j.part = p.part;
   j.d = r->d;
   j.accumulate = accumulate != 0;
-  residual_join_kernel<<<dim3((unsigned)((r->d + 31) / 32), (unsigned)kinds), dim3(32, 8), 0, st>>>(j);
+  residual_join_kernel<<<dim3((unsigned)((r->d + 31) / 32), (unsigned)kinds), dim3(32, kRsShares), 0, st>>>(j);
   CKL();
   return OAPL_OK;
 }

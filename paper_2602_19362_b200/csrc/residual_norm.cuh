@@ -760,28 +760,33 @@ __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual
   }
 }
 
-// Sums of a column over the workers: blockDim = (32 columns, 8 shares of the workers), blockIdx.y the kind.
+// Sums of a column over the workers: blockDim = (32 columns, kRsShares shares of the workers), blockIdx.y the kind.
 struct ResidualJoinParams {
   const float* part;
   int64_t workers;
   int32_t d, accumulate;
   float* out[3];
 };
-__global__ void __launch_bounds__(256) residual_join_kernel(ResidualJoinParams p) {
-  __shared__ float sh[8][33];
+constexpr int kRsShares = 32;
+__global__ void __launch_bounds__(32 * kRsShares) residual_join_kernel(ResidualJoinParams p) {
+  __shared__ float sh[kRsShares][33];
   const int c = (int)blockIdx.x * 32 + (int)threadIdx.x;
   float s = 0.f;
   if (c < p.d) {
     const float* from = p.part + (int64_t)blockIdx.y * p.workers * p.d + c;
 #pragma unroll 8
-    for (int64_t w = threadIdx.y; w < p.workers; w += 8) s += from[w * p.d];
+    for (int64_t w = threadIdx.y; w < p.workers; w += kRsShares) s += from[w * p.d];
   }
   sh[threadIdx.y][threadIdx.x] = s;
   __syncthreads();
-  if (threadIdx.y == 0 && c < p.d) {
-    float v = 0.f;
-    for (int i = 0; i < 8; ++i) v += sh[i][threadIdx.x];
-    float* o = p.out[blockIdx.y] + c;
+  // a warp to a column, a lane to a share
+  const int col = threadIdx.y;
+  float v = sh[threadIdx.x][col];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  const int at = (int)blockIdx.x * 32 + col;
+  if (threadIdx.x == 0 && at < p.d) {
+    float* o = (blockIdx.y == 0 ? p.out[0] : blockIdx.y == 1 ? p.out[1] : p.out[2]) + at;
     *o = p.accumulate ? *o + v : v;
   }
 }
