@@ -10,9 +10,10 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liboapl.so")
-SOURCES = ["oapl_api.cu", "step_api.cu", "residual_api.cu"]
-DEPS = ["oapl_api.cu", "gemm_sm100.cuh", "small_kernels.cuh", "sm100_ptx.cuh", "sweep_schedule.cuh", "adamw.cuh",
-        "logits_ops.cuh", "quantize.cuh", "scaled_matmul.cuh", "step_api.cu", "residual_api.cu", "elements.cuh", "host_common.cuh",
+SOURCES = ["oapl_api.cu", "step_api.cu", "residual_api.cu", "residual_bwd_bf16.cu", "residual_bwd_f16.cu",
+           "residual_bwd_f32.cu"]
+DEPS = [*SOURCES, "gemm_sm100.cuh", "small_kernels.cuh", "sm100_ptx.cuh", "sweep_schedule.cuh", "adamw.cuh",
+        "logits_ops.cuh", "quantize.cuh", "scaled_matmul.cuh", "residual_host.cuh", "elements.cuh", "host_common.cuh",
         "embedding.cuh", "residual_norm.cuh", "grad_clip.cuh", "logits_adjust.cuh",
         os.path.join("..", "..", "include", "oapl.h")]
 
@@ -45,15 +46,20 @@ def _stale() -> bool:
 
 def _run(commands: list, verbose: bool) -> str:
     """Run the commands side by side; what they reported, one after the other.  Raises if one of them fails."""
-    running = [subprocess.Popen(c, stderr=subprocess.PIPE, text=True) for c in commands]
-    logs = [p.communicate()[1] for p in running]
-    for p, c, log in zip(running, commands, logs):
-        if verbose or p.returncode:
-            sys.stderr.write(log)
-    for p, c in zip(running, commands):
-        if p.returncode:
-            raise subprocess.CalledProcessError(p.returncode, c)
-    return "".join(logs)
+    logs = [tempfile.TemporaryFile("w+") for _ in commands]      # not pipes, which would fill up unread
+    running = [subprocess.Popen(c, stderr=f) for c, f in zip(commands, logs)]
+    codes = [p.wait() for p in running]
+    texts = []
+    for f, code in zip(logs, codes):
+        f.seek(0)
+        texts.append(f.read())
+        f.close()
+        if verbose or code:
+            sys.stderr.write(texts[-1])
+    for c, code in zip(commands, codes):
+        if code:
+            raise subprocess.CalledProcessError(code, c)
+    return "".join(texts)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -4,14 +4,9 @@
 #include <cmath>
 #include <cstring>
 
-#include "host_common.cuh"
-#include "residual_norm.cuh"
+#include "residual_host.cuh"
 
 namespace oapl {
-
-constexpr int kRsWarpD = 512;          // rows of a warp: 16 elements a lane
-constexpr int64_t kRsWarpWorkers = 8192, kRsCtaWorkers = 1024;
-constexpr size_t kRsSmem = 200 * 1024; // shared memory of an SM that rows on their way may take
 
 static int64_t residual_workers(int64_t N, int32_t d) {
   const int64_t most = d <= kRsWarpD ? kRsWarpWorkers : kRsCtaWorkers;
@@ -76,106 +71,18 @@ static bool residual_level(const ResidualParams& p, int es, const Place* m, int 
   return on16(p.w_post) && on16(p.w_pre) && (p.gate_kind != OAPL_GATE_COLUMN || on16(p.gate));
 }
 
-// The launch: threads of a row, rows in flight, CTAs of an SM (per_sm, from the registers; fewer where shared memory asks
-// for it) and workers, each with rows of its own.
-struct ResidualShape {
-  int threads, grid, smem;
-  int64_t workers;
-};
-static ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int es, bool warp, bool level, int arrays, int regs) {
-  ResidualShape s;
-  const int ke = 16 / es, units = (p.d + ke - 1) / ke;
-  const bool direct = es == 4 && elems == 32;
-  p.pitch = (int32_t)(direct ? 0 : level ? units * 16 : (p.d * es + 15) / 16 * 16 + 16);
-  s.threads = warp ? 256 : (int)round_up((size_t)((units + elems / ke - 1) / (elems / ke)), 32);
-  const int groups = warp ? 8 : 1;
-  const size_t row = (size_t)arrays * p.pitch * groups, sink = level ? 0 : (size_t)(s.threads / 32) * 66 * 16;
-  const size_t factors = residual_factors(elems, level) == kFactorShared ? (size_t)2 * elems * 4 * (warp ? 32 : s.threads) : 0;
-  // 65536 registers, handed to warps eight a lane at a time
-  int per_sm = 65536 / ((regs + 7) / 8 * 8 * 32) / (s.threads / 32);
-  if (per_sm < 1) per_sm = 1;
-  if (per_sm > 2048 / s.threads) per_sm = 2048 / s.threads;
-  // two rows ahead where there is room, and one at least before CTAs are given up
-  p.stages = 3;
-  auto room = [&] { return (row * p.stages + sink + factors) * per_sm <= kRsSmem; };
-  while (p.stages > 2 && !room()) --p.stages;
-  while (per_sm > 1 && !room()) --per_sm;
-  while (p.stages > 1 && !room()) --p.stages;
-  int64_t grid = (p.N + groups - 1) / groups;
-  if (grid > (int64_t)n_sm * per_sm) grid = (int64_t)n_sm * per_sm;
-  const int64_t most = (warp ? kRsWarpWorkers : kRsCtaWorkers) / groups;
-  if (grid > most) grid = most;
-  s.grid = (int)grid;
-  s.workers = grid * groups;
-  p.sink = (int32_t)(row * p.stages);
-  p.factors = (int32_t)(row * p.stages + sink);
-  s.smem = (int)(row * p.stages + sink + factors);
-  return s;
+static int residual_fwd(const ResidualParams& p, int32_t type, bool level, int arrays, int n_sm, cudaStream_t st) {
+  int64_t workers = 0;
+  if (type == OAPL_TYPE_BF16) return route_residual_level<__nv_bfloat16, true>(p, level, arrays, n_sm, &workers, st);
+  if (type == OAPL_TYPE_F16) return route_residual_level<__half, true>(p, level, arrays, n_sm, &workers, st);
+  return route_residual_level<float, true>(p, level, arrays, n_sm, &workers, st);
 }
 
-// A kernel's registers, with its shared memory allowed, looked up once for each device.
-template <typename F>
-static int residual_registers(F kern, int (&known)[kMaxDevices], int* regs) {
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return OAPL_ERR_CUDA;
-  if (!known[dev]) {
-    cudaFuncAttributes fa;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024) != cudaSuccess ||
-        cudaFuncGetAttributes(&fa, kern) != cudaSuccess)
-      return OAPL_ERR_CUDA;
-    known[dev] = fa.numRegs;
-  }
-  *regs = known[dev];
-  return OAPL_OK;
-}
-
-template <typename T, int E, bool WARP, int NT, bool FWD, bool LEVEL, bool COMMON>
-static int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  static int known[kMaxDevices] = {0};
-  constexpr int KE = Elem<T>::kN, K = E / KE;
-  auto kern = FWD ? residual_fwd_kernel<T, KE, K, WARP, NT, LEVEL, COMMON>
-                  : residual_bwd_kernel<T, KE, K, WARP, NT, LEVEL, COMMON>;
-  int regs = 0;
-  const int rc = residual_registers(kern, known, &regs);
-  if (rc != OAPL_OK) return rc;
-  const ResidualShape s = residual_shape(p, n_sm, E, (int)sizeof(T), WARP, LEVEL, arrays, regs);
-  *workers = s.workers;
-  kern<<<s.grid, s.threads, s.smem, st>>>(p);
-  CKL();
-  return OAPL_OK;
-}
-
-template <typename T, int E, bool WARP, int NT, bool FWD>
-static int pick_residual(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  const bool common = p.y && p.w_post && p.w_pre && p.gate_kind != kGateFull && p.x_out &&
-                      (FWD || (p.dx_out && p.dx && p.dy));
-  if (level)
-    return common ? launch_residual<T, E, WARP, NT, FWD, true, true>(p, arrays, n_sm, workers, st)
-                  : launch_residual<T, E, WARP, NT, FWD, true, false>(p, arrays, n_sm, workers, st);
-  return common ? launch_residual<T, E, WARP, NT, FWD, false, true>(p, arrays, n_sm, workers, st)
-                : launch_residual<T, E, WARP, NT, FWD, false, false>(p, arrays, n_sm, workers, st);
-}
-
-template <typename T, bool FWD>
-static int route_residual(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  // elements a thread: as few as give a CTA at most 256 threads, 32 beyond that
-  if (p.d <= kRsWarpD / 2) return pick_residual<T, 8, true, 256, FWD>(p, level, arrays, n_sm, workers, st);
-  if (p.d <= kRsWarpD) return pick_residual<T, 16, true, 256, FWD>(p, level, arrays, n_sm, workers, st);
-  if (p.d <= 2048) return pick_residual<T, 8, false, 256, FWD>(p, level, arrays, n_sm, workers, st);
-  if (p.d <= 4096) return pick_residual<T, 16, false, 256, FWD>(p, level, arrays, n_sm, workers, st);
-  // (fp32 rows off 16-byte boundaries have no room beside their factors where there are five arrays of them)
-  const bool room = level || (size_t)arrays * p.d * sizeof(T) + (size_t)8 * p.d <= kRsSmem;
-  if (p.d <= 8192 && room) return pick_residual<T, 16, false, 512, FWD>(p, level, arrays, n_sm, workers, st);
-  // fp32 rows are read where they are
-  return pick_residual<T, 32, false, 512, FWD>(p, level && sizeof(T) == 2, arrays, n_sm, workers, st);
-}
-
-template <bool FWD>
-static int route_residual_type(const ResidualParams& p, int32_t type, bool level, int arrays, int n_sm, int64_t* workers,
-                               cudaStream_t st) {
-  if (type == OAPL_TYPE_BF16) return route_residual<__nv_bfloat16, FWD>(p, level, arrays, n_sm, workers, st);
-  if (type == OAPL_TYPE_F16) return route_residual<__half, FWD>(p, level, arrays, n_sm, workers, st);
-  return route_residual<float, FWD>(p, level, arrays, n_sm, workers, st);
+static int residual_bwd(const ResidualParams& p, int32_t type, bool level, int arrays, int n_sm, int64_t* workers,
+                        cudaStream_t st) {
+  if (type == OAPL_TYPE_BF16) return residual_bwd_bf16(p, level, arrays, n_sm, workers, st);
+  if (type == OAPL_TYPE_F16) return residual_bwd_f16(p, level, arrays, n_sm, workers, st);
+  return residual_bwd_f32(p, level, arrays, n_sm, workers, st);
 }
 
 }  // namespace oapl
@@ -210,11 +117,9 @@ int oapl_residual_norm(const oapl_residual* r, void* x_out, int64_t ld_x_out, vo
   p.ld_h = ld_h;
   p.rstd_post = rstd_post;
   p.rstd_pre = rstd_pre;
-  int64_t workers = 0;
   const int arrays = 1 + (r->y != nullptr) + full;
   const bool level = residual_level(p, es, m, 5);
-  return route_residual_type<true>(p, r->type, level, arrays, n_sm, &workers,
-                                   static_cast<cudaStream_t>(stream));
+  return residual_fwd(p, r->type, level, arrays, n_sm, static_cast<cudaStream_t>(stream));
 }
 
 size_t oapl_residual_norm_workspace_bytes(int64_t N, int32_t d) {
@@ -286,7 +191,7 @@ int oapl_residual_norm_bwd(const oapl_residual* r, const void* x_out, int64_t ld
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int arrays = 2 * pre + (dx_out != nullptr) + (r->y != nullptr) + full;
   const bool level = residual_level(p, es, m, 8);
-  const int run = route_residual_type<false>(p, r->type, level, arrays, n_sm, &j.workers, st);
+  const int run = residual_bwd(p, r->type, level, arrays, n_sm, &j.workers, st);
   if (run != OAPL_OK || !kinds) return run;
   j.part = p.part;
   j.d = r->d;

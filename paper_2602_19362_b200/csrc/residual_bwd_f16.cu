@@ -1,0 +1,10 @@
+// The kernels of the residual norm's gradient for rows of f16.
+#include "residual_host.cuh"
+
+namespace oapl {
+
+int residual_bwd_f16(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
+  return route_residual_level<__half, false>(p, level, arrays, n_sm, workers, st);
+}
+
+}  // namespace oapl

@@ -453,17 +453,20 @@ constexpr int residual_ctas(bool forward, int elems, int nt) {
   return nt > 256 ? 1 : forward ? (elems == 8 ? 4 : 3) : (elems == 8 ? 3 : 2);
 }
 
-// What a call has.  COMMON: the form that blocks with both norms have, known when the kernel is compiled (16384 x 3584
-// bf16, gradient: %COMMON%).
-template <bool COMMON>
+// What a call has.  Blocks as they are come in four forms, all with y, w_pre, dx' and every result: with or without w_post,
+// with a gate per element or without.  Kernels that know theirs when they are compiled have no branches for the rest, and
+// registers for all they need (16384 x 3584 bf16, gradient: %FORMS% against what kFormAny takes).
+enum { kFormAny = 0, kFormPost = 1, kFormPlain = 2, kFormPostFull = 3, kFormFull = 4 };
+template <int FORM>
 struct ResidualHas {
   bool y, post, pre, full, dx_out;
   __device__ __forceinline__ explicit ResidualHas(const ResidualParams& p) {
-    y = COMMON || p.y != nullptr;
-    post = COMMON || p.w_post != nullptr;
-    pre = COMMON || p.w_pre != nullptr;
-    full = !COMMON && p.gate_kind == kGateFull;
-    dx_out = COMMON || p.dx_out != nullptr;
+    constexpr bool kAny = FORM == kFormAny;
+    y = !kAny || p.y != nullptr;
+    post = kAny ? p.w_post != nullptr : FORM == kFormPost || FORM == kFormPostFull;
+    pre = !kAny || p.w_pre != nullptr;
+    full = kAny ? p.gate_kind == kGateFull : FORM == kFormPostFull || FORM == kFormFull;
+    dx_out = !kAny || p.dx_out != nullptr;
   }
 };
 
@@ -497,11 +500,11 @@ __device__ __forceinline__ void form_y(const ResidualParams& p, bool post, int c
 }
 
 // ------------------------------------------------------------------------------------------------ forward
-template <typename T, int KE, int K, bool WARP, int NT, bool LEVEL, bool COMMON>
+template <typename T, int KE, int K, bool WARP, int NT, bool LEVEL, int FORM>
 __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_fwd_kernel(ResidualParams p) {
   __shared__ __align__(512) float red[kRsRedFloats];
   RowGroup<WARP> grp(red);
-  const ResidualHas<COMMON> has(p);
+  const ResidualHas<FORM> has(p);
   RowFeed<T, KE, K, LEVEL> feed;
   feed.init(p, 1 + has.y + has.full, grp);
   feed.array(0, p.x, p.ld_x, grp);
@@ -566,7 +569,7 @@ __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_
         }
         v_dot(ss, v[k], v[k]);
       }
-      if (COMMON || p.x_out) sink.put(x_out, k, v[k]);
+      if (FORM != kFormAny || p.x_out) sink.put(x_out, k, v[k]);
     }
     if (has.pre) {
       const float r = 1.f / sqrtf(fmaf(grp.sum(ss.x + ss.y), inv_d, p.eps));
@@ -591,11 +594,11 @@ __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_
 // ------------------------------------------------------------------------------------------------ gradient
 // Of a column only two sums are needed: dw_pre, and S = sum_n t yh (times a row's or an element's gate).  Without these
 // gates dw_post = b g S and dg = b w_post S, both per channel; with them dw_post = b S.
-template <typename T, int KE, int K, bool WARP, int NT, bool LEVEL, bool COMMON>
+template <typename T, int KE, int K, bool WARP, int NT, bool LEVEL, int FORM>
 __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual_bwd_kernel(ResidualParams p) {
   __shared__ __align__(512) float red[kRsRedFloats];
   RowGroup<WARP> grp(red);
-  const ResidualHas<COMMON> has(p);
+  const ResidualHas<FORM> has(p);
   // the arrays of a stage, in this order, those that there are
   const int i_dx = has.pre ? 2 : 0, i_y = i_dx + has.dx_out, i_g = i_y + has.y;
   RowFeed<T, KE, K, LEVEL> feed;
@@ -694,7 +697,7 @@ __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual
           v_fma(c[k], xo, m1x, c[k]);
         }
         v_mul(o_dx, c[k], p.a);
-        if (LEVEL && (COMMON || p.dx)) sink.put(dx, k, o_dx);
+        if (LEVEL && (FORM != kFormAny || p.dx)) sink.put(dx, k, o_dx);
         if (has.y) {
           float y[KE];
           feed.read(at_y, k, y);
@@ -713,11 +716,11 @@ __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual
           }
           v_mul(o, o, e_row);
           if (has.post) v_fma(o, y, m2y, o);
-          if (LEVEL && (COMMON || p.dy)) sink.put(dy, k, o);
+          if (LEVEL && (FORM != kFormAny || p.dy)) sink.put(dy, k, o);
         }
       }
-      if (!LEVEL && (COMMON || p.dx)) sink.put(dx, k, o_dx);
-      if (!LEVEL && (COMMON || p.dy)) sink.put(dy, k, o);
+      if (!LEVEL && (FORM != kFormAny || p.dx)) sink.put(dx, k, o_dx);
+      if (!LEVEL && (FORM != kFormAny || p.dy)) sink.put(dy, k, o);
       if (has.full && p.dgate) sink.put(static_cast<T*>(p.dgate) + row * p.ld_dg, k, o_dg);
     }
     dx += grp.step * p.ld_dx;
@@ -768,7 +771,7 @@ struct ResidualJoinParams {
   float* out[3];
 };
 constexpr int kRsShares = 32;
-__global__ void __launch_bounds__(32 * kRsShares) residual_join_kernel(ResidualJoinParams p) {
+static __global__ void __launch_bounds__(32 * kRsShares) residual_join_kernel(ResidualJoinParams p) {
   __shared__ float sh[kRsShares][33];
   const int c = (int)blockIdx.x * 32 + (int)threadIdx.x;
   float s = 0.f;
