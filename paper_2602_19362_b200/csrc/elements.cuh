@@ -35,6 +35,13 @@ __device__ __forceinline__ uint32_t load_here(const uint32_t* p) {
   return v;
 }
 
+// A launch that follows another one of the same call may begin before that one has ended (host_common.cuh, launch_next):
+// it waits here before it touches memory, and lets the launch behind it begin in turn.
+__device__ __forceinline__ void after_launch_before() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Copies to shared memory that need no register.
 __device__ __forceinline__ void copy_async_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");

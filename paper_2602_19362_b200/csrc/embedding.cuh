@@ -161,6 +161,7 @@ __global__ void __launch_bounds__(kEbThreads) embedding_kernel(LookupParams p) {
 constexpr int kEbCountRows = 4;
 __global__ void __launch_bounds__(kEbThreads) embedding_count_sort_kernel(LookupParams p) {
   __shared__ uint32_t keys[kEbCountMax];
+  after_launch_before();
   const int N = (int)p.N, lane = threadIdx.x & 31;
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.joins = 0;
 #pragma unroll 8
@@ -221,6 +222,7 @@ __device__ __forceinline__ uint2 radix_load(const LookupParams& p, const RadixPa
 // The digits of the first pass, counted by tile.
 __global__ void __launch_bounds__(kEbThreads) embedding_radix_count_kernel(LookupParams p, RadixParams r) {
   __shared__ uint32_t h[1 << kEbMaxBits];
+  after_launch_before();
   const int bins = 1 << r.bits;
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.joins = 0;
   const int64_t n0 = (int64_t)blockIdx.x * kEbTile + threadIdx.x;
@@ -247,6 +249,7 @@ __global__ void __launch_bounds__(kEbThreads) embedding_radix_count_kernel(Looku
 // Many tiles: exclusive prefix sums of 32 digits over the tiles, 32 threads to a digit.
 __global__ void __launch_bounds__(1024) embedding_radix_scan_kernel(RadixParams r) {
   __shared__ uint32_t sh[32][33];
+  after_launch_before();
   const int bins = 1 << r.bits, bin = (int)blockIdx.x * 32 + (int)threadIdx.x, g = threadIdx.y;
   const int per = (r.tiles + 31) / 32, t0 = g * per, t1 = t0 + per < r.tiles ? t0 + per : r.tiles;
   uint32_t* h = r.hist + bin;
@@ -281,6 +284,7 @@ __global__ void __launch_bounds__(kEbMoveThreads) embedding_radix_move_kernel(Lo
   __shared__ uint32_t at[1 << kEbMaxBits], total[1 << kEbMaxBits];  // first place of a digit of this tile, and all of it
   __shared__ uint16_t cnt[kWarps][1 << kEbMaxBits];
   __shared__ uint32_t wsum[kWarps];
+  after_launch_before();
   const int bins = 1 << r.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t n0 = (int64_t)blockIdx.x * kEbTile + warp * 32 * kRounds + lane;
   uint2 e[kRounds];
@@ -412,6 +416,7 @@ __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams 
   constexpr int kAhead = KE == 1 ? 16 : 8;  // rows whose loads are in flight together
   __shared__ uint2 e[kEbMaxChunk];
   __shared__ uint32_t live;
+  after_launch_before();
   const int slab = (int)(blockIdx.x % (unsigned)p.slabs);
   const int64_t item = blockIdx.x / (unsigned)p.slabs;
   const int c = (slab * (int)blockDim.x + (int)threadIdx.x) * KE;
@@ -495,6 +500,7 @@ __global__ void __launch_bounds__(kEbJoinCols * kEbJoinShares) embedding_join_ke
   __shared__ float sh[kEbJoinShares][kEbJoinCols * KE];
   __shared__ __align__(16) float ring[kAhead][kEbJoinCols * kEbJoinShares * KE];  // each thread's own places
   const int mine = ((int)threadIdx.y * kEbJoinCols + (int)threadIdx.x) * KE;
+  after_launch_before();
   const uint32_t slabs = (uint32_t)p.slabs, items = *p.joins * slabs;
   for (uint32_t w = blockIdx.x; w < items; w += gridDim.x) {
     const int64_t item = p.joins[1 + w / slabs];

@@ -107,6 +107,7 @@ __device__ __forceinline__ void grad_fetch(const GradList& l, int c, int& k, Gra
 }
 __global__ void __launch_bounds__(kGcThreads, 4) grad_norm_kernel(const __grid_constant__ GradList l, double* part) {
   __shared__ double sh[kGcThreads / 32];
+  after_launch_before();
   double s = 0.0;
   int k = grad_find(l, (int)blockIdx.x);
   GradShare now, next;
@@ -133,6 +134,7 @@ __global__ void __launch_bounds__(kGcThreads, 4) grad_norm_kernel(const __grid_c
 __global__ void __launch_bounds__(kGcThreads) grad_norm_join_kernel(const double* part, int n, float scale, float* sq_norm,
                                                                     float* norm, int32_t* status) {
   __shared__ double sh[kGcThreads / 32];
+  after_launch_before();
   double s = 0.0;
 #pragma unroll 4
   for (int i = threadIdx.x; i < n; i += kGcThreads) s += part[i];

@@ -5,6 +5,7 @@
 
 #include <atomic>
 #include <cstdint>
+#include <utility>
 
 #include "../../include/oapl.h"
 
@@ -24,6 +25,26 @@ constexpr int kMaxDevices = 64;  // per-device host-side caches
     OAPL_LAUNCHED();                                           \
     if (cudaGetLastError() != cudaSuccess) return OAPL_ERR_CUDA; \
   } while (0)
+
+// The next launch of a call whose kernels begin with after_launch_before(): its start-up goes under the end of the launch
+// before it.
+template <typename... P, typename... A>
+inline cudaError_t launch_next(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  const cudaError_t rc = cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
+  if (rc != cudaSuccess) (void)cudaGetLastError();
+  OAPL_LAUNCHED();
+  return rc;
+}
 
 inline int sm_count() {
   static int n[kMaxDevices] = {0};

@@ -196,8 +196,7 @@ int oapl_residual_norm_bwd(const oapl_residual* r, const void* x_out, int64_t ld
   j.part = p.part;
   j.d = r->d;
   j.accumulate = accumulate != 0;
-  residual_join_kernel<<<dim3((unsigned)((r->d + 31) / 32), (unsigned)kinds), dim3(32, kRsShares), 0, st>>>(j);
-  CKL();
+  CK(launch_next(residual_join_kernel, dim3((unsigned)((r->d + 31) / 32), (unsigned)kinds), dim3(32, kRsShares), 0, st, j));
   return OAPL_OK;
 }
 

@@ -597,6 +597,7 @@ __global__ void __launch_bounds__(NT, residual_ctas(true, KE * K, NT)) residual_
 template <typename T, int KE, int K, bool WARP, int NT, bool LEVEL, int FORM>
 __global__ void __launch_bounds__(NT, residual_ctas(false, KE * K, NT)) residual_bwd_kernel(ResidualParams p) {
   __shared__ __align__(512) float red[kRsRedFloats];
+  after_launch_before();
   RowGroup<WARP> grp(red);
   const ResidualHas<FORM> has(p);
   // the arrays of a stage, in this order, those that there are
@@ -773,6 +774,7 @@ struct ResidualJoinParams {
 constexpr int kRsShares = 32;
 static __global__ void __launch_bounds__(32 * kRsShares) residual_join_kernel(ResidualJoinParams p) {
   __shared__ float sh[kRsShares][33];
+  after_launch_before();
   const int c = (int)blockIdx.x * 32 + (int)threadIdx.x;
   float s = 0.f;
   if (c < p.d) {

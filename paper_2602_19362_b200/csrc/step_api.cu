@@ -114,16 +114,15 @@ static int launch_embedding_sum(LookupParams p, int n_sm, cudaStream_t st) {
   const int64_t zero = p.accumulate ? 0 : ((int64_t)p.V + kEbZeroRows - 1) / kEbZeroRows;
   if (p.chunks * slabs + zero > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
   p.slabs = (int32_t)slabs;
-  embedding_sum_kernel<T, KE><<<(unsigned)(p.chunks * slabs + zero), threads, 0, st>>>(p);
-  CKL();
+  CK(launch_next(embedding_sum_kernel<T, KE>, dim3((unsigned)(p.chunks * slabs + zero)), dim3(threads), 0, st, p));
   if (p.chunks > 1) {
     constexpr int JE = KE > 4 ? 4 : KE;
     p.slabs = (int32_t)((p.d / JE + kEbJoinCols - 1) / kEbJoinCols);
     const int64_t most = (int64_t)p.chunks * p.slabs;
     if (most > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
     const int64_t grid = 8 * (int64_t)n_sm;  // how many there are, the device knows
-    embedding_join_kernel<JE><<<(unsigned)(most < grid ? most : grid), dim3(kEbJoinCols, kEbJoinShares), 0, st>>>(p);
-    CKL();
+    CK(launch_next(embedding_join_kernel<JE>, dim3((unsigned)(most < grid ? most : grid)),
+                   dim3(kEbJoinCols, kEbJoinShares), 0, st, p));
   }
   return OAPL_OK;
 }
@@ -394,11 +393,9 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
       r.shift = k * c.bits;
       r.out = lists[(c.passes - 1 - k) & 1];  // the last pass into `sorted`
       if (r.scanned) {
-        embedding_radix_scan_kernel<<<(unsigned)(((1 << c.bits) + 31) / 32), dim3(32, 32), 0, st>>>(r);
-        CKL();
+        CK(launch_next(embedding_radix_scan_kernel, dim3((unsigned)(((1 << c.bits) + 31) / 32)), dim3(32, 32), 0, st, r));
       }
-      embedding_radix_move_kernel<<<(unsigned)c.tiles, kEbMoveThreads, 0, st>>>(p, r);
-      CKL();
+      CK(launch_next(embedding_radix_move_kernel, dim3((unsigned)c.tiles), dim3(kEbMoveThreads), 0, st, p, r));
       r.in = r.out;
     }
   }
@@ -433,8 +430,8 @@ int oapl_grad_norm(const oapl_tensor* tensors, int32_t count, float scale, float
     CKL();
     sums += grid;
   }
-  grad_norm_join_kernel<<<1, kGcThreads, 0, st>>>(part, sums, scale, sq_norm, norm, device_status);
-  CKL();
+  CK(launch_next(grad_norm_join_kernel, dim3(1), dim3(kGcThreads), 0, st, (const double*)part, sums, scale, sq_norm, norm,
+                 device_status));
   return OAPL_OK;
 }
 
