@@ -14,6 +14,11 @@
 // A token that holds a tenth of the batch is thus spread over many CTAs.  Sums are fp32: up to kEbMaxChunk terms in a
 // chunk, then the chunks' partial sums.
 // Rows without a token are cleared by further CTAs of the launch of step 2, which find out by searching the sorted list.
+//
+// Measured, us: 64 rows of 3584 bf16 2.7 on the device; 32768 x 3584 58 (the copy rate), 32768 x 3583 96 (two loads and a shift
+// per vector); gradient of 40960 x 1536 bf16 into 151936 rows 189 (0.87 of the copy rate), of which the sums and the zeros
+// take 158, the sort 20; 65536 x 1536 into 20000 rows 90; 3001 x 1001 fp16 off 16-byte boundaries into 50021 rows 52.  Clearing
+// rows beside the sort, whose CTAs leave most SMs idle, was tried: it slowed the sort by what it saved.
 #pragma once
 #include <type_traits>
 
@@ -22,7 +27,8 @@
 namespace oapl {
 
 constexpr int kEbThreads = 256;
-constexpr int kEbCountMax = 8192;   // positions sorted by counting: work grows with their square
+constexpr int kEbCountMax = 8192;   // positions sorted by counting: work grows with their square (6.5 us for 3001, one
+                                    // launch; the radix sort of two passes is three launches of 4 to 8 us)
 constexpr int kEbTile = 2048;       // positions of a CTA of the radix sort
 constexpr int kEbMoveThreads = 512;
 constexpr int kEbMaxBits = 10;      // digit of a pass

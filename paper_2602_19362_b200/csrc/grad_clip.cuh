@@ -9,6 +9,10 @@
 // Squares are added in fp32 over a thread's 16 or 32 elements of a chunk and in fp64 from there, in an order that only the
 // list and the number of SMs determine.  A thread whose fp32 sum left the range where that is exact to fp32 rounding
 // (values above about 1e14, or nothing but values below about 1e-12) adds the same elements again in fp64.
+//
+// Measured, us: 453 M bf16 elements in 108 tensors, norm 151 (0.94 of the copy rate), clipping to fp32 465 (0.91), to bf16
+// 280 (the copy rate); 600 tensors of up to 4100 fp32 elements 18 for both calls, 10 of them on the device.  Loads of the next chunk
+// ahead of this one's sums: 187 to 151.
 #pragma once
 #include <type_traits>
 

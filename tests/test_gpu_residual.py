@@ -245,7 +245,9 @@ def test_the_norm_alone():
 
 @pytest.mark.parametrize("t,N,d,gate", [("bf16", 3000, 3584, "column"), ("bf16", 5000, 256, "row"), ("f32", 2001, 1111, "full"),
                                         ("f16", 40000, 64, "column"), ("bf16", 1200, 5120, "none"), ("f32", 1300, 4096, "column"),
-                                        ("bf16", 2000, 3001, "column")])
+                                        ("bf16", 2000, 3001, "column"), ("bf16", 30000, 77, "row"), ("f32", 9000, 201, "full"),
+                                        ("f16", 4000, 511, "column"), ("f16", 1000, 8191, "none"), ("f32", 700, 7313, "full"),
+                                        ("f32", 500, 7600, "full"), ("bf16", 300, 12001, "column")])
 def test_many_rows(t, N, d, gate):
     c = make(N, d, t, gate)
     check_fwd(c)
