@@ -283,13 +283,17 @@ struct RowFeed {
     } else {
       const int have = d - (t + k * nt) * KE;  // elements from here to the row's end, at least one
       const uint4 lo = q.p[k * nt];
-      uint4 hi = lo;
-      if constexpr (kDirect) {  // memory behind the row's last block may be nobody's
-        if (q.off + (uint32_t)(have < KE ? have : KE) * (uint32_t)sizeof(T) > 16u) hi = q.p[k * nt + 1];
+      if (q.off == 0) {  // the same for all threads
+        Elem<T>::widen(lo, f);
       } else {
-        hi = q.p[k * nt + 1];
+        uint4 hi = lo;
+        if constexpr (kDirect) {  // memory behind the row's last block may be nobody's
+          if (q.off + (uint32_t)(have < KE ? have : KE) * (uint32_t)sizeof(T) > 16u) hi = q.p[k * nt + 1];
+        } else {
+          hi = q.p[k * nt + 1];
+        }
+        Elem<T>::widen(shift_16(lo, hi, q.off), f);
       }
-      Elem<T>::widen(shift_16(lo, hi, q.off), f);
       if (have < KE) {
 #pragma unroll
         for (int i = 0; i < KE; ++i)
@@ -318,12 +322,24 @@ struct RowSink {
       int n = d - first;
       if (n <= 0) return;
       n = n < 32 * KE ? n : 32 * KE;
+      T* to = row + first;
+      // elements before the first boundary, the same for all units of a row
+      int head = (int)(-(reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (KE - 1));
+      if (head == 0) {
+        const int have = n - lane * KE;
+        if (have >= KE) {
+          Raw<T, KE>::store(to + lane * KE, o);
+        } else {
+#pragma unroll
+          for (int i = 0; i < KE; ++i)
+            if (i < have) Elem<T>::put(to, lane * KE + i, o[i]);
+        }
+        return;
+      }
       uint4* b = buf + turn * 33;
       turn ^= 1;
       b[lane] = Elem<T>::narrow(o);
       __syncwarp();
-      T* to = row + first;
-      int head = (int)(-(reinterpret_cast<uintptr_t>(to) / sizeof(T)) & (KE - 1));
       head = head < n ? head : n;
       const int blocks = (n - head) / KE;
       if (lane < blocks)
