@@ -14,6 +14,8 @@
 // A token that holds a tenth of the batch is thus spread over many CTAs.  Sums are fp32: up to kEbMaxChunk terms in a
 // chunk, then the chunks' partial sums.
 // Rows without a token are cleared by further CTAs of the launch of step 2, which find out by searching the sorted list.
+// Batches of up to kEbFew positions take one launch: a CTA for each position, which ends when the token has occurred before
+// and otherwise finds its other positions and adds up their rows.
 //
 // Measured, us: 64 rows of 3584 bf16 2.7 on the device; 32768 x 3584 58 (the copy rate), 32768 x 3583 96 (two loads and a shift
 // per vector); gradient of 40960 x 1536 bf16 into 151936 rows 189 (0.87 of the copy rate), of which the sums and the zeros
@@ -33,7 +35,8 @@ constexpr int kEbTile = 2048;       // positions of a CTA of the radix sort
 constexpr int kEbMoveThreads = 512;
 constexpr int kEbMaxBits = 10;      // digit of a pass
 constexpr int kEbMinChunk = 32, kEbMaxChunk = 256;
-constexpr int kEbZeroRows = 32;     // rows of the table of a CTA that clears
+constexpr int kEbMaxZeroRows = 32;  // rows of the table of a CTA that clears
+constexpr int kEbFew = 1024;        // positions of the single launch
 constexpr int kErrBadId = -5;       // OAPL_ERR_BAD_TARGET
 
 struct LookupParams {
@@ -50,7 +53,7 @@ struct LookupParams {
   // gradient
   uint2* sorted;   // (token, position); tokens of rows that do not count are V
   float* part;     // [chunks][2][d]: sums of a chunk's first run, when it came from before, and of its last one
-  int32_t chunk, chunks, slabs;
+  int32_t chunk, chunks, slabs, zero_rows;
   int32_t accumulate;
   uint32_t* joins; // chunks whose last run reaches further: how many, then which
 };
@@ -65,15 +68,15 @@ __device__ __forceinline__ void lookup_check(const LookupParams& p, int64_t n) {
   if (p.status && !(p.mask && !p.mask[n]) && (uint32_t)p.ids[n] >= (uint32_t)p.V) atomicCAS(p.status, 0, kErrBadId);
 }
 
-// Clears a row of the table's gradient, by a whole CTA.
-__device__ __forceinline__ void clear_row(const LookupParams& p, int64_t v) {
+// Clears a row of the table's gradient, by all `threads` of a CTA.
+__device__ __forceinline__ void clear_row(const LookupParams& p, int64_t v, int t, int threads) {
   float* row = static_cast<float*>(p.out) + v * p.ld_out;
   // up to the first 16-byte boundary, vectors, and the rest
   int head = (int)(-(reinterpret_cast<uintptr_t>(row) >> 2) & 3);
   head = head < p.d ? head : p.d;
-  const int vecs = (p.d - head) / 4, tail = (p.d - head) % 4, t = threadIdx.x;
+  const int vecs = (p.d - head) / 4, tail = (p.d - head) % 4;
   float4* body = reinterpret_cast<float4*>(row + head);
-  for (int i = t; i < vecs; i += blockDim.x) body[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = t; i < vecs; i += threads) body[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   if (t < head) row[t] = 0.f;
   else if (t < head + tail) row[vecs * 4 + t] = 0.f;
 }
@@ -389,14 +392,30 @@ __global__ void __launch_bounds__(kEbMoveThreads) embedding_radix_move_kernel(Lo
 }
 
 // ------------------------------------------------------------------------------------------------ sums
-// First place in the sorted list whose token is at least `key`.
-__device__ __forceinline__ int64_t sorted_lower(const uint2* s, int64_t n, uint32_t key) {
-  int64_t lo = 0, hi = n;
+// Which of the `rows` tokens from v0 on are in the sorted list, a bit each; for a whole warp.  Each half of the warp finds
+// one end of their places, 16 probes at a time, and then each lane its token between the two.
+__device__ __forceinline__ uint32_t sorted_has(const uint2* s, int64_t n, int64_t v0, int rows) {
+  const int lane = threadIdx.x & 31, half = lane >> 4, l = lane & 15;
+  const uint32_t key = (uint32_t)(v0 + half * rows);
+  int64_t lo = 0, hi = n;  // the first place whose token is at least `key` is in lo .. hi
+  while (__any_sync(0xffffffffu, hi > lo)) {
+    const int64_t step = (hi - lo + 16) / 17, at = lo + (l + 1) * step - 1;
+    const uint32_t less = __ballot_sync(0xffffffffu, at < hi && s[at < n ? at : n - 1].x < key);
+    if (hi > lo) {  // the other half may take longer
+      const int before = __popc(less >> (half * 16) & 0xFFFFu);
+      const int64_t end = lo + (before + 1) * step - 1;  // the first probe that was not less
+      lo += before * step;
+      hi = before < 16 && end < hi ? end : hi;
+    }
+  }
+  const int64_t from = __shfl_sync(0xffffffffu, lo, 0), to = __shfl_sync(0xffffffffu, lo, 16);
+  lo = from, hi = to;
+  const uint32_t mine = (uint32_t)(v0 + lane);
   while (lo < hi) {
     const int64_t mid = (lo + hi) >> 1;
-    if (s[mid].x < key) lo = mid + 1; else hi = mid;
+    if (s[mid].x < mine) lo = mid + 1; else hi = mid;
   }
-  return lo;
+  return __ballot_sync(0xffffffffu, lane < rows && lo < to && s[lo < n ? lo : n - 1].x == mine);
 }
 
 template <int KE>
@@ -428,21 +447,16 @@ __global__ void __launch_bounds__(kEbThreads) embedding_sum_kernel(LookupParams 
   const int c = (slab * (int)blockDim.x + (int)threadIdx.x) * KE;
   if (item >= p.chunks) {
     // clear the rows that no position names
-    const int64_t v0 = ((int64_t)blockIdx.x - (int64_t)p.chunks * p.slabs) * kEbZeroRows;
+    const int64_t v0 = ((int64_t)blockIdx.x - (int64_t)p.chunks * p.slabs) * p.zero_rows;
+    const int rows = p.V - v0 < p.zero_rows ? (int)(p.V - v0) : p.zero_rows;
     if (threadIdx.x < 32) {
-      const int64_t v = v0 + threadIdx.x;
-      bool has = true;
-      if (v < p.V) {
-        const int64_t at = sorted_lower(p.sorted, p.N, (uint32_t)v);
-        has = at < p.N && p.sorted[at].x == (uint32_t)v;
-      }
-      const uint32_t m = __ballot_sync(0xffffffffu, has);
+      const uint32_t m = sorted_has(p.sorted, p.N, v0, rows);
       if (threadIdx.x == 0) live = m;
     }
     __syncthreads();
     const uint32_t m = live;
-    for (int r = 0; r < kEbZeroRows; ++r)
-      if (!(m >> r & 1)) clear_row(p, v0 + r);
+    for (int r = 0; r < rows; ++r)
+      if (!(m >> r & 1)) clear_row(p, v0 + r, threadIdx.x, blockDim.x);
     return;
   }
   const int64_t first = item * p.chunk;
@@ -559,6 +573,97 @@ __global__ void __launch_bounds__(kEbJoinCols * kEbJoinShares) embedding_join_ke
     }
     __syncthreads();
   }
+}
+
+// ------------------------------------------------------------------------------------------------ few positions
+// Grid: N positions x slabs of columns, then CTAs that clear.  blockDim = (columns, shares of a token's positions).
+template <typename T, int KE>
+__global__ void __launch_bounds__(kEbThreads) embedding_few_kernel(LookupParams p) {
+  constexpr int kAhead = 8;
+  __shared__ uint32_t keys[kEbFew];
+  __shared__ uint16_t list[kEbFew];
+  __shared__ uint32_t wsum[kEbThreads / 32];
+  __shared__ uint32_t live;
+  __shared__ float sh[kEbThreads * KE];
+  const int N = (int)p.N, cols = blockDim.x, shares = blockDim.y, t = (int)threadIdx.y * cols + (int)threadIdx.x;
+  const int lane = t & 31, warp = t >> 5;
+#pragma unroll 4
+  for (int m = t; m < N; m += kEbThreads) keys[m] = lookup_key(p, m);
+  if (t == 0) live = 0;
+  __syncthreads();
+  const int64_t item = blockIdx.x / (unsigned)p.slabs;
+  if (item >= N) {
+    const int64_t v0 = ((int64_t)blockIdx.x - (int64_t)N * p.slabs) * p.zero_rows;
+    const int rows = p.V - v0 < p.zero_rows ? (int)(p.V - v0) : p.zero_rows;
+    for (int m = t; m < N; m += kEbThreads) {
+      const int64_t r = (int64_t)keys[m] - v0;
+      if (r >= 0 && r < rows) atomicOr(&live, 1u << r);
+    }
+    __syncthreads();
+    const uint32_t m = live;
+    for (int r = 0; r < rows; ++r)
+      if (!(m >> r & 1)) clear_row(p, v0 + r, t, kEbThreads);
+    return;
+  }
+  const int slab = (int)(blockIdx.x % (unsigned)p.slabs), n = (int)item;
+  const uint32_t key = keys[n];
+  if (slab == 0 && t == 0) lookup_check(p, n);
+  if (key >= (uint32_t)p.V) return;
+  bool before = false;
+  for (int m = t; m < n; m += kEbThreads) before = before || keys[m] == key;
+  if (__syncthreads_or(before)) return;
+  // the token's positions, in order: neighbouring ones a thread
+  const int per = (N + kEbThreads - 1) / kEbThreads, m0 = t * per, m1 = m0 + per < N ? m0 + per : N;
+  uint32_t has = 0;
+  for (int m = m0; m < m1; ++m) has += keys[m] == key;
+  uint32_t inc = has;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t u = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += u;
+  }
+  if (lane == 31) wsum[warp] = inc;
+  __syncthreads();
+  uint32_t at = inc - has, all = 0;
+  for (int w = 0; w < kEbThreads / 32; ++w) {
+    at += w < warp ? wsum[w] : 0u;
+    all += wsum[w];
+  }
+  for (int m = m0; m < m1; ++m)
+    if (keys[m] == key) list[at++] = (uint16_t)m;
+  __syncthreads();
+  // this share of them
+  const int count = (int)all, each = (count + shares - 1) / shares, i0 = (int)threadIdx.y * each;
+  const int i1 = i0 + each < count ? i0 + each : count;
+  const int c = (slab * cols + (int)threadIdx.x) * KE;
+  float acc[KE];
+#pragma unroll
+  for (int i = 0; i < KE; ++i) acc[i] = 0.f;
+  if (c < p.d) {
+    const T* in = static_cast<const T*>(p.in) + c;
+    for (int i = i0; i < i1; i += kAhead) {
+      Raw<T, KE> v[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j < i1) v[j].load_stream(in + (int64_t)list[i + j] * p.ld_in);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j < i1) {
+          float f[KE];
+          v[j].widen(f);
+#pragma unroll
+          for (int k = 0; k < KE; ++k) acc[k] += f[k];
+        }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < KE; ++k) sh[k * kEbThreads + t] = acc[k];
+  __syncthreads();
+  if (threadIdx.y || c >= p.d) return;
+  for (int y = 1; y < shares; ++y)
+#pragma unroll
+    for (int k = 0; k < KE; ++k) acc[k] += sh[k * kEbThreads + y * cols + t];
+  table_put<KE>(p, key, c, acc);
 }
 
 }  // namespace oapl

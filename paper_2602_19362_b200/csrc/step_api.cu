@@ -106,12 +106,35 @@ static bool lookup_carve(int64_t N, int32_t V, int32_t d, LookupCarve* c) {
   return true;
 }
 
+// Rows of the table that a CTA clears: about 16 KB, so that a CTA's search for them goes under the writes of others, and
+// between 8 and 32 of them.
+static int zero_rows(int32_t d) {
+  const int rows = 4096 / d;
+  return rows < 8 ? 8 : rows > kEbMaxZeroRows ? kEbMaxZeroRows : rows;
+}
+
+template <typename T, int KE>
+static int launch_embedding_few(LookupParams p, cudaStream_t st) {
+  const int64_t units = p.d / KE;
+  int cols = 32;
+  while (cols < 128 && cols < units) cols *= 2;
+  const int64_t slabs = (units + cols - 1) / cols;
+  p.zero_rows = zero_rows(p.d);
+  const int64_t zero = p.accumulate ? 0 : ((int64_t)p.V + p.zero_rows - 1) / p.zero_rows;
+  if (p.N * slabs + zero > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
+  p.slabs = (int32_t)slabs;
+  embedding_few_kernel<T, KE><<<(unsigned)(p.N * slabs + zero), dim3(cols, kEbThreads / cols), 0, st>>>(p);
+  CKL();
+  return OAPL_OK;
+}
+
 template <typename T, int KE>
 static int launch_embedding_sum(LookupParams p, int n_sm, cudaStream_t st) {
   const int64_t units = p.d / KE;
   const int64_t slabs = (units + kEbThreads - 1) / kEbThreads;
   const int threads = (int)round_up((size_t)((units + slabs - 1) / slabs), 32);
-  const int64_t zero = p.accumulate ? 0 : ((int64_t)p.V + kEbZeroRows - 1) / kEbZeroRows;
+  p.zero_rows = zero_rows(p.d);
+  const int64_t zero = p.accumulate ? 0 : ((int64_t)p.V + p.zero_rows - 1) / p.zero_rows;
   if (p.chunks * slabs + zero > kMaxGrid) return OAPL_ERR_UNSUPPORTED_SHAPE;
   p.slabs = (int32_t)slabs;
   CK(launch_next(embedding_sum_kernel<T, KE>, dim3((unsigned)(p.chunks * slabs + zero)), dim3(threads), 0, st, p));
@@ -133,6 +156,7 @@ static int route_embedding_sum(const LookupParams& p, int n_sm, cudaStream_t st)
   // 1536 into 151936 rows)
   constexpr int KE = Elem<T>::kN;
   const bool vec = on16(p.in) && on16(p.out) && p.d % KE == 0 && p.ld_in % KE == 0 && p.ld_out % 4 == 0;
+  if (p.N <= kEbFew) return vec ? launch_embedding_few<T, KE>(p, st) : launch_embedding_few<T, 1>(p, st);
   return vec ? launch_embedding_sum<T, KE>(p, n_sm, st) : launch_embedding_sum<T, 1>(p, n_sm, st);
 }
 
@@ -368,7 +392,9 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
   p.sorted = reinterpret_cast<uint2*>(w + c.sorted);
   p.part = reinterpret_cast<float*>(w + c.part);
   p.joins = reinterpret_cast<uint32_t*>(w + c.joins);
-  if (!c.passes) {
+  if (p.N <= kEbFew) {
+    // one launch, see the kernel
+  } else if (!c.passes) {
     const int per = kEbThreads / 32 * kEbCountRows;
     embedding_count_sort_kernel<<<(unsigned)((p.N + per - 1) / per), kEbThreads, 0, st>>>(p);
     CKL();

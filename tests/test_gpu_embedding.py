@@ -137,6 +137,7 @@ def check_bwd(N, V, d, t, kind="any", scale=1.0, accumulate=False, pad=0, offset
 @pytest.mark.parametrize("t", list(TYPES))
 @pytest.mark.parametrize("N,V,d,pad,offset", [(1, 1, 1, 0, 0), (1, 1000, 64, 0, 0), (3, 2, 7, 1, 0), (31, 40, 8, 0, 0),
                                               (32, 5, 16, 8, 0), (33, 33, 1000, 0, 1), (64, 64, 257, 3, 0), (1000, 300, 129, 0, 0),
+                                              (1024, 200, 264, 0, 0), (1025, 200, 264, 0, 0), (700, 3001, 2056, 0, 0),
                                               (8192, 5000, 72, 0, 0), (8193, 5000, 72, 0, 0), (20011, 1023, 40, 0, 0),
                                               (20011, 1024, 33, 2, 1), (30000, 70001, 24, 0, 0)])
 def test_gradient_sizes(t, N, V, d, pad, offset):
@@ -144,7 +145,7 @@ def test_gradient_sizes(t, N, V, d, pad, offset):
     check_bwd(N, V, d, t, "rank", 31.6, True, pad, offset, True)
 
 
-@pytest.mark.parametrize("N", [33, 100, 8192, 8200, 70000, 300007])
+@pytest.mark.parametrize("N", [33, 100, 1024, 1025, 8192, 8200, 70000, 300007])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_gradient_of_one_token_for_all_rows(N, accumulate):
     # a run over all chunks, joined by one CTA for each slab
@@ -156,6 +157,20 @@ def test_gradient_of_a_text_like_batch_with_wide_rows():
     check_bwd(40960, 20000, 1536, "bf16", "rank")
     check_bwd(9001, 3000, 3584, "f16", "rank", 2.0, True, masked=True)
     check_bwd(3001, 5021, 1001, "f16", "rank", 31.6, False, pad=2, masked=True)
+
+
+@pytest.mark.parametrize("N", [1105, 1156, 1190, 4913, 8177, 8211, 20230])
+def test_gradient_writes_the_last_tokens_of_the_list(N):
+    # every row of the table has a token, or all but one: what is cleared lies between the ends that a search finds
+    V, d = -(-N // 5), 8
+    ids = torch.arange(N, device="cuda", dtype=torch.int32) // 5
+    for gone in (None, 0, 31, 32, V // 2, V - 1):
+        keep = ids[ids != gone] if gone is not None else ids
+        dout = torch.ones(keep.numel(), d, device="cuda")
+        table = torch.full((V, d), 7.0, device="cuda")
+        B.oapl_embedding_bwd(B.make_lookup(keep, V), dout, table, False, workspace(keep.numel(), V, d))
+        want = torch.bincount(keep.long(), minlength=V).float()[:, None].expand(V, d)
+        assert torch.equal(table, want), gone
 
 
 def test_gradient_runs_that_begin_and_end_at_chunks():
@@ -185,7 +200,7 @@ def test_gradient_without_any_row_that_counts():
 
 
 def test_gradient_ids_outside_count_for_nothing():
-    for N in (500, 9000):
+    for N in (500, 2000, 9000):
         g = torch.Generator(device="cuda").manual_seed(N)
         V, d = 64, 16
         ids = torch.randint(-5, V + 5, (N,), device="cuda", generator=g).to(torch.int32)
@@ -200,7 +215,7 @@ def test_gradient_ids_outside_count_for_nothing():
 
 def test_gradient_repeats_bit_for_bit():
     g = torch.Generator(device="cuda").manual_seed(5)
-    for N in (5000, 50000):
+    for N in (900, 5000, 50000):
         ids, dout = ids_of(g, N, 3000, "rank"), rand(g, N, 256, "bf16")
         got = []
         for _ in range(3):
