@@ -179,7 +179,8 @@ constexpr int kRsRedFloats = 64 + RowGroup<false>::kSlot;
 // LEVEL: all rows start on 16-byte boundaries and have whole units.  A thread copies the units that it will read, so a wait
 // for its own copies is all that a stage needs.
 // Otherwise the aligned 16-byte blocks that hold a row are copied as they are, whoever reads them, and a barrier follows
-// the wait.  A unit is then two blocks shifted in registers, its elements behind the row's end taken as 0.
+// the wait.  A unit is then two blocks shifted in registers (fp32: four words), its elements behind the row's end taken
+// as 0.
 // kDirect: fp32 rows above 8192 elements, five of which shared memory has no room for, are read where they are.
 extern __shared__ __align__(16) unsigned char rs_ring[];
 
@@ -282,17 +283,19 @@ struct RowFeed {
       Elem<T>::widen(q.p[k * nt], f);
     } else {
       const int have = d - (t + k * nt) * KE;  // elements from here to the row's end, at least one
-      const uint4 lo = q.p[k * nt];
-      if (q.off == 0) {  // the same for all threads
-        Elem<T>::widen(lo, f);
+      if constexpr (sizeof(T) == 4) {
+        // fp32 off its boundary: a word at a time is a third of the instructions of shifting whole blocks
+        const float* e = reinterpret_cast<const float*>(reinterpret_cast<const unsigned char*>(q.p + k * nt) + q.off);
+#pragma unroll
+        for (int i = 0; i < KE; ++i) f[i] = i < have ? e[i] : 0.f;
+        return;
       } else {
-        uint4 hi = lo;
-        if constexpr (kDirect) {  // memory behind the row's last block may be nobody's
-          if (q.off + (uint32_t)(have < KE ? have : KE) * (uint32_t)sizeof(T) > 16u) hi = q.p[k * nt + 1];
+        const uint4 lo = q.p[k * nt];
+        if (q.off == 0) {  // the same for all threads
+          Elem<T>::widen(lo, f);
         } else {
-          hi = q.p[k * nt + 1];
+          Elem<T>::widen(shift_16(lo, q.p[k * nt + 1], q.off), f);
         }
-        Elem<T>::widen(shift_16(lo, hi, q.off), f);
       }
       if (have < KE) {
 #pragma unroll
@@ -325,9 +328,9 @@ struct RowSink {
       T* to = row + first;
       // elements before the first boundary, the same for all units of a row
       int head = (int)(-(reinterpret_cast<uintptr_t>(row) / sizeof(T)) & (KE - 1));
-      if (head == 0) {
+      if (head == 0 || sizeof(T) == 4) {  // (fp32: a word at a time, as it is read)
         const int have = n - lane * KE;
-        if (have >= KE) {
+        if (have >= KE && head == 0) {
           Raw<T, KE>::store(to + lane * KE, o);
         } else {
 #pragma unroll
@@ -499,8 +502,13 @@ __device__ __forceinline__ void row_weight(const void* w, int type, int d, int c
   if constexpr (LEVEL) {
     load_weight<KE>(w, type, c, offset, f);
   } else {
+    auto some = [&](auto one) {
 #pragma unroll
-    for (int i = 0; i < KE; ++i) f[i] = c + i < d ? load_one(w, type, c + i) + offset : 0.f;
+      for (int i = 0; i < KE; ++i) f[i] = c + i < d ? one(c + i) + offset : 0.f;
+    };
+    if (type == 0) some([&](int i) { return Elem<__nv_bfloat16>::one(w, i); });
+    else if (type == 1) some([&](int i) { return Elem<__half>::one(w, i); });
+    else some([&](int i) { return Elem<float>::one(w, i); });
   }
 }
 
