@@ -18,9 +18,10 @@
 // and otherwise finds its other positions and adds up their rows.
 //
 // Measured, us: 64 rows of 3584 bf16 2.7 on the device; 32768 x 3584 58 (the copy rate), 32768 x 3583 96 (two loads and a shift
-// per vector); gradient of 40960 x 1536 bf16 into 151936 rows 189 (0.87 of the copy rate), of which the sums and the zeros
-// take 158, the sort 20; 65536 x 1536 into 20000 rows 90; 3001 x 1001 fp16 off 16-byte boundaries into 50021 rows 52.  Clearing
-// rows beside the sort, whose CTAs leave most SMs idle, was tried: it slowed the sort by what it saved.
+// per vector); gradient of 40960 x 1536 bf16 into 151936 rows 185 (0.89 of the copy rate), of which the sums and the zeros
+// take 158, the sort 17; 65536 x 1536 into 20000 rows 85; 3001 x 1001 fp16 off 16-byte boundaries into 50021 rows 53; 23 x 313
+// into 1486 rows, in one launch, 8.2 (13.3 with the sort and the sums apart).  Clearing rows beside the sort, whose CTAs leave
+// most SMs idle, was tried: it slowed the sort by what it saved.
 #pragma once
 #include <type_traits>
 
@@ -400,8 +401,9 @@ __device__ __forceinline__ uint32_t sorted_has(const uint2* s, int64_t n, int64_
   int64_t lo = 0, hi = n;  // the first place whose token is at least `key` is in lo .. hi
   while (__any_sync(0xffffffffu, hi > lo)) {
     const int64_t step = (hi - lo + 16) / 17, at = lo + (l + 1) * step - 1;
-    const uint32_t less = __ballot_sync(0xffffffffu, at < hi && s[at < n ? at : n - 1].x < key);
-    if (hi > lo) {  // the other half may take longer
+    // (a half that is done, maybe at the list's start, reads nothing while the other goes on)
+    const uint32_t less = __ballot_sync(0xffffffffu, hi > lo && at < hi && s[at].x < key);
+    if (hi > lo) {
       const int before = __popc(less >> (half * 16) & 0xFFFFu);
       const int64_t end = lo + (before + 1) * step - 1;  // the first probe that was not less
       lo += before * step;
@@ -415,7 +417,7 @@ __device__ __forceinline__ uint32_t sorted_has(const uint2* s, int64_t n, int64_
     const int64_t mid = (lo + hi) >> 1;
     if (s[mid].x < mine) lo = mid + 1; else hi = mid;
   }
-  return __ballot_sync(0xffffffffu, lane < rows && lo < to && s[lo < n ? lo : n - 1].x == mine);
+  return __ballot_sync(0xffffffffu, lane < rows && lo < to && s[lo].x == mine);
 }
 
 template <int KE>
