@@ -549,7 +549,7 @@ typedef struct {
  * changes is touched) or memory apart.  Rows with the logits' mask==0 are neither read nor written; targets and scale of
  * `logits` are not used.  Unchanged logits keep their bits.  Spans that decrease or leave [0,T], biases that leave
  * [0,biases]: none for that row, status OAPL_ERR_BAD_SEQ_ORDER; an allowed_row past allowed_rows: no mask for that row,
- * OAPL_ERR_BAD_TARGET.
+ * OAPL_ERR_BAD_TARGET.  Each of a row's biases is compared with all of them: lists are meant to have up to a few hundred.
  */
 int oapl_logits_adjust(const oapl_logits* logits /*host*/, const oapl_adjust* adjust /*host*/, void* out, int64_t ld_out,
                        int32_t* device_status, void* stream);

@@ -18,9 +18,9 @@
 // Sums over rows (dw_pre, dw_post, dg per channel) are kept in registers over a CTA's rows, written as one partial row per
 // CTA, and joined in a fixed order by a second launch.  All sums are fp32.
 //
-// Measured, us, 16384 x 3584 bf16: forward 86 (0.85 of the copy rate), gradient 132 with its join (0.83); 11000 x 5120: 82 and
-// 146; 100000 x 256: 43 and 75; fp32, 8000 x 3584, gradient 137.  Rows of 3583, off 16-byte boundaries: 152 and 259, where
-// shifting takes three times the instructions of the arithmetic.  The gradient's arithmetic is written two wide and takes
+// Measured, us, 16384 x 3584 bf16: forward 88 (0.83 of the copy rate), gradient 131 with its join (0.84); 11000 x 5120: 84 and
+// 148; 100000 x 256: 42 and 74; fp32, 8000 x 3584, gradient 134.  Rows of 3583 elements that start on 16-byte boundaries: 113
+// and 252; off them: 159 and 317, where shifting takes three times the instructions of the arithmetic.  The gradient's arithmetic is written two wide and takes
 // half of the issue slots; one wide, with weights widened for each row and parts left out at run time, it took 83
 // instructions an element and 270 us.  What is left forward is the chain of two sums over a row, which the other CTAs of an SM cover.
 #pragma once
