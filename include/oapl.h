@@ -503,9 +503,10 @@ typedef struct {
 
 /*
  * sq_norm [1] f32 = sum of (scale * g)^2 over all elements of the list, norm [1] f32 its square root; one of them may be
- * NULL.  Sums are fp64, so norm is right where sq_norm leaves the range of fp32.  A norm that is not finite:
- * OAPL_ERR_NONFINITE_INPUT.  The list is read during the call only.  ws: oapl_grad_norm_workspace_bytes(count) bytes,
- * 16-byte aligned.  sq_norm is what oapl_adamw_step takes as other_sq_norm.
+ * NULL.  Sums are fp64, so norm is right where sq_norm leaves the range of fp32: a norm above 1.8e19 makes sq_norm infinite.
+ * OAPL_ERR_NONFINITE_INPUT: a norm that is not finite in fp32, or an infinite sq_norm where norm is NULL.  The list is read
+ * during the call only.  ws: oapl_grad_norm_workspace_bytes(count) bytes, 16-byte aligned.  sq_norm is what
+ * oapl_adamw_step takes as other_sq_norm; an infinite one makes the clipped gradient of that step 0.
  */
 size_t oapl_grad_norm_workspace_bytes(int32_t count);
 int oapl_grad_norm(const oapl_tensor* tensors /*host*/, int32_t count, float scale, float* sq_norm, float* norm,
@@ -514,11 +515,18 @@ int oapl_grad_norm(const oapl_tensor* tensors /*host*/, int32_t count, float sca
 /*
  * out = g * scale * min(1, clip_norm / (sqrt(*sq_norm) + 1e-6)) for every tensor of the list, rounded once.  sq_norm: of
  * oapl_grad_norm with the same scale, or such a sum over several ranks.  Where it is not finite the factor is scale
- * alone: the caller leaves out the step.  Elements that the factor 1 would leave in place are not read.
- * No out overlaps a tensor other than its own.
+ * alone, so a norm above 1.8e19 is not clipped by its square: the caller leaves out the step, or calls the form below.
+ * Elements that the factor 1 would leave in place are not read.  No out overlaps a tensor other than its own.
  */
 int oapl_grad_clip(const oapl_tensor* tensors /*host*/, int32_t count, float scale, const float* sq_norm,
                    float clip_norm, void* stream);
+
+/*
+ * The same with the norm itself, which is finite wherever oapl_grad_norm reports no error: with norm [1] f32 the factor is
+ * scale * min(1, clip_norm / (*norm + 1e-6)) and sq_norm, which may be NULL, is not read; without norm it is the call above.
+ */
+int oapl_grad_clip_ex(const oapl_tensor* tensors /*host*/, int32_t count, float scale, const float* sq_norm,
+                      const float* norm, float clip_norm, void* stream);
 
 /*
  * What a sampler does to logits before it samples, which a trainer that re-scores its tokens has to repeat.  For a token v

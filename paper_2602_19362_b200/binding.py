@@ -29,8 +29,8 @@ EXPORTS = ["oapl_workspace_bytes", "oapl_token_logprobs", "oapl_value_estimate",
            "oapl_logits_logprobs", "oapl_logits_logprobs_bwd", "oapl_quantize", "oapl_scaled_matmul",
            "oapl_debug_scaled_matmul", "oapl_embedding", "oapl_embedding_workspace_bytes", "oapl_embedding_bwd",
            "oapl_residual_norm", "oapl_residual_norm_workspace_bytes", "oapl_residual_norm_bwd",
-           "oapl_grad_norm_workspace_bytes", "oapl_grad_norm", "oapl_grad_clip", "oapl_logits_adjust",
-           "oapl_logits_adjust_bwd"]
+           "oapl_grad_norm_workspace_bytes", "oapl_grad_norm", "oapl_grad_clip", "oapl_grad_clip_ex",
+           "oapl_logits_adjust", "oapl_logits_adjust_bwd"]
 
 
 class OaplProblem(ctypes.Structure):
@@ -182,6 +182,8 @@ def lib() -> ctypes.CDLL:
         L.oapl_grad_norm.argtypes = [pt, c32, f32, vp, vp, vp, vp, sz, vp]
         L.oapl_grad_clip.restype = i32
         L.oapl_grad_clip.argtypes = [pt, c32, f32, vp, f32, vp]
+        L.oapl_grad_clip_ex.restype = i32
+        L.oapl_grad_clip_ex.argtypes = [pt, c32, f32, vp, vp, f32, vp]
         L.oapl_logits_adjust.restype = i32
         L.oapl_logits_adjust.argtypes = [pl, pa, vp, i64, vp, vp]
         L.oapl_logits_adjust_bwd.restype = i32
@@ -754,13 +756,15 @@ def oapl_grad_norm(tensors: TensorList, sq_norm, norm, ws, scale: float = 1.0, d
         raise OaplError(rc, "oapl_grad_norm")
 
 
-def oapl_grad_clip(tensors: TensorList, sq_norm, clip_norm: float, scale: float = 1.0):
-    """Every tensor times scale * min(1, clip_norm / (sqrt(sq_norm) + 1e-6)), into the list's outs."""
-    dev = tensors.device
-    if sq_norm is None:
-        raise TypeError("sq_norm: expected the fp32 [1] of oapl_grad_norm")
-    rc = lib().oapl_grad_clip(tensors.array, tensors.count, scale, _vec(sq_norm, torch.float32, (1,), dev, "sq_norm"),
-                              clip_norm, _stream_of(dev))
+def oapl_grad_clip(tensors: TensorList, sq_norm, clip_norm: float, scale: float = 1.0, norm=None):
+    """Every tensor times scale * min(1, clip_norm / (sqrt(sq_norm) + 1e-6)), into the list's outs.  norm: fp32 [1] of
+    oapl_grad_norm, read in the place of the root of sq_norm, which may then be None: a norm above 1.8e19 makes sq_norm
+    infinite, and the tensors would leave with the factor scale."""
+    dev, f32 = tensors.device, torch.float32
+    if sq_norm is None and norm is None:
+        raise TypeError("sq_norm, norm: expected the fp32 [1] of oapl_grad_norm")
+    rc = lib().oapl_grad_clip_ex(tensors.array, tensors.count, scale, _vec(sq_norm, f32, (1,), dev, "sq_norm"),
+                                 _vec(norm, f32, (1,), dev, "norm"), clip_norm, _stream_of(dev))
     if rc != OAPL_OK:
         raise OaplError(rc, "oapl_grad_clip")
 

@@ -151,8 +151,10 @@ __global__ void __launch_bounds__(kGcThreads) grad_norm_join_kernel(const double
     for (int w = 0; w < kGcThreads / 32; ++w) t += sh[w];
     t *= (double)scale * (double)scale;
     if (sq_norm) *sq_norm = (float)t;
-    if (norm) *norm = (float)sqrt(t);
-    if (status && !(t <= 1.7976931348623157e308)) atomicCAS(status, 0, kErrNonfiniteGrad);
+    const float root = (float)sqrt(t), square = (float)t;
+    if (norm) *norm = root;
+    // reported where what the caller gets does not hold the norm: its square leaves fp32 long before it does
+    if (status && !(norm ? root <= 3.402823466e38f : square <= 3.402823466e38f)) atomicCAS(status, 0, kErrNonfiniteGrad);
   }
 }
 
@@ -199,13 +201,14 @@ __device__ __forceinline__ void grad_scale_types(const GradTensor& t, int64_t at
 // TI, TO: the types of the whole list, void where it has several.
 template <typename TI, typename TO>
 __global__ void __launch_bounds__(kGcThreads, 4) grad_clip_kernel(const __grid_constant__ GradList l, const float* sq_norm,
-                                                                  float clip, float scale) {
+                                                                  const float* norm_of, float clip, float scale) {
   __shared__ float sh;
   if (threadIdx.x == 0) {
-    const double sq = *sq_norm;
+    // (the norm itself where it is given: a square is infinite from a norm of 1.8e19 on)
+    const double norm = norm_of ? (double)*norm_of : sqrt((double)*sq_norm);
     double f = 1.0;
-    if (sq <= 3.4028234663852886e38) f = fmin(1.0, (double)clip / (sqrt(sq) + 1e-6));  // not for inf or NaN
-    sh = (float)f * scale;
+    if (norm <= 3.4028234663852886e38) f = fmin(1.0, (double)clip / (norm + 1e-6));  // not for inf or NaN
+    sh = (float)f * scale;  // (below 1e-38 with fewer bits)
   }
   __syncthreads();
   const float factor = sh;

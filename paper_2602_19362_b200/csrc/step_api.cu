@@ -213,7 +213,7 @@ static int32_t fill_list(const oapl_tensor* t, int32_t count, bool clip, GradLis
 }
 
 template <typename TI>
-static auto pick_clip(int out) -> void (*)(GradList, const float*, float, float) {
+static auto pick_clip(int out) -> void (*)(GradList, const float*, const float*, float, float) {
   return out == 0 ? grad_clip_kernel<TI, __nv_bfloat16> : out == 1 ? grad_clip_kernel<TI, __half> : grad_clip_kernel<TI, float>;
 }
 
@@ -465,10 +465,16 @@ int oapl_grad_norm(const oapl_tensor* tensors, int32_t count, float scale, float
 
 int oapl_grad_clip(const oapl_tensor* tensors, int32_t count, float scale, const float* sq_norm, float clip_norm,
                    void* stream) {
+  return oapl_grad_clip_ex(tensors, count, scale, sq_norm, nullptr, clip_norm, stream);
+}
+
+int oapl_grad_clip_ex(const oapl_tensor* tensors, int32_t count, float scale, const float* sq_norm, const float* norm,
+                      float clip_norm, void* stream) {
   const int rc = check_tensors(tensors, count, true);
   if (rc != OAPL_OK) return rc;
-  if (!sq_norm || !std::isfinite(scale) || !(clip_norm > 0.f) || !std::isfinite(clip_norm)) return OAPL_ERR_INVALID_ARG;
-  if ((uintptr_t)sq_norm & 3) return OAPL_ERR_MISALIGNED;
+  if ((!sq_norm && !norm) || !std::isfinite(scale) || !(clip_norm > 0.f) || !std::isfinite(clip_norm))
+    return OAPL_ERR_INVALID_ARG;
+  if (((uintptr_t)sq_norm | (uintptr_t)norm) & 3) return OAPL_ERR_MISALIGNED;
   const int n_sm = sm_count();
   if (n_sm <= 0) return OAPL_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -484,7 +490,7 @@ int oapl_grad_clip(const oapl_tensor* tensors, int32_t count, float scale, const
     const int in = l.t[0].in_type, out = l.t[0].out_type;
     auto kern = !one ? grad_clip_kernel<void, void>
                      : in == 0 ? pick_clip<__nv_bfloat16>(out) : in == 1 ? pick_clip<__half>(out) : pick_clip<float>(out);
-    kern<<<l.chunks < most ? l.chunks : most, kGcThreads, 0, st>>>(l, sq_norm, clip_norm, scale);
+    kern<<<l.chunks < most ? l.chunks : most, kGcThreads, 0, st>>>(l, sq_norm, norm, clip_norm, scale);
     CKL();
   }
   return OAPL_OK;
