@@ -66,8 +66,9 @@ template <typename T, int E, bool WARP, int NT, bool FWD, bool LEVEL, int FORM>
 int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
   static int known[kMaxDevices] = {0};
   constexpr int KE = Elem<T>::kN, K = E / KE;
-  auto kern = FWD ? residual_fwd_kernel<T, KE, K, WARP, NT, LEVEL, FORM>
-                  : residual_bwd_kernel<T, KE, K, WARP, NT, LEVEL, FORM>;
+  void (*kern)(ResidualParams);
+  if constexpr (FWD) kern = residual_fwd_kernel<T, KE, K, WARP, NT, LEVEL, FORM>;  // a choice that compiles one of the two
+  else kern = residual_bwd_kernel<T, KE, K, WARP, NT, LEVEL, FORM>;
   int regs = 0;
   const int rc = residual_registers(kern, known, &regs);
   if (rc != OAPL_OK) return rc;

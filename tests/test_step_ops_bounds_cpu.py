@@ -1,5 +1,7 @@
 """The ends of what the host sides of the embedding, the residual norm, the gradient norm and clipping take."""
 import ctypes
+import re
+import subprocess
 
 import pytest
 
@@ -25,3 +27,22 @@ def test_clipping_by_the_norm_checks_its_arguments(L):
     assert f() == INVALID
     with pytest.raises(TypeError):
         B.oapl_grad_clip(type("List", (), dict(device=0, array=t, count=2))(), None, 1.0)
+
+
+def test_the_library_holds_the_residual_kernels_that_calls_reach_and_no_others(L):
+    names = subprocess.run(["nm", "-C", "--defined-only", build.LIB], capture_output=True, text=True, check=True).stdout
+    have = set(re.findall(r"oapl::residual_(fwd|bwd)_kernel<(\w+), (\d+), (\d+), (\w+), (\d+), (\w+), (\d+)>", names))
+    anything, post, plain, post_full, full = range(5)
+    want = set()
+    for t, ke in (("__nv_bfloat16", 8), ("__half", 8), ("float", 4)):
+        # elements a thread, whether a row is a warp's, threads at most
+        for e, warp, threads in ((8, True, 256), (16, True, 256), (8, False, 256), (16, False, 256), (16, False, 512), (32, False, 512)):
+            for level in (True, False):
+                if t == "float" and e == 32 and level:
+                    continue        # fp32 rows as wide as these are read where they are
+                forms = {anything}
+                forms |= {post, post_full} if e < 32 or level else set()
+                forms |= {plain, full} if e < 32 and level else set()
+                shape = (t, str(ke), str(e // ke), str(warp).lower(), str(threads), str(level).lower())
+                want |= {("bwd", *shape, str(f)) for f in forms} | {("fwd", *shape, str(f)) for f in (anything, post)}
+    assert have == want, (sorted(have - want)[:5], sorted(want - have)[:5])
