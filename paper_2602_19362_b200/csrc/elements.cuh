@@ -23,18 +23,6 @@ __device__ __forceinline__ uint4 ldg_stream(const uint4* p) {
   return v;
 }
 
-// A load that stays where it is written, ahead of the test that decides whether its value counts.
-__device__ __forceinline__ uint4 load_here(const uint4* p) {
-  uint4 v;
-  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint32_t load_here(const uint32_t* p) {
-  uint32_t v;
-  asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p));
-  return v;
-}
-
 // A launch that follows another one of the same call may begin before that one has ended (host_common.cuh, launch_next):
 // it waits here before it touches memory, and lets the launch behind it begin in turn.
 __device__ __forceinline__ void after_launch_before() {
