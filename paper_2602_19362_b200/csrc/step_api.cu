@@ -433,7 +433,7 @@ int oapl_embedding_bwd(const oapl_lookup* lookup, const void* dout, int32_t type
 }
 
 size_t oapl_grad_norm_workspace_bytes(int32_t count) {
-  return count <= 0 ? 0 : sizeof(double) * kGcMaxSums * (size_t)((count + kGcList - 1) / kGcList);
+  return count <= 0 ? 0 : sizeof(double) * kGcMaxSums * (((size_t)count + kGcList - 1) / kGcList);
 }
 
 int oapl_grad_norm(const oapl_tensor* tensors, int32_t count, float scale, float* sq_norm, float* norm,

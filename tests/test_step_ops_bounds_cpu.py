@@ -46,3 +46,12 @@ def test_the_library_holds_the_residual_kernels_that_calls_reach_and_no_others(L
                 shape = (t, str(ke), str(e // ke), str(warp).lower(), str(threads), str(level).lower())
                 want |= {("bwd", *shape, str(f)) for f in forms} | {("fwd", *shape, str(f)) for f in (anything, post)}
     assert have == want, (sorted(have - want)[:5], sorted(want - have)[:5])
+
+
+def test_workspace_of_the_longest_list(L):
+    w = L.oapl_grad_norm_workspace_bytes
+    one = w(1)                                       # a launch's partial sums
+    most = 2 ** 31 - 1
+    launches = [n for n in range(950, 970) if w(n) == one][-1]      # tensors of a launch
+    for count in (launches + 1, most - launches, most - launches + 1, most - 1, most):
+        assert w(count) == one * -(-count // launches), count
