@@ -3,6 +3,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "residual_host.cuh"
 
@@ -72,17 +73,41 @@ static bool residual_level(const ResidualParams& p, int es, const Place* m, int 
 }
 
 static int residual_fwd(const ResidualParams& p, int32_t type, bool level, int arrays, int n_sm, cudaStream_t st) {
-  int64_t workers = 0;
-  if (type == OAPL_TYPE_BF16) return route_residual_level<__nv_bfloat16, true>(p, level, arrays, n_sm, &workers, st);
-  if (type == OAPL_TYPE_F16) return route_residual_level<__half, true>(p, level, arrays, n_sm, &workers, st);
-  return route_residual_level<float, true>(p, level, arrays, n_sm, &workers, st);
+  ResidualRun run;
+  if (type == OAPL_TYPE_BF16) return route_residual_level<__nv_bfloat16, true>(p, level, arrays, n_sm, &run, st);
+  if (type == OAPL_TYPE_F16) return route_residual_level<__half, true>(p, level, arrays, n_sm, &run, st);
+  return route_residual_level<float, true>(p, level, arrays, n_sm, &run, st);
 }
 
-static int residual_bwd(const ResidualParams& p, int32_t type, bool level, int arrays, int n_sm, int64_t* workers,
+static int residual_bwd(const ResidualParams& p, int32_t type, bool level, int arrays, int n_sm, ResidualRun* run,
                         cudaStream_t st) {
-  if (type == OAPL_TYPE_BF16) return residual_bwd_bf16(p, level, arrays, n_sm, workers, st);
-  if (type == OAPL_TYPE_F16) return residual_bwd_f16(p, level, arrays, n_sm, workers, st);
-  return residual_bwd_f32(p, level, arrays, n_sm, workers, st);
+  if (type == OAPL_TYPE_BF16) return residual_bwd_bf16(p, level, arrays, n_sm, run, st);
+  if (type == OAPL_TYPE_F16) return residual_bwd_f16(p, level, arrays, n_sm, run, st);
+  return residual_bwd_f32(p, level, arrays, n_sm, run, st);
+}
+
+// The gradient's rows from `rows` on.
+static void residual_skip(ResidualParams& p, int64_t rows, int es) {
+  auto skip = [&](auto& at, int64_t bytes) {
+    using P = std::remove_reference_t<decltype(at)>;
+    if (at) at = reinterpret_cast<P>(reinterpret_cast<uintptr_t>(at) + (uintptr_t)(rows * bytes));
+  };
+  skip(p.x_out, p.ld_xo * es);
+  skip(p.dh, p.ld_dh * es);
+  skip(p.dx_out, p.ld_dxo * es);
+  skip(p.y, p.ld_y * es);
+  skip(p.dx, p.ld_dx * es);
+  skip(p.dy, p.ld_dy * es);
+  skip(p.rstd_post, 4);
+  skip(p.rstd_pre, 4);
+  if (p.gate_kind == kGateFull) {
+    skip(p.gate, p.ld_gate * es);
+    skip(p.dgate, p.ld_dg * es);
+  } else if (p.gate_kind == kGateRow) {
+    skip(p.gate, p.ld_gate * type_size(p.gate_type));
+    skip(p.dgate, p.ld_dg * 4);
+  }
+  p.N -= rows;
 }
 
 }  // namespace oapl
@@ -191,12 +216,19 @@ int oapl_residual_norm_bwd(const oapl_residual* r, const void* x_out, int64_t ld
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int arrays = 2 * pre + (dx_out != nullptr) + (r->y != nullptr) + full;
   const bool level = residual_level(p, es, m, 8);
-  const int run = residual_bwd(p, r->type, level, arrays, n_sm, &j.workers, st);
-  if (run != OAPL_OK || !kinds) return run;
   j.part = p.part;
   j.d = r->d;
   j.accumulate = accumulate != 0;
-  CK(launch_next(residual_join_kernel, dim3((unsigned)((r->d + 31) / 32), (unsigned)kinds), dim3(32, kRsShares), 0, st, j));
+  for (;;) {
+    ResidualRun run;
+    const int ran = residual_bwd(p, r->type, level, arrays, n_sm, &run, st);
+    if (ran != OAPL_OK || !kinds) return ran;
+    j.workers = run.workers;
+    CK(launch_next(residual_join_kernel, dim3((unsigned)((r->d + 31) / 32), (unsigned)kinds), dim3(32, kRsShares), 0, st, j));
+    if (run.rows == p.N) break;
+    residual_skip(p, run.rows, es);
+    j.accumulate = 1;
+  }
   return OAPL_OK;
 }
 

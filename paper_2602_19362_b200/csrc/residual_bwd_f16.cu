@@ -3,8 +3,8 @@
 
 namespace oapl {
 
-int residual_bwd_f16(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  return route_residual_level<__half, false>(p, level, arrays, n_sm, workers, st);
+int residual_bwd_f16(const ResidualParams& p, bool level, int arrays, int n_sm, ResidualRun* run, cudaStream_t st) {
+  return route_residual_level<__half, false>(p, level, arrays, n_sm, run, st);
 }
 
 }  // namespace oapl

@@ -46,6 +46,11 @@ inline ResidualShape residual_shape(ResidualParams& p, int n_sm, int elems, int 
   return s;
 }
 
+// What a launch has done: its workers, and the rows that they took.
+struct ResidualRun {
+  int64_t workers, rows;
+};
+
 // A kernel's registers, with its shared memory allowed, looked up once for each device.
 template <typename F>
 int residual_registers(F kern, int (&known)[kMaxDevices], int* regs) {
@@ -63,7 +68,7 @@ int residual_registers(F kern, int (&known)[kMaxDevices], int* regs) {
 }
 
 template <typename T, int E, bool WARP, int NT, bool FWD, bool LEVEL, int FORM>
-int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
+int launch_residual(ResidualParams p, int arrays, int n_sm, ResidualRun* run, cudaStream_t st) {
   static int known[kMaxDevices] = {0};
   constexpr int KE = Elem<T>::kN, K = E / KE;
   void (*kern)(ResidualParams);
@@ -73,14 +78,17 @@ int launch_residual(ResidualParams p, int arrays, int n_sm, int64_t* workers, cu
   const int rc = residual_registers(kern, known, &regs);
   if (rc != OAPL_OK) return rc;
   const ResidualShape s = residual_shape(p, n_sm, E, (int)sizeof(T), WARP, LEVEL, arrays, regs);
-  *workers = s.workers;
+  const bool sums = p.kind_pre >= 0 || p.kind_post >= 0 || p.kind_gate >= 0;
+  if (sums && p.N > s.workers * kRsFold) p.N = s.workers * kRsFold;
+  run->workers = s.workers;
+  run->rows = p.N;
   kern<<<s.grid, s.threads, s.smem, st>>>(p);
   CKL();
   return OAPL_OK;
 }
 
 template <typename T, int E, bool WARP, int NT, bool FWD, bool LEVEL>
-int pick_residual(const ResidualParams& p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
+int pick_residual(const ResidualParams& p, int arrays, int n_sm, ResidualRun* run, cudaStream_t st) {
   const bool whole = p.y && p.w_pre && p.x_out && (FWD || (p.dx_out && p.dx && p.dy && (p.dgate || p.gate_kind != kGateFull)));
   const int form = !whole ? kFormAny : p.gate_kind == kGateFull ? (p.w_post ? kFormPostFull : kFormFull)
                                                                  : (p.w_post ? kFormPost : kFormPlain);
@@ -90,45 +98,45 @@ int pick_residual(const ResidualParams& p, int arrays, int n_sm, int64_t* worker
   // w_post, whose second mean costs most; of rows above 8192 those as far as they are on boundaries (4700 x 12288 with a
   // gate per element: 293 us, 364 for any form).
   if constexpr (FWD || E < 32 || LEVEL) {
-    if (form == kFormPost) return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormPost>(p, arrays, n_sm, workers, st);
+    if (form == kFormPost) return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormPost>(p, arrays, n_sm, run, st);
   }
   if constexpr (!FWD) {
     if constexpr (E < 32 || LEVEL) {
       if (form == kFormPostFull)
-        return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormPostFull>(p, arrays, n_sm, workers, st);
+        return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormPostFull>(p, arrays, n_sm, run, st);
     }
     if constexpr (E < 32 && LEVEL) {
       if (form == kFormPlain)
-        return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormPlain>(p, arrays, n_sm, workers, st);
-      if (form == kFormFull) return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormFull>(p, arrays, n_sm, workers, st);
+        return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormPlain>(p, arrays, n_sm, run, st);
+      if (form == kFormFull) return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormFull>(p, arrays, n_sm, run, st);
     }
   }
-  return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormAny>(p, arrays, n_sm, workers, st);
+  return launch_residual<T, E, WARP, NT, FWD, LEVEL, kFormAny>(p, arrays, n_sm, run, st);
 }
 
 template <typename T, bool FWD, bool LEVEL>
-int route_residual(const ResidualParams& p, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
+int route_residual(const ResidualParams& p, int arrays, int n_sm, ResidualRun* run, cudaStream_t st) {
   // elements a thread: as few as give a CTA at most 256 threads, 32 beyond that
-  if (p.d <= kRsWarpD / 2) return pick_residual<T, 8, true, 256, FWD, LEVEL>(p, arrays, n_sm, workers, st);
-  if (p.d <= kRsWarpD) return pick_residual<T, 16, true, 256, FWD, LEVEL>(p, arrays, n_sm, workers, st);
-  if (p.d <= 2048) return pick_residual<T, 8, false, 256, FWD, LEVEL>(p, arrays, n_sm, workers, st);
-  if (p.d <= 4096) return pick_residual<T, 16, false, 256, FWD, LEVEL>(p, arrays, n_sm, workers, st);
+  if (p.d <= kRsWarpD / 2) return pick_residual<T, 8, true, 256, FWD, LEVEL>(p, arrays, n_sm, run, st);
+  if (p.d <= kRsWarpD) return pick_residual<T, 16, true, 256, FWD, LEVEL>(p, arrays, n_sm, run, st);
+  if (p.d <= 2048) return pick_residual<T, 8, false, 256, FWD, LEVEL>(p, arrays, n_sm, run, st);
+  if (p.d <= 4096) return pick_residual<T, 16, false, 256, FWD, LEVEL>(p, arrays, n_sm, run, st);
   // (fp32 rows off 16-byte boundaries have no room beside their factors where there are five arrays of them)
   const bool room = LEVEL || (size_t)arrays * p.d * sizeof(T) + (size_t)8 * p.d <= kRsSmem;
-  if (p.d <= 8192 && room) return pick_residual<T, 16, false, 512, FWD, LEVEL>(p, arrays, n_sm, workers, st);
+  if (p.d <= 8192 && room) return pick_residual<T, 16, false, 512, FWD, LEVEL>(p, arrays, n_sm, run, st);
   // fp32 rows are read where they are
-  return pick_residual<T, 32, false, 512, FWD, LEVEL && sizeof(T) == 2>(p, arrays, n_sm, workers, st);
+  return pick_residual<T, 32, false, 512, FWD, LEVEL && sizeof(T) == 2>(p, arrays, n_sm, run, st);
 }
 
 template <typename T, bool FWD>
-int route_residual_level(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st) {
-  return level ? route_residual<T, FWD, true>(p, arrays, n_sm, workers, st)
-               : route_residual<T, FWD, false>(p, arrays, n_sm, workers, st);
+int route_residual_level(const ResidualParams& p, bool level, int arrays, int n_sm, ResidualRun* run, cudaStream_t st) {
+  return level ? route_residual<T, FWD, true>(p, arrays, n_sm, run, st)
+               : route_residual<T, FWD, false>(p, arrays, n_sm, run, st);
 }
 
 // Compiled apart, a type to a file.
-int residual_bwd_bf16(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st);
-int residual_bwd_f16(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st);
-int residual_bwd_f32(const ResidualParams& p, bool level, int arrays, int n_sm, int64_t* workers, cudaStream_t st);
+int residual_bwd_bf16(const ResidualParams& p, bool level, int arrays, int n_sm, ResidualRun* run, cudaStream_t st);
+int residual_bwd_f16(const ResidualParams& p, bool level, int arrays, int n_sm, ResidualRun* run, cudaStream_t st);
+int residual_bwd_f32(const ResidualParams& p, bool level, int arrays, int n_sm, ResidualRun* run, cudaStream_t st);
 
 }  // namespace oapl

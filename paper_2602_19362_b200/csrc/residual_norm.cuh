@@ -15,8 +15,9 @@
 // no barrier is needed for them.  The gradient's second mean needs t, which needs the first; with A = b g u it is
 //     sum A t = sum A (dx' + r_x w_pre dh) - r_x mean(w_pre dh xh) sum A xh,
 // so one exchange between the row's threads gives all three sums.
-// Sums over rows (dw_pre, dw_post, dg per channel) are kept in registers over a CTA's rows, written as one partial row per
-// CTA, and joined in a fixed order by a second launch.  All sums are fp32.
+// Sums over rows (dw_pre, dw_post, dg per channel) are kept in registers over a worker's rows, written as its partial row, and
+// joined in a fixed order by a second launch.  All sums are fp32.  A launch gives a worker at most kRsFold rows, so that no
+// running sum has more terms than that; more rows take further launches, whose joins add to what is there.
 //
 // Measured, us, 16384 x 3584 bf16: forward 88 (0.83 of the copy rate), gradient 131 with its join (0.84); 11000 x 5120: 84 and
 // 148; 100000 x 256: 42 and 74; fp32, 8000 x 3584, gradient 134.  Rows of 3583 elements that start on 16-byte boundaries: 113
@@ -30,6 +31,10 @@ namespace oapl {
 
 constexpr int kRsMaxThreads = 512;
 constexpr int kRsMaxD = 16384;
+// Rows of a worker in a launch, where sums over rows are asked for.  One running sum over 4096 rows of like sign was off by 418
+// half steps of fp32, 256 rows at a time by 15.  A further launch costs 14 to 17 us: 131072 x 5120, whose workers are 148,
+// 1642 us in four launches, 1690 in seven of 128 rows, 1590 in one; up to 37888 rows of it take one, 75776 of 3584.
+constexpr int kRsFold = 256;
 enum { kGateNone = 0, kGateRow = 1, kGateColumn = 2, kGateFull = 3 };
 
 struct ResidualParams {

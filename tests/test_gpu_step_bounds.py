@@ -74,3 +74,69 @@ def test_a_norm_that_leaves_fp32_is_reported():
         st = torch.zeros(1, dtype=torch.int32, device="cuda")
         B.oapl_grad_norm(B.make_tensor_list([v]), *args, scratch(B.oapl_grad_norm_workspace_bytes(1)), 1.0, st)
         assert int(st) == status, (float(v[0]), args)
+
+
+# ------------------------------------------------------------------------------------------------ residual norm
+
+def residual_scratch(N, d):
+    return scratch(B.oapl_residual_norm_workspace_bytes(N, d))
+
+
+@pytest.mark.parametrize("which", ["pre", "post"])
+def test_sums_over_many_rows_stay_near_their_value(which):
+    # every row adds c to a column.  A running sum of c beyond 1024 loses nearly 2^-14 of each c, so that one sum over a
+    # worker's thousands of rows would be off by hundreds of half steps
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    N, d, c = 3 * 4096 * sms, 520, 1 + 2.0 ** -14 - 2.0 ** -20
+    ones, w = torch.ones(N, d, dtype=torch.bfloat16, device="cuda"), torch.ones(d, device="cuda")
+    r = torch.full((N,), c, device="cuda")
+    got = [torch.zeros(d, device="cuda") for _ in range(2)]
+    if which == "pre":
+        B.oapl_residual_norm_bwd(B.make_residual(ones, w_pre=w), ones, None, r, ones, None, dw_pre=got[0], ws=residual_scratch(N, d))
+        got = got[:1]
+    else:
+        B.oapl_residual_norm_bwd(B.make_residual(ones, ones, w, w_post=w), None, r, None, None, ones, dgate=got[0], dw_post=got[1],
+                                 ws=residual_scratch(N, d))
+    # 256 rows in a register, the launches' sums of 256 (one worker per SM at least), 1024 workers in 32 shares and their
+    # tree; the terms' and the factors' own roundings
+    steps = 256 + N // sms // 256 + 1024 // 32 + 5 + 4
+    for g in got:
+        off = (g.double() - N * c).abs().max()
+        assert float(off) <= steps * U * N * c, float(off) / (U * N * c)
+
+
+@pytest.mark.parametrize("t,N,d,pad", [("bf16", 1200007, 24, 0), ("f32", 900001, 77, 1), ("f16", 700001, 400, 0), ("bf16", 500001, 401, 2),
+                                       ("bf16", 200003, 1112, 0), ("f16", 150001, 1111, 0), ("f32", 60001, 4100, 0),
+                                       ("bf16", 60001, 4101, 3), ("bf16", 40003, 9008, 0), ("f32", 20001, 9001, 0)])
+@pytest.mark.parametrize("gate", ["none", "row", "column", "full"])
+def test_sums_over_many_rows_of_whole_numbers_are_exact(t, N, d, pad, gate):
+    g = torch.Generator(device="cuda").manual_seed(d)
+    whole = lambda *s, ld=0: torch.randint(-3, 4, (s[0], s[1] + ld) if ld else s, device="cuda", generator=g,  # noqa: E731
+                                           dtype=torch.int8).to(TYPES[t])[..., :s[-1]]
+    a, b = whole(N, d, ld=pad), whole(N, d, ld=pad)
+    w, v = whole(d), whole(d)
+    one = torch.ones(N, device="cuda")
+
+    def total(*parts):
+        s = torch.zeros(d, dtype=torch.float64, device="cuda")
+        for at in range(0, N, 20000):
+            x = parts[0][at:at + 20000].double()
+            for p in parts[1:]:
+                x = x * p[at:at + 20000].double()
+            s += x.sum(0)
+        return s
+
+    if gate == "none":
+        dw = torch.full((d,), 5.0, device="cuda")
+        B.oapl_residual_norm_bwd(B.make_residual(a, w_pre=w), a, None, one, b, None, dw_pre=dw, accumulate=True, ws=residual_scratch(N, d))
+        assert torch.equal(dw.double(), total(a, b) + 5)
+        dw2 = torch.full((d,), 3.0, device="cuda")
+        B.oapl_residual_norm_bwd(B.make_residual(a, a, w_pre=w), a, None, one, b, b, dx=torch.empty_like(a), dy=torch.empty_like(a), dw_pre=dw2,
+                                 ws=residual_scratch(N, d))
+        assert torch.equal(dw2, dw - 5)
+    k = {"none": None, "row": whole(N, 1).float(), "column": v, "full": whole(N, d, ld=pad)}[gate]
+    dw, dg = torch.empty(d, device="cuda"), torch.empty(d, device="cuda") if gate == "column" else None
+    B.oapl_residual_norm_bwd(B.make_residual(a, a, k, w_post=w), None, one, None, None, b, dgate=dg, dw_post=dw, ws=residual_scratch(N, d))
+    s = total(a, b, *([k] if gate in ("row", "full") else []))
+    assert torch.equal(dw.double(), s * v.double() if gate == "column" else s)
+    assert dg is None or torch.equal(dg.double(), s * w.double())
