@@ -1,10 +1,12 @@
 """The embedding's gradient, the residual norm, clipping and the adjustments of logits at the ends of their ranges."""
+import itertools
 import math
 
 import pytest
 import torch
 
 from paper_2602_19362_b200 import binding as B
+from tests import test_gpu_residual as res
 
 pytestmark = pytest.mark.gpu
 
@@ -140,3 +142,53 @@ def test_sums_over_many_rows_of_whole_numbers_are_exact(t, N, d, pad, gate):
     s = total(a, b, *([k] if gate in ("row", "full") else []))
     assert torch.equal(dw.double(), s * v.double() if gate == "column" else s)
     assert dg is None or torch.equal(dg.double(), s * w.double())
+
+
+@pytest.mark.parametrize("t,d", [("f32", 1537), ("f32", 7600), ("f32", 9001), ("f32", 12288), ("bf16", 9001), ("bf16", 12288)])
+@pytest.mark.parametrize("gate", ["column", "full"])
+def test_wide_results_over_inputs(t, d, gate):
+    # fp32 rows above 8192 are read where they are, twice, while their results are written
+    N = 200
+    c = res.make(N, d, t, gate)
+    xo, h, rp, rq = [x.clone() for x in res.check_fwd(c)]
+    places = ["x", "y"] + (["gate"] if gate == "full" else [])
+    for p, q in itertools.permutations(places, 2):
+        e = dict(c, **{k: c[k].clone() for k in places})
+        rp2, rq2 = torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+        B.oapl_residual_norm(res.struct(e), e[p], e[q], rp2, rq2)
+        assert torch.equal(e[p], xo) and torch.equal(e[q], h) and torch.equal(rp2, rp) and torch.equal(rq2, rq), (p, q)
+    dx, dy = torch.empty_like(xo), torch.empty_like(xo)
+    dg = torch.empty_like(xo) if gate == "full" else None
+    B.oapl_residual_norm_bwd(res.struct(c), xo, rp, rq, c["dh"], c["dxo"], dx, dy, dg)
+    places = ["xo", "dh", "dxo", "y"] + (["gate"] if gate == "full" else [])
+    for p, q in itertools.permutations(places, 2):
+        e = dict(c, xo=xo)
+        e = {**e, **{k: e[k].clone() for k in places}}
+        dg2 = torch.empty_like(xo) if gate == "full" else None
+        B.oapl_residual_norm_bwd(res.struct(e), e["xo"], rp, rq, e["dh"], e["dxo"], e[p], e[q], dg2)
+        assert torch.equal(e[p], dx) and torch.equal(e[q], dy), (p, q)
+        assert dg is None or torch.equal(dg, dg2)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("d", [72, 256, 1536, 1537, 3584, 5120, 9001])
+@pytest.mark.parametrize("alone", [False, True])
+def test_gradient_of_the_norm_that_makes_the_heads_rows(t, d, alone):
+    # nothing but the head reads x', so dx_out is left out; alone: without a block's result
+    N = 300
+    c = res.make(N, d, t)
+    c["dxo"].zero_()
+    if alone:
+        c.update(y=None, w_post=None)
+    r = res.ref_fwd(c)
+    xo = torch.empty_like(c["x"]).copy_(r["xo"])
+    rp, rq = (r[k].float() if k in r else None for k in ("rp", "rq"))
+    new = lambda: torch.empty_like(c["x"])  # noqa: E731
+    dx, dy, dwp, dwq = new(), None if alone else new(), None if alone else torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    B.oapl_residual_norm_bwd(res.struct(c), xo, rp, rq, c["dh"], None, dx, dy, None, dwp, dwq, False, residual_scratch(N, d))
+    w = res.ref_bwd(c, xo, rp, rq)
+    res.within(dx, w["dx"], w["t_dx"], "dx")
+    res.within(dwq, w["dw_pre"], w["t_dw_pre"], "dw_pre")
+    if not alone:
+        res.within(dy, w["dy"], w["t_dy"], "dy")
+        res.within(dwp, w["dw_post"], w["t_dw_post"], "dw_post")
