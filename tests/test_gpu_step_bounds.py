@@ -192,3 +192,60 @@ def test_gradient_of_the_norm_that_makes_the_heads_rows(t, d, alone):
     if not alone:
         res.within(dy, w["dy"], w["t_dy"], "dy")
         res.within(dwp, w["dw_post"], w["t_dw_post"], "dw_post")
+
+
+# ------------------------------------------------------------------------------------------------ embedding's gradient
+
+def whole_rows(g, N, d, t="f32"):
+    return torch.randint(-8, 9, (N, d), device="cuda", generator=g, dtype=torch.int8).to(TYPES[t])
+
+
+def check_whole(ids, V, dout, accumulate):
+    """Sums of whole numbers are exact in any order, as long as all of them stay below 2^24."""
+    N, d = dout.shape
+    table = torch.full((V, d), 3.0, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.oapl_embedding_bwd(B.make_lookup(ids, V), dout, table, accumulate, scratch(B.oapl_embedding_workspace_bytes(N, V, d)), st)
+    want = torch.full((V, d), 3.0 if accumulate else 0.0, device="cuda").index_add_(0, ids.long(), dout.float())
+    assert torch.equal(table, want) and int(st) == 0
+
+
+# sizes of one launch, of a sort by counting, by digits with the tiles' counts added up by each, and with a launch that
+# adds them up; chunks of 32, 32, 32, 64, 128 and 256 positions
+@pytest.mark.parametrize("N,chunk", [(1025, 32), (8192, 32), (8193, 32), (40960, 64), (70000, 128), (131073, 256), (300007, 256)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_long_runs_is_exact(N, chunk, accumulate):
+    g = torch.Generator(device="cuda").manual_seed(N)
+    # one token everywhere, with positive terms: a chunk that is left out shows
+    dout = whole_rows(g, N, 24, "bf16").abs()
+    check_whole(torch.full((N,), 2, dtype=torch.int32, device="cuda"), 4, dout, accumulate)
+    # runs in every alignment to the chunks, in the sorted list; what is left is one run over the rest
+    c = chunk
+    lens = [c, c, c - 1, 1, c + 1, c - 1, 2 * c, 1, 1, 2 * c - 2, 4 * c, 5, c - 5, c, 1]
+    lens += [N - sum(lens)] if N > sum(lens) else []
+    ids = torch.repeat_interleave(torch.arange(len(lens)), torch.tensor(lens))[:N].to(torch.int32).cuda()
+    ids = ids[torch.randperm(N, generator=torch.Generator().manual_seed(3)).cuda()]
+    check_whole(ids, len(lens) + 2, dout, accumulate)
+    check_whole(ids, len(lens) + 2, whole_rows(g, N, 25, "f16"), accumulate)
+
+
+@pytest.mark.parametrize("N", [9001, 131072, 131073, 300007])
+@pytest.mark.parametrize("V", [1000, 151936, (1 << 20) + 5, 1 << 21])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_large_batches_and_vocabularies_is_exact(N, V, accumulate):
+    # one to three passes of digits
+    g = torch.Generator(device="cuda").manual_seed(V % 1000 + N)
+    u = torch.rand(N, device="cuda", generator=g, dtype=torch.float64)
+    ids = ((V ** u).long() - 1).clamp(0, V - 1).to(torch.int32)
+    ids[::3] = torch.randint(0, V, (ids[::3].numel(),), device="cuda", generator=g).to(torch.int32)
+    ids[5], ids[77] = V - 1, 0
+    check_whole(ids, V, whole_rows(g, N, 8, "bf16"), accumulate)
+
+
+@pytest.mark.parametrize("N", [9001, 140001])
+def test_gradient_of_the_largest_vocabulary_is_exact(N):
+    V = 2 * 10 ** 9             # four passes of digits, 8 GB
+    g = torch.Generator(device="cuda").manual_seed(N)
+    ids = torch.randint(0, V, (N,), device="cuda", generator=g).to(torch.int32)
+    ids[::5], ids[1], ids[2] = 1999999999, 0, 1999999998
+    check_whole(ids, V, whole_rows(g, N, 1), False)
