@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2602_19362_b200 import binding as B
+from tests import test_gpu_adjust as adj
 from tests import test_gpu_residual as res
 
 pytestmark = pytest.mark.gpu
@@ -249,3 +250,15 @@ def test_gradient_of_the_largest_vocabulary_is_exact(N):
     ids = torch.randint(0, V, (N,), device="cuda", generator=g).to(torch.int32)
     ids[::5], ids[1], ids[2] = 1999999999, 0, 1999999998
     check_whole(ids, V, whole_rows(g, N, 1), False)
+
+
+# ------------------------------------------------------------------------------------------------ adjustments
+
+# slices of 2048, 4096 and 8192 tokens (16384 for the gradient apart) by vectors, of 2048 and 4096 an element at a time;
+# more than 512 tokens of a slice change
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("N,V,pad,offset", [(7, 5000, 16, 0), (600, 5001, 16, 0), (700, 8203, 16, 0), (7, 5001, 1, 1), (600, 5000, 1, 1)])
+def test_gradient_of_long_histories_over_its_inputs(t, N, V, pad, offset):
+    for where in ("z", "d", "apart"):
+        c = adj.make(N, V, t, 21, prompt=3000, answer=2500, pad=pad, offset=offset)
+        adj.check_bwd(c, torch.tensor([i % 5 != 3 for i in range(N)], dtype=torch.uint8, device="cuda"), where)
