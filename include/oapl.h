@@ -37,7 +37,7 @@ typedef enum {
   OAPL_ERR_UNSUPPORTED_SHAPE = -4,   /* d not a multiple of 64, or sizes beyond int32 index range */
   OAPL_ERR_BAD_TARGET = -5,          /* device: mask==1 and target outside [0,V) */
   OAPL_ERR_BAD_SEQ_ORDER = -6,       /* device: seq_id decreasing or outside [0,S) */
-  OAPL_ERR_NONFINITE_INPUT = -7,     /* device: non-finite reward, or group_id outside [0,P) */
+  OAPL_ERR_NONFINITE_INPUT = -7,     /* device: non-finite reward, logit or gradient norm, or group_id outside [0,P) */
   OAPL_ERR_DEVICE_TIMEOUT = -8,      /* device: a bounded pipeline wait expired */
   OAPL_ERR_CUDA = -9,                /* a CUDA runtime/driver call failed */
   OAPL_ERR_BAD_STATE = -10,          /* oapl_loss_bwd without a matching oapl_loss_fwd in ws */
@@ -408,7 +408,7 @@ int oapl_scaled_matmul(const oapl_scaled* A /*host*/, const oapl_scaled* B /*hos
 /* N token ids of a vocabulary of V. */
 typedef struct {
   const int32_t* ids;  /* [N]; in [0,V) where mask==1                                        */
-  const uint8_t* mask; /* [N] or NULL (all rows count); ids of rows with mask==0 are not read */
+  const uint8_t* mask; /* [N] or NULL (all rows count); ids of rows with mask==0 may hold anything */
   int64_t N;
   int32_t V;
   float scale;         /* finite; a scaled embedding's factor, otherwise 1                   */
@@ -445,6 +445,8 @@ int oapl_embedding_bwd(const oapl_lookup* lookup /*host*/, const void* dout, int
  *   h = w_pre * x' / rms(x'),                         rms(v) = sqrt(mean v^2 + eps).
  * Without y: x' = residual_scale * x, the norm alone.  A weight counts as weight + weight_offset (1 where a model stores
  * the difference from 1).
+ * Squares are added in fp32: a row whose sum of squares leaves its range (elements of 1.8e19 / sqrt(d) and more) has
+ * 1 / rms = 0, and a row of zeros needs eps > 0.
  */
 typedef struct {
   int64_t N;
@@ -503,7 +505,8 @@ typedef struct {
 
 /*
  * sq_norm [1] f32 = sum of (scale * g)^2 over all elements of the list, norm [1] f32 its square root; one of them may be
- * NULL.  Sums are fp64, so norm is right where sq_norm leaves the range of fp32: a norm above 1.8e19 makes sq_norm infinite.
+ * NULL.  A thread adds 16 or 32 squares in fp32 where that is exact to fp32 rounding, else in fp64, as all sums from there, so
+ * norm is right where sq_norm leaves the range of fp32: a norm above 1.8e19 makes sq_norm infinite.
  * OAPL_ERR_NONFINITE_INPUT: a norm that is not finite in fp32, or an infinite sq_norm where norm is NULL.  The list is read
  * during the call only.  ws: oapl_grad_norm_workspace_bytes(count) bytes, 16-byte aligned.  sq_norm is what
  * oapl_adamw_step takes as other_sq_norm; an infinite one makes the clipped gradient of that step 0.
@@ -533,6 +536,8 @@ int oapl_grad_clip_ex(const oapl_tensor* tensors /*host*/, int32_t count, float 
  * of row n, c: how often it is in the row's answer, seen: whether it is in the row's prompt or answer,
  *   z1 = seen ? (z > 0 ? z / repetition : z * repetition) : z,
  *   z2 = z1 - frequency * c - presence * [c > 0],   z3 = z2 + the sum of its biases,   result = allowed ? z3 : -inf.
+ * Samplers differ in their order.  One that adds biases before the repetition penalty gives a token with both another logit;
+ * its rows are had from two calls, the biases first (16-bit logits are rounded in between), gradients from the second's.
  */
 typedef struct {
   const int32_t* tokens;    /* [T] or NULL: token ids of all rows' prompts and answers; ids outside [0,V) count for nothing */

@@ -948,7 +948,7 @@ const char* oapl_status_string(int status) {
     case OAPL_ERR_UNSUPPORTED_SHAPE: return "unsupported shape (d must be a multiple of 64)";
     case OAPL_ERR_BAD_TARGET: return "target outside [0,V) on a live row";
     case OAPL_ERR_BAD_SEQ_ORDER: return "seq_id decreasing or outside [0,S)";
-    case OAPL_ERR_NONFINITE_INPUT: return "non-finite reward or group_id outside [0,P)";
+    case OAPL_ERR_NONFINITE_INPUT: return "non-finite reward, logit or gradient norm, or group_id outside [0,P)";
     case OAPL_ERR_DEVICE_TIMEOUT: return "device pipeline wait timed out";
     case OAPL_ERR_CUDA: return "CUDA call failed";
     case OAPL_ERR_BAD_STATE: return "backward called without a matching forward";
