@@ -716,7 +716,8 @@ def oapl_residual_norm_bwd(r: OaplResidual, x_out, rstd_post, rstd_pre, dh, dx_o
 
 class TensorList:
     """A host array of oapl_tensor for the tensors of a model, which it keeps alive.  Made once for gradients that keep
-    their memory."""
+    their memory (zero_grad(set_to_none=False)); checking and filling it takes 1.15 us a tensor, 690 for 600 of them, which
+    a list made anew at every step adds to the two calls' 22."""
 
     def __init__(self, tensors, outs=None):
         if not tensors:

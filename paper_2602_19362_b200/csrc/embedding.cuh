@@ -20,8 +20,9 @@
 // Measured, us: 64 rows of 3584 bf16 2.7 on the device; 32768 x 3584 58 (the copy rate), 32768 x 3583 96 (two loads and a shift
 // per vector); gradient of 40960 x 1536 bf16 into 151936 rows 185 (0.89 of the copy rate), of which the sums and the zeros
 // take 158, the sort 17; 65536 x 1536 into 20000 rows 85; 3001 x 1001 fp16 off 16-byte boundaries into 50021 rows 53; 23 x 313
-// into 1486 rows, in one launch, 8.2 (13.3 with the sort and the sums apart).  Clearing rows beside the sort, whose CTAs leave
-// most SMs idle, was tried: it slowed the sort by what it saved.
+// into 1486 rows, in one launch, 8.2 (13.3 with the sort and the sums apart).  Added to what is there: 40960 x 1536 into 151936
+// rows 100, 65536 x 1536 into 20000 rows 129, 524288 x 1536 into 152064 rows 509 (480 with every row written).
+// Clearing rows beside the sort, whose CTAs leave most SMs idle, was tried: it slowed the sort by what it saved.
 #pragma once
 #include <type_traits>
 

@@ -11,8 +11,9 @@
 // (values above about 1e14, or nothing but values below about 1e-12) adds the same elements again in fp64.
 //
 // Measured, us: 453 M bf16 elements in 108 tensors, norm 151 (0.94 of the copy rate), clipping to fp32 465 (0.91), to bf16
-// 280 (the copy rate); 600 tensors of up to 4100 fp32 elements 18 for both calls, 10 of them on the device.  Loads of the next chunk
-// ahead of this one's sums: 187 to 151.
+// 280 (the copy rate); 600 tensors of up to 4100 fp32 elements 18 for both calls after a flush of L2, 14 of them in kernels.
+// Loads of the next chunk ahead of this one's sums: 187 to 151.  Tensors off 16-byte boundaries go an element at a time: 100 M
+// bf16 elements two bytes off, norm 356 instead of 49, clipping to fp32 217 instead of 115.
 #pragma once
 #include <type_traits>
 

@@ -21,9 +21,11 @@
 //
 // Measured, us: the gradient 2048 x 152064 bf16, 300 tokens of prompt and up to 1024 of answer, 232 (0.83 of the copy
 // rate); the adjustment with all penalties and eight biases 299 (0.65), with a mask 349, rows off 16-byte boundaries 318;
-// one row of 152064 fp32 with 8000 tokens and 40 biases 6.0 on the device; a mask over 64 x 128256 bf16 8.0.  What is left
-// is latency: spans, tokens and listed logits are loads that wait for one another, with barriers between them, and six CTAs
-// (forward) to cover them; issue slots are a quarter busy.
+// a mask alone, apart, 199, with sides off by different amounts 449; answers of up to 16384 tokens, each row its own, 661 and
+// the gradient 510; one row of 152064 fp32 with 8000 tokens and 40 biases 6.0 on the device; a mask over 64 x 128256 bf16 8.0.
+// What is left is latency: spans, tokens and listed logits are loads that wait for one another, with barriers between them, and
+// six CTAs (forward) to cover them; issue slots are a quarter busy.  With long answers it is the tokens, which every slice of a
+// row reads and tests: a list of them by slice, made once for a row, would be read once.
 #pragma once
 #include "elements.cuh"
 

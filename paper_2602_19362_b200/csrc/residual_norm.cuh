@@ -21,9 +21,11 @@
 //
 // Measured, us, 16384 x 3584 bf16: forward 88 (0.83 of the copy rate), gradient 131 with its join (0.84); 11000 x 5120: 84 and
 // 148; 100000 x 256: 42 and 74; fp32, 8000 x 3584, gradient 134.  Rows of 3583 elements that start on 16-byte boundaries: 113
-// and 252; off them: 159 and 317, where shifting takes three times the instructions of the arithmetic.  The gradient's arithmetic is written two wide and takes
-// half of the issue slots; one wide, with weights widened for each row and parts left out at run time, it took 83
-// instructions an element and 270 us.  What is left forward is the chain of two sums over a row, which the other CTAs of an SM cover.
+// and 252; off them: 159 and 317, where every array is shifted by itself, three times the instructions of the arithmetic.
+// The gradient's arithmetic is written two wide and takes half of the issue slots; one wide, with weights widened for each row
+// and parts left out at run time, it took 83 instructions an element and 270 us.  Calls without dx_out or without y have no form
+// of their own (see ResidualHas): 191 without dx_out, of five matrices; the norm alone 61 forward and 134 back without dx_out.
+// What is left forward is the chain of two sums over a row, which the other CTAs of an SM cover.
 #pragma once
 #include "elements.cuh"
 
@@ -483,8 +485,9 @@ constexpr int residual_ctas(bool forward, int elems, int nt) {
   return nt > 256 ? 1 : forward ? (elems == 8 ? 4 : 3) : (elems == 8 ? 3 : 2);
 }
 
-// What a call has.  Blocks as they are come in four forms, all with y, w_pre, dx' and every result: with or without w_post,
-// with a gate per element or without.  Kernels that know theirs when they are compiled have no branches for the rest, and
+// What a call has.  The blocks of a model come in four forms, all with y, w_pre, dx' and every result: with or without w_post,
+// with a gate per element or without.  (The norm that makes the head's rows has no dx' from elsewhere, the first one no y: these
+// take the kernel for any form.)  Kernels that know theirs when they are compiled have no branches for the rest, and
 // registers for all they need (16384 x 3584 bf16, gradient: 118 us without w_post and 171 with a gate per element, 196 and
 // 245 for any form).
 enum { kFormAny = 0, kFormPost = 1, kFormPlain = 2, kFormPostFull = 3, kFormFull = 4 };

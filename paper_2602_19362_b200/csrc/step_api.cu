@@ -297,8 +297,8 @@ static int launch_adjust(AdjustParams p, cudaStream_t st) {
 
 template <typename T, int KE, bool GRAD, bool OVER>
 static int route_adjust_size(const AdjustParams& p, int n_sm, cudaStream_t st) {
-  // Slices of 16384 tokens (8192 for the gradient over the logits, which needs the room, and 4096 an element at a time)
-  // where they give every SM four CTAs, else half of that where they do, else 2048.
+  // Slices of 8192 tokens (16384 for the gradient apart from the logits, which counts nothing and keeps nothing, and 4096 an
+  // element at a time) where they give every SM four CTAs, else half of that where they do, else 2048.
   constexpr int kMany = (KE == 1 ? 16 : GRAD && !OVER ? 64 : 32) / KE, kSome = kMany / 2, kFew = 8 / KE;
   const int64_t many = (int64_t)p.N * p.V / (kMany * KE * kAdThreads);
   if (many >= 4 * (int64_t)n_sm) return launch_adjust<T, KE, kMany, GRAD, OVER>(p, st);
