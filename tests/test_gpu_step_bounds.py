@@ -262,3 +262,28 @@ def test_gradient_of_long_histories_over_its_inputs(t, N, V, pad, offset):
     for where in ("z", "d", "apart"):
         c = adj.make(N, V, t, 21, prompt=3000, answer=2500, pad=pad, offset=offset)
         adj.check_bwd(c, torch.tensor([i % 5 != 3 for i in range(N)], dtype=torch.uint8, device="cuda"), where)
+
+
+def test_biases_before_the_penalties_take_two_calls():
+    # the order of some samplers; a token with a bias that changes its sign takes the other branch of the penalty
+    N, V = 40, 3001
+    c = adj.make(N, V, "f32", 31, allowed=0.8)
+    first = {k: c[k] for k in ("bias_start", "bias_id", "bias")}
+    rest = {k: v for k, v in c.items() if k not in first}
+    count, seen, bias, size, open_ = adj.parts(c)
+    mid, out = torch.empty_like(c["z"]), torch.empty_like(c["z"])
+    L = B.make_logits(c["z"])
+    B.oapl_logits_adjust(L, B.make_adjust(L, **first), mid)
+    M = B.make_logits(mid)
+    B.oapl_logits_adjust(M, adj.args(M, rest), out)
+    r, f, p = (adj.row(c, k, 0.0) for k in ("repetition", "frequency", "presence"))
+    z1 = c["z"].double() + bias
+    z1 = torch.where(size > 0, mid.double(), z1)        # its rounding decides on the branch where the sum is near zero
+    assert bool(((z1 - c["z"].double() - bias).abs() <= 8 * U * (c["z"].double().abs() + size)).all())
+    slope = torch.where(seen, torch.where(z1 > 0, 1 / r, r * torch.ones_like(z1)), 1.0)
+    want = z1 * slope - f * count - p * (count > 0)
+    tol = 4 * U * ((z1 * slope).abs() + (f * count).abs() + (p * (count > 0)).abs()) + half_step(want, torch.float32)
+    assert bool(((out.double() - want).abs() <= tol)[open_].all()) and bool((out[~open_] == -math.inf).all())
+    d, dz = torch.randn_like(mid), torch.empty_like(mid)
+    B.oapl_logits_adjust_bwd(M, adj.args(M, rest), d, dz)
+    assert bool(((dz.double() - torch.where(open_, d.double() * slope, 0.0)).abs() <= 4 * U * d.double().abs() * slope).all())
